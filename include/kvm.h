@@ -372,6 +372,97 @@ kvm_status_t kvm_merge_gate(const void* x, const float* w_gate, int32_t batch, i
 kvm_status_t kvm_head_layernorm(void* x, const float* weight, const float* bias, int32_t batch, int32_t n_heads,
                                 int64_t n_tokens, int32_t head_dim, float eps, void* cuda_stream);
 
+/* ---- Exact attention beside the compressed one: a cache of keys and values in 8 bits ------------------------------
+ * The uncompressed layers of a hybrid stack (sliding-window or full attention between KVM layers) keep their keys and
+ * values in pages of `page_tokens` tokens ("blocks").  A page holds, for every kv head, the codes of its rows in e4m3
+ * (an 8-bit floating-point type: 4 exponent bits, 3 mantissa bits, largest value 448) and one scale for the keys and
+ * one for the values; a row stands for code * scale.  Scales are powers of two 2^e, -64 <= e <= 120, so what a code
+ * stands for is exact.  All device memory is the caller's; the library keeps nothing of it and allocates nothing. */
+typedef struct {
+  void *k, *v;                 /* device e4m3 [n_pages, n_kv_heads, page_tokens, head_dim], 16-byte aligned */
+  float *k_scale, *v_scale;    /* device fp32 [n_pages, n_kv_heads] */
+  int64_t n_pages;
+  int32_t n_kv_heads, head_dim, page_tokens;   /* head_dim 64 or 128; page_tokens 16, 32, 64 or 128 */
+} kvm_cache_t;
+
+/* The sequences of one call.  Sequence b has start[b] tokens in the cache before the call and count[b] tokens in it, at
+ * positions start[b] .. start[b] + count[b] - 1; block i of sequence b is page pages[b * max_pages + i].  The arrays are
+ * device memory, so that a captured graph may be replayed with new lengths and pages; the kernels check them: a sequence
+ * with start < 0, count < 0, count > n_tokens or start + count > max_pages * page_tokens, or with a page outside
+ * [0, n_pages) that the call needs, is reported as KVM_ERR_INVALID_ARG in *status (where status is given: a device word that
+ * the library never clears) and none of what it names is read or written out of bounds.  Entries of blocks that the call
+ * neither writes nor sees may be anything. */
+typedef struct {
+  const int32_t* pages;        /* device [batch, max_pages] */
+  const int32_t* start;        /* device [batch] */
+  const int32_t* count;        /* device [batch], or NULL: n_tokens for every sequence */
+  int32_t batch, max_pages;    /* batch <= 1024 */
+  int64_t n_tokens;            /* padded number of tokens per sequence of this call */
+} kvm_cache_call_t;
+
+/* Appends the keys and values of a call: k, v device bf16 [batch, n_kv_heads, n_tokens, head_dim], element strides of the first three
+ * dims in k_strides / v_strides (NULL = contiguous), channel stride 1; rows behind a sequence's count are not read.  A block's scale
+ * is the least 2^e, e >= -64, with max |x| <= 448 * 2^e over the rows written so far, codes are x / 2^e rounded to nearest even; where new
+ * rows raise the scale of a block in progress, the codes it holds are divided by the factor and rounded again.  The row at offset 0
+ * starts a page anew, whatever it held.  A row with an infinity or a NaN makes the scale of its block NaN (attention over the block
+ * gives NaN until the page is started anew).  Pages written by one call must be distinct: a page that two sequences share is
+ * copied first (kvm_pages_extend says which).  A sequence that is reported in *status may have been written in part.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
+kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* k, const void* v,
+                              const int64_t* k_strides, const int64_t* v_strides, int32_t* status, void* cuda_stream);
+
+/* Attention of the call's tokens over the cache, which holds their own keys and values already:
+ *     out_i = sum_j p_ij v_j,  p_i = softmax over the visible j of scale * q_i . k_j,
+ * position i sees the positions j <= i with j > i - window, or j < sinks (sliding window and a few first tokens that stay
+ * visible); window = 0: every j <= i.
+ *   q, out   device bf16 [batch, n_q_heads, n_tokens, head_dim]; strides as in kvm_cache_append; n_q_heads a multiple of n_kv_heads;
+ *            rows of out behind a sequence's count are left as they were; out must not overlap q
+ *   workspace device memory, 16-byte aligned, at least kvm_cache_workspace() bytes, whatever it holds; calls that may overlap
+ *            on the GPU need one each
+ * Products of bf16 and e4m3 and the softmax statistics are held in fp32.  A sequence that is reported in *status gets NaN rows (those up to
+ * its count, when that is valid), as does a query whose q, or whose visible blocks, hold an infinity or a NaN.
+ * Results are deterministic.  Waits on the device are bounded: should one run out, *status is KVM_ERR_TIMEOUT.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (workspace too small), CUDA; nothing is launched on an error. */
+kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale,
+                              int32_t window, int32_t sinks, void* out, const int64_t* q_strides, const int64_t* out_strides,
+                              void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+
+/* Bytes of workspace that kvm_cache_attend needs for these sizes (pointers are not looked at); -1 on invalid arguments. */
+int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_q_heads);
+
+/* Copies whole pages (codes and scales of every head): page src[i] to page dst[i], i < n.  src, dst: HOST arrays, not kept.  Every dst
+ * is named once and is no src, else INVALID_ARG.  The lists travel in the launches' arguments: no copy, no
+ * synchronisation. */
+kvm_status_t kvm_cache_copy_pages(const kvm_cache_t* cache, const int32_t* src, const int32_t* dst, int64_t n, void* cuda_stream);
+
+/* Which page holds what: host bookkeeping for one pool of pages (no device access; not thread safe).  Pages are counted by the
+ * sequences that use them, so a fork shares its parent's pages, and a page in progress is copied only when one of them writes to it. */
+typedef struct kvm_pages kvm_pages_t;   /* opaque, library-owned */
+kvm_status_t kvm_pages_create(int64_t n_pages, int32_t page_tokens, kvm_pages_t** out);
+kvm_status_t kvm_pages_destroy(kvm_pages_t* p);   /* NULL is accepted */
+/* A new, empty sequence; its number is the least one not in use. */
+kvm_status_t kvm_pages_open(kvm_pages_t* p, int32_t* seq);
+/* A new sequence with the tokens of `seq`, on the same pages. */
+kvm_status_t kvm_pages_fork(kvm_pages_t* p, int32_t seq, int32_t* child);
+/* Gives the pages of a sequence back that no other one uses. */
+kvm_status_t kvm_pages_close(kvm_pages_t* p, int32_t seq);
+/* Makes room for n_tokens more tokens of a sequence.  If its last page is in progress and shared, the sequence gets one of its own:
+ * *src, *dst are then the page to copy (kvm_cache_copy_pages, before the append) and the new one, else -1.
+ * CAPACITY (nothing changed) when the pool has too few free pages. */
+kvm_status_t kvm_pages_extend(kvm_pages_t* p, int32_t seq, int64_t n_tokens, int32_t* src, int32_t* dst);
+/* Gives back the blocks of a sequence that no later token of a layer with this window and these sinks sees; their table entries are
+ * -1.  window >= 1. */
+kvm_status_t kvm_pages_trim(kvm_pages_t* p, int32_t seq, int32_t window, int32_t sinks);
+/* Moves the used pages to the front of the pool: src[i] -> dst[i], i < *n, are the copies to make (kvm_cache_copy_pages) before the next
+ * call that reads or writes the cache; every table is changed at once.  capacity: entries of src and dst; *n never exceeds the number of
+ * used pages.  CAPACITY (nothing changed) when the lists are too short. */
+kvm_status_t kvm_pages_compact(kvm_pages_t* p, int32_t* src, int32_t* dst, int64_t capacity, int64_t* n);
+/* The table of a sequence: *n_blocks blocks for *n_tokens tokens, copied to pages[0 .. capacity) with -1 behind the last block (pages
+ * may be NULL with capacity 0).  CAPACITY when the blocks do not fit.  Any of n_blocks, n_tokens may be NULL. */
+kvm_status_t kvm_pages_table(const kvm_pages_t* p, int32_t seq, int32_t* pages, int64_t capacity, int64_t* n_blocks, int64_t* n_tokens);
+/* Pages that no sequence uses, and the largest page number in use plus one.  Either may be NULL. */
+kvm_status_t kvm_pages_info(const kvm_pages_t* p, int64_t* n_free, int64_t* high);
+
 const char* kvm_status_string(kvm_status_t s);
 
 #ifdef __cplusplus

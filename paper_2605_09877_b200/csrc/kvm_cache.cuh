@@ -1,0 +1,88 @@
+// Shared by the kernels over the 8-bit cache (kvm_cache.cu, kvm_cache_decode.cu, kvm_cache_prompt.cu): what a launch is given, which keys a
+// position sees, and the e4m3 conversions.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "kvm.h"
+
+namespace kvm {
+namespace cache {
+
+constexpr int kMaxBatch = 1024;   // sequences of one call
+constexpr int kTile = 128;        // keys of one tile of the attention kernels
+
+struct Params {
+  const uint8_t *k, *v;
+  const float *ks, *vs;
+  const int32_t *pages, *start, *count;
+  int32_t* status;
+  int64_t n_pages, T;
+  int Hkv, page, page_shift, batch, max_pages;
+};
+
+// Tokens before the call (start) and in it (n) of sequence b; false: lengths that the call does not allow.
+__device__ __forceinline__ bool seq_lengths(const Params& p, int b, int& start, int& n) {
+  start = p.start[b];
+  n = p.count ? p.count[b] : (int)p.T;
+  return start >= 0 && n >= 0 && n <= p.T && (int64_t)start + n <= (int64_t)p.max_pages * p.page;
+}
+__device__ __forceinline__ void report(int32_t* status, int code) {
+  if (status) atomicExch(status, code);
+}
+// Position i sees j <= i with j > i - window, or j < sinks.  (window: INT32_MAX stands for all)
+__device__ __forceinline__ bool sees(int i, int j, int window, int sinks) {
+  return j <= i && (j > i - window || j < sinks);
+}
+// The key tiles that positions [first, last] see: the tiles of the first `sinks` tokens, then the window's, without those counted twice.
+struct Tiles { int n_sink, first, n; };   // tile i is i < n_sink ? i : first + (i - n_sink); n in all
+__device__ __forceinline__ Tiles tiles_of(int first, int last, int window, int sinks) {
+  Tiles t;
+  const int end = last / kTile + 1;
+  const int low = first - window + 1;   // (first >= 0 and window >= 1: no overflow)
+  const int w0 = low > 0 ? low / kTile : 0;
+  t.n_sink = min(w0, (sinks + kTile - 1) / kTile);
+  t.first = w0;
+  t.n = t.n_sink + end - w0;
+  return t;
+}
+__device__ __forceinline__ int tile_at(const Tiles& t, int i) { return i < t.n_sink ? i : t.first + (i - t.n_sink); }
+
+// Exponent of a scale 2^e.  A NaN scale has exponent 128: scale_value(128) is NaN.
+__device__ __forceinline__ int scale_exp(float s) { return (int)((__float_as_uint(s) >> 23) & 255u) - 127; }
+__device__ __forceinline__ float exp2i(int e) {   // 2^e, -126 <= e <= 127; 128: NaN
+  return e > 127 ? __int_as_float(0x7fc00000) : __int_as_float((e + 127) << 23);
+}
+
+// two floats -> two e4m3 codes (a in the low byte), round to nearest even, saturating
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+// two e4m3 codes -> two fp16 (exact)
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t c) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)c));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t c) {
+  const uint32_t h = e4m3x2_to_f16x2(c);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+struct AttendArgs {
+  Params p;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  int64_t sq[3], so[3];
+  int Hq, G, d, window, sinks;   // window: INT32_MAX = all
+  float scale_log2;              // scale * log2(e)
+  float* part;                   // workspace
+};
+kvm_status_t launch_attend(const AttendArgs& a, cudaStream_t s);
+
+}  // namespace cache
+}  // namespace kvm

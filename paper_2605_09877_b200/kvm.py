@@ -6,6 +6,7 @@ been built (python -m paper_2605_09877_b200.build) -- there is no CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -28,7 +29,10 @@ EXPORTS = ["kvm_plan_capacity", "kvm_state_create", "kvm_prefill", "kvm_decode_s
            "kvm_profile_enable", "kvm_profile_read", "kvm_debug_counters", "kvm_attend_rows_noalloc", "kvm_merge_gate", "kvm_head_layernorm",
            "kvm_state_snapshot_info", "kvm_state_export_window", "kvm_state_import", "kvm_debug_expire_wait",
            "kvm_debug_decode_plan", "kvm_debug_decode_ahead", "kvm_debug_apply_plan", "kvm_debug_attention_plan",
-           "kvm_debug_drop_exchange"]
+           "kvm_debug_drop_exchange",
+           "kvm_cache_append", "kvm_cache_attend", "kvm_cache_workspace", "kvm_cache_copy_pages",
+           "kvm_pages_create", "kvm_pages_destroy", "kvm_pages_open", "kvm_pages_fork", "kvm_pages_close", "kvm_pages_extend",
+           "kvm_pages_trim", "kvm_pages_compact", "kvm_pages_table", "kvm_pages_info"]
 
 
 class KVMError(RuntimeError):
@@ -64,6 +68,16 @@ class Config(C.Structure):
         ("ln_q_weight", C.POINTER(C.c_float)), ("ln_q_bias", C.POINTER(C.c_float)),
         ("ln_k_weight", C.POINTER(C.c_float)), ("ln_k_bias", C.POINTER(C.c_float)),
     ]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int64),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32)]
+
+
+class CacheCall(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("start", C.c_void_p), ("count", C.c_void_p), ("batch", C.c_int32), ("max_pages", C.c_int32),
+                ("n_tokens", C.c_int64)]
 
 
 def _load():
@@ -128,6 +142,35 @@ def _load():
     L.kvm_state_export_window.argtypes = [vp, vp, vp, vp, vp]
     L.kvm_state_import.restype = C.c_int
     L.kvm_state_import.argtypes = [vp, C.POINTER(SnapshotInfo)] + [vp] * 9
+    cd, cc, i32p, i64p = C.POINTER(CacheDesc), C.POINTER(CacheCall), C.POINTER(C.c_int32), C.POINTER(C.c_int64)
+    L.kvm_cache_append.restype = C.c_int
+    L.kvm_cache_append.argtypes = [cd, cc, vp, vp, i64p, i64p, vp, vp]
+    L.kvm_cache_attend.restype = C.c_int
+    L.kvm_cache_attend.argtypes = [cd, cc, vp, C.c_int32, C.c_float, C.c_int32, C.c_int32, vp, i64p, i64p, vp, C.c_int64, vp, vp]
+    L.kvm_cache_workspace.restype = C.c_int64
+    L.kvm_cache_workspace.argtypes = [cd, cc, C.c_int32]
+    L.kvm_cache_copy_pages.restype = C.c_int
+    L.kvm_cache_copy_pages.argtypes = [cd, vp, vp, C.c_int64, vp]
+    L.kvm_pages_create.restype = C.c_int
+    L.kvm_pages_create.argtypes = [C.c_int64, C.c_int32, C.POINTER(vp)]
+    L.kvm_pages_destroy.restype = C.c_int
+    L.kvm_pages_destroy.argtypes = [vp]
+    L.kvm_pages_open.restype = C.c_int
+    L.kvm_pages_open.argtypes = [vp, i32p]
+    L.kvm_pages_fork.restype = C.c_int
+    L.kvm_pages_fork.argtypes = [vp, C.c_int32, i32p]
+    L.kvm_pages_close.restype = C.c_int
+    L.kvm_pages_close.argtypes = [vp, C.c_int32]
+    L.kvm_pages_extend.restype = C.c_int
+    L.kvm_pages_extend.argtypes = [vp, C.c_int32, C.c_int64, i32p, i32p]
+    L.kvm_pages_trim.restype = C.c_int
+    L.kvm_pages_trim.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32]
+    L.kvm_pages_compact.restype = C.c_int
+    L.kvm_pages_compact.argtypes = [vp, vp, vp, C.c_int64, i64p]
+    L.kvm_pages_table.restype = C.c_int
+    L.kvm_pages_table.argtypes = [vp, C.c_int32, vp, C.c_int64, i64p, i64p]
+    L.kvm_pages_info.restype = C.c_int
+    L.kvm_pages_info.argtypes = [vp, i64p, i64p]
     L.kvm_status_string.restype = C.c_char_p
     L.kvm_status_string.argtypes = [C.c_int]
     return L
@@ -456,3 +499,173 @@ class KVMState:
         if rc != KVM_OK:
             raise KVMError(rc, "kvm_debug_assignments")
         return slot, app
+
+
+def _strides3(t):
+    """Element strides of the first three dims; None where the tensor is contiguous."""
+    if t.is_contiguous():
+        return None
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError("the channels of a row must be contiguous")
+    return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
+
+
+class Cache:
+    """A pool of pages for exact keys and values in 8 bits (kvm_cache_t): codes k8, v8 float8_e4m3fn [n_pages, n_kv_heads, page_tokens,
+    head_dim], scales fp32 [n_pages, n_kv_heads] (powers of two; a row stands for code * scale).  The tensors are the caller's;
+    Cache.empty makes them.  Which page holds what is the caller's too (Pages keeps book of it).
+
+    pages int32 [B, max_pages], start int32 [B] (tokens in the cache before the call) and count int32 [B] (tokens of the call; None: all of
+    them) are CUDA tensors.  `status`: optional int32 CUDA tensor of one element that receives KVM_ERR_INVALID_ARG where the kernels
+    meet lengths or pages that the call does not allow, KVM_ERR_TIMEOUT should a bounded device-side wait run out."""
+
+    def __init__(self, k8, v8, k_scale, v_scale):
+        if k8.dim() != 4 or v8.shape != k8.shape or k_scale.shape != k8.shape[:2] or v_scale.shape != k8.shape[:2]:
+            raise ValueError("k8, v8 [n_pages, n_kv_heads, page_tokens, head_dim], k_scale, v_scale [n_pages, n_kv_heads]")
+        for t, dt in ((k8, torch.float8_e4m3fn), (v8, torch.float8_e4m3fn), (k_scale, torch.float32), (v_scale, torch.float32)):
+            if t.dtype != dt or not t.is_cuda or not t.is_contiguous() or t.device != k8.device:
+                raise ValueError("codes are contiguous float8_e4m3fn, scales contiguous float32, on one CUDA device")
+        self.k8, self.v8, self.k_scale, self.v_scale = k8, v8, k_scale, v_scale
+        self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k8.shape
+        self._device = k8.device
+        self._desc = CacheDesc(k8.data_ptr(), v8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.n_pages, self.n_kv_heads,
+                               self.head_dim, self.page_tokens)
+        self._ref = C.byref(self._desc)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int = 64, device="cuda"):
+        codes = [torch.zeros((n_pages, n_kv_heads, page_tokens, head_dim), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+                 for _ in range(2)]
+        return cls(*codes, *(torch.ones((n_pages, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+    def _call(self, pages, start, count, batch, n_tokens, tensors, status):
+        for t in (pages, start, count, status):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != self._device):
+                raise ValueError("pages, start, count and status are contiguous int32 tensors on the cache's device")
+        for t in tensors:
+            if t.dtype != torch.bfloat16 or t.device != self._device:
+                raise ValueError("rows are bfloat16 on the cache's device")
+        if pages.dim() != 2 or pages.shape[0] != batch or start.numel() != batch or (count is not None and count.numel() != batch):
+            raise ValueError("pages [batch, max_pages], start [batch], count [batch]")
+        return CacheCall(pages.data_ptr(), start.data_ptr(), count.data_ptr() if count is not None else None, batch, pages.shape[1], n_tokens)
+
+    def _on_device(self):
+        """A context in which the cache's device is the current one."""
+        return torch.cuda.device(self._device) if torch._C._cuda_getDevice() != self._device.index else contextlib.nullcontext()
+
+    def append(self, k, v, pages, start, count=None, status=None, stream=None):
+        """kvm_cache_append: k, v bf16 [B, n_kv_heads, T, head_dim] (channels contiguous) behind the tokens that the sequences hold."""
+        if k.dim() != 4 or v.shape != k.shape or k.shape[1] != self.n_kv_heads or k.shape[3] != self.head_dim:
+            raise ValueError("k, v [batch, n_kv_heads, tokens, head_dim]")
+        call = self._call(pages, start, count, k.shape[0], k.shape[2], (k, v), status)
+        with self._on_device():
+            rc = lib.kvm_cache_append(self._ref, C.byref(call), k.data_ptr(), v.data_ptr(), _strides3(k), _strides3(v),
+                                      status.data_ptr() if status is not None else None, _stream_ptr(stream))
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_cache_append")
+
+    def attend(self, q, pages, start, count=None, window: int = 0, sinks: int = 0, scale=None, out=None, status=None, stream=None):
+        """kvm_cache_attend: q bf16 [B, n_q_heads, T, head_dim] over the cache, which holds the T tokens' own keys already; a token sees
+        the last `window` positions up to its own (0: all) and the first `sinks`.  scale: 1 / sqrt(head_dim) unless given.  Rows of `out`
+        behind a sequence's count are left as they were (unset where `out` is made here)."""
+        if q.dim() != 4 or q.shape[3] != self.head_dim or (out is not None and out.shape != q.shape):
+            raise ValueError("q, out [batch, n_q_heads, tokens, head_dim]")
+        with self._on_device(), torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            if out is None:
+                out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+            call = self._call(pages, start, count, q.shape[0], q.shape[2], (q, out), status)
+            n = lib.kvm_cache_workspace(self._ref, C.byref(call), q.shape[1])
+            # (from the stream's own memory: neither a call on another stream nor another captured graph gets the same bytes)
+            ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
+            rc = lib.kvm_cache_attend(self._ref, C.byref(call), q.data_ptr(), q.shape[1], self.head_dim ** -0.5 if scale is None else scale,
+                                      window, sinks, out.data_ptr(), _strides3(q), _strides3(out), ws.data_ptr() if n > 0 else None,
+                                      max(n, 0), status.data_ptr() if status is not None else None, _stream_ptr(stream))
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_cache_attend")
+        return out
+
+    def copy_pages(self, src, dst, stream=None):
+        """kvm_cache_copy_pages: page src[i] to page dst[i]; lists or CPU int32 tensors."""
+        src, dst = (torch.as_tensor(x, dtype=torch.int32).contiguous() for x in (src, dst))
+        if src.is_cuda or dst.is_cuda or src.dim() != 1 or src.shape != dst.shape:
+            raise ValueError("src and dst are lists of the same length on the host")
+        with self._on_device():
+            rc = lib.kvm_cache_copy_pages(self._ref, src.data_ptr(), dst.data_ptr(), src.numel(), _stream_ptr(stream))
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_cache_copy_pages")
+
+
+class Pages:
+    """Which page of a pool holds which block of which sequence (kvm_pages_t): host bookkeeping, pages shared by forks until written."""
+
+    def __init__(self, n_pages: int, page_tokens: int = 64):
+        self._h = None
+        h = C.c_void_p()
+        self._do("kvm_pages_create", n_pages, page_tokens, C.byref(h))
+        self._h = h
+        self.n_pages = n_pages
+
+    def __del__(self):
+        if getattr(self, "_h", None):
+            lib.kvm_pages_destroy(self._h)
+            self._h = None
+
+    def _do(self, fn, *args):
+        rc = getattr(lib, fn)(*args)
+        if rc != KVM_OK:
+            raise KVMError(rc, fn)
+
+    def open(self) -> int:
+        seq = C.c_int32()
+        self._do("kvm_pages_open", self._h, C.byref(seq))
+        return seq.value
+
+    def fork(self, seq: int) -> int:
+        child = C.c_int32()
+        self._do("kvm_pages_fork", self._h, seq, C.byref(child))
+        return child.value
+
+    def close(self, seq: int):
+        self._do("kvm_pages_close", self._h, seq)
+
+    def extend(self, seq: int, n_tokens: int):
+        """Room for n_tokens more tokens; (src, dst) of the page to copy before the append, or None."""
+        src, dst = C.c_int32(), C.c_int32()
+        self._do("kvm_pages_extend", self._h, seq, n_tokens, C.byref(src), C.byref(dst))
+        return (src.value, dst.value) if src.value >= 0 else None
+
+    def trim(self, seq: int, window: int, sinks: int = 0):
+        self._do("kvm_pages_trim", self._h, seq, window, sinks)
+
+    def compact(self):
+        """(src, dst): the copies to make before the next call over the cache, as CPU int32 tensors."""
+        src, dst = torch.empty(self.n_pages, dtype=torch.int32), torch.empty(self.n_pages, dtype=torch.int32)
+        n = C.c_int64()
+        self._do("kvm_pages_compact", self._h, src.data_ptr(), dst.data_ptr(), self.n_pages, C.byref(n))
+        return src[:n.value].clone(), dst[:n.value].clone()
+
+    def table(self, seq: int):
+        n = C.c_int64()
+        self._do("kvm_pages_table", self._h, seq, None, 0, C.byref(n), None)
+        out = (C.c_int32 * max(1, n.value))()
+        self._do("kvm_pages_table", self._h, seq, out, n.value, None, None)
+        return list(out[:n.value])
+
+    def length(self, seq: int) -> int:
+        n = C.c_int64()
+        self._do("kvm_pages_table", self._h, seq, None, 0, None, C.byref(n))
+        return n.value
+
+    def tables(self, seqs, max_pages: int = 0, device="cuda"):
+        """pages [len(seqs), max_pages] and lengths [len(seqs)], int32 on `device`: what Cache.append and Cache.attend take."""
+        rows = [self.table(s) for s in seqs]
+        width = max([max_pages, 1] + [len(r) for r in rows])
+        t = torch.full((len(rows), width), -1, dtype=torch.int32)
+        for i, r in enumerate(rows):
+            t[i, :len(r)] = torch.tensor(r, dtype=torch.int32)
+        return t.to(device), torch.tensor([self.length(s) for s in seqs], dtype=torch.int32).to(device)
+
+    def info(self):
+        free, high = C.c_int64(), C.c_int64()
+        self._do("kvm_pages_info", self._h, C.byref(free), C.byref(high))
+        return dict(n_free=free.value, high=high.value)
