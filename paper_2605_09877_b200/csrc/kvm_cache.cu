@@ -8,11 +8,13 @@
 // thread and load, all loads in flight together), the maximum is taken on the bit patterns, and the codes are written from the registers.
 // Reads 2 bytes and writes 1 per element: bound by HBM for prompts, by one chain of dependent loads (lengths, page, rows) for single tokens.
 #include <algorithm>
+#include <atomic>
 #include <new>
 #include <vector>
 
 #include "kvm_cache.cuh"
 #include "kvm_internal.h"
+#include "tc_common.cuh"
 
 namespace kvm {
 namespace cache {
@@ -165,6 +167,28 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(const __grid_constant__
     for (int h = threadIdx.x; h < a.Hkv; h += 256) a.scales[which][dst * a.Hkv + h] = a.scales[which][src * a.Hkv + h];
 }
 
+// Codes as rows of d bytes, a box of one page of one head; rows land swizzled as the tensor core reads them (128 or 64 bytes).
+bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page) {
+  typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static std::atomic<void*> fn{nullptr};
+  void* f = fn.load(std::memory_order_acquire);
+  if (!f) {
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &qres) != cudaSuccess || !f) {
+      cudaGetLastError();
+      return false;
+    }
+    fn.store(f, std::memory_order_release);
+  }
+  const cuuint64_t gdim[2] = {(cuuint64_t)d, (cuuint64_t)rows}, gstr[1] = {(cuuint64_t)d};
+  const cuuint32_t box[2] = {(cuuint32_t)d, (cuuint32_t)page}, estr[2] = {1, 1};
+  return reinterpret_cast<EncodeFn>(f)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstr, box, estr,
+                                       CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // ---- arguments ----
 
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -189,8 +213,8 @@ kvm_status_t check_call(const kvm_cache_t* c, const kvm_cache_call_t* call, bool
     if (!aligned(call->pages, 4) || !aligned(call->start, 4) || !aligned(call->count, 4)) return KVM_ERR_INVALID_ARG;
   }
   const int64_t room = (int64_t)call->max_pages * c->page_tokens;   // positions are 32-bit numbers
-  if (call->n_tokens > room) return KVM_ERR_INVALID_ARG;
-  if (call->batch > kMaxBatch || room > (1 << 30)) return KVM_ERR_UNSUPPORTED;
+  if (call->n_tokens > room && !call->count) return KVM_ERR_INVALID_ARG;   // (with counts, n_tokens is only the padded extent)
+  if (call->batch > kMaxBatch || room > (1 << 30) || call->n_tokens > (1 << 30)) return KVM_ERR_UNSUPPORTED;
   return KVM_OK;
 }
 

@@ -187,7 +187,7 @@ BAD_CACHE = [(dict(k=None), 1), (dict(v=None), 1), (dict(k_scale=None), 1), (dic
              (dict(k_scale=(1 << 20) + 2), 1), (dict(n_pages=0), 1), (dict(n_kv_heads=0), 1), (dict(n_kv_heads=-2), 1), (dict(head_dim=96), 2),
              (dict(head_dim=256), 2), (dict(page_tokens=48), 2), (dict(page_tokens=8), 2), (dict(n_pages=1 << 31), 2), (dict(n_pages=(1 << 31) // 128), 2)]
 BAD_CALL = [(dict(pages=None), 1), (dict(start=None), 1), (dict(pages=(1 << 24) + 2), 1), (dict(start=(1 << 24) + 1), 1), (dict(count=(1 << 24) + 2), 1),
-            (dict(batch=0), 1), (dict(batch=1025), 2), (dict(max_pages=0), 1), (dict(n_tokens=0), 1), (dict(n_tokens=257), 1),
+            (dict(batch=0), 1), (dict(batch=1025), 2), (dict(max_pages=0), 1), (dict(n_tokens=0), 1), (dict(n_tokens=257), 1), (dict(n_tokens=(1 << 30) + 1, count=1 << 24), 2),
             (dict(max_pages=(1 << 24) + 1), 2)]
 
 
