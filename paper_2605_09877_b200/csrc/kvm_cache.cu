@@ -218,6 +218,8 @@ kvm_status_t check_call(const kvm_cache_t* c, const kvm_cache_call_t* call, bool
   return KVM_OK;
 }
 
+int64_t tiles_most(const kvm_cache_t* c, const kvm_cache_call_t* call) { return ((int64_t)call->max_pages * c->page_tokens + kTile - 1) / kTile; }
+
 Params params_of(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t* status) {
   Params p;
   p.k = (const uint8_t*)c->k; p.v = (const uint8_t*)c->v; p.ks = c->k_scale; p.vs = c->v_scale;
@@ -317,7 +319,9 @@ KVM_API kvm_status_t kvm_cache_copy_pages(const kvm_cache_t* cache, const int32_
 KVM_API int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_q_heads) {
   if (check_cache(cache, false) != KVM_OK || check_call(cache, call, false) != KVM_OK) return -1;
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads) return -1;
-  return 0;
+  const int64_t units = (int64_t)call->batch * cache->n_kv_heads, tiles = tiles_most(cache, call);
+  const int64_t cols = call->n_tokens * (n_q_heads / cache->n_kv_heads);
+  return cols <= kDecodeCols ? decode_workspace(units, tiles, cache->head_dim, (int)cols) : 0;
 }
 
 KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale,
@@ -335,14 +339,17 @@ KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_
   if (!strides_of(q_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, false, a.sq) ||
       !strides_of(out_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, true, a.so)) return KVM_ERR_INVALID_ARG;
   a.Hq = n_q_heads; a.G = n_q_heads / cache->n_kv_heads; a.d = cache->head_dim;
-  a.window = window ? window : INT32_MAX; a.sinks = sinks;
+  a.window = window ? window : INT32_MAX; a.sinks = std::min(sinks, 1 << 30);
+  const int64_t tiles = tiles_most(cache, call);
+  if (tiles * a.p.batch * a.p.Hkv > INT32_MAX) return KVM_ERR_UNSUPPORTED;   // (tiles of the call are numbered in 32 bits)
   a.scale_log2 = scale * 1.4426950408889634f;
   const int64_t need = kvm_cache_workspace(cache, call, n_q_heads);
   if (need < 0) return KVM_ERR_UNSUPPORTED;
   if (need > 0 && (!workspace || !aligned(workspace, 16))) return KVM_ERR_INVALID_ARG;
   if (workspace_bytes < need) return KVM_ERR_CAPACITY;
   a.part = (float*)workspace;
-  return launch_attend(a, (cudaStream_t)cuda_stream);
+  if (a.p.T * a.G <= kDecodeCols) return launch_decode8(a, tiles, rows_aligned(q, a.sq), (cudaStream_t)cuda_stream);
+  return launch_attend_rows(a, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(128) attend_rows_kernel(const AttendArgs a) {
   for (int e = 0; e < E; ++e) o[e] = __float2bfloat16_rn(acc[e] / l);
 }
 
-kvm_status_t launch_attend(const AttendArgs& a, cudaStream_t s) {
+kvm_status_t launch_attend_rows(const AttendArgs& a, cudaStream_t s) {
   const dim3 grid((unsigned)((a.p.T + 3) / 4), a.Hq, a.p.batch);
   if (a.d == 128) attend_rows_kernel<128><<<grid, 128, 0, s>>>(a); else attend_rows_kernel<64><<<grid, 128, 0, s>>>(a);
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
