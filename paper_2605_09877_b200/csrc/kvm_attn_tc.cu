@@ -29,6 +29,7 @@
 #include <algorithm>
 
 #include "kvm_internal.h"
+#include "out_stage.cuh"
 #include "tc_common.cuh"
 
 namespace kvm {
@@ -50,28 +51,6 @@ struct AttnTcParams {
   int out_vec;       // rows of `out` can be written with 16-byte stores (alignment of base and strides)
 };
 
-// Output staging: a 128 x D bf16 tile, row-major in shared memory, the 16-byte chunks of a row
-// permuted by the row index so that neither the row-per-thread writes nor the row-contiguous reads
-// conflict on the banks.
-template <int D>
-__device__ __forceinline__ uint4* stage_chunk(uint8_t* stage, int row, int k) {
-  constexpr int CPR = D / 8;   // chunks per row
-  return reinterpret_cast<uint4*>(stage + row * (D * 2) + ((k ^ (row & (CPR - 1))) << 4));
-}
-// 32 fp32 accumulator values of one row -> four chunks (channels [32 c, 32 c + 32)), scaled
-template <int D>
-__device__ __forceinline__ void stage_row32(uint8_t* stage, int row, int c, const uint32_t (&r)[32], float inv) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[8 * q + 2 * i]) * inv, __uint_as_float(r[8 * q + 2 * i + 1]) * inv);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    *stage_chunk<D>(stage, row, 4 * c + q) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
 // One warp writes rows [row0, row0 + nrows) of the staged tile to global memory, 32 / (D / 8) rows
 // per instruction, every row as one contiguous run of 16-byte stores.
 template <int D>

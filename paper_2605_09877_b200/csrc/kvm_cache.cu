@@ -321,7 +321,7 @@ KVM_API int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_ca
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads) return -1;
   const int64_t units = (int64_t)call->batch * cache->n_kv_heads, tiles = tiles_most(cache, call);
   const int64_t cols = call->n_tokens * (n_q_heads / cache->n_kv_heads);
-  return cols <= kDecodeCols ? decode_workspace(units, tiles, cache->head_dim, (int)cols) : 0;
+  return cols <= kDecodeCols ? decode_workspace(units, tiles, cache->head_dim, (int)cols) : prompt_workspace(units, cols, tiles, cache->head_dim);
 }
 
 KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale,
@@ -341,7 +341,9 @@ KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_
   a.Hq = n_q_heads; a.G = n_q_heads / cache->n_kv_heads; a.d = cache->head_dim;
   a.window = window ? window : INT32_MAX; a.sinks = std::min(sinks, 1 << 30);
   const int64_t tiles = tiles_most(cache, call);
-  if (tiles * a.p.batch * a.p.Hkv > INT32_MAX) return KVM_ERR_UNSUPPORTED;   // (tiles of the call are numbered in 32 bits)
+  // tiles of the call, and its rows of queries, are numbered in 32 bits
+  if (tiles * a.p.batch * a.p.Hkv > INT32_MAX || a.p.T * a.G > INT32_MAX - 128) return KVM_ERR_UNSUPPORTED;
+  if ((a.p.T * a.G + 127) / 128 * a.p.batch * a.p.Hkv > INT32_MAX) return KVM_ERR_UNSUPPORTED;
   a.scale_log2 = scale * 1.4426950408889634f;
   const int64_t need = kvm_cache_workspace(cache, call, n_q_heads);
   if (need < 0) return KVM_ERR_UNSUPPORTED;
@@ -349,7 +351,7 @@ KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_
   if (workspace_bytes < need) return KVM_ERR_CAPACITY;
   a.part = (float*)workspace;
   if (a.p.T * a.G <= kDecodeCols) return launch_decode8(a, tiles, rows_aligned(q, a.sq), (cudaStream_t)cuda_stream);
-  return launch_attend_rows(a, (cudaStream_t)cuda_stream);
+  return launch_prompt8(a, tiles, rows_aligned(q, a.sq), rows_aligned(out, a.so), (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

@@ -82,11 +82,13 @@ struct AttendArgs {
   float scale_log2;              // scale * log2(e)
   float* part;                   // workspace
 };
-kvm_status_t launch_attend_rows(const AttendArgs& a, cudaStream_t s);
 // tokens times heads of a group <= kDecodeCols; tiles: most key tiles of a sequence
 constexpr int kDecodeCols = 16;
 kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s);
 int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols);
+// more than that; rows: tokens times heads of a group
+kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s);
+int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d);
 
 }  // namespace cache
 }  // namespace kvm

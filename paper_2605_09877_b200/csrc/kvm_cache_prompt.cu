@@ -1,0 +1,676 @@
+// Attention of many tokens per sequence (prompts, pieces of prompts) over the 8-bit cache.
+//
+// The rows of a (sequence, kv head) unit are its query rows, row = token * G + head of the group, so that the heads of a group share the
+// key tiles.  One CTA owns 128 rows and walks the key tiles that they see: those of the first `sinks` tokens, then the window's.
+//     S = (q_hi + q_lo) K8^T   kind::f8f6f4: the codes as they lie in memory, q in two parts of e4m3 (see kvm_cache_decode.cu; exact for bf16)
+//     O += P V16               kind::f16: P in fp16 from tensor memory, V16 = the codes of the values in fp16 (exact)
+// Two products with e4m3 operands take the tensor core as long as one with 16-bit operands, so the keys need no conversion; the weights would
+// need their two parts for every element, on the warps that already bound the kernel, so for P V it is the codes that are converted, once
+// per tile, by four warps of their own.
+// Scales: that of a block of keys multiplies the logits of its columns, that of a block of values is added to the exponent of the weights
+// (relative to the largest of the CTA's visible blocks, 2^vbase) and taken out of the row sum again, 16 columns (the smallest page) at a time.
+//   warp 0       producer: page numbers and scales ahead, TMA into rings of three key tiles and two value tiles
+//   warp 1       issues S, warp 2 issues P V (one thread each), warp 3 idles
+//   warps 4-11   softmax, two warpgroups, each one half of the columns of every tile, a thread per row and half
+//   warps 12-15  value codes -> fp16, swizzled as the MMA reads them
+// With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.
+//
+#include <algorithm>
+#include <atomic>
+
+#include "kvm_cache.cuh"
+#include "out_stage.cuh"
+#include "tc_common.cuh"
+
+namespace kvm {
+namespace cache {
+
+bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page);   // kvm_cache.cu
+
+constexpr int kSplitTiles = 4;    // least key tiles of a split
+constexpr int kMaxSplits = 32;
+
+struct PromptArgs {
+  AttendArgs a;
+  int units, qtiles, nsplit;
+  int q_vec, out_vec;
+};
+
+struct Group { float ks, vr, back, drop; };   // 16 columns: scale of the keys; exponent taken over from the values' scale, 2^-that; 1: no products
+struct PromptTile {
+  int pos, flags;     // first key position; 1: some scale is NaN, 2: some group is dropped
+  int row[8];         // rows of the pages in the pool, -1: not loaded
+  int pad[2];
+  Group g[8];
+};
+constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written after the products of tile j + 2 at the earliest
+
+template <int D>
+struct PromptCfg {
+  static constexpr int NK = 3, NV = 2, NACC = 3;
+  static constexpr int T8 = 128 * D, T16 = 256 * D;
+  static constexpr int OFF_Q = 0;                        // hi, lo
+  static constexpr int OFF_K = OFF_Q + 2 * T8;
+  static constexpr int OFF_V8 = OFF_K + NK * T8;
+  static constexpr int OFF_V = OFF_V8 + NV * T8;
+  static constexpr int OFF_INFO = OFF_V + NV * T16;
+  static constexpr int OFF_XM = OFF_INFO + kInfo * (int)sizeof(PromptTile);   // float [2][2][128]
+  static constexpr int OFF_CQ = OFF_XM + 2 * 2 * 128 * 4;                     // float [128]
+  static constexpr int OFF_BAR = OFF_CQ + 128 * 4;
+  // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
+  static constexpr int SMEM = (OFF_BAR + 512 + 1024) > 120 * 1024 ? (OFF_BAR + 512 + 1024) : 120 * 1024;
+  static constexpr uint32_t COL_S = 0, COL_O = 384;
+};
+enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 8, PB_VFULL = 10, PB_VFREE = 12, PB_SFULL = 14, PB_PFULL = 17, PB_PVDONE = 20,
+       PB_XM = 23, PB_INFO = 25, PB_QFULL = 33, PB_COUNT = 34 };
+
+// What a CTA does: its rows and its key tiles.  (Also what the merge needs to know.)
+struct PromptWork {
+  int b, hk, start, row0, rows, first, last, jb, ntiles, parts;
+  Tiles t;
+};
+__device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int sp, PromptWork& w) {
+  const Params& p = args.a.p;
+  const int unit = idx % args.units, qt = args.qtiles - 1 - idx / args.units;   // (the last rows see the most keys: first)
+  w.b = unit / p.Hkv; w.hk = unit % p.Hkv;
+  int n;
+  if (!seq_lengths(p, w.b, w.start, n)) {
+    if (idx == unit && w.hk == 0 && sp == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
+    return false;
+  }
+  w.row0 = qt * 128;
+  const int64_t left = (int64_t)n * args.a.G - w.row0;
+  if (left <= 0) return false;
+  w.rows = (int)min((int64_t)128, left);
+  w.first = w.start + w.row0 / args.a.G;
+  w.last = w.start + (w.row0 + w.rows - 1) / args.a.G;
+  w.t = tiles_of(w.first, w.last, args.a.window, args.a.sinks);
+  const int per = max(kSplitTiles, (w.t.n + args.nsplit - 1) / args.nsplit);
+  w.parts = (w.t.n + per - 1) / per;
+  w.jb = sp * per;
+  w.ntiles = min(per, w.t.n - w.jb);
+  return w.ntiles > 0;
+}
+
+template <int D>
+__global__ void __launch_bounds__(512, 1)
+prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ PromptArgs args) {
+  using Cfg = PromptCfg<D>;
+  const AttendArgs& a = args.a;
+  const Params& p = a.p;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  PromptTile* info = reinterpret_cast<PromptTile*>(base + Cfg::OFF_INFO);
+  float* xm = reinterpret_cast<float*>(base + Cfg::OFF_XM);
+  float* s_cq = reinterpret_cast<float*>(base + Cfg::OFF_CQ);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + PB_COUNT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [16]
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  PromptWork w;
+  if (!prompt_work(args, blockIdx.x, blockIdx.y, w)) return;
+
+  if (tid == 0) {
+    tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
+    for (int s = 0; s < 3; ++s) {
+      tc::mbar_init(&bars[PB_KFULL + s], 1);
+      tc::mbar_init(&bars[PB_KFREE + s], 1);
+      tc::mbar_init(&bars[PB_SFULL + s], 1);
+      tc::mbar_init(&bars[PB_PFULL + s], 8);
+      tc::mbar_init(&bars[PB_PVDONE + s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      tc::mbar_init(&bars[PB_V8FULL + s], 1);
+      tc::mbar_init(&bars[PB_V8FREE + s], 4);
+      tc::mbar_init(&bars[PB_VFULL + s], 4);
+      tc::mbar_init(&bars[PB_VFREE + s], 1);
+      tc::mbar_init(&bars[PB_XM + s], 8);
+    }
+    for (int s = 0; s < kInfo; ++s) tc::mbar_init(&bars[PB_INFO + s], 1);
+    tc::mbar_init(&bars[PB_QFULL], 8);
+    *abort_flag = 0;
+    tc::fence_barrier_init();
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_relinquish();
+  }
+  // Page i of the CTA's tiles (ppt pages a tile): whether some row sees some key of it, and where it is.
+  const int ppt = kTile / p.page;
+  auto page_of = [&](int i, int& p0) -> int {   // >= 0: page; -1: not seen; -2: outside the pool
+    p0 = tile_at(w.t, w.jb + i / ppt) * kTile + (i % ppt) * p.page;
+    if (p0 > w.last || !(p0 + p.page > w.first - a.window + 1 || p0 < a.sinks)) return -1;
+    const int page = p.pages[(int64_t)w.b * p.max_pages + (p0 >> p.page_shift)];
+    return page >= 0 && page < p.n_pages ? page : -2;
+  };
+  {
+    int v = -1000;
+    for (int i = tid; i < w.ntiles * ppt; i += 512) {
+      int p0;
+      const int page = page_of(i, p0);
+      if (page < 0) continue;
+      const int e = scale_exp(p.vs[page * p.Hkv + w.hk]);
+      if (e < 128) v = max(v, e);
+    }
+    v = __reduce_max_sync(0xffffffffu, v);
+    if (lane == 0) s_vmax[warp] = v;
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  int vbase = -1000;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) vbase = max(vbase, s_vmax[i]);
+  if (vbase == -1000) vbase = 0;
+
+  auto fail = [&]() {
+    if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
+    *abort_flag = 1;
+  };
+#define KVM_WAIT(bar, par)                 \
+  if (!tc::mbar_wait((bar), (par))) {      \
+    fail();                                \
+    break;                                 \
+  }
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 0) {
+      // ------------------------------ producer ------------------------------
+      const int tpb = 32 / ppt, lt = lane / ppt, lp = lane % ppt;
+      struct Page { int row, ke, ve, pos; };
+      auto fetch = [&](int k) {
+        Page g{-1, 0, 0, 0};
+        const int j = k * tpb + lt;
+        if (j < w.ntiles) {
+          int p0;
+          const int page = page_of(j * ppt + lp, p0);
+          g.pos = p0 - lp * p.page;
+          g.ve = vbase;
+          if (page == -2) {
+            report(p.status, KVM_ERR_INVALID_ARG);
+            g.ke = g.ve = 128;
+          } else if (page >= 0) {
+            const int unit = page * p.Hkv + w.hk;
+            g.row = unit * p.page;
+            g.ke = scale_exp(p.ks[unit]);
+            g.ve = scale_exp(p.vs[unit]);
+          }
+        }
+        return g;
+      };
+      Page cur = fetch(0), nxt = fetch(1);
+      bool ok = true;
+      int nk = 0, nv = 0;   // tiles issued
+      for (int j = 0, k = 0, t = 0; j < w.ntiles; ++j) {
+        const int s = j % Cfg::NK, sv = j % Cfg::NV, in = j % kInfo;
+        if (lane == 0) ok = !*abort_flag && (j < Cfg::NK || tc::mbar_wait(&bars[PB_KFREE + s], ((j / Cfg::NK) - 1) & 1));
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        const bool mine = lt == t;
+        const uint32_t loads = __ballot_sync(0xffffffffu, mine && cur.row >= 0);
+        const uint32_t nans = __ballot_sync(0xffffffffu, mine && (cur.ke > 127 || cur.ve > 127));
+        const uint32_t drops = __ballot_sync(0xffffffffu, mine && cur.ve < vbase - 60);
+        const int bytes = __popc(loads) * p.page * D;
+        if (mine) {
+          if (lp == 0) { info[in].pos = cur.pos; info[in].flags = (nans ? 1 : 0) | (drops ? 2 : 0); }
+          const int vr = cur.ve > 127 ? 0 : max(cur.ve - vbase, -60);
+          const bool nan = cur.ke > 127 || cur.ve > 127;
+          const Group g{nan ? __int_as_float(0x7fc00000) : exp2i(cur.ke), (float)vr, exp2i(-vr), cur.ve < vbase - 60 ? 1.f : 0.f};
+          for (int i = 0; i < p.page / 16; ++i) info[in].g[lp * (p.page / 16) + i] = g;
+        }
+        __syncwarp();
+        if (lane == 0) {
+          tc::mbar_arrive(&bars[PB_INFO + in]);
+          tc::mbar_expect_tx(&bars[PB_KFULL + s], bytes);
+        }
+        __syncwarp();
+        if (mine && cur.row >= 0) tc::tma_load_2d(base + Cfg::OFF_K + s * Cfg::T8 + lp * p.page * D, &mapK, &bars[PB_KFULL + s], 0, cur.row);
+        nk = j + 1;
+        if (lane == 0) ok = j < Cfg::NV || tc::mbar_wait(&bars[PB_V8FREE + sv], ((j / Cfg::NV) - 1) & 1);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        if (lane == 0) tc::mbar_expect_tx(&bars[PB_V8FULL + sv], bytes);
+        __syncwarp();
+        if (mine && cur.row >= 0) tc::tma_load_2d(base + Cfg::OFF_V8 + sv * Cfg::T8 + lp * p.page * D, &mapV, &bars[PB_V8FULL + sv], 0, cur.row);
+        nv = j + 1;
+        if (++t == tpb) { t = 0; ++k; cur = nxt; nxt = fetch(k + 1); }
+      }
+      if (lane == 0) {
+        if (!ok) fail();
+        // nothing may be in flight into shared memory when the CTA ends, whatever became of the others
+        for (int j = max(0, nk - Cfg::NK); j < nk; ++j) tc::mbar_wait(&bars[PB_KFULL + j % Cfg::NK], (j / Cfg::NK) & 1);
+        for (int j = max(0, nv - Cfg::NV); j < nv; ++j) tc::mbar_wait(&bars[PB_V8FULL + j % Cfg::NV], (j / Cfg::NV) & 1);
+      }
+    } else if (warp == 1) {
+      // ------------------------------ S ------------------------------
+      if (lane == 0) {
+        constexpr uint32_t ID = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
+        const uint32_t aQ = tc::smem_u32(base + Cfg::OFF_Q), aK = tc::smem_u32(base + Cfg::OFF_K);
+        auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
+        bool dead = !tc::mbar_wait(&bars[PB_QFULL], 0);
+        for (int j = 0; j < w.ntiles && !dead; ++j) {
+          const int s = j % Cfg::NK, acc = j % Cfg::NACC;
+          if (*abort_flag) { dead = true; break; }
+          if (j >= Cfg::NACC && !tc::mbar_wait(&bars[PB_PVDONE + acc], ((j / Cfg::NACC) - 1) & 1)) { dead = true; break; }
+          if (!tc::mbar_wait(&bars[PB_KFULL + s], (j / Cfg::NK) & 1)) { dead = true; break; }
+          tc::tc_fence_after();
+          const uint32_t dS = tmem + Cfg::COL_S + 128 * acc;
+#pragma unroll
+          for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, desc(aQ + ks * 32), desc(aK + s * Cfg::T8 + ks * 32), ID, ks > 0);
+#pragma unroll
+          for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, desc(aQ + Cfg::T8 + ks * 32), desc(aK + s * Cfg::T8 + ks * 32), ID, 1u);
+          tc::mma_commit(&bars[PB_SFULL + acc]);
+          tc::mma_commit(&bars[PB_KFREE + s]);
+        }
+        if (dead) fail();
+      }
+    } else if (warp == 2) {
+      // ------------------------------ P V ------------------------------
+      if (lane == 0) {
+        constexpr uint32_t ID = tc::idesc_f16(128, D, true);
+        const uint32_t aV = tc::smem_u32(base + Cfg::OFF_V);
+        bool dead = false;
+        for (int j = 0; j < w.ntiles; ++j) {
+          const int s = j % Cfg::NV, acc = j % Cfg::NACC;
+          if (*abort_flag) { dead = true; break; }
+          if (!tc::mbar_wait(&bars[PB_VFULL + s], (j / Cfg::NV) & 1)) { dead = true; break; }
+          if (!tc::mbar_wait(&bars[PB_PFULL + acc], (j / Cfg::NACC) & 1)) { dead = true; break; }
+          tc::tc_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
+            tc::mma_f16_ts(tmem + Cfg::COL_O, tmem + Cfg::COL_S + 128 * acc + 64 * (kk >> 2) + 8 * (kk & 3),
+                           tc::smem_desc_sw128(aV + s * Cfg::T16 + kk * 2048, 128 * 128, 1024), ID, (j > 0 || kk > 0) ? 1u : 0u);
+          tc::mma_commit(&bars[PB_PVDONE + acc]);
+          tc::mma_commit(&bars[PB_VFREE + s]);
+        }
+        if (dead) fail();
+      }
+    }
+  } else if (warp >= 12) {
+    // ------------------------------ values to fp16 ------------------------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    constexpr int PIECES = D / 16;                 // 16-byte pieces of a row of codes
+    const int t = tid - 384, r8 = t & 7, pc = (t >> 3) & (PIECES - 1), r0 = (t >> 3) / PIECES * 8 + r8;   // rows r0 + 8 (16 / PIECES) i
+    constexpr int STEP = 8 * 16 / PIECES;
+    bool ok = true;
+    for (int j = 0; j < w.ntiles; ++j) {
+      const int sv = j % Cfg::NV, in = j % kInfo;
+      bool good = tc::mbar_wait(&bars[PB_V8FULL + sv], (j / Cfg::NV) & 1) && tc::mbar_wait(&bars[PB_INFO + in], (j / kInfo) & 1) && !*abort_flag;
+      if (good && j >= Cfg::NV) good = tc::mbar_wait(&bars[PB_VFREE + sv], ((j / Cfg::NV) - 1) & 1);
+      ok = __all_sync(0xffffffffu, good);
+      if (!ok) break;
+      const int pos = info[in].pos;
+      const bool all = pos + 127 <= w.last && (pos > w.first - a.window || pos + 127 < a.sinks);   // every key is seen by some row
+      const uint8_t* src = base + Cfg::OFF_V8 + sv * Cfg::T8;
+      uint8_t* dst = base + Cfg::OFF_V + sv * Cfg::T16;
+#pragma unroll
+      for (int r = r0; r < 128; r += STEP) {
+        const int piece = D == 128 ? (pc ^ (r & 7)) : (pc ^ ((r >> 1) & 3));
+        uint4 c = *reinterpret_cast<const uint4*>(src + r * D + piece * 16);
+        if (!all) {   // whatever the ring or the page holds there must not meet the weight 0
+          const int key = pos + r;
+          if (!(key <= w.last && (key > w.first - a.window || key < a.sinks))) c = make_uint4(0, 0, 0, 0);
+        }
+        uint4 lo, hi;
+        lo.x = e4m3x2_to_f16x2(c.x & 0xffff); lo.y = e4m3x2_to_f16x2(c.x >> 16); lo.z = e4m3x2_to_f16x2(c.y & 0xffff); lo.w = e4m3x2_to_f16x2(c.y >> 16);
+        hi.x = e4m3x2_to_f16x2(c.z & 0xffff); hi.y = e4m3x2_to_f16x2(c.z >> 16); hi.z = e4m3x2_to_f16x2(c.w & 0xffff); hi.w = e4m3x2_to_f16x2(c.w >> 16);
+        uint8_t* row = dst + (pc >> 2) * (128 * 128) + r * 128;
+        *reinterpret_cast<uint4*>(row + (((2 * (pc & 3)) ^ r8) << 4)) = lo;
+        *reinterpret_cast<uint4*>(row + (((2 * (pc & 3) + 1) ^ r8) << 4)) = hi;
+      }
+      tc::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        tc::mbar_arrive(&bars[PB_VFULL + sv]);
+        tc::mbar_arrive(&bars[PB_V8FREE + sv]);
+      }
+    }
+    if (!ok && lane == 0) fail();
+  } else {
+    // ------------------------------ q; softmax; results ------------------------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    {
+      // two threads per row: power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
+      const int t = tid - 128, r = t >> 1, hf = t & 1;
+      constexpr int E = D / 2;
+      const bool live = r < w.rows;
+      const int rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
+      const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + hf * E;
+      uint32_t x[E / 2];
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) x[i] = 0;
+      if (live && args.q_vec) {
+#pragma unroll
+        for (int i = 0; i < E / 8; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * i);
+          x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        }
+      } else if (live) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) x[i] = (uint32_t)__bfloat16_as_ushort(src[2 * i]) | ((uint32_t)__bfloat16_as_ushort(src[2 * i + 1]) << 16);
+      }
+      uint32_t top2 = 0;
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) top2 = __vmaxu2(top2, x[i] & 0x7fff7fffu);
+      uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      const bool bad = top >= 0x7f80u;
+      const int e = max((int)(top >> 7), 10);
+      const float mul = bad ? 0.f : exp2i(134 - e);
+#pragma unroll
+      for (int i = 0; i < E / 16; ++i) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          hi[q] = lo[q] = 0;
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const uint32_t v = x[8 * i + 2 * q + z];
+            const float y0 = bad ? 0.f : __uint_as_float(v << 16) * mul, y1 = bad ? 0.f : __uint_as_float(v & 0xffff0000u) * mul;
+            const uint32_t h = to_e4m3x2(y0, y1);
+            const float2 back = e4m3x2_to_float2(h);
+            hi[q] |= h << (16 * z);
+            lo[q] |= to_e4m3x2(y0 - back.x, y1 - back.y) << (16 * z);
+          }
+        }
+        const int piece = hf * (E / 16) + i;
+        uint8_t* at = base + Cfg::OFF_Q + r * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
+        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+      if (hf == 0) s_cq[r] = bad ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
+      tc::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars[PB_QFULL]);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+    }
+    const int half = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+    constexpr int HD = D / 2;
+    const uint32_t to_mine = tmem + lane_base + Cfg::COL_O + half * HD;   // this thread's share of O
+    const int pos_row = row < w.rows ? w.start + (w.row0 + row) / a.G : w.last;
+    float cq = s_cq[row];
+    bool bad = !(cq == cq);   // NaN rows are marked, not computed with
+    if (bad) cq = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    bool ok = true;
+    for (int j = 0; j < w.ntiles && ok; ++j) {
+      do {
+        ok = false;
+        const int acc = j % Cfg::NACC, in = j % kInfo;
+        KVM_WAIT(&bars[PB_INFO + in], (j / kInfo) & 1);
+        KVM_WAIT(&bars[PB_SFULL + acc], (j / Cfg::NACC) & 1);
+        __syncwarp();
+        tc::tc_fence_after();
+        const uint32_t ts = tmem + lane_base + Cfg::COL_S + 128 * acc + half * 64;
+        float x[64];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t r[32];
+          tc::tmem_ld32(ts + c * 32, r);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[c * 32 + i] = __uint_as_float(r[i]);
+        }
+        tc::tmem_wait_ld();
+        const int pos = info[in].pos, flags = info[in].flags;
+        Group g[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = info[in].g[half * 4 + i];
+        const bool all = pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks);   // (uniform) all rows see all keys
+        if (!all || flags) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool nan = !(g[i].ks == g[i].ks);
+            if (nan) g[i].ks = 0.f;
+#pragma unroll
+            for (int c = 16 * i; c < 16 * i + 16; ++c) {
+              const bool see = sees(pos_row, pos + half * 64 + c, a.window, a.sinks);
+              bad = bad || (see && nan);
+              x[c] = see && !nan ? x[c] : -INFINITY;
+            }
+            if (nan) g[i].ks = 1.f;
+          }
+        }
+        float mx = -INFINITY;
+        float cg[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          cg[i] = fmaxf(cq * g[i].ks, 1.17549435e-38f);   // (never 0: a masked column is -inf)
+          float m2[2] = {x[16 * i], x[16 * i + 1]};
+#pragma unroll
+          for (int c = 2; c < 16; c += 2) { m2[0] = fmaxf(m2[0], x[16 * i + c]); m2[1] = fmaxf(m2[1], x[16 * i + c + 1]); }
+          const float m = fmaxf(m2[0], m2[1]);
+          mx = fmaxf(mx, fmaf(m, cg[i], g[i].vr));
+        }
+        xm[((j & 1) * 2 + half) * 128 + row] = mx;
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars[PB_XM + (j & 1)]);
+        KVM_WAIT(&bars[PB_XM + (j & 1)], (j >> 1) & 1);
+        mx = fmaxf(mx, xm[((j & 1) * 2 + (1 - half)) * 128 + row]);
+        const float mnew = fmaxf(m_run, mx);
+        if (j == 0) {
+          m_run = mnew;
+        } else if (__any_sync(0xffffffffu, mnew > m_run + 8.0f)) {   // the same decision in both warps that share these rows
+          KVM_WAIT(&bars[PB_PVDONE + (j - 1) % Cfg::NACC], ((j - 1) / Cfg::NACC) & 1);
+          __syncwarp();
+          tc::tc_fence_after();
+          const float corr = (m_run == -INFINITY) ? 0.f : tc::ex2_approx(m_run - mnew);
+          l_run *= corr;
+          m_run = mnew;
+#pragma unroll
+          for (int c = 0; c < HD / 32; ++c) {
+            uint32_t r[32];
+            tc::tmem_ld32(to_mine + c * 32, r);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+            tc::tmem_st32(to_mine + c * 32, r);
+          }
+          tc::tmem_wait_st();
+        }
+        const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+        uint32_t wd[32];
+        float lsum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float add = neg_m + g[i].vr;
+          float l0 = 0.f, l1 = 0.f;
+          const float cc = cg[i];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const int at = 16 * i + 2 * c;
+            const float y0 = fmaf(x[at], cc, add), y1 = fmaf(x[at + 1], cc, add);
+            const float p0 = tc::ex2_approx(y0), p1 = (c & 1) ? tc::ex2_poly(y1) : tc::ex2_approx(y1);
+            l0 += p0; l1 += p1;
+            const __half2 h = __floats2half2_rn(p0, p1);
+            wd[8 * i + c] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          lsum = fmaf(l0 + l1, g[i].back, lsum);
+        }
+        if (flags & 2) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (g[i].drop != 0.f) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c) wd[8 * i + c] = 0;
+            }
+        }
+        tc::tmem_st32(ts, wd);
+        tc::tmem_wait_st();
+        l_run += lsum;
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars[PB_PFULL + acc]);
+        ok = true;
+      } while (false);
+    }
+    // the row sum is the sum of the halves' sums (through the exchange of the maxima, idle by now); half h stores channels [h D/2, (h+1) D/2)
+    if (ok) {
+      ok = tc::mbar_wait(&bars[PB_PVDONE + (w.ntiles - 1) % Cfg::NACC], ((w.ntiles - 1) / Cfg::NACC) & 1);
+      if (!ok) fail();
+      tc::tc_fence_after();
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");   // (every thread has read the last maxima)
+    xm[half * 128 + row] = l_run;
+    xm[(2 + half) * 128 + row] = bad ? 1.f : 0.f;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const bool good = ok && !*abort_flag;
+    const float l = l_run + xm[(1 - half) * 128 + row];
+    bad = bad || xm[(3 - half) * 128 + row] != 0.f;
+    const float nan = __int_as_float(0x7fc00000);
+    uint8_t* stage = base + Cfg::OFF_K;   // (the key and value tiles are idle)
+    __syncwarp();
+    if (w.parts == 1) {
+      const float inv = bad ? nan : exp2i(vbase) / l;
+      if (args.out_vec) {
+        if (good) {
+#pragma unroll
+          for (int c = 0; c < HD / 32; ++c) {
+            uint32_t r[32];
+            tc::tmem_ld32(to_mine + c * 32, r);
+            tc::tmem_wait_ld();
+            stage_row32<D>(stage, row, half * (HD / 32) + c, r, inv);
+          }
+        }
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (good) {
+          constexpr int CPR = D / 8, RPI = 32 / CPR;
+          const int k = lane % CPR;
+          for (int r = (warp - 4) * 16 + lane / CPR; r < (warp - 3) * 16; r += RPI) {
+            if (r >= w.rows) continue;
+            const int rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
+            *reinterpret_cast<uint4*>(a.out + w.b * a.so[0] + hq * a.so[1] + tokq * a.so[2] + k * 8) = *stage_chunk<D>(stage, r, k);
+          }
+        }
+      } else if (good) {
+        const int rg = w.row0 + row, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
+        __nv_bfloat16* orow = a.out + w.b * a.so[0] + hq * a.so[1] + tokq * a.so[2] + half * HD;
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t r[32];
+          tc::tmem_ld32(to_mine + c * 32, r);
+          tc::tmem_wait_ld();
+          if (row < w.rows) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) orow[c * 32 + i] = __float2bfloat16_rn(__uint_as_float(r[i]) * inv);
+          }
+        }
+      }
+    } else if (good) {
+      // partial result: O (in units of 2^m_run), m_run and the sum, [channel][row]
+      float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
+      const float unit = bad ? nan : exp2i(vbase);
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        uint32_t r[32];
+        tc::tmem_ld32(to_mine + c * 32, r);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mine[(half * HD + c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;
+      }
+      if (half == 0) {
+        mine[D * 128 + row] = m_run;
+        mine[(D + 1) * 128 + row] = bad ? nan : l;
+      }
+    }
+  }
+#undef KVM_WAIT
+  tc::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+// Rows whose key tiles were split: thread = (row, half of the channels).
+template <int D>
+__global__ void __launch_bounds__(256) prompt_combine_kernel(const __grid_constant__ PromptArgs args) {
+  const AttendArgs& a = args.a;
+  PromptWork w;
+  if (!prompt_work(args, blockIdx.x, 0, w) || w.parts == 1) return;
+  const int row = threadIdx.x & 127, half = threadIdx.x >> 7;
+  if (row >= w.rows) return;
+  constexpr int HD = D / 2, ST = (D + 2) * 128;
+  const float* part = a.part + (int64_t)blockIdx.x * args.nsplit * ST + row;
+  float m = -INFINITY;
+  for (int z = 0; z < w.parts; ++z) m = fmaxf(m, part[z * ST + D * 128]);
+  float wz[kMaxSplits], l = 0.f;
+#pragma unroll
+  for (int z = 0; z < kMaxSplits; ++z) {
+    wz[z] = 0.f;
+    if (z < w.parts) {
+      const float mz = part[z * ST + D * 128], lz = part[z * ST + (D + 1) * 128];
+      wz[z] = mz == -INFINITY ? 0.f : exp2f(mz - m);
+      l += lz == lz ? lz * wz[z] : lz;   // (a NaN row stays one where its weight is 0)
+    }
+  }
+  const int rg = w.row0 + row, tok = rg / a.G, hq = w.hk * a.G + rg - tok * a.G;
+  __nv_bfloat16* out = a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + half * HD;
+  const float inv = 1.f / l;
+  for (int c = 0; c < HD; c += 8) {
+    float o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int z = 0; z < kMaxSplits; ++z) {
+      if (z >= w.parts) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = fmaf(part[z * ST + (half * HD + c + i) * 128], wz[z], o[i]);
+    }
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(o[2 * i] * inv, o[2 * i + 1] * inv);
+    if (args.out_vec) {
+      *reinterpret_cast<uint4*>(out + c) = *reinterpret_cast<uint4*>(h);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { out[c + 2 * i] = h[i].x; out[c + 2 * i + 1] = h[i].y; }
+    }
+  }
+}
+
+// (row tiles of 128, key splits) of a call.  Few row tiles: as many splits as fill the SMs.
+static void prompt_plan(int64_t units, int64_t rows, int64_t tiles, int& qtiles, int& nsplit) {
+  qtiles = (int)((rows + 127) / 128);
+  const int64_t ctas = units * qtiles;
+  nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({148 / ctas, (tiles + kSplitTiles - 1) / kSplitTiles, kMaxSplits}));
+}
+
+int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d) {
+  int qt, ns;
+  prompt_plan(units, rows, tiles, qt, ns);
+  return ns == 1 ? 0 : units * qt * ns * (d + 2) * 128 * 4;
+}
+
+template <int D>
+static kvm_status_t launch_prompt_d(const PromptArgs& args, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};   // devices on which the limit has been raised
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (cudaFuncSetAttribute(prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptCfg<D>::SMEM) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+    if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  prompt_kernel<D><<<dim3((unsigned)(args.units * args.qtiles), args.nsplit), 512, PromptCfg<D>::SMEM, s>>>(mapK, mapV, args);
+  if (args.nsplit > 1) prompt_combine_kernel<D><<<args.units * args.qtiles, 256, 0, s>>>(args);
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+
+kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s) {
+  PromptArgs args;
+  args.a = a;
+  args.units = a.p.batch * a.p.Hkv;
+  prompt_plan(args.units, a.p.T * a.G, tiles, args.qtiles, args.nsplit);
+  args.q_vec = q_vec ? 1 : 0; args.out_vec = out_vec ? 1 : 0;
+  CUtensorMap mapK, mapV;
+  const int64_t rows = a.p.n_pages * a.p.Hkv * a.p.page;
+  if (!encode_tmap_codes(&mapK, a.p.k, a.d, rows, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, rows, a.p.page)) return KVM_ERR_CUDA;
+  return a.d == 128 ? launch_prompt_d<128>(args, mapK, mapV, s) : launch_prompt_d<64>(args, mapK, mapV, s);
+}
+
+}  // namespace cache
+}  // namespace kvm
