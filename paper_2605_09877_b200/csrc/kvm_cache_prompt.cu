@@ -6,13 +6,13 @@
 //     O += P V16               kind::f16: P in fp16 from tensor memory, V16 = the codes of the values in fp16 (exact)
 // Two products with e4m3 operands take the tensor core as long as one with 16-bit operands, so the keys need no conversion; the weights would
 // need their two parts for every element, on the warps that already bound the kernel, so for P V it is the codes that are converted, once
-// per tile, by four warps of their own.
+// per tile, by warps of their own.
 // Scales: that of a block of keys multiplies the logits of its columns, that of a block of values is added to the exponent of the weights
 // (relative to the largest of the CTA's visible blocks, 2^vbase) and taken out of the row sum again, 16 columns (the smallest page) at a time.
 //   warp 0       producer: page numbers and scales ahead, TMA into rings of three key tiles and two value tiles
-//   warp 1       issues S, warp 2 issues P V (one thread each), warp 3 idles
-//   warps 4-11   softmax, two warpgroups, each one half of the columns of every tile, a thread per row and half
-//   warps 12-15  value codes -> fp16, swizzled as the MMA reads them
+//   warp 1       issues S into three accumulators, warp 2 issues P V (one thread each), warp 3 idles
+//   warps 4-19   softmax: four threads per row, 32 columns of every tile each; P goes over the columns of S that the thread has read
+//   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 // With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.
 //
 #include <algorithm>
@@ -39,11 +39,12 @@ struct PromptArgs {
 struct Group { float ks, vr, back, drop; };   // 16 columns: scale of the keys; exponent taken over from the values' scale, 2^-that; 1: no products
 struct PromptTile {
   int pos, flags;     // first key position; 1: some scale is NaN, 2: some group is dropped
-  int row[8];         // rows of the pages in the pool, -1: not loaded
   int pad[2];
   Group g[8];
 };
-constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written after the products of tile j + 2 at the earliest
+constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
+constexpr int kRows = 128; // rows of a CTA
+constexpr int kThreads = 768;
 
 template <int D>
 struct PromptCfg {
@@ -54,15 +55,16 @@ struct PromptCfg {
   static constexpr int OFF_V8 = OFF_K + NK * T8;
   static constexpr int OFF_V = OFF_V8 + NV * T8;
   static constexpr int OFF_INFO = OFF_V + NV * T16;
-  static constexpr int OFF_XM = OFF_INFO + kInfo * (int)sizeof(PromptTile);   // float [2][2][128]
-  static constexpr int OFF_CQ = OFF_XM + 2 * 2 * 128 * 4;                     // float [128]
+  static constexpr int OFF_XM = OFF_INFO + kInfo * (int)sizeof(PromptTile);   // float4 [2][128]: maxima of the row's quarters, by tile parity
+  static constexpr int OFF_CQ = OFF_XM + 2 * 128 * 16;                        // float [128]
   static constexpr int OFF_BAR = OFF_CQ + 128 * 4;
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static constexpr int SMEM = (OFF_BAR + 512 + 1024) > 120 * 1024 ? (OFF_BAR + 512 + 1024) : 120 * 1024;
-  static constexpr uint32_t COL_S = 0, COL_O = 384;
+  static constexpr uint32_t COL_S = 0, COL_O = 384;      // S / P accumulator i at 128 i
 };
-enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 8, PB_VFULL = 10, PB_VFREE = 12, PB_SFULL = 14, PB_PFULL = 17, PB_PVDONE = 20,
-       PB_XM = 23, PB_INFO = 25, PB_QFULL = 33, PB_COUNT = 34 };
+// PB_READY: P of the tile is in tensor memory (16 softmax warps) and its values are in fp16 (4 converting warps)
+enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 8, PB_VFREE = 10, PB_SFULL = 12, PB_READY = 15, PB_PVDONE = 18, PB_QFULL = 21,
+       PB_COUNT = 22 };
 
 // What a CTA does: its rows and its key tiles.  (Also what the merge needs to know.)
 struct PromptWork {
@@ -78,10 +80,10 @@ __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int
     if (idx == unit && w.hk == 0 && sp == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
     return false;
   }
-  w.row0 = qt * 128;
+  w.row0 = qt * kRows;
   const int64_t left = (int64_t)n * args.a.G - w.row0;
   if (left <= 0) return false;
-  w.rows = (int)min((int64_t)128, left);
+  w.rows = (int)min((int64_t)kRows, left);
   w.first = w.start + w.row0 / args.a.G;
   w.last = w.start + (w.row0 + w.rows - 1) / args.a.G;
   w.t = tiles_of(w.first, w.last, args.a.window, args.a.sinks);
@@ -91,9 +93,55 @@ __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int
   w.ntiles = min(per, w.t.n - w.jb);
   return w.ntiles > 0;
 }
+// Barrier of the four warps that share 32 rows, which also tells whether all are well.
+__device__ __forceinline__ bool row_barrier(int id, bool ok) {
+  uint32_t r;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.and.aligned.pred q, %2, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"(ok ? 1u : 0u), "r"(id) : "memory");
+  return r != 0;
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// tc::ex2_poly for two
+__device__ __forceinline__ void ex2_poly2(uint64_t v, float& p0, float& p1) {
+  float x, y;
+  unpack2(v, x, y);
+  v = pack2(fmaxf(x, -125.f), fmaxf(y, -125.f));
+  const uint64_t r = add2(v, pack2(12582912.f, 12582912.f));
+  const uint64_t f = fma2(add2(r, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), v);
+  uint64_t p = fma2(f, pack2(0.0096181291f, 0.0096181291f), pack2(0.0555041087f, 0.0555041087f));
+  p = fma2(p, f, pack2(0.2402265070f, 0.2402265070f));
+  p = fma2(p, f, pack2(0.6931471806f, 0.6931471806f));
+  p = fma2(p, f, pack2(1.0f, 1.0f));
+  float r0, r1;
+  unpack2(r, r0, r1);
+  unpack2(p, p0, p1);
+  p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
+  p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
+}
 
 template <int D>
-__global__ void __launch_bounds__(512, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ PromptArgs args) {
   using Cfg = PromptCfg<D>;
   const AttendArgs& a = args.a;
@@ -106,7 +154,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + PB_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [16]
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [24]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   PromptWork w;
   if (!prompt_work(args, blockIdx.x, blockIdx.y, w)) return;
@@ -117,18 +165,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::mbar_init(&bars[PB_KFULL + s], 1);
       tc::mbar_init(&bars[PB_KFREE + s], 1);
       tc::mbar_init(&bars[PB_SFULL + s], 1);
-      tc::mbar_init(&bars[PB_PFULL + s], 8);
+      tc::mbar_init(&bars[PB_READY + s], 16 + 4);
       tc::mbar_init(&bars[PB_PVDONE + s], 1);
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&bars[PB_V8FULL + s], 1);
       tc::mbar_init(&bars[PB_V8FREE + s], 4);
-      tc::mbar_init(&bars[PB_VFULL + s], 4);
       tc::mbar_init(&bars[PB_VFREE + s], 1);
-      tc::mbar_init(&bars[PB_XM + s], 8);
     }
-    for (int s = 0; s < kInfo; ++s) tc::mbar_init(&bars[PB_INFO + s], 1);
-    tc::mbar_init(&bars[PB_QFULL], 8);
+    tc::mbar_init(&bars[PB_QFULL], 16);
     *abort_flag = 0;
     tc::fence_barrier_init();
   }
@@ -146,7 +191,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   };
   {
     int v = -1000;
-    for (int i = tid; i < w.ntiles * ppt; i += 512) {
+    for (int i = tid; i < w.ntiles * ppt; i += kThreads) {
       int p0;
       const int page = page_of(i, p0);
       if (page < 0) continue;
@@ -162,21 +207,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   const uint32_t tmem = *tmem_slot;
   int vbase = -1000;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) vbase = max(vbase, s_vmax[i]);
+  for (int i = 0; i < kThreads / 32; ++i) vbase = max(vbase, s_vmax[i]);
   if (vbase == -1000) vbase = 0;
 
   auto fail = [&]() {
     if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
     *abort_flag = 1;
   };
-#define KVM_WAIT(bar, par)                 \
-  if (!tc::mbar_wait((bar), (par))) {      \
-    fail();                                \
-    break;                                 \
-  }
-
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
       // ------------------------------ producer ------------------------------
       const int tpb = 32 / ppt, lt = lane / ppt, lp = lane % ppt;
@@ -223,8 +261,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         __syncwarp();
         if (lane == 0) {
-          tc::mbar_arrive(&bars[PB_INFO + in]);
-          tc::mbar_expect_tx(&bars[PB_KFULL + s], bytes);
+          tc::mbar_expect_tx(&bars[PB_KFULL + s], bytes);   // (and what was written about the tile: the issuing thread and, by its products,
+                                                            // the softmax warps, come after this)
         }
         __syncwarp();
         if (mine && cur.row >= 0) tc::tma_load_2d(base + Cfg::OFF_K + s * Cfg::T8 + lp * p.page * D, &mapK, &bars[PB_KFULL + s], 0, cur.row);
@@ -246,99 +284,114 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       }
     } else if (warp == 1) {
       // ------------------------------ S ------------------------------
+      // (an issuing thread competes with the softmax warps for every instruction: descriptors are advanced, not built, and nothing but
+      // barriers is looked at)
       if (lane == 0) {
         constexpr uint32_t ID = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
-        const uint32_t aQ = tc::smem_u32(base + Cfg::OFF_Q), aK = tc::smem_u32(base + Cfg::OFF_K);
         auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
-        bool dead = !tc::mbar_wait(&bars[PB_QFULL], 0);
-        for (int j = 0; j < w.ntiles && !dead; ++j) {
-          const int s = j % Cfg::NK, acc = j % Cfg::NACC;
-          if (*abort_flag) { dead = true; break; }
-          if (j >= Cfg::NACC && !tc::mbar_wait(&bars[PB_PVDONE + acc], ((j / Cfg::NACC) - 1) & 1)) { dead = true; break; }
-          if (!tc::mbar_wait(&bars[PB_KFULL + s], (j / Cfg::NK) & 1)) { dead = true; break; }
+        const uint64_t dQ = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
+        bool ok = tc::mbar_wait(&bars[PB_QFULL], 0);
+        uint32_t s = 0, par = 0;   // ring of three: key tiles and accumulators
+        for (int j = 0; j < w.ntiles && ok; ++j) {
+          ok = j < Cfg::NACC || tc::mbar_wait(&bars[PB_PVDONE + s], par ^ 1);
+          ok = ok && tc::mbar_wait(&bars[PB_KFULL + s], par);
+          if (!ok) break;
           tc::tc_fence_after();
-          const uint32_t dS = tmem + Cfg::COL_S + 128 * acc;
+          const uint64_t k = dK + s * (Cfg::T8 >> 4);
+          const uint32_t dS = tmem + Cfg::COL_S + 128 * s;
 #pragma unroll
-          for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, desc(aQ + ks * 32), desc(aK + s * Cfg::T8 + ks * 32), ID, ks > 0);
+          for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + 2 * ks, k + 2 * ks, ID, ks > 0);
 #pragma unroll
-          for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, desc(aQ + Cfg::T8 + ks * 32), desc(aK + s * Cfg::T8 + ks * 32), ID, 1u);
-          tc::mma_commit(&bars[PB_SFULL + acc]);
+          for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID, 1u);
+          tc::mma_commit(&bars[PB_SFULL + s]);
           tc::mma_commit(&bars[PB_KFREE + s]);
+          if (++s == 3) { s = 0; par ^= 1; }
         }
-        if (dead) fail();
+        if (!ok) fail();
       }
     } else if (warp == 2) {
       // ------------------------------ P V ------------------------------
       if (lane == 0) {
         constexpr uint32_t ID = tc::idesc_f16(128, D, true);
-        const uint32_t aV = tc::smem_u32(base + Cfg::OFF_V);
-        bool dead = false;
+        const uint64_t dV = tc::smem_desc_sw128(tc::smem_u32(base + Cfg::OFF_V), 128 * 128, 1024);
+        uint32_t s = 0, par = 0;
+        bool ok = true;
         for (int j = 0; j < w.ntiles; ++j) {
-          const int s = j % Cfg::NV, acc = j % Cfg::NACC;
-          if (*abort_flag) { dead = true; break; }
-          if (!tc::mbar_wait(&bars[PB_VFULL + s], (j / Cfg::NV) & 1)) { dead = true; break; }
-          if (!tc::mbar_wait(&bars[PB_PFULL + acc], (j / Cfg::NACC) & 1)) { dead = true; break; }
+          ok = tc::mbar_wait(&bars[PB_READY + s], par);
+          if (!ok) break;
           tc::tc_fence_after();
+          const uint64_t v = dV + (j & 1) * (Cfg::T16 >> 4);
+          const uint32_t aP = tmem + Cfg::COL_S + 128 * s;
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
-            tc::mma_f16_ts(tmem + Cfg::COL_O, tmem + Cfg::COL_S + 128 * acc + 64 * (kk >> 2) + 8 * (kk & 3),
-                           tc::smem_desc_sw128(aV + s * Cfg::T16 + kk * 2048, 128 * 128, 1024), ID, (j > 0 || kk > 0) ? 1u : 0u);
-          tc::mma_commit(&bars[PB_PVDONE + acc]);
-          tc::mma_commit(&bars[PB_VFREE + s]);
+            tc::mma_f16_ts(tmem + Cfg::COL_O, aP + 32 * (kk >> 1) + 8 * (kk & 1), v + kk * (2048 >> 4), ID, (j > 0 || kk > 0) ? 1u : 0u);
+          tc::mma_commit(&bars[PB_PVDONE + s]);
+          tc::mma_commit(&bars[PB_VFREE + (j & 1)]);
+          if (++s == 3) { s = 0; par ^= 1; }
         }
-        if (dead) fail();
+        if (!ok) fail();
       }
     }
-  } else if (warp >= 12) {
+  } else if (warp >= 20) {
     // ------------------------------ values to fp16 ------------------------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    constexpr int PIECES = D / 16;                 // 16-byte pieces of a row of codes
-    const int t = tid - 384, r8 = t & 7, pc = (t >> 3) & (PIECES - 1), r0 = (t >> 3) / PIECES * 8 + r8;   // rows r0 + 8 (16 / PIECES) i
-    constexpr int STEP = 8 * 16 / PIECES;
+    constexpr int PIECES = D / 16;             // 16-byte pieces of a row of codes
+    constexpr int N = PIECES / 4;              // a warp's lanes take eight rows and four pieces at a time: no two share a bank
+    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
     bool ok = true;
+    uint32_t s3 = 0;
     for (int j = 0; j < w.ntiles; ++j) {
-      const int sv = j % Cfg::NV, in = j % kInfo;
-      bool good = tc::mbar_wait(&bars[PB_V8FULL + sv], (j / Cfg::NV) & 1) && tc::mbar_wait(&bars[PB_INFO + in], (j / kInfo) & 1) && !*abort_flag;
-      if (good && j >= Cfg::NV) good = tc::mbar_wait(&bars[PB_VFREE + sv], ((j / Cfg::NV) - 1) & 1);
+      const int sv = j & 1;
+      bool good = tc::mbar_wait(&bars[PB_V8FULL + sv], (j >> 1) & 1);
+      if (good && j >= Cfg::NV) good = tc::mbar_wait(&bars[PB_VFREE + sv], ((j >> 1) - 1) & 1);
       ok = __all_sync(0xffffffffu, good);
       if (!ok) break;
-      const int pos = info[in].pos;
+      const int pos = info[j % kInfo].pos;
       const bool all = pos + 127 <= w.last && (pos > w.first - a.window || pos + 127 < a.sinks);   // every key is seen by some row
       const uint8_t* src = base + Cfg::OFF_V8 + sv * Cfg::T8;
       uint8_t* dst = base + Cfg::OFF_V + sv * Cfg::T16;
+      uint4 c[4 * N];
 #pragma unroll
-      for (int r = r0; r < 128; r += STEP) {
-        const int piece = D == 128 ? (pc ^ (r & 7)) : (pc ^ ((r >> 1) & 3));
-        uint4 c = *reinterpret_cast<const uint4*>(src + r * D + piece * 16);
-        if (!all) {   // whatever the ring or the page holds there must not meet the weight 0
-          const int key = pos + r;
-          if (!(key <= w.last && (key > w.first - a.window || key < a.sinks))) c = make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < 4 * N; ++i) {
+        const int r = rows0 + 8 * (i / N) + r8, pc = pc0 + 4 * (i % N);
+        c[i] = *reinterpret_cast<const uint4*>(src + r * D + (D == 128 ? (pc ^ r8) : (pc ^ ((r8 >> 1) & 3))) * 16);
+      }
+      if (!all) {   // whatever the ring or the page holds there must not meet the weight 0
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) {
+          const int key = pos + rows0 + 8 * (i / N) + r8;
+          if (!(key <= w.last && (key > w.first - a.window || key < a.sinks))) c[i] = make_uint4(0, 0, 0, 0);
         }
+      }
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const int r = rows0 + 8 * (i / N) + r8, pc = pc0 + 4 * (i % N);
         uint4 lo, hi;
-        lo.x = e4m3x2_to_f16x2(c.x & 0xffff); lo.y = e4m3x2_to_f16x2(c.x >> 16); lo.z = e4m3x2_to_f16x2(c.y & 0xffff); lo.w = e4m3x2_to_f16x2(c.y >> 16);
-        hi.x = e4m3x2_to_f16x2(c.z & 0xffff); hi.y = e4m3x2_to_f16x2(c.z >> 16); hi.z = e4m3x2_to_f16x2(c.w & 0xffff); hi.w = e4m3x2_to_f16x2(c.w >> 16);
-        uint8_t* row = dst + (pc >> 2) * (128 * 128) + r * 128;
-        *reinterpret_cast<uint4*>(row + (((2 * (pc & 3)) ^ r8) << 4)) = lo;
-        *reinterpret_cast<uint4*>(row + (((2 * (pc & 3) + 1) ^ r8) << 4)) = hi;
+        lo.x = e4m3x2_to_f16x2(c[i].x & 0xffff); lo.y = e4m3x2_to_f16x2(c[i].x >> 16); lo.z = e4m3x2_to_f16x2(c[i].y & 0xffff); lo.w = e4m3x2_to_f16x2(c[i].y >> 16);
+        hi.x = e4m3x2_to_f16x2(c[i].z & 0xffff); hi.y = e4m3x2_to_f16x2(c[i].z >> 16); hi.z = e4m3x2_to_f16x2(c[i].w & 0xffff); hi.w = e4m3x2_to_f16x2(c[i].w >> 16);
+        uint8_t* at = dst + (pc >> 2) * (128 * 128) + r * 128;
+        *reinterpret_cast<uint4*>(at + (((2 * (pc & 3)) ^ r8) << 4)) = lo;
+        *reinterpret_cast<uint4*>(at + (((2 * (pc & 3) + 1) ^ r8) << 4)) = hi;
       }
       tc::fence_proxy_async();
       __syncwarp();
       if (lane == 0) {
-        tc::mbar_arrive(&bars[PB_VFULL + sv]);
+        tc::mbar_arrive(&bars[PB_READY + s3]);
         tc::mbar_arrive(&bars[PB_V8FREE + sv]);
       }
+      if (++s3 == 3) s3 = 0;
     }
     if (!ok && lane == 0) fail();
   } else {
     // ------------------------------ q; softmax; results ------------------------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    const int seg = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;   // columns [32 seg, 32 seg + 32) of every tile
+    auto all_barrier = []() { asm volatile("bar.sync 5, 512;" ::: "memory"); };
     {
-      // two threads per row: power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
-      const int t = tid - 128, r = t >> 1, hf = t & 1;
-      constexpr int E = D / 2;
+      // four threads per row: power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
+      const int t = tid - 128, r = t >> 2, part = t & 3;
+      constexpr int E = D / 4;
       const bool live = r < w.rows;
       const int rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
-      const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + hf * E;
+      const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + part * E;
       uint32_t x[E / 2];
 #pragma unroll
       for (int i = 0; i < E / 2; ++i) x[i] = 0;
@@ -357,9 +410,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       for (int i = 0; i < E / 2; ++i) top2 = __vmaxu2(top2, x[i] & 0x7fff7fffu);
       uint32_t top = max(top2 & 0xffffu, top2 >> 16);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      const bool bad = top >= 0x7f80u;
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const bool nan = top >= 0x7f80u;
       const int e = max((int)(top >> 7), 10);
-      const float mul = bad ? 0.f : exp2i(134 - e);
+      const float mul = nan ? 0.f : exp2i(134 - e);
 #pragma unroll
       for (int i = 0; i < E / 16; ++i) {
         uint32_t hi[4], lo[4];
@@ -369,194 +423,197 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
             const uint32_t v = x[8 * i + 2 * q + z];
-            const float y0 = bad ? 0.f : __uint_as_float(v << 16) * mul, y1 = bad ? 0.f : __uint_as_float(v & 0xffff0000u) * mul;
+            const float y0 = nan ? 0.f : __uint_as_float(v << 16) * mul, y1 = nan ? 0.f : __uint_as_float(v & 0xffff0000u) * mul;
             const uint32_t h = to_e4m3x2(y0, y1);
             const float2 back = e4m3x2_to_float2(h);
             hi[q] |= h << (16 * z);
             lo[q] |= to_e4m3x2(y0 - back.x, y1 - back.y) << (16 * z);
           }
         }
-        const int piece = hf * (E / 16) + i;
+        const int piece = part * (E / 16) + i;
         uint8_t* at = base + Cfg::OFF_Q + r * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
-      if (hf == 0) s_cq[r] = bad ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
+      if (part == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
       tc::fence_proxy_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[PB_QFULL]);
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+      all_barrier();
     }
-    const int half = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    constexpr int HD = D / 2;
-    const uint32_t to_mine = tmem + lane_base + Cfg::COL_O + half * HD;   // this thread's share of O
+    constexpr int QD = D / 4;
+    const uint32_t to_mine = tmem + lane_base + Cfg::COL_O + seg * QD;   // this thread's share of O
+    const uint32_t ts0 = tmem + lane_base + Cfg::COL_S + seg * 32;       // and of S
+    // its share of O as 32-bit words (channels [QD seg, QD seg + QD))
+    auto load_o = [&](uint32_t (&r)[QD]) {
+      if constexpr (QD == 32) tc::tmem_ld32(to_mine, r); else tc::tmem_ld16(to_mine, r);
+      tc::tmem_wait_ld();
+    };
     const int pos_row = row < w.rows ? w.start + (w.row0 + row) / a.G : w.last;
     float cq = s_cq[row];
     bool bad = !(cq == cq);   // NaN rows are marked, not computed with
     if (bad) cq = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
     bool ok = true;
-    for (int j = 0; j < w.ntiles && ok; ++j) {
-      do {
-        ok = false;
-        const int acc = j % Cfg::NACC, in = j % kInfo;
-        KVM_WAIT(&bars[PB_INFO + in], (j / kInfo) & 1);
-        KVM_WAIT(&bars[PB_SFULL + acc], (j / Cfg::NACC) & 1);
+    uint32_t s = 0, par = 0;
+    for (int j = 0; j < w.ntiles; ++j) {
+      if (!tc::mbar_wait(&bars[PB_SFULL + s], par)) ok = false;
+      __syncwarp();
+      tc::tc_fence_after();
+      const uint32_t ts = ts0 + 128 * s;
+      uint32_t x[32];
+      tc::tmem_ld32(ts, x);
+      const PromptTile& ti = info[j % kInfo];
+      const int flags = ti.flags, pos = ti.pos;
+      Group gr[2] = {ti.g[2 * seg], ti.g[2 * seg + 1]};
+      tc::tmem_wait_ld();
+      if (flags || !(pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks))) {   // (uniform) masks, or NaN scales
+        const int key0 = pos + 32 * seg;
+        // bit c: the row sees column c.  j <= pos_row, and j > pos_row - window or j < sinks
+        auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // columns c < n
+        const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
+        uint32_t see = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          if (!(gr[g].ks == gr[g].ks)) {
+            const uint32_t cols = 0xffffu << (16 * g);
+            bad = bad || (see & cols);
+            see &= ~cols;
+          }
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] = (see >> c) & 1 ? x[c] : 0xff800000u;
+      }
+      float mx = -INFINITY, f[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        f[g] = fmaxf(cq * gr[g].ks, 1.17549435e-38f);   // (never 0 or NaN: a masked column is -inf)
+        float m = __uint_as_float(x[16 * g]), m2 = __uint_as_float(x[16 * g + 1]);
+#pragma unroll
+        for (int c = 2; c < 14; c += 4) {
+          m = tc::fmax3(m, __uint_as_float(x[16 * g + c]), __uint_as_float(x[16 * g + c + 1]));
+          m2 = tc::fmax3(m2, __uint_as_float(x[16 * g + c + 2]), __uint_as_float(x[16 * g + c + 3]));
+        }
+        m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
+        mx = fmaxf(mx, fmaf(fmaxf(m, m2), f[g], gr[g].vr));
+      }
+      // the maximum of the row's other columns
+      float* x4 = xm + (j & 1) * 512 + row * 4;
+      x4[seg] = mx;
+      ok = row_barrier(1 + quarter, ok);
+      if (!ok) break;
+      const float4 m4 = *reinterpret_cast<const float4*>(x4);
+      const float mnew = fmaxf(m_run, fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w)));
+      if (j == 0) {
+        m_run = mnew;
+      } else if (__any_sync(0xffffffffu, mnew > m_run + 8.0f)) {   // the same decision in all warps that share these rows
+        // all earlier P V products must have landed before O is touched (commits complete in order)
+        if (!tc::mbar_wait(&bars[PB_PVDONE + (s == 0 ? 2 : s - 1)], s == 0 ? par ^ 1 : par)) ok = false;
         __syncwarp();
         tc::tc_fence_after();
-        const uint32_t ts = tmem + lane_base + Cfg::COL_S + 128 * acc + half * 64;
-        float x[64];
+        const float corr = (m_run == -INFINITY) ? 0.f : tc::ex2_approx(m_run - mnew);
+        l_run *= corr;
+        m_run = mnew;
+        uint32_t r[QD];
+        load_o(r);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t r[32];
-          tc::tmem_ld32(ts + c * 32, r);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) x[c * 32 + i] = __uint_as_float(r[i]);
-        }
-        tc::tmem_wait_ld();
-        const int pos = info[in].pos, flags = info[in].flags;
-        Group g[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = info[in].g[half * 4 + i];
-        const bool all = pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks);   // (uniform) all rows see all keys
-        if (!all || flags) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool nan = !(g[i].ks == g[i].ks);
-            if (nan) g[i].ks = 0.f;
-#pragma unroll
-            for (int c = 16 * i; c < 16 * i + 16; ++c) {
-              const bool see = sees(pos_row, pos + half * 64 + c, a.window, a.sinks);
-              bad = bad || (see && nan);
-              x[c] = see && !nan ? x[c] : -INFINITY;
-            }
-            if (nan) g[i].ks = 1.f;
-          }
-        }
-        float mx = -INFINITY;
-        float cg[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          cg[i] = fmaxf(cq * g[i].ks, 1.17549435e-38f);   // (never 0: a masked column is -inf)
-          float m2[2] = {x[16 * i], x[16 * i + 1]};
-#pragma unroll
-          for (int c = 2; c < 16; c += 2) { m2[0] = fmaxf(m2[0], x[16 * i + c]); m2[1] = fmaxf(m2[1], x[16 * i + c + 1]); }
-          const float m = fmaxf(m2[0], m2[1]);
-          mx = fmaxf(mx, fmaf(m, cg[i], g[i].vr));
-        }
-        xm[((j & 1) * 2 + half) * 128 + row] = mx;
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bars[PB_XM + (j & 1)]);
-        KVM_WAIT(&bars[PB_XM + (j & 1)], (j >> 1) & 1);
-        mx = fmaxf(mx, xm[((j & 1) * 2 + (1 - half)) * 128 + row]);
-        const float mnew = fmaxf(m_run, mx);
-        if (j == 0) {
-          m_run = mnew;
-        } else if (__any_sync(0xffffffffu, mnew > m_run + 8.0f)) {   // the same decision in both warps that share these rows
-          KVM_WAIT(&bars[PB_PVDONE + (j - 1) % Cfg::NACC], ((j - 1) / Cfg::NACC) & 1);
-          __syncwarp();
-          tc::tc_fence_after();
-          const float corr = (m_run == -INFINITY) ? 0.f : tc::ex2_approx(m_run - mnew);
-          l_run *= corr;
-          m_run = mnew;
-#pragma unroll
-          for (int c = 0; c < HD / 32; ++c) {
-            uint32_t r[32];
-            tc::tmem_ld32(to_mine + c * 32, r);
-            tc::tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
-            tc::tmem_st32(to_mine + c * 32, r);
-          }
-          tc::tmem_wait_st();
-        }
-        const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
-        uint32_t wd[32];
-        float lsum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float add = neg_m + g[i].vr;
-          float l0 = 0.f, l1 = 0.f;
-          const float cc = cg[i];
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const int at = 16 * i + 2 * c;
-            const float y0 = fmaf(x[at], cc, add), y1 = fmaf(x[at + 1], cc, add);
-            const float p0 = tc::ex2_approx(y0), p1 = (c & 1) ? tc::ex2_poly(y1) : tc::ex2_approx(y1);
-            l0 += p0; l1 += p1;
-            const __half2 h = __floats2half2_rn(p0, p1);
-            wd[8 * i + c] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-          lsum = fmaf(l0 + l1, g[i].back, lsum);
-        }
-        if (flags & 2) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (g[i].drop != 0.f) {
-#pragma unroll
-              for (int c = 0; c < 8; ++c) wd[8 * i + c] = 0;
-            }
-        }
-        tc::tmem_st32(ts, wd);
+        for (int i = 0; i < QD; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+        if constexpr (QD == 32) tc::tmem_st32(to_mine, r); else tc::tmem_st16(to_mine, r);
         tc::tmem_wait_st();
-        l_run += lsum;
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bars[PB_PFULL + acc]);
-        ok = true;
-      } while (false);
+      }
+      const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+      uint32_t wd[16];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float add = neg_m + gr[g].vr;
+        const uint64_t f2 = pack2(f[g], f[g]), a2 = pack2(add, add);
+        uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const uint64_t y = fma2(pack2(__uint_as_float(x[16 * g + 2 * c]), __uint_as_float(x[16 * g + 2 * c + 1])), f2, a2);
+          float p0, p1;
+          // a quarter of the exponentials on the FMA pipe instead of the special-function unit (P is rounded to fp16 anyway: the
+          // polynomial's relative error is below 5e-5)
+          if ((c & 3) == 3) {
+            ex2_poly2(y, p0, p1);
+          } else {
+            unpack2(y, p0, p1);
+            p0 = tc::ex2_approx(p0);
+            p1 = tc::ex2_approx(p1);
+          }
+          const uint64_t p2 = pack2(p0, p1);
+          if (c & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
+          const __half2 h2 = __floats2half2_rn(p0, p1);
+          wd[8 * g + c] = *reinterpret_cast<const uint32_t*>(&h2);
+        }
+        float l0, l1;
+        unpack2(add2(s0, s1), l0, l1);
+        l_run = fmaf(l0 + l1, gr[g].back, l_run);
+        if (flags & 2) {
+          if (gr[g].drop != 0.f) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) wd[8 * g + c] = 0;
+          }
+        }
+      }
+      tc::tmem_st16(ts, wd);
+      tc::tmem_wait_st();
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars[PB_READY + s]);
+      if (++s == 3) { s = 0; par ^= 1; }
     }
-    // the row sum is the sum of the halves' sums (through the exchange of the maxima, idle by now); half h stores channels [h D/2, (h+1) D/2)
     if (ok) {
-      ok = tc::mbar_wait(&bars[PB_PVDONE + (w.ntiles - 1) % Cfg::NACC], ((w.ntiles - 1) / Cfg::NACC) & 1);
-      if (!ok) fail();
-      tc::tc_fence_after();
+      const int last = (w.ntiles - 1) % 3;
+      ok = tc::mbar_wait(&bars[PB_PVDONE + last], ((w.ntiles - 1) / 3) & 1);
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");   // (every thread has read the last maxima)
-    xm[half * 128 + row] = l_run;
-    xm[(2 + half) * 128 + row] = bad ? 1.f : 0.f;
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    const bool good = ok && !*abort_flag;
-    const float l = l_run + xm[(1 - half) * 128 + row];
-    bad = bad || xm[(3 - half) * 128 + row] != 0.f;
-    const float nan = __int_as_float(0x7fc00000);
-    uint8_t* stage = base + Cfg::OFF_K;   // (the key and value tiles are idle)
+    if (!ok) fail();
     __syncwarp();
+    tc::tc_fence_after();
+    // the row sum is the sum of the quarters' sums (through the exchange of the maxima)
+    all_barrier();   // (every thread has read the last maxima)
+    xm[row * 4 + seg] = l_run;
+    xm[512 + row * 4 + seg] = bad ? 1.f : 0.f;
+    all_barrier();
+    const bool good = ok && !*abort_flag;
+    const float4 l4 = *reinterpret_cast<const float4*>(xm + row * 4), b4 = *reinterpret_cast<const float4*>(xm + 512 + row * 4);
+    const float l = (l4.x + l4.y) + (l4.z + l4.w), nan = __int_as_float(0x7fc00000);
+    bad = b4.x + b4.y + b4.z + b4.w != 0.f;
+    uint8_t* stage = base + Cfg::OFF_Q;   // (the queries are not needed any more)
+    const int rg = w.row0 + row, tokr = rg / a.G, hqr = w.hk * a.G + rg - tokr * a.G;
+    uint32_t r[QD];
+    __syncwarp();
+    if (good) load_o(r);
     if (w.parts == 1) {
       const float inv = bad ? nan : exp2i(vbase) / l;
-      if (args.out_vec) {
+      uint32_t h[QD / 2];
+#pragma unroll
+      for (int i = 0; i < QD / 2; ++i) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * i]) * inv, __uint_as_float(r[2 * i + 1]) * inv);
+        h[i] = *reinterpret_cast<const uint32_t*>(&v);
+      }
+      if (args.out_vec) {   // rows go through shared memory, so that the global stores are whole rows of 16-byte pieces
         if (good) {
 #pragma unroll
-          for (int c = 0; c < HD / 32; ++c) {
-            uint32_t r[32];
-            tc::tmem_ld32(to_mine + c * 32, r);
-            tc::tmem_wait_ld();
-            stage_row32<D>(stage, row, half * (HD / 32) + c, r, inv);
-          }
+          for (int i = 0; i < QD / 8; ++i) *stage_chunk<D>(stage, row, seg * (QD / 8) + i) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
         }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        all_barrier();
         if (good) {
           constexpr int CPR = D / 8, RPI = 32 / CPR;
-          const int k = lane % CPR;
-          for (int r = (warp - 4) * 16 + lane / CPR; r < (warp - 3) * 16; r += RPI) {
-            if (r >= w.rows) continue;
-            const int rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
-            *reinterpret_cast<uint4*>(a.out + w.b * a.so[0] + hq * a.so[1] + tokq * a.so[2] + k * 8) = *stage_chunk<D>(stage, r, k);
+          const int k = lane % CPR, w16 = warp - 4;
+          for (int i = w16 * 8 + lane / CPR; i < w16 * 8 + 8; i += RPI) {
+            if (i >= w.rows) continue;
+            const int ri = w.row0 + i, tok = ri / a.G, hq = w.hk * a.G + ri - tok * a.G;
+            *reinterpret_cast<uint4*>(a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + k * 8) = *stage_chunk<D>(stage, i, k);
           }
         }
-      } else if (good) {
-        const int rg = w.row0 + row, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
-        __nv_bfloat16* orow = a.out + w.b * a.so[0] + hq * a.so[1] + tokq * a.so[2] + half * HD;
+      } else if (good && row < w.rows) {
+        __nv_bfloat16* orow = a.out + w.b * a.so[0] + hqr * a.so[1] + tokr * a.so[2] + seg * QD;
 #pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-          uint32_t r[32];
-          tc::tmem_ld32(to_mine + c * 32, r);
-          tc::tmem_wait_ld();
-          if (row < w.rows) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) orow[c * 32 + i] = __float2bfloat16_rn(__uint_as_float(r[i]) * inv);
-          }
+        for (int i = 0; i < QD / 2; ++i) {
+          const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&h[i]);
+          orow[2 * i] = v.x;
+          orow[2 * i + 1] = v.y;
         }
       }
     } else if (good) {
@@ -564,20 +621,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
       const float unit = bad ? nan : exp2i(vbase);
 #pragma unroll
-      for (int c = 0; c < HD / 32; ++c) {
-        uint32_t r[32];
-        tc::tmem_ld32(to_mine + c * 32, r);
-        tc::tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) mine[(half * HD + c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;
-      }
-      if (half == 0) {
+      for (int i = 0; i < QD; ++i) mine[(seg * QD + i) * 128 + row] = __uint_as_float(r[i]) * unit;
+      if (seg == 0) {
         mine[D * 128 + row] = m_run;
         mine[(D + 1) * 128 + row] = bad ? nan : l;
       }
     }
   }
-#undef KVM_WAIT
   tc::tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -635,7 +685,7 @@ __global__ void __launch_bounds__(256) prompt_combine_kernel(const __grid_consta
 
 // (row tiles of 128, key splits) of a call.  Few row tiles: as many splits as fill the SMs.
 static void prompt_plan(int64_t units, int64_t rows, int64_t tiles, int& qtiles, int& nsplit) {
-  qtiles = (int)((rows + 127) / 128);
+  qtiles = (int)((rows + kRows - 1) / kRows);
   const int64_t ctas = units * qtiles;
   nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({148 / ctas, (tiles + kSplitTiles - 1) / kSplitTiles, kMaxSplits}));
 }
@@ -655,7 +705,7 @@ static kvm_status_t launch_prompt_d(const PromptArgs& args, const CUtensorMap& m
     if (cudaFuncSetAttribute(prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptCfg<D>::SMEM) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
     if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  prompt_kernel<D><<<dim3((unsigned)(args.units * args.qtiles), args.nsplit), 512, PromptCfg<D>::SMEM, s>>>(mapK, mapV, args);
+  prompt_kernel<D><<<dim3((unsigned)(args.units * args.qtiles), args.nsplit), kThreads, PromptCfg<D>::SMEM, s>>>(mapK, mapV, args);
   if (args.nsplit > 1) prompt_combine_kernel<D><<<args.units * args.qtiles, 256, 0, s>>>(args);
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
