@@ -11,8 +11,11 @@
 // (relative to the largest of the CTA's visible blocks, 2^vbase) and taken out of the row sum again, 16 columns (the smallest page) at a time.
 //   warp 0       producer: page numbers and scales ahead, TMA into rings of three key tiles and two value tiles
 //   warp 1       issues S into three accumulators, warp 2 issues P V (one thread each), warp 3 idles
-//   warps 4-19   softmax: four threads per row, 32 columns of every tile each; P goes over the columns of S that the thread has read
-//   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
+//   warps 4-15   softmax: tile j belongs to the four warps of group j % 3, a thread per row; S is read from tensor memory twice, 32 columns at a
+//                time (maximum, then weights), and P goes over columns that have been read.  A scheduler of the SM thus holds three warps that
+//                work on three different tiles of the same rows, one in its maxima while another is in its exponentials; all they
+//                hand on from tile to tile is the reference of each row (with which O is scaled), decided after the maximum.
+//   warps 16-19  value codes -> fp16, swizzled as the MMA reads them
 // With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.
 //
 #include <algorithm>
@@ -44,7 +47,7 @@ struct PromptTile {
 };
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
 constexpr int kRows = 128; // rows of a CTA
-constexpr int kThreads = 768;
+constexpr int kThreads = 640;
 
 template <int D>
 struct PromptCfg {
@@ -55,16 +58,18 @@ struct PromptCfg {
   static constexpr int OFF_V8 = OFF_K + NK * T8;
   static constexpr int OFF_V = OFF_V8 + NV * T8;
   static constexpr int OFF_INFO = OFF_V + NV * T16;
-  static constexpr int OFF_XM = OFF_INFO + kInfo * (int)sizeof(PromptTile);   // float4 [2][128]: maxima of the row's quarters, by tile parity
-  static constexpr int OFF_CQ = OFF_XM + 2 * 128 * 16;                        // float [128]
+  static constexpr int OFF_M = OFF_INFO + kInfo * (int)sizeof(PromptTile);    // float [128]: references of the rows
+  static constexpr int OFF_L = OFF_M + 128 * 4;                               // float [3][128]: sums of the groups, [3][128]: NaN marks
+  static constexpr int OFF_CQ = OFF_L + 6 * 128 * 4;                          // float [128]
   static constexpr int OFF_BAR = OFF_CQ + 128 * 4;
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static constexpr int SMEM = (OFF_BAR + 512 + 1024) > 120 * 1024 ? (OFF_BAR + 512 + 1024) : 120 * 1024;
   static constexpr uint32_t COL_S = 0, COL_O = 384;      // S / P accumulator i at 128 i
 };
-// PB_READY: P of the tile is in tensor memory (16 softmax warps) and its values are in fp16 (4 converting warps)
+// PB_READY: P of the tile is in tensor memory (4 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
+// 32 rows are decided for a tile, [row quarter][tile % 3]
 enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 8, PB_VFREE = 10, PB_SFULL = 12, PB_READY = 15, PB_PVDONE = 18, PB_QFULL = 21,
-       PB_COUNT = 22 };
+       PB_REF = 22, PB_LAST = 34, PB_COUNT = 35 };
 
 // What a CTA does: its rows and its key tiles.  (Also what the merge needs to know.)
 struct PromptWork {
@@ -92,18 +97,6 @@ __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int
   w.jb = sp * per;
   w.ntiles = min(per, w.t.n - w.jb);
   return w.ntiles > 0;
-}
-// Barrier of the four warps that share 32 rows, which also tells whether all are well.
-__device__ __forceinline__ bool row_barrier(int id, bool ok) {
-  uint32_t r;
-  __syncwarp();
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.and.aligned.pred q, %2, 128, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r) : "r"(ok ? 1u : 0u), "r"(id) : "memory");
-  return r != 0;
 }
 // two fp32 operations in one instruction
 __device__ __forceinline__ uint64_t pack2(float x, float y) {
@@ -149,12 +142,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   PromptTile* info = reinterpret_cast<PromptTile*>(base + Cfg::OFF_INFO);
-  float* xm = reinterpret_cast<float*>(base + Cfg::OFF_XM);
+  float* s_m = reinterpret_cast<float*>(base + Cfg::OFF_M);
+  float* s_l = reinterpret_cast<float*>(base + Cfg::OFF_L);
   float* s_cq = reinterpret_cast<float*>(base + Cfg::OFF_CQ);
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + PB_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [24]
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [20]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   PromptWork w;
   if (!prompt_work(args, blockIdx.x, blockIdx.y, w)) return;
@@ -165,7 +159,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::mbar_init(&bars[PB_KFULL + s], 1);
       tc::mbar_init(&bars[PB_KFREE + s], 1);
       tc::mbar_init(&bars[PB_SFULL + s], 1);
-      tc::mbar_init(&bars[PB_READY + s], 16 + 4);
+      tc::mbar_init(&bars[PB_READY + s], 4 + 4);
       tc::mbar_init(&bars[PB_PVDONE + s], 1);
     }
     for (int s = 0; s < 2; ++s) {
@@ -173,7 +167,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::mbar_init(&bars[PB_V8FREE + s], 4);
       tc::mbar_init(&bars[PB_VFREE + s], 1);
     }
-    tc::mbar_init(&bars[PB_QFULL], 16);
+    for (int s = 0; s < 12; ++s) tc::mbar_init(&bars[PB_REF + s], 1);
+    tc::mbar_init(&bars[PB_QFULL], 8);
+    tc::mbar_init(&bars[PB_LAST], 1);
     *abort_flag = 0;
     tc::fence_barrier_init();
   }
@@ -324,19 +320,20 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           const uint32_t aP = tmem + Cfg::COL_S + 128 * s;
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
-            tc::mma_f16_ts(tmem + Cfg::COL_O, aP + 32 * (kk >> 1) + 8 * (kk & 1), v + kk * (2048 >> 4), ID, (j > 0 || kk > 0) ? 1u : 0u);
+            tc::mma_f16_ts(tmem + Cfg::COL_O, aP + 8 * kk, v + kk * (2048 >> 4), ID, (j > 0 || kk > 0) ? 1u : 0u);
           tc::mma_commit(&bars[PB_PVDONE + s]);
           tc::mma_commit(&bars[PB_VFREE + (j & 1)]);
           if (++s == 3) { s = 0; par ^= 1; }
         }
         if (!ok) fail();
+        tc::mma_commit(&bars[PB_LAST]);   // (a barrier of its own: a group whose tiles are done may be more than a phase ahead of PB_PVDONE)
       }
     }
-  } else if (warp >= 20) {
+  } else if (warp >= 16) {
     // ------------------------------ values to fp16 ------------------------------
     constexpr int PIECES = D / 16;             // 16-byte pieces of a row of codes
     constexpr int N = PIECES / 4;              // a warp's lanes take eight rows and four pieces at a time: no two share a bank
-    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
+    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 16) * 32;
     bool ok = true;
     uint32_t s3 = 0;
     for (int j = 0; j < w.ntiles; ++j) {
@@ -383,12 +380,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!ok && lane == 0) fail();
   } else {
     // ------------------------------ q; softmax; results ------------------------------
-    const int seg = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;   // columns [32 seg, 32 seg + 32) of every tile
-    auto all_barrier = []() { asm volatile("bar.sync 5, 512;" ::: "memory"); };
-    {
-      // four threads per row: power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
-      const int t = tid - 128, r = t >> 2, part = t & 3;
-      constexpr int E = D / 4;
+    const int group = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    auto all_barrier = []() { asm volatile("bar.sync 1, 384;" ::: "memory"); };
+    if (group < 2) {
+      // two threads per row: power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
+      const int t = tid - 128, r = t >> 1, part = t & 1;
+      constexpr int E = D / 2;
       const bool live = r < w.rows;
       const int rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
       const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + part * E;
@@ -410,7 +407,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       for (int i = 0; i < E / 2; ++i) top2 = __vmaxu2(top2, x[i] & 0x7fff7fffu);
       uint32_t top = max(top2 & 0xffffu, top2 >> 16);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const bool nan = top >= 0x7f80u;
       const int e = max((int)(top >> 7), 10);
       const float mul = nan ? 0.f : exp2i(134 - e);
@@ -439,192 +435,196 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::fence_proxy_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[PB_QFULL]);
-      all_barrier();
     }
-    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    constexpr int QD = D / 4;
-    const uint32_t to_mine = tmem + lane_base + Cfg::COL_O + seg * QD;   // this thread's share of O
-    const uint32_t ts0 = tmem + lane_base + Cfg::COL_S + seg * 32;       // and of S
-    // its share of O as 32-bit words (channels [QD seg, QD seg + QD))
-    auto load_o = [&](uint32_t (&r)[QD]) {
-      if constexpr (QD == 32) tc::tmem_ld32(to_mine, r); else tc::tmem_ld16(to_mine, r);
-      tc::tmem_wait_ld();
-    };
+    all_barrier();
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = lanes + Cfg::COL_O, ts = lanes + Cfg::COL_S + 128 * group;
     const int pos_row = row < w.rows ? w.start + (w.row0 + row) / a.G : w.last;
     float cq = s_cq[row];
     bool bad = !(cq == cq);   // NaN rows are marked, not computed with
     if (bad) cq = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_ref = -INFINITY, l_run = 0.f;   // l_run is relative to 2^m_ref
     bool ok = true;
-    uint32_t s = 0, par = 0;
-    for (int j = 0; j < w.ntiles; ++j) {
-      if (!tc::mbar_wait(&bars[PB_SFULL + s], par)) ok = false;
+    uint32_t par = 0;
+#pragma unroll 1
+    for (int j = group; j < w.ntiles; j += 3, par ^= 1) {
+      if (!tc::mbar_wait(&bars[PB_SFULL + group], par)) ok = false;
       __syncwarp();
       tc::tc_fence_after();
-      const uint32_t ts = ts0 + 128 * s;
-      uint32_t x[32];
-      tc::tmem_ld32(ts, x);
       const PromptTile& ti = info[j % kInfo];
       const int flags = ti.flags, pos = ti.pos;
-      Group gr[2] = {ti.g[2 * seg], ti.g[2 * seg + 1]};
-      tc::tmem_wait_ld();
-      if (flags || !(pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks))) {   // (uniform) masks, or NaN scales
-        const int key0 = pos + 32 * seg;
-        // bit c: the row sees column c.  j <= pos_row, and j > pos_row - window or j < sinks
-        auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // columns c < n
-        const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
-        uint32_t see = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
+      const bool slow = flags || !(pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks));   // (uniform) masks, or NaN scales
+      // S of columns 32 c .. 32 c + 31; what the row does not see as -inf
+      auto load = [&](int c, uint32_t (&x)[32]) {
+        tc::tmem_ld32(ts + 32 * c, x);
+        tc::tmem_wait_ld();
+        if (slow) {
+          const int key0 = pos + 32 * c;
+          // bit i: the row sees column i.  j <= pos_row, and j > pos_row - window or j < sinks
+          auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // columns i < n
+          const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
+          uint32_t see = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
-          if (!(gr[g].ks == gr[g].ks)) {
-            const uint32_t cols = 0xffffu << (16 * g);
-            bad = bad || (see & cols);
-            see &= ~cols;
+          for (int g = 0; g < 2; ++g) {
+            const float ks = ti.g[2 * c + g].ks;
+            if (!(ks == ks)) {
+              const uint32_t cols = 0xffffu << (16 * g);
+              bad = bad || (see & cols);
+              see &= ~cols;
+            }
           }
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = (see >> c) & 1 ? x[c] : 0xff800000u;
-      }
-      float mx = -INFINITY, f[2];
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        f[g] = fmaxf(cq * gr[g].ks, 1.17549435e-38f);   // (never 0 or NaN: a masked column is -inf)
-        float m = __uint_as_float(x[16 * g]), m2 = __uint_as_float(x[16 * g + 1]);
-#pragma unroll
-        for (int c = 2; c < 14; c += 4) {
-          m = tc::fmax3(m, __uint_as_float(x[16 * g + c]), __uint_as_float(x[16 * g + c + 1]));
-          m2 = tc::fmax3(m2, __uint_as_float(x[16 * g + c + 2]), __uint_as_float(x[16 * g + c + 3]));
+          for (int i = 0; i < 32; ++i) x[i] = (see >> i) & 1 ? x[i] : 0xff800000u;
         }
-        m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
-        mx = fmaxf(mx, fmaf(fmaxf(m, m2), f[g], gr[g].vr));
+      };
+      float mx = -INFINITY;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t x[32];
+        load(c, x);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const Group gr = ti.g[2 * c + g];
+          float m = __uint_as_float(x[16 * g]), m2 = __uint_as_float(x[16 * g + 1]);
+#pragma unroll
+          for (int i = 2; i < 14; i += 4) {
+            m = tc::fmax3(m, __uint_as_float(x[16 * g + i]), __uint_as_float(x[16 * g + i + 1]));
+            m2 = tc::fmax3(m2, __uint_as_float(x[16 * g + i + 2]), __uint_as_float(x[16 * g + i + 3]));
+          }
+          m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
+          // (the factor is never 0 or NaN: a masked column is -inf)
+          mx = fmaxf(mx, fmaf(fmaxf(m, m2), fmaxf(cq * gr.ks, 1.17549435e-38f), gr.vr));
+        }
       }
-      // the maximum of the row's other columns
-      float* x4 = xm + (j & 1) * 512 + row * 4;
-      x4[seg] = mx;
-      ok = row_barrier(1 + quarter, ok);
-      if (!ok) break;
-      const float4 m4 = *reinterpret_cast<const float4*>(x4);
-      const float mnew = fmaxf(m_run, fmaxf(fmaxf(m4.x, m4.y), fmaxf(m4.z, m4.w)));
-      if (j == 0) {
-        m_run = mnew;
-      } else if (__any_sync(0xffffffffu, mnew > m_run + 8.0f)) {   // the same decision in all warps that share these rows
-        // all earlier P V products must have landed before O is touched (commits complete in order)
-        if (!tc::mbar_wait(&bars[PB_PVDONE + (s == 0 ? 2 : s - 1)], s == 0 ? par ^ 1 : par)) ok = false;
+      // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
+      float m = -INFINITY;
+      if (j > 0) {
+        const int before = j - 1, gb = group == 0 ? 2 : group - 1;
+        if (!tc::mbar_wait(&bars[PB_REF + quarter * 3 + gb], (before / 3) & 1)) ok = false;
         __syncwarp();
-        tc::tc_fence_after();
-        const float corr = (m_run == -INFINITY) ? 0.f : tc::ex2_approx(m_run - mnew);
-        l_run *= corr;
-        m_run = mnew;
-        uint32_t r[QD];
-        load_o(r);
-#pragma unroll
-        for (int i = 0; i < QD; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
-        if constexpr (QD == 32) tc::tmem_st32(to_mine, r); else tc::tmem_st16(to_mine, r);
-        tc::tmem_wait_st();
+        m = s_m[row];
       }
-      const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
-      uint32_t wd[16];
+      if (__any_sync(0xffffffffu, mx > m + 8.0f || (j == 0))) {
+        const float mnew = fmaxf(m, mx);
+        if (j > 0) {
+          // all earlier P V products must have landed before O is touched
+          const int gb = group == 0 ? 2 : group - 1;
+          if (!tc::mbar_wait(&bars[PB_PVDONE + gb], ((j - 1) / 3) & 1)) ok = false;
+          __syncwarp();
+          tc::tc_fence_after();
+          const float corr = (m == -INFINITY) ? 0.f : tc::ex2_approx(m - mnew);
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t r[32];
+            tc::tmem_ld32(to + c * 32, r);
+            tc::tmem_wait_ld();
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const float add = neg_m + gr[g].vr;
-        const uint64_t f2 = pack2(f[g], f[g]), a2 = pack2(add, add);
-        uint64_t s0 = 0, s1 = 0;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const uint64_t y = fma2(pack2(__uint_as_float(x[16 * g + 2 * c]), __uint_as_float(x[16 * g + 2 * c + 1])), f2, a2);
-          float p0, p1;
-          // a quarter of the exponentials on the FMA pipe instead of the special-function unit (P is rounded to fp16 anyway: the
-          // polynomial's relative error is below 5e-5)
-          if ((c & 3) == 3) {
-            ex2_poly2(y, p0, p1);
-          } else {
-            unpack2(y, p0, p1);
-            p0 = tc::ex2_approx(p0);
-            p1 = tc::ex2_approx(p1);
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+            tc::tmem_st32(to + c * 32, r);
           }
-          const uint64_t p2 = pack2(p0, p1);
-          if (c & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
-          const __half2 h2 = __floats2half2_rn(p0, p1);
-          wd[8 * g + c] = *reinterpret_cast<const uint32_t*>(&h2);
+          tc::tmem_wait_st();
         }
-        float l0, l1;
-        unpack2(add2(s0, s1), l0, l1);
-        l_run = fmaf(l0 + l1, gr[g].back, l_run);
-        if (flags & 2) {
-          if (gr[g].drop != 0.f) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) wd[8 * g + c] = 0;
-          }
-        }
+        m = mnew;
+        s_m[row] = m;
       }
-      tc::tmem_st16(ts, wd);
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars[PB_REF + quarter * 3 + group]);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      l_run = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m);
+      m_ref = m;
+      const float neg_m = (m == -INFINITY) ? 0.f : -m;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t x[32], wd[16];
+        load(c, x);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const Group gr = ti.g[2 * c + g];
+          const float f = fmaxf(cq * gr.ks, 1.17549435e-38f), add = neg_m + gr.vr;
+          const uint64_t f2 = pack2(f, f), a2 = pack2(add, add);
+          uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint64_t y = fma2(pack2(__uint_as_float(x[16 * g + 2 * i]), __uint_as_float(x[16 * g + 2 * i + 1])), f2, a2);
+            float p0, p1;
+            // a quarter of the exponentials on the FMA pipe instead of the special-function unit (P is rounded to fp16 anyway: the
+            // polynomial's relative error is below 5e-5)
+            if ((i & 3) == 3) {
+              ex2_poly2(y, p0, p1);
+            } else {
+              unpack2(y, p0, p1);
+              p0 = tc::ex2_approx(p0);
+              p1 = tc::ex2_approx(p1);
+            }
+            const uint64_t p2 = pack2(p0, p1);
+            if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
+            const __half2 h2 = __floats2half2_rn(p0, p1);
+            wd[8 * g + i] = *reinterpret_cast<const uint32_t*>(&h2);
+          }
+          float l0, l1;
+          unpack2(add2(s0, s1), l0, l1);
+          l_run = fmaf(l0 + l1, gr.back, l_run);
+          if (flags & 2) {
+            if (gr.drop != 0.f) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) wd[8 * g + i] = 0;
+            }
+          }
+        }
+        tc::tmem_st16(ts + 16 * c, wd);   // (columns that have been read)
+      }
       tc::tmem_wait_st();
       tc::tc_fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&bars[PB_READY + s]);
-      if (++s == 3) { s = 0; par ^= 1; }
+      if (lane == 0) tc::mbar_arrive(&bars[PB_READY + group]);
     }
-    if (ok) {
-      const int last = (w.ntiles - 1) % 3;
-      ok = tc::mbar_wait(&bars[PB_PVDONE + last], ((w.ntiles - 1) / 3) & 1);
-    }
+    if (ok) ok = tc::mbar_wait(&bars[PB_LAST], 0);
     if (!ok) fail();
     __syncwarp();
     tc::tc_fence_after();
-    // the row sum is the sum of the quarters' sums (through the exchange of the maxima)
-    all_barrier();   // (every thread has read the last maxima)
-    xm[row * 4 + seg] = l_run;
-    xm[512 + row * 4 + seg] = bad ? 1.f : 0.f;
+    // (the last P V is done: every reference has been decided) the row sum is the sum of the groups' sums
+    const float m_end = s_m[row];
+    s_l[group * 128 + row] = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m_end);
+    s_l[(3 + group) * 128 + row] = bad ? 1.f : 0.f;
     all_barrier();
     const bool good = ok && !*abort_flag;
-    const float4 l4 = *reinterpret_cast<const float4*>(xm + row * 4), b4 = *reinterpret_cast<const float4*>(xm + 512 + row * 4);
-    const float l = (l4.x + l4.y) + (l4.z + l4.w), nan = __int_as_float(0x7fc00000);
-    bad = b4.x + b4.y + b4.z + b4.w != 0.f;
+    const float l = s_l[row] + s_l[128 + row] + s_l[256 + row], nan = __int_as_float(0x7fc00000);
+    bad = s_l[384 + row] + s_l[512 + row] + s_l[640 + row] != 0.f;
     uint8_t* stage = base + Cfg::OFF_Q;   // (the queries are not needed any more)
     const int rg = w.row0 + row, tokr = rg / a.G, hqr = w.hk * a.G + rg - tokr * a.G;
-    uint32_t r[QD];
-    __syncwarp();
-    if (good) load_o(r);
-    if (w.parts == 1) {
-      const float inv = bad ? nan : exp2i(vbase) / l;
-      uint32_t h[QD / 2];
+    const float unit = bad ? nan : w.parts == 1 ? exp2i(vbase) / l : exp2i(vbase);
+    if (good) {
+#pragma unroll 1
+      for (int c = group; c < D / 32; c += 3) {   // 32 channels at a time
+        uint32_t r[32];
+        __syncwarp();
+        tc::tmem_ld32(to + c * 32, r);
+        tc::tmem_wait_ld();
+        if (w.parts > 1) {   // partial result: O (in units of 2^m_end), m_end and the sum, [channel][row]
+          float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
 #pragma unroll
-      for (int i = 0; i < QD / 2; ++i) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * i]) * inv, __uint_as_float(r[2 * i + 1]) * inv);
-        h[i] = *reinterpret_cast<const uint32_t*>(&v);
-      }
-      if (args.out_vec) {   // rows go through shared memory, so that the global stores are whole rows of 16-byte pieces
-        if (good) {
-#pragma unroll
-          for (int i = 0; i < QD / 8; ++i) *stage_chunk<D>(stage, row, seg * (QD / 8) + i) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-        }
-        all_barrier();
-        if (good) {
-          constexpr int CPR = D / 8, RPI = 32 / CPR;
-          const int k = lane % CPR, w16 = warp - 4;
-          for (int i = w16 * 8 + lane / CPR; i < w16 * 8 + 8; i += RPI) {
-            if (i >= w.rows) continue;
-            const int ri = w.row0 + i, tok = ri / a.G, hq = w.hk * a.G + ri - tok * a.G;
-            *reinterpret_cast<uint4*>(a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + k * 8) = *stage_chunk<D>(stage, i, k);
+          for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;
+          if (c == 0) {
+            mine[D * 128 + row] = m_end;
+            mine[(D + 1) * 128 + row] = bad ? nan : l;
           }
-        }
-      } else if (good && row < w.rows) {
-        __nv_bfloat16* orow = a.out + w.b * a.so[0] + hqr * a.so[1] + tokr * a.so[2] + seg * QD;
+        } else if (args.out_vec) {   // rows go through shared memory, so that the global stores are whole rows of 16-byte pieces
+          stage_row32<D>(stage, row, c, r, unit);
+        } else if (row < w.rows) {
+          __nv_bfloat16* orow = a.out + w.b * a.so[0] + hqr * a.so[1] + tokr * a.so[2] + c * 32;
 #pragma unroll
-        for (int i = 0; i < QD / 2; ++i) {
-          const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&h[i]);
-          orow[2 * i] = v.x;
-          orow[2 * i + 1] = v.y;
+          for (int i = 0; i < 32; ++i) orow[i] = __float2bfloat16_rn(__uint_as_float(r[i]) * unit);
         }
       }
-    } else if (good) {
-      // partial result: O (in units of 2^m_run), m_run and the sum, [channel][row]
-      float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
-      const float unit = bad ? nan : exp2i(vbase);
-#pragma unroll
-      for (int i = 0; i < QD; ++i) mine[(seg * QD + i) * 128 + row] = __uint_as_float(r[i]) * unit;
-      if (seg == 0) {
-        mine[D * 128 + row] = m_run;
-        mine[(D + 1) * 128 + row] = bad ? nan : l;
+    }
+    if (w.parts == 1 && args.out_vec) {
+      all_barrier();
+      if (good) {
+        constexpr int CPR = D / 8, RPI = 32 / CPR;
+        const int k = lane % CPR;
+        for (int i = (warp - 4) * RPI + lane / CPR; i < w.rows; i += 12 * RPI) {
+          const int ri = w.row0 + i, tok = ri / a.G, hq = w.hk * a.G + ri - tok * a.G;
+          *reinterpret_cast<uint4*>(a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + k * 8) = *stage_chunk<D>(stage, i, k);
+        }
       }
     }
   }
