@@ -7,10 +7,11 @@
 // Two products with e4m3 operands take the tensor core as long as one with 16-bit operands, so the keys need no conversion; the weights would
 // need their two parts for every element, on the warps that already bound the kernel, so for P V it is the codes that are converted, once
 // per tile, by warps of their own.
-// Scales: that of a block of keys multiplies the logits of its columns, that of a block of values is added to the exponent of the weights
-// (relative to the largest of the CTA's visible blocks, 2^vbase) and taken out of the row sum again, 16 columns (the smallest page) at a time.
-//   warp 0       producer: page numbers and scales ahead, TMA into rings of three key tiles and two value tiles
-//   warp 1       issues S into three accumulators, warp 2 issues P V (one thread each), warp 3 idles
+// Scales: that of a block of keys multiplies the logits of its columns, 16 columns (the smallest page) at a time; that of a block of values
+// goes into its fp16 form, relative to the largest of the CTA's visible blocks, 2^vbase (a power of two: exact, but for what is
+// below 2^-24 of it).
+//   warp 0       producer of keys: page numbers and scales ahead, TMA into a ring of three tiles; warp 3 the same for values, four tiles
+//   warp 1       issues S into three accumulators, warp 2 issues P V (one thread each)
 //   warps 4-15   softmax: tile j belongs to the four warps of group j % 3, a thread per row; S is read from tensor memory twice, 32 columns at a
 //                time (maximum, then weights), and P goes over columns that have been read.  A scheduler of the SM thus holds three warps that
 //                work on three different tiles of the same rows, one in its maxima while another is in its exponentials; all they
@@ -39,26 +40,31 @@ struct PromptArgs {
   int q_vec, out_vec;
 };
 
-struct Group { float ks, vr, back, drop; };   // 16 columns: scale of the keys; exponent taken over from the values' scale, 2^-that; 1: no products
 struct PromptTile {
-  int pos, flags;     // first key position; 1: some scale is NaN, 2: some group is dropped
+  int pos, flags;     // first key position; 1: some scale is NaN
   int pad[2];
-  Group g[8];
+  float ks[8];        // scales of the keys, per 16 columns
+};
+struct ValueTile {
+  int pos, pad;
+  uint32_t vs[8];     // scales of the values per page, two fp16 each, relative to 2^vbase
 };
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
 constexpr int kRows = 128; // rows of a CTA
 constexpr int kThreads = 640;
+constexpr int kValueInfo = 4;   // (as many as value tiles: written when the tile is free)
 
 template <int D>
 struct PromptCfg {
-  static constexpr int NK = 3, NV = 2, NACC = 3;
+  static constexpr int NK = 3, NV8 = 4, NV = 2, NACC = 3;
   static constexpr int T8 = 128 * D, T16 = 256 * D;
   static constexpr int OFF_Q = 0;                        // hi, lo
   static constexpr int OFF_K = OFF_Q + 2 * T8;
   static constexpr int OFF_V8 = OFF_K + NK * T8;
-  static constexpr int OFF_V = OFF_V8 + NV * T8;
+  static constexpr int OFF_V = OFF_V8 + NV8 * T8;
   static constexpr int OFF_INFO = OFF_V + NV * T16;
-  static constexpr int OFF_M = OFF_INFO + kInfo * (int)sizeof(PromptTile);    // float [128]: references of the rows
+  static constexpr int OFF_VINFO = OFF_INFO + kInfo * (int)sizeof(PromptTile);
+  static constexpr int OFF_M = OFF_VINFO + kValueInfo * (int)sizeof(ValueTile);    // float [128]: references of the rows
   static constexpr int OFF_L = OFF_M + 128 * 4;                               // float [3][128]: sums of the groups, [3][128]: NaN marks
   static constexpr int OFF_CQ = OFF_L + 6 * 128 * 4;                          // float [128]
   static constexpr int OFF_BAR = OFF_CQ + 128 * 4;
@@ -68,8 +74,8 @@ struct PromptCfg {
 };
 // PB_READY: P of the tile is in tensor memory (4 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
 // 32 rows are decided for a tile, [row quarter][tile % 3]
-enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 8, PB_VFREE = 10, PB_SFULL = 12, PB_READY = 15, PB_PVDONE = 18, PB_QFULL = 21,
-       PB_REF = 22, PB_LAST = 34, PB_COUNT = 35 };
+enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 10, PB_VFREE = 14, PB_SFULL = 16, PB_READY = 19, PB_PVDONE = 22, PB_QFULL = 25,
+       PB_REF = 26, PB_LAST = 38, PB_COUNT = 39 };
 
 // What a CTA does: its rows and its key tiles.  (Also what the merge needs to know.)
 struct PromptWork {
@@ -115,24 +121,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// tc::ex2_poly for two
-__device__ __forceinline__ void ex2_poly2(uint64_t v, float& p0, float& p1) {
-  float x, y;
-  unpack2(v, x, y);
-  v = pack2(fmaxf(x, -125.f), fmaxf(y, -125.f));
-  const uint64_t r = add2(v, pack2(12582912.f, 12582912.f));
-  const uint64_t f = fma2(add2(r, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f), v);
-  uint64_t p = fma2(f, pack2(0.0096181291f, 0.0096181291f), pack2(0.0555041087f, 0.0555041087f));
-  p = fma2(p, f, pack2(0.2402265070f, 0.2402265070f));
-  p = fma2(p, f, pack2(0.6931471806f, 0.6931471806f));
-  p = fma2(p, f, pack2(1.0f, 1.0f));
-  float r0, r1;
-  unpack2(r, r0, r1);
-  unpack2(p, p0, p1);
-  p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23));
-  p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23));
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ PromptArgs args) {
@@ -142,6 +130,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   PromptTile* info = reinterpret_cast<PromptTile*>(base + Cfg::OFF_INFO);
+  ValueTile* vinfo = reinterpret_cast<ValueTile*>(base + Cfg::OFF_VINFO);
   float* s_m = reinterpret_cast<float*>(base + Cfg::OFF_M);
   float* s_l = reinterpret_cast<float*>(base + Cfg::OFF_L);
   float* s_cq = reinterpret_cast<float*>(base + Cfg::OFF_CQ);
@@ -162,11 +151,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::mbar_init(&bars[PB_READY + s], 4 + 4);
       tc::mbar_init(&bars[PB_PVDONE + s], 1);
     }
-    for (int s = 0; s < 2; ++s) {
-      tc::mbar_init(&bars[PB_V8FULL + s], 1);
-      tc::mbar_init(&bars[PB_V8FREE + s], 4);
-      tc::mbar_init(&bars[PB_VFREE + s], 1);
-    }
+    for (int s = 0; s < Cfg::NV8; ++s) { tc::mbar_init(&bars[PB_V8FULL + s], 1); tc::mbar_init(&bars[PB_V8FREE + s], 4); }
+    for (int s = 0; s < Cfg::NV; ++s) tc::mbar_init(&bars[PB_VFREE + s], 1);
     for (int s = 0; s < 12; ++s) tc::mbar_init(&bars[PB_REF + s], 1);
     tc::mbar_init(&bars[PB_QFULL], 8);
     tc::mbar_init(&bars[PB_LAST], 1);
@@ -185,9 +171,32 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     const int page = p.pages[(int64_t)w.b * p.max_pages + (p0 >> p.page_shift)];
     return page >= 0 && page < p.n_pages ? page : -2;
   };
-  {
+  // The producer of keys needs nothing but the barriers that its own thread has set up: it starts at once, beside the search for vbase.
+  int vbase = 0;
+  constexpr int E = D / 2;
+  uint32_t xq[E / 2];   // (warps 4-11) half a row of queries
+  if (warp == 0) {
+    __syncwarp();
+    asm volatile("barrier.cta.arrive 2, %0;" ::"n"(kThreads) : "memory");
+  } else {
+    if (warp >= 4 && warp < 12) {
+      const int r = (tid - 128) >> 1, rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
+      const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + (tid & 1) * E;
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) xq[i] = 0;
+      if (r < w.rows && args.q_vec) {
+#pragma unroll
+        for (int i = 0; i < E / 8; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * i);
+          xq[4 * i] = v.x; xq[4 * i + 1] = v.y; xq[4 * i + 2] = v.z; xq[4 * i + 3] = v.w;
+        }
+      } else if (r < w.rows) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) xq[i] = (uint32_t)__bfloat16_as_ushort(src[2 * i]) | ((uint32_t)__bfloat16_as_ushort(src[2 * i + 1]) << 16);
+      }
+    }
     int v = -1000;
-    for (int i = tid; i < w.ntiles * ppt; i += kThreads) {
+    for (int i = tid - 32; i < w.ntiles * ppt; i += kThreads - 32) {
       int p0;
       const int page = page_of(i, p0);
       if (page < 0) continue;
@@ -196,25 +205,30 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     }
     v = __reduce_max_sync(0xffffffffu, v);
     if (lane == 0) s_vmax[warp] = v;
-  }
-  tc::tc_fence_before();
-  __syncthreads();
-  tc::tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  int vbase = -1000;
+    tc::tc_fence_before();
+    __syncwarp();
+    asm volatile("barrier.cta.sync 2, %0;" ::"n"(kThreads) : "memory");
+    tc::tc_fence_after();
+    vbase = -1000;
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) vbase = max(vbase, s_vmax[i]);
-  if (vbase == -1000) vbase = 0;
+    for (int i = 1; i < kThreads / 32; ++i) vbase = max(vbase, s_vmax[i]);
+    if (vbase == -1000) vbase = 0;
+  }
+  const uint32_t tmem = warp == 0 ? 0 : *tmem_slot;
 
   auto fail = [&]() {
     if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
     *abort_flag = 1;
   };
   if (warp < 4) {
-    if (warp == 0) {
-      // ------------------------------ producer ------------------------------
-      const int tpb = 32 / ppt, lt = lane / ppt, lp = lane % ppt;
-      struct Page { int row, ke, ve, pos; };
+    if (warp == 0 || warp == 3) {
+      // ------------------------------ producers of keys (warp 0) and values (warp 3) ------------------------------
+      const bool keys = warp == 0;
+      const int ring = keys ? Cfg::NK : Cfg::NV8, full = keys ? PB_KFULL : PB_V8FULL, empty = keys ? PB_KFREE : PB_V8FREE;
+      const CUtensorMap* map = keys ? &mapK : &mapV;
+      uint8_t* tiles = base + (keys ? Cfg::OFF_K : Cfg::OFF_V8);
+      const int tpb = 32 / ppt, lt = lane / ppt, lp = lane % ppt;   // tiles whose pages the warp's lanes hold at a time
+      struct Page { int row, ke, ve, pos; };   // row < 0: not loaded
       auto fetch = [&](int k) {
         Page g{-1, 0, 0, 0};
         const int j = k * tpb + lt;
@@ -222,7 +236,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           int p0;
           const int page = page_of(j * ppt + lp, p0);
           g.pos = p0 - lp * p.page;
-          g.ve = vbase;
           if (page == -2) {
             report(p.status, KVM_ERR_INVALID_ARG);
             g.ke = g.ve = 128;
@@ -237,46 +250,38 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       };
       Page cur = fetch(0), nxt = fetch(1);
       bool ok = true;
-      int nk = 0, nv = 0;   // tiles issued
+      int s = 0, issued = 0;
+      uint32_t par = 0;
       for (int j = 0, k = 0, t = 0; j < w.ntiles; ++j) {
-        const int s = j % Cfg::NK, sv = j % Cfg::NV, in = j % kInfo;
-        if (lane == 0) ok = !*abort_flag && (j < Cfg::NK || tc::mbar_wait(&bars[PB_KFREE + s], ((j / Cfg::NK) - 1) & 1));
+        if (lane == 0) ok = j < ring || tc::mbar_wait(&bars[empty + s], par ^ 1);
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
-        const bool mine = lt == t;
+        const bool mine = lt == t, nan = cur.ke > 127 || cur.ve > 127;
         const uint32_t loads = __ballot_sync(0xffffffffu, mine && cur.row >= 0);
-        const uint32_t nans = __ballot_sync(0xffffffffu, mine && (cur.ke > 127 || cur.ve > 127));
-        const uint32_t drops = __ballot_sync(0xffffffffu, mine && cur.ve < vbase - 60);
-        const int bytes = __popc(loads) * p.page * D;
-        if (mine) {
-          if (lp == 0) { info[in].pos = cur.pos; info[in].flags = (nans ? 1 : 0) | (drops ? 2 : 0); }
-          const int vr = cur.ve > 127 ? 0 : max(cur.ve - vbase, -60);
-          const bool nan = cur.ke > 127 || cur.ve > 127;
-          const Group g{nan ? __int_as_float(0x7fc00000) : exp2i(cur.ke), (float)vr, exp2i(-vr), cur.ve < vbase - 60 ? 1.f : 0.f};
-          for (int i = 0; i < p.page / 16; ++i) info[in].g[lp * (p.page / 16) + i] = g;
+        const uint32_t nans = __ballot_sync(0xffffffffu, mine && nan);   // (pages outside the pool among them)
+        if (mine && keys) {
+          PromptTile& ti = info[j % kInfo];
+          if (lp == 0) { ti.pos = cur.pos; ti.flags = nans ? 1 : 0; }
+          const float ks = nan ? __int_as_float(0x7fc00000) : exp2i(cur.ke);
+          for (int i = 0; i < p.page / 16; ++i) ti.ks[lp * (p.page / 16) + i] = ks;
+        } else if (mine) {
+          if (lp == 0) vinfo[s].pos = cur.pos;
+          const __half h = __float2half_rn(nan || cur.row < 0 ? 0.f : exp2i(max(cur.ve - vbase, -126)));
+          vinfo[s].vs[lp] = (uint32_t)__half_as_ushort(h) * 0x10001u;
         }
         __syncwarp();
-        if (lane == 0) {
-          tc::mbar_expect_tx(&bars[PB_KFULL + s], bytes);   // (and what was written about the tile: the issuing thread and, by its products,
-                                                            // the softmax warps, come after this)
-        }
+        // (the arrival also hands on what was written about the tile: to the converting warps, and by the products to the softmax warps)
+        if (lane == 0) tc::mbar_expect_tx(&bars[full + s], __popc(loads) * p.page * D);
         __syncwarp();
-        if (mine && cur.row >= 0) tc::tma_load_2d(base + Cfg::OFF_K + s * Cfg::T8 + lp * p.page * D, &mapK, &bars[PB_KFULL + s], 0, cur.row);
-        nk = j + 1;
-        if (lane == 0) ok = j < Cfg::NV || tc::mbar_wait(&bars[PB_V8FREE + sv], ((j / Cfg::NV) - 1) & 1);
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-        if (lane == 0) tc::mbar_expect_tx(&bars[PB_V8FULL + sv], bytes);
-        __syncwarp();
-        if (mine && cur.row >= 0) tc::tma_load_2d(base + Cfg::OFF_V8 + sv * Cfg::T8 + lp * p.page * D, &mapV, &bars[PB_V8FULL + sv], 0, cur.row);
-        nv = j + 1;
+        if (mine && cur.row >= 0) tc::tma_load_2d(tiles + s * Cfg::T8 + lp * p.page * D, map, &bars[full + s], 0, cur.row);
+        issued = j + 1;
+        if (++s == ring) { s = 0; par ^= 1; }
         if (++t == tpb) { t = 0; ++k; cur = nxt; nxt = fetch(k + 1); }
       }
       if (lane == 0) {
         if (!ok) fail();
         // nothing may be in flight into shared memory when the CTA ends, whatever became of the others
-        for (int j = max(0, nk - Cfg::NK); j < nk; ++j) tc::mbar_wait(&bars[PB_KFULL + j % Cfg::NK], (j / Cfg::NK) & 1);
-        for (int j = max(0, nv - Cfg::NV); j < nv; ++j) tc::mbar_wait(&bars[PB_V8FULL + j % Cfg::NV], (j / Cfg::NV) & 1);
+        for (int j = max(0, issued - ring); j < issued; ++j) tc::mbar_wait(&bars[full + j % ring], (j / ring) & 1);
       }
     } else if (warp == 1) {
       // ------------------------------ S ------------------------------
@@ -289,8 +294,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         bool ok = tc::mbar_wait(&bars[PB_QFULL], 0);
         uint32_t s = 0, par = 0;   // ring of three: key tiles and accumulators
         for (int j = 0; j < w.ntiles && ok; ++j) {
-          ok = j < Cfg::NACC || tc::mbar_wait(&bars[PB_PVDONE + s], par ^ 1);
-          ok = ok && tc::mbar_wait(&bars[PB_KFULL + s], par);
+          ok = tc::mbar_wait(&bars[PB_KFULL + s], par);   // (long there, as a rule: not behind the wait that matters)
+          ok = ok && (j < Cfg::NACC || tc::mbar_wait(&bars[PB_PVDONE + s], par ^ 1));
           if (!ok) break;
           tc::tc_fence_after();
           const uint64_t k = dK + s * (Cfg::T8 >> 4);
@@ -337,14 +342,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     bool ok = true;
     uint32_t s3 = 0;
     for (int j = 0; j < w.ntiles; ++j) {
-      const int sv = j & 1;
-      bool good = tc::mbar_wait(&bars[PB_V8FULL + sv], (j >> 1) & 1);
+      const int sv = j & 1, s8 = j % Cfg::NV8;
+      bool good = tc::mbar_wait(&bars[PB_V8FULL + s8], (j / Cfg::NV8) & 1);
       if (good && j >= Cfg::NV) good = tc::mbar_wait(&bars[PB_VFREE + sv], ((j >> 1) - 1) & 1);
       ok = __all_sync(0xffffffffu, good);
       if (!ok) break;
-      const int pos = info[j % kInfo].pos;
+      const ValueTile& vt = vinfo[s8];
+      const int pos = vt.pos;
       const bool all = pos + 127 <= w.last && (pos > w.first - a.window || pos + 127 < a.sinks);   // every key is seen by some row
-      const uint8_t* src = base + Cfg::OFF_V8 + sv * Cfg::T8;
+      const uint8_t* src = base + Cfg::OFF_V8 + s8 * Cfg::T8;
       uint8_t* dst = base + Cfg::OFF_V + sv * Cfg::T16;
       uint4 c[4 * N];
 #pragma unroll
@@ -362,9 +368,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) {
         const int r = rows0 + 8 * (i / N) + r8, pc = pc0 + 4 * (i % N);
+        const uint32_t f2 = vt.vs[(rows0 + 8 * (i / N)) >> p.page_shift];
+        auto scaled = [&](uint32_t code2) {
+          const uint32_t h = e4m3x2_to_f16x2(code2);
+          const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&f2));
+          return *reinterpret_cast<const uint32_t*>(&r);
+        };
         uint4 lo, hi;
-        lo.x = e4m3x2_to_f16x2(c[i].x & 0xffff); lo.y = e4m3x2_to_f16x2(c[i].x >> 16); lo.z = e4m3x2_to_f16x2(c[i].y & 0xffff); lo.w = e4m3x2_to_f16x2(c[i].y >> 16);
-        hi.x = e4m3x2_to_f16x2(c[i].z & 0xffff); hi.y = e4m3x2_to_f16x2(c[i].z >> 16); hi.z = e4m3x2_to_f16x2(c[i].w & 0xffff); hi.w = e4m3x2_to_f16x2(c[i].w >> 16);
+        lo.x = scaled(c[i].x & 0xffff); lo.y = scaled(c[i].x >> 16); lo.z = scaled(c[i].y & 0xffff); lo.w = scaled(c[i].y >> 16);
+        hi.x = scaled(c[i].z & 0xffff); hi.y = scaled(c[i].z >> 16); hi.z = scaled(c[i].w & 0xffff); hi.w = scaled(c[i].w >> 16);
         uint8_t* at = dst + (pc >> 2) * (128 * 128) + r * 128;
         *reinterpret_cast<uint4*>(at + (((2 * (pc & 3)) ^ r8) << 4)) = lo;
         *reinterpret_cast<uint4*>(at + (((2 * (pc & 3) + 1) ^ r8) << 4)) = hi;
@@ -373,7 +385,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       __syncwarp();
       if (lane == 0) {
         tc::mbar_arrive(&bars[PB_READY + s3]);
-        tc::mbar_arrive(&bars[PB_V8FREE + sv]);
+        tc::mbar_arrive(&bars[PB_V8FREE + s8]);
       }
       if (++s3 == 3) s3 = 0;
     }
@@ -383,28 +395,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     const int group = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     auto all_barrier = []() { asm volatile("bar.sync 1, 384;" ::: "memory"); };
     if (group < 2) {
-      // two threads per row: power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
-      const int t = tid - 128, r = t >> 1, part = t & 1;
-      constexpr int E = D / 2;
-      const bool live = r < w.rows;
-      const int rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
-      const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + part * E;
-      uint32_t x[E / 2];
-#pragma unroll
-      for (int i = 0; i < E / 2; ++i) x[i] = 0;
-      if (live && args.q_vec) {
-#pragma unroll
-        for (int i = 0; i < E / 8; ++i) {
-          const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * i);
-          x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-        }
-      } else if (live) {
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) x[i] = (uint32_t)__bfloat16_as_ushort(src[2 * i]) | ((uint32_t)__bfloat16_as_ushort(src[2 * i + 1]) << 16);
-      }
+      // (two threads per row) power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
       uint32_t top2 = 0;
 #pragma unroll
-      for (int i = 0; i < E / 2; ++i) top2 = __vmaxu2(top2, x[i] & 0x7fff7fffu);
+      for (int i = 0; i < E / 2; ++i) top2 = __vmaxu2(top2, xq[i] & 0x7fff7fffu);
       uint32_t top = max(top2 & 0xffffu, top2 >> 16);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       const bool nan = top >= 0x7f80u;
@@ -418,7 +412,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           hi[q] = lo[q] = 0;
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
-            const uint32_t v = x[8 * i + 2 * q + z];
+            const uint32_t v = xq[8 * i + 2 * q + z];
             const float y0 = nan ? 0.f : __uint_as_float(v << 16) * mul, y1 = nan ? 0.f : __uint_as_float(v & 0xffff0000u) * mul;
             const uint32_t h = to_e4m3x2(y0, y1);
             const float2 back = e4m3x2_to_float2(h);
@@ -426,12 +420,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             lo[q] |= to_e4m3x2(y0 - back.x, y1 - back.y) << (16 * z);
           }
         }
-        const int piece = part * (E / 16) + i;
+        const int r = (tid - 128) >> 1, part = tid & 1, piece = part * (E / 16) + i;
         uint8_t* at = base + Cfg::OFF_Q + r * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
-      if (part == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
+      if ((tid & 1) == 0) s_cq[(tid - 128) >> 1] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
       tc::fence_proxy_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[PB_QFULL]);
@@ -465,7 +459,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           uint32_t see = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const float ks = ti.g[2 * c + g].ks;
+            const float ks = ti.ks[2 * c + g];
             if (!(ks == ks)) {
               const uint32_t cols = 0xffffu << (16 * g);
               bad = bad || (see & cols);
@@ -483,7 +477,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         load(c, x);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          const Group gr = ti.g[2 * c + g];
           float m = __uint_as_float(x[16 * g]), m2 = __uint_as_float(x[16 * g + 1]);
 #pragma unroll
           for (int i = 2; i < 14; i += 4) {
@@ -492,7 +485,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           }
           m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
           // (the factor is never 0 or NaN: a masked column is -inf)
-          mx = fmaxf(mx, fmaf(fmaxf(m, m2), fmaxf(cq * gr.ks, 1.17549435e-38f), gr.vr));
+          mx = fmaxf(mx, fmaxf(m, m2) * fmaxf(cq * ti.ks[2 * c + g], 1.17549435e-38f));
         }
       }
       // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
@@ -532,42 +525,27 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       l_run = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m);
       m_ref = m;
       const float neg_m = (m == -INFINITY) ? 0.f : -m;
+      const uint64_t a2 = pack2(neg_m, neg_m);
+      uint64_t s0 = 0, s1 = 0;   // sums of the tile's weights
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         uint32_t x[32], wd[16];
         load(c, x);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          const Group gr = ti.g[2 * c + g];
-          const float f = fmaxf(cq * gr.ks, 1.17549435e-38f), add = neg_m + gr.vr;
-          const uint64_t f2 = pack2(f, f), a2 = pack2(add, add);
-          uint64_t s0 = 0, s1 = 0;
+          const float f = fmaxf(cq * ti.ks[2 * c + g], 1.17549435e-38f);
+          const uint64_t f2 = pack2(f, f);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const uint64_t y = fma2(pack2(__uint_as_float(x[16 * g + 2 * i]), __uint_as_float(x[16 * g + 2 * i + 1])), f2, a2);
             float p0, p1;
-            // a quarter of the exponentials on the FMA pipe instead of the special-function unit (P is rounded to fp16 anyway: the
-            // polynomial's relative error is below 5e-5)
-            if ((i & 3) == 3) {
-              ex2_poly2(y, p0, p1);
-            } else {
-              unpack2(y, p0, p1);
-              p0 = tc::ex2_approx(p0);
-              p1 = tc::ex2_approx(p1);
-            }
+            unpack2(y, p0, p1);
+            p0 = tc::ex2_approx(p0);
+            p1 = tc::ex2_approx(p1);
             const uint64_t p2 = pack2(p0, p1);
             if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
             const __half2 h2 = __floats2half2_rn(p0, p1);
             wd[8 * g + i] = *reinterpret_cast<const uint32_t*>(&h2);
-          }
-          float l0, l1;
-          unpack2(add2(s0, s1), l0, l1);
-          l_run = fmaf(l0 + l1, gr.back, l_run);
-          if (flags & 2) {
-            if (gr.drop != 0.f) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) wd[8 * g + i] = 0;
-            }
           }
         }
         tc::tmem_st16(ts + 16 * c, wd);   // (columns that have been read)
@@ -576,6 +554,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::tc_fence_before();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[PB_READY + group]);
+      float l0, l1;
+      unpack2(add2(s0, s1), l0, l1);
+      l_run += l0 + l1;
     }
     if (ok) ok = tc::mbar_wait(&bars[PB_LAST], 0);
     if (!ok) fail();
