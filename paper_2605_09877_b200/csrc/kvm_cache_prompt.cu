@@ -12,11 +12,12 @@
 // below 2^-24 of it).
 //   warp 0       producer of keys: page numbers and scales ahead, TMA into a ring of three tiles; warp 3 the same for values, four tiles
 //   warp 1       issues S into three accumulators, warp 2 issues P V (one thread each)
-//   warps 4-15   softmax: tile j belongs to the four warps of group j % 3, a thread per row; S is read from tensor memory twice, 32 columns at a
-//                time (maximum, then weights), and P goes over columns that have been read.  A scheduler of the SM thus holds three warps that
-//                work on three different tiles of the same rows, one in its maxima while another is in its exponentials; all they
-//                hand on from tile to tile is the reference of each row (with which O is scaled), decided after the maximum.
-//   warps 16-19  value codes -> fp16, swizzled as the MMA reads them
+//   warps 4-19   softmax: tile j belongs to the eight warps of group j % 2, two threads per row, 64 columns each; S is read from tensor memory
+//                twice, 32 columns at a time (maximum, then weights), and P goes over columns that have been read.  A scheduler of the SM
+//                thus holds two pairs of warps that work on two different tiles of the same rows, one in its maxima while another is in its
+//                exponentials; all they hand on from tile to tile is the reference of each row (with which O is scaled), decided after
+//                the maximum.
+//   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 // With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.
 //
 #include <algorithm>
@@ -34,8 +35,20 @@ bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, 
 constexpr int kSplitTiles = 4;    // least key tiles of a split
 constexpr int kMaxSplits = 32;
 
+// n / d for 0 <= n < 2^31: with 2^(l-1) < d <= 2^l, m = floor(2^(31+l) / d) + 1, m d exceeds 2^(31+l) by at most 2^l, so n m >> (31 + l) is exact.
+struct FastDiv {
+  uint32_t m, s, d;
+  explicit FastDiv(uint32_t x = 1) : d(x) {
+    int l = 0;
+    while ((1ull << l) < x) ++l;
+    s = 31 + l;
+    m = (uint32_t)((1ull << s) / x + 1);
+  }
+  __device__ __forceinline__ int div(int n) const { return (int)(((uint64_t)(uint32_t)n * m) >> s); }
+};
 struct PromptArgs {
   AttendArgs a;
+  FastDiv by_units, by_heads, by_group;
   int units, qtiles, nsplit;
   int q_vec, out_vec;
 };
@@ -51,7 +64,7 @@ struct ValueTile {
 };
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
 constexpr int kRows = 128; // rows of a CTA
-constexpr int kThreads = 640;
+constexpr int kThreads = 768;
 constexpr int kValueInfo = 4;   // (as many as value tiles: written when the tile is free)
 
 template <int D>
@@ -65,14 +78,15 @@ struct PromptCfg {
   static constexpr int OFF_INFO = OFF_V + NV * T16;
   static constexpr int OFF_VINFO = OFF_INFO + kInfo * (int)sizeof(PromptTile);
   static constexpr int OFF_M = OFF_VINFO + kValueInfo * (int)sizeof(ValueTile);    // float [128]: references of the rows
-  static constexpr int OFF_L = OFF_M + 128 * 4;                               // float [3][128]: sums of the groups, [3][128]: NaN marks
-  static constexpr int OFF_CQ = OFF_L + 6 * 128 * 4;                          // float [128]
+  static constexpr int OFF_XM = OFF_M + 128 * 4;                              // float [2 groups][2][2 halves][128]: maxima
+  static constexpr int OFF_L = OFF_XM + 8 * 128 * 4;                          // float [4][128]: sums of the row's four threads, [4][128]: NaN marks
+  static constexpr int OFF_CQ = OFF_L + 8 * 128 * 4;                          // float [128]
   static constexpr int OFF_BAR = OFF_CQ + 128 * 4;
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static constexpr int SMEM = (OFF_BAR + 512 + 1024) > 120 * 1024 ? (OFF_BAR + 512 + 1024) : 120 * 1024;
   static constexpr uint32_t COL_S = 0, COL_O = 384;      // S / P accumulator i at 128 i
 };
-// PB_READY: P of the tile is in tensor memory (4 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
+// PB_READY: P of the tile is in tensor memory (8 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
 // 32 rows are decided for a tile, [row quarter][tile % 3]
 enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 10, PB_VFREE = 14, PB_SFULL = 16, PB_READY = 19, PB_PVDONE = 22, PB_QFULL = 25,
        PB_REF = 26, PB_LAST = 38, PB_COUNT = 39 };
@@ -84,8 +98,8 @@ struct PromptWork {
 };
 __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int sp, PromptWork& w) {
   const Params& p = args.a.p;
-  const int unit = idx % args.units, qt = args.qtiles - 1 - idx / args.units;   // (the last rows see the most keys: first)
-  w.b = unit / p.Hkv; w.hk = unit % p.Hkv;
+  const int turn = args.by_units.div(idx), unit = idx - turn * args.units, qt = args.qtiles - 1 - turn;   // (the last rows see the most keys: first)
+  w.b = args.by_heads.div(unit); w.hk = unit - w.b * p.Hkv;
   int n;
   if (!seq_lengths(p, w.b, w.start, n)) {
     if (idx == unit && w.hk == 0 && sp == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
@@ -95,14 +109,34 @@ __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int
   const int64_t left = (int64_t)n * args.a.G - w.row0;
   if (left <= 0) return false;
   w.rows = (int)min((int64_t)kRows, left);
-  w.first = w.start + w.row0 / args.a.G;
-  w.last = w.start + (w.row0 + w.rows - 1) / args.a.G;
+  w.first = w.start + args.by_group.div(w.row0);
+  w.last = w.start + args.by_group.div(w.row0 + w.rows - 1);
   w.t = tiles_of(w.first, w.last, args.a.window, args.a.sinks);
-  const int per = max(kSplitTiles, (w.t.n + args.nsplit - 1) / args.nsplit);
-  w.parts = (w.t.n + per - 1) / per;
-  w.jb = sp * per;
-  w.ntiles = min(per, w.t.n - w.jb);
+  w.parts = 1;
+  w.jb = 0;
+  w.ntiles = w.t.n;
+  if (args.nsplit > 1) {
+    const int per = max(kSplitTiles, (w.t.n + args.nsplit - 1) / args.nsplit);
+    w.parts = (w.t.n + per - 1) / per;
+    w.jb = sp * per;
+    w.ntiles = min(per, w.t.n - w.jb);
+  }
   return w.ntiles > 0;
+}
+// Barrier of the two warps of a group that share 32 rows, which also tells whether both are well.
+__device__ __forceinline__ bool pair_barrier(int id, bool ok) {
+  uint32_t r;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.and.aligned.pred q, %2, 64, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"(ok ? 1u : 0u), "r"(id) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void copy16_async(void* smem, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(smem)), "l"(global) : "memory");
 }
 // two fp32 operations in one instruction
 __device__ __forceinline__ uint64_t pack2(float x, float y) {
@@ -132,12 +166,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   PromptTile* info = reinterpret_cast<PromptTile*>(base + Cfg::OFF_INFO);
   ValueTile* vinfo = reinterpret_cast<ValueTile*>(base + Cfg::OFF_VINFO);
   float* s_m = reinterpret_cast<float*>(base + Cfg::OFF_M);
+  float* xm = reinterpret_cast<float*>(base + Cfg::OFF_XM);
   float* s_l = reinterpret_cast<float*>(base + Cfg::OFF_L);
   float* s_cq = reinterpret_cast<float*>(base + Cfg::OFF_CQ);
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + PB_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [20]
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [24]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   PromptWork w;
   if (!prompt_work(args, blockIdx.x, blockIdx.y, w)) return;
@@ -148,13 +183,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::mbar_init(&bars[PB_KFULL + s], 1);
       tc::mbar_init(&bars[PB_KFREE + s], 1);
       tc::mbar_init(&bars[PB_SFULL + s], 1);
-      tc::mbar_init(&bars[PB_READY + s], 4 + 4);
+      tc::mbar_init(&bars[PB_READY + s], 8 + 4);
       tc::mbar_init(&bars[PB_PVDONE + s], 1);
     }
     for (int s = 0; s < Cfg::NV8; ++s) { tc::mbar_init(&bars[PB_V8FULL + s], 1); tc::mbar_init(&bars[PB_V8FREE + s], 4); }
     for (int s = 0; s < Cfg::NV; ++s) tc::mbar_init(&bars[PB_VFREE + s], 1);
-    for (int s = 0; s < 12; ++s) tc::mbar_init(&bars[PB_REF + s], 1);
-    tc::mbar_init(&bars[PB_QFULL], 8);
+    for (int s = 0; s < 12; ++s) tc::mbar_init(&bars[PB_REF + s], 2);
+    tc::mbar_init(&bars[PB_QFULL], 16);
     tc::mbar_init(&bars[PB_LAST], 1);
     *abort_flag = 0;
     tc::fence_barrier_init();
@@ -164,36 +199,37 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   // Page i of the CTA's tiles (ppt pages a tile): whether some row sees some key of it, and where it is.
-  const int ppt = kTile / p.page;
+  const int tshift = 7 - p.page_shift, ppt = 1 << tshift;
   auto page_of = [&](int i, int& p0) -> int {   // >= 0: page; -1: not seen; -2: outside the pool
-    p0 = tile_at(w.t, w.jb + i / ppt) * kTile + (i % ppt) * p.page;
+    p0 = tile_at(w.t, w.jb + (i >> tshift)) * kTile + (i & (ppt - 1)) * p.page;
     if (p0 > w.last || !(p0 + p.page > w.first - a.window + 1 || p0 < a.sinks)) return -1;
     const int page = p.pages[(int64_t)w.b * p.max_pages + (p0 >> p.page_shift)];
     return page >= 0 && page < p.n_pages ? page : -2;
   };
   // The producer of keys needs nothing but the barriers that its own thread has set up: it starts at once, beside the search for vbase.
   int vbase = 0;
-  constexpr int E = D / 2;
-  uint32_t xq[E / 2];   // (warps 4-11) half a row of queries
   if (warp == 0) {
     __syncwarp();
     asm volatile("barrier.cta.arrive 2, %0;" ::"n"(kThreads) : "memory");
   } else {
-    if (warp >= 4 && warp < 12) {
-      const int r = (tid - 128) >> 1, rg = w.row0 + r, tokq = rg / a.G, hq = w.hk * a.G + rg - tokq * a.G;
-      const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tokq * a.sq[2] + (tid & 1) * E;
-#pragma unroll
-      for (int i = 0; i < E / 2; ++i) xq[i] = 0;
-      if (r < w.rows && args.q_vec) {
-#pragma unroll
-        for (int i = 0; i < E / 8; ++i) {
-          const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * i);
-          xq[4 * i] = v.x; xq[4 * i + 1] = v.y; xq[4 * i + 2] = v.z; xq[4 * i + 3] = v.w;
+    // the queries as they are, to where the fp16 values will be (the converting warps wait for them to be used up)
+    if (warp >= 4 && warp < 20) {
+      uint8_t* raw = base + Cfg::OFF_V;
+      constexpr int CPR = D / 8;   // 16-byte pieces of a row
+      for (int i = tid - 128; i < 128 * CPR; i += 512) {
+        const int r = i / CPR, c = i % CPR, rg = w.row0 + r, tok = args.by_group.div(rg), hq = w.hk * a.G + rg - tok * a.G;
+        uint4* dst = reinterpret_cast<uint4*>(raw + r * (2 * D) + ((c ^ (r & 7)) << 4));
+        const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tok * a.sq[2] + 8 * c;
+        if (r >= w.rows) {
+          *dst = make_uint4(0, 0, 0, 0);
+        } else if (args.q_vec) {
+          copy16_async(dst, src);
+        } else {
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[e] = src[e];
         }
-      } else if (r < w.rows) {
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) xq[i] = (uint32_t)__bfloat16_as_ushort(src[2 * i]) | ((uint32_t)__bfloat16_as_ushort(src[2 * i + 1]) << 16);
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
     int v = -1000;
     for (int i = tid - 32; i < w.ntiles * ppt; i += kThreads - 32) {
@@ -227,7 +263,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       const int ring = keys ? Cfg::NK : Cfg::NV8, full = keys ? PB_KFULL : PB_V8FULL, empty = keys ? PB_KFREE : PB_V8FREE;
       const CUtensorMap* map = keys ? &mapK : &mapV;
       uint8_t* tiles = base + (keys ? Cfg::OFF_K : Cfg::OFF_V8);
-      const int tpb = 32 / ppt, lt = lane / ppt, lp = lane % ppt;   // tiles whose pages the warp's lanes hold at a time
+      const int tpb = 32 >> tshift, lt = lane >> tshift, lp = lane & (ppt - 1);   // tiles whose pages the warp's lanes hold at a time
       struct Page { int row, ke, ve, pos; };   // row < 0: not loaded
       auto fetch = [&](int k) {
         Page g{-1, 0, 0, 0};
@@ -325,7 +361,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           const uint32_t aP = tmem + Cfg::COL_S + 128 * s;
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
-            tc::mma_f16_ts(tmem + Cfg::COL_O, aP + 8 * kk, v + kk * (2048 >> 4), ID, (j > 0 || kk > 0) ? 1u : 0u);
+            tc::mma_f16_ts(tmem + Cfg::COL_O, aP + 64 * (kk >> 2) + 8 * (kk & 3), v + kk * (2048 >> 4), ID, (j > 0 || kk > 0) ? 1u : 0u);
           tc::mma_commit(&bars[PB_PVDONE + s]);
           tc::mma_commit(&bars[PB_VFREE + (j & 1)]);
           if (++s == 3) { s = 0; par ^= 1; }
@@ -334,16 +370,16 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         tc::mma_commit(&bars[PB_LAST]);   // (a barrier of its own: a group whose tiles are done may be more than a phase ahead of PB_PVDONE)
       }
     }
-  } else if (warp >= 16) {
+  } else if (warp >= 20) {
     // ------------------------------ values to fp16 ------------------------------
     constexpr int PIECES = D / 16;             // 16-byte pieces of a row of codes
     constexpr int N = PIECES / 4;              // a warp's lanes take eight rows and four pieces at a time: no two share a bank
-    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 16) * 32;
-    bool ok = true;
+    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
+    bool ok = tc::mbar_wait(&bars[PB_QFULL], 0);   // (the queries lay where the first tiles go)
     uint32_t s3 = 0;
     for (int j = 0; j < w.ntiles; ++j) {
       const int sv = j & 1, s8 = j % Cfg::NV8;
-      bool good = tc::mbar_wait(&bars[PB_V8FULL + s8], (j / Cfg::NV8) & 1);
+      bool good = ok && tc::mbar_wait(&bars[PB_V8FULL + s8], (j / Cfg::NV8) & 1);
       if (good && j >= Cfg::NV) good = tc::mbar_wait(&bars[PB_VFREE + sv], ((j >> 1) - 1) & 1);
       ok = __all_sync(0xffffffffu, good);
       if (!ok) break;
@@ -392,74 +428,83 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!ok && lane == 0) fail();
   } else {
     // ------------------------------ q; softmax; results ------------------------------
-    const int group = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
-    auto all_barrier = []() { asm volatile("bar.sync 1, 384;" ::: "memory"); };
-    if (group < 2) {
-      // (two threads per row) power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
-      uint32_t top2 = 0;
-#pragma unroll
-      for (int i = 0; i < E / 2; ++i) top2 = __vmaxu2(top2, xq[i] & 0x7fff7fffu);
-      uint32_t top = max(top2 & 0xffffu, top2 >> 16);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      const bool nan = top >= 0x7f80u;
-      const int e = max((int)(top >> 7), 10);
-      const float mul = nan ? 0.f : exp2i(134 - e);
-#pragma unroll
-      for (int i = 0; i < E / 16; ++i) {
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          hi[q] = lo[q] = 0;
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const uint32_t v = xq[8 * i + 2 * q + z];
-            const float y0 = nan ? 0.f : __uint_as_float(v << 16) * mul, y1 = nan ? 0.f : __uint_as_float(v & 0xffff0000u) * mul;
-            const uint32_t h = to_e4m3x2(y0, y1);
-            const float2 back = e4m3x2_to_float2(h);
-            hi[q] |= h << (16 * z);
-            lo[q] |= to_e4m3x2(y0 - back.x, y1 - back.y) << (16 * z);
-          }
+    const int group = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
+    auto all_barrier = []() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+    {
+      // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys; D / 16 threads per row
+      constexpr int TPR = D / 16;
+      const uint8_t* raw = base + Cfg::OFF_V;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      all_barrier();
+#pragma unroll 1
+      for (int i = tid - 128; i < 128 * TPR; i += 512) {
+        const int r = i / TPR, piece = i % TPR;
+        uint32_t x[8];
+        {
+          const uint4 u = *reinterpret_cast<const uint4*>(raw + r * (2 * D) + (((2 * piece) ^ (r & 7)) << 4));
+          const uint4 v = *reinterpret_cast<const uint4*>(raw + r * (2 * D) + (((2 * piece + 1) ^ (r & 7)) << 4));
+          x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
         }
-        const int r = (tid - 128) >> 1, part = tid & 1, piece = part * (E / 16) + i;
+        uint32_t top2 = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) top2 = __vmaxu2(top2, x[q] & 0x7fff7fffu);
+        uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+#pragma unroll
+        for (int o = 1; o < TPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool nan = top >= 0x7f80u;
+        const int e = max((int)(top >> 7), 10);
+        const float mul = nan ? 0.f : exp2i(134 - e);
+        uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const uint32_t v = nan ? 0u : x[q];
+          const float y0 = __uint_as_float(v << 16) * mul, y1 = __uint_as_float(v & 0xffff0000u) * mul;
+          const uint32_t h = to_e4m3x2(y0, y1);
+          const float2 back = e4m3x2_to_float2(h);
+          hi[q >> 1] |= h << (16 * (q & 1));
+          lo[q >> 1] |= to_e4m3x2(y0 - back.x, y1 - back.y) << (16 * (q & 1));
+        }
         uint8_t* at = base + Cfg::OFF_Q + r * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        if (piece == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
       }
-      if ((tid & 1) == 0) s_cq[(tid - 128) >> 1] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
       tc::fence_proxy_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[PB_QFULL]);
+      all_barrier();
     }
-    all_barrier();
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = lanes + Cfg::COL_O, ts = lanes + Cfg::COL_S + 128 * group;
-    const int pos_row = row < w.rows ? w.start + (w.row0 + row) / a.G : w.last;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = lanes + Cfg::COL_O;
+    const int pos_row = row < w.rows ? w.start + args.by_group.div(w.row0 + row) : w.last;
     float cq = s_cq[row];
     bool bad = !(cq == cq);   // NaN rows are marked, not computed with
     if (bad) cq = 0.f;
     float m_ref = -INFINITY, l_run = 0.f;   // l_run is relative to 2^m_ref
     bool ok = true;
-    uint32_t par = 0;
+    float* my_xm = xm + group * 512;   // [tile parity of the group][half][row]
+    uint32_t s = group, par = 0, flip = 0;   // tile j: accumulator j % 3, its phase (j / 3) & 1
 #pragma unroll 1
-    for (int j = group; j < w.ntiles; j += 3, par ^= 1) {
-      if (!tc::mbar_wait(&bars[PB_SFULL + group], par)) ok = false;
+    for (int j = group; j < w.ntiles; j += 2, flip ^= 1) {
+      const uint32_t ts = lanes + Cfg::COL_S + 128 * s, sb = s == 0 ? 2 : s - 1, parb = s == 0 ? par ^ 1 : par;   // (sb, parb: of the tile before)
+      if (!tc::mbar_wait(&bars[PB_SFULL + s], par)) ok = false;
       __syncwarp();
       tc::tc_fence_after();
       const PromptTile& ti = info[j % kInfo];
       const int flags = ti.flags, pos = ti.pos;
       const bool slow = flags || !(pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks));   // (uniform) masks, or NaN scales
-      // S of columns 32 c .. 32 c + 31; what the row does not see as -inf
+      // S of columns 64 half + 32 c .. + 31; what the row does not see as -inf
       auto load = [&](int c, uint32_t (&x)[32]) {
-        tc::tmem_ld32(ts + 32 * c, x);
+        tc::tmem_ld32(ts + 64 * half + 32 * c, x);
         tc::tmem_wait_ld();
         if (slow) {
-          const int key0 = pos + 32 * c;
+          const int key0 = pos + 64 * half + 32 * c;
           // bit i: the row sees column i.  j <= pos_row, and j > pos_row - window or j < sinks
           auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // columns i < n
           const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
           uint32_t see = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const float ks = ti.ks[2 * c + g];
+            const float ks = ti.ks[4 * half + 2 * c + g];
             if (!(ks == ks)) {
               const uint32_t cols = 0xffffu << (16 * g);
               bad = bad || (see & cols);
@@ -472,7 +517,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       };
       float mx = -INFINITY;
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t x[32];
         load(c, x);
 #pragma unroll
@@ -485,28 +530,32 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           }
           m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
           // (the factor is never 0 or NaN: a masked column is -inf)
-          mx = fmaxf(mx, fmaxf(m, m2) * fmaxf(cq * ti.ks[2 * c + g], 1.17549435e-38f));
+          mx = fmaxf(mx, fmaxf(m, m2) * fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f));
         }
       }
+      // the maximum of the row's other half
+      float* x2 = my_xm + flip * 256;
+      x2[half * 128 + row] = mx;
+      ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);
+      if (!ok) break;
+      mx = fmaxf(mx, x2[(1 - half) * 128 + row]);
       // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
       float m = -INFINITY;
       if (j > 0) {
-        const int before = j - 1, gb = group == 0 ? 2 : group - 1;
-        if (!tc::mbar_wait(&bars[PB_REF + quarter * 3 + gb], (before / 3) & 1)) ok = false;
+        if (!tc::mbar_wait(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
         __syncwarp();
         m = s_m[row];
       }
-      if (__any_sync(0xffffffffu, mx > m + 8.0f || (j == 0))) {
+      if (__any_sync(0xffffffffu, mx > m + 8.0f || j == 0)) {   // (the same decision in both warps)
         const float mnew = fmaxf(m, mx);
         if (j > 0) {
-          // all earlier P V products must have landed before O is touched
-          const int gb = group == 0 ? 2 : group - 1;
-          if (!tc::mbar_wait(&bars[PB_PVDONE + gb], ((j - 1) / 3) & 1)) ok = false;
+          // all earlier P V products must have landed before O is touched; each warp takes half of the channels
+          if (!tc::mbar_wait(&bars[PB_PVDONE + sb], parb)) ok = false;
           __syncwarp();
           tc::tc_fence_after();
           const float corr = (m == -INFINITY) ? 0.f : tc::ex2_approx(m - mnew);
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
+          for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
             uint32_t r[32];
             tc::tmem_ld32(to + c * 32, r);
             tc::tmem_wait_ld();
@@ -515,25 +564,26 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             tc::tmem_st32(to + c * 32, r);
           }
           tc::tmem_wait_st();
+          ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);   // (both have read the reference)
         }
         m = mnew;
-        s_m[row] = m;
+        if (half == 0) s_m[row] = m;
       }
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&bars[PB_REF + quarter * 3 + group]);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      if (lane == 0) tc::mbar_arrive(&bars[PB_REF + quarter * 3 + s]);
+      // (a wait that ran out is acted on at the next barrier of the pair, by both warps)
       l_run = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m);
       m_ref = m;
       const float neg_m = (m == -INFINITY) ? 0.f : -m;
       const uint64_t a2 = pack2(neg_m, neg_m);
       uint64_t s0 = 0, s1 = 0;   // sums of the tile's weights
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t x[32], wd[16];
         load(c, x);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          const float f = fmaxf(cq * ti.ks[2 * c + g], 1.17549435e-38f);
+          const float f = fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f);
           const uint64_t f2 = pack2(f, f);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -548,12 +598,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             wd[8 * g + i] = *reinterpret_cast<const uint32_t*>(&h2);
           }
         }
-        tc::tmem_st16(ts + 16 * c, wd);   // (columns that have been read)
+        tc::tmem_st16(ts + 64 * half + 16 * c, wd);   // (columns that this thread has read)
       }
       tc::tmem_wait_st();
       tc::tc_fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&bars[PB_READY + group]);
+      if (lane == 0) tc::mbar_arrive(&bars[PB_READY + s]);
+      if (s == 0) s = 2; else { --s; par ^= 1; }
       float l0, l1;
       unpack2(add2(s0, s1), l0, l1);
       l_run += l0 + l1;
@@ -562,39 +613,38 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!ok) fail();
     __syncwarp();
     tc::tc_fence_after();
-    // (the last P V is done: every reference has been decided) the row sum is the sum of the groups' sums
+    // (the last P V is done: every reference has been decided) the row sum is the sum of its four threads' sums
     const float m_end = s_m[row];
-    s_l[group * 128 + row] = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m_end);
-    s_l[(3 + group) * 128 + row] = bad ? 1.f : 0.f;
+    const int part4 = group * 2 + half;
+    s_l[part4 * 128 + row] = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m_end);
+    s_l[(4 + part4) * 128 + row] = bad ? 1.f : 0.f;
     all_barrier();
     const bool good = ok && !*abort_flag;
-    const float l = s_l[row] + s_l[128 + row] + s_l[256 + row], nan = __int_as_float(0x7fc00000);
-    bad = s_l[384 + row] + s_l[512 + row] + s_l[640 + row] != 0.f;
+    const float l = (s_l[row] + s_l[128 + row]) + (s_l[256 + row] + s_l[384 + row]), nan = __int_as_float(0x7fc00000);
+    bad = s_l[512 + row] + s_l[640 + row] + s_l[768 + row] + s_l[896 + row] != 0.f;
     uint8_t* stage = base + Cfg::OFF_Q;   // (the queries are not needed any more)
-    const int rg = w.row0 + row, tokr = rg / a.G, hqr = w.hk * a.G + rg - tokr * a.G;
+    const int rg = w.row0 + row, tokr = args.by_group.div(rg), hqr = w.hk * a.G + rg - tokr * a.G;
     const float unit = bad ? nan : w.parts == 1 ? exp2i(vbase) / l : exp2i(vbase);
-    if (good) {
-#pragma unroll 1
-      for (int c = group; c < D / 32; c += 3) {   // 32 channels at a time
-        uint32_t r[32];
-        __syncwarp();
-        tc::tmem_ld32(to + c * 32, r);
-        tc::tmem_wait_ld();
-        if (w.parts > 1) {   // partial result: O (in units of 2^m_end), m_end and the sum, [channel][row]
-          float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
+    if (good && part4 < D / 32) {
+      const int c = part4;   // 32 channels
+      uint32_t r[32];
+      __syncwarp();
+      tc::tmem_ld32(to + c * 32, r);
+      tc::tmem_wait_ld();
+      if (w.parts > 1) {   // partial result: O (in units of 2^m_end), m_end and the sum, [channel][row]
+        float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;
-          if (c == 0) {
-            mine[D * 128 + row] = m_end;
-            mine[(D + 1) * 128 + row] = bad ? nan : l;
-          }
-        } else if (args.out_vec) {   // rows go through shared memory, so that the global stores are whole rows of 16-byte pieces
-          stage_row32<D>(stage, row, c, r, unit);
-        } else if (row < w.rows) {
-          __nv_bfloat16* orow = a.out + w.b * a.so[0] + hqr * a.so[1] + tokr * a.so[2] + c * 32;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) orow[i] = __float2bfloat16_rn(__uint_as_float(r[i]) * unit);
+        for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;
+        if (c == 0) {
+          mine[D * 128 + row] = m_end;
+          mine[(D + 1) * 128 + row] = bad ? nan : l;
         }
+      } else if (args.out_vec) {   // rows go through shared memory, so that the global stores are whole rows of 16-byte pieces
+        stage_row32<D>(stage, row, c, r, unit);
+      } else if (row < w.rows) {
+        __nv_bfloat16* orow = a.out + w.b * a.so[0] + hqr * a.so[1] + tokr * a.so[2] + c * 32;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) orow[i] = __float2bfloat16_rn(__uint_as_float(r[i]) * unit);
       }
     }
     if (w.parts == 1 && args.out_vec) {
@@ -602,8 +652,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       if (good) {
         constexpr int CPR = D / 8, RPI = 32 / CPR;
         const int k = lane % CPR;
-        for (int i = (warp - 4) * RPI + lane / CPR; i < w.rows; i += 12 * RPI) {
-          const int ri = w.row0 + i, tok = ri / a.G, hq = w.hk * a.G + ri - tok * a.G;
+#pragma unroll 1
+        for (int i = (warp - 4) * RPI + lane / CPR; i < w.rows; i += 16 * RPI) {
+          const int ri = w.row0 + i, tok = args.by_group.div(ri), hq = w.hk * a.G + ri - tok * a.G;
           *reinterpret_cast<uint4*>(a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + k * 8) = *stage_chunk<D>(stage, i, k);
         }
       }
@@ -639,7 +690,7 @@ __global__ void __launch_bounds__(256) prompt_combine_kernel(const __grid_consta
       l += lz == lz ? lz * wz[z] : lz;   // (a NaN row stays one where its weight is 0)
     }
   }
-  const int rg = w.row0 + row, tok = rg / a.G, hq = w.hk * a.G + rg - tok * a.G;
+  const int rg = w.row0 + row, tok = args.by_group.div(rg), hq = w.hk * a.G + rg - tok * a.G;
   __nv_bfloat16* out = a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + half * HD;
   const float inv = 1.f / l;
   for (int c = 0; c < HD; c += 8) {
@@ -696,6 +747,7 @@ kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool
   args.a = a;
   args.units = a.p.batch * a.p.Hkv;
   prompt_plan(args.units, a.p.T * a.G, tiles, args.qtiles, args.nsplit);
+  args.by_units = FastDiv(args.units); args.by_heads = FastDiv(a.p.Hkv); args.by_group = FastDiv(a.G);
   args.q_vec = q_vec ? 1 : 0; args.out_vec = out_vec ? 1 : 0;
   CUtensorMap mapK, mapV;
   const int64_t rows = a.p.n_pages * a.p.Hkv * a.p.page;
