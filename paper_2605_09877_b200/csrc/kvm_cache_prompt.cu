@@ -289,7 +289,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       int s = 0, issued = 0;
       uint32_t par = 0;
       for (int j = 0, k = 0, t = 0; j < w.ntiles; ++j) {
-        if (lane == 0) ok = j < ring || tc::mbar_wait(&bars[empty + s], par ^ 1);
+        if (lane == 0) ok = j < ring || tc::mbar_wait_tight(&bars[empty + s], par ^ 1);
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
         const bool mine = lt == t, nan = cur.ke > 127 || cur.ve > 127;
@@ -317,7 +317,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       if (lane == 0) {
         if (!ok) fail();
         // nothing may be in flight into shared memory when the CTA ends, whatever became of the others
-        for (int j = max(0, issued - ring); j < issued; ++j) tc::mbar_wait(&bars[full + j % ring], (j / ring) & 1);
+#pragma unroll 1
+        for (int j = max(0, issued - ring); j < issued; ++j) tc::mbar_wait_tight(&bars[full + j % ring], (j / ring) & 1);
       }
     } else if (warp == 1) {
       // ------------------------------ S ------------------------------
@@ -327,11 +328,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         constexpr uint32_t ID = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
         auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
         const uint64_t dQ = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
-        bool ok = tc::mbar_wait(&bars[PB_QFULL], 0);
+        bool ok = tc::mbar_wait_tight(&bars[PB_QFULL], 0);
         uint32_t s = 0, par = 0;   // ring of three: key tiles and accumulators
         for (int j = 0; j < w.ntiles && ok; ++j) {
-          ok = tc::mbar_wait(&bars[PB_KFULL + s], par);   // (long there, as a rule: not behind the wait that matters)
-          ok = ok && (j < Cfg::NACC || tc::mbar_wait(&bars[PB_PVDONE + s], par ^ 1));
+          ok = tc::mbar_wait_tight(&bars[PB_KFULL + s], par);   // (long there, as a rule: not behind the wait that matters)
+          ok = ok && (j < Cfg::NACC || tc::mbar_wait_tight(&bars[PB_PVDONE + s], par ^ 1));
           if (!ok) break;
           tc::tc_fence_after();
           const uint64_t k = dK + s * (Cfg::T8 >> 4);
@@ -354,7 +355,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         uint32_t s = 0, par = 0;
         bool ok = true;
         for (int j = 0; j < w.ntiles; ++j) {
-          ok = tc::mbar_wait(&bars[PB_READY + s], par);
+          ok = tc::mbar_wait_tight(&bars[PB_READY + s], par);
           if (!ok) break;
           tc::tc_fence_after();
           const uint64_t v = dV + (j & 1) * (Cfg::T16 >> 4);
@@ -375,12 +376,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     constexpr int PIECES = D / 16;             // 16-byte pieces of a row of codes
     constexpr int N = PIECES / 4;              // a warp's lanes take eight rows and four pieces at a time: no two share a bank
     const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
-    bool ok = tc::mbar_wait(&bars[PB_QFULL], 0);   // (the queries lay where the first tiles go)
+    bool ok = tc::mbar_wait_tight(&bars[PB_QFULL], 0);   // (the queries lay where the first tiles go)
     uint32_t s3 = 0;
     for (int j = 0; j < w.ntiles; ++j) {
       const int sv = j & 1, s8 = j % Cfg::NV8;
-      bool good = ok && tc::mbar_wait(&bars[PB_V8FULL + s8], (j / Cfg::NV8) & 1);
-      if (good && j >= Cfg::NV) good = tc::mbar_wait(&bars[PB_VFREE + sv], ((j >> 1) - 1) & 1);
+      bool good = ok && tc::mbar_wait_tight(&bars[PB_V8FULL + s8], (j / Cfg::NV8) & 1);
+      if (good && j >= Cfg::NV) good = tc::mbar_wait_tight(&bars[PB_VFREE + sv], ((j >> 1) - 1) & 1);
       ok = __all_sync(0xffffffffu, good);
       if (!ok) break;
       const ValueTile& vt = vinfo[s8];
@@ -486,7 +487,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll 1
     for (int j = group; j < w.ntiles; j += 2, flip ^= 1) {
       const uint32_t ts = lanes + Cfg::COL_S + 128 * s, sb = s == 0 ? 2 : s - 1, parb = s == 0 ? par ^ 1 : par;   // (sb, parb: of the tile before)
-      if (!tc::mbar_wait(&bars[PB_SFULL + s], par)) ok = false;
+      if (!tc::mbar_wait_tight(&bars[PB_SFULL + s], par)) ok = false;
       __syncwarp();
       tc::tc_fence_after();
       const PromptTile& ti = info[j % kInfo];
@@ -542,7 +543,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
       float m = -INFINITY;
       if (j > 0) {
-        if (!tc::mbar_wait(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
+        if (!tc::mbar_wait_tight(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
         __syncwarp();
         m = s_m[row];
       }
@@ -550,7 +551,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const float mnew = fmaxf(m, mx);
         if (j > 0) {
           // all earlier P V products must have landed before O is touched; each warp takes half of the channels
-          if (!tc::mbar_wait(&bars[PB_PVDONE + sb], parb)) ok = false;
+          if (!tc::mbar_wait_tight(&bars[PB_PVDONE + sb], parb)) ok = false;
           __syncwarp();
           tc::tc_fence_after();
           const float corr = (m == -INFINITY) ? 0.f : tc::ex2_approx(m - mnew);
@@ -609,7 +610,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       unpack2(add2(s0, s1), l0, l1);
       l_run += l0 + l1;
     }
-    if (ok) ok = tc::mbar_wait(&bars[PB_LAST], 0);
+    if (ok) ok = tc::mbar_wait_tight(&bars[PB_LAST], 0);
     if (!ok) fail();
     __syncwarp();
     tc::tc_fence_after();
