@@ -297,11 +297,17 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       }
       return x;
     };
-    Page cur = fetch(0), nxt = fetch(1);
+    Page cur{}, nxt{};
     bool ok = true;
     int s = 0, issued = 0;
     uint32_t par = 0;
-    for (int k = 0, t = 0; issued < ntile; ++issued) {
+    int ahead = 0, t = tpb;   // batches of pages fetched so far, tiles of the current one that are issued
+    for (; issued < ntile; ++issued) {
+      if (t == tpb) {
+        t = 0;
+#pragma unroll 1
+        do { cur = nxt; nxt = fetch(ahead++); } while (ahead < 2);   // (one batch is always on its way)
+      }
       if (lane == 0) ok = !*abort_flag && (issued < ST || tc::mbar_wait_tight(&bars[Cfg::FREE + s], par ^ 1));
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
@@ -326,7 +332,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         tc::tma_load_2d(dst + Cfg::TILE, &mapV, &bars[Cfg::FULL + s], 0, cur.row);
       }
       if (++s == ST) { s = 0; par ^= 1; }
-      if (++t == tpb) { t = 0; ++k; cur = nxt; nxt = fetch(k + 1); }
+      ++t;
     }
     if (lane == 0) {
       if (!ok) fail();
@@ -545,18 +551,41 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       const float lw = sum_lanes<NC>(l_run, lane);
       if ((lane & (32 / NC - 1)) == 0) s_l[(lane / (32 / NC)) * 4 + w4] = lw;
       group_barrier(g, true);
-      float* part = a.part + (int64_t)(2 * worker + (pflags & kBegins ? 1 : 0)) * NC * (D + 2);
+      if (pflags & kWhole) {
+        // (each thread's channel of the columns through its own bytes of the weights, which nothing reads now: the loop over the columns
+        // stays small)
+        uint32_t h[NC / 2];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (c >= ncol) continue;
-        const float4 l4 = *reinterpret_cast<const float4*>(s_l + 4 * c);
-        const float l = (l4.x + l4.y) + (l4.z + l4.w);
-        if (pflags & kWhole) {
-          const int t = a.p.T == 1 ? 0 : c / a.G, hq = phk * a.G + c - t * a.G;
-          if (tok < D) a.out[pb * a.so[0] + hq * a.so[1] + t * a.so[2] + tok] = __float2bfloat16_rn(__fdividef(o_run[c], l));
-        } else {
+        for (int c = 0; c < NC; c += 2) {
+          float x[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float4 l4 = *reinterpret_cast<const float4*>(s_l + 4 * (c + k));
+            x[k] = __fdividef(o_run[c + k], (l4.x + l4.y) + (l4.z + l4.w));
+          }
+          const __nv_bfloat162 b2 = __floats2bfloat162_rn(x[0], x[1]);
+          h[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+        }
+        *reinterpret_cast<uint4*>(sP) = make_uint4(h[0], h[1], h[2], h[3]);
+        if (NC == 16) *reinterpret_cast<uint4*>(sP + 2048) = make_uint4(h[NC / 2 - 4], h[NC / 2 - 3], h[NC / 2 - 2], h[NC / 2 - 1]);
+        __nv_bfloat16* o = a.out + pb * a.so[0] + (int64_t)phk * a.G * a.so[1] + tok;
+        int hg = 0;
+#pragma unroll 1
+        for (int c = 0; c < ncol; ++c) {
+          if (tok < D) *o = *reinterpret_cast<const __nv_bfloat16*>(sP + (c >> 3) * 2048 + (c & 7) * 2);
+          o += a.so[1];
+          if (++hg == a.G) { hg = 0; o += a.so[2] - a.G * a.so[1]; }
+        }
+      } else {
+        float* part = a.part + (int64_t)(2 * worker + (pflags & kBegins ? 1 : 0)) * NC * (D + 2);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {   // (columns that are not in use give something that nobody reads)
           if (tok < D) part[c * (D + 2) + tok] = o_run[c];
-          if (tok == c) { part[c * (D + 2) + D] = (i == n_mine - 1) ? m_run : m_old; part[c * (D + 2) + D + 1] = l; }
+          if (tok == c) {
+            const float4 l4 = *reinterpret_cast<const float4*>(s_l + 4 * c);
+            part[c * (D + 2) + D] = (i == n_mine - 1) ? m_run : m_old;
+            part[c * (D + 2) + D + 1] = (l4.x + l4.y) + (l4.z + l4.w);
+          }
         }
       }
       group_barrier(g, true);   // (s_l is free again)

@@ -216,6 +216,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (warp >= 4 && warp < 20) {
       uint8_t* raw = base + Cfg::OFF_V;
       constexpr int CPR = D / 8;   // 16-byte pieces of a row
+#pragma unroll 1
       for (int i = tid - 128; i < 128 * CPR; i += 512) {
         const int r = i / CPR, c = i % CPR, rg = w.row0 + r, tok = args.by_group.div(rg), hq = w.hk * a.G + rg - tok * a.G;
         uint4* dst = reinterpret_cast<uint4*>(raw + r * (2 * D) + ((c ^ (r & 7)) << 4));
@@ -232,6 +233,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     int v = -1000;
+#pragma unroll 1
     for (int i = tid - 32; i < w.ntiles * ppt; i += kThreads - 32) {
       int p0;
       const int page = page_of(i, p0);
@@ -284,11 +286,16 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         return g;
       };
-      Page cur = fetch(0), nxt = fetch(1);
+      Page cur{}, nxt{};
       bool ok = true;
       int s = 0, issued = 0;
       uint32_t par = 0;
-      for (int j = 0, k = 0, t = 0; j < w.ntiles; ++j) {
+      for (int j = 0, ahead = 0, t = tpb; j < w.ntiles; ++j) {   // (ahead: batches of pages fetched; t: tiles of the current one that are issued)
+        if (t == tpb) {
+          t = 0;
+#pragma unroll 1
+          do { cur = nxt; nxt = fetch(ahead++); } while (ahead < 2);   // (one batch is always on its way)
+        }
         if (lane == 0) ok = j < ring || tc::mbar_wait_tight(&bars[empty + s], par ^ 1);
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
@@ -312,7 +319,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         if (mine && cur.row >= 0) tc::tma_load_2d(tiles + s * Cfg::T8 + lp * p.page * D, map, &bars[full + s], 0, cur.row);
         issued = j + 1;
         if (++s == ring) { s = 0; par ^= 1; }
-        if (++t == tpb) { t = 0; ++k; cur = nxt; nxt = fetch(k + 1); }
+        ++t;
       }
       if (lane == 0) {
         if (!ok) fail();
