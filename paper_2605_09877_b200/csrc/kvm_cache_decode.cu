@@ -39,7 +39,8 @@ constexpr float kPShift = 8.f;   // the largest weight of a tile is 2^8 (e4m3 en
 
 struct TileInfo {
   int pos, b, hk, flags;   // first key position; unit; kFirst ...
-  int vmax, start, n, pad; // largest exponent of the visible blocks' value scales; lengths of the sequence
+  int vmax, start, n;      // largest exponent of the visible blocks' value scales; lengths of the sequence
+  int ze;                  // last worker that has tiles of the unit
   int16_t ke[8], ve[8];    // exponents of the scales per page of the tile
 };
 enum { kFirst = 1, kLast = 2, kWhole = 4, kBegins = 8 };   // first / last tile of the worker's share of the unit; the share is all of it / begins with it
@@ -70,8 +71,12 @@ struct DecodeCfg {
   static_assert(COUNT * 8 + 64 <= 1024, "barriers");
 };
 
+// What a worker leaves for combine_kernel beside its partial results: the unit that begins in its share and goes on in the next one's (b < 0: none).
+struct Cut { int b, hk, n, ze; };
+
 struct DecodeArgs8 {
   AttendArgs a;
+  Cut* cuts;     // [workers]
   int grid;      // CTAs
   int q_vec;
 };
@@ -80,9 +85,9 @@ struct DecodeArgs8 {
 // tiles in the order of their number within the share, group by group.
 template <int NG>
 struct Shares {
-  int f0[NG], n[NG];
+  int f0[NG], n[NG], share;
   __device__ __forceinline__ Shares(int total, int grid, int cta) {
-    const int share = (total + grid * NG - 1) / (grid * NG);
+    share = (total + grid * NG - 1) / (grid * NG);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       f0[g] = min(total, (g * grid + cta) * share);
@@ -159,9 +164,9 @@ __device__ __forceinline__ int seq_of(const int* pre, int batch, int f) {
   return lo;
 }
 
-// pre[0 .. batch]: tiles of the sequences before b, all heads; by all NT threads of the block.  bad(): lengths that are not allowed
-template <int NT, class F>
-__device__ __forceinline__ void list_tiles(const AttendArgs& a, int* pre, int* scratch, F bad) {
+// pre[0 .. batch]: tiles of the sequences before b, all heads; by all NT threads of the block
+template <int NT>
+__device__ __forceinline__ void list_tiles(const AttendArgs& a, int* pre, int* scratch) {
   const Params& p = a.p;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int per = (p.batch + NT - 1) / NT, b0 = tid * per;
@@ -169,7 +174,10 @@ __device__ __forceinline__ void list_tiles(const AttendArgs& a, int* pre, int* s
 #pragma unroll 1
   for (int b = b0; b < min(b0 + per, p.batch); ++b) {
     int start, n;
-    if (!seq_lengths(p, b, start, n)) { bad(); start = n = 0; }
+    if (!seq_lengths(p, b, start, n)) {
+      if (blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
+      start = n = 0;
+    }
     pre[b] = sum;
     sum += seq_tiles(a, start, n) * p.Hkv;
   }
@@ -247,7 +255,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   tc::tc_fence_before();
-  list_tiles<Cfg::THREADS>(a, pre, reinterpret_cast<int*>(base + Cfg::OFF_AB), [&]() { if (blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG); });
+  list_tiles<Cfg::THREADS>(a, pre, reinterpret_cast<int*>(base + Cfg::OFF_AB));
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Shares<NG> sh(pre[p.batch], args.grid, blockIdx.x);
@@ -265,9 +273,9 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     // ------------------------------ producer ------------------------------
     const int tshift = 7 - p.page_shift, ppt = 1 << tshift, tpb = 32 >> tshift;   // pages of a tile; tiles whose pages the warp's lanes hold at a time
     const int lt = lane >> tshift, lp = lane & (ppt - 1);
-    struct Page { int row, ke, ve, pos, b, hk, flags, start, n; };   // row < 0: not loaded
+    struct Page { int row, ke, ve, pos, b, hk, flags, start, n, ze; };   // row < 0: not loaded
     auto fetch = [&](int k) {
-      Page x{-1, 0, 0, 0, 0, 0, 0, 0, 0};
+      Page x{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0};
       const int jj = k * tpb + lt;
       if (jj < ntile) {
         int i, g;
@@ -281,6 +289,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         x.b = b; x.hk = hk; x.pos = tile_at(t, it) * kTile;
         x.flags = (it == 0 || i == 0 ? kFirst : 0) | (it == t.n - 1 || i == n - 1 ? kLast : 0) | (u0 >= F0 ? kBegins : 0) |
                   (u0 >= F0 && u0 + t.n <= F0 + n ? kWhole : 0);
+        x.ze = (u0 + t.n - 1) / sh.share;
         const int p0 = x.pos + lp * p.page;   // the page is needed if any token of the call sees any of its positions
         if (p0 <= last && (p0 + p.page > x.start - a.window + 1 || p0 < a.sinks)) {
           const int page = p.pages[(int64_t)b * p.max_pages + (p0 >> p.page_shift)];
@@ -303,10 +312,10 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     uint32_t par = 0;
     int ahead = 0, t = tpb;   // batches of pages fetched so far, tiles of the current one that are issued
     for (; issued < ntile; ++issued) {
-      if (t == tpb) {
-        t = 0;
-#pragma unroll 1
-        do { cur = nxt; nxt = fetch(ahead++); } while (ahead < 2);   // (one batch is always on its way)
+      if (t == tpb && ahead > 0) { t = 0; cur = nxt; }
+      if (ahead == 0 || t == 1) {   // (the next batch, behind the first tile of the one before)
+        nxt = fetch(ahead++);
+        if (ahead == 1) { cur = nxt; t = 0; }
       }
       if (lane == 0) ok = !*abort_flag && (issued < ST || tc::mbar_wait_tight(&bars[Cfg::FREE + s], par ^ 1));
       ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -319,7 +328,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         ti.ke[lp] = (int16_t)cur.ke;
         ti.ve[lp] = (int16_t)cur.ve;
         if (lp == 0) {
-          ti.pos = cur.pos; ti.b = cur.b; ti.hk = cur.hk; ti.flags = cur.flags; ti.start = cur.start; ti.n = cur.n;
+          ti.pos = cur.pos; ti.b = cur.b; ti.hk = cur.hk; ti.flags = cur.flags; ti.start = cur.start; ti.n = cur.n; ti.ze = cur.ze;
           ti.vmax = v == -1000 ? 0 : v;
         }
       }
@@ -515,7 +524,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     float o_run[NC], l_run[NC], l_new[NC];
     float m_run = -INFINITY, m_old = -INFINITY;   // (threads below NC: running reference of column tok)
     int seg = -1;
-    int pb = 0, phk = 0, pflags = 0, pn = 0;      // the tile before
+    int pb = 0, phk = 0, pflags = 0, pn = 0, pze = 0;   // the tile before
     bool ok = true;
     auto columns = [&](uint32_t at, float (&y)[NC]) {   // hi + lo
       if (NC == 8) {
@@ -595,7 +604,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll 1
     for (int i = 0; i <= n_mine && n_mine > 0; ++i) {   // (the last time round only the products of the tile before are left)
       float y[NC];
-      int flags = 0, b = 0, hk = 0, vmax = 0, n = 0, vr = 0;
+      int flags = 0, b = 0, hk = 0, vmax = 0, n = 0, ze = 0, vr = 0;
       bool dropped = false;
       if (i < n_mine) {
         if (!tc::mbar_wait_tight(&bars[Cfg::SFULL + 2 * g + (i & 1)], (i >> 1) & 1)) ok = false;
@@ -606,7 +615,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         columns(lanes + NB * (i & 1), y);
         const TileInfo& ti = info[s];
         const int pos = ti.pos, start = ti.start;
-        flags = ti.flags; b = ti.b; hk = ti.hk; vmax = ti.vmax; n = ti.n;
+        flags = ti.flags; b = ti.b; hk = ti.hk; vmax = ti.vmax; n = ti.n; ze = ti.ze;
         const int ke = ti.ke[tok >> p.page_shift], ve = ti.ve[tok >> p.page_shift];
         if (flags & kFirst) {
           // (four slots: the factors of unit seg + 4 are written after the products of seg + 2, hence after this thread's use of seg's)
@@ -703,10 +712,11 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::tc_fence_before();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[Cfg::PFULL + g]);
-      pb = b; phk = hk; pflags = flags; pn = n;
+      pb = b; phk = hk; pflags = flags; pn = n; pze = ze;
       s += sh.active(i);
       if (s >= ST) { s -= ST; par ^= 1; }
     }
+    if (tok == 0) args.cuts[worker] = Cut{ok && (pflags & (kBegins | kWhole)) == kBegins ? pb : -1, phk, pn, pze};
     if (!ok) fail();
   }
   tc::tc_fence_before();
@@ -717,65 +727,72 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   }
 }
 
-// Units that several workers shared: out = sum_z 2^(m_z - m) O_z / sum_z 2^(m_z - m) l_z.  Block w stands for the border between workers w - 1 and
-// w, and merges the unit that it cuts when it is the first border to cut it.  Threads: D channels, 256 / D parts of the list of workers.
+// Units that several workers shared: out = sum_z 2^(m_z - m) O_z / sum_z 2^(m_z - m) l_z.  Block (w, c): column c of the unit that begins in worker
+// w's share and goes on behind it, if there is one.  Threads: D channels, 256 / D parts of the list of workers, eight of them in flight.
 template <int D, int NC>
 __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ DecodeArgs8 args) {
-  constexpr int NG = DecodeCfg<D, NC>::NG, ZP = 256 / D;
+  constexpr int ZP = 256 / D;
   const AttendArgs& a = args.a;
-  const Params& p = a.p;
-  extern __shared__ int pre[];
-  __shared__ int s_scan[8];
   __shared__ float s_o[ZP][D], s_ml[ZP][2];
-  list_tiles<256>(a, pre, s_scan, []() {});   // (beside the end of the kernel before: the lengths are its inputs too)
-  const int total = pre[p.batch], workers = args.grid * NG;
-  const int share = (total + workers - 1) / workers, z1 = blockIdx.x + 1;
-  const int64_t f = (int64_t)z1 * share;
-  if (z1 >= workers || f >= total) return;
-  const int b = seq_of(pre, p.batch, (int)f), nt = (pre[b + 1] - pre[b]) / p.Hkv, hk = ((int)f - pre[b]) / nt, u0 = pre[b] + hk * nt;
-  if (u0 == f || u0 / share != z1 - 1) return;   // (not cut here, or cut before)
-  const int z0 = z1 - 1, ze = (u0 + nt - 1) / share;
-  const int n = p.count ? p.count[b] : (int)p.T;
-  const int64_t stride = 2 * NC * (D + 2);
-  const int ch = threadIdx.x % D, zp = threadIdx.x / D;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Cut cut = args.cuts[blockIdx.x];
+  const int c = blockIdx.y, z0 = blockIdx.x;
+  if (cut.b < 0 || c >= cut.n * a.G) return;
+  const int ch = threadIdx.x % D, zp = threadIdx.x / D;
   // the first worker's share begins with the unit (slot 1), those of the others in its middle (slot 0)
-  for (int c = 0; c < n * a.G; ++c) {
-    float m = -INFINITY, o = 0.f, l = 0.f;
-    for (int z = z0 + zp; z <= ze; z += ZP) {
-      const float* r = a.part + z * stride + ((z == z0 ? NC : 0) + c) * (D + 2);
-      const float mz = r[D], mn = fmaxf(m, mz);
-      const float f0 = m == -INFINITY ? 0.f : tc::ex2_approx(m - mn), f1 = mz == -INFINITY ? 0.f : tc::ex2_approx(mz - mn);
-      o = fmaf(o, f0, r[ch] * f1);
-      l = fmaf(l, f0, r[D + 1] * f1);
-      m = mn;
-    }
-    if (c > 0) __syncthreads();
-    s_o[zp][ch] = o;
-    if (ch == 0) { s_ml[zp][0] = m; s_ml[zp][1] = l; }
-    __syncthreads();
-    if (zp == 0) {
-      float mm = s_ml[0][0];
+  const float* first = a.part + (int64_t)z0 * 2 * NC * (D + 2) + c * (D + 2);
+  float m = -INFINITY, o = 0.f, l = 0.f;
+  for (int z = zp; z <= cut.ze - z0; z += 8 * ZP) {
+    float mz[8], lz[8], oz[8];
 #pragma unroll
-      for (int z = 1; z < ZP; ++z) mm = fmaxf(mm, s_ml[z][0]);
-      o = l = 0.f;
-#pragma unroll
-      for (int z = 0; z < ZP; ++z) {
-        const float fz = s_ml[z][0] == -INFINITY ? 0.f : tc::ex2_approx(s_ml[z][0] - mm);
-        o = fmaf(s_o[z][ch], fz, o);
-        l = fmaf(s_ml[z][1], fz, l);
+    for (int k = 0; k < 8; ++k) {
+      const int zk = z + k * ZP;
+      mz[k] = -INFINITY; lz[k] = oz[k] = 0.f;
+      if (zk <= cut.ze - z0) {
+        const float* r = first + (int64_t)zk * 2 * NC * (D + 2) + (zk == 0 ? NC * (D + 2) : 0);
+        mz[k] = r[D]; lz[k] = r[D + 1]; oz[k] = r[ch];
       }
-      const int t = c / a.G, hq = hk * a.G + c - t * a.G;
-      a.out[b * a.so[0] + hq * a.so[1] + t * a.so[2] + ch] = __float2bfloat16_rn(o / l);
+    }
+    float mn = m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mn = fmaxf(mn, mz[k]);
+    const float f = m == -INFINITY ? 0.f : tc::ex2_approx(m - mn);
+    o *= f;
+    l *= f;
+    m = mn;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = mz[k] == -INFINITY ? 0.f : tc::ex2_approx(mz[k] - m);
+      o = fmaf(oz[k], w, o);
+      l = fmaf(lz[k], w, l);
     }
   }
+  s_o[zp][ch] = o;
+  if (ch == 0) { s_ml[zp][0] = m; s_ml[zp][1] = l; }
+  __syncthreads();
+  if (zp > 0) return;
+  float mm = s_ml[0][0];
+#pragma unroll
+  for (int z = 1; z < ZP; ++z) mm = fmaxf(mm, s_ml[z][0]);
+  o = l = 0.f;
+#pragma unroll
+  for (int z = 0; z < ZP; ++z) {
+    const float w = s_ml[z][0] == -INFINITY ? 0.f : tc::ex2_approx(s_ml[z][0] - mm);
+    o = fmaf(s_o[z][ch], w, o);
+    l = fmaf(s_ml[z][1], w, l);
+  }
+  const int t = c / a.G, hq = cut.hk * a.G + c - t * a.G;
+  a.out[cut.b * a.so[0] + hq * a.so[1] + t * a.so[2] + ch] = __float2bfloat16_rn(o / l);
 }
 
 // At most so many CTAs have tiles: `units` units of at most `tiles` tiles each.
 static int decode_grid(int64_t units, int64_t tiles) { return (int)std::min<int64_t>(kCtas, units * tiles); }
 
+static int64_t decode_partials(int workers, int d, int cols) { return (int64_t)workers * 2 * (cols <= 8 ? 8 : 16) * (d + 2) * 4; }   // bytes
+
 int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols) {
-  return (int64_t)decode_grid(units, tiles) * (cols <= 8 ? 4 : 3) * 2 * (cols <= 8 ? 8 : 16) * (d + 2) * 4;
+  const int workers = decode_grid(units, tiles) * (cols <= 8 ? 4 : 3);
+  return decode_partials(workers, d, cols) + workers * (int64_t)sizeof(Cut);
 }
 
 template <int D, int NC>
@@ -793,8 +810,7 @@ static kvm_status_t launch_decode_nc(const DecodeArgs8& args, const CUtensorMap&
   }
   decode_kernel<D, NC><<<args.grid, Cfg::THREADS, smem, s>>>(mapK, mapV, args);
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(args.grid * Cfg::NG); lc.blockDim = dim3(256); lc.stream = s;
-  lc.dynamicSmemBytes = (args.a.p.batch + 1) * 4;
+  lc.gridDim = dim3(args.grid * Cfg::NG, (unsigned)(args.a.p.T * args.a.G)); lc.blockDim = dim3(256); lc.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -807,11 +823,13 @@ kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cuda
   DecodeArgs8 args;
   args.a = a;
   args.grid = decode_grid((int64_t)a.p.batch * a.p.Hkv, tiles);
+  const int cols = (int)(a.p.T * a.G);
+  args.cuts = reinterpret_cast<Cut*>(reinterpret_cast<uint8_t*>(a.part) + decode_partials(args.grid * (cols <= 8 ? 4 : 3), a.d, cols));
   args.q_vec = q_vec ? 1 : 0;
   CUtensorMap mapK, mapV;
   const int64_t rows = a.p.n_pages * a.p.Hkv * a.p.page;
   if (!encode_tmap_codes(&mapK, a.p.k, a.d, rows, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, rows, a.p.page)) return KVM_ERR_CUDA;
-  const bool few = a.p.T * a.G <= 8;
+  const bool few = cols <= 8;
   if (a.d == 128) return few ? launch_decode_nc<128, 8>(args, mapK, mapV, s) : launch_decode_nc<128, 16>(args, mapK, mapV, s);
   return few ? launch_decode_nc<64, 8>(args, mapK, mapV, s) : launch_decode_nc<64, 16>(args, mapK, mapV, s);
 }
