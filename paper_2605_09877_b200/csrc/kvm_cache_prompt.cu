@@ -89,7 +89,7 @@ struct PromptCfg {
 // PB_READY: P of the tile is in tensor memory (8 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
 // 32 rows are decided for a tile, [row quarter][tile % 3]
 enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 10, PB_VFREE = 14, PB_SFULL = 16, PB_READY = 19, PB_PVDONE = 22, PB_QFULL = 25,
-       PB_REF = 26, PB_LAST = 38, PB_COUNT = 39 };
+       PB_REF = 26, PB_LAST = 38, PB_VBASE = 39, PB_COUNT = 40 };
 
 // What a CTA does: its rows and its key tiles.  (Also what the merge needs to know.)
 struct PromptWork {
@@ -172,11 +172,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + PB_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [24]
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [4]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   PromptWork w;
   if (!prompt_work(args, blockIdx.x, blockIdx.y, w)) return;
 
+  // Set-up: the barriers, tensor memory, and no other barrier of the whole CTA: the producers, the queries' conversion and the search for vbase
+  // (each a chain of loads) run side by side from here on.
   if (tid == 0) {
     tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
     for (int s = 0; s < 3; ++s) {
@@ -191,6 +193,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     for (int s = 0; s < 12; ++s) tc::mbar_init(&bars[PB_REF + s], 2);
     tc::mbar_init(&bars[PB_QFULL], 16);
     tc::mbar_init(&bars[PB_LAST], 1);
+    tc::mbar_init(&bars[PB_VBASE], 4);
     *abort_flag = 0;
     tc::fence_barrier_init();
   }
@@ -206,53 +209,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     const int page = p.pages[(int64_t)w.b * p.max_pages + (p0 >> p.page_shift)];
     return page >= 0 && page < p.n_pages ? page : -2;
   };
-  // The producer of keys needs nothing but the barriers that its own thread has set up: it starts at once, beside the search for vbase.
-  int vbase = 0;
-  if (warp == 0) {
-    __syncwarp();
-    asm volatile("barrier.cta.arrive 2, %0;" ::"n"(kThreads) : "memory");
-  } else {
-    // the queries as they are, to where the fp16 values will be (the converting warps wait for them to be used up)
-    if (warp >= 4 && warp < 20) {
-      uint8_t* raw = base + Cfg::OFF_V;
-      constexpr int CPR = D / 8;   // 16-byte pieces of a row
-#pragma unroll 1
-      for (int i = tid - 128; i < 128 * CPR; i += 512) {
-        const int r = i / CPR, c = i % CPR, rg = w.row0 + r, tok = args.by_group.div(rg), hq = w.hk * a.G + rg - tok * a.G;
-        uint4* dst = reinterpret_cast<uint4*>(raw + r * (2 * D) + ((c ^ (r & 7)) << 4));
-        const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tok * a.sq[2] + 8 * c;
-        if (r >= w.rows) {
-          *dst = make_uint4(0, 0, 0, 0);
-        } else if (args.q_vec) {
-          copy16_async(dst, src);
-        } else {
-#pragma unroll 1
-          for (int e = 0; e < 8; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[e] = src[e];
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    int v = -1000;
-#pragma unroll 1
-    for (int i = tid - 32; i < w.ntiles * ppt; i += kThreads - 32) {
-      int p0;
-      const int page = page_of(i, p0);
-      if (page < 0) continue;
-      const int e = scale_exp(p.vs[page * p.Hkv + w.hk]);
-      if (e < 128) v = max(v, e);
-    }
-    v = __reduce_max_sync(0xffffffffu, v);
-    if (lane == 0) s_vmax[warp] = v;
-    tc::tc_fence_before();
-    __syncwarp();
-    asm volatile("barrier.cta.sync 2, %0;" ::"n"(kThreads) : "memory");
-    tc::tc_fence_after();
-    vbase = -1000;
-#pragma unroll
-    for (int i = 1; i < kThreads / 32; ++i) vbase = max(vbase, s_vmax[i]);
-    if (vbase == -1000) vbase = 0;
-  }
-  const uint32_t tmem = warp == 0 ? 0 : *tmem_slot;
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // largest exponent of the visible blocks' value scales, found by the converting warps (complete behind PB_VBASE)
+  auto vbase_found = [&]() {
+    const int v = max(max(s_vmax[0], s_vmax[1]), max(s_vmax[2], s_vmax[3]));
+    return v == -1000 ? 0 : v;
+  };
 
   auto fail = [&]() {
     if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
@@ -286,6 +251,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         return g;
       };
+      int vbase = 0;
+      if (!keys) {
+        tc::mbar_wait_tight(&bars[PB_VBASE], 0);   // (should it run out, so do the waits for what comes after)
+        vbase = vbase_found();
+      }
       Page cur{}, nxt{};
       bool ok = true;
       int s = 0, issued = 0;
@@ -383,6 +353,22 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     constexpr int PIECES = D / 16;             // 16-byte pieces of a row of codes
     constexpr int N = PIECES / 4;              // a warp's lanes take eight rows and four pieces at a time: no two share a bank
     const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
+    {
+      int v = -1000;
+#pragma unroll 1
+      for (int i = tid - 640; i < w.ntiles * ppt; i += 128) {
+        int p0;
+        const int page = page_of(i, p0);
+        if (page < 0) continue;
+        const int e = scale_exp(p.vs[page * p.Hkv + w.hk]);
+        if (e < 128) v = max(v, e);
+      }
+      v = __reduce_max_sync(0xffffffffu, v);
+      if (lane == 0) {
+        s_vmax[warp - 20] = v;
+        tc::mbar_arrive(&bars[PB_VBASE]);
+      }
+    }
     bool ok = tc::mbar_wait_tight(&bars[PB_QFULL], 0);   // (the queries lay where the first tiles go)
     uint32_t s3 = 0;
     for (int j = 0; j < w.ntiles; ++j) {
@@ -438,6 +424,25 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     // ------------------------------ q; softmax; results ------------------------------
     const int group = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
     auto all_barrier = []() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+    // the queries as they are, to where the fp16 values will be (the converting warps wait for them to be used up)
+    {
+      uint8_t* raw = base + Cfg::OFF_V;
+      constexpr int CPR = D / 8;   // 16-byte pieces of a row
+#pragma unroll 1
+      for (int i = tid - 128; i < 128 * CPR; i += 512) {
+        const int r = i / CPR, c = i % CPR, rg = w.row0 + r, tok = args.by_group.div(rg), hq = w.hk * a.G + rg - tok * a.G;
+        uint4* dst = reinterpret_cast<uint4*>(raw + r * (2 * D) + ((c ^ (r & 7)) << 4));
+        const __nv_bfloat16* src = a.q + w.b * a.sq[0] + hq * a.sq[1] + tok * a.sq[2] + 8 * c;
+        if (r >= w.rows) {
+          *dst = make_uint4(0, 0, 0, 0);
+        } else if (args.q_vec) {
+          copy16_async(dst, src);
+        } else {
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[e] = src[e];
+        }
+      }
+    }
     {
       // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys; D / 16 threads per row
       constexpr int TPR = D / 16;
@@ -632,7 +637,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     bad = s_l[512 + row] + s_l[640 + row] + s_l[768 + row] + s_l[896 + row] != 0.f;
     uint8_t* stage = base + Cfg::OFF_Q;   // (the queries are not needed any more)
     const int rg = w.row0 + row, tokr = args.by_group.div(rg), hqr = w.hk * a.G + rg - tokr * a.G;
-    const float unit = bad ? nan : w.parts == 1 ? exp2i(vbase) / l : exp2i(vbase);
+    const float vunit = exp2i(vbase_found()), unit = bad ? nan : w.parts == 1 ? vunit / l : vunit;
     if (good && part4 < D / 32) {
       const int c = part4;   // 32 channels
       uint32_t r[32];
