@@ -73,6 +73,19 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t c) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+// Two values below 2^8 as sums of two e4m3 numbers each, hi + lo (a in the low bytes).  By way of fp16, which holds 8-bit significands exactly
+// down to 2^-14 and their part above 2^-24 below: far less than the 2^-10 that e4m3 leaves.
+__device__ __forceinline__ void split_e4m3x2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __half2 y = __floats2half2_rn(a, b);
+  uint16_t h, l;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(h) : "r"(*reinterpret_cast<const uint32_t*>(&y)));
+  const uint32_t back = e4m3x2_to_f16x2(h);
+  const __half2 d = __hsub2(y, *reinterpret_cast<const __half2*>(&back));   // (exact: a difference of neighbours)
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l) : "r"(*reinterpret_cast<const uint32_t*>(&d)));
+  hi = h;
+  lo = l;
+}
+
 struct AttendArgs {
   Params p;
   const __nv_bfloat16* q;

@@ -485,9 +485,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
             const float y0 = bad ? 0.f : x[4 * k + 2 * q] * mul, y1 = bad ? 0.f : x[4 * k + 2 * q + 1] * mul;
-            h2[q] = to_e4m3x2(y0, y1);
-            const float2 back = e4m3x2_to_float2(h2[q]);
-            l2[q] = to_e4m3x2(y0 - back.x, y1 - back.y);
+            split_e4m3x2(y0, y1, h2[q], l2[q]);
           }
           hi[k] = h2[0] | (h2[1] << 16);
           lo[k] = l2[0] | (l2[1] << 16);

@@ -472,10 +472,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         for (int q = 0; q < 8; ++q) {
           const uint32_t v = nan ? 0u : x[q];
           const float y0 = __uint_as_float(v << 16) * mul, y1 = __uint_as_float(v & 0xffff0000u) * mul;
-          const uint32_t h = to_e4m3x2(y0, y1);
-          const float2 back = e4m3x2_to_float2(h);
+          uint32_t h, l;
+          split_e4m3x2(y0, y1, h, l);
           hi[q >> 1] |= h << (16 * (q & 1));
-          lo[q >> 1] |= to_e4m3x2(y0 - back.x, y1 - back.y) << (16 * (q & 1));
+          lo[q >> 1] |= l << (16 * (q & 1));
         }
         uint8_t* at = base + Cfg::OFF_Q + r * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);

@@ -40,24 +40,23 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
   }
   return false;
 }
-// The same in as few instructions as there are, and asking for a long suspension (the hint, in ns) before the instruction gives up: for kernels
-// whose warps do many different things.  The loop above is unrolled at every use, and its polls take issue slots from the warps that
-// have work.  At most kTightTries suspensions: about two seconds.
-constexpr uint32_t kTightHint = 1000000, kTightTries = 2000;
+// The same in as few instructions as there are, for kernels whose warps do many different things: the loop above is unrolled at every
+// use, and there the fetching of instructions is what a wait costs (each try suspends the thread for a while by itself; with a hint
+// for a long suspension the shortest calls took 2 us longer).
 __device__ __forceinline__ bool mbar_wait_tight(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
       "mov.u32 n, %3;\n\t"
       "AGAIN:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %4;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "@p bra DONE;\n\t"
       "sub.u32 n, n, 1;\n\t"
       "setp.ne.u32 p, n, 0;\n\t"
       "@p bra AGAIN;\n\t"
       "DONE:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "n"(kTightTries), "r"(kTightHint) : "memory");
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "n"(kSpinLimit) : "memory");
   return ok != 0;
 }
 __device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
