@@ -6,7 +6,6 @@ been built (python -m paper_2605_09877_b200.build) -- there is no CPU fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -538,29 +537,33 @@ class Cache:
                  for _ in range(2)]
         return cls(*codes, *(torch.ones((n_pages, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2)))
 
-    def _call(self, pages, start, count, batch, n_tokens, tensors, status):
+    def _call(self, pages, start, count, rows, status):
+        B, _, T, _ = rows[0].shape
+        dev = self._device
         for t in (pages, start, count, status):
-            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != self._device):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != dev):
                 raise ValueError("pages, start, count and status are contiguous int32 tensors on the cache's device")
-        for t in tensors:
-            if t.dtype != torch.bfloat16 or t.device != self._device:
+        for t in rows:
+            if t.dtype != torch.bfloat16 or t.device != dev:
                 raise ValueError("rows are bfloat16 on the cache's device")
-        if pages.dim() != 2 or pages.shape[0] != batch or start.numel() != batch or (count is not None and count.numel() != batch):
+        if pages.dim() != 2 or pages.shape[0] != B or start.numel() != B or (count is not None and count.numel() != B):
             raise ValueError("pages [batch, max_pages], start [batch], count [batch]")
-        return CacheCall(pages.data_ptr(), start.data_ptr(), count.data_ptr() if count is not None else None, batch, pages.shape[1], n_tokens)
+        return C.byref(CacheCall(pages.data_ptr(), start.data_ptr(), count.data_ptr() if count is not None else None, B, pages.shape[1], T))
 
-    def _on_device(self):
-        """A context in which the cache's device is the current one."""
-        return torch.cuda.device(self._device) if torch._C._cuda_getDevice() != self._device.index else contextlib.nullcontext()
+    def _elsewhere(self):
+        """Whether another device than the cache's is the current one."""
+        return torch._C._cuda_getDevice() != self._device.index
 
     def append(self, k, v, pages, start, count=None, status=None, stream=None):
         """kvm_cache_append: k, v bf16 [B, n_kv_heads, T, head_dim] (channels contiguous) behind the tokens that the sequences hold."""
         if k.dim() != 4 or v.shape != k.shape or k.shape[1] != self.n_kv_heads or k.shape[3] != self.head_dim:
             raise ValueError("k, v [batch, n_kv_heads, tokens, head_dim]")
-        call = self._call(pages, start, count, k.shape[0], k.shape[2], (k, v), status)
-        with self._on_device():
-            rc = lib.kvm_cache_append(self._ref, C.byref(call), k.data_ptr(), v.data_ptr(), _strides3(k), _strides3(v),
-                                      status.data_ptr() if status is not None else None, _stream_ptr(stream))
+        if self._elsewhere():
+            with torch.cuda.device(self._device):
+                return self.append(k, v, pages, start, count, status, stream)
+        call = self._call(pages, start, count, (k, v), status)
+        rc = lib.kvm_cache_append(self._ref, call, k.data_ptr(), v.data_ptr(), _strides3(k), _strides3(v),
+                                  status.data_ptr() if status is not None else None, _stream_ptr(stream))
         if rc != KVM_OK:
             raise KVMError(rc, "kvm_cache_append")
 
@@ -570,16 +573,19 @@ class Cache:
         behind a sequence's count are left as they were (unset where `out` is made here)."""
         if q.dim() != 4 or q.shape[3] != self.head_dim or (out is not None and out.shape != q.shape):
             raise ValueError("q, out [batch, n_q_heads, tokens, head_dim]")
-        with self._on_device(), torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-            if out is None:
-                out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-            call = self._call(pages, start, count, q.shape[0], q.shape[2], (q, out), status)
-            n = lib.kvm_cache_workspace(self._ref, C.byref(call), q.shape[1])
-            # (from the stream's own memory: neither a call on another stream nor another captured graph gets the same bytes)
-            ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
-            rc = lib.kvm_cache_attend(self._ref, C.byref(call), q.data_ptr(), q.shape[1], self.head_dim ** -0.5 if scale is None else scale,
-                                      window, sinks, out.data_ptr(), _strides3(q), _strides3(out), ws.data_ptr() if n > 0 else None,
-                                      max(n, 0), status.data_ptr() if status is not None else None, _stream_ptr(stream))
+        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+            # (memory made here comes from the stream's own: neither a call on another stream nor another captured graph gets the same bytes)
+            with torch.cuda.device(self._device), torch.cuda.stream(stream):
+                return self.attend(q, pages, start, count, window, sinks, scale, out, status)
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        call = self._call(pages, start, count, (q, out), status)
+        Hq = q.shape[1]
+        n = lib.kvm_cache_workspace(self._ref, call, Hq)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
+        rc = lib.kvm_cache_attend(self._ref, call, q.data_ptr(), Hq, self.head_dim ** -0.5 if scale is None else scale, window, sinks,
+                                  out.data_ptr(), _strides3(q), _strides3(out), ws.data_ptr() if n > 0 else None, max(n, 0),
+                                  status.data_ptr() if status is not None else None, _stream_ptr(None))
         if rc != KVM_OK:
             raise KVMError(rc, "kvm_cache_attend")
         return out
@@ -589,8 +595,10 @@ class Cache:
         src, dst = (torch.as_tensor(x, dtype=torch.int32).contiguous() for x in (src, dst))
         if src.is_cuda or dst.is_cuda or src.dim() != 1 or src.shape != dst.shape:
             raise ValueError("src and dst are lists of the same length on the host")
-        with self._on_device():
-            rc = lib.kvm_cache_copy_pages(self._ref, src.data_ptr(), dst.data_ptr(), src.numel(), _stream_ptr(stream))
+        if self._elsewhere():
+            with torch.cuda.device(self._device):
+                return self.copy_pages(src, dst, stream)
+        rc = lib.kvm_cache_copy_pages(self._ref, src.data_ptr(), dst.data_ptr(), src.numel(), _stream_ptr(stream))
         if rc != KVM_OK:
             raise KVMError(rc, "kvm_cache_copy_pages")
 
