@@ -234,20 +234,13 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (combine_kernel waits for this one before it reads what it wrote)
-  if (tid == 0) {
-    tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
-    for (int s = 0; s < ST; ++s) { tc::mbar_init(&bars[Cfg::FULL + s], 1); tc::mbar_init(&bars[Cfg::FREE + s], 1); }
-    for (int g = 0; g < NG; ++g) {
-      for (int s = 0; s < 4; ++s) tc::mbar_init(&bars[Cfg::QFULL + 4 * g + s], 1);
-      for (int s = 0; s < 2; ++s) {
-        tc::mbar_init(&bars[Cfg::QFREE + 2 * g + s], 1);
-        tc::mbar_init(&bars[Cfg::SFULL + 2 * g + s], 1);
-        tc::mbar_init(&bars[Cfg::SFREE + 2 * g + s], 4);
-      }
-      tc::mbar_init(&bars[Cfg::PFULL + g], 4);
-      tc::mbar_init(&bars[Cfg::ODONE + g], 1);
+  if (warp == 0) {
+    for (int i = lane; i < Cfg::COUNT; i += 32)   // (one after the other they would take a thousand cycles)
+      tc::mbar_init(&bars[i], (i >= Cfg::SFREE && i < Cfg::PFULL) || (i >= Cfg::PFULL && i < Cfg::ODONE) ? 4 : 1);
+    if (lane == 0) {
+      tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
+      *abort_flag = 0;
     }
-    *abort_flag = 0;
     tc::fence_barrier_init();
   }
   if (warp == 1) {

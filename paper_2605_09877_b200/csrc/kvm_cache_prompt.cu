@@ -174,27 +174,21 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [4]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the merge waits for this kernel before it reads what it wrote)
   PromptWork w;
   if (!prompt_work(args, blockIdx.x, blockIdx.y, w)) return;
 
   // Set-up: the barriers, tensor memory, and no other barrier of the whole CTA: the producers, the queries' conversion and the search for vbase
   // (each a chain of loads) run side by side from here on.
-  if (tid == 0) {
-    tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
-    for (int s = 0; s < 3; ++s) {
-      tc::mbar_init(&bars[PB_KFULL + s], 1);
-      tc::mbar_init(&bars[PB_KFREE + s], 1);
-      tc::mbar_init(&bars[PB_SFULL + s], 1);
-      tc::mbar_init(&bars[PB_READY + s], 8 + 4);
-      tc::mbar_init(&bars[PB_PVDONE + s], 1);
+  if (warp == 0) {
+    for (int i = lane; i < PB_COUNT; i += 32) {   // (one after the other they would take a thousand cycles)
+      auto in = [&](int first, int n) { return i >= first && i < first + n; };
+      tc::mbar_init(&bars[i], in(PB_READY, 3) ? 8 + 4 : in(PB_V8FREE, Cfg::NV8) || in(PB_VBASE, 1) ? 4 : in(PB_REF, 12) ? 2 : in(PB_QFULL, 1) ? 16 : 1);
     }
-    for (int s = 0; s < Cfg::NV8; ++s) { tc::mbar_init(&bars[PB_V8FULL + s], 1); tc::mbar_init(&bars[PB_V8FREE + s], 4); }
-    for (int s = 0; s < Cfg::NV; ++s) tc::mbar_init(&bars[PB_VFREE + s], 1);
-    for (int s = 0; s < 12; ++s) tc::mbar_init(&bars[PB_REF + s], 2);
-    tc::mbar_init(&bars[PB_QFULL], 16);
-    tc::mbar_init(&bars[PB_LAST], 1);
-    tc::mbar_init(&bars[PB_VBASE], 4);
-    *abort_flag = 0;
+    if (lane == 0) {
+      tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
+      *abort_flag = 0;
+    }
     tc::fence_barrier_init();
   }
   if (warp == 1) {
@@ -681,58 +675,58 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   }
 }
 
-// Rows whose key tiles were split: thread = (row, half of the channels).
+// Rows whose key tiles were split: thread = row, block (row tile, 16 channels).
 template <int D>
-__global__ void __launch_bounds__(256) prompt_combine_kernel(const __grid_constant__ PromptArgs args) {
+__global__ void __launch_bounds__(128) prompt_combine_kernel(const __grid_constant__ PromptArgs args) {
   const AttendArgs& a = args.a;
   PromptWork w;
   if (!prompt_work(args, blockIdx.x, 0, w) || w.parts == 1) return;
-  const int row = threadIdx.x & 127, half = threadIdx.x >> 7;
-  if (row >= w.rows) return;
-  constexpr int HD = D / 2, ST = (D + 2) * 128;
+  const int row = threadIdx.x, c0 = blockIdx.y * 16;
+  constexpr int ST = (D + 2) * 128;
   const float* part = a.part + (int64_t)blockIdx.x * args.nsplit * ST + row;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   float m = -INFINITY;
+#pragma unroll 8
   for (int z = 0; z < w.parts; ++z) m = fmaxf(m, part[z * ST + D * 128]);
-  float wz[kMaxSplits], l = 0.f;
+  float o[16], l = 0.f;
 #pragma unroll
-  for (int z = 0; z < kMaxSplits; ++z) {
-    wz[z] = 0.f;
-    if (z < w.parts) {
-      const float mz = part[z * ST + D * 128], lz = part[z * ST + (D + 1) * 128];
-      wz[z] = mz == -INFINITY ? 0.f : exp2f(mz - m);
-      l += lz == lz ? lz * wz[z] : lz;   // (a NaN row stays one where its weight is 0)
-    }
+  for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll 2
+  for (int z = 0; z < w.parts; ++z) {
+    const float mz = part[z * ST + D * 128], lz = part[z * ST + (D + 1) * 128];
+    const float wz = mz == -INFINITY ? 0.f : tc::ex2_approx(mz - m);
+    l += lz == lz ? lz * wz : lz;   // (a NaN row stays one where its weight is 0)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = fmaf(part[z * ST + (c0 + i) * 128], wz, o[i]);
   }
+  if (row >= w.rows) return;
   const int rg = w.row0 + row, tok = args.by_group.div(rg), hq = w.hk * a.G + rg - tok * a.G;
-  __nv_bfloat16* out = a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + half * HD;
+  __nv_bfloat16* out = a.out + w.b * a.so[0] + hq * a.so[1] + tok * a.so[2] + c0;
   const float inv = 1.f / l;
-  for (int c = 0; c < HD; c += 8) {
-    float o[8];
+  __nv_bfloat162 h[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+  for (int i = 0; i < 8; ++i) h[i] = __floats2bfloat162_rn(o[2 * i] * inv, o[2 * i + 1] * inv);
+  if (args.out_vec) {
+    reinterpret_cast<uint4*>(out)[0] = reinterpret_cast<uint4*>(h)[0];
+    reinterpret_cast<uint4*>(out)[1] = reinterpret_cast<uint4*>(h)[1];
+  } else {
 #pragma unroll
-    for (int z = 0; z < kMaxSplits; ++z) {
-      if (z >= w.parts) break;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = fmaf(part[z * ST + (half * HD + c + i) * 128], wz[z], o[i]);
-    }
-    __nv_bfloat162 h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(o[2 * i] * inv, o[2 * i + 1] * inv);
-    if (args.out_vec) {
-      *reinterpret_cast<uint4*>(out + c) = *reinterpret_cast<uint4*>(h);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { out[c + 2 * i] = h[i].x; out[c + 2 * i + 1] = h[i].y; }
-    }
+    for (int i = 0; i < 8; ++i) { out[2 * i] = h[i].x; out[2 * i + 1] = h[i].y; }
   }
 }
 
-// (row tiles of 128, key splits) of a call.  Few row tiles: as many splits as fill the SMs.
+// (row tiles of 128, key splits) of a call: the number of splits that the launch is done with first, if every row tile saw `tiles` key tiles, a CTA's
+// set-up and end took as long as five of them (measured: 8 us and 1.3 us a tile) and the merge as three.  Row tiles that see fewer take
+// fewer (prompt_work).  300 tokens behind 3000, 32 heads on 8 (80 row tiles of 26): one split 42 us, three %s.
 static void prompt_plan(int64_t units, int64_t rows, int64_t tiles, int& qtiles, int& nsplit) {
   qtiles = (int)((rows + kRows - 1) / kRows);
   const int64_t ctas = units * qtiles;
-  nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({148 / ctas, (tiles + kSplitTiles - 1) / kSplitTiles, kMaxSplits}));
+  nsplit = 1;
+  int64_t best = INT64_MAX;
+  for (int ns = 1; ns <= kMaxSplits && ns <= (tiles + kSplitTiles - 1) / kSplitTiles && (ns == 1 || ctas * ns <= 4 * 148); ++ns) {
+    const int64_t cost = (ctas * ns + 147) / 148 * ((tiles + ns - 1) / ns + 5) + (ns > 1 ? 3 : 0);
+    if (cost < best) { best = cost; nsplit = ns; }
+  }
 }
 
 int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d) {
@@ -751,7 +745,15 @@ static kvm_status_t launch_prompt_d(const PromptArgs& args, const CUtensorMap& m
     if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   prompt_kernel<D><<<dim3((unsigned)(args.units * args.qtiles), args.nsplit), kThreads, PromptCfg<D>::SMEM, s>>>(mapK, mapV, args);
-  if (args.nsplit > 1) prompt_combine_kernel<D><<<args.units * args.qtiles, 256, 0, s>>>(args);
+  if (args.nsplit > 1) {
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)(args.units * args.qtiles), D / 16); lc.blockDim = dim3(128); lc.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at; lc.numAttrs = 1;
+    if (cudaLaunchKernelEx(&lc, prompt_combine_kernel<D>, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+  }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 
