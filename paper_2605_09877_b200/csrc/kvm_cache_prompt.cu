@@ -540,19 +540,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           mx = fmaxf(mx, fmaxf(m, m2) * fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f));
         }
       }
-      // the maximum of the row's other half
+      // the maximum of the row's other half, and the reference of the tile before
       float* x2 = my_xm + flip * 256;
       x2[half * 128 + row] = mx;
+      if (j > 0 && !tc::mbar_wait_tight(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
       ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);
       if (!ok) break;
       mx = fmaxf(mx, x2[(1 - half) * 128 + row]);
       // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
-      float m = -INFINITY;
-      if (j > 0) {
-        if (!tc::mbar_wait_tight(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
-        __syncwarp();
-        m = s_m[row];
-      }
+      float m = j > 0 ? s_m[row] : -INFINITY;
       if (__any_sync(0xffffffffu, mx > m + 8.0f || j == 0)) {   // (the same decision in both warps)
         const float mnew = fmaxf(m, mx);
         if (j > 0) {
@@ -680,11 +676,12 @@ template <int D>
 __global__ void __launch_bounds__(128) prompt_combine_kernel(const __grid_constant__ PromptArgs args) {
   const AttendArgs& a = args.a;
   PromptWork w;
-  if (!prompt_work(args, blockIdx.x, 0, w) || w.parts == 1) return;
+  const bool split = prompt_work(args, blockIdx.x, 0, w) && w.parts > 1;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // (by every block: what follows this grid counts on the end of the one before it)
+  if (!split) return;
   const int row = threadIdx.x, c0 = blockIdx.y * 16;
   constexpr int ST = (D + 2) * 128;
   const float* part = a.part + (int64_t)blockIdx.x * args.nsplit * ST + row;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   float m = -INFINITY;
 #pragma unroll 8
   for (int z = 0; z < w.parts; ++z) m = fmaxf(m, part[z * ST + D * 128]);
@@ -717,7 +714,7 @@ __global__ void __launch_bounds__(128) prompt_combine_kernel(const __grid_consta
 
 // (row tiles of 128, key splits) of a call: the number of splits that the launch is done with first, if every row tile saw `tiles` key tiles, a CTA's
 // set-up and end took as long as five of them (measured: 8 us and 1.3 us a tile) and the merge as three.  Row tiles that see fewer take
-// fewer (prompt_work).  300 tokens behind 3000, 32 heads on 8 (80 row tiles of 26): one split 42 us, three %s.
+// fewer (prompt_work).  300 tokens behind 3000, 32 heads on 8 (80 row tiles of 26): one split 48 us, three 52.
 static void prompt_plan(int64_t units, int64_t rows, int64_t tiles, int& qtiles, int& nsplit) {
   qtiles = (int)((rows + kRows - 1) / kRows);
   const int64_t ctas = units * qtiles;

@@ -567,7 +567,6 @@ def test_captured_calls_follow_the_lengths_and_pages_they_are_replayed_with(kvm,
         g.replay()
         s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
         s1.wait_stream(torch.cuda.current_stream()); s2.wait_stream(torch.cuda.current_stream())
-        out.fill_(7.0) if False else None
         with torch.cuda.stream(s1):
             g2.replay()
         torch.cuda.synchronize()
@@ -577,6 +576,64 @@ def test_captured_calls_follow_the_lengths_and_pages_they_are_replayed_with(kvm,
             m.len[b] += T
         m.compare(qn, out, [T, T], 0, 0)
         m.compare(qn, out2, [T, T], 100, 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(16))
+def test_attend_over_random_shapes(kvm, seed):
+    """Shapes, lengths, windows and scales drawn over the range that the calls allow (small enough for the definition on the host)."""
+    r = random.Random(1000 + seed)
+    d, P, Hkv, G = r.choice([64, 128]), r.choice([16, 32, 64, 128]), r.choice([1, 2, 3]), r.choice([1, 2, 3, 5, 8, 16])
+    B, T = r.randint(1, 4), r.choice([1, 1, 2, 5, 17, 60, 200])
+    ctx = [r.choice([0, r.randint(1, 20), r.randint(100, 1500)]) for _ in range(B)]
+    tokens = [r.randint(0, T) for _ in range(B)]
+    tokens[r.randrange(B)] = T
+    window, sinks = r.choice([(0, 0), (r.randint(1, 600), r.choice([0, 1, 4, 130, 700]))])
+    m = Model(kvm, B, Hkv, d, P, -(-(max(ctx) + T) // P) + r.randint(0, 30), seed=seed)
+    if max(ctx):
+        m.append(rows((B, Hkv, max(ctx), d), seed), rows((B, Hkv, max(ctx), d), seed + 1) * 2.0 ** r.randint(-20, 20), ctx)
+    m.append(rows((B, Hkv, T, d), seed + 2), rows((B, Hkv, T, d), seed + 3), tokens)
+    m.attend(rows((B, Hkv * G, T, d), seed + 4) * r.choice([0.1, 1.0, 4.0]), tokens, window, sinks, scale=r.choice([None, 0.02, 0.5]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 40])
+def test_calls_side_by_side_on_two_streams(kvm, T):
+    """Calls that overlap do not touch one another's workspaces."""
+    ms = [Model(kvm, 2, 2, 128, 64, 40, seed=s) for s in range(2)]
+    for s, m in enumerate(ms):
+        m.append(rows((2, 2, 2000, 128), s), rows((2, 2, 2000, 128), 10 + s), [2000, 1500])
+        m.append(rows((2, 2, T, 128), 20 + s), rows((2, 2, T, 128), 30 + s), [T, T])
+    qs = [rows((2, 8, T, 128), 40 + s) for s in range(2)]
+    outs = [[torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(20)] for q in qs]
+    dev, starts = [q.cuda() for q in qs], [torch.tensor([n - T for n in m.len], dtype=torch.int32).cuda() for m in ms]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s in range(2):
+            ms[s].cache.attend(dev[s], ms[s].table, starts[s], out=outs[s][i], stream=streams[s])
+    torch.cuda.synchronize()
+    for s in range(2):
+        ms[s].compare(qs[s], outs[s][0], [T, T], 0, 0)
+        assert all(torch.equal(outs[s][0], o) for o in outs[s])
+
+
+@pytest.mark.gpu
+def test_a_call_after_a_split_one_sees_its_results(kvm):
+    """What is enqueued behind a call - here a copy of its output - runs after all of it, whether or not anything was left to merge."""
+    m = Model(kvm, 1, 2, 128, 64, 40)
+    m.append(rows((1, 2, 2300, 128), 1), rows((1, 2, 2300, 128), 2), [2300])
+    for T, start in ((1, 2000), (17, 2000), (200, 2000), (300, 0), (20, 100)):
+        q, st = rows((1, 8, T, 128), 3).cuda(), torch.tensor([start], dtype=torch.int32).cuda()
+        want = m.cache.attend(q, m.table, st)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            out = torch.zeros_like(q)
+            m.cache.attend(q, m.table, st, out=out)
+            got = out.clone()
+            out.fill_(9.0)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and (out == 9.0).all()
 
 
 @pytest.mark.gpu
