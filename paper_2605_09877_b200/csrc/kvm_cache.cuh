@@ -36,19 +36,30 @@ __device__ __forceinline__ void report(int32_t* status, int code) {
 __device__ __forceinline__ bool sees(int i, int j, int window, int sinks) {
   return j <= i && (j > i - window || j < sinks);
 }
-// The key tiles that positions [first, last] see: the tiles of the first `sinks` tokens, then the window's, without those counted twice.
-struct Tiles { int n_sink, first, n; };   // tile i is i < n_sink ? i : first + (i - n_sink); n in all
-__device__ __forceinline__ Tiles tiles_of(int first, int last, int window, int sinks) {
-  Tiles t;
-  const int end = last / kTile + 1;
+// The pages that positions [first, last] see: those of the first `sinks` tokens, then the window's, without those counted twice; a key tile is
+// the next kTile / page of them, whatever their numbers are (so a window with sinks costs no more tiles than its pages fill).
+struct PageList {
+  int n_sink, first, n, tiles;   // page i of the list is page page_at(i) of the sequence; n pages, so many tiles
+};
+__device__ __forceinline__ PageList pages_of(const Params& p, int first, int last, int window, int sinks) {
+  PageList t;
+  const int end = (last >> p.page_shift) + 1;
   const int low = first - window + 1;   // (first >= 0 and window >= 1: no overflow)
-  const int w0 = low > 0 ? low / kTile : 0;
-  t.n_sink = min(w0, (sinks + kTile - 1) / kTile);
+  const int w0 = low > 0 ? low >> p.page_shift : 0;
+  t.n_sink = min(w0, (sinks + p.page - 1) >> p.page_shift);
   t.first = w0;
   t.n = t.n_sink + end - w0;
+  const int per = kTile >> p.page_shift;
+  t.tiles = (t.n + per - 1) >> (7 - p.page_shift);
   return t;
 }
-__device__ __forceinline__ int tile_at(const Tiles& t, int i) { return i < t.n_sink ? i : t.first + (i - t.n_sink); }
+__device__ __forceinline__ int page_at(const PageList& t, int i) { return i < t.n_sink ? i : t.first + (i - t.n_sink); }
+constexpr int kNowhere = 0x7fff0000;   // position of the keys of a page that a tile lacks: behind all others
+// Whether all of positions [first, last] see all keys of a page that begins at p0.
+__device__ __forceinline__ bool page_seen_by_all(const Params& p, int p0, int first, int last, int window, int sinks) {
+  const int end = p0 + p.page - 1;
+  return end <= first && (p0 > last - window || end < sinks);
+}
 
 // Exponent of a scale 2^e.  A NaN scale has exponent 128: scale_value(128) is NaN.
 __device__ __forceinline__ int scale_exp(float s) { return (int)((__float_as_uint(s) >> 23) & 255u) - 127; }

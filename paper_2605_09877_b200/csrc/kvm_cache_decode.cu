@@ -37,13 +37,15 @@ bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, 
 constexpr int kCtas = 148;
 constexpr float kPShift = 8.f;   // the largest weight of a tile is 2^8 (e4m3 ends at 448)
 
-struct TileInfo {
-  int pos, b, hk, flags;   // first key position; unit; kFirst ...
+struct alignas(16) TileInfo {
+  int b, hk, flags;        // unit; kFirst ...
   int vmax, start, n;      // largest exponent of the visible blocks' value scales; lengths of the sequence
   int ze;                  // last worker that has tiles of the unit
-  int16_t ke[8], ve[8];    // exponents of the scales per page of the tile
+  int pos[8];              // per page of the tile: position of its first key,
+  int16_t ke[8], ve[8];    // exponents of its scales
 };
-enum { kFirst = 1, kLast = 2, kWhole = 4, kBegins = 8 };   // first / last tile of the worker's share of the unit; the share is all of it / begins with it
+// first / last tile of the worker's share of the unit; the share is all of it / begins with it; all columns see all keys of the tile
+enum { kFirst = 1, kLast = 2, kWhole = 4, kBegins = 8, kAll = 16 };
 
 template <int D, int NC>
 struct DecodeCfg {
@@ -69,6 +71,8 @@ struct DecodeCfg {
   static constexpr int FULL = 0, FREE = FULL + ST, QFULL = FREE + ST, QFREE = QFULL + 4 * NG, SFULL = QFREE + 2 * NG, SFREE = SFULL + 2 * NG,
                        PFULL = SFREE + 2 * NG, ODONE = PFULL + NG, COUNT = ODONE + NG;
   static_assert(COUNT * 8 + 64 <= 1024, "barriers");
+  static_assert(OFF_Q % 1024 == 0 && OFF_P % 1024 == 0 && OFF_CQ % 16 == 0 && OFF_MAX % 16 == 0 && OFF_AB % 16 == 0 && OFF_L % 16 == 0 && OFF_BAR % 8 == 0,
+                "alignment");
 };
 
 // What a worker leaves for combine_kernel beside its partial results: the unit that begins in its share and goes on in the next one's (b < 0: none).
@@ -151,7 +155,7 @@ __device__ __forceinline__ bool group_barrier(int g, bool ok) {
 }
 // Tiles that the call's tokens of a sequence see (0: none, or lengths that are not allowed).
 __device__ __forceinline__ int seq_tiles(const AttendArgs& a, int start, int n) {
-  return n > 0 ? tiles_of(start, start + n - 1, a.window, a.sinks).n : 0;
+  return n > 0 ? pages_of(a.p, start, start + n - 1, a.window, a.sinks).tiles : 0;
 }
 // Last b with pre[b] <= f (pre ascends; f < pre[batch], so that sequence b has tiles).
 __device__ __forceinline__ int seq_of(const int* pre, int batch, int f) {
@@ -266,9 +270,9 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     // ------------------------------ producer ------------------------------
     const int tshift = 7 - p.page_shift, ppt = 1 << tshift, tpb = 32 >> tshift;   // pages of a tile; tiles whose pages the warp's lanes hold at a time
     const int lt = lane >> tshift, lp = lane & (ppt - 1);
-    struct Page { int row, ke, ve, pos, b, hk, flags, start, n, ze; };   // row < 0: not loaded
+    struct Page { int row, ke, ve, pos, b, hk, flags, start, n, ze; bool all; };   // row < 0: not loaded
     auto fetch = [&](int k) {
-      Page x{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+      Page x{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
       const int jj = k * tpb + lt;
       if (jj < ntile) {
         int i, g;
@@ -277,15 +281,18 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const int b = seq_of(pre, p.batch, f);
         lengths(b, x.start, x.n);
         const int last = x.start + x.n - 1;
-        const Tiles t = tiles_of(x.start, last, a.window, a.sinks);
-        const int rem = f - pre[b], hk = rem / t.n, it = rem - hk * t.n, u0 = f - it;
-        x.b = b; x.hk = hk; x.pos = tile_at(t, it) * kTile;
-        x.flags = (it == 0 || i == 0 ? kFirst : 0) | (it == t.n - 1 || i == n - 1 ? kLast : 0) | (u0 >= F0 ? kBegins : 0) |
-                  (u0 >= F0 && u0 + t.n <= F0 + n ? kWhole : 0);
-        x.ze = (u0 + t.n - 1) / sh.share;
-        const int p0 = x.pos + lp * p.page;   // the page is needed if any token of the call sees any of its positions
-        if (p0 <= last && (p0 + p.page > x.start - a.window + 1 || p0 < a.sinks)) {
-          const int page = p.pages[(int64_t)b * p.max_pages + (p0 >> p.page_shift)];
+        const PageList t = pages_of(p, x.start, last, a.window, a.sinks);
+        const int rem = f - pre[b], hk = rem / t.tiles, it = rem - hk * t.tiles, u0 = f - it;
+        x.b = b; x.hk = hk; x.pos = kNowhere;
+        x.flags = (it == 0 || i == 0 ? kFirst : 0) | (it == t.tiles - 1 || i == n - 1 ? kLast : 0) | (u0 >= F0 ? kBegins : 0) |
+                  (u0 >= F0 && u0 + t.tiles <= F0 + n ? kWhole : 0);
+        x.ze = (u0 + t.tiles - 1) / sh.share;
+        const int at = it * ppt + lp;
+        if (at < t.n) {
+          const int block = page_at(t, at);
+          x.pos = block << p.page_shift;
+          x.all = page_seen_by_all(p, x.pos, x.start, last, a.window, a.sinks);
+          const int page = p.pages[(int64_t)b * p.max_pages + block];
           if (page < 0 || page >= p.n_pages) {
             report(p.status, KVM_ERR_INVALID_ARG);
             x.ke = x.ve = 128;
@@ -316,12 +323,14 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       const bool mine = lt == t;
       const uint32_t loads = __ballot_sync(0xffffffffu, mine && cur.row >= 0);
       const int v = __reduce_max_sync(0xffffffffu, mine && cur.row >= 0 && cur.ve < 128 ? cur.ve : -1000);
+      const bool all = __all_sync(0xffffffffu, !mine || cur.all);
       if (mine) {
         TileInfo& ti = info[s];
+        ti.pos[lp] = cur.pos;
         ti.ke[lp] = (int16_t)cur.ke;
         ti.ve[lp] = (int16_t)cur.ve;
         if (lp == 0) {
-          ti.pos = cur.pos; ti.b = cur.b; ti.hk = cur.hk; ti.flags = cur.flags; ti.start = cur.start; ti.n = cur.n; ti.ze = cur.ze;
+          ti.b = cur.b; ti.hk = cur.hk; ti.flags = cur.flags | (all ? kAll : 0); ti.start = cur.start; ti.n = cur.n; ti.ze = cur.ze;
           ti.vmax = v == -1000 ? 0 : v;
         }
       }
@@ -605,7 +614,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         tc::tc_fence_after();
         columns(lanes + NB * (i & 1), y);
         const TileInfo& ti = info[s];
-        const int pos = ti.pos, start = ti.start;
+        const int start = ti.start;
         flags = ti.flags; b = ti.b; hk = ti.hk; vmax = ti.vmax; n = ti.n; ze = ti.ze;
         const int ke = ti.ke[tok >> p.page_shift], ve = ti.ve[tok >> p.page_shift];
         if (flags & kFirst) {
@@ -613,13 +622,12 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           ++seg;
           if (!tc::mbar_wait_tight(&bars[Cfg::QFULL + 4 * g + (seg & 3)], (seg >> 2) & 1)) ok = false;
         }
-        const int last = start + n - 1, key = pos + tok;
+        const int last = start + n - 1, key = ti.pos[tok >> p.page_shift] + (tok & (p.page - 1));
         const float ks = exp2i(ke);
         vr = ve > 127 ? 0 : max(ve - vmax, -60);   // exponent that the weights take over from the values' scale
         const float vrel = ve > 127 ? __int_as_float(0x7fc00000) : (float)vr;
         dropped = ve < 128 && ve - vmax < -60;   // its values are below 2^-60 of the tile's largest
         const bool any = key <= last && (key > start - a.window || key < a.sinks);   // some column sees the key
-        const bool all = pos + 127 <= start && (pos > last - a.window || pos + 127 < a.sinks);   // (uniform) all columns see all keys
 #pragma unroll
         for (int c4 = 0; c4 < NC / 4; ++c4) {
           const float4 f = reinterpret_cast<const float4*>(cq + (seg & 3) * NC)[c4];
@@ -629,7 +637,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&bars[Cfg::SFREE + 2 * g + (i & 1)]);
-        if (!all) {
+        if (!(flags & kAll)) {
           if (n == 1) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) y[c] = any ? y[c] : -INFINITY;

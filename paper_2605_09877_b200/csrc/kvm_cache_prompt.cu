@@ -53,19 +53,25 @@ struct PromptArgs {
   int q_vec, out_vec;
 };
 
-struct PromptTile {
-  int pos, flags;     // first key position; 1: some scale is NaN
-  int pad[2];
-  float ks[8];        // scales of the keys, per 16 columns
+struct alignas(16) PromptTile {
+  int flags;          // 1: some scale is NaN, or some row does not see some key
+  int pos[8];         // per 16 columns: position of the first key,
+  float ks[8];        // scale of the keys
 };
-struct ValueTile {
-  int pos, pad;
-  uint32_t vs[8];     // scales of the values per page, two fp16 each, relative to 2^vbase
+struct alignas(16) ValueTile {
+  int all;            // every key is seen by some row
+  int pos[8];         // per page: position of the first key,
+  uint32_t vs[8];     // scale of the values, two fp16 each, relative to 2^vbase
 };
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
 constexpr int kRows = 128; // rows of a CTA
 constexpr int kThreads = 768;
 constexpr int kValueInfo = 4;   // (as many as value tiles: written when the tile is free)
+
+// PB_READY: P of the tile is in tensor memory (8 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
+// 32 rows are decided for a tile, [row quarter][tile % 3]
+enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 10, PB_VFREE = 14, PB_SFULL = 16, PB_READY = 19, PB_PVDONE = 22, PB_QFULL = 25,
+       PB_REF = 26, PB_LAST = 38, PB_VBASE = 39, PB_COUNT = 40 };
 
 template <int D>
 struct PromptCfg {
@@ -85,16 +91,14 @@ struct PromptCfg {
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static constexpr int SMEM = (OFF_BAR + 512 + 1024) > 120 * 1024 ? (OFF_BAR + 512 + 1024) : 120 * 1024;
   static constexpr uint32_t COL_S = 0, COL_O = 384;      // S / P accumulator i at 128 i
+  static_assert(OFF_K % 1024 == 0 && OFF_V8 % 1024 == 0 && OFF_V % 1024 == 0 && OFF_M % 16 == 0 && OFF_XM % 16 == 0 && OFF_L % 16 == 0 && OFF_BAR % 8 == 0,
+                "alignment");
+  static_assert(PB_COUNT * 8 + 64 <= 512 && SMEM <= 227 * 1024, "shared memory");
 };
-// PB_READY: P of the tile is in tensor memory (8 softmax warps) and its values are in fp16 (4 converting warps); PB_REF: the references of
-// 32 rows are decided for a tile, [row quarter][tile % 3]
-enum { PB_KFULL = 0, PB_KFREE = 3, PB_V8FULL = 6, PB_V8FREE = 10, PB_VFREE = 14, PB_SFULL = 16, PB_READY = 19, PB_PVDONE = 22, PB_QFULL = 25,
-       PB_REF = 26, PB_LAST = 38, PB_VBASE = 39, PB_COUNT = 40 };
-
 // What a CTA does: its rows and its key tiles.  (Also what the merge needs to know.)
 struct PromptWork {
   int b, hk, start, row0, rows, first, last, jb, ntiles, parts;
-  Tiles t;
+  PageList t;
 };
 __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int sp, PromptWork& w) {
   const Params& p = args.a.p;
@@ -111,15 +115,15 @@ __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int
   w.rows = (int)min((int64_t)kRows, left);
   w.first = w.start + args.by_group.div(w.row0);
   w.last = w.start + args.by_group.div(w.row0 + w.rows - 1);
-  w.t = tiles_of(w.first, w.last, args.a.window, args.a.sinks);
+  w.t = pages_of(p, w.first, w.last, args.a.window, args.a.sinks);
   w.parts = 1;
   w.jb = 0;
-  w.ntiles = w.t.n;
+  w.ntiles = w.t.tiles;
   if (args.nsplit > 1) {
-    const int per = max(kSplitTiles, (w.t.n + args.nsplit - 1) / args.nsplit);
-    w.parts = (w.t.n + per - 1) / per;
+    const int per = max(kSplitTiles, (w.t.tiles + args.nsplit - 1) / args.nsplit);
+    w.parts = (w.t.tiles + per - 1) / per;
     w.jb = sp * per;
-    w.ntiles = min(per, w.t.n - w.jb);
+    w.ntiles = min(per, w.t.tiles - w.jb);
   }
   return w.ntiles > 0;
 }
@@ -197,10 +201,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   }
   // Page i of the CTA's tiles (ppt pages a tile): whether some row sees some key of it, and where it is.
   const int tshift = 7 - p.page_shift, ppt = 1 << tshift;
-  auto page_of = [&](int i, int& p0) -> int {   // >= 0: page; -1: not seen; -2: outside the pool
-    p0 = tile_at(w.t, w.jb + (i >> tshift)) * kTile + (i & (ppt - 1)) * p.page;
-    if (p0 > w.last || !(p0 + p.page > w.first - a.window + 1 || p0 < a.sinks)) return -1;
-    const int page = p.pages[(int64_t)w.b * p.max_pages + (p0 >> p.page_shift)];
+  auto page_of = [&](int i, int& p0) -> int {   // >= 0: page; -1: there is none; -2: outside the pool
+    i += w.jb * ppt;
+    p0 = kNowhere;
+    if (i >= w.t.n) return -1;
+    const int block = page_at(w.t, i);
+    p0 = block << p.page_shift;
+    const int page = p.pages[(int64_t)w.b * p.max_pages + block];
     return page >= 0 && page < p.n_pages ? page : -2;
   };
   tc::tc_fence_before();
@@ -232,7 +239,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         if (j < w.ntiles) {
           int p0;
           const int page = page_of(j * ppt + lp, p0);
-          g.pos = p0 - lp * p.page;
+          g.pos = p0;
           if (page == -2) {
             report(p.status, KVM_ERR_INVALID_ARG);
             g.ke = g.ve = 128;
@@ -266,13 +273,21 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const bool mine = lt == t, nan = cur.ke > 127 || cur.ve > 127;
         const uint32_t loads = __ballot_sync(0xffffffffu, mine && cur.row >= 0);
         const uint32_t nans = __ballot_sync(0xffffffffu, mine && nan);   // (pages outside the pool among them)
+        // keys: all rows see all keys of the page; values: some row sees each of them
+        const bool seen = keys ? page_seen_by_all(p, cur.pos, w.first, w.last, a.window, a.sinks)
+                               : cur.pos + p.page - 1 <= w.last && (cur.pos > w.first - a.window || cur.pos + p.page - 1 < a.sinks);
+        const bool all = __all_sync(0xffffffffu, !mine || seen);
         if (mine && keys) {
           PromptTile& ti = info[j % kInfo];
-          if (lp == 0) { ti.pos = cur.pos; ti.flags = nans ? 1 : 0; }
+          if (lp == 0) ti.flags = nans || !all ? 1 : 0;
           const float ks = nan ? __int_as_float(0x7fc00000) : exp2i(cur.ke);
-          for (int i = 0; i < p.page / 16; ++i) ti.ks[lp * (p.page / 16) + i] = ks;
+          for (int i = 0; i < p.page / 16; ++i) {
+            ti.ks[lp * (p.page / 16) + i] = ks;
+            ti.pos[lp * (p.page / 16) + i] = cur.pos + 16 * i;
+          }
         } else if (mine) {
-          if (lp == 0) vinfo[s].pos = cur.pos;
+          if (lp == 0) vinfo[s].all = all;
+          vinfo[s].pos[lp] = cur.pos;
           const __half h = __float2half_rn(nan || cur.row < 0 ? 0.f : exp2i(max(cur.ve - vbase, -126)));
           vinfo[s].vs[lp] = (uint32_t)__half_as_ushort(h) * 0x10001u;
         }
@@ -372,8 +387,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       ok = __all_sync(0xffffffffu, good);
       if (!ok) break;
       const ValueTile& vt = vinfo[s8];
-      const int pos = vt.pos;
-      const bool all = pos + 127 <= w.last && (pos > w.first - a.window || pos + 127 < a.sinks);   // every key is seen by some row
+      const bool all = vt.all;
       const uint8_t* src = base + Cfg::OFF_V8 + s8 * Cfg::T8;
       uint8_t* dst = base + Cfg::OFF_V + sv * Cfg::T16;
       uint4 c[4 * N];
@@ -385,7 +399,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       if (!all) {   // whatever the ring or the page holds there must not meet the weight 0
 #pragma unroll
         for (int i = 0; i < 4 * N; ++i) {
-          const int key = pos + rows0 + 8 * (i / N) + r8;
+          const int row = rows0 + 8 * (i / N) + r8, key = vt.pos[row >> p.page_shift] + (row & (p.page - 1));
           if (!(key <= w.last && (key > w.first - a.window || key < a.sinks))) c[i] = make_uint4(0, 0, 0, 0);
         }
       }
@@ -497,26 +511,26 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       __syncwarp();
       tc::tc_fence_after();
       const PromptTile& ti = info[j % kInfo];
-      const int flags = ti.flags, pos = ti.pos;
-      const bool slow = flags || !(pos + 127 <= w.first && (pos > w.last - a.window || pos + 127 < a.sinks));   // (uniform) masks, or NaN scales
+      const bool slow = ti.flags;   // (uniform) masks, or NaN scales
       // S of columns 64 half + 32 c .. + 31; what the row does not see as -inf
       auto load = [&](int c, uint32_t (&x)[32]) {
         tc::tmem_ld32(ts + 64 * half + 32 * c, x);
         tc::tmem_wait_ld();
         if (slow) {
-          const int key0 = pos + 64 * half + 32 * c;
           // bit i: the row sees column i.  j <= pos_row, and j > pos_row - window or j < sinks
-          auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // columns i < n
+          auto below = [&](int n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1u; };   // columns i < n of 16
           const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
-          uint32_t see = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
+          uint32_t see = 0;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
+            const int key0 = ti.pos[4 * half + 2 * c + g];
             const float ks = ti.ks[4 * half + 2 * c + g];
+            uint32_t cols = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
             if (!(ks == ks)) {
-              const uint32_t cols = 0xffffu << (16 * g);
-              bad = bad || (see & cols);
-              see &= ~cols;
+              bad = bad || cols;
+              cols = 0;
             }
+            see |= cols << (16 * g);
           }
 #pragma unroll
           for (int i = 0; i < 32; ++i) x[i] = (see >> i) & 1 ? x[i] : 0xff800000u;
