@@ -271,8 +271,13 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     const int tshift = 7 - p.page_shift, ppt = 1 << tshift, tpb = 32 >> tshift;   // pages of a tile; tiles whose pages the warp's lanes hold at a time
     const int lt = lane >> tshift, lp = lane & (ppt - 1);
     struct Page { int row, ke, ve, pos, b, hk, flags, start, n, ze; bool all; };   // row < 0: not loaded
-    auto fetch = [&](int k) {
-      Page x{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
+    // What there is to know of a batch of tiles is fetched in three steps, a few tiles apart: each waits for what the step before has asked the
+    // memory for (together they take several thousand cycles when it is busy, more than the ring covers).
+    Page cur{}, nxt{};
+    float ks = 0.f, vs = 0.f;   // scales on their way
+    auto ask_page = [&](int k) {
+      Page& x = nxt;
+      x = Page{-1, 0, 0, kNowhere, 0, 0, 0, 0, 0, 0, false};
       const int jj = k * tpb + lt;
       if (jj < ntile) {
         int i, g;
@@ -283,7 +288,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const int last = x.start + x.n - 1;
         const PageList t = pages_of(p, x.start, last, a.window, a.sinks);
         const int rem = f - pre[b], hk = rem / t.tiles, it = rem - hk * t.tiles, u0 = f - it;
-        x.b = b; x.hk = hk; x.pos = kNowhere;
+        x.b = b; x.hk = hk;
         x.flags = (it == 0 || i == 0 ? kFirst : 0) | (it == t.tiles - 1 || i == n - 1 ? kLast : 0) | (u0 >= F0 ? kBegins : 0) |
                   (u0 >= F0 && u0 + t.tiles <= F0 + n ? kWhole : 0);
         x.ze = (u0 + t.tiles - 1) / sh.share;
@@ -292,31 +297,38 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           const int block = page_at(t, at);
           x.pos = block << p.page_shift;
           x.all = page_seen_by_all(p, x.pos, x.start, last, a.window, a.sinks);
-          const int page = p.pages[(int64_t)b * p.max_pages + block];
-          if (page < 0 || page >= p.n_pages) {
-            report(p.status, KVM_ERR_INVALID_ARG);
-            x.ke = x.ve = 128;
-          } else {
-            const int unit = page * p.Hkv + hk;
-            x.row = unit * p.page;
-            x.ke = scale_exp(p.ks[unit]);
-            x.ve = scale_exp(p.vs[unit]);
-          }
+          x.row = p.pages[(int64_t)b * p.max_pages + block];
         }
       }
-      return x;
     };
-    Page cur{}, nxt{};
+    auto ask_scales = [&]() {
+      if (nxt.pos == kNowhere) return;   // (no page)
+      if (nxt.row < 0 || nxt.row >= p.n_pages) {
+        report(p.status, KVM_ERR_INVALID_ARG);
+        nxt.row = -1;
+        ks = vs = __int_as_float(0x7fc00000);
+      } else {
+        const int unit = nxt.row * p.Hkv + nxt.hk;
+        nxt.row = unit * p.page;
+        ks = p.ks[unit];
+        vs = p.vs[unit];
+      }
+    };
+    auto take = [&]() {
+      cur = nxt;
+      if (cur.pos == kNowhere) { cur.row = -1; return; }
+      cur.ke = scale_exp(ks);
+      cur.ve = scale_exp(vs);
+    };
     bool ok = true;
     int s = 0, issued = 0;
     uint32_t par = 0;
-    int ahead = 0, t = tpb;   // batches of pages fetched so far, tiles of the current one that are issued
+    int ahead = 0, t = 0;   // batches asked for so far, tiles of the current one that are issued
     for (; issued < ntile; ++issued) {
-      if (t == tpb && ahead > 0) { t = 0; cur = nxt; }
-      if (ahead == 0 || t == 1) {   // (the next batch, behind the first tile of the one before)
-        nxt = fetch(ahead++);
-        if (ahead == 1) { cur = nxt; t = 0; }
-      }
+      const bool none = ahead == 0;
+      if (none || t == 1) ask_page(ahead++);
+      if (none || t == (tpb > 4 ? 4 : 2)) ask_scales();
+      if (none || t == tpb) { take(); t = 0; }
       if (lane == 0) ok = !*abort_flag && (issued < ST || tc::mbar_wait_tight(&bars[Cfg::FREE + s], par ^ 1));
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
