@@ -67,6 +67,11 @@ __device__ __forceinline__ float exp2i(int e) {   // 2^e, -126 <= e <= 127; 128:
   return e > 127 ? __int_as_float(0x7fc00000) : __int_as_float((e + 127) << 23);
 }
 
+// Scales of values are taken into the exponents of the weights, relative to the largest of those that are looked at together, and out of the row
+// sums again: 2^90 and its inverse leave the sums within fp32.  Blocks further below contribute to the row sum only (their values are
+// less than 2^-90 of the others').  Results before the division are held in units of 2^40, so that values up to bf16's largest do not overflow.
+constexpr int kFoldMost = 90, kUnitExp = 40;
+
 // two floats -> two e4m3 codes (a in the low byte), round to nearest even, saturating
 __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
   uint16_t r;

@@ -582,7 +582,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const float4 l4 = *reinterpret_cast<const float4*>(s_l + 4 * (c + k));
-            x[k] = __fdividef(o_run[c + k], (l4.x + l4.y) + (l4.z + l4.w));
+            x[k] = __fdividef(o_run[c + k], (l4.x + l4.y) + (l4.z + l4.w)) * exp2i(kUnitExp);
           }
           const __nv_bfloat162 b2 = __floats2bfloat162_rn(x[0], x[1]);
           h[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
@@ -636,9 +636,9 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         const int last = start + n - 1, key = ti.pos[tok >> p.page_shift] + (tok & (p.page - 1));
         const float ks = exp2i(ke);
-        vr = ve > 127 ? 0 : max(ve - vmax, -60);   // exponent that the weights take over from the values' scale
+        vr = ve > 127 ? 0 : max(ve - vmax, -kFoldMost);   // exponent that the weights take over from the values' scale
         const float vrel = ve > 127 ? __int_as_float(0x7fc00000) : (float)vr;
-        dropped = ve < 128 && ve - vmax < -60;   // its values are below 2^-60 of the tile's largest
+        dropped = ve < 128 && ve - vmax < -kFoldMost;
         const bool any = key <= last && (key > start - a.window || key < a.sinks);   // some column sees the key
 #pragma unroll
         for (int c4 = 0; c4 < NC / 4; ++c4) {
@@ -683,7 +683,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         m_run = fmaxf(from, m);
         const float alpha = from == -INFINITY ? 0.f : tc::ex2_approx(from - m_run);
         const float beta = m == -INFINITY ? 0.f : tc::ex2_approx(m - m_run);
-        s_ab[(i & 1) * NC + tok] = make_float4(alpha, beta, beta * exp2i(vmax), 0.f);
+        s_ab[(i & 1) * NC + tok] = make_float4(alpha, beta, beta * exp2i(vmax - kUnitExp), 0.f);
       }
       if (i > 0) gather(i - 1);   // (whose factors all warps have seen written)
       if (i == n_mine) break;
@@ -793,7 +793,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ De
     l = fmaf(s_ml[z][1], w, l);
   }
   const int t = c / a.G, hq = cut.hk * a.G + c - t * a.G;
-  a.out[cut.b * a.so[0] + hq * a.so[1] + t * a.so[2] + ch] = __float2bfloat16_rn(o / l);
+  a.out[cut.b * a.so[0] + hq * a.so[1] + t * a.so[2] + ch] = __float2bfloat16_rn(o / l * exp2i(kUnitExp));
 }
 
 // At most so many CTAs have tiles: `units` units of at most `tiles` tiles each.

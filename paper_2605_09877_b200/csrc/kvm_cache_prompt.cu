@@ -7,9 +7,11 @@
 // Two products with e4m3 operands take the tensor core as long as one with 16-bit operands, so the keys need no conversion; the weights would
 // need their two parts for every element, on the warps that already bound the kernel, so for P V it is the codes that are converted, once
 // per tile, by warps of their own.
-// Scales: that of a block of keys multiplies the logits of its columns, 16 columns (the smallest page) at a time; that of a block of values
-// goes into its fp16 form, relative to the largest of the CTA's visible blocks, 2^vbase (a power of two: exact, but for what is
-// below 2^-24 of it).
+// Scales: that of a block of keys multiplies the logits of its columns, 16 columns (the smallest page) at a time.  That of a block of values is a
+// power of two relative to the largest of the CTA's visible blocks, 2^vbase: it goes into the fp16 values (exact to 2^-24) unless some visible
+// block lies more than kNarrow powers below.  Then a row that does not see the largest block could lose what it sees, so the scales are
+// added to the exponents of the weights instead and taken out of the row sum again (625 -> 692 us where every CTA does that, two prompts of
+// 8192 tokens and 16 heads).
 //   warp 0       producer of keys: page numbers and scales ahead, TMA into a ring of three tiles; warp 3 the same for values, four tiles
 //   warp 1       issues S into three accumulators, warp 2 issues P V (one thread each)
 //   warps 4-19   softmax: tile j belongs to the eight warps of group j % 2, two threads per row, 64 columns each; S is read from tensor memory
@@ -22,6 +24,7 @@
 //
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "kvm_cache.cuh"
 #include "out_stage.cuh"
@@ -56,15 +59,16 @@ struct PromptArgs {
 struct alignas(16) PromptTile {
   int flags;          // 1: some scale is NaN, or some row does not see some key
   int pos[8];         // per 16 columns: position of the first key,
-  float ks[8];        // scale of the keys
+  float ks[8], ve[8]; // scale of the keys, exponent of the values' scale
 };
 struct alignas(16) ValueTile {
   int all;            // every key is seen by some row
   int pos[8];         // per page: position of the first key,
-  uint32_t vs[8];     // scale of the values, two fp16 each, relative to 2^vbase
+  uint32_t vs[8];     // scale of the values for their fp16 form, two fp16 each
 };
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
 constexpr int kRows = 128; // rows of a CTA
+constexpr int kNarrow = 14;
 constexpr int kThreads = 768;
 constexpr int kValueInfo = 4;   // (as many as value tiles: written when the tile is free)
 
@@ -176,7 +180,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + PB_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [4]
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);   // [4] largest, [4] smallest
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the merge waits for this kernel before it reads what it wrote)
   PromptWork w;
@@ -214,9 +218,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  // largest exponent of the visible blocks' value scales, found by the converting warps (complete behind PB_VBASE)
-  auto vbase_found = [&]() {
+  // largest exponent of the visible blocks' value scales, and whether some lie too far below, found by the converting warps (complete
+  // behind PB_VBASE)
+  auto vbase_found = [&](bool& wide) {
     const int v = max(max(s_vmax[0], s_vmax[1]), max(s_vmax[2], s_vmax[3]));
+    wide = v - min(min(s_vmax[4], s_vmax[5]), min(s_vmax[6], s_vmax[7])) > kNarrow;
     return v == -1000 ? 0 : v;
   };
 
@@ -253,9 +259,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         return g;
       };
       int vbase = 0;
+      bool wide = false;
       if (!keys) {
         tc::mbar_wait_tight(&bars[PB_VBASE], 0);   // (should it run out, so do the waits for what comes after)
-        vbase = vbase_found();
+        vbase = vbase_found(wide);
       }
       Page cur{}, nxt{};
       bool ok = true;
@@ -281,14 +288,16 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           PromptTile& ti = info[j % kInfo];
           if (lp == 0) ti.flags = nans || !all ? 1 : 0;
           const float ks = nan ? __int_as_float(0x7fc00000) : exp2i(cur.ke);
+          const float ve = nan ? 0.f : (float)cur.ve;   // (nobody looks at what is NaN or not there)
           for (int i = 0; i < p.page / 16; ++i) {
             ti.ks[lp * (p.page / 16) + i] = ks;
             ti.pos[lp * (p.page / 16) + i] = cur.pos + 16 * i;
+            ti.ve[lp * (p.page / 16) + i] = ve;
           }
         } else if (mine) {
           if (lp == 0) vinfo[s].all = all;
           vinfo[s].pos[lp] = cur.pos;
-          const __half h = __float2half_rn(nan || cur.row < 0 ? 0.f : exp2i(max(cur.ve - vbase, -126)));
+          const __half h = __float2half_rn(nan || cur.row < 0 ? 0.f : wide ? 1.f : exp2i(cur.ve - vbase));
           vinfo[s].vs[lp] = (uint32_t)__half_as_ushort(h) * 0x10001u;
         }
         __syncwarp();
@@ -363,18 +372,20 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     constexpr int N = PIECES / 4;              // a warp's lanes take eight rows and four pieces at a time: no two share a bank
     const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
     {
-      int v = -1000;
+      int v = -1000, low = 1000;
 #pragma unroll 1
       for (int i = tid - 640; i < w.ntiles * ppt; i += 128) {
         int p0;
         const int page = page_of(i, p0);
         if (page < 0) continue;
         const int e = scale_exp(p.vs[page * p.Hkv + w.hk]);
-        if (e < 128) v = max(v, e);
+        if (e < 128) { v = max(v, e); low = min(low, e); }
       }
       v = __reduce_max_sync(0xffffffffu, v);
+      low = __reduce_min_sync(0xffffffffu, low);
       if (lane == 0) {
         s_vmax[warp - 20] = v;
+        s_vmax[4 + warp - 20] = low;
         tc::mbar_arrive(&bars[PB_VBASE]);
       }
     }
@@ -409,8 +420,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const uint32_t f2 = vt.vs[(rows0 + 8 * (i / N)) >> p.page_shift];
         auto scaled = [&](uint32_t code2) {
           const uint32_t h = e4m3x2_to_f16x2(code2);
-          const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&f2));
-          return *reinterpret_cast<const uint32_t*>(&r);
+          const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&f2));
+          return *reinterpret_cast<const uint32_t*>(&x);
         };
         uint4 lo, hi;
         lo.x = scaled(c[i].x & 0xffff); lo.y = scaled(c[i].x >> 16); lo.z = scaled(c[i].y & 0xffff); lo.w = scaled(c[i].y >> 16);
@@ -501,131 +512,157 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     bool bad = !(cq == cq);   // NaN rows are marked, not computed with
     if (bad) cq = 0.f;
     float m_ref = -INFINITY, l_run = 0.f;   // l_run is relative to 2^m_ref
-    bool ok = true;
+    bool ok = tc::mbar_wait_tight(&bars[PB_VBASE], 0);
+    bool wide;   // (uniform)
+    const float vbase = (float)vbase_found(wide);
     float* my_xm = xm + group * 512;   // [tile parity of the group][half][row]
-    uint32_t s = group, par = 0, flip = 0;   // tile j: accumulator j % 3, its phase (j / 3) & 1
+    // (one of two builds of the loop: with the values' scales in the exponents, and without)
+    auto walk = [&](auto in_exponents) {
+      constexpr bool wide = decltype(in_exponents)::value;
+      uint32_t s = group, par = 0, flip = 0;   // tile j: accumulator j % 3, its phase (j / 3) & 1
 #pragma unroll 1
-    for (int j = group; j < w.ntiles; j += 2, flip ^= 1) {
-      const uint32_t ts = lanes + Cfg::COL_S + 128 * s, sb = s == 0 ? 2 : s - 1, parb = s == 0 ? par ^ 1 : par;   // (sb, parb: of the tile before)
-      if (!tc::mbar_wait_tight(&bars[PB_SFULL + s], par)) ok = false;
-      __syncwarp();
-      tc::tc_fence_after();
-      const PromptTile& ti = info[j % kInfo];
-      const bool slow = ti.flags;   // (uniform) masks, or NaN scales
-      // S of columns 64 half + 32 c .. + 31; what the row does not see as -inf
-      auto load = [&](int c, uint32_t (&x)[32]) {
-        tc::tmem_ld32(ts + 64 * half + 32 * c, x);
-        tc::tmem_wait_ld();
-        if (slow) {
-          // bit i: the row sees column i.  j <= pos_row, and j > pos_row - window or j < sinks
-          auto below = [&](int n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1u; };   // columns i < n of 16
-          const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
-          uint32_t see = 0;
+      for (int j = group; j < w.ntiles; j += 2, flip ^= 1) {
+        const uint32_t ts = lanes + Cfg::COL_S + 128 * s, sb = s == 0 ? 2 : s - 1, parb = s == 0 ? par ^ 1 : par;   // (sb, parb: of the tile before)
+        if (!tc::mbar_wait_tight(&bars[PB_SFULL + s], par)) ok = false;
+        __syncwarp();
+        tc::tc_fence_after();
+        const PromptTile& ti = info[j % kInfo];
+        const bool slow = ti.flags;   // (uniform) masks, or NaN scales
+        // S of columns 64 half + 32 c .. + 31; what the row does not see as -inf
+        auto load = [&](int c, uint32_t (&x)[32]) {
+          tc::tmem_ld32(ts + 64 * half + 32 * c, x);
+          tc::tmem_wait_ld();
+          if (slow) {
+            // bit i: the row sees column i.  j <= pos_row, and j > pos_row - window or j < sinks
+            auto below = [&](int n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1u; };   // columns i < n of 16
+            const int low = pos_row - a.window;   // (window <= 2^31 - 1 and pos_row >= 0: no overflow)
+            uint32_t see = 0;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const int key0 = ti.pos[4 * half + 2 * c + g];
+              const float ks = ti.ks[4 * half + 2 * c + g];
+              uint32_t cols = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
+              if (!(ks == ks)) {
+                bad = bad || cols;
+                cols = 0;
+              }
+              see |= cols << (16 * g);
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = (see >> i) & 1 ? x[i] : 0xff800000u;
+          }
+        };
+        float mx = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          uint32_t x[32];
+          load(c, x);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const int key0 = ti.pos[4 * half + 2 * c + g];
-            const float ks = ti.ks[4 * half + 2 * c + g];
-            uint32_t cols = below(pos_row - key0 + 1) & (~below(low < key0 ? 0 : low - key0 + 1) | below(a.sinks - key0));
-            if (!(ks == ks)) {
-              bad = bad || cols;
-              cols = 0;
+            float m = __uint_as_float(x[16 * g]), m2 = __uint_as_float(x[16 * g + 1]);
+#pragma unroll
+            for (int i = 2; i < 14; i += 4) {
+              m = tc::fmax3(m, __uint_as_float(x[16 * g + i]), __uint_as_float(x[16 * g + i + 1]));
+              m2 = tc::fmax3(m2, __uint_as_float(x[16 * g + i + 2]), __uint_as_float(x[16 * g + i + 3]));
             }
-            see |= cols << (16 * g);
+            m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
+            // (the factor is never 0 or NaN: a masked column is -inf)
+            float y = fmaxf(m, m2) * fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f);
+            if constexpr (wide) y += fmaxf(ti.ve[4 * half + 2 * c + g] - vbase, -(float)kFoldMost);
+            mx = fmaxf(mx, y);
           }
-#pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = (see >> i) & 1 ? x[i] : 0xff800000u;
         }
-      };
-      float mx = -INFINITY;
+        // the maximum of the row's other half, and the reference of the tile before
+        float* x2 = my_xm + flip * 256;
+        x2[half * 128 + row] = mx;
+        if (j > 0 && !tc::mbar_wait_tight(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
+        ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);
+        if (!ok) break;
+        mx = fmaxf(mx, x2[(1 - half) * 128 + row]);
+        // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
+        float m = j > 0 ? s_m[row] : -INFINITY;
+        if (__any_sync(0xffffffffu, mx > m + 8.0f || j == 0)) {   // (the same decision in both warps)
+          const float mnew = fmaxf(m, mx);
+          if (j > 0) {
+            // all earlier P V products must have landed before O is touched; each warp takes half of the channels
+            if (!tc::mbar_wait_tight(&bars[PB_PVDONE + sb], parb)) ok = false;
+            __syncwarp();
+            tc::tc_fence_after();
+            const float corr = (m == -INFINITY) ? 0.f : tc::ex2_approx(m - mnew);
 #pragma unroll 1
-      for (int c = 0; c < 2; ++c) {
-        uint32_t x[32];
-        load(c, x);
+            for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
+              uint32_t r[32];
+              tc::tmem_ld32(to + c * 32, r);
+              tc::tmem_wait_ld();
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          float m = __uint_as_float(x[16 * g]), m2 = __uint_as_float(x[16 * g + 1]);
-#pragma unroll
-          for (int i = 2; i < 14; i += 4) {
-            m = tc::fmax3(m, __uint_as_float(x[16 * g + i]), __uint_as_float(x[16 * g + i + 1]));
-            m2 = tc::fmax3(m2, __uint_as_float(x[16 * g + i + 2]), __uint_as_float(x[16 * g + i + 3]));
+              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+              tc::tmem_st32(to + c * 32, r);
+            }
+            tc::tmem_wait_st();
+            ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);   // (both have read the reference)
           }
-          m = tc::fmax3(m, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
-          // (the factor is never 0 or NaN: a masked column is -inf)
-          mx = fmaxf(mx, fmaxf(m, m2) * fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f));
+          m = mnew;
+          if (half == 0) s_m[row] = m;
         }
-      }
-      // the maximum of the row's other half, and the reference of the tile before
-      float* x2 = my_xm + flip * 256;
-      x2[half * 128 + row] = mx;
-      if (j > 0 && !tc::mbar_wait_tight(&bars[PB_REF + quarter * 3 + sb], parb)) ok = false;
-      ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);
-      if (!ok) break;
-      mx = fmaxf(mx, x2[(1 - half) * 128 + row]);
-      // the reference of the row: that of the tile before, unless this tile's maximum is more than 2^8 above it
-      float m = j > 0 ? s_m[row] : -INFINITY;
-      if (__any_sync(0xffffffffu, mx > m + 8.0f || j == 0)) {   // (the same decision in both warps)
-        const float mnew = fmaxf(m, mx);
-        if (j > 0) {
-          // all earlier P V products must have landed before O is touched; each warp takes half of the channels
-          if (!tc::mbar_wait_tight(&bars[PB_PVDONE + sb], parb)) ok = false;
-          __syncwarp();
-          tc::tc_fence_after();
-          const float corr = (m == -INFINITY) ? 0.f : tc::ex2_approx(m - mnew);
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars[PB_REF + quarter * 3 + s]);
+        // (a wait that ran out is acted on at the next barrier of the pair, by both warps)
+        l_run = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m);
+        m_ref = m;
+        const float neg_m = (m == -INFINITY) ? 0.f : -m;
+        const uint64_t neg_m2 = pack2(neg_m, neg_m);
+        uint64_t s0 = 0, s1 = 0;   // sums of the tile's weights
 #pragma unroll 1
-          for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
-            uint32_t r[32];
-            tc::tmem_ld32(to + c * 32, r);
-            tc::tmem_wait_ld();
+        for (int c = 0; c < 2; ++c) {
+          uint32_t x[32], wd[16];
+          load(c, x);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
-            tc::tmem_st32(to + c * 32, r);
+          for (int g = 0; g < 2; ++g) {
+            const float f = fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f);
+            const uint64_t f2 = pack2(f, f);
+            float vr = 0.f, fold = 0.f;
+            uint64_t a2 = neg_m2;
+            if constexpr (wide) {
+              vr = ti.ve[4 * half + 2 * c + g] - vbase;
+              fold = fmaxf(vr, -(float)kFoldMost);
+              a2 = pack2(neg_m + fold, neg_m + fold);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint64_t y = fma2(pack2(__uint_as_float(x[16 * g + 2 * i]), __uint_as_float(x[16 * g + 2 * i + 1])), f2, a2);
+              float p0, p1;
+              unpack2(y, p0, p1);
+              p0 = tc::ex2_approx(p0);
+              p1 = tc::ex2_approx(p1);
+              const uint64_t p2 = pack2(p0, p1);
+              if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
+              const __half2 h2 = __floats2half2_rn(p0, p1);
+              wd[8 * g + i] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            if constexpr (wide) {
+              float l0, l1;
+              unpack2(add2(s0, s1), l0, l1);
+              l_run = fmaf(l0 + l1, exp2i(-(int)fold), l_run);
+              s0 = s1 = 0;
+              if (vr < fold) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wd[8 * g + i] = 0;
+              }
+            }
           }
-          tc::tmem_wait_st();
-          ok = pair_barrier(2 + 1 + group * 4 + quarter, ok);   // (both have read the reference)
+          tc::tmem_st16(ts + 64 * half + 16 * c, wd);   // (columns that this thread has read)
         }
-        m = mnew;
-        if (half == 0) s_m[row] = m;
+        tc::tmem_wait_st();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars[PB_READY + s]);
+        float l0, l1;
+        unpack2(add2(s0, s1), l0, l1);
+        l_run += l0 + l1;
+        if (s == 0) s = 2; else { --s; par ^= 1; }
       }
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&bars[PB_REF + quarter * 3 + s]);
-      // (a wait that ran out is acted on at the next barrier of the pair, by both warps)
-      l_run = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m);
-      m_ref = m;
-      const float neg_m = (m == -INFINITY) ? 0.f : -m;
-      const uint64_t a2 = pack2(neg_m, neg_m);
-      uint64_t s0 = 0, s1 = 0;   // sums of the tile's weights
-#pragma unroll 1
-      for (int c = 0; c < 2; ++c) {
-        uint32_t x[32], wd[16];
-        load(c, x);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const float f = fmaxf(cq * ti.ks[4 * half + 2 * c + g], 1.17549435e-38f);
-          const uint64_t f2 = pack2(f, f);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint64_t y = fma2(pack2(__uint_as_float(x[16 * g + 2 * i]), __uint_as_float(x[16 * g + 2 * i + 1])), f2, a2);
-            float p0, p1;
-            unpack2(y, p0, p1);
-            p0 = tc::ex2_approx(p0);
-            p1 = tc::ex2_approx(p1);
-            const uint64_t p2 = pack2(p0, p1);
-            if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
-            const __half2 h2 = __floats2half2_rn(p0, p1);
-            wd[8 * g + i] = *reinterpret_cast<const uint32_t*>(&h2);
-          }
-        }
-        tc::tmem_st16(ts + 64 * half + 16 * c, wd);   // (columns that this thread has read)
-      }
-      tc::tmem_wait_st();
-      tc::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&bars[PB_READY + s]);
-      if (s == 0) s = 2; else { --s; par ^= 1; }
-      float l0, l1;
-      unpack2(add2(s0, s1), l0, l1);
-      l_run += l0 + l1;
-    }
+    };
+    if (wide) walk(std::true_type{}); else walk(std::false_type{});
     if (ok) ok = tc::mbar_wait_tight(&bars[PB_LAST], 0);
     if (!ok) fail();
     __syncwarp();
@@ -641,7 +678,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     bad = s_l[512 + row] + s_l[640 + row] + s_l[768 + row] + s_l[896 + row] != 0.f;
     uint8_t* stage = base + Cfg::OFF_Q;   // (the queries are not needed any more)
     const int rg = w.row0 + row, tokr = args.by_group.div(rg), hqr = w.hk * a.G + rg - tokr * a.G;
-    const float vunit = exp2i(vbase_found()), unit = bad ? nan : w.parts == 1 ? vunit / l : vunit;
+    const float vunit = exp2i((int)vbase - kUnitExp), unit = bad ? nan : w.parts == 1 ? vunit / l : vunit;
     if (good && part4 < D / 32) {
       const int c = part4;   // 32 channels
       uint32_t r[32];
@@ -657,11 +694,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           mine[(D + 1) * 128 + row] = bad ? nan : l;
         }
       } else if (args.out_vec) {   // rows go through shared memory, so that the global stores are whole rows of 16-byte pieces
-        stage_row32<D>(stage, row, c, r, unit);
+        stage_row32<D>(stage, row, c, r, unit * exp2i(kUnitExp));
       } else if (row < w.rows) {
         __nv_bfloat16* orow = a.out + w.b * a.so[0] + hqr * a.so[1] + tokr * a.so[2] + c * 32;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) orow[i] = __float2bfloat16_rn(__uint_as_float(r[i]) * unit);
+        for (int i = 0; i < 32; ++i) orow[i] = __float2bfloat16_rn(__uint_as_float(r[i]) * unit * exp2i(kUnitExp));
       }
     }
     if (w.parts == 1 && args.out_vec) {
@@ -716,7 +753,7 @@ __global__ void __launch_bounds__(128) prompt_combine_kernel(const __grid_consta
   const float inv = 1.f / l;
   __nv_bfloat162 h[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) h[i] = __floats2bfloat162_rn(o[2 * i] * inv, o[2 * i + 1] * inv);
+  for (int i = 0; i < 8; ++i) h[i] = __floats2bfloat162_rn(o[2 * i] * inv * exp2i(kUnitExp), o[2 * i + 1] * inv * exp2i(kUnitExp));
   if (args.out_vec) {
     reinterpret_cast<uint4*>(out)[0] = reinterpret_cast<uint4*>(h)[0];
     reinterpret_cast<uint4*>(out)[1] = reinterpret_cast<uint4*>(h)[1];

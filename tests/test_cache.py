@@ -399,6 +399,49 @@ def test_attend_against_the_definition(kvm, B, Hq, Hkv, d, P, ctx, tokens, windo
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,far", [(1, 80), (4, 40), (4, 80), (150, 30), (150, 80)])
+def test_a_huge_block_does_not_touch_the_tokens_that_do_not_see_it(kvm, T, far):
+    """The values of the call's last block (for a single token: of blocks outside its window) are 2^far times the others: tokens before it get
+    what they would get without it, to the same bound."""
+    B, H, d, P, n = 1, 2, 64, 16, 318 if T == 4 else 320
+    m = Model(kvm, B, H, d, P, 40)
+    v = rows((B, H, n, d), 2, False)
+    if T == 1:
+        v[:, :, 100:180] *= 2.0 ** far
+    m.append(rows((B, H, n, d), 1, False), v, [n])
+    v = rows((B, H, T, d), 4, False)
+    late = 2 if T == 4 else T - 50                 # (of four tokens, the last two lie in a block of their own)
+    if T > 1:
+        v[:, :, late:] *= 2.0 ** far
+    m.append(rows((B, H, T, d), 3, False), v, [T])
+    q = rows((B, 2 * H, T, d), 5)
+    if T == 1:
+        m.attend(q, [T], window=100, sinks=3)
+        return
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    m.cache.attend(q.cuda(), m.table, torch.tensor([n], dtype=torch.int32).cuda(), out=out)
+    on, qn = out.float().cpu().double().numpy(), q.double().numpy()
+    early = late // P * P if T > 4 else 2          # (a block's scale is one: rows that share the block of huge ones lose their codes to it)
+    for h in range(H):
+        K, V = m.k[0][h].values(), m.v[0][h].values()
+        for a, b, L in ((0, early, n + early), (late, T, n + T)):
+            ref, bound = ec.attend(qn[0, 2 * h:2 * h + 2, a:b].reshape(-1, d), K[:L], V[:L], np.tile(np.arange(n + a, n + b), 2), float(np.float32(d ** -0.5)))
+            assert (np.abs(on[0, 2 * h:2 * h + 2, a:b].reshape(-1, d) - ref) <= bound).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 20, 400])
+@pytest.mark.parametrize("e", [-120, 120])
+def test_values_at_the_ends_of_the_range(kvm, T, e):
+    """Values near bf16's largest and smallest: results are in range wherever the definition's are."""
+    m = Model(kvm, 1, 2, 128, 64, 40)
+    v = rows((1, 2, 1500, 128), 2, False).clamp(-4, 4) * 2.0 ** e
+    m.append(rows((1, 2, 1500, 128), 1), v, [1500])
+    m.append(rows((1, 2, T, 128), 3), v[:, :, :T], [T])
+    m.attend(rows((1, 4, T, 128), 5), [T])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 3, 150])
 def test_attend_over_blocks_of_very_different_scales(kvm, T):
     """Neighbouring blocks whose keys and values lie orders of magnitude apart, zero blocks among them; peaked and flat rows."""
