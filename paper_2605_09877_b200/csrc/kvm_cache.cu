@@ -6,7 +6,8 @@
 // relative step does not depend on the scale.  2^e over a bf16 maximum (1 + M/128) * 2^(E-127): 448 = 1.75 * 2^8, so e = E - 135, and one
 // more when M > 96.  One thread block per (block of tokens, head, k or v): every new row is read once into registers (16 bytes per
 // thread and load, all loads in flight together), the maximum is taken on the bit patterns, and the codes are written from the registers.
-// Reads 2 bytes and writes 1 per element: bound by HBM for prompts, by one chain of dependent loads (lengths, page, rows) for single tokens.
+// Reads 2 bytes and writes 1 per element: bound by HBM for prompts (4 x 8192 tokens, 32 heads, d = 128: 143 us, 5.6 TB/s, 86 % of the measured
+// copy rate), by one chain of dependent loads (lengths, page, rows) for single tokens (64 sequences, 8 heads: 6 us on the GPU).
 #include <algorithm>
 #include <atomic>
 #include <new>
@@ -152,7 +153,8 @@ void launch_append(const AppendArgs& a, cudaStream_t s) {
 }
 
 // Copies of pages: (source, destination) pairs in the launch's arguments, at most N at a time.  Block (pair, part): a run of kCopyPart
-// bytes of the pair's keys or values, all loads of a thread in flight before its first store; part 0 moves the scales too.
+// bytes of the pair's keys or values, all loads of a thread in flight before its first store; part 0 moves the scales too.  2000 pages of
+// 64 x 128, 8 heads: 88 us, 6.0 TB/s (91 % of the measured copy rate; 102 us with 480 pairs per launch).
 constexpr int kCopyPart = 256 * 16 * 4;
 template <int N>
 struct CopyArgs {

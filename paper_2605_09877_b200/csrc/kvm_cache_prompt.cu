@@ -22,6 +22,10 @@
 //   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 // With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.
 //
+// Bound by the softmax warps and the conversion: 1600 instructions per scheduler and tile (128 x 128) against 1024 cycles of the tensor core, 2300
+// cycles a tile; and by 8 us of set-up, filling and emptying per CTA, which is most of what short windows cost.  Measured: two prompts of
+// 8192 tokens, 16 heads, d = 128: 628 us, 875 TFLOP/s (54 % of the measured burst rate; 699 us under the power cap, 58 % of the sustained one);
+// three of 4915 to 8192, 16 heads on 4, d = 64, window 512: 189 us; 300 tokens behind 3000, 32 heads on 8: 43 us.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
