@@ -640,6 +640,20 @@ def test_attend_over_random_shapes(kvm, seed):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,Hkv,T", [(1024, 2, 1), (700, 1, 3), (300, 1, 20)])
+def test_large_batches_of_short_sequences(kvm, B, Hkv, T):
+    """As many sequences as a call may have, most of them a tile or less, some without tokens."""
+    r = random.Random(B)
+    m = Model(kvm, B, Hkv, 64, 16, 14)
+    ctx = [r.choice([0, 1, 15, 16, 17, r.randint(0, 200)]) for _ in range(B)]
+    m.append(rows((B, Hkv, 200, 64), 1), rows((B, Hkv, 200, 64), 2), ctx)
+    tokens = [r.choice([0, 1, T, T]) for _ in range(B)]
+    m.append(rows((B, Hkv, T, 64), 3), rows((B, Hkv, T, 64), 4), tokens)
+    m.attend(rows((B, 4 * Hkv, T, 64), 5), tokens)
+    m.attend(rows((B, 4 * Hkv, T, 64), 5), tokens, window=40, sinks=2)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 40])
 def test_calls_side_by_side_on_two_streams(kvm, T):
     """Calls that overlap do not touch one another's workspaces."""
