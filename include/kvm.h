@@ -419,7 +419,7 @@ kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* 
  *            rows of out behind a sequence's count are left as they were; out must not overlap q
  *   workspace device memory, 16-byte aligned, at least kvm_cache_workspace() bytes, whatever it holds; calls that may overlap
  *            on the GPU need one each
- * Products of bf16 and e4m3 and the softmax statistics are held in fp32.  Where the blocks of values that are looked at together (a tile of 128
+ * Products of bf16 and e4m3, logits and softmax statistics are held in fp32 (a query with a logit beyond its range may give NaN).  Where the blocks of values that are looked at together (a tile of 128
  * keys; for many tokens, what 128 rows of queries see) lie more than 2^90 apart, the smallest count in the row sum only.  A query that sees a page outside the pool gets NaN rows, as does
  * one whose q, or whose visible blocks, hold an infinity or a NaN; a sequence whose lengths are not allowed gets none.
  * Results are deterministic.  Waits on the device are bounded: should one run out, *status is KVM_ERR_TIMEOUT.

@@ -663,7 +663,9 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
               if (++gg == a.G) { gg = 0; ++t; }
             }
           }
-          if (!any) {   // whatever the ring or the page holds there must not meet the weight 0
+          // whatever the ring or the page holds there must not meet the weight 0 (a block with a NaN scale may be one that was not loaded, and
+          // that some columns do not see)
+          if (!any || ve > 127) {
             uint4* row = reinterpret_cast<uint4*>(base + s * Cfg::STAGE + Cfg::TILE + tok * D);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) row[(k + lane) % (D / 16)] = make_uint4(0, 0, 0, 0);   // (in an order that spreads over the banks)

@@ -66,8 +66,8 @@ struct alignas(16) PromptTile {
   float ks[8], ve[8]; // scale of the keys, exponent of the values' scale
 };
 struct alignas(16) ValueTile {
-  int all;            // every key is seen by some row
-  int pos[8];         // per page: position of the first key,
+  int all;            // every key is there and is seen by some row
+  int pos[8];         // per page: position of the first key (kNowhere: not loaded),
   uint32_t vs[8];     // scale of the values for their fp16 form, two fp16 each
 };
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
@@ -284,9 +284,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const bool mine = lt == t, nan = cur.ke > 127 || cur.ve > 127;
         const uint32_t loads = __ballot_sync(0xffffffffu, mine && cur.row >= 0);
         const uint32_t nans = __ballot_sync(0xffffffffu, mine && nan);   // (pages outside the pool among them)
-        // keys: all rows see all keys of the page; values: some row sees each of them
+        // keys: all rows see all keys of the page; values: they are there, and some row sees each of them
         const bool seen = keys ? page_seen_by_all(p, cur.pos, w.first, w.last, a.window, a.sinks)
-                               : cur.pos + p.page - 1 <= w.last && (cur.pos > w.first - a.window || cur.pos + p.page - 1 < a.sinks);
+                               : cur.row >= 0 && cur.pos + p.page - 1 <= w.last && (cur.pos > w.first - a.window || cur.pos + p.page - 1 < a.sinks);
         const bool all = __all_sync(0xffffffffu, !mine || seen);
         if (mine && keys) {
           PromptTile& ti = info[j % kInfo];
@@ -300,7 +300,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           }
         } else if (mine) {
           if (lp == 0) vinfo[s].all = all;
-          vinfo[s].pos[lp] = cur.pos;
+          vinfo[s].pos[lp] = cur.row >= 0 ? cur.pos : kNowhere;
           const __half h = __float2half_rn(nan || cur.row < 0 ? 0.f : wide ? 1.f : exp2i(cur.ve - vbase));
           vinfo[s].vs[lp] = (uint32_t)__half_as_ushort(h) * 0x10001u;
         }

@@ -528,6 +528,35 @@ def test_bad_lengths_and_pages_are_reported_and_nothing_else_is_touched(kvm, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [(2, 128), (8, 64), (130, 128), (130, 64)])
+def test_a_page_outside_the_pool_reaches_the_tokens_that_see_it_and_no_others(kvm, T, d):
+    """The block of the call's last token is not there: the tokens in front of the block are right, whatever an earlier call left on the chip."""
+    held = 32 if T > 2 else 31
+    last = (held + T - 1) // 16 * 16                   # the block's first position
+    m = Model(kvm, 1, 2, d, 16, 20)
+    m.append(rows((1, 2, held + T, d), 1), rows((1, 2, held + T, d), 2), [held + T])
+    q = rows((1, 4, T, d), 5)
+    table = m.table.clone()
+    table[0, last // 16] = 10 ** 6
+    nan = garbage_cache(kvm, 64, 8, d, 16)             # codes of NaN
+    nan.k_scale.fill_(1.0)
+    nan.v_scale.fill_(1.0)
+    for rep in range(3):
+        nan.attend(rows((64, 16, T, d), 3).cuda(), torch.arange(64, dtype=torch.int32).repeat(64, 1).cuda(), torch.full((64,), 800, dtype=torch.int32).cuda())
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = m.cache.attend(q.cuda(), table, torch.tensor([held], dtype=torch.int32).cuda(), status=status)
+        assert status.item() == 1
+        ahead = last - held
+        assert torch.isnan(out[0, :, ahead:].float()).all()
+        on = out[:, :, :ahead].float().cpu().double().numpy()
+        for h in range(2):
+            K, V = m.k[0][h].values(), m.v[0][h].values()
+            ref, bound = ec.attend(q[0, 2 * h:2 * h + 2, :ahead].double().numpy().reshape(-1, d), K, V, np.tile(np.arange(held, last), 2), float(np.float32(d ** -0.5)), 0, 0)
+            err = np.abs(on[0, 2 * h:2 * h + 2].reshape(-1, d) - ref)
+            assert (err <= bound).all(), (rep, h, float(np.nanmax(err / bound)), np.isnan(err).sum())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 2, 130])
 def test_infinities_and_nans_stay_where_they_are_seen(kvm, T):
     """A NaN among the keys or values reaches the queries that see its block and no other; one in q its own row only."""
