@@ -683,6 +683,27 @@ def test_large_batches_of_short_sequences(kvm, B, Hkv, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,Hq,Hkv,d,P,counts,window,sinks", [
+    (3, 8, 4, 128, 16, [1500, 0, 411], 100, 5), (3, 8, 4, 64, 64, [1500, 1, 130], 300, 0), (2, 9, 9, 64, 128, [1300, 1290], 1, 0),
+    (5, 16, 8, 128, 32, [40, 700, 64, 128, 129], 0, 0), (160, 1, 1, 64, 16, [33 + i % 3 for i in range(160)], 0, 0)])
+def test_more_row_tiles_than_there_are_multiprocessors(kvm, B, Hq, Hkv, d, P, counts, window, sinks):
+    """Short windows and short prompts: what a multiprocessor goes on to has fewer, other or no tiles.  Twice: the same bits."""
+    T = max(counts)
+    m = Model(kvm, B, Hkv, d, P, (T + 70 + P - 1) // P)
+    held = [(7 * b) % 65 for b in range(B)]
+    m.append(rows((B, Hkv, 65, d), 1), rows((B, Hkv, 65, d), 2), held)
+    k, v = rows((B, Hkv, T, d), 3), rows((B, Hkv, T, d), 4)
+    v[:, 0, T // 3] *= 2.0 ** 20                       # (blocks of values that lie far apart, for some of the rows)
+    m.append(k, v, counts)
+    q = rows((B, T, Hq, d), 5).transpose(1, 2)
+    first = m.attend(q, counts, window=window, sinks=sinks)
+    odd = torch.full((B, Hq, T, d + 1), 7.0, dtype=torch.bfloat16, device="cuda")[..., :d]     # (rows that are not 16-byte aligned)
+    qo = torch.zeros((B, Hq, T, d + 1), dtype=torch.bfloat16, device="cuda")[..., :d]
+    qo.copy_(q)
+    assert torch.equal(m.attend(qo, counts, window=window, sinks=sinks, out=odd), first)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 40])
 def test_calls_side_by_side_on_two_streams(kvm, T):
     """Calls that overlap do not touch one another's workspaces."""
