@@ -28,7 +28,7 @@
 // Bound by the softmax warps and the conversion: 1600 instructions per scheduler and tile (128 x 128) against 1024 cycles of the tensor core, 2300
 // cycles a tile; and by the set-up, filling and emptying per block of 128 rows (8 us, 7 where a CTA goes on), most of what short windows
 // cost.  Measured: two prompts of 8192 tokens, 16 heads, d = 128: 625 us, 880 TFLOP/s (54 % of the measured burst rate; 699 us under the power
-// cap, 58 % of the sustained one); three of 4915 to 8192, 16 heads on 4, d = 64, window 512: 169 us; 300 tokens behind 3000, 32 heads on 8: 43 us.
+// cap, 58 % of the sustained one); three of 4915 to 8192, 16 heads on 4, d = 64, window 512: 169 us; 300 tokens behind 3000, 32 heads on 8: 42 us.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
