@@ -98,6 +98,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
     const int w0 = warp / (TPP / 32) * (TPP / 32);
 #pragma unroll
     for (int w = 0; w < TPP / 32; ++w) top = max(top, s_top[w0 + w]);
+  } else {
+    __syncwarp();   // (every lane has read the old scale before lane 0 writes the new one: the reduction above promises no order of memory)
   }
   if (!live) return;
   const int e_old = r0 > 0 ? max(scale_exp(old), kLeastExp) : kLeastExp;

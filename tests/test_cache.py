@@ -838,3 +838,18 @@ def test_a_served_run_of_forks_windows_and_compaction(kvm):
     assert book.info()["high"] == 64 - book.info()["n_free"]
     for i in range(20):
         step([c, a], [1, 2], 600 + 10 * i, W)
+
+
+# ---- mends -----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,P", [(64, 16), (64, 32), (128, 16)])
+def test_scales_that_rise_with_every_row_of_many_blocks(kvm, d, P):
+    """One row a call, each twice the one before, in many blocks at once: every lane of a page divides what the block holds by the old scale
+    over the new one, so all of them have to read the old scale before one of them writes the new one."""
+    B, H = 24, 5
+    m = Model(kvm, B, H, d, P, 2)
+    for i in range(P + 3):
+        m.append(rows((B, H, 1, d), 100 + i) * 2.0 ** (i % P), rows((B, H, 1, d), 200 + i) * 2.0 ** (i % P // 2), [1] * B)
+    torch.cuda.synchronize()
+    m.check_codes()
