@@ -76,6 +76,10 @@ struct alignas(16) ValueTile {
 constexpr int kInfo = 8;   // ring of tile descriptions: that of tile j + 8 is written when S of tile j + 5 is done, hence P V of tile j + 2
 constexpr int kRows = 128; // rows of a CTA
 constexpr int kNarrow = 14;
+// Weights are held in units of 2^-kShift of what the row's reference stands for: at most 2^(8 + kShift) (fp16 ends at 2^16), and exact or rounded
+// to 2^-(24 + kShift) below.  A weight that comes to nothing there still counts in the row sum, so n such keys shift a row by up to
+// n 2^-(25 + kShift): with 6, 2^-11 for a million of them (without it, 2^-5: the tail of a million keys 2^-26 below the first one was lost).
+constexpr float kShift = 6.f;
 constexpr int kThreads = 768;
 constexpr int kValueInfo = 4;   // (as many as value tiles: written when the tile is free)
 
@@ -194,6 +198,12 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// two floats -> two fp16 (a in the low half), round to nearest even, saturating (logits beyond 2^24 are rounded to more than 1)
+__device__ __forceinline__ uint32_t to_f16x2(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
 }
 template <int D, bool MORE>
@@ -615,7 +625,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       float cq = s_cq[row];
       bool bad = !(cq == cq);   // NaN rows are marked, not computed with
       if (bad) cq = 0.f;
-      float m_ref = -INFINITY, l_run = 0.f;   // l_run is relative to 2^m_ref
+      float m_ref = -INFINITY, l_run = 0.f;   // l_run is relative to 2^(m_ref - kShift)
       if (!tc::mbar_wait_tight(&bars[PB_VBASE + (item & 1)], (item >> 1) & 1)) ok = false;
       bool wide;   // (uniform)
       const float vbase = (float)vbase_found(item, wide);
@@ -715,7 +725,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           // (a wait that ran out is acted on at the next barrier of the pair, by both warps)
           l_run = m_ref == -INFINITY ? 0.f : l_run * tc::ex2_approx(m_ref - m);
           m_ref = m;
-          const float neg_m = (m == -INFINITY) ? 0.f : -m;
+          const float neg_m = (m == -INFINITY) ? 0.f : kShift - m;
           const uint64_t neg_m2 = pack2(neg_m, neg_m);
           uint64_t s0 = 0, s1 = 0;   // sums of the tile's weights
 #pragma unroll 1
@@ -742,8 +752,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 p1 = tc::ex2_approx(p1);
                 const uint64_t p2 = pack2(p0, p1);
                 if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
-                const __half2 h2 = __floats2half2_rn(p0, p1);
-                wd[8 * g + i] = *reinterpret_cast<const uint32_t*>(&h2);
+                wd[8 * g + i] = to_f16x2(p0, p1);
               }
               if constexpr (wide) {
                 float l0, l1;
@@ -801,7 +810,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         __syncwarp();
         tc::tmem_ld32(to + c * 32, r);
         tc::tmem_wait_ld();
-        if (w.parts > 1) {   // partial result: O (in units of 2^m_end), m_end and the sum, [channel][row]
+        if (w.parts > 1) {   // partial result: O (in units of 2^(m_end - kShift), as the sum), m_end and the sum, [channel][row]
           float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
 #pragma unroll
           for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;

@@ -853,3 +853,24 @@ def test_scales_that_rise_with_every_row_of_many_blocks(kvm, d, P):
         m.append(rows((B, H, 1, d), 100 + i) * 2.0 ** (i % P), rows((B, H, 1, d), 200 + i) * 2.0 ** (i % P // 2), [1] * B)
     torch.cuda.synchronize()
     m.check_codes()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,G", [(1, 8), (4, 4), (75, 512)])
+@pytest.mark.parametrize("below", [22.0, 26.0, 28.5])
+def test_a_long_flat_tail_below_a_peak_counts_in_the_result(kvm, T, G, below):
+    """A million keys, each 2^-below of the first one's weight: together up to a quarter of it, and all of the result, since the first one's value is 0.
+    In closed form, to the same bound as everywhere: n w / (1 + n w)."""
+    n, d, P = 1 << 20, 64, 128
+    c = kvm.Cache.empty(n // P, 1, d, P)
+    c.v8.view(torch.uint8).fill_(0x38)                 # 1.0
+    c.k8.view(torch.uint8)[0, 0, 0, 0] = 0x38
+    c.v8.view(torch.uint8)[0, 0, 0] = 0
+    q = torch.zeros((1, G, T, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    table = torch.arange(n // P, dtype=torch.int32, device="cuda")[None]
+    out = c.attend(q, table, torch.tensor([n - T], dtype=torch.int32).cuda(), scale=below * math.log(2.0)).double().cpu()
+    tail = (torch.arange(n - T, n).double() * math.exp(-float(np.float32(below * math.log(2.0)))))[None, None, :, None]
+    ref = tail / (1 + tail)
+    bound = (2.0 ** -7 + 2.0 ** -20) * ref + 2.0 ** -11
+    assert ((out - ref).abs() <= bound).all(), (float(ref.mean()), float(out.mean()), float(out.min()))
