@@ -428,7 +428,8 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
                               int32_t window, int32_t sinks, void* out, const int64_t* q_strides, const int64_t* out_strides,
                               void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
 
-/* Bytes of workspace that kvm_cache_attend needs for these sizes (pointers are not looked at); -1 on invalid arguments. */
+/* Bytes of workspace that kvm_cache_attend needs for these sizes (pointers are not looked at); -1 on invalid arguments and on
+ * sizes that kvm_cache_attend refuses. */
 int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_q_heads);
 
 /* Copies whole pages (codes and scales of every head): page src[i] to page dst[i], i < n.  src, dst: HOST arrays, not kept.  Every dst

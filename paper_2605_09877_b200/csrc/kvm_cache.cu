@@ -253,6 +253,12 @@ kvm_status_t check_call(const kvm_cache_t* c, const kvm_cache_call_t* call, bool
 
 int64_t tiles_most(const kvm_cache_t* c, const kvm_cache_call_t* call) { return ((int64_t)call->max_pages * c->page_tokens + kTile - 1) / kTile; }
 
+// Whether what attention numbers in 32 bits fits: key tiles of the call, rows of queries of a unit, row tiles of the call.
+bool attend_fits(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t n_q_heads) {
+  const int64_t units = (int64_t)call->batch * c->n_kv_heads, rows = call->n_tokens * (n_q_heads / c->n_kv_heads);
+  return tiles_most(c, call) * units <= INT32_MAX / 2 && rows <= INT32_MAX - 128 && (rows + 127) / 128 * units <= INT32_MAX;
+}
+
 Params params_of(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t* status) {
   Params p;
   p.k = (const uint8_t*)c->k; p.v = (const uint8_t*)c->v; p.ks = c->k_scale; p.vs = c->v_scale;
@@ -343,7 +349,7 @@ KVM_API kvm_status_t kvm_cache_copy_pages(const kvm_cache_t* cache, const int32_
 
 KVM_API int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_q_heads) {
   if (check_cache(cache, false) != KVM_OK || check_call(cache, call, false) != KVM_OK) return -1;
-  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads) return -1;
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || !attend_fits(cache, call, n_q_heads)) return -1;
   const int64_t units = (int64_t)call->batch * cache->n_kv_heads, tiles = tiles_most(cache, call);
   const int64_t cols = call->n_tokens * (n_q_heads / cache->n_kv_heads);
   return cols <= kDecodeCols ? decode_workspace(units, tiles, cache->head_dim, (int)cols) : prompt_workspace(units, cols, tiles, cache->head_dim);
@@ -365,10 +371,8 @@ KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_
       !strides_of(out_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, true, a.so)) return KVM_ERR_INVALID_ARG;
   a.Hq = n_q_heads; a.G = n_q_heads / cache->n_kv_heads; a.d = cache->head_dim;
   a.window = window ? window : INT32_MAX; a.sinks = std::min(sinks, 1 << 30);
+  if (!attend_fits(cache, call, n_q_heads)) return KVM_ERR_UNSUPPORTED;
   const int64_t tiles = tiles_most(cache, call);
-  // tiles of the call, and its rows of queries, are numbered in 32 bits
-  if (tiles * a.p.batch * a.p.Hkv > INT32_MAX / 2 || a.p.T * a.G > INT32_MAX - 128) return KVM_ERR_UNSUPPORTED;
-  if ((a.p.T * a.G + 127) / 128 * a.p.batch * a.p.Hkv > INT32_MAX) return KVM_ERR_UNSUPPORTED;
   a.scale_log2 = scale * 1.4426950408889634f;
   const int64_t need = kvm_cache_workspace(cache, call, n_q_heads);
   if (need < 0) return KVM_ERR_UNSUPPORTED;

@@ -874,3 +874,12 @@ def test_a_long_flat_tail_below_a_peak_counts_in_the_result(kvm, T, G, below):
     ref = tail / (1 + tail)
     bound = (2.0 ** -7 + 2.0 ** -20) * ref + 2.0 ** -11
     assert ((out - ref).abs() <= bound).all(), (float(ref.mean()), float(out.mean()), float(out.min()))
+
+
+@pytest.mark.parametrize("groups,batch,n_tokens,max_pages", [(256, 4, 1 << 30, 256), (512, 4, 1 << 30, 256), (2, 4, 1 << 30, 256), (64, 1024, 1 << 24, 256), (1, 1024, 1, 1 << 24)])
+def test_sizes_that_attention_refuses_have_no_workspace(kvm, groups, batch, n_tokens, max_pages):
+    """Query rows, row tiles and key tiles of a call are numbered in 32 bits; both entry points say so before anything is narrowed."""
+    d, x = C.byref(_desc(kvm, n_pages=1 << 16, n_kv_heads=128)), 1 << 26
+    c = C.byref(_call(kvm, count=1 << 24, batch=batch, n_tokens=n_tokens, max_pages=max_pages))
+    assert kvm.lib.kvm_cache_attend(d, c, x, 128 * groups, 1.0, 0, 0, 2 * x, None, None, x, 1 << 62, None, None) == 2
+    assert kvm.lib.kvm_cache_workspace(d, c, 128 * groups) == -1
