@@ -614,7 +614,7 @@ class Pages:
         self.n_pages = n_pages
 
     def __del__(self):
-        if getattr(self, "_h", None):
+        if getattr(self, "_h", None) and lib is not None:   # (None: the interpreter is ending, and the memory goes with it)
             lib.kvm_pages_destroy(self._h)
             self._h = None
 

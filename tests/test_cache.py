@@ -883,3 +883,13 @@ def test_sizes_that_attention_refuses_have_no_workspace(kvm, groups, batch, n_to
     c = C.byref(_call(kvm, count=1 << 24, batch=batch, n_tokens=n_tokens, max_pages=max_pages))
     assert kvm.lib.kvm_cache_attend(d, c, x, 128 * groups, 1.0, 0, 0, 2 * x, None, None, x, 1 << 62, None, None) == 2
     assert kvm.lib.kvm_cache_workspace(d, c, 128 * groups) == -1
+
+
+def test_a_book_of_pages_that_outlives_the_module_ends_quietly(kvm):
+    """At the interpreter's end the module's names may be gone before the last Pages is."""
+    import os
+    import subprocess
+    import sys
+    code = "import sys; from paper_2605_09877_b200 import kvm; p = kvm.Pages(8, 16); sys.kept = kvm.Pages(8, 16); q = kvm.Pages(4, 64); del q"
+    r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stderr == "", r.stderr
