@@ -7,6 +7,7 @@ been built (python -m paper_2605_09877_b200.build) -- there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from dataclasses import dataclass
 
@@ -509,6 +510,28 @@ def _strides3(t):
     return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
+def _int(x, bits=32):
+    """x as a number that a C integer of so many bits holds (ctypes would cut off the rest)."""
+    x = operator.index(x)
+    if not -(1 << bits - 1) <= x < 1 << bits - 1:
+        raise ValueError(f"{x} does not fit into {bits} bits")
+    return x
+
+
+def _page_list(x):
+    """Page numbers on the host as contiguous int32."""
+    x = torch.as_tensor(x)
+    if x.is_cuda or x.dim() != 1:
+        raise ValueError("src and dst are lists of page numbers on the host")
+    if x.dtype != torch.int32 and x.numel():
+        if x.dtype == torch.bool or x.is_floating_point() or x.is_complex():
+            raise ValueError("page numbers are whole numbers")
+        x = x.to(torch.int64)
+        if x.min() < -(1 << 31) or x.max() >= 1 << 31:
+            raise ValueError("page numbers are of 32 bits")
+    return x.to(torch.int32).contiguous()
+
+
 class Cache:
     """A pool of pages for exact keys and values in 8 bits (kvm_cache_t): codes k8, v8 float8_e4m3fn [n_pages, n_kv_heads, page_tokens,
     head_dim], scales fp32 [n_pages, n_kv_heads] (powers of two; a row stands for code * scale).  The tensors are the caller's;
@@ -571,6 +594,7 @@ class Cache:
         """kvm_cache_attend: q bf16 [B, n_q_heads, T, head_dim] over the cache, which holds the T tokens' own keys already; a token sees
         the last `window` positions up to its own (0: all) and the first `sinks`.  scale: 1 / sqrt(head_dim) unless given.  Rows of `out`
         behind a sequence's count are left as they were (unset where `out` is made here)."""
+        window, sinks = _int(window), _int(sinks)
         if q.dim() != 4 or q.shape[3] != self.head_dim or (out is not None and out.shape != q.shape):
             raise ValueError("q, out [batch, n_q_heads, tokens, head_dim]")
         if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
@@ -592,9 +616,9 @@ class Cache:
 
     def copy_pages(self, src, dst, stream=None):
         """kvm_cache_copy_pages: page src[i] to page dst[i]; lists or CPU int32 tensors."""
-        src, dst = (torch.as_tensor(x, dtype=torch.int32).contiguous() for x in (src, dst))
-        if src.is_cuda or dst.is_cuda or src.dim() != 1 or src.shape != dst.shape:
-            raise ValueError("src and dst are lists of the same length on the host")
+        src, dst = _page_list(src), _page_list(dst)
+        if src.shape != dst.shape:
+            raise ValueError("src and dst are lists of the same length")
         if self._elsewhere():
             with torch.cuda.device(self._device):
                 return self.copy_pages(src, dst, stream)
@@ -609,7 +633,7 @@ class Pages:
     def __init__(self, n_pages: int, page_tokens: int = 64):
         self._h = None
         h = C.c_void_p()
-        self._do("kvm_pages_create", n_pages, page_tokens, C.byref(h))
+        self._do("kvm_pages_create", _int(n_pages, 64), _int(page_tokens), C.byref(h))
         self._h = h
         self.n_pages = n_pages
 
@@ -630,20 +654,20 @@ class Pages:
 
     def fork(self, seq: int) -> int:
         child = C.c_int32()
-        self._do("kvm_pages_fork", self._h, seq, C.byref(child))
+        self._do("kvm_pages_fork", self._h, _int(seq), C.byref(child))
         return child.value
 
     def close(self, seq: int):
-        self._do("kvm_pages_close", self._h, seq)
+        self._do("kvm_pages_close", self._h, _int(seq))
 
     def extend(self, seq: int, n_tokens: int):
         """Room for n_tokens more tokens; (src, dst) of the page to copy before the append, or None."""
         src, dst = C.c_int32(), C.c_int32()
-        self._do("kvm_pages_extend", self._h, seq, n_tokens, C.byref(src), C.byref(dst))
+        self._do("kvm_pages_extend", self._h, _int(seq), _int(n_tokens, 64), C.byref(src), C.byref(dst))
         return (src.value, dst.value) if src.value >= 0 else None
 
     def trim(self, seq: int, window: int, sinks: int = 0):
-        self._do("kvm_pages_trim", self._h, seq, window, sinks)
+        self._do("kvm_pages_trim", self._h, _int(seq), _int(window), _int(sinks))
 
     def compact(self):
         """(src, dst): the copies to make before the next call over the cache, as CPU int32 tensors."""
@@ -653,7 +677,7 @@ class Pages:
         return src[:n.value].clone(), dst[:n.value].clone()
 
     def table(self, seq: int):
-        n = C.c_int64()
+        seq, n = _int(seq), C.c_int64()
         self._do("kvm_pages_table", self._h, seq, None, 0, C.byref(n), None)
         out = (C.c_int32 * max(1, n.value))()
         self._do("kvm_pages_table", self._h, seq, out, n.value, None, None)
@@ -661,7 +685,7 @@ class Pages:
 
     def length(self, seq: int) -> int:
         n = C.c_int64()
-        self._do("kvm_pages_table", self._h, seq, None, 0, None, C.byref(n))
+        self._do("kvm_pages_table", self._h, _int(seq), None, 0, None, C.byref(n))
         return n.value
 
     def tables(self, seqs, max_pages: int = 0, device="cuda"):

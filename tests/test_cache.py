@@ -893,3 +893,24 @@ def test_a_book_of_pages_that_outlives_the_module_ends_quietly(kvm):
     code = "import sys; from paper_2605_09877_b200 import kvm; p = kvm.Pages(8, 16); sys.kept = kvm.Pages(8, 16); q = kvm.Pages(4, 64); del q"
     r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stderr == "", r.stderr
+
+
+def test_binding_takes_no_number_for_another(kvm):
+    """Numbers that 32 (or 64) bits do not hold are refused, not cut to those that are left; page numbers are whole."""
+    p = kvm.Pages(8, 16)
+    s = p.open()
+    p.extend(s, 40)
+    for bad in (lambda: kvm.Pages(8, (1 << 32) + 16), lambda: kvm.Pages((1 << 64) + 8, 16), lambda: p.fork((1 << 32) + s), lambda: p.close((1 << 32) + s),
+                lambda: p.table((1 << 32) + s), lambda: p.length(s - (1 << 32)), lambda: p.tables([(1 << 32) + s], device="cpu"),
+                lambda: p.extend(s + (1 << 32), 1), lambda: p.extend(s, (1 << 64) + 1), lambda: p.trim((1 << 32) + s, 8), lambda: p.trim(s, (1 << 32) + 8, 0),
+                lambda: p.trim(s, 8, 1 << 32)):
+        with pytest.raises(ValueError):
+            bad()
+    assert p.table(s) == [0, 1, 2] and p.length(s) == 40 and p.info() == dict(n_free=5, high=3)
+    for kw in (dict(window=1 << 32), dict(window=(1 << 32) + 512), dict(window=1 << 31), dict(sinks=1 << 32), dict(sinks=-(1 << 32) + 4)):
+        with pytest.raises(ValueError):
+            kvm.Cache.attend(None, torch.zeros(1, 1, 1, 64), None, None, **kw)
+    for src, dst in (([0], torch.tensor([(1 << 32) + 1])), (torch.tensor([1 << 32]), [1]), (np.array([-(1 << 32)]), [1]), ([0.7], [1]), (torch.tensor([0.0]), [1]),
+                     ([0], [True]), ([0, 1], [2])):
+        with pytest.raises(ValueError):
+            kvm.Cache.copy_pages(None, src, dst)
