@@ -416,7 +416,8 @@ kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* 
  * position i sees the positions j <= i with j > i - window, or j < sinks (sliding window and a few first tokens that stay
  * visible); window = 0: every j <= i.
  *   q, out   device bf16 [batch, n_q_heads, n_tokens, head_dim]; strides as in kvm_cache_append; n_q_heads a multiple of n_kv_heads;
- *            rows of out behind a sequence's count are left as they were; out must not overlap q
+ *            rows of out behind a sequence's count are left as they were; out must not overlap q, nor its rows one another
+ *            (in the order of the strides, each dimension has to step over what the smaller ones span, else INVALID_ARG)
  *   workspace device memory, 16-byte aligned, at least kvm_cache_workspace() bytes, whatever it holds; calls that may overlap
  *            on the GPU need one each
  * Products of bf16 and e4m3, logits and softmax statistics are held in fp32 (a query with a logit beyond its range may give NaN).  Where the blocks of values that are looked at together (a tile of 128

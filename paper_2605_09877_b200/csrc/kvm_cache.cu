@@ -269,13 +269,18 @@ Params params_of(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t* st
   return p;
 }
 
-// Strides of [batch, heads, tokens, d] (NULL: contiguous); vec: rows start on 16 bytes.  Rows that are written must not lie on one another.
+// Strides of [batch, heads, tokens, d] (NULL: contiguous).  Rows that are written must not lie on one another: each dimension, in the order of
+// the strides, has to step over all that the smaller ones span.
 bool strides_of(const int64_t* st, int64_t B, int64_t H, int64_t T, int d, bool written, int64_t (&out)[3]) {
   if (!st) { out[0] = H * T * d; out[1] = T * d; out[2] = d; return true; }
   const int64_t n[3] = {B, H, T};
-  for (int i = 0; i < 3; ++i) {
+  int by[3] = {0, 1, 2};
+  std::sort(by, by + 3, [&](int i, int j) { return st[i] < st[j]; });
+  __int128 span = d;   // channels from the first to the last of the rows so far
+  for (int i : by) {
     out[i] = st[i];
-    if (st[i] < 0 || (written && n[i] > 1 && st[i] < d)) return false;
+    if (st[i] < 0 || (written && n[i] > 1 && st[i] < span)) return false;
+    if (n[i] > 1) span += (__int128)(n[i] - 1) * st[i];
   }
   return true;
 }

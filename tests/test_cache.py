@@ -914,3 +914,27 @@ def test_binding_takes_no_number_for_another(kvm):
                      ([0], [True]), ([0, 1], [2])):
         with pytest.raises(ValueError):
             kvm.Cache.copy_pages(None, src, dst)
+
+
+def test_rows_of_the_output_that_lie_on_one_another_are_refused(kvm):
+    """Two heads, tokens or sequences that share bytes of `out` would be written in any order."""
+    d, c, x = C.byref(_desc(kvm)), C.byref(_call(kvm)), 1 << 26     # 2 sequences, 4 heads, 4 tokens, 128 channels
+    for st in ((128, 128, 128), (2048, 128, 128), (512, 512, 128), (1024, 512, 128), (2048, 256, 128), (2048, 512, 510), (128, 512, 128), (1 << 62, 1 << 62, 1 << 61),
+               (2047, 512, 128)):
+        assert kvm.lib.kvm_cache_attend(d, c, x, 4, 1.0, 0, 0, 2 * x, None, (C.c_int64 * 3)(*st), x, 1 << 30, None, None) == 1, st
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 40])
+def test_the_output_may_have_its_dimensions_in_any_order(kvm, T):
+    import itertools
+    B, Hq, Hkv, d = 2, 4, 2, 64
+    m = Model(kvm, B, Hkv, d, 16, 10)
+    m.append(rows((B, Hkv, 100, d), 1), rows((B, Hkv, 100, d), 2), [100, 70])
+    q = rows((B, Hq, T, d), 3)
+    for order in itertools.permutations(range(3)):
+        shape = [(B, Hq, T)[i] for i in order]
+        for pad in (0, 8):
+            wide = torch.full((*shape, d + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+            m.attend(q, [T, T], out=wide[..., :d].permute(*[order.index(i) for i in range(3)], 3))
+            assert (wide[..., d:] == 7.0).all()
