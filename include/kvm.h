@@ -194,9 +194,9 @@ kvm_status_t kvm_state_info(const kvm_state_t* state, int64_t* n_slots, int64_t*
  * (kvm_state_reset) or restored (kvm_state_import) and used again. */
 kvm_status_t kvm_state_check(kvm_state_t* state, void* cuda_stream);
 
-/* Failure-detection self test (no counterpart in the paper): launches one thread that waits, with the
- * library's bounded wait and a limit of `spins` iterations (1 .. 2^20), on a barrier that nothing ever
- * arrives at, and reports the expiry exactly as the production kernels do: KVM_ERR_TIMEOUT in the
+/* Failure-detection self test (no counterpart in the paper): launches one thread that waits, with
+ * both forms of the library's bounded wait and a limit of `spins` iterations each (1 .. 2^20), on a barrier that
+ * nothing ever arrives at, and reports the expiry of both exactly as the production kernels do: KVM_ERR_TIMEOUT in the
  * state's status word, normal return.  kvm_state_check then returns KVM_ERR_TIMEOUT once.  Touches
  * nothing else of the state. */
 kvm_status_t kvm_debug_expire_wait(kvm_state_t* state, int32_t spins, void* cuda_stream);

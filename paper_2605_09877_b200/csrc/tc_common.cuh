@@ -43,7 +43,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
 // The same in as few instructions as there are, for kernels whose warps do many different things: the loop above is unrolled at every
 // use, and there the fetching of instructions is what a wait costs (each try suspends the thread for a while by itself; with a hint
 // for a long suspension the shortest calls took 2 us longer).
-__device__ __forceinline__ bool mbar_wait_tight(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait_tight(uint64_t* bar, uint32_t parity, uint32_t limit = kSpinLimit) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
@@ -56,7 +56,7 @@ __device__ __forceinline__ bool mbar_wait_tight(uint64_t* bar, uint32_t parity) 
       "@p bra AGAIN;\n\t"
       "DONE:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "n"(kSpinLimit) : "memory");
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(limit) : "memory");
   return ok != 0;
 }
 __device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }

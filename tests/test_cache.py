@@ -938,3 +938,25 @@ def test_the_output_may_have_its_dimensions_in_any_order(kvm, T):
             wide = torch.full((*shape, d + pad), 7.0, dtype=torch.bfloat16, device="cuda")
             m.attend(q, [T, T], out=wide[..., :d].permute(*[order.index(i) for i in range(3)], 3))
             assert (wide[..., d:] == 7.0).all()
+
+
+@pytest.mark.gpu
+def test_calls_after_an_expired_wait(kvm):
+    """The self test lets both forms of the bounded wait run out, the one that the cache's kernels use among them; it is reported once, ends
+    in bounded time, and calls over a cache are as before."""
+    from paper_2605_09877_b200 import synth
+    from tests import parity_util as pu
+    wl = synth.Workload("expire", 1, 2, 2, 64, 64 * 3, 64, "sqrt", sqrt_coeff=6, r=16, seed=3)
+    st, _ = pu.gpu_layer(wl, synth.make_layer_params(wl))
+    m = Model(kvm, 2, 2, 64, 16, 20)
+    m.append(rows((2, 2, 200, 64), 1), rows((2, 2, 200, 64), 2), [200, 150])
+    for spins in (1, 10000):
+        t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        t0.record()
+        st.debug_expire_wait(spins)
+        t1.record()
+        assert st.check() == 7 and st.check() == 0
+        assert t0.elapsed_time(t1) < 2000
+        for T in (1, 30):
+            m.attend(rows((2, 4, T, 64), 3), [T, T])
+    st.free()
