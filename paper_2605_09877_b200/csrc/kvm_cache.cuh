@@ -61,7 +61,7 @@ __device__ __forceinline__ bool page_seen_by_all(const Params& p, int p0, int fi
   return end <= first && (p0 > last - window || end < sinks);
 }
 
-// Exponent of a scale 2^e.  A NaN scale has exponent 128: scale_value(128) is NaN.
+// Exponent of a scale 2^e.  A NaN scale has exponent 128: exp2i(128) is NaN.
 __device__ __forceinline__ int scale_exp(float s) { return (int)((__float_as_uint(s) >> 23) & 255u) - 127; }
 __device__ __forceinline__ float exp2i(int e) {   // 2^e, -126 <= e <= 127; 128: NaN
   return e > 127 ? __int_as_float(0x7fc00000) : __int_as_float((e + 127) << 23);
