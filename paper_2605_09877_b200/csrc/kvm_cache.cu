@@ -154,20 +154,26 @@ void launch_append(const AppendArgs& a, cudaStream_t s) {
   }
 }
 
-// Copies of pages: (source, destination) pairs in the launch's arguments, at most N at a time.  Block (pair, part): a run of kCopyPart
-// bytes of the pair's keys or values, all loads of a thread in flight before its first store; part 0 moves the scales too.  2000 pages of
-// 64 x 128, 8 heads: 88 us, 6.0 TB/s (91 % of the measured copy rate; 102 us with 480 pairs per launch).
+// Copies of pages: (source, destination) pairs in the launch's arguments.  Block (pair, part): a run of kCopyPart bytes of the pair's keys or
+// values, all loads of a thread in flight before its first store; part 0 moves the scales too.  How many bytes of arguments, measured with 1, 4,
+// 8, 16 and 32 KB, the last of which is all that a launch may have, in us between calls that follow one another on the GPU:
+//   48 pages of 64 x 128, 8 heads: 4.2  4.2  4.2  4.2  5.9;   400: 23.1  14.5  14.5  14.5  14.7;   2500: 172  122  113  110  106;
+//   48 pages of 16 x 64, 1 head:   4.1  4.2  4.2  3.5  5.8;   400: 16.3   4.2   4.2   3.7   6.9;   2500:  86  20.6  12.4  10.4  7.4
+// and on the host a call of 1 to 120 pairs takes 3.5 to 4.1 us with 1 KB, 4.6 to 5.0 with 16: the arguments are copied whole.  So a list that 1 KB
+// holds has a launch of its own kind, and others go 16 KB at a time.  20000 pages of 64 x 128, 8 heads: 850 us, 6.2 TB/s (94 % of the
+// measured copy rate).
 constexpr int kCopyPart = 256 * 16 * 4;
-template <int N>
+template <int BYTES>
 struct CopyArgs {
+  static constexpr int kPairs = (BYTES - 48) / 8;
   uint8_t* codes[2];
   float* scales[2];
   int64_t page_bytes;   // codes of one page, all heads
   int Hkv;
-  int32_t src[N], dst[N];
+  int32_t src[kPairs], dst[kPairs];
 };
-template <int N>
-__global__ void __launch_bounds__(256) copy_pages_kernel(const __grid_constant__ CopyArgs<N> a) {
+template <int BYTES>
+__global__ void __launch_bounds__(256) copy_pages_kernel(const __grid_constant__ CopyArgs<BYTES> a) {
   const int64_t src = a.src[blockIdx.x], dst = a.dst[blockIdx.x];
   const int which = blockIdx.z;
   const uint8_t* from = a.codes[which] + src * a.page_bytes;
@@ -206,19 +212,21 @@ bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, 
                                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int N>
+template <int BYTES>
 static void launch_copies(const kvm_cache_t* cache, const int32_t* src, const int32_t* dst, int64_t n, int64_t page_bytes, cudaStream_t s) {
-  CopyArgs<N> a;
+  using Args = CopyArgs<BYTES>;
+  static_assert(sizeof(Args) <= BYTES, "arguments of a launch");
+  Args a;
   a.codes[0] = (uint8_t*)cache->k; a.codes[1] = (uint8_t*)cache->v;
   a.scales[0] = cache->k_scale; a.scales[1] = cache->v_scale;
   a.Hkv = cache->n_kv_heads;
   a.page_bytes = page_bytes;
   const unsigned parts = (unsigned)((page_bytes + kCopyPart - 1) / kCopyPart);
-  for (int64_t at = 0; at < n; at += N) {
-    const int m = (int)std::min<int64_t>(N, n - at);
+  for (int64_t at = 0; at < n; at += Args::kPairs) {
+    const int m = (int)std::min<int64_t>(Args::kPairs, n - at);
     std::copy(src + at, src + at + m, a.src);
     std::copy(dst + at, dst + at + m, a.dst);
-    copy_pages_kernel<N><<<dim3(m, parts, 2), 256, 0, s>>>(a);
+    copy_pages_kernel<BYTES><<<dim3(m, parts, 2), 256, 0, s>>>(a);
   }
 }
 
@@ -346,9 +354,8 @@ KVM_API kvm_status_t kvm_cache_copy_pages(const kvm_cache_t* cache, const int32_
   }
   const int64_t page_bytes = (int64_t)cache->n_kv_heads * cache->page_tokens * cache->head_dim;
   if ((page_bytes + kCopyPart - 1) / kCopyPart > 65535) return KVM_ERR_UNSUPPORTED;
-  // few pairs: the arguments of a launch are copied whole, so a small list has a launch of its own kind
-  if (n <= 120) launch_copies<120>(cache, src, dst, n, page_bytes, (cudaStream_t)cuda_stream);
-  else launch_copies<2000>(cache, src, dst, n, page_bytes, (cudaStream_t)cuda_stream);
+  if (n <= CopyArgs<1024>::kPairs) launch_copies<1024>(cache, src, dst, n, page_bytes, (cudaStream_t)cuda_stream);
+  else launch_copies<16384>(cache, src, dst, n, page_bytes, (cudaStream_t)cuda_stream);
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 

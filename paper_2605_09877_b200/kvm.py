@@ -520,16 +520,19 @@ def _int(x, bits=32):
 
 def _page_list(x):
     """Page numbers on the host as contiguous int32."""
-    x = torch.as_tensor(x)
+    if not isinstance(x, torch.Tensor):
+        x = torch.as_tensor(x)
     if x.is_cuda or x.dim() != 1:
         raise ValueError("src and dst are lists of page numbers on the host")
-    if x.dtype != torch.int32 and x.numel():
+    if x.dtype == torch.int32:
+        return x.contiguous()
+    if x.numel():
         if x.dtype == torch.bool or x.is_floating_point() or x.is_complex():
             raise ValueError("page numbers are whole numbers")
         x = x.to(torch.int64)
         if x.min() < -(1 << 31) or x.max() >= 1 << 31:
             raise ValueError("page numbers are of 32 bits")
-    return x.to(torch.int32).contiguous()
+    return x.to(torch.int32)
 
 
 class Cache:

@@ -960,3 +960,23 @@ def test_calls_after_an_expired_wait(kvm):
         for T in (1, 30):
             m.attend(rows((2, 4, T, 64), 3), [T, T])
     st.free()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,d,P,n", [(1, 64, 16, 2041), (1, 64, 16, 2042), (1, 64, 16, 2043), (2, 64, 32, 9001), (1, 64, 16, 1)])
+def test_copies_of_more_pages_than_one_launch_takes(kvm, H, d, P, n):
+    N = 2 * n + 3
+    c = kvm.Cache.empty(N, H, d, P)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    parts = [c.k8.view(torch.uint8), c.v8.view(torch.uint8), c.k_scale, c.v_scale]
+    for t in parts[:2]:
+        t.copy_(torch.randint(0, 256, t.shape, generator=g, device="cuda", dtype=torch.uint8))
+    for t in parts[2:]:
+        t.copy_(torch.rand(t.shape, generator=g, device="cuda"))
+    ids = torch.randperm(N, generator=torch.Generator().manual_seed(n))
+    src, dst = ids[:n], ids[n:2 * n]
+    want = [x.clone() for x in parts]
+    for x in want:
+        x[dst.cuda()] = x[src.cuda()]
+    c.copy_pages(src, dst)
+    assert all(torch.equal(a, b) for a, b in zip(want, parts))
