@@ -895,7 +895,8 @@ __global__ void __launch_bounds__(128) prompt_combine_kernel(const __grid_consta
 
 // (row tiles of 128, key splits) of a call: the number of splits that the launch is done with first, if every row tile saw `tiles` key tiles, a CTA's
 // set-up and end took as long as five of them (measured: 8 us and 1.3 us a tile) and the merge as three.  Row tiles that see fewer take
-// fewer (prompt_work).  300 tokens behind 3000, 32 heads on 8 (80 row tiles of 26): one split 48 us, three 52.
+// fewer (prompt_work).  Lengths are on the device, so without a window `tiles` is what the page table has room for: a table wider than the sequences
+// costs splits, and a merge, that they do not ask for (300 tokens behind 3000, 32 heads on 8: 40 us, 66 with a table for 32768).
 static void prompt_plan(int64_t units, int64_t rows, int64_t tiles, int& qtiles, int& nsplit) {
   qtiles = (int)((rows + kRows - 1) / kRows);
   const int64_t ctas = units * qtiles;
@@ -939,7 +940,15 @@ kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool
   PromptArgs args;
   args.a = a;
   args.units = a.p.batch * a.p.Hkv;
-  prompt_plan(args.units, a.p.T * a.G, tiles, args.qtiles, args.nsplit);
+  // Key tiles that 128 rows see: of a window layer far fewer than its table has, whose entries behind the window are only numbers.  Planned by the
+  // table's width and by what is seen, behind 30000 tokens, 32 heads on 8: 300 tokens with a window of 128 22 and 18 us, 512 28 and 21, 2048 52 and 34,
+  // 4096 72 and 54; 20 tokens 23 and 18, 23 and 20, 22 and 23, 25 and 23.  (Never more splits than the workspace is for, which is counted
+  // without the window.)
+  const int64_t seen = std::min<int64_t>(tiles, ((int64_t)a.window + a.sinks + 128 / a.G) / kTile + 2);
+  int most;
+  prompt_plan(args.units, a.p.T * a.G, tiles, args.qtiles, most);
+  prompt_plan(args.units, a.p.T * a.G, seen, args.qtiles, args.nsplit);
+  args.nsplit = std::min(args.nsplit, most);
   args.by_units = FastDiv(args.units); args.by_heads = FastDiv(a.p.Hkv); args.by_group = FastDiv(a.G);
   args.q_vec = q_vec ? 1 : 0; args.out_vec = out_vec ? 1 : 0;
   CUtensorMap mapK, mapV;
@@ -949,7 +958,6 @@ kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool
   // d = 128, without and with: window 128 193 -> 177 us, 512 239 -> 224, 2048 387 -> 384, 4096 524 -> 534, all 622 -> 641; d = 64 on 4 heads:
   // 144 -> 128, 192 -> 179, 326 -> 317, 453 -> 451, 548 -> 554).  Not where a merge waits for the grid.
   constexpr int kMoreTiles = 18;
-  const int64_t seen = std::min<int64_t>(tiles, ((int64_t)a.window + a.sinks + 128 / a.G) / kTile + 2);
   const bool more = args.nsplit == 1 && seen <= kMoreTiles && (int64_t)args.units * args.qtiles > 148;
   if (a.d == 128) return more ? launch_prompt_d<128, true>(args, mapK, mapV, s) : launch_prompt_d<128, false>(args, mapK, mapV, s);
   return more ? launch_prompt_d<64, true>(args, mapK, mapV, s) : launch_prompt_d<64, false>(args, mapK, mapV, s);

@@ -980,3 +980,30 @@ def test_copies_of_more_pages_than_one_launch_takes(kvm, H, d, P, n):
         x[dst.cuda()] = x[src.cuda()]
     c.copy_pages(src, dst)
     assert all(torch.equal(a, b) for a, b in zip(want, parts))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hkv,d,P,ctx,T,window,sinks,split", [
+    (32, 8, 128, 64, 9000, 300, 512, 4, False), (16, 4, 64, 16, 9000, 300, 200, 0, False), (4, 2, 128, 32, 9000, 60, 6000, 3, True), (4, 2, 128, 32, 9000, 60, 0, 0, True)])
+def test_a_window_is_planned_as_the_tiles_it_sees(kvm, Hq, Hkv, d, P, ctx, T, window, sinks, split):
+    """Behind a long context a window layer's table is as wide as a full one's, with -1 for the pages given back; key tiles that no row sees are no
+    reason for key splits, their partial results in the workspace, and a merge."""
+    lengths = [ctx + T]
+    m = Model(kvm, 1, Hkv, d, P, -(-lengths[0] // P))
+    m.append(rows((1, Hkv, ctx + T, d), 1), rows((1, Hkv, ctx + T, d), 2), lengths)
+    q = rows((1, Hq, T, d), 3)
+    table = m.table.clone()
+    if window:
+        gone = [i for i in range(table.shape[1]) if (i + 1) * P <= ctx - window + 1 and i * P >= sinks]
+        table[0, gone] = -1
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    start = torch.tensor([ctx], dtype=torch.int32).cuda()
+    call = kvm.CacheCall(table.data_ptr(), start.data_ptr(), None, 1, table.shape[1], T)
+    n = kvm.lib.kvm_cache_workspace(m.cache._ref, C.byref(call), Hq)
+    ws = torch.full((max(n, 16),), 0xAB, dtype=torch.uint8, device="cuda")
+    qd = q.cuda()
+    assert kvm.lib.kvm_cache_attend(m.cache._ref, C.byref(call), qd.data_ptr(), Hq, d ** -0.5, window, sinks, out.data_ptr(), None, None, ws.data_ptr(), n, None,
+                                    torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    m.compare(q, out, [T], window, sinks)
+    assert (ws != 0xAB).any().item() == split
