@@ -186,3 +186,36 @@ def test_borders_of_what_a_token_sees(kvm, n, T, G, d, P, window, sinks):  # noq
     k, v = marked_rows(n, d, marks(n, T, window, sinks))
     m.append(k, v, [n])
     m.attend(marked_query(G, T, d, n), [T], window, sinks, scale=1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,P", [(1, 128, 64), (3, 64, 16), (300, 128, 128), (300, 64, 16)])
+def test_positions_up_to_the_largest(kvm, T, d, P):  # noqa: F811
+    """A stream that a window layer has followed to the last position that a call may name: the same bits as the same rows near the front."""
+    B, Hq, Hkv, W, S = 1, 8, 2, 500, 5
+    width = (1 << 30) // P                             # the widest table
+    near = 40 * P
+    far = near + ((1 << 30) - T - near) // P * P        # the same place within a page
+    blocks = (W + T) // P + 3
+    g = torch.Generator().manual_seed(T)
+    k, v, q = (torch.randn((B, h, n, d), generator=g).to(torch.bfloat16).cuda() for h, n in ((Hkv, W + T), (Hkv, W + T), (Hq, T)))
+    out = []
+    for at in (near, far):
+        assert at % P == near % P and at + T <= 1 << 30
+        cache = kvm.Cache.empty(blocks + 2, Hkv, d, P)
+        table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+        first = (at - W) // P
+        used = -(-(at + T) // P) - first
+        table[0, first:first + used] = torch.arange(1, used + 1, dtype=torch.int32, device="cuda")
+        table[0, 0] = 0
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        place = lambda x: torch.tensor([x], dtype=torch.int32).cuda()  # noqa: E731
+        cache.append(k[:, :, :S], v[:, :, :S], table, place(0), status=status)
+        cache.append(k, v, table, place(at - W), status=status)
+        out.append(cache.attend(q, table, place(at), window=W, sinks=S, status=status))
+        assert status.item() == 0
+    assert torch.isfinite(out[0].float()).all() and out[0].float().abs().max() > 0.05 and torch.equal(*out)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    still = torch.full_like(q, 7.0)
+    cache.attend(q, table, torch.tensor([(1 << 30) - T + 1], dtype=torch.int32).cuda(), window=W, sinks=S, out=still, status=status)
+    assert status.item() == 1 and (still == 7.0).all()
