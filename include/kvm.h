@@ -420,9 +420,15 @@ kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* 
  *            (in the order of the strides, each dimension has to step over what the smaller ones span, else INVALID_ARG)
  *   workspace device memory, 16-byte aligned, at least kvm_cache_workspace() bytes, whatever it holds; calls that may overlap
  *            on the GPU need one each
- * Products of bf16 and e4m3, logits and softmax statistics are held in fp32 (a query with a logit beyond its range may give NaN).  Where the blocks of values that are looked at together (a tile of 128
- * keys; for many tokens, what 128 rows of queries see) lie more than 2^90 apart, the smallest count in the row sum only.  A query that sees a page outside the pool gets NaN rows, as does
- * one whose q, or whose visible blocks, hold an infinity or a NaN; a sequence whose lengths are not allowed gets none.
+ * Sums of products, logits, softmax statistics and row sums are held in fp32 (a query with a logit beyond its range may give NaN).  What goes
+ * into the products in fewer bits: q as two e4m3 numbers, all of it but what lies below 2^-18 of the row's largest channel; the weights, for
+ * at most 16 (token, head of a group) pairs per sequence, as two e4m3 numbers, 2^-8 of a weight and 2^-18 of the largest one of 128 keys (the
+ * row sum takes them as they are rounded), beyond that in fp16, 2^-11 of a weight and 2^-31 of the row's largest so far (the row sum takes them
+ * in fp32).  Where the blocks of values that are looked at together (a tile of 128 keys; for many tokens, what 128 rows of queries see) lie more
+ * than 2^90 apart, the smallest count in the row sum only.
+ * A query that sees a page outside the pool gets NaN rows, as does one whose q, or whose visible blocks (by their scale, as kvm_cache_append leaves
+ * it), hold an infinity or a NaN; a sequence whose lengths are not allowed gets none.  Codes of NaN under a finite scale, which append never
+ * writes, may reach tokens that do not see them.
  * Results are deterministic.  Waits on the device are bounded: should one run out, *status is KVM_ERR_TIMEOUT.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (workspace too small), CUDA; nothing is launched on an error. */
 kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale,

@@ -23,7 +23,7 @@
 // merged by combine_kernel from their partial results.  The code is kept small: at 197 KB it ran from the instruction cache's misses (317 us).
 //
 // Bound by HBM (2 d bytes per key and kv head), a tile every 1280 cycles and SM once it runs, 8 us after its start.  Measured, d = 128: 64 sequences
-// of up to 16384 tokens, 32 heads on 8: 205 us, 5.3 TB/s (81 % of the measured copy rate); one of 131072, 8 heads: 57 us, 4.7 TB/s; 64
+// of up to 16384 tokens, 32 heads on 8: 193 to 210 us, 5.2 to 5.7 TB/s (80 to 86 % of the measured copy rate); one of 131072, 8 heads: 57 us, 4.7 TB/s; 64
 // with a window of 512, 32 heads: 77 us, 3.4 TB/s (640 keys are read where 516 are seen); one of 1000: 14 us, two launches.
 #include <algorithm>
 #include <atomic>

@@ -27,8 +27,9 @@
 //
 // Bound by the softmax warps and the conversion: 1600 instructions per scheduler and tile (128 x 128) against 1024 cycles of the tensor core, 2300
 // cycles a tile; and by the set-up, filling and emptying per block of 128 rows (8 us, 7 where a CTA goes on), most of what short windows
-// cost.  Measured: two prompts of 8192 tokens, 16 heads, d = 128: 625 us, 880 TFLOP/s (54 % of the measured burst rate; 699 us under the power
-// cap, 58 % of the sustained one); three of 4915 to 8192, 16 heads on 4, d = 64, window 512: 169 us; 300 tokens behind 3000, 32 heads on 8: 42 us.
+// cost.  Measured: two prompts of 8192 tokens, 16 heads, d = 128: 673 to 698 us in long runs, under the power cap, 790 to 820 TFLOP/s (58 to 60 % of the
+// measured sustained rate, 49 % of the burst rate), 625 us in a short one; three of 3994, 7032 and 5154, 16 heads on 4, d = 64, window 512: 164 us;
+// 300 tokens behind 3000, 32 heads on 8: 42 us.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -894,7 +895,7 @@ __global__ void __launch_bounds__(128) prompt_combine_kernel(const __grid_consta
 }
 
 // (row tiles of 128, key splits) of a call: the number of splits that the launch is done with first, if every row tile saw `tiles` key tiles, a CTA's
-// set-up and end took as long as five of them (measured: 8 us and 1.3 us a tile) and the merge as three.  Row tiles that see fewer take
+// set-up and end took as long as five of them (8 us and 1.3 us a tile, when the rule was made) and the merge as three.  Row tiles that see fewer take
 // fewer (prompt_work).  Lengths are on the device, so without a window `tiles` is what the page table has room for: a table wider than the sequences
 // costs splits, and a merge, that they do not ask for (300 tokens behind 3000, 32 heads on 8: 40 us, 66 with a table for 32768).
 static void prompt_plan(int64_t units, int64_t rows, int64_t tiles, int& qtiles, int& nsplit) {

@@ -30,8 +30,8 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
       : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
   return ok != 0;
 }
-// Bounded wait: every spin has an iteration limit (by default about a second); on expiry the caller
-// sets the error word, leaves its loops, and the CTA tears down normally.
+// Bounded wait: every spin has an iteration limit; on expiry the caller sets the error word, leaves its loops, and the CTA tears down
+// normally.  A try on a barrier that nothing arrives at takes 4 us (the hardware suspends the thread for that long): 17 s by default.
 constexpr uint32_t kSpinLimit = 1u << 22;
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32_t limit = kSpinLimit) {
   for (uint32_t it = 0; it < limit; ++it) {

@@ -542,7 +542,8 @@ class Cache:
 
     pages int32 [B, max_pages], start int32 [B] (tokens in the cache before the call) and count int32 [B] (tokens of the call; None: all of
     them) are CUDA tensors.  `status`: optional int32 CUDA tensor of one element that receives KVM_ERR_INVALID_ARG where the kernels
-    meet lengths or pages that the call does not allow, KVM_ERR_TIMEOUT should a bounded device-side wait run out."""
+    meet lengths or pages that the call does not allow, KVM_ERR_TIMEOUT should a bounded device-side wait run out.  Arguments that the
+    binding can see to be wrong, numbers beyond 32 bits among them, raise ValueError."""
 
     def __init__(self, k8, v8, k_scale, v_scale):
         if k8.dim() != 4 or v8.shape != k8.shape or k_scale.shape != k8.shape[:2] or v_scale.shape != k8.shape[:2]:
