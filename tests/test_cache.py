@@ -1007,3 +1007,24 @@ def test_a_window_is_planned_as_the_tiles_it_sees(kvm, Hq, Hkv, d, P, ctx, T, wi
     torch.cuda.synchronize()
     m.compare(q, out, [T], window, sinks)
     assert (ws != 0xAB).any().item() == split
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,P,far", [(128, 64, 0), (128, 64, 20), (64, 16, 20), (128, 128, 100)])
+def test_a_long_flat_tail_counts_over_values_of_any_scale(kvm, d, P, far):
+    """As above, with one block of values 2^far below the others (from 2^14 on the scales go through the weights' exponents)."""
+    n, T, G, below = 1 << 19, 80, 512, 25.0
+    c = kvm.Cache.empty(n // P, 1, d, P)
+    c.v8.view(torch.uint8).fill_(0x38)                 # 1.0
+    c.k8.view(torch.uint8)[0, 0, 0, 0] = 0x38
+    c.v8.view(torch.uint8)[0, 0, 0] = 0
+    c.v_scale[7] = 2.0 ** -far
+    q = torch.zeros((1, G, T, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    table = torch.arange(n // P, dtype=torch.int32, device="cuda")[None]
+    out = c.attend(q, table, torch.tensor([n - T], dtype=torch.int32).cuda(), scale=below * math.log(2.0)).double().cpu()
+    keys, w = torch.arange(n - T, n).double(), math.exp(-float(np.float32(below * math.log(2.0))))
+    ref = ((keys - P * (1 - 2.0 ** -far)) * w / (1 + keys * w))[None, None, :, None]
+    bound = (2.0 ** -7 + 2.0 ** -20) * ref + 2.0 ** -11
+    err = (out - ref).abs()
+    assert (err <= bound).all(), (float(ref.mean()), float(out.mean()), float(out.min()))
