@@ -372,6 +372,55 @@ kvm_status_t kvm_merge_gate(const void* x, const float* w_gate, int32_t batch, i
 kvm_status_t kvm_head_layernorm(void* x, const float* weight, const float* bias, int32_t batch, int32_t n_heads,
                                 int64_t n_tokens, int32_t head_dim, float eps, void* cuda_stream);
 
+/* ---- Front end of an exact layer: norm of every head's row and rotary positions ------------------------------------
+ * For the uncompressed layers of a hybrid stack, whose attention (kvm_cache_attend below) takes q and k as they are.  A row x of head_dim
+ * channels becomes
+ *     KVM_NORM_LAYER  (x - mean) / sqrt(var + eps) * weight + bias      (biased variance)
+ *     KVM_NORM_RMS    x / sqrt(mean(x^2) + eps) * weight + bias
+ *     KVM_NORM_NONE   x
+ * and then its first rope_dims = r channels are rotated by the position t, in pairs (a, b) -> magnitude * (a cos u - b sin u, b cos u + a sin u),
+ * u = t * f_i, i = 0 .. r/2 - 1:
+ *     KVM_ROPE_HALF         pairs (i, i + r/2)          KVM_ROPE_INTERLEAVED  pairs (2i, 2i + 1)
+ *     KVM_ROPE_PLAIN        f_i = w_i = base^(-2i/r)
+ *     KVM_ROPE_LINEAR       f_i = w_i / factor          (positions interpolated)
+ *     KVM_ROPE_PARTS        f_i = g w_i + (1 - g) w_i / factor,  g = clamp((n_i - low) / (high - low), 0, 1),  n_i = original_len * w_i / (2 pi):
+ *                           pairs that turn more than `high` times within the length that the model was made for keep their frequency,
+ *                           those that turn less than `low` times are interpolated (arXiv 2309.00071, section 3.2)
+ * Statistics, rotation and sums in fp32 (the mean taken off before the squares), angles in fp64, one rounding at the end.  Values up to
+ * 2^60 in magnitude: beyond, the sums of squares of a norm may leave fp32's range. */
+typedef enum { KVM_NORM_NONE = 0, KVM_NORM_LAYER = 1, KVM_NORM_RMS = 2 } kvm_norm_kind_t;
+typedef enum { KVM_ROPE_HALF = 0, KVM_ROPE_INTERLEAVED = 1 } kvm_rope_layout_t;
+typedef enum { KVM_ROPE_PLAIN = 0, KVM_ROPE_LINEAR = 1, KVM_ROPE_PARTS = 2 } kvm_rope_scaling_t;
+typedef struct {
+  int32_t norm, layout, scaling;           /* the kinds above */
+  int32_t rope_dims;                       /* r: even, 0 .. head_dim; 0: no rotation (what follows is not looked at) */
+  double base, factor, low, high;          /* base >= 1; factor >= 1 (LINEAR, PARTS); 0 <= low < high (PARTS) */
+  double magnitude;                        /* of cos and sin; 1 unless a long context asks for another */
+  int64_t original_len;                    /* PARTS: tokens, >= 1 */
+  float eps;                               /* >= 0, with a norm */
+  const float *q_weight, *q_bias;          /* device fp32 [n_q_heads, head_dim] or NULL (1, 0); NULL without a norm */
+  const float *k_weight, *k_bias;          /* device fp32 [n_kv_heads, head_dim] */
+} kvm_front_t;
+
+/* f_i in radians per position, i < rope_dims / 2, into a HOST array (host arithmetic). */
+kvm_status_t kvm_rope_frequencies(const kvm_front_t* front, int32_t head_dim, double* out);
+
+/* q and k of a call through the front end, in one launch.
+ *   q, q_out  device bf16 [batch, n_q_heads, n_tokens, head_dim], k, k_out with n_kv_heads; element strides of the first three dims (NULL =
+ *             contiguous), channel stride 1.  q or k may be NULL (its number of heads is not looked at).  An out may be its input (same pointer
+ *             and strides: in place); else it must not overlap it, nor rows of an out one another
+ *   start     device int32 [batch] or NULL (0): position of each sequence's first token
+ *   count     device int32 [batch] or NULL (n_tokens): tokens of each sequence; rows of the outs behind them are left as they were, rows of q and k
+ *             there may be read, but nothing comes of them
+ *   status    device int32 word or NULL: KVM_ERR_INVALID_ARG where start < 0, count < 0 or count > n_tokens (no row of that
+ *             sequence is written); never cleared by the library
+ * head_dim 64 or 128, batch <= 65535, heads <= 16384, n_tokens <= 2^30, else UNSUPPORTED.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
+kvm_status_t kvm_qk_norm_rope(const kvm_front_t* front, const void* q, const void* k, const int32_t* start, const int32_t* count, int32_t batch,
+                              int32_t n_q_heads, int32_t n_kv_heads, int64_t n_tokens, int32_t head_dim, void* q_out, void* k_out,
+                              const int64_t* q_strides, const int64_t* k_strides, const int64_t* q_out_strides,
+                              const int64_t* k_out_strides, int32_t* status, void* cuda_stream);
+
 /* ---- Exact attention beside the compressed one: a cache of keys and values in 8 bits ------------------------------
  * The uncompressed layers of a hybrid stack (sliding-window or full attention between KVM layers) keep their keys and
  * values in pages of `page_tokens` tokens ("blocks").  A page holds, for every kv head, the codes of its rows in e4m3
@@ -410,6 +459,23 @@ typedef struct {
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
 kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* k, const void* v,
                               const int64_t* k_strides, const int64_t* v_strides, int32_t* status, void* cuda_stream);
+
+/* kvm_qk_norm_rope and kvm_cache_append in one launch: q (with the positions start[b] ..) to q_out, k through the same front end into the cache,
+ * v into the cache.  The codes of k are those of the normalised and rotated row in fp32, rounded once (not by way of bf16); a row that leaves fp32's
+ * range there counts as infinite.  q may be NULL: k and v only.  Rows of q_out behind a sequence's count, and of a sequence that is reported, are
+ * left as they were; rows of q, k and v behind the count may be read, but nothing comes of them.  q_out may be q (same strides), and must not overlap
+ * k or v.  What kvm_cache_append says of pages, scales, distinct pages and infinities holds here.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
+kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_call_t* call, const kvm_front_t* front, const void* q, int32_t n_q_heads,
+                              const void* k, const void* v, void* q_out, const int64_t* q_strides, const int64_t* k_strides,
+                              const int64_t* v_strides, const int64_t* q_out_strides, int32_t* status, void* cuda_stream);
+
+/* Rows back out of the cache: positions start[b] .. start[b] + count[b] - 1 of every sequence as bf16, code * scale (exact; what would be 2^128 is
+ * bf16's largest value), k_out, v_out device bf16 [batch, n_kv_heads, n_tokens, head_dim], strides as in kvm_cache_attend's out.  Rows behind a
+ * sequence's count are left as they were.  Rows of a block whose scale is NaN, or whose page lies outside the pool (which is reported), are NaN.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
+kvm_status_t kvm_cache_read(const kvm_cache_t* cache, const kvm_cache_call_t* call, void* k_out, void* v_out, const int64_t* k_strides,
+                            const int64_t* v_strides, int32_t* status, void* cuda_stream);
 
 /* Attention of the call's tokens over the cache, which holds their own keys and values already:
  *     out_i = sum_j p_ij v_j,  p_i = softmax over the visible j of scale * q_i . k_j,

@@ -20,8 +20,6 @@
 namespace kvm {
 namespace cache {
 
-constexpr int kLeastExp = -64;
-
 struct AppendArgs {
   Params p;
   uint8_t* codes[2];
@@ -190,6 +188,82 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(const __grid_constant__
     for (int h = threadIdx.x; h < a.Hkv; h += 256) a.scales[which][dst * a.Hkv + h] = a.scales[which][src * a.Hkv + h];
 }
 
+// Rows back out of the cache: code * scale in bf16, which holds it exactly (4 significant bits, exponents -73 to 128; 2^128, which stands for a value
+// that was rounded up from bf16's largest, becomes that one again).  16 codes per thread and row, four rows in flight: one chain of loads (lengths,
+// page, then codes and scale) per block of 128 tokens (256 with 64 channels).
+struct ReadArgs {
+  Params p;
+  __nv_bfloat16* y[2];
+  int64_t st[2][3];
+  int vec;   // rows are 16-byte aligned
+};
+template <int D>
+__global__ void __launch_bounds__(256) read_kernel(const ReadArgs a) {
+  constexpr int LPR = D / 16, RP = 256 / LPR, CH = 4;
+  const Params& p = a.p;
+  const int which = blockIdx.y & 1, hk = blockIdx.y >> 1, b = blockIdx.z, lane = threadIdx.x % LPR;
+  int start, n;
+  if (!seq_lengths(p, b, start, n)) {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
+    return;
+  }
+  const int64_t t0 = (int64_t)blockIdx.x * (RP * CH) + threadIdx.x / LPR;
+  uint4 w[CH];
+  float scale[CH];
+  int page[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int64_t t = t0 + i * RP;
+    page[i] = t < n ? p.pages[(int64_t)b * p.max_pages + ((start + t) >> p.page_shift)] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int64_t t = t0 + i * RP;
+    w[i] = make_uint4(0, 0, 0, 0);
+    scale[i] = __int_as_float(0x7fc00000);
+    if (t >= n) continue;
+    if (page[i] < 0 || page[i] >= p.n_pages) {
+      report(p.status, KVM_ERR_INVALID_ARG);
+    } else {
+      const int64_t unit = (int64_t)page[i] * p.Hkv + hk;
+      w[i] = __ldcs(reinterpret_cast<const uint4*>((which ? p.v : p.k) + (unit * p.page + ((start + t) & (p.page - 1))) * D) + lane);
+      scale[i] = (which ? p.vs : p.ks)[unit];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int64_t t = t0 + i * RP;
+    if (t >= n) continue;
+    const uint32_t c[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+    __nv_bfloat162 o[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float2 x = e4m3x2_to_float2((c[q >> 1] >> (16 * (q & 1))) & 0xffffu);
+      x.x *= scale[i];
+      x.y *= scale[i];
+      if (scale[i] >= 1.3e36f) {   // (2^120)
+        const float most = __int_as_float(0x7f7f0000);
+        if (fabsf(x.x) > most) x.x = copysignf(most, x.x);
+        if (fabsf(x.y) > most) x.y = copysignf(most, x.y);
+      }
+      o[q] = __floats2bfloat162_rn(x.x, x.y);
+    }
+    __nv_bfloat16* dst = a.y[which] + b * a.st[which][0] + hk * a.st[which][1] + t * a.st[which][2] + lane * 16;
+    if (a.vec) {
+      __stcs(reinterpret_cast<uint4*>(dst), *reinterpret_cast<const uint4*>(&o[0]));
+      __stcs(reinterpret_cast<uint4*>(dst) + 1, *reinterpret_cast<const uint4*>(&o[4]));
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) { dst[2 * q] = o[q].x; dst[2 * q + 1] = o[q].y; }
+    }
+  }
+}
+template <int D>
+static void launch_read(const ReadArgs& a, cudaStream_t s) {
+  constexpr int TOK = 256 / (D / 16) * 4;
+  read_kernel<D><<<dim3((unsigned)((a.p.T + TOK - 1) / TOK), 2 * a.p.Hkv, a.p.batch), 256, 0, s>>>(a);
+}
+
 // Codes as rows of d bytes, a box of one page of one head; rows land swizzled as the tensor core reads them (128 or 64 bytes).
 bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page) {
   typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -322,6 +396,23 @@ KVM_API kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_
   a.vec = rows_aligned(k, a.st[0]) && rows_aligned(v, a.st[1]) ? 1 : 0;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   if (cache->head_dim == 128) launch_append<128>(a, s); else launch_append<64>(a, s);
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+
+KVM_API kvm_status_t kvm_cache_read(const kvm_cache_t* cache, const kvm_cache_call_t* call, void* k_out, void* v_out, const int64_t* k_strides,
+                                    const int64_t* v_strides, int32_t* status, void* cuda_stream) {
+  kvm_status_t rc = check_cache(cache, true);
+  if (rc == KVM_OK) rc = check_call(cache, call, true);
+  if (rc != KVM_OK) return rc;
+  if (!k_out || !v_out || !aligned(k_out, 2) || !aligned(v_out, 2) || !aligned(status, 4)) return KVM_ERR_INVALID_ARG;
+  ReadArgs a;
+  a.p = params_of(cache, call, status);
+  a.y[0] = (__nv_bfloat16*)k_out; a.y[1] = (__nv_bfloat16*)v_out;
+  if (!strides_of(k_strides, a.p.batch, a.p.Hkv, a.p.T, cache->head_dim, true, a.st[0]) ||
+      !strides_of(v_strides, a.p.batch, a.p.Hkv, a.p.T, cache->head_dim, true, a.st[1])) return KVM_ERR_INVALID_ARG;
+  a.vec = rows_aligned(k_out, a.st[0]) && rows_aligned(v_out, a.st[1]) ? 1 : 0;
+  cudaStream_t s = (cudaStream_t)cuda_stream;
+  if (cache->head_dim == 128) launch_read<128>(a, s); else launch_read<64>(a, s);
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 

@@ -13,6 +13,7 @@ namespace cache {
 
 constexpr int kMaxBatch = 1024;   // sequences of one call
 constexpr int kTile = 128;        // keys of one tile of the attention kernels
+constexpr int kLeastExp = -64;    // least exponent of a scale
 
 struct Params {
   const uint8_t *k, *v;
@@ -118,6 +119,21 @@ int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols);
 // more than that; rows: tokens times heads of a group
 kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s);
 int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d);
+
+// Codes and scales that a call writes: keys, values.
+struct AppendOut {
+  uint8_t* codes[2];
+  float* scales[2];
+};
+
+// Checks of arguments (kvm_cache.cu).  check_*: pointers too, or sizes only.
+bool aligned(const void* p, uintptr_t n);
+kvm_status_t check_cache(const kvm_cache_t* c, bool pointers);
+kvm_status_t check_call(const kvm_cache_t* c, const kvm_cache_call_t* call, bool pointers);
+Params params_of(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t* status);
+// Strides of [batch, heads, tokens, d] (NULL: contiguous); false: negative ones, or rows that are written and lie on one another.
+bool strides_of(const int64_t* st, int64_t B, int64_t H, int64_t T, int d, bool written, int64_t (&out)[3]);
+bool rows_aligned(const void* p, const int64_t (&st)[3]);
 
 }  // namespace cache
 }  // namespace kvm

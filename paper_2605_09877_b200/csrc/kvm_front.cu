@@ -1,0 +1,594 @@
+// Front end of an exact layer: norm of every head's queries and keys and rotary positions in one pass (kvm_qk_norm_rope), and the same on the
+// way into the 8-bit cache (kvm_cache_ingest), where the keys are normalised, rotated and quantised as they are written.
+#include <algorithm>
+#include <cmath>
+
+#include "kvm_cache.cuh"
+#include "kvm_front.cuh"
+
+namespace kvm {
+namespace front {
+
+using cache::AppendOut;
+
+constexpr int kFourths = 4;   // rows of a lane (tokens) in the kernels for many tokens
+
+struct QkArgs {
+  FrontDev f;
+  Rows r[2];            // q, k
+  const int32_t *start, *count;
+  int32_t* status;
+  int64_t T;
+  int batch, chunks[2], heads;   // head chunks of q and k, heads of a chunk
+};
+
+// Tokens before the call and in it; false: lengths that the call does not allow.
+__device__ __forceinline__ bool qk_lengths(const QkArgs& a, int b, int& start, int& n) {
+  start = a.start ? a.start[b] : 0;
+  n = a.count ? a.count[b] : (int)a.T;
+  return start >= 0 && n >= 0 && n <= a.T;
+}
+
+// One row: (b, t, head) of q or k.
+template <int D>
+__device__ __forceinline__ void row_through(const FrontDev& f, const Rows& r, const Lane<D>& L, const Raw& raw, int head, bool live, const float (&c)[4], const float (&s)[4],
+                                            const float (&wx)[4], const float (&wy)[4], const float (&bx)[4], const float (&by)[4], __nv_bfloat16* dst) {
+  float x[4], y[4];
+  to_pairs(raw, r.vx ? L.side : true, x, y);
+  norm<D>(f, wx, wy, bx, by, x, y);
+  rotate<D>(L, c, s, x, y);
+  if (live) store_row<D>(dst, L, r.vy, L.side, x, y);
+}
+
+// Few rows: D / 8 lanes per row, every row by itself.
+template <int D>
+__global__ void __launch_bounds__(128) qk_rows_kernel(const __grid_constant__ QkArgs a) {
+  constexpr int LPR = D / 8;
+  const int lane = threadIdx.x % LPR;
+  const Lane<D> L(a.f.half, a.f.h, lane);
+  const int H = a.r[0].H + a.r[1].H;
+  const int64_t row = (int64_t)blockIdx.x * (128 / LPR) + threadIdx.x / LPR, rows = a.batch * a.T * H;
+  const bool there = row < rows;
+  int64_t rest = there ? row : 0;
+  const int hh = (int)(rest % H);
+  rest /= H;
+  const int b = (int)(rest / a.T), t = (int)(rest - b * a.T);
+  const int which = hh >= a.r[0].H, head = hh - (which ? a.r[0].H : 0);
+  const Rows& r = a.r[which];
+  // (a row that the lengths leave out is read all the same: it is there)
+  const Raw raw = load_raw<D>(r.x + b * r.sx[0] + head * r.sx[1] + t * r.sx[2], L, r.vx);
+  int start, n;
+  const bool valid = qk_lengths(a, b, start, n);
+  if (!valid && there && hh == 0 && t == 0 && lane == 0) cache::report(a.status, KVM_ERR_INVALID_ARG);
+  float wx[4], wy[4], bx[4], by[4], c[4], s[4];
+  const bool side = r.vw ? L.side : true;
+  load_affine<D>(r.w, head, L, r.vw, side, 1.f, wx, wy);
+  load_affine<D>(r.b, head, L, r.vw, side, 0.f, bx, by);
+  angles<D>(a.f, L, (int64_t)start + t, c, s);
+  row_through<D>(a.f, r, L, raw, head, there && valid && t < n, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2]);
+}
+
+// Many rows: a block takes 256 / LPR * 4 tokens (of the whole batch, one behind the other) through a run of heads.  A lane has four tokens: their
+// angles stay in registers over the heads, a head's weights over the tokens, and four rows are on their way at a time.
+template <int D, int TH, class A>
+__device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t token0, int h0, int h1) {
+  constexpr int LPR = D / 8, RP = TH / LPR, CH = kFourths;
+  const FrontDev& f = a.f;
+  const Lane<D> L(f.half, f.h, threadIdx.x % LPR);
+  const __nv_bfloat16* px[CH];
+  __nv_bfloat16* py[CH];
+  float c[CH][4], s[CH][4];
+  uint32_t live = 0;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int64_t token = token0 + threadIdx.x / LPR + i * RP;
+    int64_t b = token / a.tokens(), t = token - b * a.tokens();
+    int start = 0, n = 0;
+    if (b >= a.sequences()) b = t = 0;
+    else if (!a.lengths((int)b, start, n)) {
+      if (t == 0 && h0 == 0 && L.i0 == 0) cache::report(a.status_word(), KVM_ERR_INVALID_ARG);
+      start = n = 0;
+    }
+    if (t < n) live |= 1u << i;
+    px[i] = r.x + b * r.sx[0] + t * r.sx[2];
+    py[i] = r.y + b * r.sy[0] + t * r.sy[2];
+    angles<D>(f, L, start + t, c[i], s[i]);
+  }
+  Raw raw[CH];
+  auto fetch = [&](int h) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) raw[i] = load_raw<D>(px[i] + h * r.sx[1], L, r.vx);
+  };
+  fetch(h0);
+  const bool side = r.vw ? L.side : true;
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    float wx[4], wy[4], bx[4], by[4];
+    load_affine<D>(r.w, h, L, r.vw, side, 1.f, wx, wy);
+    load_affine<D>(r.b, h, L, r.vw, side, 0.f, bx, by);
+    Raw now[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) now[i] = raw[i];
+    if (h + 1 < h1) fetch(h + 1);
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      row_through<D>(f, r, L, now[i], h, live >> i & 1, c[i], s[i], wx, wy, bx, by, py[i] + h * r.sy[1]);
+  }
+}
+
+struct QkTile {   // what rows_tile asks of a call without a cache
+  const QkArgs& a;
+  const FrontDev& f;
+  __device__ int64_t tokens() const { return a.T; }
+  __device__ int sequences() const { return a.batch; }
+  __device__ bool lengths(int b, int& start, int& n) const { return qk_lengths(a, b, start, n); }
+  __device__ int32_t* status_word() const { return a.status; }
+};
+template <int D>
+__global__ void __launch_bounds__(256, 2) qk_tile_kernel(const __grid_constant__ QkArgs a) {
+  const int which = (int)blockIdx.y >= a.chunks[0], chunk = blockIdx.y - (which ? a.chunks[0] : 0);
+  const int h0 = chunk * a.heads;
+  rows_tile<D, 256>(QkTile{a, a.f}, a.r[which], (int64_t)blockIdx.x * (256 / (D / 8) * kFourths), h0, min(h0 + a.heads, a.r[which].H));
+}
+
+// ---- into the cache ----------------------------------------------------------------------------------------------------------
+
+struct IngestArgs {
+  FrontDev f;
+  cache::Params p;
+  Rows q, k, v;         // (k.y, v.y and their strides are not used)
+  AppendOut o;
+  int chunks_q, heads_q, chunks, heads;       // head chunks of q; of k and v
+  int groups;           // blocks that share the pages of one sequence
+  int64_t kv_blocks;    // blocks of k, and as many of v; those of q follow
+};
+struct IngestTile {
+  const IngestArgs& a;
+  const FrontDev& f;
+  __device__ int64_t tokens() const { return a.p.T; }
+  __device__ int sequences() const { return a.p.batch; }
+  __device__ bool lengths(int b, int& start, int& n) const { return cache::seq_lengths(a.p, b, start, n); }
+  __device__ int32_t* status_word() const { return nullptr; }   // (the blocks of k report)
+};
+
+// Least e >= -64 with x <= 448 * 2^e, from the bits of x >= 0.
+__device__ __forceinline__ int least_exp(uint32_t bits) {
+  return max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), cache::kLeastExp);
+}
+// A lane's eight values as codes, in the order of memory (two runs of four channels) where the layout has runs.
+__device__ __forceinline__ void codes_of(const float (&v)[8], float inv, uint32_t& a, uint32_t& b) {
+  a = cache::to_e4m3x2(v[0] * inv, v[1] * inv) | (cache::to_e4m3x2(v[2] * inv, v[3] * inv) << 16);
+  b = cache::to_e4m3x2(v[4] * inv, v[5] * inv) | (cache::to_e4m3x2(v[6] * inv, v[7] * inv) << 16);
+}
+template <int D>
+__device__ __forceinline__ void store_codes(uint8_t* row, const Lane<D>& L, bool runs, uint32_t a, uint32_t b) {
+  if (runs) {
+    *reinterpret_cast<uint32_t*>(row + L.c0) = a;
+    *reinterpret_cast<uint32_t*>(row + L.c1) = b;
+  } else {   // (x0 y0 x1 y1 ...)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = (j < 2 ? a : b) >> (16 * (j & 1));
+      row[L.ch_x(j)] = (uint8_t)w;
+      row[L.ch_y(j)] = (uint8_t)(w >> 8);
+    }
+  }
+}
+__device__ __forceinline__ uint32_t rescaled4(uint32_t w, float m) {
+  const float2 a = cache::e4m3x2_to_float2(w & 0xffffu), b = cache::e4m3x2_to_float2(w >> 16);
+  return cache::to_e4m3x2(a.x * m, a.y * m) | (cache::to_e4m3x2(b.x * m, b.y * m) << 16);
+}
+
+// The pages of one sequence, k or v, through a run of heads: TPP threads per page, four rows per thread; see append_kernel for the scale and
+// the codes, which follow the maximum over the rows of a page.
+template <int D, int TPP, int TH, bool KEYS>
+__device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int chunk, int b) {
+  constexpr int LPR = D / 8, RP = TPP / LPR, CH = kFourths, WARPS = TH / 32;
+  __shared__ uint32_t s_top[2][WARPS];
+  const cache::Params& p = a.p;
+  const Rows& r = KEYS ? a.k : a.v;
+  FrontDev const& f = a.f;
+  const int tt = threadIdx.x % TPP, warp = threadIdx.x >> 5;
+  int start, n;
+  if (!cache::seq_lengths(p, b, start, n)) {   // (the same for the whole block)
+    if (KEYS && group == 0 && chunk == 0 && threadIdx.x == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
+    return;
+  }
+  const int block0 = (start >> p.page_shift) + group * (TH / TPP), block = block0 + threadIdx.x / TPP;
+  if ((int64_t)block0 << p.page_shift >= (int64_t)start + n) return;   // (so is this)
+  const int64_t pos0 = (int64_t)block << p.page_shift;
+  const int r0 = (int)max((int64_t)0, start - pos0);                           // rows [0, r0) are held, [r0, r1) are new
+  int r1 = (int)max((int64_t)0, min((int64_t)p.page, (int64_t)start + n - pos0));
+  int page = 0;
+  if (r1 > r0) {
+    page = p.pages[(int64_t)b * p.max_pages + block];
+    if (page < 0 || page >= p.n_pages) {
+      if (tt == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
+      r1 = 0;
+    }
+  }
+  const bool live = r1 > r0;
+  const Lane<D> L(KEYS && f.half, KEYS ? f.h : 0, tt % LPR);   // (values: eight channels side by side)
+  const bool runs = !L.half || (L.h & 3) == 0;
+  const __nv_bfloat16* px[CH];
+  float c[CH][4], s[CH][4];
+  uint32_t fresh = 0;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int row = tt / LPR + i * RP;
+    const bool in = row >= r0 && row < r1;
+    if (in) fresh |= 1u << i;
+    const int64_t t = in ? pos0 + row - start : 0;
+    px[i] = r.x + b * r.sx[0] + t * r.sx[2];
+    if (KEYS && in) angles<D>(f, L, pos0 + row, c[i], s[i]);
+  }
+  const int h0 = chunk * a.heads, h1 = min(h0 + a.heads, p.Hkv);
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    const int64_t unit = (int64_t)page * p.Hkv + h;
+    uint8_t* codes = a.o.codes[KEYS ? 0 : 1] + unit * p.page * D;
+    float* scale = a.o.scales[KEYS ? 0 : 1] + unit;
+    const float old = live && r0 > 0 ? *scale : 0.f;
+    Raw raw[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      raw[i].a = raw[i].b = make_uint2(0, 0);
+      if (fresh >> i & 1) raw[i] = load_raw<D>(px[i] + h * r.sx[1], L, r.vx);
+    }
+    float v[CH][8];
+    uint32_t top = 0;
+    if (KEYS) {
+      float wx[4], wy[4], bx[4], by[4];
+      const bool side = r.vw ? L.side : true;
+      load_affine<D>(r.w, h, L, r.vw, side, 1.f, wx, wy);
+      load_affine<D>(r.b, h, L, r.vw, side, 0.f, bx, by);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        float x[4], y[4];
+        to_pairs(raw[i], r.vx ? L.side : true, x, y);
+        norm<D>(f, wx, wy, bx, by, x, y);
+        rotate<D>(L, c[i], s[i], x, y);
+        from_pairs(x, y, runs ? L.side : true, v[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        float x[4], y[4];
+        to_pairs(raw[i], r.vx ? L.side : true, x, y);
+        from_pairs(x, y, runs ? L.side : true, v[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      if (fresh >> i & 1) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+      }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (TPP > 32) {
+      const int at = (h - h0) & 1;   // (two sets: a thread is never two heads ahead of another)
+      if ((threadIdx.x & 31) == 0) s_top[at][warp] = top;
+      __syncthreads();
+      const int w0 = warp / (TPP / 32) * (TPP / 32);
+#pragma unroll
+      for (int w = 0; w < TPP / 32; ++w) top = max(top, s_top[at][w0 + w]);
+    } else {
+      __syncwarp();   // (every lane has read the old scale before one writes the new one)
+    }
+    if (!live) continue;
+    const int e_old = r0 > 0 ? max(cache::scale_exp(old), cache::kLeastExp) : cache::kLeastExp;
+    const bool poisoned = top >= 0x7f800000u || e_old > 127;
+    const int e = max(least_exp(top), e_old);
+    if (tt == 0) *scale = poisoned ? __int_as_float(0x7fc00000) : cache::exp2i(e);
+    const float inv = poisoned ? 0.f : cache::exp2i(-e);
+    const float down = e - e_old > 126 ? 0.f : cache::exp2i(e_old - e);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int row = tt / LPR + i * RP;
+      uint8_t* dst = codes + (int64_t)row * D;
+      if (fresh >> i & 1) {
+        uint32_t ca = 0, cb = 0;
+        if (!poisoned) codes_of(v[i], inv, ca, cb);
+        store_codes<D>(dst, L, runs, ca, cb);
+      } else if (row < r0 && e > e_old && !poisoned) {
+        uint2* held = reinterpret_cast<uint2*>(dst + (tt % LPR) * 8);
+        const uint2 w = *held;
+        *held = make_uint2(rescaled4(w.x, down), rescaled4(w.y, down));
+      }
+    }
+  }
+}
+
+template <int D, int TPP, int TH>
+__global__ void __launch_bounds__(TH, 512 / TH) ingest_kernel(const __grid_constant__ IngestArgs a) {
+  int64_t i = blockIdx.x;
+  const bool q = i >= 2 * a.kv_blocks;
+  if (q) {
+    i -= 2 * a.kv_blocks;
+    const int chunk = (int)(i % a.chunks_q), h0 = chunk * a.heads_q;
+    rows_tile<D, TH>(IngestTile{a, a.f}, a.q, i / a.chunks_q * (TH / (D / 8) * kFourths), h0, min(h0 + a.heads_q, a.q.H));
+    return;
+  }
+  const bool keys = i < a.kv_blocks;
+  if (!keys) i -= a.kv_blocks;
+  const int chunk = (int)(i % a.chunks);
+  i /= a.chunks;
+  const int group = (int)(i % a.groups), b = (int)(i / a.groups);
+  if (keys) pages_tile<D, TPP, TH, true>(a, group, chunk, b);
+  else pages_tile<D, TPP, TH, false>(a, group, chunk, b);
+}
+
+// One token per sequence: a warp per row of k or v, D / 8 lanes per row of q.
+template <int D>
+__global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant__ IngestArgs a) {
+  constexpr int LPR = D / 8;
+  const cache::Params& p = a.p;
+  const FrontDev& f = a.f;
+  const int lane = threadIdx.x & 31, sub = lane % LPR;
+  Lane<D> L(f.half, f.h, sub);
+  int64_t warp = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int64_t units = (int64_t)p.batch * p.Hkv;
+  float c[4], s[4], wx[4], wy[4], bx[4], by[4];
+  if (warp >= 2 * units) {   // ---- q ----
+    const Rows& r = a.q;
+    if (r.H == 0) return;    // (a block's warps beyond the work of a call without q)
+    int64_t row = (warp - 2 * units) * (32 / LPR) + lane / LPR;
+    const bool there = row < (int64_t)p.batch * r.H;
+    if (!there) row = 0;
+    const int b = (int)(row / r.H), h = (int)(row - (int64_t)b * r.H);
+    const Raw raw = load_raw<D>(r.x + b * r.sx[0] + h * r.sx[1], L, r.vx);
+    const bool side = r.vw ? L.side : true;
+    load_affine<D>(r.w, h, L, r.vw, side, 1.f, wx, wy);
+    load_affine<D>(r.b, h, L, r.vw, side, 0.f, bx, by);
+    int start, n;
+    const bool valid = cache::seq_lengths(p, b, start, n);
+    angles<D>(f, L, start, c, s);
+    row_through<D>(f, r, L, raw, h, there && valid && n > 0, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + h * r.sy[1]);
+    return;
+  }
+  const bool keys = warp < units;
+  if (!keys) { warp -= units; L = Lane<D>(false, 0, sub); }   // (values: eight channels side by side)
+  const Rows& r = keys ? a.k : a.v;
+  const int b = (int)(warp / p.Hkv), h = (int)(warp - (int64_t)b * p.Hkv);
+  const Raw raw = load_raw<D>(r.x + b * r.sx[0] + h * r.sx[1], L, r.vx);   // (there whatever the lengths are)
+  const bool side = r.vw ? L.side : true;
+  load_affine<D>(keys ? r.w : nullptr, h, L, r.vw, side, 1.f, wx, wy);
+  load_affine<D>(keys ? r.b : nullptr, h, L, r.vw, side, 0.f, bx, by);
+  int start, n;
+  if (!cache::seq_lengths(p, b, start, n)) {
+    if (keys && h == 0 && lane == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
+    return;
+  }
+  if (n == 0) return;
+  const int page = p.pages[(int64_t)b * p.max_pages + (start >> p.page_shift)], r0 = start & (p.page - 1);
+  if (page < 0 || page >= p.n_pages) {
+    if (lane == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
+    return;
+  }
+  const int64_t unit = (int64_t)page * p.Hkv + h;
+  uint8_t* codes = a.o.codes[keys ? 0 : 1] + unit * p.page * D;
+  float* scale = a.o.scales[keys ? 0 : 1] + unit;
+  const float old = r0 > 0 ? *scale : 0.f;
+  float x[4], y[4], v[8];
+  to_pairs(raw, r.vx ? L.side : true, x, y);
+  if (keys) {
+    angles<D>(f, L, start, c, s);
+    norm<D>(f, wx, wy, bx, by, x, y);
+    rotate<D>(L, c, s, x, y);
+  }
+  const bool runs = !L.half || (L.h & 3) == 0;
+  from_pairs(x, y, runs ? L.side : true, v);
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  top = __reduce_max_sync(0xffffffffu, top);
+  const int e_old = r0 > 0 ? max(cache::scale_exp(old), cache::kLeastExp) : cache::kLeastExp;
+  const bool poisoned = top >= 0x7f800000u || e_old > 127;
+  const int e = max(least_exp(top), e_old);
+  __syncwarp();   // (every lane has read the old scale before one writes the new one)
+  if (lane == 0) *scale = poisoned ? __int_as_float(0x7fc00000) : cache::exp2i(e);
+  if (lane < LPR) {
+    uint32_t ca = 0, cb = 0;
+    if (!poisoned) codes_of(v, cache::exp2i(-e), ca, cb);
+    store_codes<D>(codes + (int64_t)r0 * D, L, runs, ca, cb);
+  }
+  if (e > e_old && !poisoned) {   // (never where the row starts the page: r0 = 0)
+    const float down = e - e_old > 126 ? 0.f : cache::exp2i(e_old - e);
+#pragma unroll 1
+    for (int i = lane; i < r0 * (D / 16); i += 32) {
+      uint4* held = reinterpret_cast<uint4*>(codes) + i;
+      const uint4 w = *held;
+      *held = make_uint4(rescaled4(w.x, down), rescaled4(w.y, down), rescaled4(w.z, down), rescaled4(w.w, down));
+    }
+  }
+}
+
+// ---- arguments ---------------------------------------------------------------------------------------------------------------
+
+static bool within(double x, double lo, double hi) { return x >= lo && x <= hi; }   // (false for a NaN)
+
+static kvm_status_t check_front(const kvm_front_t* f, int d) {
+  if (!f) return KVM_ERR_INVALID_ARG;
+  if (f->norm < KVM_NORM_NONE || f->norm > KVM_NORM_RMS || f->layout < KVM_ROPE_HALF || f->layout > KVM_ROPE_INTERLEAVED ||
+      f->scaling < KVM_ROPE_PLAIN || f->scaling > KVM_ROPE_PARTS) return KVM_ERR_INVALID_ARG;
+  if (f->rope_dims < 0 || f->rope_dims > d || f->rope_dims % 2) return KVM_ERR_INVALID_ARG;
+  if (f->norm == KVM_NORM_NONE) {
+    if (f->q_weight || f->q_bias || f->k_weight || f->k_bias) return KVM_ERR_INVALID_ARG;
+  } else if (!within(f->eps, 0.0, 1e30)) {
+    return KVM_ERR_INVALID_ARG;
+  }
+  if (f->rope_dims > 0) {
+    if (!within(f->base, 1.0, 1e30) || !within(f->magnitude, 1e-30, 1e30)) return KVM_ERR_INVALID_ARG;
+    if (f->scaling != KVM_ROPE_PLAIN && !within(f->factor, 1.0, 1e30)) return KVM_ERR_INVALID_ARG;
+    if (f->scaling == KVM_ROPE_PARTS && (f->original_len < 1 || !within(f->low, 0.0, 1e30) || !within(f->high, 0.0, 1e30) || f->low >= f->high)) return KVM_ERR_INVALID_ARG;
+  }
+  for (const float* w : {f->q_weight, f->q_bias, f->k_weight, f->k_bias})
+    if (!cache::aligned(w, 4)) return KVM_ERR_INVALID_ARG;
+  return KVM_OK;
+}
+
+// Radians per position of pair i.
+static double frequency(const kvm_front_t* f, int i) {
+  const double w = std::pow(f->base, -2.0 * i / f->rope_dims);
+  if (f->scaling == KVM_ROPE_LINEAR) return w / f->factor;
+  if (f->scaling == KVM_ROPE_PARTS) {
+    const double turns = (double)f->original_len * w / 6.283185307179586476925;
+    const double keep = std::min(1.0, std::max(0.0, (turns - f->low) / (f->high - f->low)));
+    return keep * w + (1.0 - keep) * w / f->factor;
+  }
+  return w;
+}
+
+static FrontDev device_front(const kvm_front_t* f) {
+  FrontDev x = {};
+  x.norm = f->norm;
+  x.eps = f->norm == KVM_NORM_NONE ? 0.f : f->eps;
+  x.half = f->layout == KVM_ROPE_HALF;
+  x.h = f->rope_dims / 2;
+  x.mag = x.h ? (float)f->magnitude : 1.f;
+  for (int i = 0; i < x.h; ++i) x.quarter[i] = frequency(f, i) / 1.570796326794896619231;
+  return x;
+}
+
+static bool runs_aligned(const void* p, const int64_t (&st)[3]) { return cache::aligned(p, 8) && st[0] % 4 == 0 && st[1] % 4 == 0 && st[2] % 4 == 0; }
+
+// Rows of q, k or v with their strides; y may be NULL (nothing is written).
+static bool rows_of(Rows& r, const kvm_front_t* f, int which, const void* x, void* y, int64_t B, int64_t H, int64_t T, int d, const int64_t* sx, const int64_t* sy) {
+  if (!x || !cache::aligned(x, 2) || !cache::aligned(y, 2)) return false;
+  if (!cache::strides_of(sx, B, H, T, d, false, r.sx) || !cache::strides_of(sy, B, H, T, d, true, r.sy)) return false;
+  if (x == y) {   // in place: the same rows
+    const int64_t n[3] = {B, H, T};
+    for (int i = 0; i < 3; ++i)
+      if (n[i] > 1 && r.sx[i] != r.sy[i]) return false;
+  }
+  const bool runs = which == 2 || f->layout == KVM_ROPE_INTERLEAVED || f->rope_dims / 2 % 4 == 0;
+  r.x = (const __nv_bfloat16*)x; r.y = (__nv_bfloat16*)y;
+  r.H = (int)H;
+  r.w = which == 0 ? f->q_weight : which == 1 ? f->k_weight : nullptr;
+  r.b = which == 0 ? f->q_bias : which == 1 ? f->k_bias : nullptr;
+  r.vx = runs && runs_aligned(x, r.sx);
+  r.vy = runs && runs_aligned(y, r.sy);
+  r.vw = runs && cache::aligned(r.w, 16) && cache::aligned(r.b, 16);
+  return true;
+}
+
+// Heads of a chunk: as many as leave `want` blocks, 16 at most (the angles of a block's tokens are computed once per chunk).
+static int heads_of_chunk(int64_t blocks_per_head, int H, int64_t want) {
+  const int most = (int)std::max<int64_t>(1, std::min<int64_t>({blocks_per_head * H / want, 16, H}));
+  const int chunks = (H + most - 1) / most;
+  return (H + chunks - 1) / chunks;
+}
+
+template <int D, int TPP, int TH>
+static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
+  const cache::Params& p = a.p;
+  const int64_t pages = (p.T + p.page - 2) / p.page + 1;   // pages that T consecutive tokens can touch
+  const int64_t groups = (pages + TH / TPP - 1) / (TH / TPP);
+  a.groups = (int)groups;
+  a.heads = heads_of_chunk(groups * p.batch, p.Hkv, 4 * 148);
+  a.chunks = (p.Hkv + a.heads - 1) / a.heads;
+  a.kv_blocks = groups * p.batch * a.chunks;
+  int64_t q_blocks = 0;
+  if (a.q.H > 0) {
+    constexpr int TOK = TH / (D / 8) * kFourths;
+    const int64_t tiles = (p.T * p.batch + TOK - 1) / TOK;
+    a.heads_q = heads_of_chunk(tiles, a.q.H, 4 * 148);
+    a.chunks_q = (a.q.H + a.heads_q - 1) / a.heads_q;
+    q_blocks = tiles * a.chunks_q;
+  }
+  const int64_t blocks = 2 * a.kv_blocks + q_blocks;
+  if (blocks > INT32_MAX) return KVM_ERR_UNSUPPORTED;
+  ingest_kernel<D, TPP, TH><<<(unsigned)blocks, TH, 0, s>>>(a);
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+template <int D>
+static kvm_status_t launch_ingest_d(IngestArgs& a, cudaStream_t s) {
+  if (a.p.T == 1) {
+    const int64_t units = (int64_t)a.p.batch * a.p.Hkv, rpw = 32 / (D / 8);
+    const int64_t warps = 2 * units + ((int64_t)a.p.batch * a.q.H + rpw - 1) / rpw;
+    ingest_token_kernel<D><<<(unsigned)((warps + 3) / 4), 128, 0, s>>>(a);
+    return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+  }
+  switch (a.p.page * D / 32) {   // threads per page
+    case 32: return launch_ingest<D, 32, 256>(a, s);
+    case 64: return launch_ingest<D, 64, 256>(a, s);
+    case 128: return launch_ingest<D, 128, 256>(a, s);
+    case 256: return launch_ingest<D, 256, 256>(a, s);
+    default: return launch_ingest<D, 512, 512>(a, s);
+  }
+}
+
+}  // namespace front
+}  // namespace kvm
+
+using namespace kvm;
+using namespace kvm::front;
+
+#define KVM_API __attribute__((visibility("default")))
+
+extern "C" {
+
+KVM_API kvm_status_t kvm_rope_frequencies(const kvm_front_t* front, int32_t head_dim, double* out) {
+  if (head_dim != 64 && head_dim != 128) return KVM_ERR_UNSUPPORTED;
+  const kvm_status_t rc = check_front(front, head_dim);
+  if (rc != KVM_OK) return rc;
+  if (!out && front->rope_dims > 0) return KVM_ERR_INVALID_ARG;
+  for (int i = 0; i < front->rope_dims / 2; ++i) out[i] = frequency(front, i);
+  return KVM_OK;
+}
+
+KVM_API kvm_status_t kvm_qk_norm_rope(const kvm_front_t* front, const void* q, const void* k, const int32_t* start, const int32_t* count, int32_t batch,
+                                      int32_t n_q_heads, int32_t n_kv_heads, int64_t n_tokens, int32_t head_dim, void* q_out, void* k_out,
+                                      const int64_t* q_strides, const int64_t* k_strides, const int64_t* q_out_strides,
+                                      const int64_t* k_out_strides, int32_t* status, void* cuda_stream) {
+  if (head_dim != 64 && head_dim != 128) return KVM_ERR_UNSUPPORTED;
+  const kvm_status_t rc = check_front(front, head_dim);
+  if (rc != KVM_OK) return rc;
+  if (batch < 1 || n_tokens < 1 || (!q && !k) || (q && n_q_heads < 1) || (k && n_kv_heads < 1)) return KVM_ERR_INVALID_ARG;
+  if (!cache::aligned(start, 4) || !cache::aligned(count, 4) || !cache::aligned(status, 4)) return KVM_ERR_INVALID_ARG;
+  if (batch > 65535 || n_tokens > (1 << 30) || (q && n_q_heads > 16384) || (k && n_kv_heads > 16384)) return KVM_ERR_UNSUPPORTED;
+  QkArgs a = {};
+  a.f = device_front(front);
+  if (q && (!q_out || !rows_of(a.r[0], front, 0, q, q_out, batch, n_q_heads, n_tokens, head_dim, q_strides, q_out_strides))) return KVM_ERR_INVALID_ARG;
+  if (k && (!k_out || !rows_of(a.r[1], front, 1, k, k_out, batch, n_kv_heads, n_tokens, head_dim, k_strides, k_out_strides))) return KVM_ERR_INVALID_ARG;
+  a.start = start; a.count = count; a.status = status;
+  a.T = n_tokens; a.batch = batch;
+  const int H = a.r[0].H + a.r[1].H, lpr = head_dim / 8;
+  const int64_t tokens = (int64_t)batch * n_tokens;
+  cudaStream_t s = (cudaStream_t)cuda_stream;
+  const int64_t tiles = (tokens + 256 / lpr * kFourths - 1) / (256 / lpr * kFourths);
+  if (tokens * H <= 16384) {
+    const unsigned blocks = (unsigned)((tokens * H * lpr + 127) / 128);
+    if (head_dim == 128) qk_rows_kernel<128><<<blocks, 128, 0, s>>>(a); else qk_rows_kernel<64><<<blocks, 128, 0, s>>>(a);
+  } else {
+    if (tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
+    a.heads = heads_of_chunk(tiles, H, 4 * 148);
+    for (int i = 0; i < 2; ++i) a.chunks[i] = (a.r[i].H + a.heads - 1) / a.heads;
+    const dim3 grid((unsigned)tiles, (unsigned)(a.chunks[0] + a.chunks[1]));
+    if (head_dim == 128) qk_tile_kernel<128><<<grid, 256, 0, s>>>(a); else qk_tile_kernel<64><<<grid, 256, 0, s>>>(a);
+  }
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+
+KVM_API kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_call_t* call, const kvm_front_t* front, const void* q, int32_t n_q_heads,
+                                      const void* k, const void* v, void* q_out, const int64_t* q_strides, const int64_t* k_strides,
+                                      const int64_t* v_strides, const int64_t* q_out_strides, int32_t* status, void* cuda_stream) {
+  kvm_status_t rc = cache::check_cache(cache, true);
+  if (rc == KVM_OK) rc = cache::check_call(cache, call, true);
+  if (rc == KVM_OK) rc = check_front(front, cache->head_dim);
+  if (rc != KVM_OK) return rc;
+  if (!cache::aligned(status, 4) || (q && (n_q_heads < 1 || !q_out))) return KVM_ERR_INVALID_ARG;
+  if (q && n_q_heads > 16384) return KVM_ERR_UNSUPPORTED;
+  IngestArgs a = {};
+  a.f = device_front(front);
+  a.p = cache::params_of(cache, call, status);
+  const int64_t B = a.p.batch, T = a.p.T;
+  const int d = cache->head_dim;
+  if (q && !rows_of(a.q, front, 0, q, q_out, B, n_q_heads, T, d, q_strides, q_out_strides)) return KVM_ERR_INVALID_ARG;
+  if (!rows_of(a.k, front, 1, k, nullptr, B, a.p.Hkv, T, d, k_strides, nullptr) || !rows_of(a.v, front, 2, v, nullptr, B, a.p.Hkv, T, d, v_strides, nullptr)) return KVM_ERR_INVALID_ARG;
+  a.o.codes[0] = (uint8_t*)cache->k; a.o.codes[1] = (uint8_t*)cache->v;
+  a.o.scales[0] = cache->k_scale; a.o.scales[1] = cache->v_scale;
+  return d == 128 ? launch_ingest_d<128>(a, (cudaStream_t)cuda_stream) : launch_ingest_d<64>(a, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

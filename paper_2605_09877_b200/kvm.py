@@ -30,6 +30,7 @@ EXPORTS = ["kvm_plan_capacity", "kvm_state_create", "kvm_prefill", "kvm_decode_s
            "kvm_state_snapshot_info", "kvm_state_export_window", "kvm_state_import", "kvm_debug_expire_wait",
            "kvm_debug_decode_plan", "kvm_debug_decode_ahead", "kvm_debug_apply_plan", "kvm_debug_attention_plan",
            "kvm_debug_drop_exchange",
+           "kvm_rope_frequencies", "kvm_qk_norm_rope", "kvm_cache_ingest", "kvm_cache_read",
            "kvm_cache_append", "kvm_cache_attend", "kvm_cache_workspace", "kvm_cache_copy_pages",
            "kvm_pages_create", "kvm_pages_destroy", "kvm_pages_open", "kvm_pages_fork", "kvm_pages_close", "kvm_pages_extend",
            "kvm_pages_trim", "kvm_pages_compact", "kvm_pages_table", "kvm_pages_info"]
@@ -78,6 +79,13 @@ class CacheDesc(C.Structure):
 class CacheCall(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("start", C.c_void_p), ("count", C.c_void_p), ("batch", C.c_int32), ("max_pages", C.c_int32),
                 ("n_tokens", C.c_int64)]
+
+
+class FrontDesc(C.Structure):
+    _fields_ = [("norm", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("rope_dims", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double),
+                ("original_len", C.c_int64), ("eps", C.c_float),
+                ("q_weight", C.c_void_p), ("q_bias", C.c_void_p), ("k_weight", C.c_void_p), ("k_bias", C.c_void_p)]
 
 
 def _load():
@@ -143,6 +151,15 @@ def _load():
     L.kvm_state_import.restype = C.c_int
     L.kvm_state_import.argtypes = [vp, C.POINTER(SnapshotInfo)] + [vp] * 9
     cd, cc, i32p, i64p = C.POINTER(CacheDesc), C.POINTER(CacheCall), C.POINTER(C.c_int32), C.POINTER(C.c_int64)
+    fd = C.POINTER(FrontDesc)
+    L.kvm_rope_frequencies.restype = C.c_int
+    L.kvm_rope_frequencies.argtypes = [fd, C.c_int32, vp]
+    L.kvm_qk_norm_rope.restype = C.c_int
+    L.kvm_qk_norm_rope.argtypes = [fd, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, vp, vp, i64p, i64p, i64p, i64p, vp, vp]
+    L.kvm_cache_ingest.restype = C.c_int
+    L.kvm_cache_ingest.argtypes = [cd, cc, fd, vp, C.c_int32, vp, vp, vp, i64p, i64p, i64p, i64p, vp, vp]
+    L.kvm_cache_read.restype = C.c_int
+    L.kvm_cache_read.argtypes = [cd, cc, vp, vp, i64p, i64p, vp, vp]
     L.kvm_cache_append.restype = C.c_int
     L.kvm_cache_append.argtypes = [cd, cc, vp, vp, i64p, i64p, vp, vp]
     L.kvm_cache_attend.restype = C.c_int
@@ -535,6 +552,94 @@ def _page_list(x):
     return x.to(torch.int32)
 
 
+class Front:
+    """What an exact layer does to q and k before its attention (kvm_front_t): norm "layer", "rms" or "none" of every head's row, then rotary positions
+    in its first `rope_dims` channels, layout "half" (pairs i, i + r/2) or "interleaved" (2i, 2i + 1), scaling "none", "linear" or "parts" (factor, original_len,
+    low, high), cos and sin times `magnitude`.  Weights and biases: contiguous fp32 CUDA tensors [heads, head_dim] or None; they are kept."""
+
+    def __init__(self, norm="layer", eps: float = 1e-5, rope_dims: int = 0, layout="half", base: float = 10000.0, scaling="none", factor: float = 1.0,
+                 original_len: int = 0, low: float = 1.0, high: float = 32.0, magnitude: float = 1.0, q_weight=None, q_bias=None, k_weight=None, k_bias=None):
+        kinds = []
+        for x, names in ((norm, ("none", "layer", "rms")), (layout, ("half", "interleaved")), (scaling, ("none", "linear", "parts"))):
+            if x not in names:
+                raise ValueError(f"{x!r} is none of {names}")
+            kinds.append(names.index(x))
+        self._affine = (q_weight, q_bias, k_weight, k_bias)
+        self._device = None
+        for t in self._affine:
+            if t is not None:
+                if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or self._device not in (None, t.device):
+                    raise ValueError("weights and biases are contiguous float32 [heads, head_dim] on one CUDA device")
+                self._device = t.device
+        for pair in (self._affine[:2], self._affine[2:]):
+            if None not in pair and pair[0].shape != pair[1].shape:
+                raise ValueError("a bias has its weight's shape")
+        self.rope_dims = _int(rope_dims)
+        self._desc = FrontDesc(*kinds, self.rope_dims, base, factor, low, high, magnitude, _int(original_len, 64), eps,
+                               *(t.data_ptr() if t is not None else None for t in self._affine))
+        self._ref = C.byref(self._desc)
+
+    def frequencies(self, head_dim: int):
+        """Radians per position of each pair (kvm_rope_frequencies), a list of rope_dims / 2."""
+        out = (C.c_double * max(1, self.rope_dims // 2))()
+        rc = lib.kvm_rope_frequencies(self._ref, _int(head_dim), out)
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_rope_frequencies")
+        return list(out[:self.rope_dims // 2])
+
+    def _check(self, q, k, device):
+        """That the weights are those of q's and k's heads."""
+        if self._device not in (None, device):
+            raise ValueError("weights and biases are on the rows' device")
+        for x, pair in ((q, self._affine[:2]), (k, self._affine[2:])):
+            for t in pair:
+                if x is not None and t is not None and tuple(t.shape) != (x.shape[1], x.shape[3]):
+                    raise ValueError("weights and biases [heads, head_dim]")
+
+
+def _front_rows(pairs, lengths):
+    """Checks (rows, their out or None) pairs and the int32 tensors of a front-end call."""
+    first = next(x for x, _ in pairs if x is not None)
+    for x, y in pairs:
+        for t in (x, y):
+            if t is not None and (t.dtype != torch.bfloat16 or not t.is_cuda or t.device != first.device or t.dim() != 4):
+                raise ValueError("rows are bfloat16 [batch, heads, tokens, head_dim] on one CUDA device")
+        if x is not None:
+            if (x.shape[0], x.shape[2], x.shape[3]) != (first.shape[0], first.shape[2], first.shape[3]):
+                raise ValueError("q and k have the same batch, tokens and head_dim")
+            if y is not None and y.shape != x.shape:
+                raise ValueError("an out has its input's shape")
+    for t in lengths:
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != first.device):
+            raise ValueError("start, count and status are contiguous int32 tensors on the rows' device")
+    return first
+
+
+def qk_norm_rope(q, k, front: Front, start=None, count=None, q_out=None, k_out=None, status=None, stream=None):
+    """kvm_qk_norm_rope: q bf16 [B, n_q_heads, T, head_dim] and k bf16 [B, n_kv_heads, T, head_dim] (channels contiguous; either may be None) through
+    `front`, at positions start[b] + t (start None: t).  Returns (q_out, k_out), made here unless given; an out may be its input.  Rows behind a sequence's
+    count are left as they were (unset where the out is made here).  `status` as in Cache."""
+    if q is None and k is None:
+        raise ValueError("q or k")
+    x = _front_rows(((q, q_out), (k, k_out)), (start, count, status))
+    B, _, T, d = x.shape
+    for t in (start, count):
+        if t is not None and t.numel() != B:
+            raise ValueError("start [batch], count [batch]")
+    front._check(q, k, x.device)
+    if torch._C._cuda_getDevice() != x.device.index or (stream is not None and stream != torch.cuda.current_stream()):
+        with torch.cuda.device(x.device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
+            return qk_norm_rope(q, k, front, start, count, q_out, k_out, status)
+    outs = [y if y is not None or t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t, y in ((q, q_out), (k, k_out))]
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    st = lambda t: _strides3(t) if t is not None else None  # noqa: E731
+    rc = lib.kvm_qk_norm_rope(front._ref, ptr(q), ptr(k), ptr(start), ptr(count), B, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, T, d,
+                              ptr(outs[0]), ptr(outs[1]), st(q), st(k), st(outs[0]), st(outs[1]), ptr(status), _stream_ptr(None))
+    if rc != KVM_OK:
+        raise KVMError(rc, "kvm_qk_norm_rope")
+    return tuple(outs)
+
+
 class Cache:
     """A pool of pages for exact keys and values in 8 bits (kvm_cache_t): codes k8, v8 float8_e4m3fn [n_pages, n_kv_heads, page_tokens,
     head_dim], scales fp32 [n_pages, n_kv_heads] (powers of two; a row stands for code * scale).  The tensors are the caller's;
@@ -593,6 +698,46 @@ class Cache:
                                   status.data_ptr() if status is not None else None, _stream_ptr(stream))
         if rc != KVM_OK:
             raise KVMError(rc, "kvm_cache_append")
+
+    def ingest(self, q, k, v, front: Front, pages, start, count=None, q_out=None, status=None, stream=None):
+        """kvm_cache_ingest: q and k bf16 [B, heads, T, head_dim] through `front` at positions start[b] + t, k and v into the cache behind the tokens that the
+        sequences hold.  Returns q_out, made here unless given; it may be q.  q may be None: k and v only."""
+        if k.dim() != 4 or v.shape != k.shape or k.shape[1] != self.n_kv_heads or k.shape[3] != self.head_dim:
+            raise ValueError("k, v [batch, n_kv_heads, tokens, head_dim]")
+        if q is None and q_out is not None:
+            raise ValueError("q_out without q")
+        _front_rows(((k, None), (v, None), (q, q_out)), ())
+        front._check(q, k, k.device)
+        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+            with torch.cuda.device(self._device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
+                return self.ingest(q, k, v, front, pages, start, count, q_out, status)
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        call = self._call(pages, start, count, (k, v), status)
+        rc = lib.kvm_cache_ingest(self._ref, call, front._ref, q.data_ptr() if q is not None else None, q.shape[1] if q is not None else 0, k.data_ptr(), v.data_ptr(),
+                                  q_out.data_ptr() if q is not None else None, _strides3(q) if q is not None else None, _strides3(k), _strides3(v),
+                                  _strides3(q_out) if q is not None else None, status.data_ptr() if status is not None else None, _stream_ptr(None))
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_cache_ingest")
+        return q_out
+
+    def read(self, pages, start, n_tokens: int, count=None, k_out=None, v_out=None, status=None, stream=None):
+        """kvm_cache_read: positions start[b] .. start[b] + count[b] - 1 as bf16 [B, n_kv_heads, n_tokens, head_dim], (k_out, v_out), made here unless given.  Rows behind a
+        sequence's count are left as they were (unset where made here)."""
+        shape = (pages.shape[0], self.n_kv_heads, _int(n_tokens), self.head_dim)
+        for t in (k_out, v_out):
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError("k_out, v_out [batch, n_kv_heads, n_tokens, head_dim]")
+        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+            with torch.cuda.device(self._device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
+                return self.read(pages, start, n_tokens, count, k_out, v_out, status)
+        k_out, v_out = (torch.empty(shape, dtype=torch.bfloat16, device=self._device) if t is None else t for t in (k_out, v_out))
+        call = self._call(pages, start, count, (k_out, v_out), status)
+        rc = lib.kvm_cache_read(self._ref, call, k_out.data_ptr(), v_out.data_ptr(), _strides3(k_out), _strides3(v_out),
+                                status.data_ptr() if status is not None else None, _stream_ptr(None))
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_cache_read")
+        return k_out, v_out
 
     def attend(self, q, pages, start, count=None, window: int = 0, sinks: int = 0, scale=None, out=None, status=None, stream=None):
         """kvm_cache_attend: q bf16 [B, n_q_heads, T, head_dim] over the cache, which holds the T tokens' own keys already; a token sees
