@@ -501,6 +501,22 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
                               int32_t window, int32_t sinks, void* out, const int64_t* q_strides, const int64_t* out_strides,
                               void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
 
+/* kvm_cache_attend (window = 0) for a batch whose sequences share their first blocks in groups: a system prompt, a document, the samples or beams of one
+ * prompt.  Group g is sequences groups[g] .. groups[g + 1] - 1, and the first shared[g] blocks of their tables hold the same tokens (forks: the same
+ * pages; kvm_pages_shared counts them).  Those blocks are read once for the group, from the table of its first sequence; entries of the other tables there
+ * may be anything.  Every token sees what it sees in kvm_cache_attend; the results differ by rounding.
+ *   groups   device int32 [n_groups + 1]: ascends (groups of no sequences are allowed) from 0 to batch
+ *   shared   device int32 [n_groups], 0 <= shared[g] <= max_pages, and shared[g] * page_tokens <= start[b] for the sequences of g
+ * Groups that are none, or a number of blocks that is not allowed, are reported like lengths that are not, and their sequences get no rows.
+ * Otherwise as kvm_cache_attend, the precision of a weight and of q included; workspace: kvm_cache_shared_workspace() bytes.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA; nothing is launched on an error. */
+kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm_cache_call_t* call, const int32_t* groups, const int32_t* shared, int32_t n_groups,
+                                     const void* q, int32_t n_q_heads, float scale, void* out, const int64_t* q_strides, const int64_t* out_strides,
+                                     void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+
+/* Bytes of workspace that kvm_cache_attend_shared needs for these sizes; -1 on invalid arguments and on sizes that it refuses. */
+int64_t kvm_cache_shared_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_groups, int32_t n_q_heads);
+
 /* Bytes of workspace that kvm_cache_attend needs for these sizes (pointers are not looked at); -1 on invalid arguments and on
  * sizes that kvm_cache_attend refuses. */
 int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_q_heads);
@@ -535,6 +551,9 @@ kvm_status_t kvm_pages_compact(kvm_pages_t* p, int32_t* src, int32_t* dst, int64
 /* The table of a sequence: *n_blocks blocks for *n_tokens tokens, copied to pages[0 .. capacity) with -1 behind the last block (pages
  * may be NULL with capacity 0).  CAPACITY when the blocks do not fit.  Any of n_blocks, n_tokens may be NULL. */
 kvm_status_t kvm_pages_table(const kvm_pages_t* p, int32_t seq, int32_t* pages, int64_t capacity, int64_t* n_blocks, int64_t* n_tokens);
+/* The number of leading blocks that `n` sequences have in common in front of the last n_tokens tokens of each (those of a call to come): full ones, on the same
+ * pages, none of them given back.  What kvm_cache_attend_shared takes for a group. */
+kvm_status_t kvm_pages_shared(const kvm_pages_t* p, const int32_t* seqs, int64_t n, int64_t n_tokens, int32_t* n_blocks);
 /* Pages that no sequence uses, and the largest page number in use plus one.  Either may be NULL. */
 kvm_status_t kvm_pages_info(const kvm_pages_t* p, int64_t* n_free, int64_t* high);
 

@@ -370,6 +370,26 @@ bool rows_aligned(const void* p, const int64_t (&st)[3]) {
   return aligned(p, 16) && st[0] % 8 == 0 && st[1] % 8 == 0 && st[2] % 8 == 0;
 }
 
+// What the attention kernels are given, but for the workspace.
+kvm_status_t attend_args(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale, int32_t window, int32_t sinks, void* out,
+                         const int64_t* q_strides, const int64_t* out_strides, int32_t* status, AttendArgs& a) {
+  kvm_status_t rc = check_cache(cache, true);
+  if (rc == KVM_OK) rc = check_call(cache, call, true);
+  if (rc != KVM_OK) return rc;
+  if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || !aligned(status, 4)) return KVM_ERR_INVALID_ARG;
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || window < 0 || sinks < 0) return KVM_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || scale > 3.0e38f) return KVM_ERR_INVALID_ARG;   // (a NaN is refused too)
+  a = AttendArgs{};
+  a.p = params_of(cache, call, status);
+  a.q = (const __nv_bfloat16*)q; a.out = (__nv_bfloat16*)out;
+  if (!strides_of(q_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, false, a.sq) ||
+      !strides_of(out_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, true, a.so)) return KVM_ERR_INVALID_ARG;
+  a.Hq = n_q_heads; a.G = n_q_heads / cache->n_kv_heads; a.d = cache->head_dim;
+  a.window = window ? window : INT32_MAX; a.sinks = std::min(sinks, 1 << 30);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  return attend_fits(cache, call, n_q_heads) ? KVM_OK : KVM_ERR_UNSUPPORTED;
+}
+
 }  // namespace cache
 }  // namespace kvm
 
@@ -461,22 +481,10 @@ KVM_API int64_t kvm_cache_workspace(const kvm_cache_t* cache, const kvm_cache_ca
 KVM_API kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale,
                                       int32_t window, int32_t sinks, void* out, const int64_t* q_strides, const int64_t* out_strides,
                                       void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream) {
-  kvm_status_t rc = check_cache(cache, true);
-  if (rc == KVM_OK) rc = check_call(cache, call, true);
-  if (rc != KVM_OK) return rc;
-  if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || !aligned(status, 4)) return KVM_ERR_INVALID_ARG;
-  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || window < 0 || sinks < 0) return KVM_ERR_INVALID_ARG;
-  if (!(scale > 0.f) || scale > 3.0e38f) return KVM_ERR_INVALID_ARG;   // (a NaN is refused too)
   AttendArgs a;
-  a.p = params_of(cache, call, status);
-  a.q = (const __nv_bfloat16*)q; a.out = (__nv_bfloat16*)out;
-  if (!strides_of(q_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, false, a.sq) ||
-      !strides_of(out_strides, a.p.batch, n_q_heads, a.p.T, cache->head_dim, true, a.so)) return KVM_ERR_INVALID_ARG;
-  a.Hq = n_q_heads; a.G = n_q_heads / cache->n_kv_heads; a.d = cache->head_dim;
-  a.window = window ? window : INT32_MAX; a.sinks = std::min(sinks, 1 << 30);
-  if (!attend_fits(cache, call, n_q_heads)) return KVM_ERR_UNSUPPORTED;
+  const kvm_status_t rc = attend_args(cache, call, q, n_q_heads, scale, window, sinks, out, q_strides, out_strides, status, a);
+  if (rc != KVM_OK) return rc;
   const int64_t tiles = tiles_most(cache, call);
-  a.scale_log2 = scale * 1.4426950408889634f;
   const int64_t need = kvm_cache_workspace(cache, call, n_q_heads);
   if (need < 0) return KVM_ERR_UNSUPPORTED;
   if (need > 0 && (!workspace || !aligned(workspace, 16))) return KVM_ERR_INVALID_ARG;

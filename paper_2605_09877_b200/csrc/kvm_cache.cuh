@@ -42,11 +42,12 @@ __device__ __forceinline__ bool sees(int i, int j, int window, int sinks) {
 struct PageList {
   int n_sink, first, n, tiles;   // page i of the list is page page_at(i) of the sequence; n pages, so many tiles
 };
-__device__ __forceinline__ PageList pages_of(const Params& p, int first, int last, int window, int sinks) {
+// (skip: blocks in front that somebody else looks at)
+__device__ __forceinline__ PageList pages_of(const Params& p, int first, int last, int window, int sinks, int skip = 0) {
   PageList t;
   const int end = (last >> p.page_shift) + 1;
   const int low = first - window + 1;   // (first >= 0 and window >= 1: no overflow)
-  const int w0 = low > 0 ? low >> p.page_shift : 0;
+  const int w0 = max(skip, low > 0 ? low >> p.page_shift : 0);
   t.n_sink = min(w0, (sinks + p.page - 1) >> p.page_shift);
   t.first = w0;
   t.n = t.n_sink + end - w0;
@@ -103,6 +104,72 @@ __device__ __forceinline__ void split_e4m3x2(float a, float b, uint32_t& hi, uin
   lo = l;
 }
 
+// n / d for 0 <= n < 2^31: with 2^(l-1) < d <= 2^l, m = floor(2^(31+l) / d) + 1, m d exceeds 2^(31+l) by at most 2^l, so n m >> (31 + l) is exact.
+struct FastDiv {
+  uint32_t m, s, d;
+  explicit FastDiv(uint32_t x = 1) : d(x) {
+    int l = 0;
+    while ((1ull << l) < x) ++l;
+    s = 31 + l;
+    m = (uint32_t)((1ull << s) / x + 1);
+  }
+  __device__ __forceinline__ int div(int n) const { return (int)(((uint64_t)(uint32_t)n * m) >> s); }
+};
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// two floats -> two fp16 (a in the low half), round to nearest even, saturating (logits beyond 2^24 are rounded to more than 1)
+__device__ __forceinline__ uint32_t to_f16x2(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+// Groups of sequences that share their first blocks (kvm_cache_attend_shared): sequences offsets[g] .. offsets[g + 1] - 1 share shared[g] blocks.
+struct Groups {
+  const int32_t *offsets, *shared;
+  int n;
+};
+// The group of sequence b: the last whose offset is not behind it (by a whole warp).
+__device__ __forceinline__ int group_of(const Groups& g, int b) {
+  int before = 0;
+  for (int i0 = 0; i0 < g.n; i0 += 32) {
+    const int i = i0 + (int)(threadIdx.x & 31);
+    before += __popc(__ballot_sync(0xffffffffu, i < g.n && g.offsets[i] <= b));
+  }
+  return max(0, before - 1);
+}
+// The offsets, n + 1, to shared memory, by all NT threads of a block; whether they ascend from 0 to the batch (else nothing may be made of them).
+template <int NT>
+__device__ __forceinline__ bool load_groups(const Groups& g, int batch, int* offsets) {
+  bool ok = true;
+#pragma unroll 1
+  for (int i = threadIdx.x; i <= g.n; i += NT) {
+    const int x = g.offsets[i], before = i ? g.offsets[i - 1] : 0;
+    offsets[i] = x;
+    ok = ok && (i ? x >= before : x == 0) && (i < g.n || x == batch);
+  }
+  return __syncthreads_and(ok);
+}
+// Lengths of a sequence behind `skip` shared blocks: they have to lie in front of the call's tokens.
+__device__ __forceinline__ bool shared_lengths(const Params& p, int b, int skip, int& start, int& n) {
+  return seq_lengths(p, b, start, n) && skip >= 0 && skip <= p.max_pages && start >= skip << p.page_shift;
+}
+
 struct AttendArgs {
   Params p;
   const __nv_bfloat16* q;
@@ -111,14 +178,29 @@ struct AttendArgs {
   int Hq, G, d, window, sinks;   // window: INT32_MAX = all
   float scale_log2;              // scale * log2(e)
   float* part;                   // workspace
+  // The kernels' SIDE builds: over the blocks behind the shared ones; results are left as partial ones for shared_merge_kernel.
+  Groups groups;
+  float* side;                   // few tokens: [unit][column][D + 2] of the units that one worker did
+  int2* found;                   // few tokens: per unit its first and last worker (last -1: it is in `side`)
 };
 // tokens times heads of a group <= kDecodeCols; tiles: most key tiles of a sequence
 constexpr int kDecodeCols = 16;
 kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s);
 int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols);
+// ... SIDE: how many workers there are
+kvm_status_t launch_decode8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, int& workers);
 // more than that; rows: tokens times heads of a group
 kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s);
 int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d);
+// ... SIDE: row tiles of a unit and key splits, [((row tiles - 1 - row tile) * units + unit) * splits + split][D + 2][128] in a.part
+struct PromptSide { int qtiles, nsplit; };
+kvm_status_t launch_prompt8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, PromptSide& side);
+int64_t prompt_side_workspace(int64_t units, int64_t rows, int64_t tiles, int d);
+constexpr int kSplitTiles = 4;    // least key tiles of a split
+__host__ __device__ __forceinline__ int split_tiles(int tiles, int nsplit) {   // key tiles of a split, of a row tile that sees so many
+  const int per = (tiles + nsplit - 1) / nsplit;
+  return per < kSplitTiles ? kSplitTiles : per;
+}
 
 // Codes and scales that a call writes: keys, values.
 struct AppendOut {

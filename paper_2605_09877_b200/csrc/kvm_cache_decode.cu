@@ -22,6 +22,9 @@
 // one group per CTA and two CTAs per SM the kernel was bound by that chain (247 us where it takes 205 now).  A unit that spans several workers is
 // merged by combine_kernel from their partial results.  The code is kept small: at 197 KB it ran from the instruction cache's misses (317 us).
 //
+// The SIDE build looks at the blocks behind those that a group of sequences shares (kvm_cache_shared.cu), and merges nothing: results of a unit that one
+// worker did go to a place of their own, unnormalised, and `found` says where those of the others are.
+//
 // Bound by HBM (2 d bytes per key and kv head), a tile every 1280 cycles and SM once it runs, 8 us after its start.  Measured, d = 128: 64 sequences
 // of up to 16384 tokens, 32 heads on 8: 193 to 210 us, 5.2 to 5.7 TB/s (80 to 86 % of the measured copy rate); one of 131072, 8 heads: 57 us, 4.7 TB/s; 64
 // with a window of 512, 32 heads: 77 us, 3.4 TB/s (640 keys are read where 516 are seen); one of 1000: 14 us, two launches.
@@ -49,10 +52,10 @@ struct alignas(16) TileInfo {
 // first / last tile of the worker's share of the unit; the share is all of it / begins with it; all columns see all keys of the tile
 enum { kFirst = 1, kLast = 2, kWhole = 4, kBegins = 8, kAll = 16 };
 
-template <int D, int NC>
+template <int D, int NC, bool SIDE = false>
 struct DecodeCfg {
   static constexpr int NG = NC == 8 ? 4 : 3;             // groups (16 columns take 128 registers)
-  static constexpr int ST = (NC == 8 ? 6 : 5) * (128 / D);   // tiles of the ring
+  static constexpr int ST = (NC == 8 && !SIDE ? 6 : 5) * (128 / D);   // tiles of the ring (SIDE: one less, for what it knows of the sequences)
   static constexpr int THREADS = 128 + 128 * NG;
   static constexpr int TILE = 128 * D;                   // codes of a tile of keys or values
   static constexpr int STAGE = 2 * TILE;
@@ -66,7 +69,7 @@ struct DecodeCfg {
   static constexpr int OFF_AB = OFF_MAX + NG * 2 * NC * 16;              // float4 [group][2][NC]
   static constexpr int OFF_L = OFF_AB + NG * 2 * NC * 16;                // float [group][4][NC]
   static constexpr int OFF_BAR = OFF_L + NG * 4 * NC * 4;
-  static constexpr int OFF_PRE = OFF_BAR + 1024;         // int [batch + 1]
+  static constexpr int OFF_PRE = OFF_BAR + 1024;         // int [batch + 1]; SIDE: and [batch], the shared blocks of each sequence
   static constexpr uint32_t TMEM_COLS = NC == 8 ? 256 : 512;
   static constexpr uint32_t GROUP_COLS = 3 * NB;         // two S, then O
   // barriers
@@ -156,8 +159,8 @@ __device__ __forceinline__ bool group_barrier(int g, bool ok) {
   return r != 0;
 }
 // Tiles that the call's tokens of a sequence see (0: none, or lengths that are not allowed).
-__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int start, int n) {
-  return n > 0 ? pages_of(a.p, start, start + n - 1, a.window, a.sinks).tiles : 0;
+__device__ __forceinline__ int seq_tiles(const AttendArgs& a, int start, int n, int skip) {
+  return n > 0 ? pages_of(a.p, start, start + n - 1, a.window, a.sinks, skip).tiles : 0;
 }
 // Last b with pre[b] <= f (pre ascends; f < pre[batch], so that sequence b has tiles).
 __device__ __forceinline__ int seq_of(const int* pre, int batch, int f) {
@@ -170,22 +173,33 @@ __device__ __forceinline__ int seq_of(const int* pre, int batch, int f) {
   return lo;
 }
 
-// pre[0 .. batch]: tiles of the sequences before b, all heads; by all NT threads of the block
-template <int NT>
-__device__ __forceinline__ void list_tiles(const AttendArgs& a, int* pre, int* scratch) {
+// pre[0 .. batch]: tiles of the sequences before b, all heads; by all NT threads of the block.  SIDE: skip[b], the shared blocks of each sequence
+// (offsets: room for the groups' offsets, n + 1); groups that are none leave nothing to do.
+template <int NT, bool SIDE>
+__device__ __forceinline__ void list_tiles(const AttendArgs& a, int* pre, int* scratch, int* skip, int* offsets) {
   const Params& p = a.p;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int per = (p.batch + NT - 1) / NT, b0 = tid * per;
+  bool groups = true;
+  if constexpr (SIDE) groups = load_groups<NT>(a.groups, p.batch, offsets);
   int sum = 0;
 #pragma unroll 1
   for (int b = b0; b < min(b0 + per, p.batch); ++b) {
-    int start, n;
-    if (!seq_lengths(p, b, start, n)) {
+    int start, n, sk = 0;
+    bool valid;
+    if constexpr (SIDE) {
+      sk = groups ? a.groups.shared[seq_of(offsets, a.groups.n, b)] : 0;
+      valid = groups && shared_lengths(p, b, sk, start, n);
+      skip[b] = valid ? sk : 0;
+    } else {
+      valid = seq_lengths(p, b, start, n);
+    }
+    if (!valid) {
       if (blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
-      start = n = 0;
+      start = n = sk = 0;
     }
     pre[b] = sum;
-    sum += seq_tiles(a, start, n) * p.Hkv;
+    sum += seq_tiles(a, start, n, sk) * p.Hkv;
   }
   int incl = sum;
 #pragma unroll
@@ -222,10 +236,10 @@ __device__ __forceinline__ float sum_lanes(float (&v)[N], int lane) {
   return s;
 }
 
-template <int D, int NC>
-__global__ void __launch_bounds__(DecodeCfg<D, NC>::THREADS, 1)
+template <int D, int NC, bool SIDE>
+__global__ void __launch_bounds__(DecodeCfg<D, NC, SIDE>::THREADS, 1)
 decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ DecodeArgs8 args) {
-  using Cfg = DecodeCfg<D, NC>;
+  using Cfg = DecodeCfg<D, NC, SIDE>;
   constexpr int NB = Cfg::NB, NG = Cfg::NG, ST = Cfg::ST;
   const AttendArgs& a = args.a;
   const Params& p = a.p;
@@ -237,6 +251,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + Cfg::COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* pre = reinterpret_cast<int*>(base + Cfg::OFF_PRE);
+  const int* skip = pre + p.batch + 1;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (combine_kernel waits for this one before it reads what it wrote)
@@ -254,7 +269,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   tc::tc_fence_before();
-  list_tiles<Cfg::THREADS>(a, pre, reinterpret_cast<int*>(base + Cfg::OFF_AB));
+  list_tiles<Cfg::THREADS, SIDE>(a, pre, reinterpret_cast<int*>(base + Cfg::OFF_AB), pre + p.batch + 1, reinterpret_cast<int*>(base));   // (offsets: where the first tiles go)
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Shares<NG> sh(pre[p.batch], args.grid, blockIdx.x);
@@ -288,7 +303,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const int b = seq_of(pre, p.batch, f);
         lengths(b, x.start, x.n);
         const int last = x.start + x.n - 1;
-        const PageList t = pages_of(p, x.start, last, a.window, a.sinks);
+        const PageList t = pages_of(p, x.start, last, a.window, a.sinks, SIDE ? skip[b] : 0);
         const int rem = f - pre[b], hk = rem / t.tiles, it = rem - hk * t.tiles, u0 = f - it;
         x.b = b; x.hk = hk;
         x.flags = (it == 0 || i == 0 ? kFirst : 0) | (it == t.tiles - 1 || i == n - 1 ? kLast : 0) | (u0 >= F0 ? kBegins : 0) |
@@ -574,7 +589,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       const float lw = sum_lanes<NC>(l_run, lane);
       if ((lane & (32 / NC - 1)) == 0) s_l[(lane / (32 / NC)) * 4 + w4] = lw;
       group_barrier(g, true);
-      if (pflags & kWhole) {
+      if (!SIDE && (pflags & kWhole)) {
         // (each thread's channel of the columns through its own bytes of the weights, which nothing reads now: the loop over the columns
         // stays small)
         uint32_t h[NC / 2];
@@ -601,6 +616,11 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
       } else {
         float* part = a.part + (int64_t)(2 * worker + (pflags & kBegins ? 1 : 0)) * NC * (D + 2);
+        if constexpr (SIDE) {
+          const int64_t unit = (int64_t)pb * p.Hkv + phk;
+          if (pflags & kWhole) part = a.side + unit * NC * (D + 2);
+          if (tok == 0 && (pflags & kBegins)) a.found[unit] = make_int2(worker, pflags & kWhole ? -1 : pze);
+        }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {   // (columns that are not in use give something that nobody reads)
           if (tok < D) part[c * (D + 2) + tok] = o_run[c];
@@ -731,9 +751,10 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       s += sh.active(i);
       if (s >= ST) { s -= ST; par ^= 1; }
     }
-    if (tok == 0) args.cuts[worker] = Cut{ok && (pflags & (kBegins | kWhole)) == kBegins ? pb : -1, phk, pn, pze};
+    if (!SIDE && tok == 0) args.cuts[worker] = Cut{ok && (pflags & (kBegins | kWhole)) == kBegins ? pb : -1, phk, pn, pze};
     if (!ok) fail();
   }
+  if constexpr (SIDE) asm volatile("griddepcontrol.wait;" ::: "memory");   // (the merge counts on the end of this grid and of the one before it)
   tc::tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -810,43 +831,57 @@ int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols) {
   return decode_partials(workers, d, cols) + workers * (int64_t)sizeof(Cut);
 }
 
-template <int D, int NC>
+template <int D, int NC, bool SIDE>
 static kvm_status_t launch_decode_nc(const DecodeArgs8& args, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
-  using Cfg = DecodeCfg<D, NC>;
-  static_assert(Cfg::OFF_PRE + (kMaxBatch + 1) * 4 + 1024 <= 227 * 1024, "shared memory");
-  const int smem = Cfg::OFF_PRE + (args.a.p.batch + 1) * 4 + 1024;
+  using Cfg = DecodeCfg<D, NC, SIDE>;
+  constexpr int most = Cfg::OFF_PRE + (kMaxBatch + 1) * (SIDE ? 8 : 4) + 1024;
+  static_assert(most <= 227 * 1024, "shared memory");
+  const int smem = Cfg::OFF_PRE + (args.a.p.batch + 1) * (SIDE ? 8 : 4) + 1024;
   static std::atomic<uint64_t> ready{0};   // devices on which the limit has been raised
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    constexpr int most = Cfg::OFF_PRE + (kMaxBatch + 1) * 4 + 1024;
-    if (cudaFuncSetAttribute(decode_kernel<D, NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+    if (cudaFuncSetAttribute(decode_kernel<D, NC, SIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
     if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  decode_kernel<D, NC><<<args.grid, Cfg::THREADS, smem, s>>>(mapK, mapV, args);
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(args.grid * Cfg::NG, (unsigned)(args.a.p.T * args.a.G)); lc.blockDim = dim3(256); lc.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = at; lc.numAttrs = 1;
+  lc.attrs = at; lc.numAttrs = 1; lc.stream = s;
+  if constexpr (SIDE) {   // (beside the end of the kernel over the shared blocks)
+    lc.gridDim = dim3(args.grid); lc.blockDim = dim3(Cfg::THREADS); lc.dynamicSmemBytes = smem;
+    if (cudaLaunchKernelEx(&lc, decode_kernel<D, NC, true>, mapK, mapV, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+    return KVM_OK;
+  }
+  decode_kernel<D, NC, SIDE><<<args.grid, Cfg::THREADS, smem, s>>>(mapK, mapV, args);
+  lc.gridDim = dim3(args.grid * Cfg::NG, (unsigned)(args.a.p.T * args.a.G)); lc.blockDim = dim3(256);
   if (cudaLaunchKernelEx(&lc, combine_kernel<D, NC>, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 
-kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s) {
+template <bool SIDE>
+static kvm_status_t launch_decode8_any(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, int& workers) {
   DecodeArgs8 args;
   args.a = a;
   args.grid = decode_grid((int64_t)a.p.batch * a.p.Hkv, tiles);
   const int cols = (int)(a.p.T * a.G);
-  args.cuts = reinterpret_cast<Cut*>(reinterpret_cast<uint8_t*>(a.part) + decode_partials(args.grid * (cols <= 8 ? 4 : 3), a.d, cols));
+  workers = args.grid * (cols <= 8 ? 4 : 3);
+  args.cuts = reinterpret_cast<Cut*>(reinterpret_cast<uint8_t*>(a.part) + decode_partials(workers, a.d, cols));
   args.q_vec = q_vec ? 1 : 0;
   CUtensorMap mapK, mapV;
   const int64_t rows = a.p.n_pages * a.p.Hkv * a.p.page;
   if (!encode_tmap_codes(&mapK, a.p.k, a.d, rows, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, rows, a.p.page)) return KVM_ERR_CUDA;
   const bool few = cols <= 8;
-  if (a.d == 128) return few ? launch_decode_nc<128, 8>(args, mapK, mapV, s) : launch_decode_nc<128, 16>(args, mapK, mapV, s);
-  return few ? launch_decode_nc<64, 8>(args, mapK, mapV, s) : launch_decode_nc<64, 16>(args, mapK, mapV, s);
+  if (a.d == 128) return few ? launch_decode_nc<128, 8, SIDE>(args, mapK, mapV, s) : launch_decode_nc<128, 16, SIDE>(args, mapK, mapV, s);
+  return few ? launch_decode_nc<64, 8, SIDE>(args, mapK, mapV, s) : launch_decode_nc<64, 16, SIDE>(args, mapK, mapV, s);
+}
+kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s) {
+  int workers;
+  return launch_decode8_any<false>(a, tiles, q_vec, s, workers);
+}
+kvm_status_t launch_decode8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, int& workers) {
+  return launch_decode8_any<true>(a, tiles, q_vec, s, workers);
 }
 
 }  // namespace cache

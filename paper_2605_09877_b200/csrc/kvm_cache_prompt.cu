@@ -23,7 +23,8 @@
 // A CTA that is done may go on with a block of the grid that has not begun (MORE): the warp that produces keys asks the hardware for it when it has
 // three tiles left to load, works out what there is to do and tells the others, whose rings and barriers go on; keys, values and the search for
 // vbase are then under way while the last tiles are still in their softmax.
-// With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.
+// With few rows the key tiles are dealt over several CTAs (splits), whose partial results prompt_combine_kernel merges.  The SIDE build looks at the
+// blocks behind those that a group of sequences shares (kvm_cache_shared.cu) and leaves partial results only.
 //
 // Bound by the softmax warps and the conversion: 1600 instructions per scheduler and tile (128 x 128) against 1024 cycles of the tensor core, 2300
 // cycles a tile; and by the set-up, filling and emptying per block of 128 rows (8 us, 7 where a CTA goes on), most of what short windows
@@ -43,20 +44,8 @@ namespace cache {
 
 bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page);   // kvm_cache.cu
 
-constexpr int kSplitTiles = 4;    // least key tiles of a split
 constexpr int kMaxSplits = 32;
 
-// n / d for 0 <= n < 2^31: with 2^(l-1) < d <= 2^l, m = floor(2^(31+l) / d) + 1, m d exceeds 2^(31+l) by at most 2^l, so n m >> (31 + l) is exact.
-struct FastDiv {
-  uint32_t m, s, d;
-  explicit FastDiv(uint32_t x = 1) : d(x) {
-    int l = 0;
-    while ((1ull << l) < x) ++l;
-    s = 31 + l;
-    m = (uint32_t)((1ull << s) / x + 1);
-  }
-  __device__ __forceinline__ int div(int n) const { return (int)(((uint64_t)(uint32_t)n * m) >> s); }
-};
 struct PromptArgs {
   AttendArgs a;
   FastDiv by_units, by_heads, by_group;
@@ -122,12 +111,20 @@ struct alignas(16) PromptWork {
   int b, hk, start, row0, rows, first, last, jb, ntiles, parts;
   PageList t;
 };
+template <bool SIDE = false>
 __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int sp, PromptWork& w) {
   const Params& p = args.a.p;
   const int turn = args.by_units.div(idx), unit = idx - turn * args.units, qt = args.qtiles - 1 - turn;   // (the last rows see the most keys: first)
   w.b = args.by_heads.div(unit); w.hk = unit - w.b * p.Hkv;
-  int n;
-  if (!seq_lengths(p, w.b, w.start, n)) {
+  int n, skip = 0;
+  bool valid;
+  if constexpr (SIDE) {
+    skip = args.a.groups.shared[group_of(args.a.groups, w.b)];
+    valid = shared_lengths(p, w.b, skip, w.start, n);
+  } else {
+    valid = seq_lengths(p, w.b, w.start, n);
+  }
+  if (!valid) {
     if (idx == unit && w.hk == 0 && sp == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
     return false;
   }
@@ -137,12 +134,12 @@ __device__ __forceinline__ bool prompt_work(const PromptArgs& args, int idx, int
   w.rows = (int)min((int64_t)kRows, left);
   w.first = w.start + args.by_group.div(w.row0);
   w.last = w.start + args.by_group.div(w.row0 + w.rows - 1);
-  w.t = pages_of(p, w.first, w.last, args.a.window, args.a.sinks);
+  w.t = pages_of(p, w.first, w.last, args.a.window, args.a.sinks, skip);
   w.parts = 1;
   w.jb = 0;
   w.ntiles = w.t.tiles;
   if (args.nsplit > 1) {
-    const int per = max(kSplitTiles, (w.t.tiles + args.nsplit - 1) / args.nsplit);
+    const int per = split_tiles(w.t.tiles, args.nsplit);
     w.parts = (w.t.tiles + per - 1) / per;
     w.jb = sp * per;
     w.ntiles = min(per, w.t.tiles - w.jb);
@@ -184,30 +181,7 @@ __device__ __forceinline__ bool pair_barrier(int id, bool ok) {
 __device__ __forceinline__ void copy16_async(void* smem, const void* global) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(smem)), "l"(global) : "memory");
 }
-// two fp32 operations in one instruction
-__device__ __forceinline__ uint64_t pack2(float x, float y) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-// two floats -> two fp16 (a in the low half), round to nearest even, saturating (logits beyond 2^24 are rounded to more than 1)
-__device__ __forceinline__ uint32_t to_f16x2(float a, float b) {
-  uint32_t r;
-  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
-template <int D, bool MORE>
+template <int D, bool MORE, bool SIDE>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ PromptArgs args) {
   using Cfg = PromptCfg<D>;
@@ -229,7 +203,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the merge waits for this kernel before it reads what it wrote)
   PromptWork first;
-  if (!prompt_work(args, blockIdx.x, blockIdx.y, first)) return;
+  if (!prompt_work<SIDE>(args, blockIdx.x, blockIdx.y, first)) {
+    if constexpr (SIDE) asm volatile("griddepcontrol.wait;" ::: "memory");   // (the merge counts on the end of this grid and of the one before it)
+    return;
+  }
   if (MORE && tid == 0) works[0] = first;
   auto work = [&](int item) -> const PromptWork& { return MORE ? works[item % kWorks] : first; };
 
@@ -804,14 +781,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       bad = s_l[512 + row] + s_l[640 + row] + s_l[768 + row] + s_l[896 + row] != 0.f;
       uint8_t* stage = base + Cfg::OFF_Q;   // (the queries are not needed any more)
       const int rg = w.row0 + row, tokr = args.by_group.div(rg), hqr = w.hk * a.G + rg - tokr * a.G;
-      const float vunit = exp2i((int)vbase - kUnitExp), unit = bad ? nan : w.parts == 1 ? vunit / l : vunit;
+      const float vunit = exp2i((int)vbase - kUnitExp), unit = bad ? nan : w.parts == 1 && !SIDE ? vunit / l : vunit;
       if (good && part4 < D / 32) {
         const int c = part4;   // 32 channels
         uint32_t r[32];
         __syncwarp();
         tc::tmem_ld32(to + c * 32, r);
         tc::tmem_wait_ld();
-        if (w.parts > 1) {   // partial result: O (in units of 2^(m_end - kShift), as the sum), m_end and the sum, [channel][row]
+        if (w.parts > 1 || SIDE) {   // partial result: O (in units of 2^(m_end - kShift), as the sum), m_end and the sum, [channel][row]
           float* mine = a.part + ((int64_t)blockIdx.x * args.nsplit + blockIdx.y) * (D + 2) * 128;
 #pragma unroll
           for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row] = __uint_as_float(r[i]) * unit;
@@ -828,7 +805,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
       }
       tc::tc_fence_before();   // (O has been read: the next product may be issued behind the barriers to come)
-      if (w.parts == 1 && args.out_vec) {
+      if (w.parts == 1 && !SIDE && args.out_vec) {
         all_barrier();
         if (good) {
           constexpr int CPR = D / 8, RPI = 32 / CPR;
@@ -845,6 +822,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     }
     asm volatile("cp.async.wait_all;" ::: "memory");   // (queries of a work that is not begun, should a wait have run out)
   }
+  if constexpr (SIDE) asm volatile("griddepcontrol.wait;" ::: "memory");
   tc::tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -915,29 +893,41 @@ int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d) {
   return ns == 1 ? 0 : units * qt * ns * (d + 2) * 128 * 4;
 }
 
-template <int D, bool MORE>
+int64_t prompt_side_workspace(int64_t units, int64_t rows, int64_t tiles, int d) {
+  int qt, ns;
+  prompt_plan(units, rows, tiles, qt, ns);
+  return units * qt * ns * (d + 2) * 128 * 4;
+}
+
+template <int D, bool MORE, bool SIDE>
 static kvm_status_t launch_prompt_d(const PromptArgs& args, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};   // devices on which the limit has been raised
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    if (cudaFuncSetAttribute(prompt_kernel<D, MORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptCfg<D>::SMEM) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+    if (cudaFuncSetAttribute(prompt_kernel<D, MORE, SIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptCfg<D>::SMEM) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
     if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
-  prompt_kernel<D, MORE><<<dim3((unsigned)(args.units * args.qtiles), args.nsplit), kThreads, PromptCfg<D>::SMEM, s>>>(mapK, mapV, args);
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at; lc.numAttrs = 1; lc.stream = s;
+  if constexpr (SIDE) {   // (beside the end of the kernel over the shared blocks)
+    lc.gridDim = dim3((unsigned)(args.units * args.qtiles), args.nsplit); lc.blockDim = dim3(kThreads); lc.dynamicSmemBytes = PromptCfg<D>::SMEM;
+    if (cudaLaunchKernelEx(&lc, prompt_kernel<D, MORE, true>, mapK, mapV, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+    return KVM_OK;
+  }
+  prompt_kernel<D, MORE, SIDE><<<dim3((unsigned)(args.units * args.qtiles), args.nsplit), kThreads, PromptCfg<D>::SMEM, s>>>(mapK, mapV, args);
   if (args.nsplit > 1) {
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)(args.units * args.qtiles), D / 16); lc.blockDim = dim3(128); lc.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = at; lc.numAttrs = 1;
+    lc.gridDim = dim3((unsigned)(args.units * args.qtiles), D / 16); lc.blockDim = dim3(128);
     if (cudaLaunchKernelEx(&lc, prompt_combine_kernel<D>, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 
-kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s) {
+template <bool SIDE>
+static kvm_status_t launch_prompt8_any(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s, PromptSide& side) {
   PromptArgs args;
   args.a = a;
   args.units = a.p.batch * a.p.Hkv;
@@ -959,9 +949,18 @@ kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool
   // d = 128, without and with: window 128 193 -> 177 us, 512 239 -> 224, 2048 387 -> 384, 4096 524 -> 534, all 622 -> 641; d = 64 on 4 heads:
   // 144 -> 128, 192 -> 179, 326 -> 317, 453 -> 451, 548 -> 554).  Not where a merge waits for the grid.
   constexpr int kMoreTiles = 18;
+  side = PromptSide{args.qtiles, args.nsplit};
+  if constexpr (SIDE) return a.d == 128 ? launch_prompt_d<128, false, true>(args, mapK, mapV, s) : launch_prompt_d<64, false, true>(args, mapK, mapV, s);
   const bool more = args.nsplit == 1 && seen <= kMoreTiles && (int64_t)args.units * args.qtiles > 148;
-  if (a.d == 128) return more ? launch_prompt_d<128, true>(args, mapK, mapV, s) : launch_prompt_d<128, false>(args, mapK, mapV, s);
-  return more ? launch_prompt_d<64, true>(args, mapK, mapV, s) : launch_prompt_d<64, false>(args, mapK, mapV, s);
+  if (a.d == 128) return more ? launch_prompt_d<128, true, false>(args, mapK, mapV, s) : launch_prompt_d<128, false, false>(args, mapK, mapV, s);
+  return more ? launch_prompt_d<64, true, false>(args, mapK, mapV, s) : launch_prompt_d<64, false, false>(args, mapK, mapV, s);
+}
+kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s) {
+  PromptSide side;
+  return launch_prompt8_any<false>(a, tiles, q_vec, out_vec, s, side);
+}
+kvm_status_t launch_prompt8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, PromptSide& side) {
+  return launch_prompt8_any<true>(a, tiles, q_vec, true, s, side);
 }
 
 }  // namespace cache

@@ -1,0 +1,847 @@
+// Attention for a batch whose sequences share their first blocks in groups (a system prompt, a document, the samples or beams of one prompt):
+// every shared block is read, and multiplied with the queries of its whole group, once.
+//
+// Three launches.  shared_kernel: the rows of a group, (sequence, token, head of a kv head's group), over the group's shared blocks, all of which
+// all of them see.  The kernels of kvm_cache_attend in their SIDE builds: every sequence's rows over its own blocks.  shared_merge_kernel: partial
+// results (O, reference m and sum l of a row, over some of its keys) to out = sum_z 2^(m_z - m) O_z / sum_z 2^(m_z - m) l_z.
+//
+// shared_kernel.  A unit is a (group, kv head) and 256 of the group's rows, or what is left of them.  The key tiles (128 tokens) of all units form one
+// list, in which a tile of more than 128 rows counts twice; every CTA takes an equal, contiguous share of it, whatever the lengths and the sizes of
+// the groups are, and leaves one partial result per unit that it has tiles of.
+//     S = (q_hi + q_lo) K8^T   kind::f8f6f4: the codes as they lie in memory, q in two parts of e4m3
+//     O += P V16               kind::f16: P in fp16 from tensor memory, V16 = the codes of the values in fp16 (exact)
+// as in kvm_cache_prompt.cu, but with two streams of one S and one O each: of two row tiles on the same keys (a tile of values is converted once for
+// 256 rows), or of one row tile on the even and the odd key tiles.  A stream goes S, softmax, P V, S, ...; while one is in its softmax the other is in the
+// tensor core, and nothing is handed from stream to stream.  One thread per row, which reads S once: weights are computed with the reference so far and kept in
+// registers; only where a row's maximum lies more than 2^8 above it is the reference moved, O rescaled and the tile computed again.
+// Scales of values go into the exponents of the weights, relative to the largest of the share's blocks, and out of the row sums again.
+//   warp 0       producer of keys (TMA, page numbers and scales ahead), warp 3 of values
+//   warp 1       issues S, warp 2 issues P V (one thread each)
+//   warps 4-11   queries (scaled, split); softmax, thread = row; results
+//   warps 12-15  value codes -> fp16, swizzled as the MMA reads them
+#include <algorithm>
+#include <atomic>
+
+#include "kvm_cache.cuh"
+#include "kvm_internal.h"
+#include "tc_common.cuh"
+
+namespace kvm {
+namespace cache {
+
+bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page);   // kvm_cache.cu
+kvm_status_t attend_args(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale, int32_t window, int32_t sinks, void* out,
+                         const int64_t* q_strides, const int64_t* out_strides, int32_t* status, AttendArgs& a);
+
+namespace {
+
+constexpr int kCtas = 148;
+constexpr int kThreads = 512;
+constexpr int kInfo = 8;
+constexpr float kShift = 6.f;    // weights in units of 2^-6 of the reference (kvm_cache_prompt.cu)
+constexpr float kRaise = 8.f;    // a reference is moved when a maximum lies more than 2^8 above it: weights stay below 2^14
+
+struct SharedArgs {
+  AttendArgs a;
+  FastDiv by_seq, by_group;      // rows of a sequence, heads of a group
+  int seq_rows, grid, q_vec, out_vec;
+  float* part;                   // partial results of shared_kernel
+  // what the kernels over the other blocks leave: of few tokens (cols columns), of many (cols = 0)
+  const float* own;
+  int cols, workers;
+  PromptSide many;
+};
+
+// What there is to do: prefix sums over the groups, in shared memory.
+struct Plan {
+  const int *offsets, *pre, *rows;   // sequences, weight of the list, rows of the partial results before each group
+  int total, share;
+};
+// One unit, as a CTA sees it that begins at position f of the list and ends at most at `end`.
+struct Unit {
+  int g, hk, blocks, tiles;      // group, kv head; shared blocks, key tiles of the unit
+  int row0, n;                   // the unit's rows among the group's
+  int w, begin;                  // weight of a tile, position of the first one
+  int at;                        // rows of partial results before the unit's first
+  int pitch;                     // rows that a channel of a partial result takes
+  __device__ __forceinline__ bool tall() const { return w == 2; }
+  // tiles [jb, je) of the CTA whose share begins at w0
+  __device__ __forceinline__ void of(int w0, int share, int& jb, int& je) const {
+    jb = max(0, w0 - begin + w - 1) / w;
+    je = min(tiles, max(0, w0 + share - begin + w - 1) / w);
+  }
+  // where the partial result of that CTA (its number: cta) is: one step further in the list is one unit or one CTA further
+  __device__ __forceinline__ int64_t slot(int cta) const { return at + (int64_t)cta * 256; }
+};
+__device__ __forceinline__ int rows_of_group(const SharedArgs& s, const int* offsets, int g) { return (offsets[g + 1] - offsets[g]) * s.seq_rows; }
+// The shared blocks of a group (out of range: none, and the call is reported).
+__device__ __forceinline__ int blocks_of_group(const SharedArgs& s, int g) {
+  const int x = s.a.groups.shared[g];
+  return x >= 0 && x <= s.a.p.max_pages ? x : -1;
+}
+__device__ __forceinline__ int tiles_of(const Params& p, int blocks) { return (blocks + (kTile >> p.page_shift) - 1) >> (7 - p.page_shift); }
+__device__ __forceinline__ int pad8(int x) { return (x + 7) & ~7; }
+// weight of a unit of n rows per tile, rows of its partial results
+__device__ __forceinline__ int weight_of(int n) { return n > 128 ? 2 : 1; }
+__device__ __forceinline__ int space_of(int n) { return n > 128 ? 256 : 2 * pad8(n); }
+
+// The plan, by all NT threads of a block; mem: 3 (n_groups + 1) ints and a scratch of NT / 32 (two sums each).  false: groups that are none.
+template <int NT>
+__device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, int2* scratch, Plan& plan) {
+  const Groups& gr = s.a.groups;
+  const Params& p = s.a.p;
+  int *offsets = mem, *pre = offsets + gr.n + 1, *rows = pre + gr.n + 1;
+  plan.offsets = offsets; plan.pre = pre; plan.rows = rows;
+  plan.total = 0;
+  plan.share = 1;
+  if (!load_groups<NT>(gr, p.batch, offsets)) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
+    return false;
+  }
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = (gr.n + NT - 1) / NT, g0 = tid * per;
+  int2 sum = make_int2(0, 0);
+#pragma unroll 1
+  for (int g = g0; g < min(g0 + per, gr.n); ++g) {
+    pre[g] = sum.x;
+    rows[g] = sum.y;
+    const int n = rows_of_group(s, offsets, g), blocks = blocks_of_group(s, g);
+    if (blocks < 0 && blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
+    if (n > 0 && blocks > 0) {
+      const int full = n >> 8, left = n & 255;
+      sum.x += p.Hkv * tiles_of(p, blocks) * (2 * full + (left ? weight_of(left) : 0));
+      sum.y += p.Hkv * (256 * full + (left ? space_of(left) : 0));
+    }
+  }
+  int2 incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
+    if (lane >= o) { incl.x += x; incl.y += y; }
+  }
+  if (lane == 31) scratch[warp] = incl;
+  __syncthreads();
+  int2 add = make_int2(incl.x - sum.x, incl.y - sum.y);
+#pragma unroll 1
+  for (int w = 0; w < warp; ++w) { add.x += scratch[w].x; add.y += scratch[w].y; }
+#pragma unroll 1
+  for (int g = g0; g < min(g0 + per, gr.n); ++g) { pre[g] += add.x; rows[g] += add.y; }
+  if (tid == NT - 1) pre[gr.n] = add.x + sum.x;
+  __syncthreads();
+  plan.total = pre[gr.n];
+  plan.share = (plan.total + s.grid - 1) / s.grid;
+  return true;
+}
+// Last g with pre[g] <= f < pre[n].
+__device__ __forceinline__ int last_before(const int* pre, int n, int f) {
+  int lo = 0, hi = n;
+#pragma unroll 1
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (pre[mid] <= f) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+// The unit of rows 256 rb .. of a (group, kv head).
+__device__ __forceinline__ Unit unit_of(const SharedArgs& s, const Plan& plan, int g, int blocks, int hk, int rb) {
+  Unit u;
+  const int n = rows_of_group(s, plan.offsets, g), full = n >> 8, left = n & 255;
+  u.g = g; u.hk = hk; u.blocks = blocks;
+  u.tiles = tiles_of(s.a.p, blocks);
+  u.row0 = rb * 256;
+  u.n = min(256, n - u.row0);
+  u.w = weight_of(u.n);
+  u.pitch = u.w == 2 ? 128 : pad8(u.n);
+  u.begin = plan.pre[g] + u.tiles * (hk * (2 * full + (left ? weight_of(left) : 0)) + 2 * rb);
+  u.at = plan.rows[g] + hk * (256 * full + (left ? space_of(left) : 0)) + 256 * rb;
+  return u;
+}
+__device__ __forceinline__ Unit unit_at(const SharedArgs& s, const Plan& plan, int f) {
+  const int g = last_before(plan.pre, s.a.groups.n, f), blocks = blocks_of_group(s, g), tiles = tiles_of(s.a.p, blocks);
+  const int n = rows_of_group(s, plan.offsets, g), full = n >> 8, left = n & 255;
+  const int per = tiles * (2 * full + (left ? weight_of(left) : 0)), rest = f - plan.pre[g], hk = rest / per;
+  return unit_of(s, plan, g, blocks, hk, min(full, (rest - hk * per) / (2 * tiles)));
+}
+// A row of a group: its sequence, token and head (of the kv head's group).
+struct Row { int b, t, h; };
+__device__ __forceinline__ Row row_of(const SharedArgs& s, int b0, int r) {
+  Row x;
+  const int q = s.by_seq.div(r);
+  r -= q * s.seq_rows;
+  x.b = b0 + q;
+  x.t = s.by_group.div(r);
+  x.h = r - x.t * s.a.G;
+  return x;
+}
+
+struct alignas(16) KeyTile {
+  int flags;          // 1: some scale is NaN (or some page outside the pool)
+  int n;              // keys that are there
+  float ks[8], ve[8]; // per 16 keys: scale of the keys, exponent of the values' scale
+};
+
+enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 26, SB_PVDONE = 28, SB_QFULL = 30, SB_LAST = 31,
+       SB_VBASE = 32, SB_COUNT = 36 };
+
+template <int D>
+struct SharedCfg {
+  static constexpr int NK = 3 * (128 / D), NV8 = 2 * (128 / D), NV = 2;
+  static constexpr int T8 = 128 * D, T16 = 256 * D;
+  static constexpr int OFF_Q = 0;                        // [row tile] hi, lo
+  static constexpr int OFF_K = OFF_Q + 4 * T8;
+  static constexpr int OFF_V8 = OFF_K + NK * T8;
+  static constexpr int OFF_V = OFF_V8 + NV8 * T8;
+  static constexpr int OFF_INFO = OFF_V + NV * T16;
+  static constexpr int OFF_CQ = OFF_INFO + kInfo * (int)sizeof(KeyTile);   // float [2][128]
+  static constexpr int OFF_BAR = OFF_CQ + 2 * 128 * 4;
+  static constexpr int OFF_PLAN = OFF_BAR + 512;         // int [3][n_groups + 1]
+  // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
+  static int smem(int n_groups) { return std::max(OFF_PLAN + 12 * (n_groups + 1) + 1024, 120 * 1024); }
+  static constexpr uint32_t COL_S = 0, COL_O = 256;      // of stream s: + 128 s
+  static_assert(NK <= 6 && NV8 <= 4 && NK + 2 <= kInfo, "rings");
+  static_assert(OFF_K % 1024 == 0 && OFF_V8 % 1024 == 0 && OFF_V % 1024 == 0 && OFF_INFO % 16 == 0 && OFF_CQ % 16 == 0 && OFF_BAR % 8 == 0 && OFF_PLAN % 8 == 0, "alignment");
+  static_assert(SB_COUNT * 8 + 128 <= 512 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ SharedArgs args) {
+  using Cfg = SharedCfg<D>;
+  const AttendArgs& a = args.a;
+  const Params& p = a.p;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  KeyTile* info = reinterpret_cast<KeyTile*>(base + Cfg::OFF_INFO);
+  float* s_cq = reinterpret_cast<float*>(base + Cfg::OFF_CQ);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base + Cfg::OFF_BAR);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + SB_COUNT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);                  // [segment % 4][4]
+  volatile uint32_t* s_there = reinterpret_cast<uint32_t*>(s_vmax + 16); // [value tile of the ring]: pages that were loaded
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (who waits for this kernel does so before reading what it wrote)
+  if (warp == 0) {
+    for (int i = lane; i < SB_COUNT; i += 32) {
+      auto in = [&](int first, int n) { return i >= first && i < first + n; };
+      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_PREADY, 2) || in(SB_VBASE, 4) ? 4 : in(SB_QFULL, 1) ? 8 : 1);
+    }
+    if (lane == 0) {
+      tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
+      *abort_flag = 0;
+    }
+    tc::fence_barrier_init();
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_relinquish();
+  }
+  tc::tc_fence_before();
+  Plan plan;
+  const bool planned = make_plan<kThreads>(args, reinterpret_cast<int*>(base + Cfg::OFF_PLAN), reinterpret_cast<int2*>(base), plan);   // (scratch: where the queries go)
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int w0 = planned ? min(plan.total, (int)blockIdx.x * plan.share) : 0, w1 = planned ? min(plan.total, w0 + plan.share) : 0;
+  auto fail = [&]() {
+    if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
+    *abort_flag = 1;
+  };
+  // The CTA's segments: (unit, key tiles).  Every warp walks them by itself.
+  struct Segment { Unit u; int jb, n; };
+  auto next_segment = [&](int& f, Segment& g) {
+    while (f < w1) {
+      g.u = unit_at(args, plan, f);
+      int je;
+      g.u.of(w0, plan.share, g.jb, je);
+      g.n = je - g.jb;
+      f = g.u.begin + g.u.tiles * g.u.w;
+      if (g.n > 0) return true;
+    }
+    return false;
+  };
+  const int tshift = 7 - p.page_shift, ppt = 1 << tshift;
+  Segment g;
+  int f = w0;
+  if (warp < 4) {
+    if (warp == 0 || warp == 3) {
+      // ------------------------------ producers of keys (warp 0) and values (warp 3) ------------------------------
+      const bool keys = warp == 0;
+      const int ring = keys ? Cfg::NK : Cfg::NV8, full = keys ? SB_KFULL : SB_V8FULL, empty = keys ? SB_KFREE : SB_V8FREE;
+      const CUtensorMap* map = keys ? &mapK : &mapV;
+      uint8_t* tiles = base + (keys ? Cfg::OFF_K : Cfg::OFF_V8);
+      const int tpb = 32 >> tshift, lt = lane >> tshift, lp = lane & (ppt - 1);   // tiles whose pages the warp's lanes hold at a time
+      struct Page { int row, ke, ve; };   // row < 0: not loaded
+      bool ok = true;
+      int s = 0, issued = 0;
+      uint32_t par = 0;
+#pragma unroll 1
+      while (ok && next_segment(f, g)) {
+        const int32_t* table = p.pages + (int64_t)plan.offsets[g.u.g] * p.max_pages;
+        auto fetch = [&](int k) {
+          Page x{-1, 0, 0};
+          const int j = k * tpb + lt, block = (g.jb + j) * ppt + lp;
+          if (j < g.n && block < g.u.blocks) {
+            const int page = table[block];
+            if (page < 0 || page >= p.n_pages) {
+              report(p.status, KVM_ERR_INVALID_ARG);
+              x.ke = x.ve = 128;
+            } else {
+              const int unit = page * p.Hkv + g.u.hk;
+              x.row = unit * p.page;
+              x.ke = scale_exp(p.ks[unit]);
+              x.ve = scale_exp(p.vs[unit]);
+            }
+          }
+          return x;
+        };
+        Page cur{}, nxt{};
+        for (int j = 0, ahead = 0, t = tpb; j < g.n; ++j) {   // (ahead: batches of pages fetched; t: tiles of the current one that are issued)
+          if (t == tpb) {
+            t = 0;
+#pragma unroll 1
+            do { cur = nxt; nxt = fetch(ahead++); } while (ahead < 2);   // (one batch is always on its way)
+          }
+          if (lane == 0) ok = issued < ring || tc::mbar_wait_tight(&bars[empty + s], par ^ 1);
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) break;
+          const bool mine = lt == t, nan = cur.ke > 127 || cur.ve > 127;
+          const uint32_t loads = __ballot_sync(0xffffffffu, mine && cur.row >= 0);
+          const uint32_t nans = __ballot_sync(0xffffffffu, mine && nan);
+          if (mine && keys) {
+            KeyTile& ti = info[issued % kInfo];
+            if (lp == 0) {
+              ti.flags = nans ? 1 : 0;
+              ti.n = min(kTile, (g.u.blocks - (g.jb + j) * ppt) << p.page_shift);
+            }
+            for (int i = 0; i < p.page / 16; ++i) {
+              ti.ks[lp * (p.page / 16) + i] = nan ? 1.f : exp2i(cur.ke);   // (rows of a NaN are marked, not computed with)
+              ti.ve[lp * (p.page / 16) + i] = nan ? 0.f : (float)cur.ve;
+            }
+          } else if (mine && lp == 0) {
+            s_there[s] = loads >> lane;
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_expect_tx(&bars[full + s], __popc(loads) * p.page * D);
+          __syncwarp();
+          if (mine && cur.row >= 0) tc::tma_load_2d(tiles + s * Cfg::T8 + lp * p.page * D, map, &bars[full + s], 0, cur.row);
+          ++issued;
+          if (++s == ring) { s = 0; par ^= 1; }
+          ++t;
+        }
+      }
+      if (lane == 0) {
+        if (!ok) fail();
+        // nothing may be in flight into shared memory when the CTA ends, whatever became of the others
+#pragma unroll 1
+        for (int j = max(0, issued - ring); j < issued; ++j) tc::mbar_wait_tight(&bars[full + j % ring], (j / ring) & 1);
+      }
+    } else if (warp == 1) {
+      // ------------------------------ S ------------------------------
+      if (lane == 0) {
+        constexpr uint32_t ID = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
+        auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
+        const uint64_t dQ0 = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
+        bool ok = true;
+        int it[2] = {0, 0};   // tiles of the streams so far
+        uint32_t s = 0, par = 0;
+#pragma unroll 1
+        for (int seg = 0; ok && next_segment(f, g); ++seg) {
+          ok = tc::mbar_wait_tight(&bars[SB_QFULL], seg & 1);
+          const bool tall = g.u.tall();
+#pragma unroll 1
+          for (int j = 0; j < g.n && ok; ++j) {
+            ok = tc::mbar_wait_tight(&bars[SB_KFULL + s], par);
+            const uint64_t k = dK + s * (Cfg::T8 >> 4);
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+              if (!ok || (!tall && st != (j & 1))) continue;
+              if (it[st] > 0) ok = tc::mbar_wait_tight(&bars[SB_PVDONE + st], (it[st] - 1) & 1);   // (its weights lie where S goes)
+              if (!ok) continue;
+              ++it[st];
+              tc::tc_fence_after();
+              const uint64_t dQ = dQ0 + (tall ? st : 0) * (2 * Cfg::T8 >> 4);
+              const uint32_t dS = tmem + Cfg::COL_S + 128 * st;
+#pragma unroll
+              for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + 2 * ks, k + 2 * ks, ID, ks > 0);
+#pragma unroll
+              for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID, 1u);
+              tc::mma_commit(&bars[SB_SFULL + st]);
+            }
+            tc::mma_commit(&bars[SB_KFREE + s]);
+            if (++s == Cfg::NK) { s = 0; par ^= 1; }
+          }
+        }
+        if (!ok) fail();
+      }
+    } else if (lane == 0) {
+      // ------------------------------ P V ------------------------------
+      constexpr uint32_t ID = tc::idesc_f16(128, D, true);
+      const uint64_t dV = tc::smem_desc_sw128(tc::smem_u32(base + Cfg::OFF_V), 128 * 128, 1024);
+      bool ok = true;
+      int it[2] = {0, 0}, J = 0;
+#pragma unroll 1
+      while (ok && next_segment(f, g)) {
+        const bool tall = g.u.tall();
+#pragma unroll 1
+        for (int j = 0; j < g.n && ok; ++j, ++J) {
+          ok = tc::mbar_wait_tight(&bars[SB_VFULL + (J & 1)], (J >> 1) & 1);
+          const uint64_t v = dV + (J & 1) * (Cfg::T16 >> 4);
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            if (!ok || (!tall && st != (j & 1))) continue;
+            ok = tc::mbar_wait_tight(&bars[SB_PREADY + st], it[st] & 1);
+            if (!ok) continue;
+            ++it[st];
+            tc::tc_fence_after();
+            const bool first = j < (tall ? 1 : 2);
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
+              tc::mma_f16_ts(tmem + Cfg::COL_O + 128 * st, tmem + Cfg::COL_S + 128 * st + 8 * kk, v + kk * (2048 >> 4), ID, (!first || kk > 0) ? 1u : 0u);
+            tc::mma_commit(&bars[SB_PVDONE + st]);
+          }
+          tc::mma_commit(&bars[SB_VFREE + (J & 1)]);
+        }
+        if (ok) tc::mma_commit(&bars[SB_LAST]);
+      }
+      if (!ok) fail();
+    }
+  } else if (warp >= 12) {
+    // ------------------------------ values to fp16 ------------------------------
+    constexpr int PIECES = D / 16, N = PIECES / 4;   // 16-byte pieces of a row of codes; a warp's lanes take eight rows and four pieces at a time
+    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 12) * 32;
+    bool ok = true;
+    int J = 0;
+#pragma unroll 1
+    for (int seg = 0; ok && next_segment(f, g); ++seg) {
+      {   // largest exponent of the values' scales
+        const int32_t* table = p.pages + (int64_t)plan.offsets[g.u.g] * p.max_pages;
+        int v = -1000;
+#pragma unroll 1
+        for (int i = g.jb * ppt + tid - 384; i < min((g.jb + g.n) * ppt, g.u.blocks); i += 128) {
+          const int page = table[i];
+          if (page < 0 || page >= p.n_pages) continue;
+          const int e = scale_exp(p.vs[page * p.Hkv + g.u.hk]);
+          if (e < 128) v = max(v, e);
+        }
+        v = __reduce_max_sync(0xffffffffu, v);
+        if (lane == 0) {
+          // (four sets: with a tile of segment X to come, that of X - 3 has at least been used)
+          s_vmax[4 * (seg & 3) + warp - 12] = v;
+          tc::mbar_arrive(&bars[SB_VBASE + (seg & 3)]);
+        }
+      }
+#pragma unroll 1
+      for (int j = 0; j < g.n; ++j, ++J) {
+        const int sv = J & 1, s8 = J % Cfg::NV8;
+        bool good = tc::mbar_wait_tight(&bars[SB_V8FULL + s8], (J / Cfg::NV8) & 1);
+        if (good && J >= 2) good = tc::mbar_wait_tight(&bars[SB_VFREE + sv], ((J >> 1) - 1) & 1);
+        ok = __all_sync(0xffffffffu, good);
+        if (!ok) break;
+        const uint32_t there = s_there[s8];
+        const uint8_t* src = base + Cfg::OFF_V8 + s8 * Cfg::T8;
+        uint8_t* dst = base + Cfg::OFF_V + sv * Cfg::T16;
+        uint4 c[4 * N];
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) {
+          const int r = rows0 + 8 * (i / N) + r8, pc = pc0 + 4 * (i % N);
+          c[i] = *reinterpret_cast<const uint4*>(src + r * D + (D == 128 ? (pc ^ r8) : (pc ^ ((r8 >> 1) & 3))) * 16);
+        }
+        if (there != (1u << ppt) - 1) {   // whatever the ring holds there must not meet the weight 0
+#pragma unroll
+          for (int i = 0; i < 4 * N; ++i)
+            if (!(there >> ((rows0 + 8 * (i / N) + r8) >> p.page_shift) & 1)) c[i] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) {
+          const int r = rows0 + 8 * (i / N) + r8, pc = pc0 + 4 * (i % N);
+          uint4 lo, hi;
+          lo.x = e4m3x2_to_f16x2(c[i].x & 0xffff); lo.y = e4m3x2_to_f16x2(c[i].x >> 16); lo.z = e4m3x2_to_f16x2(c[i].y & 0xffff); lo.w = e4m3x2_to_f16x2(c[i].y >> 16);
+          hi.x = e4m3x2_to_f16x2(c[i].z & 0xffff); hi.y = e4m3x2_to_f16x2(c[i].z >> 16); hi.z = e4m3x2_to_f16x2(c[i].w & 0xffff); hi.w = e4m3x2_to_f16x2(c[i].w >> 16);
+          uint8_t* at = dst + (pc >> 2) * (128 * 128) + r * 128;
+          *reinterpret_cast<uint4*>(at + (((2 * (pc & 3)) ^ r8) << 4)) = lo;
+          *reinterpret_cast<uint4*>(at + (((2 * (pc & 3) + 1) ^ r8) << 4)) = hi;
+        }
+        tc::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          tc::mbar_arrive(&bars[SB_VFULL + sv]);
+          tc::mbar_arrive(&bars[SB_V8FREE + s8]);
+        }
+      }
+    }
+    if (!ok && lane == 0) fail();
+  } else {
+    // ------------------------------ q; softmax; results ------------------------------
+    const int st = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), tS = lanes + Cfg::COL_S + 128 * st, tO = lanes + Cfg::COL_O + 128 * st;
+    auto rows_barrier = []() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+    bool ok = true;
+    int it = 0, J0 = 0;   // tiles of this stream, of the CTA
+#pragma unroll 1
+    for (int seg = 0; next_segment(f, g); ++seg) {
+      const bool tall = g.u.tall();
+      const int b0 = plan.offsets[g.u.g];
+      {
+        // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys; D / 16 threads per row
+        constexpr int TPR = D / 16;
+        const int items = (tall ? 256 : 128) * TPR;
+#pragma unroll 2
+        for (int i = tid - 128; i < items; i += 256) {
+          const int r = i / TPR, piece = i % TPR;
+          uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          if (r < g.u.n) {
+            const Row rw = row_of(args, b0, g.u.row0 + r);
+            const __nv_bfloat16* src = a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
+            if (args.q_vec) {
+              const uint4 u = *reinterpret_cast<const uint4*>(src), v = *reinterpret_cast<const uint4*>(src + 8);
+              x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = (uint32_t)__bfloat16_as_ushort(src[2 * e]) | ((uint32_t)__bfloat16_as_ushort(src[2 * e + 1]) << 16);
+            }
+          }
+          uint32_t top2 = 0;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) top2 = __vmaxu2(top2, x[q] & 0x7fff7fffu);
+          uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+#pragma unroll
+          for (int o = 1; o < TPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const bool nan = top >= 0x7f80u;
+          const int e = max((int)(top >> 7), 10);
+          const float mul = nan ? 0.f : exp2i(134 - e);
+          uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const uint32_t v = nan ? 0u : x[q];
+            uint32_t h, l;
+            split_e4m3x2(__uint_as_float(v << 16) * mul, __uint_as_float(v & 0xffff0000u) * mul, h, l);
+            hi[q >> 1] |= h << (16 * (q & 1));
+            lo[q >> 1] |= l << (16 * (q & 1));
+          }
+          uint8_t* at = base + Cfg::OFF_Q + (r >> 7) * 2 * Cfg::T8 + (r & 127) * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
+          *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          if (piece == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
+        }
+        tc::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars[SB_QFULL]);
+        rows_barrier();
+      }
+      float cq = s_cq[(tall ? 128 * st : 0) + row];
+      bool bad = !(cq == cq);   // NaN rows are marked, not computed with
+      if (bad) cq = 0.f;
+      ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_VBASE + (seg & 3)], (seg >> 2) & 1));
+      const int* vm = s_vmax + 4 * (seg & 3);
+      const int vb = max(max(vm[0], vm[1]), max(vm[2], vm[3])), vbase = vb == -1000 ? 0 : vb;
+      float m = -INFINITY, l = 0.f;   // l in units of 2^(m - kShift)
+      const int step = tall ? 1 : 2;
+#pragma unroll 1
+      for (int j = tall ? 0 : st; j < g.n && ok; j += step, ++it) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SFULL + st], it & 1));
+        if (!ok) break;
+        tc::tc_fence_after();
+        const KeyTile& ti = info[(J0 + j) % kInfo];
+        if (ti.flags) bad = true;
+        const int n = ti.n;
+        uint32_t pr[2][32];   // weights, two to a word
+        float sum = 0.f;
+#pragma unroll 1
+        for (int turn = 0; turn < 2; ++turn) {
+          const float neg_m = m == -INFINITY ? 0.f : kShift - m;
+          float mx = -INFINITY;
+          sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t x[32];
+            tc::tmem_ld32(tS + 32 * c, x);
+            tc::tmem_wait_ld();
+            if (n < kTile) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = 32 * c + i < n ? x[i] : 0xff800000u;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float fac = fmaxf(cq * ti.ks[2 * c + h], 1.17549435e-38f), vr = ti.ve[2 * c + h] - (float)vbase, fold = fmaxf(vr, -(float)kFoldMost);   // (never 0: a masked column is -inf)
+              const uint64_t f2 = pack2(fac, fac), a2 = pack2(neg_m + fold, neg_m + fold);
+              uint64_t s0 = 0, s1 = 0;
+              float m0 = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float x0 = __uint_as_float(x[16 * h + 2 * i]), x1 = __uint_as_float(x[16 * h + 2 * i + 1]);
+                m0 = tc::fmax3(m0, x0, x1);
+                float p0, p1;
+                unpack2(fma2(pack2(x0, x1), f2, a2), p0, p1);
+                p0 = tc::ex2_approx(p0);
+                p1 = tc::ex2_approx(p1);
+                const uint64_t p2 = pack2(p0, p1);
+                if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
+                pr[c >> 1][16 * (c & 1) + 8 * h + i] = vr < fold ? 0u : to_f16x2(p0, p1);
+              }
+              float l0, l1;
+              unpack2(add2(s0, s1), l0, l1);
+              sum = fmaf(l0 + l1, exp2i(-(int)fold), sum);
+              mx = fmaxf(mx, fmaf(m0, fac, fold));
+            }
+          }
+          if (!__any_sync(0xffffffffu, mx > m + kRaise)) break;   // (m = -inf: the first tile)
+          // the reference moves; all earlier products of the stream have landed: its S is there
+          const float mnew = fmaxf(m, mx), corr = m == -INFINITY ? 0.f : tc::ex2_approx(m - mnew);
+          if (j >= step) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t r[32];
+              tc::tmem_ld32(tO + c * 32, r);
+              tc::tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+              tc::tmem_st32(tO + c * 32, r);
+            }
+            tc::tmem_wait_st();
+          }
+          l *= corr;
+          m = mnew;
+        }
+        l += sum;
+        tc::tmem_st32(tS, pr[0]);   // (columns that the warp has read)
+        tc::tmem_st32(tS + 32, pr[1]);
+        tc::tmem_wait_st();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bars[SB_PREADY + st]);
+      }
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_LAST], seg & 1));
+      tc::tc_fence_after();
+      const bool any = g.n > (tall ? 0 : st);   // (the odd stream may have had no tile)
+      float* mine = args.part + (g.u.slot(blockIdx.x) + st * g.u.pitch) * (D + 2);
+      const int rg = (tall ? 128 * st : 0) + row;
+      const float nan = __int_as_float(0x7fc00000), unit = bad ? nan : exp2i(vbase - kUnitExp);
+      const bool live = ok && rg < g.u.n;
+      if (any) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t r[32];
+          tc::tmem_ld32(tO + c * 32, r);
+          tc::tmem_wait_ld();
+          if (live) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * g.u.pitch + row] = __uint_as_float(r[i]) * unit;
+          }
+        }
+      }
+      if (live) {
+        mine[D * g.u.pitch + row] = any ? m - kShift : -INFINITY;
+        mine[(D + 1) * g.u.pitch + row] = !any ? 0.f : bad ? nan : l;
+      }
+      tc::tc_fence_before();   // (O has been read: the next product may be issued behind the barriers to come)
+      J0 += g.n;
+      {
+        uint32_t r;   // whether all are well, and so whether there is a next time: the same for all
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.u32 p, %1, 0;\n\t"
+            "barrier.cta.red.and.aligned.pred q, 1, 256, p;\n\t"
+            "selp.u32 %0, 1, 0, q;\n\t}"
+            : "=r"(r) : "r"(ok && !*abort_flag ? 1u : 0u) : "memory");
+        ok = r != 0;
+      }
+      if (!ok) break;
+    }
+    if (!ok) fail();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+// Merge: thread = row (b, t, head of the kv head's group), block (128 rows, CH channels, kv head).
+template <int D, int CH>
+__global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant__ SharedArgs s) {
+  extern __shared__ int s_plan[];
+  __shared__ int2 scratch[4];
+  const AttendArgs& a = s.a;
+  const Params& p = a.p;
+  Plan plan;
+  const bool planned = make_plan<128>(s, s_plan, scratch, plan);
+  const int r = blockIdx.x * 128 + threadIdx.x, c0 = blockIdx.y * CH, hk = blockIdx.z;
+  int start, n = 0;
+  Row rw{0, 0, 0};
+  Unit u;
+  u.tiles = 0;
+  int row = 0, blocks = 0;
+  bool live = planned && r < p.batch * s.seq_rows;
+  if (live) {
+    rw = row_of(s, 0, r);
+    const int g = last_before(plan.offsets, a.groups.n, rw.b);
+    blocks = blocks_of_group(s, g);
+    live = shared_lengths(p, rw.b, blocks, start, n) && rw.t < n;
+    if (live && blocks > 0) {
+      row = r - plan.offsets[g] * s.seq_rows;
+      u = unit_of(s, plan, g, blocks, hk, row >> 8);
+      row &= 255;
+    }
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!live) return;
+  float m = -INFINITY, l = 0.f, o[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) o[i] = 0.f;
+  auto add = [&](const float* x, int64_t step, int64_t at_m, int64_t at_l, float below) {   // a partial result: channel i at x[i * step], m, l
+    const float mz = x[at_m] - below, lz = x[at_l];
+    float v[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) v[i] = x[i * step];
+    if (mz == -INFINITY && lz == lz) return;   // (nothing was looked at there)
+    const float mn = fmaxf(m, mz), f0 = m == -INFINITY ? 0.f : tc::ex2_approx(m - mn), f1 = mz == -INFINITY ? 0.f : tc::ex2_approx(mz - mn);
+    l = lz == lz ? fmaf(l, f0, lz * f1) : lz;   // (a NaN row stays one where its weight is 0)
+#pragma unroll
+    for (int i = 0; i < CH; ++i) o[i] = fmaf(o[i], f0, v[i] * f1);
+    m = mn;
+  };
+  // the shared blocks
+  if (u.tiles > 0) {
+    const int64_t ch = (int64_t)c0 * u.pitch;
+    const int rr = row & (u.tall() ? 127 : 255);
+    for (int cta = u.begin / plan.share; cta <= (u.begin + u.tiles * u.w - 1) / plan.share; ++cta) {
+      int jb, je;
+      u.of(cta * plan.share, plan.share, jb, je);
+      if (jb >= je) continue;
+      const float* x = s.part + (u.slot(cta) + (u.tall() && row >= 128 ? u.pitch : 0)) * (D + 2) + rr;
+      add(x + ch, u.pitch, (int64_t)(D - c0) * u.pitch, (int64_t)(D + 1 - c0) * u.pitch, 0.f);
+      if (!u.tall()) {
+        x += (int64_t)u.pitch * (D + 2);
+        add(x + ch, u.pitch, (int64_t)(D - c0) * u.pitch, (int64_t)(D + 1 - c0) * u.pitch, 0.f);
+      }
+    }
+  }
+  // the sequence's own
+  const int64_t unit = (int64_t)rw.b * p.Hkv + hk;
+  const int col = rw.t * a.G + rw.h;
+  if (s.cols == 0) {
+    const int qt = col >> 7, row0 = qt * 128, last = min(n * a.G, row0 + 128) - 1;   // (as prompt_work has it)
+    const int tiles = pages_of(p, start + s.by_group.div(row0), start + s.by_group.div(last), INT32_MAX, 0, blocks).tiles, per = split_tiles(tiles, s.many.nsplit);
+    const float* x = s.own + ((int64_t)(s.many.qtiles - 1 - qt) * p.batch * p.Hkv + unit) * s.many.nsplit * (D + 2) * 128 + (col & 127);
+    for (int jb = 0; jb < tiles; jb += per, x += (D + 2) * 128) add(x + c0 * 128, 128, (D - c0) * 128, (D + 1 - c0) * 128, kShift);
+  } else if (const int2 from = a.found[unit]; from.y < 0) {
+    add(a.side + (unit * s.cols + col) * (D + 2) + c0, 1, D - c0, D + 1 - c0, 8.f);
+  } else {
+    const int z0 = max(0, from.x), z1 = min(from.y, s.workers - 1);   // (what a call leaves whose waits ran out may be anything)
+    for (int z = z0; z <= z1; ++z) add(s.own + ((int64_t)(2 * z + (z == z0)) * s.cols + col) * (D + 2) + c0, 1, D - c0, D + 1 - c0, 8.f);
+  }
+  __nv_bfloat16* out = a.out + rw.b * a.so[0] + (int64_t)(hk * a.G + rw.h) * a.so[1] + rw.t * a.so[2] + c0;
+  const float inv = 1.f / l;
+  __nv_bfloat162 h[CH / 2];
+#pragma unroll
+  for (int i = 0; i < CH / 2; ++i) h[i] = __floats2bfloat162_rn(o[2 * i] * inv * exp2i(kUnitExp), o[2 * i + 1] * inv * exp2i(kUnitExp));
+  if (s.out_vec) {
+#pragma unroll
+    for (int i = 0; i < CH / 8; ++i) reinterpret_cast<uint4*>(out)[i] = reinterpret_cast<const uint4*>(h)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) { out[2 * i] = h[i].x; out[2 * i + 1] = h[i].y; }
+  }
+}
+
+// ---- arguments ----
+
+struct Space {
+  int64_t part, own, side, found, all;   // bytes
+};
+int64_t align16(int64_t x) { return (x + 15) & ~(int64_t)15; }
+// Sizes of what a call leaves; false: beyond what is numbered in 32 bits.
+bool space_of_call(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t n_groups, int32_t n_q_heads, Space& x) {
+  const int64_t Hkv = c->n_kv_heads, G = n_q_heads / Hkv, B = call->batch, units = B * Hkv, cols = call->n_tokens * G, d = c->head_dim;
+  const int64_t tiles = ((int64_t)call->max_pages * c->page_tokens + kTile - 1) / kTile;
+  const int64_t rows = B * cols;
+  if (rows > INT32_MAX / 4 || (rows / 256 + n_groups) * 2 * Hkv * tiles > INT32_MAX / 2) return false;
+  const int64_t slots = Hkv * (2 * rows + 16 * (int64_t)n_groups) + 256 * (kCtas + 1);
+  if (slots > INT32_MAX / 2) return false;
+  x.part = align16(slots * (d + 2) * 4);
+  const bool few = cols <= kDecodeCols;
+  x.own = align16(few ? decode_workspace(units, tiles, (int)d, (int)cols) : prompt_side_workspace(units, cols, tiles, (int)d));
+  x.side = few ? align16(units * (cols <= 8 ? 8 : 16) * (d + 2) * 4) : 0;
+  x.found = few ? align16(units * 8) : 0;
+  x.all = x.part + x.own + x.side + x.found;
+  return true;
+}
+
+template <int D>
+kvm_status_t launch_shared(const SharedArgs& args, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};   // devices on which the limit has been raised
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (cudaFuncSetAttribute(shared_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SharedCfg<D>::smem(kMaxBatch)) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+    if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  shared_kernel<D><<<args.grid, kThreads, SharedCfg<D>::smem(args.a.groups.n), s>>>(mapK, mapV, args);
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+template <int D>
+kvm_status_t launch_merge(const SharedArgs& args, cudaStream_t s) {
+  constexpr int CH = 16;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at; lc.numAttrs = 1; lc.stream = s;
+  lc.gridDim = dim3((unsigned)((args.a.p.batch * (int64_t)args.seq_rows + 127) / 128), D / CH, args.a.p.Hkv); lc.blockDim = dim3(128);
+  lc.dynamicSmemBytes = 12 * (args.a.groups.n + 1);
+  if (cudaLaunchKernelEx(&lc, shared_merge_kernel<D, CH>, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
+  return KVM_OK;
+}
+
+}  // namespace
+}  // namespace cache
+}  // namespace kvm
+
+using namespace kvm;
+using namespace kvm::cache;
+
+#define KVM_API __attribute__((visibility("default")))
+
+extern "C" {
+
+KVM_API int64_t kvm_cache_shared_workspace(const kvm_cache_t* cache, const kvm_cache_call_t* call, int32_t n_groups, int32_t n_q_heads) {
+  if (kvm_cache_workspace(cache, call, n_q_heads) < 0 || n_groups < 1 || n_groups > call->batch) return -1;
+  Space x;
+  return space_of_call(cache, call, n_groups, n_q_heads, x) ? x.all : -1;
+}
+
+KVM_API kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm_cache_call_t* call, const int32_t* groups, const int32_t* shared, int32_t n_groups,
+                                             const void* q, int32_t n_q_heads, float scale, void* out, const int64_t* q_strides, const int64_t* out_strides,
+                                             void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream) {
+  SharedArgs args = {};
+  const kvm_status_t rc = attend_args(cache, call, q, n_q_heads, scale, 0, 0, out, q_strides, out_strides, status, args.a);
+  if (rc != KVM_OK) return rc;
+  if (!groups || !shared || !aligned(groups, 4) || !aligned(shared, 4) || n_groups < 1 || n_groups > call->batch) return KVM_ERR_INVALID_ARG;
+  AttendArgs& a = args.a;
+  Space x;
+  if (!space_of_call(cache, call, n_groups, n_q_heads, x)) return KVM_ERR_UNSUPPORTED;
+  if (!workspace || !aligned(workspace, 16)) return KVM_ERR_INVALID_ARG;
+  if (workspace_bytes < x.all) return KVM_ERR_CAPACITY;
+  uint8_t* ws = (uint8_t*)workspace;
+  args.part = (float*)ws;
+  args.own = a.part = (float*)(ws + x.part);
+  a.side = (float*)(ws + x.part + x.own);
+  a.found = (int2*)(ws + x.part + x.own + x.side);
+  a.groups = Groups{groups, shared, n_groups};
+  args.seq_rows = (int)(a.p.T * a.G);
+  args.cols = args.seq_rows <= 8 ? 8 : args.seq_rows <= kDecodeCols ? 16 : 0;
+  args.by_seq = FastDiv(args.seq_rows); args.by_group = FastDiv(a.G);
+  args.q_vec = rows_aligned(q, a.sq); args.out_vec = rows_aligned(out, a.so);
+  const int64_t tiles = ((int64_t)a.p.max_pages * a.p.page + kTile - 1) / kTile, rows = (int64_t)a.p.batch * args.seq_rows;
+  args.grid = (int)std::min<int64_t>(kCtas, (rows / 256 + n_groups) * 2 * a.p.Hkv * tiles);
+  CUtensorMap mapK, mapV;
+  const int64_t pool = a.p.n_pages * a.p.Hkv * a.p.page;
+  if (!encode_tmap_codes(&mapK, a.p.k, a.d, pool, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, pool, a.p.page)) return KVM_ERR_CUDA;
+  cudaStream_t s = (cudaStream_t)cuda_stream;
+  kvm_status_t r = a.d == 128 ? launch_shared<128>(args, mapK, mapV, s) : launch_shared<64>(args, mapK, mapV, s);
+  if (r == KVM_OK) r = args.cols ? launch_decode8_side(a, tiles, args.q_vec, s, args.workers) : launch_prompt8_side(a, tiles, args.q_vec, s, args.many);
+  if (r == KVM_OK) r = a.d == 128 ? launch_merge<128>(args, s) : launch_merge<64>(args, s);
+  return r;
+}
+
+}  // extern "C"

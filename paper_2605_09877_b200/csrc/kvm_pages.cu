@@ -188,6 +188,23 @@ KVM_API kvm_status_t kvm_pages_table(const kvm_pages_t* p, int32_t seq, int32_t*
   return KVM_OK;
 }
 
+KVM_API kvm_status_t kvm_pages_shared(const kvm_pages_t* p, const int32_t* seqs, int64_t n, int64_t n_tokens, int32_t* n_blocks) {
+  if (!p || !seqs || n < 1 || n_tokens < 0 || !n_blocks) return KVM_ERR_INVALID_ARG;
+  kvm_pages_t* book = const_cast<kvm_pages_t*>(p);
+  int64_t common = INT64_MAX;
+  const kvm_pages::Seq* first = book->seq(seqs[0]);
+  for (int64_t i = 0; i < n; ++i) {
+    const kvm_pages::Seq* s = book->seq(seqs[i]);
+    if (!s) return KVM_ERR_INVALID_ARG;
+    common = std::min(common, std::max<int64_t>(0, s->tokens - n_tokens) / p->page_tokens);   // (a block in progress is one's own as soon as it is written)
+    int64_t k = 0;
+    while (k < common && s->table[k] >= 0 && s->table[k] == first->table[k]) ++k;
+    common = k;
+  }
+  *n_blocks = (int32_t)common;
+  return KVM_OK;
+}
+
 KVM_API kvm_status_t kvm_pages_info(const kvm_pages_t* p, int64_t* n_free, int64_t* high) {
   if (!p) return KVM_ERR_INVALID_ARG;
   if (n_free) *n_free = p->n_free;

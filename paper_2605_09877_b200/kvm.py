@@ -31,6 +31,7 @@ EXPORTS = ["kvm_plan_capacity", "kvm_state_create", "kvm_prefill", "kvm_decode_s
            "kvm_debug_decode_plan", "kvm_debug_decode_ahead", "kvm_debug_apply_plan", "kvm_debug_attention_plan",
            "kvm_debug_drop_exchange",
            "kvm_rope_frequencies", "kvm_qk_norm_rope", "kvm_cache_ingest", "kvm_cache_read",
+           "kvm_cache_attend_shared", "kvm_cache_shared_workspace", "kvm_pages_shared",
            "kvm_cache_append", "kvm_cache_attend", "kvm_cache_workspace", "kvm_cache_copy_pages",
            "kvm_pages_create", "kvm_pages_destroy", "kvm_pages_open", "kvm_pages_fork", "kvm_pages_close", "kvm_pages_extend",
            "kvm_pages_trim", "kvm_pages_compact", "kvm_pages_table", "kvm_pages_info"]
@@ -166,6 +167,12 @@ def _load():
     L.kvm_cache_attend.argtypes = [cd, cc, vp, C.c_int32, C.c_float, C.c_int32, C.c_int32, vp, i64p, i64p, vp, C.c_int64, vp, vp]
     L.kvm_cache_workspace.restype = C.c_int64
     L.kvm_cache_workspace.argtypes = [cd, cc, C.c_int32]
+    L.kvm_cache_attend_shared.restype = C.c_int
+    L.kvm_cache_attend_shared.argtypes = [cd, cc, vp, vp, C.c_int32, vp, C.c_int32, C.c_float, vp, i64p, i64p, vp, C.c_int64, vp, vp]
+    L.kvm_cache_shared_workspace.restype = C.c_int64
+    L.kvm_cache_shared_workspace.argtypes = [cd, cc, C.c_int32, C.c_int32]
+    L.kvm_pages_shared.restype = C.c_int
+    L.kvm_pages_shared.argtypes = [vp, i32p, C.c_int64, C.c_int64, i32p]
     L.kvm_cache_copy_pages.restype = C.c_int
     L.kvm_cache_copy_pages.argtypes = [cd, vp, vp, C.c_int64, vp]
     L.kvm_pages_create.restype = C.c_int
@@ -763,6 +770,32 @@ class Cache:
             raise KVMError(rc, "kvm_cache_attend")
         return out
 
+    def attend_shared(self, q, pages, start, groups, shared, count=None, scale=None, out=None, status=None, stream=None):
+        """kvm_cache_attend_shared: attend (window 0) where sequences groups[g] .. groups[g + 1] - 1 have their first shared[g] blocks in common, which are read
+        once for the group.  groups int32 [n_groups + 1], shared int32 [n_groups]: CUDA tensors (Pages.shared counts the blocks)."""
+        if q.dim() != 4 or q.shape[3] != self.head_dim or (out is not None and out.shape != q.shape):
+            raise ValueError("q, out [batch, n_q_heads, tokens, head_dim]")
+        for t in (groups, shared):
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != self._device:
+                raise ValueError("groups and shared are contiguous int32 tensors on the cache's device")
+        if groups.numel() != shared.numel() + 1:
+            raise ValueError("groups [n_groups + 1], shared [n_groups]")
+        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+            with torch.cuda.device(self._device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
+                return self.attend_shared(q, pages, start, groups, shared, count, scale, out, status)
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        call = self._call(pages, start, count, (q, out), status)
+        Hq, n_groups = q.shape[1], shared.numel()
+        n = lib.kvm_cache_shared_workspace(self._ref, call, n_groups, Hq)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
+        rc = lib.kvm_cache_attend_shared(self._ref, call, groups.data_ptr(), shared.data_ptr(), n_groups, q.data_ptr(), Hq, self.head_dim ** -0.5 if scale is None else scale,
+                                         out.data_ptr(), _strides3(q), _strides3(out), ws.data_ptr() if n > 0 else None, max(n, 0),
+                                         status.data_ptr() if status is not None else None, _stream_ptr(None))
+        if rc != KVM_OK:
+            raise KVMError(rc, "kvm_cache_attend_shared")
+        return out
+
     def copy_pages(self, src, dst, stream=None):
         """kvm_cache_copy_pages: page src[i] to page dst[i]; lists or CPU int32 tensors."""
         src, dst = _page_list(src), _page_list(dst)
@@ -835,6 +868,14 @@ class Pages:
     def length(self, seq: int) -> int:
         n = C.c_int64()
         self._do("kvm_pages_table", self._h, _int(seq), None, 0, None, C.byref(n))
+        return n.value
+
+    def shared(self, seqs, n_tokens: int = 1) -> int:
+        """The number of leading blocks that the sequences have in common in front of the last n_tokens tokens of each: full ones, on the same pages (what
+        Cache.attend_shared takes for a group, in a call of n_tokens tokens)."""
+        ids = [_int(s) for s in seqs]
+        n = C.c_int32()
+        self._do("kvm_pages_shared", self._h, (C.c_int32 * max(1, len(ids)))(*ids), len(ids), _int(n_tokens, 64), C.byref(n))
         return n.value
 
     def tables(self, seqs, max_pages: int = 0, device="cuda"):

@@ -1,0 +1,404 @@
+"""Attention of groups of sequences that share their first blocks (kvm_cache_attend_shared, kvm_pages_shared) against the fp64 definition in oracle/exact_cache.py."""
+import copy
+import ctypes as C
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import exact_cache as ec
+from tests.test_cache import BAD_CACHE, BAD_CALL, Model, _call, _desc, garbage_cache, rows
+
+
+@pytest.fixture(scope="module")
+def kvm():
+    from paper_2605_09877_b200 import build
+    build.build()
+    from paper_2605_09877_b200 import kvm as mod
+    return mod
+
+
+# ---- host ------------------------------------------------------------------------------------------------------------
+
+def test_shared_blocks_of_forks(kvm):
+    p = kvm.Pages(64, 16)
+    a = p.open()
+    p.extend(a, 70)                                    # four full blocks and one in progress
+    b, c = p.fork(a), p.fork(a)
+    assert p.shared([a]) == 4 and p.shared([a], 6) == 4 and p.shared([a], 7) == 3 and p.shared([a], 0) == 4 and p.shared([a], 1000) == 0
+    assert p.shared([a, b, c], 0) == 4
+    for s in (a, b, c):
+        p.extend(s, 30)
+    assert p.shared([a, b, c], 30) == 4 and p.shared([c, a]) == 4
+    d = p.fork(b)
+    p.extend(d, 1)
+    p.extend(b, 1)
+    assert p.shared([b, d]) == 6 and p.shared([a, b, d]) == 4      # (100 tokens: six full blocks)
+    p.trim(b, 20, 16)
+    assert p.shared([b, d]) == 1 and p.shared([d, a]) == 4
+    e = p.open()
+    assert p.shared([e]) == 0 and p.shared([a, e]) == 0
+    for bad in (lambda: p.shared([]), lambda: p.shared([a, 99]), lambda: p.shared([99]), lambda: p.shared([a], -1)):
+        with pytest.raises(kvm.KVMError) as x:
+            bad()
+        assert x.value.code == 1
+    n = C.c_int32()
+    assert kvm.lib.kvm_pages_shared(None, (C.c_int32 * 1)(0), 1, 0, C.byref(n)) == 1 and kvm.lib.kvm_pages_shared(p._h, None, 1, 0, C.byref(n)) == 1
+    with pytest.raises(ValueError):
+        p.shared([1 << 32])
+
+
+@pytest.mark.parametrize("cache,call,code", [(c, {}, e) for c, e in BAD_CACHE] + [({}, c, e) for c, e in BAD_CALL])
+def test_refusals_of_the_cache_and_the_call(kvm, cache, call, code):
+    d, c, x = _desc(kvm, **cache), _call(kvm, **call), 1 << 26
+    assert kvm.lib.kvm_cache_attend_shared(C.byref(d), C.byref(c), x, x, 1, x, 4, 1.0, 2 * x, None, None, x, 1 << 40, None, None) == code
+
+
+def test_refusals_of_the_other_arguments(kvm):
+    L, d, c, x = kvm.lib, C.byref(_desc(kvm)), C.byref(_call(kvm)), 1 << 26
+    st = lambda *a: (C.c_int64 * 3)(*a)  # noqa: E731
+    need = L.kvm_cache_shared_workspace(d, c, 2, 4)
+    assert need > 0 and L.kvm_cache_shared_workspace(d, c, 0, 4) == -1 and L.kvm_cache_shared_workspace(d, c, 3, 4) == -1 and L.kvm_cache_shared_workspace(d, c, 2, 5) == -1
+    assert L.kvm_cache_shared_workspace(d, None, 2, 4) == -1 and L.kvm_cache_shared_workspace(None, c, 2, 4) == -1
+    ok = dict(groups=x, shared=x, n=2, q=x, hq=4, scale=1.0, out=2 * x, qs=None, os=None, ws=x, bytes=need, status=None)
+    for kw, code in ((dict(groups=None), 1), (dict(shared=None), 1), (dict(groups=x + 2), 1), (dict(shared=x + 1), 1), (dict(n=0), 1), (dict(n=-1), 1), (dict(n=3), 1),
+                     (dict(q=None), 1), (dict(out=None), 1), (dict(q=x + 1), 1), (dict(out=2 * x + 1), 1), (dict(hq=0), 1), (dict(hq=5), 1), (dict(scale=0.0), 1),
+                     (dict(scale=-1.0), 1), (dict(scale=math.nan), 1), (dict(scale=math.inf), 1), (dict(qs=st(1, 1, -1)), 1), (dict(os=st(4 * 512, 0, 128)), 1),
+                     (dict(os=st(2048, 512, 64)), 1), (dict(status=x + 1), 1), (dict(ws=None), 1), (dict(ws=x + 8), 1), (dict(bytes=need - 1), 6), (dict(bytes=0), 6)):
+        a = dict(ok, **kw)
+        assert L.kvm_cache_attend_shared(d, c, a["groups"], a["shared"], a["n"], a["q"], a["hq"], a["scale"], a["out"], a["qs"], a["os"], a["ws"], a["bytes"], a["status"], None) == code, kw
+
+
+# ---- kernel ----------------------------------------------------------------------------------------------------------
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Shared(Model):
+    """Groups of sequences behind lead[g] shared blocks, with own[b] tokens of their own in front of the call to come."""
+
+    def __init__(self, kvm, sizes, lead, own, Hkv, d, P, room=200, seed=0, grow=1.0):
+        B = sum(sizes)
+        self.sizes, self.lead = sizes, lead
+        super().__init__(kvm, B, Hkv, d, P, max(lead) + (max(own) + room) // P + 2, seed=seed)
+        self.first = [sum(sizes[:g]) for g in range(len(sizes))]
+        self.groups, self.shared = i32(self.first + [B]), i32(lead)
+        counts = [0] * B
+        for g, n in enumerate(sizes):
+            if n:
+                counts[self.first[g]] = lead[g] * P
+        if max(counts):
+            self.append(rows((B, Hkv, max(counts), d), 100 + seed) * grow, rows((B, Hkv, max(counts), d), 101 + seed) / grow, counts)
+        for g, n in enumerate(sizes):
+            for b in range(self.first[g] + 1, self.first[g] + n):
+                f = self.first[g]
+                self.table[b, :lead[g]] = self.table[f, :lead[g]]
+                self.k[b], self.v[b], self.len[b] = copy.deepcopy(self.k[f]), copy.deepcopy(self.v[f]), self.len[f]
+        if max(own):
+            self.append(rows((B, Hkv, max(own), d), 102 + seed), rows((B, Hkv, max(own), d), 103 + seed), own)
+
+    def hidden(self):
+        """The table with what may be anything as it may be."""
+        t = self.table.clone()
+        for g, n in enumerate(self.sizes):
+            for b in range(self.first[g] + 1, self.first[g] + n):
+                t[b, :self.lead[g]] = -7
+        return t
+
+    def step(self, T, Hq, counts, seed, status=None, scale=None, check=True, **kw):
+        """New tokens and their attention; every row is compared."""
+        self.append(rows((self.B, self.Hkv, T, self.d), 200 + seed), rows((self.B, self.Hkv, T, self.d), 201 + seed), counts)
+        q = rows((self.B, Hq, T, self.d), 202 + seed)
+        start = i32([n - c for n, c in zip(self.len, counts)])
+        out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+        got = self.cache.attend_shared(q.cuda(), self.hidden(), start, self.groups, self.shared, None if counts == [T] * self.B else i32(counts), scale=scale, out=out, status=status, **kw)
+        torch.cuda.synchronize()
+        assert got is out and status.item() == 0
+        if check:
+            self.compare(q, out, counts, 0, 0, scale)
+        return q, start, out
+
+
+CASES = [   # sizes, lead, own, Hq, Hkv, d, P, T
+    ([2], [15], [60, 31], 8, 2, 128, 64, 1),
+    ([1], [3], [0], 1, 1, 64, 16, 1),
+    ([3], [1], [0, 5, 200], 6, 3, 128, 128, 1),
+    ([5], [9], [0, 1, 15, 16, 17], 10, 2, 64, 16, 2),
+    ([4, 3], [40, 7], [0, 10, 20, 30, 40, 50, 60], 8, 1, 128, 32, 1),
+    ([33], [20], list(range(33)), 4, 1, 128, 64, 1),                         # 132 rows
+    ([64], [33], [3 * i for i in range(64)], 8, 2, 128, 64, 1),              # 256 rows
+    ([70], [31], [i % 7 for i in range(70)], 8, 2, 64, 16, 1),               # 280 rows
+    ([40], [5], [i for i in range(40)], 16, 1, 128, 128, 1),                 # 640 rows, 16 to a sequence
+    ([8, 0, 1, 50, 0], [12, 3, 0, 2, 5], [i % 40 for i in range(59)], 14, 2, 128, 64, 2),
+    ([6] * 20, [4] * 20, [i % 5 for i in range(120)], 4, 4, 64, 32, 3),
+    ([2, 2, 2], [0, 0, 0], [5, 300, 17, 0, 1, 90], 8, 2, 128, 64, 1),        # nothing shared at all
+    ([10], [130], [0] * 10, 8, 8, 128, 16, 1),
+    ([3], [8], [2, 3, 4], 6, 1, 128, 64, 5),                                 # 30 (token, head) pairs per sequence
+    ([3, 2], [10, 4], [300, 0, 77, 5, 1000], 8, 2, 64, 16, 70),              # 280, long parts of their own
+    ([9, 1], [40, 0], [17 * i for i in range(10)], 8, 1, 128, 32, 3),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes,lead,own,Hq,Hkv,d,P,T", CASES)
+def test_shared_against_the_definition(kvm, sizes, lead, own, Hq, Hkv, d, P, T):
+    m = Shared(kvm, sizes, lead, own, Hkv, d, P)
+    r = random.Random(1)
+    m.step(T, Hq, [T] * m.B, 0)
+    m.step(T, Hq, [r.randint(0, T) for _ in range(m.B)], 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(12))
+def test_shared_over_random_shapes(kvm, seed):
+    r = random.Random(seed)
+    Hkv, G, d, P = r.choice([1, 2, 3]), r.choice([1, 2, 3, 4, 7, 8]), r.choice([64, 128]), r.choice([16, 32, 64, 128])
+    sizes = [r.choice([0, 1, 2, 5, 20, 40]) for _ in range(r.choice([1, 2, 4]))] + [2]
+    lead = [r.choice([0, 1, 2, r.randint(1, 1500 // P)]) for _ in sizes]
+    own = [r.randint(0, r.choice([0, 40, 400])) for _ in range(sum(sizes))]
+    T = r.choice([1, 1, 2, 16 // G, 7])
+    m = Shared(kvm, sizes, lead, own, Hkv, d, P, seed=seed)
+    m.step(T, Hkv * G, [r.randint(0, T) if r.random() < 0.3 else T for _ in range(m.B)], seed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes,G,T", [([3], 4, 1), ([50, 9], 4, 1), ([30], 4, 4)])
+def test_long_shared_parts_and_more_tiles_than_multiprocessors(kvm, sizes, G, T):
+    """Long chains of tiles per unit and CTAs with parts of several units; results are the same every time, and on another stream, and in any strides."""
+    B = sum(sizes)
+    m = Shared(kvm, sizes, [300] * len(sizes), [37 * b % 300 for b in range(B)], 2, 128, 16, seed=5)
+    q, start, out = m.step(T, 2 * G, [T] * B, 0)
+    t, s = m.hidden(), torch.cuda.Stream()
+    for _ in range(3):
+        assert torch.equal(m.cache.attend_shared(q.cuda(), t, start, m.groups, m.shared), out)
+    s.wait_stream(torch.cuda.current_stream())
+    got = m.cache.attend_shared(q.cuda(), t, start, m.groups, m.shared, stream=s)
+    s.synchronize()
+    assert torch.equal(got, out)
+    odd = torch.empty((B, T, 2 * G, 131), dtype=torch.bfloat16, device="cuda").transpose(1, 2)[..., 1:129]
+    odd.copy_(q)
+    wide = torch.full((B, T, 2 * G, 130), 7.0, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    m.cache.attend_shared(odd, t, start, m.groups, m.shared, out=wide[..., :128])
+    assert torch.equal(wide[..., :128], out) and (wide[..., 128:] == 7.0).all()
+    m.compare(q, m.cache.attend_shared(q.cuda(), t, start, m.groups, m.shared, scale=0.3), [T] * B, 0, 0, 0.3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d", [(2, 128), (40, 64), (40, 128)])
+def test_blocks_of_very_different_scales(kvm, n, d):
+    """Shared and own blocks whose values lie up to 2^100 apart, keys of one block that decide everything."""
+    m = Shared(kvm, [n], [0], [0] * n, 1, d, 16, room=500)
+    L, P = 400, 16
+    k, v = rows((n, 1, L, d), 1), rows((n, 1, L, d), 2)
+    for i, e in enumerate((0, -60, 30, -14, -15, 3, 40, -59, 0, -100)):
+        v[:, :, 40 * i:40 * i + 40] *= 2.0 ** e
+    k[:, :, 200:216] *= 16.0
+    m.append(k[:1].expand(n, -1, -1, -1).contiguous(), v[:1].expand(n, -1, -1, -1).contiguous(), [L] + [0] * (n - 1))
+    for b in range(1, n):
+        m.table[b, :L // P] = m.table[0, :L // P]
+        m.k[b], m.v[b], m.len[b] = copy.deepcopy(m.k[0]), copy.deepcopy(m.v[0]), L
+    m.append(rows((n, 1, 33, d), 5), rows((n, 1, 33, d), 6) * 2.0 ** 20, [33] * n)
+    m.lead, m.shared = [L // P], i32([L // P])
+    m.step(1, 4, [1] * n, 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,below", [(2, 22.0), (2, 28.5), (60, 26.0)])
+def test_a_long_flat_shared_tail_below_a_peak_counts(kvm, n, below):
+    """The first shared key has logit `below` * ln 2 above all others, whose values are 1 where its own is 0: they weigh L 2^-below together."""
+    L, d, P = 1 << 18, 64, 128
+    c = kvm.Cache.empty(L // P + n + 1, 1, d, P)
+    c.k_scale.fill_(1.0)
+    c.v8.view(torch.uint8)[:L // P] = 0x38                         # 1.0
+    c.v8.view(torch.uint8)[0, 0, 0] = 0
+    k = torch.zeros(d)
+    k[0] = 64.0
+    c.k8.view(torch.uint8)[0, 0, 0] = k.to(torch.float8_e4m3fn).view(torch.uint8).cuda()
+    table = torch.full((n, L // P + 1), -1, dtype=torch.int32)
+    table[0, :L // P] = torch.arange(L // P)
+    table[:, L // P] = L // P + torch.arange(n)
+    q = torch.zeros((n, 4, 1, d), dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    scale = below * math.log(2) / 64.0
+    zero = torch.zeros((n, 1, 1, d), dtype=torch.bfloat16, device="cuda")
+    c.append(zero, zero, table.cuda(), i32([L] * n))               # (its own: value 0)
+    out = c.attend_shared(q.cuda(), table.cuda(), i32([L] * n), i32([0, n]), i32([L // P]), scale=scale).double().cpu()
+    w = math.exp(-64.0 * float(np.float32(scale)))
+    want = (L - 1) * w / (1 + L * w)
+    # bf16 2^-8; a weight 2^-11 of itself, or half a step of fp16's least number, 2^-25 in units of 2^-6 of the reference: 2^-31 each; the logit 2^-21 of itself
+    assert (abs(out - want) <= want * (2.0 ** -8 + 2.0 ** -11 + below * 2.0 ** -21) + L * 2.0 ** -31).all(), (float(out.min()), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[2, 2, 1], [40, 40, 3]])
+def test_nans_stay_where_they_are_seen(kvm, sizes):
+    """A NaN among the shared keys or values reaches the rows of its group and head, one in q its own row, one in a sequence's own block its rows."""
+    B = sum(sizes)
+    m = Shared(kvm, sizes, [20, 9, 4], [20] * B, 3, 64, 16)
+    m.cache.k_scale[m.table[0, 7], 0] = math.nan
+    m.cache.v_scale[m.table[sizes[0], 3], 1] = math.nan
+    m.cache.v_scale[m.table[B - 1, 4], 2] = math.nan
+    q, start, out = m.step(1, 12, [1] * B, 0, check=False)
+    bad = torch.isnan(out.float())
+    want = torch.zeros((B, 12), dtype=torch.bool)
+    want[:sizes[0], :4] = True
+    want[sizes[0]:sizes[0] + sizes[1], 4:8] = True
+    want[B - 1, 8:] = True
+    assert torch.equal(bad.all(-1)[:, :, 0].cpu(), want) and torch.equal(bad.any(-1)[:, :, 0].cpu(), want)
+    qn = q.clone()
+    qn[1, 11, 0, 5] = math.nan
+    qn[B - 2, 9, 0, 0] = -math.inf
+    got = m.cache.attend_shared(qn.cuda(), m.hidden(), start, m.groups, m.shared)
+    want2 = want.clone()
+    want2[1, 11] = want2[B - 2, 9] = True
+    assert torch.equal(torch.isnan(got.float()).all(-1)[:, :, 0].cpu(), want2)
+    assert torch.equal(got[~want2], out[~want2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[2, 2, 1], [40, 40, 3]])
+def test_bad_groups_lengths_and_pages_are_reported(kvm, sizes):
+    B = sum(sizes)
+    m = Shared(kvm, sizes, [20, 9, 4], [20] * B, 2, 64, 16)
+    q, start, out = m.step(1, 8, [1] * B, 0)
+    q, t = q.cuda(), m.hidden()
+    n0, n1 = sizes[0], sizes[0] + sizes[1]
+
+    def run(table=t, start=start, groups=m.groups, shared=m.shared, count=None):
+        got, status = torch.full(out.shape, 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+        m.cache.attend_shared(q, table, start, groups, shared, count, out=got, status=status)
+        assert status.item() == 1
+        return got
+
+    # offsets that do not ascend from 0 to the batch: nothing is written
+    for g in ([0, n1, n0, B], [1, n0, n1, B], [0, n0, n1, B - 1], [0, n0, n1, B + 1], [0, -5, n1, B], [-1, n0, n1, B], [0, 2 ** 31 - 1, n1, B]):
+        assert (run(groups=i32(g)) == 7.0).all()
+    # numbers of blocks that are not allowed: that group gets no rows
+    for s in (-1, 10, 2 ** 31 - 1, -2 ** 31, m.table.shape[1] + 1, m.table.shape[1]):
+        if s == 10:
+            got = run(shared=i32([20, 9 + 2, 4]), start=start)             # (start = 9 * 16 + 20: the eleventh block is not in front of it)
+        else:
+            got = run(shared=i32([20, s, 4]))
+        assert (got[n0:n1] == 7.0).all() and torch.equal(got[:n0], out[:n0]) and torch.equal(got[n1:], out[n1:])
+    # lengths
+    for b, x in ((n0, -1), (n0 + 1, 2 ** 31 - 1), (n0 + 1, 9 * 16 - 1)):
+        s2 = start.clone()
+        s2[b] = x
+        got = run(start=s2)
+        keep = [i for i in range(B) if i != b]
+        assert (got[b] == 7.0).all() and torch.equal(got[keep], out[keep])
+    # a page outside the pool among the shared ones: the group's rows are NaN
+    for x in (-1, 10 ** 6):
+        t2 = t.clone()
+        t2[n0, 5] = x
+        got = run(table=t2)
+        assert torch.isnan(got[n0:n1].float()).all() and torch.equal(got[:n0], out[:n0]) and torch.equal(got[n1:], out[n1:])
+    # among a sequence's own
+    t2 = t.clone()
+    t2[0, 20] = -1
+    got = run(table=t2)
+    assert torch.isnan(got[0].float()).all() and torch.equal(got[1:], out[1:])
+
+
+@pytest.mark.gpu
+def test_captured_calls_follow_groups_lengths_and_pages(kvm):
+    """Two graphs of the same call do not share their workspaces; a replay follows the arrays."""
+    m = Shared(kvm, [3, 5], [10, 20], [5 * b for b in range(8)], 2, 128, 32)
+    q0, start0, want0 = m.step(1, 8, [1] * 8, 0)
+    q, start, table = q0.cuda(), start0.clone(), m.hidden()
+    groups, shared = m.groups.clone(), m.shared.clone()
+    out, out2 = torch.zeros_like(q), torch.zeros_like(q)
+    warm = torch.cuda.Stream()
+    warm.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(warm):
+        m.cache.attend_shared(q, table, start, groups, shared, out=out)
+    torch.cuda.current_stream().wait_stream(warm)
+    g, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        m.cache.attend_shared(q, table, start, groups, shared, out=out)
+    with torch.cuda.graph(g2):
+        m.cache.attend_shared(q, table, start, groups, shared, out=out2)
+    s = torch.cuda.Stream()
+    for step in range(3):
+        if step == 1:                                              # sequences go on
+            qn, sn, _ = m.step(1, 8, [1] * 8, 4)
+            q.copy_(qn); start.copy_(sn); table.copy_(m.hidden())
+        if step == 2:                                              # other groups, fewer shared blocks: the tables as they are
+            groups.copy_(i32([0, 2, 8])); shared.copy_(i32([10, 0])); table.copy_(m.table)
+        g.replay()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            g2.replay()
+        g.replay()
+        torch.cuda.synchronize()
+        qc = q.cpu()
+        m.compare(qc, out, [1] * 8, 0, 0)
+        m.compare(qc, out2, [1] * 8, 0, 0)
+
+
+@pytest.mark.gpu
+def test_samples_of_prompts_served_behind_their_shared_blocks(kvm):
+    """Prompts, forks into samples, steps with ingest and shared attention, samples that end and fork again, compaction: each step against what the cache holds."""
+    P, d, Hq, Hkv = 16, 64, 8, 2
+    pages, cache = kvm.Pages(400, P), kvm.Cache.empty(400, Hkv, d, P)
+    f = kvm.Front(norm="rms", rope_dims=32)
+    r = random.Random(3)
+    prompts = []
+    for i, n in enumerate((300, 37)):
+        s = pages.open()
+        pages.extend(s, n)
+        t, length = pages.tables([s])
+        x = rows((1, 2 * Hkv, n, d), 10 + i).cuda()
+        cache.ingest(None, x[:, :Hkv], x[:, Hkv:], f, t, length - n)
+        prompts.append([s] + [pages.fork(s) for _ in range(4)])
+    for step in range(12):
+        if step == 5:
+            pages.close(prompts[0].pop(0))
+            prompts[0].append(pages.fork(prompts[0][1]))
+        if step == 8:
+            src, dst = pages.compact()
+            cache.copy_pages(src, dst)
+        seqs = [s for p in prompts for s in p]
+        T, B = r.choice([1, 1, 2]), len(seqs)
+        copies = [c for c in (pages.extend(s, T) for s in seqs) if c]
+        if copies:
+            cache.copy_pages(*[list(x) for x in zip(*copies)])
+        t, length = pages.tables(seqs)
+        x = rows((B, Hq + 2 * Hkv, T, d), 50 + step).cuda()
+        status = i32([0])
+        q = cache.ingest(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], f, t, length - T, status=status)
+        groups = i32([0, len(prompts[0]), B])
+        shared = i32([pages.shared(p, T) for p in prompts])
+        assert shared.tolist()[0] >= 300 // P and shared.tolist()[1] >= 37 // P
+        out = cache.attend_shared(q, t, length - T, groups, shared, status=status)
+        assert status.item() == 0
+        n = length.tolist()
+        held = cache.read(t, i32([0] * B), max(n), length)
+        for b in range(B):
+            for h in range(Hkv):
+                K, V = (z[b, h, :n[b]].float().cpu().double().numpy() for z in held)
+                qn = q[b, 4 * h:4 * h + 4].float().cpu().double().numpy().reshape(-1, d)
+                ref, bound = ec.attend(qn, K, V, np.tile(np.arange(n[b] - T, n[b]), 4), float(np.float32(d ** -0.5)))
+                assert (np.abs(out[b, 4 * h:4 * h + 4].float().cpu().double().numpy().reshape(-1, d) - ref) <= bound).all()
+
+
+@pytest.mark.gpu
+def test_many_groups(kvm):
+    """As many groups as a call may have sequences, and one group of all of them."""
+    B, d, P = 1024, 64, 16
+    c = kvm.Cache.empty(3 * B, 1, d, P)
+    x = torch.randn((B, 2, 40, d), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    table = torch.arange(3 * B, dtype=torch.int32, device="cuda").view(B, 3)
+    c.append(x[:, :1], x[:, 1:], table, i32([0] * B))
+    q = rows((B, 2, 1, d), 3).cuda()
+    start = i32([39] * B)
+    want = c.attend(q, table, start).float()
+    got = c.attend_shared(q, table, start, torch.arange(B + 1, dtype=torch.int32, device="cuda"), i32([2] * B)).float()
+    assert (got - want).abs().max() <= 2.0 ** -7 * want.abs().max()
+    table[:, :2] = table[0, :2].clone()
+    want = c.attend(q, table, start).float()
+    got = c.attend_shared(q, table, start, i32([0, B]), i32([2])).float()
+    assert (got - want).abs().max() <= 2.0 ** -7 * want.abs().max()
