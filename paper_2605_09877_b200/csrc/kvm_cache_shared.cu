@@ -9,16 +9,17 @@
 // list, in which a tile of more than 128 rows counts twice; every CTA takes an equal, contiguous share of it, whatever the lengths and the sizes of
 // the groups are, and leaves one partial result per unit that it has tiles of.
 //     S = (q_hi + q_lo) K8^T   kind::f8f6f4: the codes as they lie in memory, q in two parts of e4m3
-//     O += P V16               kind::f16: P in fp16 from tensor memory, V16 = the codes of the values in fp16 (exact)
-// as in kvm_cache_prompt.cu, but with two streams of one S and one O each: of two row tiles on the same keys (a tile of values is converted once for
+//     O += P V16               kind::f16: P in bf16 from tensor memory, V16 = the codes of the values as bf16 numbers (exact)
+// as in kvm_cache_prompt.cu, but with two streams of one S and one O each: of two row tiles on the same keys (a tile of values is widened once for
 // 256 rows), or of one row tile on the even and the odd key tiles.  A stream goes S, softmax, P V, S, ...; while one is in its softmax the other is in the
-// tensor core, and nothing is handed from stream to stream.  One thread per row, which reads S once: weights are computed with the reference so far and kept in
-// registers; only where a row's maximum lies more than 2^8 above it is the reference moved, O rescaled and the tile computed again.
+// tensor core, and nothing is handed from stream to stream.  bf16 weights have fp32's range, so a row's reference is not its maximum but a number that
+// has hardly ever to be changed: S is read once, no maximum is taken, and the two threads of a row, 64 columns each, need not meet.  What leaves the range shows in the sums
+// of weights; then the products wait, the stream's warps agree on references in a turn of their own, and go on.
 // Scales of values go into the exponents of the weights, relative to the largest of the share's blocks, and out of the row sums again.
 //   warp 0       producer of keys (TMA, page numbers and scales ahead), warp 3 of values
-//   warp 1       issues S, warp 2 issues P V (one thread each)
-//   warps 4-11   queries (scaled, split); softmax, thread = row; results
-//   warps 12-15  value codes -> fp16, swizzled as the MMA reads them
+//   warp 1       issues the products (one thread)
+//   warps 4-19   queries (scaled, split); softmax, eight warps per stream, two threads per row, 64 columns each; results
+//   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 #include <algorithm>
 #include <atomic>
 
@@ -36,10 +37,17 @@ kvm_status_t attend_args(const kvm_cache_t* cache, const kvm_cache_call_t* call,
 namespace {
 
 constexpr int kCtas = 148;
-constexpr int kThreads = 512;
+constexpr int kThreads = 768;
 constexpr int kInfo = 8;
-constexpr float kShift = 6.f;    // weights in units of 2^-6 of the reference (kvm_cache_prompt.cu)
-constexpr float kRaise = 8.f;    // a reference is moved when a maximum lies more than 2^8 above it: weights stay below 2^14
+// Weights of a row, 2^(y - m), y = logit + exponent of the value's scale relative to the largest, go into the products as bf16 numbers in units of 2^-kBias,
+// and the codes of the values as bf16 numbers of 2^-kCode of what they stand for (their bits, shifted: nothing is multiplied).  bf16 has fp32's range, so the
+// reference m need not be the row's maximum: it is 0 to begin with, and anything will do that lies between kHigh below the largest y and kLow above
+// it.  A weight is then at most 2^(kHigh + kBias), and with the largest one at least 2^(kBias - kLow) even products with the smallest normal code,
+// 2^(-6 - kCode), have all their bits in fp32 (2^-126 2^24).  Sums of weights (without the values' scales, which may be 2^-kFoldMost) are held in units of 2^kBias.
+constexpr int kBias = 64, kCode = 120, kHigh = 60, kLow = 40;
+static_assert(kHigh + kBias <= 124 && kBias - kLow - kCode - 6 >= -126 + 24, "range");
+constexpr float kShift = 6.f;    // what the kernels for few and for many tokens count their weights in (of 2^-8 and 2^-6 of the reference)
+constexpr float kDecodeShift = 8.f;
 
 struct SharedArgs {
   AttendArgs a;
@@ -67,8 +75,8 @@ struct Unit {
   __device__ __forceinline__ bool tall() const { return w == 2; }
   // tiles [jb, je) of the CTA whose share begins at w0
   __device__ __forceinline__ void of(int w0, int share, int& jb, int& je) const {
-    jb = max(0, w0 - begin + w - 1) / w;
-    je = min(tiles, max(0, w0 + share - begin + w - 1) / w);
+    jb = max(0, w0 - begin + w - 1) >> (w - 1);   // (w is 1 or 2)
+    je = min(tiles, max(0, w0 + share - begin + w - 1) >> (w - 1));
   }
   // where the partial result of that CTA (its number: cta) is: one step further in the list is one unit or one CTA further
   __device__ __forceinline__ int64_t slot(int cta) const { return at + (int64_t)cta * 256; }
@@ -128,7 +136,7 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, int2* s
   if (tid == NT - 1) pre[gr.n] = add.x + sum.x;
   __syncthreads();
   plan.total = pre[gr.n];
-  plan.share = (plan.total + s.grid - 1) / s.grid;
+  plan.share = max(2, (plan.total + s.grid - 1) / s.grid);   // (both streams have something to do, and no share within a unit is empty)
   return true;
 }
 // Last g with pre[g] <= f < pre[n].
@@ -161,6 +169,19 @@ __device__ __forceinline__ Unit unit_at(const SharedArgs& s, const Plan& plan, i
   const int per = tiles * (2 * full + (left ? weight_of(left) : 0)), rest = f - plan.pre[g], hk = rest / per;
   return unit_of(s, plan, g, blocks, hk, min(full, (rest - hk * per) / (2 * tiles)));
 }
+// The CTA's next unit with tiles behind position f of the list; its share is [w0, w1).
+template <class Segment>
+__device__ __forceinline__ bool segment_at(const SharedArgs& s, const Plan& plan, int w0, int w1, int& f, Segment& g) {
+  while (f < w1) {
+    g.u = unit_at(s, plan, f);
+    int je;
+    g.u.of(w0, plan.share, g.jb, je);
+    g.n = je - g.jb;
+    f = g.u.begin + g.u.tiles * g.u.w;
+    if (g.n > 0) return true;
+  }
+  return false;
+}
 // A row of a group: its sequence, token and head (of the kv head's group).
 struct Row { int b, t, h; };
 __device__ __forceinline__ Row row_of(const SharedArgs& s, int b0, int r) {
@@ -179,8 +200,15 @@ struct alignas(16) KeyTile {
   float ks[8], ve[8]; // per 16 keys: scale of the keys, exponent of the values' scale
 };
 
-enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 26, SB_PVDONE = 28, SB_QFULL = 30, SB_LAST = 31,
+enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 26, SB_PVDONE = 28, SB_QFULL = 30,
        SB_VBASE = 32, SB_COUNT = 36 };
+
+struct Segment { Unit u; int jb, n; };
+struct Walk {           // how far the softmax warps are, so that their registers need not hold it
+  Plan plan;
+  int f, w0, w1;
+  Segment g;
+};
 
 template <int D>
 struct SharedCfg {
@@ -192,15 +220,40 @@ struct SharedCfg {
   static constexpr int OFF_V = OFF_V8 + NV8 * T8;
   static constexpr int OFF_INFO = OFF_V + NV * T16;
   static constexpr int OFF_CQ = OFF_INFO + kInfo * (int)sizeof(KeyTile);   // float [2][128]
-  static constexpr int OFF_BAR = OFF_CQ + 2 * 128 * 4;
-  static constexpr int OFF_PLAN = OFF_BAR + 512;         // int [3][n_groups + 1]
+  static constexpr int OFF_X = OFF_CQ + 2 * 128 * 4;                       // float [stream][half][128]: maxima, sums
+  static constexpr int OFF_BAR = OFF_X + 4 * 128 * 4;
+  static constexpr int OFF_WALK = OFF_BAR + 512;
+  static constexpr int OFF_PLAN = OFF_WALK + 128;        // int [3][n_groups + 1]
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static int smem(int n_groups) { return std::max(OFF_PLAN + 12 * (n_groups + 1) + 1024, 120 * 1024); }
   static constexpr uint32_t COL_S = 0, COL_O = 256;      // of stream s: + 128 s
   static_assert(NK <= 6 && NV8 <= 4 && NK + 2 <= kInfo, "rings");
   static_assert(OFF_K % 1024 == 0 && OFF_V8 % 1024 == 0 && OFF_V % 1024 == 0 && OFF_INFO % 16 == 0 && OFF_CQ % 16 == 0 && OFF_BAR % 8 == 0 && OFF_PLAN % 8 == 0, "alignment");
+  static_assert(sizeof(Walk) <= 128 && OFF_WALK % 8 == 0, "shared memory");
   static_assert(SB_COUNT * 8 + 128 <= 512 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
 };
+
+// Four e4m3 codes (channels 0 .. 3) as bf16 numbers of 2^-kCode of what they stand for, channels 0 and 2, then 1 and 3: sign, four bits of exponent and three
+// of mantissa where they belong (a subnormal code is a subnormal number).  The results' channels are put in order when they are read.
+__device__ __forceinline__ void widen4(uint32_t c, uint32_t& even, uint32_t& odd) {
+  even = ((c & 0x007f007fu) << 4) | ((c << 8) & 0x80008000u);
+  odd = ((c & 0x7f007f00u) >> 4) | (c & 0x80008000u);
+}
+__device__ __forceinline__ int channel_of(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
+// two floats -> two bf16 (a in the low half)
+__device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+// Barrier of the two warps that share 32 rows of a stream.
+__device__ __forceinline__ void pair_barrier(int id) {
+  __syncwarp();
+  asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+}
+__device__ __forceinline__ void copy16_async(void* smem, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(smem)), "l"(global) : "memory");
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -217,16 +270,19 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);                  // [segment % 4][4]
   volatile uint32_t* s_there = reinterpret_cast<uint32_t*>(s_vmax + 16); // [value tile of the ring]: pages that were loaded
+  volatile int* s_flag = reinterpret_cast<int*>(s_vmax + 20);           // [stream]: the turn whose reference will not do
+  volatile int* s_redo = s_flag + 2;                                    // [stream]: the turn that does it again
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (who waits for this kernel does so before reading what it wrote)
   if (warp == 0) {
     for (int i = lane; i < SB_COUNT; i += 32) {
       auto in = [&](int first, int n) { return i >= first && i < first + n; };
-      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_PREADY, 2) || in(SB_VBASE, 4) ? 4 : in(SB_QFULL, 1) ? 8 : 1);
+      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) ? 4 : in(SB_PREADY, 2) ? 8 : in(SB_QFULL, 1) ? 16 : 1);
     }
     if (lane == 0) {
       tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
       *abort_flag = 0;
+      s_flag[0] = s_flag[1] = s_redo[0] = s_redo[1] = -1;
     }
     tc::fence_barrier_init();
   }
@@ -245,19 +301,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
     *abort_flag = 1;
   };
-  // The CTA's segments: (unit, key tiles).  Every warp walks them by itself.
-  struct Segment { Unit u; int jb, n; };
-  auto next_segment = [&](int& f, Segment& g) {
-    while (f < w1) {
-      g.u = unit_at(args, plan, f);
-      int je;
-      g.u.of(w0, plan.share, g.jb, je);
-      g.n = je - g.jb;
-      f = g.u.begin + g.u.tiles * g.u.w;
-      if (g.n > 0) return true;
-    }
-    return false;
-  };
+  // The CTA's segments: (unit, key tiles).  Every warp walks them by itself, but for those of the softmax.
+  auto next_segment = [&](int& f, Segment& g) { return segment_at(args, plan, w0, w1, f, g); };
   const int tshift = 7 - p.page_shift, ppt = 1 << tshift;
   Segment g;
   int f = w0;
@@ -314,7 +359,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             }
             for (int i = 0; i < p.page / 16; ++i) {
               ti.ks[lp * (p.page / 16) + i] = nan ? 1.f : exp2i(cur.ke);   // (rows of a NaN are marked, not computed with)
-              ti.ve[lp * (p.page / 16) + i] = nan ? 0.f : (float)cur.ve;
+              ti.ve[lp * (p.page / 16) + i] = nan || cur.row < 0 ? -1000.f : (float)cur.ve;   // (below all others: what is not there has no weight)
             }
           } else if (mine && lp == 0) {
             s_there[s] = loads >> lane;
@@ -334,80 +379,82 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll 1
         for (int j = max(0, issued - ring); j < issued; ++j) tc::mbar_wait_tight(&bars[full + j % ring], (j / ring) & 1);
       }
-    } else if (warp == 1) {
-      // ------------------------------ S ------------------------------
-      if (lane == 0) {
-        constexpr uint32_t ID = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
-        auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
-        const uint64_t dQ0 = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
-        bool ok = true;
-        int it[2] = {0, 0};   // tiles of the streams so far
-        uint32_t s = 0, par = 0;
-#pragma unroll 1
-        for (int seg = 0; ok && next_segment(f, g); ++seg) {
-          ok = tc::mbar_wait_tight(&bars[SB_QFULL], seg & 1);
-          const bool tall = g.u.tall();
-#pragma unroll 1
-          for (int j = 0; j < g.n && ok; ++j) {
-            ok = tc::mbar_wait_tight(&bars[SB_KFULL + s], par);
-            const uint64_t k = dK + s * (Cfg::T8 >> 4);
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-              if (!ok || (!tall && st != (j & 1))) continue;
-              if (it[st] > 0) ok = tc::mbar_wait_tight(&bars[SB_PVDONE + st], (it[st] - 1) & 1);   // (its weights lie where S goes)
-              if (!ok) continue;
-              ++it[st];
-              tc::tc_fence_after();
-              const uint64_t dQ = dQ0 + (tall ? st : 0) * (2 * Cfg::T8 >> 4);
-              const uint32_t dS = tmem + Cfg::COL_S + 128 * st;
-#pragma unroll
-              for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + 2 * ks, k + 2 * ks, ID, ks > 0);
-#pragma unroll
-              for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID, 1u);
-              tc::mma_commit(&bars[SB_SFULL + st]);
-            }
-            tc::mma_commit(&bars[SB_KFREE + s]);
-            if (++s == Cfg::NK) { s = 0; par ^= 1; }
-          }
-        }
-        if (!ok) fail();
-      }
-    } else if (lane == 0) {
-      // ------------------------------ P V ------------------------------
-      constexpr uint32_t ID = tc::idesc_f16(128, D, true);
+    } else if (warp == 1 && lane == 0) {
+      // ------------------------------ products ------------------------------
+      // Items of a segment: row tile i % 2 on key tile i / 2, or key tile i, in either case stream i % 2.  One thread issues P V of item i and then, when it is
+      // done (its weights lie where S goes), S of item i + 2: while the tensor core does these two, the other stream is in its softmax.  (With S and
+      // P V issued by two threads they ran as P V, P V, S, S, and both streams were in their softmax at the same time.)
+      constexpr uint32_t ID_S = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
+      constexpr uint32_t ID_O = tc::idesc_f16(128, D, true) | (1u << 7) | (1u << 10);   // (format 1: bf16)
+      auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
+      const uint64_t dQ = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
       const uint64_t dV = tc::smem_desc_sw128(tc::smem_u32(base + Cfg::OFF_V), 128 * 128, 1024);
       bool ok = true;
-      int it[2] = {0, 0}, J = 0;
+      int turn[2] = {0, 0};     // turns that the streams' softmax has been given (S, the same again, the end of a segment)
+      int back[2] = {0, 0};     // weights that have come back
+      int it[2] = {0, 0};       // P V so far
+      int J = 0;                // value tiles so far
+      uint32_t s = 0, par = 0;  // ring of keys
+      auto wait = [&](int bar, uint32_t parity) { ok = ok && tc::mbar_wait_tight(&bars[bar], parity); return ok; };
 #pragma unroll 1
-      while (ok && next_segment(f, g)) {
-        const bool tall = g.u.tall();
+      for (int seg = 0; ok && next_segment(f, g); ++seg) {
+        const int tall = g.u.tall() ? 1 : 0, items = g.n << tall;
+        if (!wait(SB_QFULL, seg & 1)) break;
 #pragma unroll 1
-        for (int j = 0; j < g.n && ok; ++j, ++J) {
-          ok = tc::mbar_wait_tight(&bars[SB_VFULL + (J & 1)], (J >> 1) & 1);
-          const uint64_t v = dV + (J & 1) * (Cfg::T16 >> 4);
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            if (!ok || (!tall && st != (j & 1))) continue;
-            ok = tc::mbar_wait_tight(&bars[SB_PREADY + st], it[st] & 1);
-            if (!ok) continue;
-            ++it[st];
+        for (int i = -2; i < items; ++i) {
+          const int st = i & 1;
+          if (i >= 0) {
+            if ((!tall || st == 0) && !wait(SB_VFULL + (J & 1), (J >> 1) & 1)) break;
+            if (!wait(SB_PREADY + st, back[st]++ & 1)) break;
+            if (s_flag[st] == turn[st] - 1) {   // (at most once)
+              s_redo[st] = turn[st]++;
+              tc::mbar_arrive(&bars[SB_SFULL + st]);
+              if (!wait(SB_PREADY + st, back[st]++ & 1)) break;
+            }
             tc::tc_fence_after();
-            const bool first = j < (tall ? 1 : 2);
+            const uint64_t v = dV + (J & 1) * (Cfg::T16 >> 4);
+            const uint32_t dO = tmem + Cfg::COL_O + 128 * st, aP = tmem + Cfg::COL_S + 128 * st;
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
-              tc::mma_f16_ts(tmem + Cfg::COL_O + 128 * st, tmem + Cfg::COL_S + 128 * st + 8 * kk, v + kk * (2048 >> 4), ID, (!first || kk > 0) ? 1u : 0u);
+              tc::mma_f16_ts(dO, aP + 64 * (kk >> 2) + 8 * (kk & 3), v + kk * (2048 >> 4), ID_O, (i >= 2 || kk > 0) ? 1u : 0u);
             tc::mma_commit(&bars[SB_PVDONE + st]);
+            if (!tall || st == 1) {
+              tc::mma_commit(&bars[SB_VFREE + (J & 1)]);
+              ++J;
+            }
+            if (i + 2 < items && !wait(SB_PVDONE + st, it[st] & 1)) break;
+            ++it[st];
           }
-          tc::mma_commit(&bars[SB_VFREE + (J & 1)]);
+          if (i + 2 < items) {
+            if ((!tall || st == 0) && !wait(SB_KFULL + s, par)) break;
+            tc::tc_fence_after();
+            const uint64_t k = dK + s * (Cfg::T8 >> 4), q = dQ + (tall & st) * (2 * Cfg::T8 >> 4);
+            const uint32_t dS = tmem + Cfg::COL_S + 128 * st;
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, q + 2 * ks, k + 2 * ks, ID_S, ks > 0);
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, q + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID_S, 1u);
+            tc::mma_commit(&bars[SB_SFULL + st]);
+            ++turn[st];
+            if (!tall || st == 1) {
+              tc::mma_commit(&bars[SB_KFREE + s]);
+              if (++s == Cfg::NK) { s = 0; par ^= 1; }
+            }
+          }
         }
-        if (ok) tc::mma_commit(&bars[SB_LAST]);
+        if (!ok) break;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {   // the end, when all products have landed
+          tc::mma_commit(&bars[SB_SFULL + st]);
+          ++turn[st];
+        }
       }
       if (!ok) fail();
     }
-  } else if (warp >= 12) {
+  } else if (warp >= 20) {
     // ------------------------------ values to fp16 ------------------------------
     constexpr int PIECES = D / 16, N = PIECES / 4;   // 16-byte pieces of a row of codes; a warp's lanes take eight rows and four pieces at a time
-    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 12) * 32;
+    const int r8 = lane & 7, pc0 = lane >> 3, rows0 = (warp - 20) * 32;
     bool ok = true;
     int J = 0;
 #pragma unroll 1
@@ -416,7 +463,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const int32_t* table = p.pages + (int64_t)plan.offsets[g.u.g] * p.max_pages;
         int v = -1000;
 #pragma unroll 1
-        for (int i = g.jb * ppt + tid - 384; i < min((g.jb + g.n) * ppt, g.u.blocks); i += 128) {
+        for (int i = g.jb * ppt + tid - 640; i < min((g.jb + g.n) * ppt, g.u.blocks); i += 128) {
           const int page = table[i];
           if (page < 0 || page >= p.n_pages) continue;
           const int e = scale_exp(p.vs[page * p.Hkv + g.u.hk]);
@@ -425,14 +472,15 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         v = __reduce_max_sync(0xffffffffu, v);
         if (lane == 0) {
           // (four sets: with a tile of segment X to come, that of X - 3 has at least been used)
-          s_vmax[4 * (seg & 3) + warp - 12] = v;
+          s_vmax[4 * (seg & 3) + warp - 20] = v;
           tc::mbar_arrive(&bars[SB_VBASE + (seg & 3)]);
         }
       }
+      ok = tc::mbar_wait_tight(&bars[SB_QFULL], seg & 1);   // (the queries lay where the first tiles go)
 #pragma unroll 1
       for (int j = 0; j < g.n; ++j, ++J) {
         const int sv = J & 1, s8 = J % Cfg::NV8;
-        bool good = tc::mbar_wait_tight(&bars[SB_V8FULL + s8], (J / Cfg::NV8) & 1);
+        bool good = ok && tc::mbar_wait_tight(&bars[SB_V8FULL + s8], (J / Cfg::NV8) & 1);
         if (good && J >= 2) good = tc::mbar_wait_tight(&bars[SB_VFREE + sv], ((J >> 1) - 1) & 1);
         ok = __all_sync(0xffffffffu, good);
         if (!ok) break;
@@ -454,8 +502,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         for (int i = 0; i < 4 * N; ++i) {
           const int r = rows0 + 8 * (i / N) + r8, pc = pc0 + 4 * (i % N);
           uint4 lo, hi;
-          lo.x = e4m3x2_to_f16x2(c[i].x & 0xffff); lo.y = e4m3x2_to_f16x2(c[i].x >> 16); lo.z = e4m3x2_to_f16x2(c[i].y & 0xffff); lo.w = e4m3x2_to_f16x2(c[i].y >> 16);
-          hi.x = e4m3x2_to_f16x2(c[i].z & 0xffff); hi.y = e4m3x2_to_f16x2(c[i].z >> 16); hi.z = e4m3x2_to_f16x2(c[i].w & 0xffff); hi.w = e4m3x2_to_f16x2(c[i].w >> 16);
+          widen4(c[i].x, lo.x, lo.y); widen4(c[i].y, lo.z, lo.w);
+          widen4(c[i].z, hi.x, hi.y); widen4(c[i].w, hi.z, hi.w);
           uint8_t* at = dst + (pc >> 2) * (128 * 128) + r * 128;
           *reinterpret_cast<uint4*>(at + (((2 * (pc & 3)) ^ r8) << 4)) = lo;
           *reinterpret_cast<uint4*>(at + (((2 * (pc & 3) + 1) ^ r8) << 4)) = hi;
@@ -471,33 +519,60 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!ok && lane == 0) fail();
   } else {
     // ------------------------------ q; softmax; results ------------------------------
-    const int st = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const int st = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, pair = 2 + 4 * st + quarter;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), tS = lanes + Cfg::COL_S + 128 * st, tO = lanes + Cfg::COL_O + 128 * st;
-    auto rows_barrier = []() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+    float* s_x = reinterpret_cast<float*>(base + Cfg::OFF_X) + st * 256;   // [half][128]
+    auto rows_barrier = []() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
     bool ok = true;
-    int it = 0, J0 = 0;   // tiles of this stream, of the CTA
+    int turn = 0, J0 = 0;   // turns of this stream, tiles of the CTA
+    Walk& walk = *reinterpret_cast<Walk*>(base + Cfg::OFF_WALK);
+    if (tid == 128) {
+      walk.plan = plan;
+      walk.f = walk.w0 = w0;
+      walk.w1 = w1;
+    }
 #pragma unroll 1
-    for (int seg = 0; next_segment(f, g); ++seg) {
+    for (int seg = 0;; ++seg) {
+      if (tid == 128 && !segment_at(args, walk.plan, walk.w0, walk.w1, walk.f, walk.g)) walk.g.n = 0;
+      rows_barrier();
+      const Segment& g = walk.g;   // (nobody reads it any more when all have passed the barrier behind the results)
+      if (g.n == 0) break;
       const bool tall = g.u.tall();
-      const int b0 = plan.offsets[g.u.g];
+      const int b0 = walk.plan.offsets[g.u.g], padded = tall ? 256 : 128;
+      uint8_t* raw = base + Cfg::OFF_V;   // the queries as they are (the converting warps wait for them to be used up)
+      {
+        constexpr int CPR = D / 8;        // 16-byte pieces of a row
+#pragma unroll 1
+        for (int i = tid - 128; i < padded * CPR; i += 512) {
+          const int r = i / CPR, c = i % CPR;
+          uint4* dst = reinterpret_cast<uint4*>(raw + r * (2 * D) + ((c ^ (r & 7)) << 4));
+          if (r >= g.u.n) {
+            *dst = make_uint4(0, 0, 0, 0);
+            continue;
+          }
+          const Row rw = row_of(args, b0, g.u.row0 + r);
+          const __nv_bfloat16* src = a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 8 * c;
+          if (args.q_vec) {
+            copy16_async(dst, src);
+          } else {
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[e] = src[e];
+          }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        rows_barrier();
+      }
       {
         // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys; D / 16 threads per row
         constexpr int TPR = D / 16;
-        const int items = (tall ? 256 : 128) * TPR;
-#pragma unroll 2
-        for (int i = tid - 128; i < items; i += 256) {
+#pragma unroll 1
+        for (int i = tid - 128; i < padded * TPR; i += 512) {
           const int r = i / TPR, piece = i % TPR;
-          uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-          if (r < g.u.n) {
-            const Row rw = row_of(args, b0, g.u.row0 + r);
-            const __nv_bfloat16* src = a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
-            if (args.q_vec) {
-              const uint4 u = *reinterpret_cast<const uint4*>(src), v = *reinterpret_cast<const uint4*>(src + 8);
-              x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = (uint32_t)__bfloat16_as_ushort(src[2 * e]) | ((uint32_t)__bfloat16_as_ushort(src[2 * e + 1]) << 16);
-            }
+          uint32_t x[8];
+          {
+            const uint4 u = *reinterpret_cast<const uint4*>(raw + r * (2 * D) + (((2 * piece) ^ (r & 7)) << 4));
+            const uint4 v = *reinterpret_cast<const uint4*>(raw + r * (2 * D) + (((2 * piece + 1) ^ (r & 7)) << 4));
+            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
           }
           uint32_t top2 = 0;
 #pragma unroll
@@ -532,63 +607,53 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       if (bad) cq = 0.f;
       ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_VBASE + (seg & 3)], (seg >> 2) & 1));
       const int* vm = s_vmax + 4 * (seg & 3);
-      const int vb = max(max(vm[0], vm[1]), max(vm[2], vm[3])), vbase = vb == -1000 ? 0 : vb;
-      float m = -INFINITY, l = 0.f;   // l in units of 2^(m - kShift)
-      const int step = tall ? 1 : 2;
+      const int vb = max(max(vm[0], vm[1]), max(vm[2], vm[3]));
+      const float vbase = vb == -1000 ? 0.f : (float)vb;
+      float m = 0.f, l = 0.f, sum = 0.f;   // reference (whole numbers); sums of the thread's weights: before the last tile, of the last tile
+      int left = tall ? g.n : (g.n + 1 - st) >> 1, tile = J0 + (tall ? 0 : st) - (tall ? 1 : 2);
+      const int ntiles = g.n;
+      bool first = true, held = false;     // the stream's first tile of the segment; weights that are not given away: the reference will not do
 #pragma unroll 1
-      for (int j = tall ? 0 : st; j < g.n && ok; j += step, ++it) {
-        ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SFULL + st], it & 1));
+      while (ok) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SFULL + st], turn & 1));
         if (!ok) break;
         tc::tc_fence_after();
-        const KeyTile& ti = info[(J0 + j) % kInfo];
-        if (ti.flags) bad = true;
-        const int n = ti.n;
-        uint32_t pr[2][32];   // weights, two to a word
-        float sum = 0.f;
-#pragma unroll 1
-        for (int turn = 0; turn < 2; ++turn) {
-          const float neg_m = m == -INFINITY ? 0.f : kShift - m;
+        const bool redo = s_redo[st] == turn;   // (uniform)
+        if (!redo) {
+          l += sum;
+          if (left == 0) break;                 // the end: all products have landed
+          first = tile < J0;
+          tile += tall ? 1 : 2;
+          --left;
+        }
+        const KeyTile& ti = info[tile % kInfo];
+        const int n = ti.n - 64 * half;         // the half's columns that are there: pages are whole, 16 columns are there or not
+        if (redo) {
+          // Some row of the stream has weights beyond the range.  A new reference for the row, the largest y (or logit - kHigh) of the halves whose weights
+          // are held back; the other half's are shifted to it where they lie.
           float mx = -INFINITY;
-          sum = 0.f;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t x[32];
-            tc::tmem_ld32(tS + 32 * c, x);
-            tc::tmem_wait_ld();
-            if (n < kTile) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = 32 * c + i < n ? x[i] : 0xff800000u;
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float fac = fmaxf(cq * ti.ks[2 * c + h], 1.17549435e-38f), vr = ti.ve[2 * c + h] - (float)vbase, fold = fmaxf(vr, -(float)kFoldMost);   // (never 0: a masked column is -inf)
-              const uint64_t f2 = pack2(fac, fac), a2 = pack2(neg_m + fold, neg_m + fold);
-              uint64_t s0 = 0, s1 = 0;
+          if (held) {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              uint32_t x[16];
+              tc::tmem_ld16(tS + 64 * half + 16 * c, x);
+              tc::tmem_wait_ld();
               float m0 = -INFINITY;
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float x0 = __uint_as_float(x[16 * h + 2 * i]), x1 = __uint_as_float(x[16 * h + 2 * i + 1]);
-                m0 = tc::fmax3(m0, x0, x1);
-                float p0, p1;
-                unpack2(fma2(pack2(x0, x1), f2, a2), p0, p1);
-                p0 = tc::ex2_approx(p0);
-                p1 = tc::ex2_approx(p1);
-                const uint64_t p2 = pack2(p0, p1);
-                if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
-                pr[c >> 1][16 * (c & 1) + 8 * h + i] = vr < fold ? 0u : to_f16x2(p0, p1);
-              }
-              float l0, l1;
-              unpack2(add2(s0, s1), l0, l1);
-              sum = fmaf(l0 + l1, exp2i(-(int)fold), sum);
-              mx = fmaxf(mx, fmaf(m0, fac, fold));
+              for (int i = 0; i < 16; ++i) m0 = fmaxf(m0, __uint_as_float(x[i]));
+              const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f), fold = fmaxf(ti.ve[4 * half + c] - vbase, -(float)kFoldMost);
+              if (16 * c < n) mx = fmaxf(mx, m0 * fac + fmaxf(fold, -(float)kHigh));
             }
+          } else if (n > 0) {
+            mx = m;
           }
-          if (!__any_sync(0xffffffffu, mx > m + kRaise)) break;   // (m = -inf: the first tile)
-          // the reference moves; all earlier products of the stream have landed: its S is there
-          const float mnew = fmaxf(m, mx), corr = m == -INFINITY ? 0.f : tc::ex2_approx(m - mnew);
-          if (j >= step) {
+          s_x[128 * half + row] = mx;
+          pair_barrier(pair);
+          mx = ceilf(fmaxf(mx, s_x[128 * (1 - half) + row]));
+          const float mnew = first ? mx : fmaxf(m, mx), corr = tc::ex2_approx(m - mnew);
+          if (!first) {
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
               uint32_t r[32];
               tc::tmem_ld32(tO + c * 32, r);
               tc::tmem_wait_ld();
@@ -596,56 +661,114 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
               for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
               tc::tmem_st32(tO + c * 32, r);
             }
-            tc::tmem_wait_st();
+            l *= corr;
           }
-          l *= corr;
           m = mnew;
+          if (!held) {
+            uint32_t r[32];
+            tc::tmem_ld32(tS + 64 * half, r);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = to_bf16x2(__uint_as_float(r[i] << 16) * corr, __uint_as_float(r[i] & 0xffff0000u) * corr);
+            tc::tmem_st32(tS + 64 * half, r);
+            sum *= corr;
+          }
         }
-        l += sum;
-        tc::tmem_st32(tS, pr[0]);   // (columns that the warp has read)
-        tc::tmem_st32(tS + 32, pr[1]);
+        if (!redo || held) {
+          if (ti.flags) bad = true;
+          uint32_t pr[32];   // weights of columns 64 half .. + 63, two to a word
+          const float neg_m = (float)kBias - m;
+          float top = 0.f, low = 0.f;   // largest sum of 16 weights, without and with the values' scales
+          sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t x[16];
+            tc::tmem_ld16(tS + 64 * half + 16 * c, x);
+            const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f);   // (never 0: what is not there is -inf)
+            const float vr = ti.ve[4 * half + c] - vbase, fold = fmaxf(vr, -(float)kFoldMost);
+            const uint64_t f2 = pack2(fac, fac), a2 = pack2(neg_m + fold, neg_m + fold);
+            tc::tmem_wait_ld();
+            if (n <= 16 * c) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[i] = 0xff800000u;
+            }
+            uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float p0, p1;
+              unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, a2), p0, p1);
+              const uint32_t w = to_bf16x2(tc::ex2_approx(p0), tc::ex2_approx(p1));
+              // (the row sum takes the weights as the products get them, so that their rounding does not shift a flat row)
+              const uint64_t p2 = pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+              if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
+              pr[8 * c + i] = w;
+            }
+            if (vr < fold) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) pr[8 * c + i] = 0;
+            }
+            float l0, l1;
+            unpack2(add2(s0, s1), l0, l1);
+            l0 += l1;
+            l1 = l0 * exp2i(-(int)fold - kBias);
+            sum += l1;
+            top = fmaxf(top, l1);
+            low = fmaxf(low, l0);
+          }
+          // in range: no sum of 16 above 2^kHigh (infinite ones among them); in the first tile, where the reference is a guess, one above 2^-kLow
+          held = !redo && __any_sync(0xffffffffu, top > 1.15e18f || (first && n > 0 && low < 1.6e7f));   // (2^60; 2^(kBias - kLow))
+          if (!held) tc::tmem_st32(tS + 64 * half, pr);   // (columns that the warp has read)
+          else if (lane == 0) s_flag[st] = turn;
+        }
         tc::tmem_wait_st();
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&bars[SB_PREADY + st]);
+        ++turn;
       }
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_LAST], seg & 1));
+      ++turn;
       tc::tc_fence_after();
-      const bool any = g.n > (tall ? 0 : st);   // (the odd stream may have had no tile)
-      float* mine = args.part + (g.u.slot(blockIdx.x) + st * g.u.pitch) * (D + 2);
-      const int rg = (tall ? 128 * st : 0) + row;
-      const float nan = __int_as_float(0x7fc00000), unit = bad ? nan : exp2i(vbase - kUnitExp);
-      const bool live = ok && rg < g.u.n;
-      if (any) {
-#pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t r[32];
-          tc::tmem_ld32(tO + c * 32, r);
-          tc::tmem_wait_ld();
-          if (live) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * g.u.pitch + row] = __uint_as_float(r[i]) * unit;
-          }
-        }
-      }
-      if (live) {
-        mine[D * g.u.pitch + row] = any ? m - kShift : -INFINITY;
-        mine[(D + 1) * g.u.pitch + row] = !any ? 0.f : bad ? nan : l;
-      }
-      tc::tc_fence_before();   // (O has been read: the next product may be issued behind the barriers to come)
-      J0 += g.n;
+      // the two halves' sums; whether all are well, and so whether there is a next time: the same for all
+      s_x[128 * half + row] = l;
       {
-        uint32_t r;   // whether all are well, and so whether there is a next time: the same for all
+        uint32_t r;
+        __syncwarp();
         asm volatile(
             "{\n\t.reg .pred p, q;\n\t"
             "setp.ne.u32 p, %1, 0;\n\t"
-            "barrier.cta.red.and.aligned.pred q, 1, 256, p;\n\t"
+            "barrier.cta.red.and.aligned.pred q, 1, 512, p;\n\t"
             "selp.u32 %0, 1, 0, q;\n\t}"
             : "=r"(r) : "r"(ok && !*abort_flag ? 1u : 0u) : "memory");
         ok = r != 0;
       }
       if (!ok) break;
+      const bool any = g.n > (tall ? 0 : st);   // (the odd stream may have had no tile)
+      float* mine = args.part + (g.u.slot(blockIdx.x) + st * g.u.pitch) * (D + 2);
+      const float nan = __int_as_float(0x7fc00000), low_values = vbase > 0.f ? 0.f : (float)(kCode - kBias);   // (so that neither the largest nor the smallest leave fp32's range)
+      const float unit = bad ? nan : exp2i((int)vbase - kUnitExp + (int)low_values);
+      const bool live = (tall ? 128 * st : 0) + row < g.u.n;
+      if (any) {
+#pragma unroll 1
+        for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
+          uint32_t r[32];
+          tc::tmem_ld32(tO + c * 32, r);
+          tc::tmem_wait_ld();
+          if (live) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) mine[(c * 32 + channel_of(i)) * g.u.pitch + row] = __uint_as_float(r[i]) * unit;
+          }
+        }
+      }
+      if (live && half == 0) {
+        const float ref = (float)(kCode - kBias) - low_values;
+        mine[D * g.u.pitch + row] = any ? m + ref : -INFINITY;
+        mine[(D + 1) * g.u.pitch + row] = !any ? 0.f : bad ? nan : (s_x[row] + s_x[128 + row]) * exp2i(-(int)ref);
+      }
+      tc::tc_fence_before();   // (O has been read: the next product may be issued behind the barriers to come)
+      J0 += ntiles;
+      rows_barrier();
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (!ok) fail();
   }
   tc::tc_fence_before();
@@ -688,33 +811,55 @@ __global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant
   float m = -INFINITY, l = 0.f, o[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) o[i] = 0.f;
-  auto add = [&](const float* x, int64_t step, int64_t at_m, int64_t at_l, float below) {   // a partial result: channel i at x[i * step], m, l
-    const float mz = x[at_m] - below, lz = x[at_l];
-    float v[CH];
+  // Partial results z = 0 .. n - 1 at x + z * next (z = 0: at x0): channel i at [i * step], m, l; FOUR of them on their way at a time.
+  auto add = [&](const float* x0, const float* x, int64_t next, int count, int64_t step, float below) {
+    constexpr int FOUR = 4;
+    const int64_t at_m = (D - c0) * step, at_l = at_m + step;
+    for (int z0 = 0; z0 < count; z0 += FOUR) {
+      float mz[FOUR], lz[FOUR], v[FOUR][CH];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) v[i] = x[i * step];
-    if (mz == -INFINITY && lz == lz) return;   // (nothing was looked at there)
-    const float mn = fmaxf(m, mz), f0 = m == -INFINITY ? 0.f : tc::ex2_approx(m - mn), f1 = mz == -INFINITY ? 0.f : tc::ex2_approx(mz - mn);
-    l = lz == lz ? fmaf(l, f0, lz * f1) : lz;   // (a NaN row stays one where its weight is 0)
+      for (int k = 0; k < FOUR; ++k) {
+        const float* y = z0 + k == 0 ? x0 : x + (z0 + k) * next;
+        mz[k] = -INFINITY;
+        lz[k] = 0.f;
+        if (z0 + k < count) {
+          mz[k] = y[at_m] - below;
+          lz[k] = y[at_l];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) o[i] = fmaf(o[i], f0, v[i] * f1);
-    m = mn;
-  };
-  // the shared blocks
-  if (u.tiles > 0) {
-    const int64_t ch = (int64_t)c0 * u.pitch;
-    const int rr = row & (u.tall() ? 127 : 255);
-    for (int cta = u.begin / plan.share; cta <= (u.begin + u.tiles * u.w - 1) / plan.share; ++cta) {
-      int jb, je;
-      u.of(cta * plan.share, plan.share, jb, je);
-      if (jb >= je) continue;
-      const float* x = s.part + (u.slot(cta) + (u.tall() && row >= 128 ? u.pitch : 0)) * (D + 2) + rr;
-      add(x + ch, u.pitch, (int64_t)(D - c0) * u.pitch, (int64_t)(D + 1 - c0) * u.pitch, 0.f);
-      if (!u.tall()) {
-        x += (int64_t)u.pitch * (D + 2);
-        add(x + ch, u.pitch, (int64_t)(D - c0) * u.pitch, (int64_t)(D + 1 - c0) * u.pitch, 0.f);
+          for (int i = 0; i < CH; ++i) v[k][i] = y[i * step];
+        }
+      }
+      float mn = m;
+#pragma unroll
+      for (int k = 0; k < FOUR; ++k) mn = fmaxf(mn, mz[k]);
+      const float f0 = m == -INFINITY ? 0.f : tc::ex2_approx(m - mn);
+      l *= f0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) o[i] *= f0;
+      m = mn;
+#pragma unroll
+      for (int k = 0; k < FOUR; ++k) {
+        l = lz[k] == lz[k] ? l : lz[k];   // (a NaN row stays one where its weight is 0)
+        if (mz[k] == -INFINITY) continue;   // (nothing was looked at there)
+        const float f1 = tc::ex2_approx(mz[k] - mn);
+        l = fmaf(lz[k], f1, l);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) o[i] = fmaf(v[k][i], f1, o[i]);
       }
     }
+  };
+  // the shared blocks: the CTAs that had tiles of the unit
+  if (u.tiles > 0) {
+    int first = u.begin / plan.share, last = (u.begin + u.tiles * u.w - 1) / plan.share, jb, je;
+    u.of(first * plan.share, plan.share, jb, je);
+    if (jb >= je) ++first;                     // (at either end: a tile that counts twice belongs to the share in which it begins)
+    u.of(last * plan.share, plan.share, jb, je);
+    if (jb >= je) --last;
+    const float* x = s.part + (u.slot(first) + (u.tall() && row >= 128 ? 128 : 0)) * (D + 2) + (row & (u.tall() ? 127 : 255)) + (int64_t)c0 * u.pitch;
+    const int64_t next = 256 * (D + 2);
+    add(x, x, next, last - first + 1, u.pitch, 0.f);
+    x += (int64_t)u.pitch * (D + 2);
+    if (!u.tall()) add(x, x, next, last - first + 1, u.pitch, 0.f);
   }
   // the sequence's own
   const int64_t unit = (int64_t)rw.b * p.Hkv + hk;
@@ -722,13 +867,16 @@ __global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant
   if (s.cols == 0) {
     const int qt = col >> 7, row0 = qt * 128, last = min(n * a.G, row0 + 128) - 1;   // (as prompt_work has it)
     const int tiles = pages_of(p, start + s.by_group.div(row0), start + s.by_group.div(last), INT32_MAX, 0, blocks).tiles, per = split_tiles(tiles, s.many.nsplit);
-    const float* x = s.own + ((int64_t)(s.many.qtiles - 1 - qt) * p.batch * p.Hkv + unit) * s.many.nsplit * (D + 2) * 128 + (col & 127);
-    for (int jb = 0; jb < tiles; jb += per, x += (D + 2) * 128) add(x + c0 * 128, 128, (D - c0) * 128, (D + 1 - c0) * 128, kShift);
-  } else if (const int2 from = a.found[unit]; from.y < 0) {
-    add(a.side + (unit * s.cols + col) * (D + 2) + c0, 1, D - c0, D + 1 - c0, 8.f);
+    const float* x = s.own + ((int64_t)(s.many.qtiles - 1 - qt) * p.batch * p.Hkv + unit) * s.many.nsplit * (D + 2) * 128 + (col & 127) + c0 * 128;
+    add(x, x, (D + 2) * 128, (tiles + per - 1) / per, 128, kShift);
   } else {
-    const int z0 = max(0, from.x), z1 = min(from.y, s.workers - 1);   // (what a call leaves whose waits ran out may be anything)
-    for (int z = z0; z <= z1; ++z) add(s.own + ((int64_t)(2 * z + (z == z0)) * s.cols + col) * (D + 2) + c0, 1, D - c0, D + 1 - c0, 8.f);
+    const int2 from = a.found[unit];
+    const float* whole = a.side + (unit * s.cols + col) * (D + 2) + c0;
+    const int z0 = max(0, min(from.x, s.workers - 1)), z1 = min(from.y, s.workers - 1);   // (what a call leaves whose waits ran out may be anything)
+    const float* x = s.own + ((int64_t)2 * z0 * s.cols + col) * (D + 2) + c0;
+    const int64_t slot = (int64_t)s.cols * (D + 2);
+    if (from.y < 0) add(whole, whole, 0, 1, 1, kDecodeShift);
+    else add(x + slot, x, 2 * slot, z1 - z0 + 1, 1, kDecodeShift);   // (the first worker's share begins with the unit)
   }
   __nv_bfloat16* out = a.out + rw.b * a.so[0] + (int64_t)(hk * a.G + rw.h) * a.so[1] + rw.t * a.so[2] + c0;
   const float inv = 1.f / l;
@@ -781,7 +929,7 @@ kvm_status_t launch_shared(const SharedArgs& args, const CUtensorMap& mapK, cons
 }
 template <int D>
 kvm_status_t launch_merge(const SharedArgs& args, cudaStream_t s) {
-  constexpr int CH = 16;
+  constexpr int CH = 8;
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -402,3 +402,62 @@ def test_many_groups(kvm):
     want = c.attend(q, table, start).float()
     got = c.attend_shared(q, table, start, i32([0, B]), i32([2])).float()
     assert (got - want).abs().max() <= 2.0 ** -7 * want.abs().max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [2, 40, 70])
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_far_from_zero_and_far_apart(kvm, n, d):
+    """Heads whose logits are tiny, large, all far below zero or far above, and rows whose maximum grows by a hundred and more from tile to tile."""
+    H, P, L = 5, 64, 640
+    m = Shared(kvm, [n], [0], [0] * n, H, d, P, room=L + 200)
+    k, v = rows((n, H, L, d), 1), rows((n, H, L, d), 2)
+    u = torch.ones(d) / math.sqrt(d)
+    k[:, 1] = k[:, 1] * 0.05 + 8 * u                               # logits near q . u * 8
+    k[:, 2] = k[:, 2] * 0.05 - 8 * u
+    k[:, 3] = (k[:, 3].float() * 0.05 + 2.0 * (torch.arange(L) // 100)[:, None] * u).bfloat16()     # grows along the keys
+    k[:, 4, 400:410] *= 8.0                                        # a few keys that decide everything
+    one = [L] + [0] * (n - 1)
+    m.append(k[:1].expand(n, -1, -1, -1).contiguous(), v[:1].expand(n, -1, -1, -1).contiguous(), one)
+    for b in range(1, n):
+        m.table[b, :L // P] = m.table[0, :L // P]
+        m.k[b], m.v[b], m.len[b] = copy.deepcopy(m.k[0]), copy.deepcopy(m.v[0]), L
+    m.lead, m.shared = [L // P], i32([L // P])
+    m.append(rows((n, H, 3, d), 5), rows((n, H, 3, d), 6), [b % 4 for b in range(n)])
+    T, G = 1, 4
+    m.append(rows((n, H, T, d), 7), rows((n, H, T, d), 8), [T] * n)
+    q = rows((n, H * G, T, d), 9)
+    q[:, G:4 * G] = (q[:, G:4 * G].float() * 0.05 + 60.0 * u).bfloat16()
+    start = i32([x - T for x in m.len])
+    for scale in (1e-4, 0.1, 1.0):                                 # heads 1 and 2: logits of +- 480 and less
+        out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+        m.cache.attend_shared(q.cuda(), m.hidden(), start, m.groups, m.shared, scale=scale, out=out, status=status)
+        assert status.item() == 0
+        m.compare(q, out, [T] * n, 0, 0, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d", [(2, 64), (50, 64), (50, 128)])
+def test_values_far_below_the_largest_of_their_block(kvm, n, d):
+    """The row that sets the blocks' scale has no weight; what is left are the least codes, 1 to 7 times 2^-9: each counts in full."""
+    P, L = 64, 512
+    c = kvm.Cache.empty(L // P + n, 1, d, P)
+    codes = torch.randint(1, 8, (L, d), generator=torch.Generator().manual_seed(1)) | (torch.randint(0, 2, (L, d), generator=torch.Generator().manual_seed(2)) << 7)
+    codes[::P] = 0x7e                                              # 448
+    c.v8.view(torch.uint8)[:L // P] = codes.to(torch.uint8).view(L // P, 1, P, d).cuda()
+    c.v_scale.fill_(2.0 ** -3)
+    k = torch.zeros((L, d))
+    k[::P, 0] = -256.0
+    c.k8.view(torch.uint8)[:L // P] = k.to(torch.float8_e4m3fn).view(torch.uint8).view(L // P, 1, P, d).cuda()
+    table = torch.cat([torch.arange(L // P).repeat(n, 1), L // P + torch.arange(n)[:, None]], 1).to(torch.int32).cuda()
+    q = torch.zeros((n, 4, 1, d), dtype=torch.bfloat16)
+    q[..., 0] = 2.0
+    zero = torch.zeros((n, 1, 1, d), dtype=torch.bfloat16, device="cuda")
+    c.append(zero, zero, table, i32([L] * n))
+    out = c.attend_shared(q.cuda(), table, i32([L] * n), i32([0, n]), i32([L // P]), scale=1.0).double().cpu()
+    v = c.v8.view(torch.uint8)[:L // P].cpu().view(torch.float8_e4m3fn).double().view(L, d) * 2.0 ** -3
+    live = torch.ones(L, dtype=torch.bool)
+    live[::P] = False
+    want = v[live].sum(0) / (live.sum() + 1)                       # (its own key: weight 1, value 0)
+    # equal weights: 2^-8 for the output; sums of 2^9 terms in fp32, 2^-24 2^9 of the sum of magnitudes
+    assert (abs(out - want) <= 2.0 ** -8 * abs(want) + 2.0 ** -15 * v[live].abs().mean(0)).all(), float(abs(out - want).max())
