@@ -11,7 +11,8 @@ namespace front {
 
 using cache::AppendOut;
 
-constexpr int kFourths = 4;   // rows of a lane (tokens) in the kernels for many tokens
+constexpr int kTokens = 2;    // tokens of a lane in the kernel over many rows
+constexpr int kRows = 4;      // rows of a lane in the kernel over pages
 
 struct QkArgs {
   FrontDev f;
@@ -29,23 +30,23 @@ __device__ __forceinline__ bool qk_lengths(const QkArgs& a, int b, int& start, i
   return start >= 0 && n >= 0 && n <= a.T;
 }
 
-// One row: (b, t, head) of q or k.
-template <int D>
-__device__ __forceinline__ void row_through(const FrontDev& f, const Rows& r, const Lane<D>& L, const Raw& raw, int head, bool live, const float (&c)[4], const float (&s)[4],
+// One row through the front end.
+template <int D, int MODE>
+__device__ __forceinline__ void row_through(const FrontDev& f, const Lane<D, MODE>& L, const Raw& raw, bool live, const float (&c)[4], const float (&s)[4],
                                             const float (&wx)[4], const float (&wy)[4], const float (&bx)[4], const float (&by)[4], __nv_bfloat16* dst) {
-  float x[4], y[4];
-  to_pairs(raw, r.vx ? L.side : true, x, y);
+  float v[8], x[4], y[4];
+  values_of(raw, v);
+  to_pairs<MODE>(v, x, y);
   norm<D>(f, wx, wy, bx, by, x, y);
-  rotate<D>(L, c, s, x, y);
-  if (live) store_row<D>(dst, L, r.vy, L.side, x, y);
+  rotate(L, c, s, x, y);
+  if (live) store_row(dst, L, x, y);
 }
 
 // Few rows: D / 8 lanes per row, every row by itself.
-template <int D>
+template <int D, int MODE>
 __global__ void __launch_bounds__(128) qk_rows_kernel(const __grid_constant__ QkArgs a) {
   constexpr int LPR = D / 8;
-  const int lane = threadIdx.x % LPR;
-  const Lane<D> L(a.f.half, a.f.h, lane);
+  const Lane<D, MODE> L(a.f, threadIdx.x % LPR);
   const int H = a.r[0].H + a.r[1].H;
   const int64_t row = (int64_t)blockIdx.x * (128 / LPR) + threadIdx.x / LPR, rows = a.batch * a.T * H;
   const bool there = row < rows;
@@ -56,25 +57,24 @@ __global__ void __launch_bounds__(128) qk_rows_kernel(const __grid_constant__ Qk
   const int which = hh >= a.r[0].H, head = hh - (which ? a.r[0].H : 0);
   const Rows& r = a.r[which];
   // (a row that the lengths leave out is read all the same: it is there)
-  const Raw raw = load_raw<D>(r.x + b * r.sx[0] + head * r.sx[1] + t * r.sx[2], L, r.vx);
+  const Raw raw = load_raw(r.x + b * r.sx[0] + head * r.sx[1] + t * r.sx[2], L);
   int start, n;
   const bool valid = qk_lengths(a, b, start, n);
-  if (!valid && there && hh == 0 && t == 0 && lane == 0) cache::report(a.status, KVM_ERR_INVALID_ARG);
+  if (!valid && there && hh == 0 && t == 0 && L.i0 == 0) cache::report(a.status, KVM_ERR_INVALID_ARG);
   float wx[4], wy[4], bx[4], by[4], c[4], s[4];
-  const bool side = r.vw ? L.side : true;
-  load_affine<D>(r.w, head, L, r.vw, side, 1.f, wx, wy);
-  load_affine<D>(r.b, head, L, r.vw, side, 0.f, bx, by);
-  angles<D>(a.f, L, (int64_t)start + t, c, s);
-  row_through<D>(a.f, r, L, raw, head, there && valid && t < n, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2]);
+  load_affine(r.w, head, L, 1.f, wx, wy);
+  load_affine(r.b, head, L, 0.f, bx, by);
+  angles(a.f, L, (int64_t)start + t, c, s);
+  row_through(a.f, L, raw, there && valid && t < n, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2]);
 }
 
-// Many rows: a block takes 256 / LPR * 4 tokens (of the whole batch, one behind the other) through a run of heads.  A lane has four tokens: their
-// angles stay in registers over the heads, a head's weights over the tokens, and four rows are on their way at a time.
-template <int D, int TH, class A>
+// Many rows: a block takes 256 / LPR * 2 tokens (of the whole batch, one behind the other) through a run of heads.  A lane has two tokens: their
+// angles stay in registers over the heads, a head's weights over the tokens, and the next head's rows are on their way.
+template <int D, int MODE, class A>
 __device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t token0, int h0, int h1) {
-  constexpr int LPR = D / 8, RP = TH / LPR, CH = kFourths;
+  constexpr int LPR = D / 8, RP = 256 / LPR, CH = kTokens;
   const FrontDev& f = a.f;
-  const Lane<D> L(f.half, f.h, threadIdx.x % LPR);
+  const Lane<D, MODE> L(f, threadIdx.x % LPR);
   const __nv_bfloat16* px[CH];
   __nv_bfloat16* py[CH];
   float c[CH][4], s[CH][4];
@@ -90,29 +90,30 @@ __device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t tok
       start = n = 0;
     }
     if (t < n) live |= 1u << i;
-    px[i] = r.x + b * r.sx[0] + t * r.sx[2];
-    py[i] = r.y + b * r.sy[0] + t * r.sy[2];
-    angles<D>(f, L, start + t, c[i], s[i]);
+    px[i] = r.x + b * r.sx[0] + t * r.sx[2] + h0 * r.sx[1];
+    py[i] = r.y + b * r.sy[0] + t * r.sy[2] + h0 * r.sy[1];
+    angles(f, L, start + t, c[i], s[i]);
   }
   Raw raw[CH];
-  auto fetch = [&](int h) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) raw[i] = load_raw<D>(px[i] + h * r.sx[1], L, r.vx);
-  };
-  fetch(h0);
-  const bool side = r.vw ? L.side : true;
+  for (int i = 0; i < CH; ++i) raw[i] = load_raw(px[i], L);
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
     float wx[4], wy[4], bx[4], by[4];
-    load_affine<D>(r.w, h, L, r.vw, side, 1.f, wx, wy);
-    load_affine<D>(r.b, h, L, r.vw, side, 0.f, bx, by);
+    load_affine(r.w, h, L, 1.f, wx, wy);
+    load_affine(r.b, h, L, 0.f, bx, by);
     Raw now[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) now[i] = raw[i];
-    if (h + 1 < h1) fetch(h + 1);
+    if (h + 1 < h1) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
-      row_through<D>(f, r, L, now[i], h, live >> i & 1, c[i], s[i], wx, wy, bx, by, py[i] + h * r.sy[1]);
+      for (int i = 0; i < CH; ++i) raw[i] = load_raw(px[i] += r.sx[1], L);
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      row_through(f, L, now[i], live >> i & 1, c[i], s[i], wx, wy, bx, by, py[i]);
+      py[i] += r.sy[1];
+    }
   }
 }
 
@@ -124,11 +125,11 @@ struct QkTile {   // what rows_tile asks of a call without a cache
   __device__ bool lengths(int b, int& start, int& n) const { return qk_lengths(a, b, start, n); }
   __device__ int32_t* status_word() const { return a.status; }
 };
-template <int D>
-__global__ void __launch_bounds__(256, 2) qk_tile_kernel(const __grid_constant__ QkArgs a) {
+template <int D, int MODE>
+__global__ void __launch_bounds__(256, 3) qk_tile_kernel(const __grid_constant__ QkArgs a) {
   const int which = (int)blockIdx.y >= a.chunks[0], chunk = blockIdx.y - (which ? a.chunks[0] : 0);
   const int h0 = chunk * a.heads;
-  rows_tile<D, 256>(QkTile{a, a.f}, a.r[which], (int64_t)blockIdx.x * (256 / (D / 8) * kFourths), h0, min(h0 + a.heads, a.r[which].H));
+  rows_tile<D, MODE>(QkTile{a, a.f}, a.r[which], (int64_t)blockIdx.x * (256 / (D / 8) * kTokens), h0, min(h0 + a.heads, a.r[which].H));
 }
 
 // ---- into the cache ----------------------------------------------------------------------------------------------------------
@@ -139,10 +140,11 @@ struct IngestArgs {
   Rows q, k, v;         // (k.y, v.y and their strides are not used)
   AppendOut o;
   int chunks_q, heads_q, chunks, heads;       // head chunks of q; of k and v
+  int tpp;              // threads per page
   int groups;           // blocks that share the pages of one sequence
-  int64_t kv_blocks;    // blocks of k, and as many of v; those of q follow
+  int64_t k_blocks;     // blocks of k, those of v follow
 };
-struct IngestTile {
+struct IngestTile {     // what rows_tile asks of a call over a cache
   const IngestArgs& a;
   const FrontDev& f;
   __device__ int64_t tokens() const { return a.p.T; }
@@ -160,9 +162,9 @@ __device__ __forceinline__ void codes_of(const float (&v)[8], float inv, uint32_
   a = cache::to_e4m3x2(v[0] * inv, v[1] * inv) | (cache::to_e4m3x2(v[2] * inv, v[3] * inv) << 16);
   b = cache::to_e4m3x2(v[4] * inv, v[5] * inv) | (cache::to_e4m3x2(v[6] * inv, v[7] * inv) << 16);
 }
-template <int D>
-__device__ __forceinline__ void store_codes(uint8_t* row, const Lane<D>& L, bool runs, uint32_t a, uint32_t b) {
-  if (runs) {
+template <int D, int MODE>
+__device__ __forceinline__ void store_codes(uint8_t* row, const Lane<D, MODE>& L, uint32_t a, uint32_t b) {
+  if (MODE != kSingle) {
     *reinterpret_cast<uint32_t*>(row + L.c0) = a;
     *reinterpret_cast<uint32_t*>(row + L.c1) = b;
   } else {   // (x0 y0 x1 y1 ...)
@@ -179,22 +181,22 @@ __device__ __forceinline__ uint32_t rescaled4(uint32_t w, float m) {
   return cache::to_e4m3x2(a.x * m, a.y * m) | (cache::to_e4m3x2(b.x * m, b.y * m) << 16);
 }
 
-// The pages of one sequence, k or v, through a run of heads: TPP threads per page, four rows per thread; see append_kernel for the scale and
+// The pages of one sequence, k or v, through a run of heads: tpp threads per page, four rows per thread; see append_kernel for the scale and
 // the codes, which follow the maximum over the rows of a page.
-template <int D, int TPP, int TH, bool KEYS>
+template <int D, int TH, int MODE, bool KEYS>
 __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int chunk, int b) {
-  constexpr int LPR = D / 8, RP = TPP / LPR, CH = kFourths, WARPS = TH / 32;
-  __shared__ uint32_t s_top[2][WARPS];
+  constexpr int LPR = D / 8, CH = kRows;
+  __shared__ uint32_t s_top[2][TH / 32];
   const cache::Params& p = a.p;
   const Rows& r = KEYS ? a.k : a.v;
-  FrontDev const& f = a.f;
-  const int tt = threadIdx.x % TPP, warp = threadIdx.x >> 5;
+  const FrontDev& f = a.f;
+  const int tpp = a.tpp, tt = threadIdx.x & (tpp - 1), warp = threadIdx.x >> 5, step = tpp / LPR;   // rows of a lane: tt / LPR + i * step
   int start, n;
   if (!cache::seq_lengths(p, b, start, n)) {   // (the same for the whole block)
     if (KEYS && group == 0 && chunk == 0 && threadIdx.x == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
     return;
   }
-  const int block0 = (start >> p.page_shift) + group * (TH / TPP), block = block0 + threadIdx.x / TPP;
+  const int per = TH / tpp, block0 = (start >> p.page_shift) + group * per, block = block0 + threadIdx.x / tpp;
   if ((int64_t)block0 << p.page_shift >= (int64_t)start + n) return;   // (so is this)
   const int64_t pos0 = (int64_t)block << p.page_shift;
   const int r0 = (int)max((int64_t)0, start - pos0);                           // rows [0, r0) are held, [r0, r1) are new
@@ -208,55 +210,52 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
     }
   }
   const bool live = r1 > r0;
-  const Lane<D> L(KEYS && f.half, KEYS ? f.h : 0, tt % LPR);   // (values: eight channels side by side)
-  const bool runs = !L.half || (L.h & 3) == 0;
-  const __nv_bfloat16* px[CH];
+  const Lane<D, MODE> L(f, tt % LPR);
+  const int h0 = chunk * a.heads, h1 = min(h0 + a.heads, p.Hkv), row0 = tt / LPR;
+  const __nv_bfloat16* px = r.x + b * r.sx[0] + h0 * r.sx[1] + (pos0 + row0 - start) * r.sx[2];   // (rows in front of the call's: not looked at)
   float c[CH][4], s[CH][4];
   uint32_t fresh = 0;
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
-    const int row = tt / LPR + i * RP;
-    const bool in = row >= r0 && row < r1;
-    if (in) fresh |= 1u << i;
-    const int64_t t = in ? pos0 + row - start : 0;
-    px[i] = r.x + b * r.sx[0] + t * r.sx[2];
-    if (KEYS && in) angles<D>(f, L, pos0 + row, c[i], s[i]);
+    const int row = row0 + i * step;
+    if (row >= r0 && row < r1) {
+      fresh |= 1u << i;
+      if (KEYS) angles(f, L, pos0 + row, c[i], s[i]);
+    }
   }
-  const int h0 = chunk * a.heads, h1 = min(h0 + a.heads, p.Hkv);
-#pragma unroll 1
-  for (int h = h0; h < h1; ++h) {
-    const int64_t unit = (int64_t)page * p.Hkv + h;
-    uint8_t* codes = a.o.codes[KEYS ? 0 : 1] + unit * p.page * D;
-    float* scale = a.o.scales[KEYS ? 0 : 1] + unit;
-    const float old = live && r0 > 0 ? *scale : 0.f;
-    Raw raw[CH];
+  auto fetch = [&](Raw (&raw)[CH]) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       raw[i].a = raw[i].b = make_uint2(0, 0);
-      if (fresh >> i & 1) raw[i] = load_raw<D>(px[i] + h * r.sx[1], L, r.vx);
+      if (fresh >> i & 1) raw[i] = load_raw(px + i * step * r.sx[2], L);
     }
+  };
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h, px += r.sx[1]) {
+    const int64_t unit = (int64_t)page * p.Hkv + h;
+    uint8_t* codes = a.o.codes[KEYS ? 0 : 1] + (unit * p.page + row0) * D;
+    float* scale = a.o.scales[KEYS ? 0 : 1] + unit;
+    const float old = live && r0 > 0 ? *scale : 0.f;
+    Raw raw[CH];
+    fetch(raw);
     float v[CH][8];
     uint32_t top = 0;
     if (KEYS) {
       float wx[4], wy[4], bx[4], by[4];
-      const bool side = r.vw ? L.side : true;
-      load_affine<D>(r.w, h, L, r.vw, side, 1.f, wx, wy);
-      load_affine<D>(r.b, h, L, r.vw, side, 0.f, bx, by);
+      load_affine(r.w, h, L, 1.f, wx, wy);
+      load_affine(r.b, h, L, 0.f, bx, by);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         float x[4], y[4];
-        to_pairs(raw[i], r.vx ? L.side : true, x, y);
+        values_of(raw[i], v[i]);
+        to_pairs<MODE>(v[i], x, y);
         norm<D>(f, wx, wy, bx, by, x, y);
-        rotate<D>(L, c[i], s[i], x, y);
-        from_pairs(x, y, runs ? L.side : true, v[i]);
+        rotate(L, c[i], s[i], x, y);
+        from_pairs<MODE>(x, y, v[i]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        float x[4], y[4];
-        to_pairs(raw[i], r.vx ? L.side : true, x, y);
-        from_pairs(x, y, runs ? L.side : true, v[i]);
-      }
+      for (int i = 0; i < CH; ++i) values_of(raw[i], v[i]);
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i)
@@ -265,13 +264,13 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
         for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
       }
     top = __reduce_max_sync(0xffffffffu, top);
-    if (TPP > 32) {
+    if (tpp > 32) {   // (uniform)
       const int at = (h - h0) & 1;   // (two sets: a thread is never two heads ahead of another)
       if ((threadIdx.x & 31) == 0) s_top[at][warp] = top;
       __syncthreads();
-      const int w0 = warp / (TPP / 32) * (TPP / 32);
-#pragma unroll
-      for (int w = 0; w < TPP / 32; ++w) top = max(top, s_top[at][w0 + w]);
+      const int warps = tpp / 32, w0 = warp & ~(warps - 1);
+#pragma unroll 1
+      for (int w = 0; w < warps; ++w) top = max(top, s_top[at][w0 + w]);
     } else {
       __syncwarp();   // (every lane has read the old scale before one writes the new one)
     }
@@ -280,17 +279,16 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
     const bool poisoned = top >= 0x7f800000u || e_old > 127;
     const int e = max(least_exp(top), e_old);
     if (tt == 0) *scale = poisoned ? __int_as_float(0x7fc00000) : cache::exp2i(e);
-    const float inv = poisoned ? 0.f : cache::exp2i(-e);
-    const float down = e - e_old > 126 ? 0.f : cache::exp2i(e_old - e);
+    const float inv = cache::exp2i(-e);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int row = tt / LPR + i * RP;
-      uint8_t* dst = codes + (int64_t)row * D;
+      uint8_t* dst = codes + i * step * D;
       if (fresh >> i & 1) {
         uint32_t ca = 0, cb = 0;
         if (!poisoned) codes_of(v[i], inv, ca, cb);
-        store_codes<D>(dst, L, runs, ca, cb);
-      } else if (row < r0 && e > e_old && !poisoned) {
+        store_codes(dst, L, ca, cb);
+      } else if (row0 + i * step < r0 && e > e_old && !poisoned) {
+        const float down = e - e_old > 126 ? 0.f : cache::exp2i(e_old - e);
         uint2* held = reinterpret_cast<uint2*>(dst + (tt % LPR) * 8);
         const uint2 w = *held;
         *held = make_uint2(rescaled4(w.x, down), rescaled4(w.y, down));
@@ -299,64 +297,40 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
   }
 }
 
-template <int D, int TPP, int TH>
-__global__ void __launch_bounds__(TH, 512 / TH) ingest_kernel(const __grid_constant__ IngestArgs a) {
+template <int D, int TH, int MODE>
+__global__ void __launch_bounds__(TH, 512 / TH) ingest_pages_kernel(const __grid_constant__ IngestArgs a) {
   int64_t i = blockIdx.x;
-  const bool q = i >= 2 * a.kv_blocks;
-  if (q) {
-    i -= 2 * a.kv_blocks;
-    const int chunk = (int)(i % a.chunks_q), h0 = chunk * a.heads_q;
-    rows_tile<D, TH>(IngestTile{a, a.f}, a.q, i / a.chunks_q * (TH / (D / 8) * kFourths), h0, min(h0 + a.heads_q, a.q.H));
-    return;
-  }
-  const bool keys = i < a.kv_blocks;
-  if (!keys) i -= a.kv_blocks;
+  const bool keys = i < a.k_blocks;
+  if (!keys) i -= a.k_blocks;
   const int chunk = (int)(i % a.chunks);
   i /= a.chunks;
   const int group = (int)(i % a.groups), b = (int)(i / a.groups);
-  if (keys) pages_tile<D, TPP, TH, true>(a, group, chunk, b);
-  else pages_tile<D, TPP, TH, false>(a, group, chunk, b);
+  if (keys) pages_tile<D, TH, MODE, true>(a, group, chunk, b);
+  else pages_tile<D, TH, MODE == kSingle ? kSingle : kSide, false>(a, group, chunk, b);
+}
+template <int D, int MODE>
+__global__ void __launch_bounds__(256, 3) ingest_q_kernel(const __grid_constant__ IngestArgs a) {
+  const int h0 = blockIdx.y * a.heads_q;
+  rows_tile<D, MODE>(IngestTile{a, a.f}, a.q, (int64_t)blockIdx.x * (256 / (D / 8) * kTokens), h0, min(h0 + a.heads_q, a.q.H));
 }
 
 // One token per sequence: a warp per row of k or v, D / 8 lanes per row of q.
-template <int D>
-__global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant__ IngestArgs a) {
+template <int D, int MODE, bool KEYS>
+__device__ __forceinline__ void token_into(const IngestArgs& a, int64_t unit_of_call) {
   constexpr int LPR = D / 8;
   const cache::Params& p = a.p;
   const FrontDev& f = a.f;
-  const int lane = threadIdx.x & 31, sub = lane % LPR;
-  Lane<D> L(f.half, f.h, sub);
-  int64_t warp = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int64_t units = (int64_t)p.batch * p.Hkv;
-  float c[4], s[4], wx[4], wy[4], bx[4], by[4];
-  if (warp >= 2 * units) {   // ---- q ----
-    const Rows& r = a.q;
-    if (r.H == 0) return;    // (a block's warps beyond the work of a call without q)
-    int64_t row = (warp - 2 * units) * (32 / LPR) + lane / LPR;
-    const bool there = row < (int64_t)p.batch * r.H;
-    if (!there) row = 0;
-    const int b = (int)(row / r.H), h = (int)(row - (int64_t)b * r.H);
-    const Raw raw = load_raw<D>(r.x + b * r.sx[0] + h * r.sx[1], L, r.vx);
-    const bool side = r.vw ? L.side : true;
-    load_affine<D>(r.w, h, L, r.vw, side, 1.f, wx, wy);
-    load_affine<D>(r.b, h, L, r.vw, side, 0.f, bx, by);
-    int start, n;
-    const bool valid = cache::seq_lengths(p, b, start, n);
-    angles<D>(f, L, start, c, s);
-    row_through<D>(f, r, L, raw, h, there && valid && n > 0, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + h * r.sy[1]);
-    return;
-  }
-  const bool keys = warp < units;
-  if (!keys) { warp -= units; L = Lane<D>(false, 0, sub); }   // (values: eight channels side by side)
-  const Rows& r = keys ? a.k : a.v;
-  const int b = (int)(warp / p.Hkv), h = (int)(warp - (int64_t)b * p.Hkv);
-  const Raw raw = load_raw<D>(r.x + b * r.sx[0] + h * r.sx[1], L, r.vx);   // (there whatever the lengths are)
-  const bool side = r.vw ? L.side : true;
-  load_affine<D>(keys ? r.w : nullptr, h, L, r.vw, side, 1.f, wx, wy);
-  load_affine<D>(keys ? r.b : nullptr, h, L, r.vw, side, 0.f, bx, by);
+  const int lane = threadIdx.x & 31;
+  const Lane<D, MODE> L(f, lane % LPR);
+  const Rows& r = KEYS ? a.k : a.v;
+  const int b = (int)(unit_of_call / p.Hkv), h = (int)(unit_of_call - (int64_t)b * p.Hkv);
+  const Raw raw = load_raw(r.x + b * r.sx[0] + h * r.sx[1], L);   // (there whatever the lengths are)
+  float wx[4], wy[4], bx[4], by[4], c[4], s[4];
+  load_affine(KEYS ? r.w : nullptr, h, L, 1.f, wx, wy);
+  load_affine(KEYS ? r.b : nullptr, h, L, 0.f, bx, by);
   int start, n;
   if (!cache::seq_lengths(p, b, start, n)) {
-    if (keys && h == 0 && lane == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
+    if (KEYS && h == 0 && lane == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
     return;
   }
   if (n == 0) return;
@@ -366,18 +340,19 @@ __global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant
     return;
   }
   const int64_t unit = (int64_t)page * p.Hkv + h;
-  uint8_t* codes = a.o.codes[keys ? 0 : 1] + unit * p.page * D;
-  float* scale = a.o.scales[keys ? 0 : 1] + unit;
+  uint8_t* codes = a.o.codes[KEYS ? 0 : 1] + unit * p.page * D;
+  float* scale = a.o.scales[KEYS ? 0 : 1] + unit;
   const float old = r0 > 0 ? *scale : 0.f;
-  float x[4], y[4], v[8];
-  to_pairs(raw, r.vx ? L.side : true, x, y);
-  if (keys) {
-    angles<D>(f, L, start, c, s);
+  float v[8];
+  values_of(raw, v);
+  if (KEYS) {
+    float x[4], y[4];
+    to_pairs<MODE>(v, x, y);
+    angles(f, L, start, c, s);
     norm<D>(f, wx, wy, bx, by, x, y);
-    rotate<D>(L, c, s, x, y);
+    rotate(L, c, s, x, y);
+    from_pairs<MODE>(x, y, v);
   }
-  const bool runs = !L.half || (L.h & 3) == 0;
-  from_pairs(x, y, runs ? L.side : true, v);
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
@@ -390,9 +365,9 @@ __global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant
   if (lane < LPR) {
     uint32_t ca = 0, cb = 0;
     if (!poisoned) codes_of(v, cache::exp2i(-e), ca, cb);
-    store_codes<D>(codes + (int64_t)r0 * D, L, runs, ca, cb);
+    store_codes(codes + (int64_t)r0 * D, L, ca, cb);
   }
-  if (e > e_old && !poisoned) {   // (never where the row starts the page: r0 = 0)
+  if (e > e_old && !poisoned) {   // (r0 = 0: nothing is held)
     const float down = e - e_old > 126 ? 0.f : cache::exp2i(e_old - e);
 #pragma unroll 1
     for (int i = lane; i < r0 * (D / 16); i += 32) {
@@ -400,6 +375,33 @@ __global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant
       const uint4 w = *held;
       *held = make_uint4(rescaled4(w.x, down), rescaled4(w.y, down), rescaled4(w.z, down), rescaled4(w.w, down));
     }
+  }
+}
+template <int D, int MODE>
+__global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant__ IngestArgs a) {
+  constexpr int LPR = D / 8;
+  const cache::Params& p = a.p;
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), units = (int64_t)p.batch * p.Hkv;
+  if (warp < units) {
+    token_into<D, MODE, true>(a, warp);
+  } else if (warp < 2 * units) {
+    token_into<D, MODE == kSingle ? kSingle : kSide, false>(a, warp - units);
+  } else if (a.q.H > 0) {   // (without q: a block's warps beyond the work)
+    const Lane<D, MODE> L(a.f, lane % LPR);
+    const Rows& r = a.q;
+    int64_t row = (warp - 2 * units) * (32 / LPR) + lane / LPR;
+    const bool there = row < (int64_t)p.batch * r.H;
+    if (!there) row = 0;
+    const int b = (int)(row / r.H), h = (int)(row - (int64_t)b * r.H);
+    const Raw raw = load_raw(r.x + b * r.sx[0] + h * r.sx[1], L);
+    float c[4], s[4], wx[4], wy[4], bx[4], by[4];
+    load_affine(r.w, h, L, 1.f, wx, wy);
+    load_affine(r.b, h, L, 0.f, bx, by);
+    int start, n;
+    const bool valid = cache::seq_lengths(p, b, start, n);
+    angles(a.f, L, start, c, s);
+    row_through(a.f, L, raw, there && valid && n > 0, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + h * r.sy[1]);
   }
 }
 
@@ -452,8 +454,8 @@ static FrontDev device_front(const kvm_front_t* f) {
 
 static bool runs_aligned(const void* p, const int64_t (&st)[3]) { return cache::aligned(p, 8) && st[0] % 4 == 0 && st[1] % 4 == 0 && st[2] % 4 == 0; }
 
-// Rows of q, k or v with their strides; y may be NULL (nothing is written).
-static bool rows_of(Rows& r, const kvm_front_t* f, int which, const void* x, void* y, int64_t B, int64_t H, int64_t T, int d, const int64_t* sx, const int64_t* sy) {
+// Rows of q, k or v with their strides; y may be NULL (nothing is written).  runs: cleared where they cannot be accessed as runs of four channels.
+static bool rows_of(Rows& r, bool& runs, const kvm_front_t* f, int which, const void* x, void* y, int64_t B, int64_t H, int64_t T, int d, const int64_t* sx, const int64_t* sy) {
   if (!x || !cache::aligned(x, 2) || !cache::aligned(y, 2)) return false;
   if (!cache::strides_of(sx, B, H, T, d, false, r.sx) || !cache::strides_of(sy, B, H, T, d, true, r.sy)) return false;
   if (x == y) {   // in place: the same rows
@@ -461,15 +463,18 @@ static bool rows_of(Rows& r, const kvm_front_t* f, int which, const void* x, voi
     for (int i = 0; i < 3; ++i)
       if (n[i] > 1 && r.sx[i] != r.sy[i]) return false;
   }
-  const bool runs = which == 2 || f->layout == KVM_ROPE_INTERLEAVED || f->rope_dims / 2 % 4 == 0;
   r.x = (const __nv_bfloat16*)x; r.y = (__nv_bfloat16*)y;
   r.H = (int)H;
   r.w = which == 0 ? f->q_weight : which == 1 ? f->k_weight : nullptr;
   r.b = which == 0 ? f->q_bias : which == 1 ? f->k_bias : nullptr;
-  r.vx = runs && runs_aligned(x, r.sx);
-  r.vy = runs && runs_aligned(y, r.sy);
-  r.vw = runs && cache::aligned(r.w, 16) && cache::aligned(r.b, 16);
+  runs = runs && runs_aligned(x, r.sx) && runs_aligned(y, r.sy) && cache::aligned(r.w, 16) && cache::aligned(r.b, 16);
   return true;
+}
+
+static int mode_of(const kvm_front_t* f, bool runs) {
+  if (!runs) return kSingle;
+  if (f->layout == KVM_ROPE_INTERLEAVED || f->rope_dims == 0) return kSide;
+  return f->rope_dims / 2 % 4 == 0 ? kHalves : kSingle;
 }
 
 // Heads of a chunk: as many as leave `want` blocks, 16 at most (the angles of a block's tokens are computed once per chunk).
@@ -479,43 +484,50 @@ static int heads_of_chunk(int64_t blocks_per_head, int H, int64_t want) {
   return (H + chunks - 1) / chunks;
 }
 
-template <int D, int TPP, int TH>
+template <int D, int MODE>
+static kvm_status_t launch_qk(QkArgs& a, cudaStream_t s) {
+  constexpr int LPR = D / 8, TOK = 256 / LPR * kTokens;
+  const int H = a.r[0].H + a.r[1].H;
+  const int64_t tokens = a.batch * a.T, tiles = (tokens + TOK - 1) / TOK;
+  if (tokens * H <= 16384) {
+    qk_rows_kernel<D, MODE><<<(unsigned)((tokens * H * LPR + 127) / 128), 128, 0, s>>>(a);
+  } else {
+    if (tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
+    a.heads = heads_of_chunk(tiles, H, 6 * 148);
+    for (int i = 0; i < 2; ++i) a.chunks[i] = (a.r[i].H + a.heads - 1) / a.heads;
+    qk_tile_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)(a.chunks[0] + a.chunks[1])), 256, 0, s>>>(a);
+  }
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+
+template <int D, int MODE>
 static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   const cache::Params& p = a.p;
+  if (p.T == 1) {
+    const int64_t units = (int64_t)p.batch * p.Hkv, rpw = 32 / (D / 8);
+    const int64_t warps = 2 * units + ((int64_t)p.batch * a.q.H + rpw - 1) / rpw;
+    ingest_token_kernel<D, MODE><<<(unsigned)((warps + 3) / 4), 128, 0, s>>>(a);
+    return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+  }
+  a.tpp = p.page * D / 8 / kRows;
+  const int TH = std::max(256, a.tpp);
   const int64_t pages = (p.T + p.page - 2) / p.page + 1;   // pages that T consecutive tokens can touch
-  const int64_t groups = (pages + TH / TPP - 1) / (TH / TPP);
+  const int64_t groups = (pages + TH / a.tpp - 1) / (TH / a.tpp);
   a.groups = (int)groups;
   a.heads = heads_of_chunk(groups * p.batch, p.Hkv, 4 * 148);
   a.chunks = (p.Hkv + a.heads - 1) / a.heads;
-  a.kv_blocks = groups * p.batch * a.chunks;
-  int64_t q_blocks = 0;
+  a.k_blocks = groups * p.batch * a.chunks;
+  constexpr int TOK = 256 / (D / 8) * kTokens;
+  const int64_t tiles = (p.T * p.batch + TOK - 1) / TOK;
+  if (2 * a.k_blocks > INT32_MAX || tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
+  if (TH == 256) ingest_pages_kernel<D, 256, MODE><<<(unsigned)(2 * a.k_blocks), 256, 0, s>>>(a);
+  else ingest_pages_kernel<D, 512, MODE><<<(unsigned)(2 * a.k_blocks), 512, 0, s>>>(a);
   if (a.q.H > 0) {
-    constexpr int TOK = TH / (D / 8) * kFourths;
-    const int64_t tiles = (p.T * p.batch + TOK - 1) / TOK;
-    a.heads_q = heads_of_chunk(tiles, a.q.H, 4 * 148);
+    a.heads_q = heads_of_chunk(tiles, a.q.H, 6 * 148);
     a.chunks_q = (a.q.H + a.heads_q - 1) / a.heads_q;
-    q_blocks = tiles * a.chunks_q;
+    ingest_q_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)a.chunks_q), 256, 0, s>>>(a);
   }
-  const int64_t blocks = 2 * a.kv_blocks + q_blocks;
-  if (blocks > INT32_MAX) return KVM_ERR_UNSUPPORTED;
-  ingest_kernel<D, TPP, TH><<<(unsigned)blocks, TH, 0, s>>>(a);
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
-}
-template <int D>
-static kvm_status_t launch_ingest_d(IngestArgs& a, cudaStream_t s) {
-  if (a.p.T == 1) {
-    const int64_t units = (int64_t)a.p.batch * a.p.Hkv, rpw = 32 / (D / 8);
-    const int64_t warps = 2 * units + ((int64_t)a.p.batch * a.q.H + rpw - 1) / rpw;
-    ingest_token_kernel<D><<<(unsigned)((warps + 3) / 4), 128, 0, s>>>(a);
-    return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
-  }
-  switch (a.p.page * D / 32) {   // threads per page
-    case 32: return launch_ingest<D, 32, 256>(a, s);
-    case 64: return launch_ingest<D, 64, 256>(a, s);
-    case 128: return launch_ingest<D, 128, 256>(a, s);
-    case 256: return launch_ingest<D, 256, 256>(a, s);
-    default: return launch_ingest<D, 512, 512>(a, s);
-  }
 }
 
 }  // namespace front
@@ -549,25 +561,15 @@ KVM_API kvm_status_t kvm_qk_norm_rope(const kvm_front_t* front, const void* q, c
   if (batch > 65535 || n_tokens > (1 << 30) || (q && n_q_heads > 16384) || (k && n_kv_heads > 16384)) return KVM_ERR_UNSUPPORTED;
   QkArgs a = {};
   a.f = device_front(front);
-  if (q && (!q_out || !rows_of(a.r[0], front, 0, q, q_out, batch, n_q_heads, n_tokens, head_dim, q_strides, q_out_strides))) return KVM_ERR_INVALID_ARG;
-  if (k && (!k_out || !rows_of(a.r[1], front, 1, k, k_out, batch, n_kv_heads, n_tokens, head_dim, k_strides, k_out_strides))) return KVM_ERR_INVALID_ARG;
+  bool runs = true;
+  if (q && (!q_out || !rows_of(a.r[0], runs, front, 0, q, q_out, batch, n_q_heads, n_tokens, head_dim, q_strides, q_out_strides))) return KVM_ERR_INVALID_ARG;
+  if (k && (!k_out || !rows_of(a.r[1], runs, front, 1, k, k_out, batch, n_kv_heads, n_tokens, head_dim, k_strides, k_out_strides))) return KVM_ERR_INVALID_ARG;
   a.start = start; a.count = count; a.status = status;
   a.T = n_tokens; a.batch = batch;
-  const int H = a.r[0].H + a.r[1].H, lpr = head_dim / 8;
-  const int64_t tokens = (int64_t)batch * n_tokens;
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  const int64_t tiles = (tokens + 256 / lpr * kFourths - 1) / (256 / lpr * kFourths);
-  if (tokens * H <= 16384) {
-    const unsigned blocks = (unsigned)((tokens * H * lpr + 127) / 128);
-    if (head_dim == 128) qk_rows_kernel<128><<<blocks, 128, 0, s>>>(a); else qk_rows_kernel<64><<<blocks, 128, 0, s>>>(a);
-  } else {
-    if (tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
-    a.heads = heads_of_chunk(tiles, H, 4 * 148);
-    for (int i = 0; i < 2; ++i) a.chunks[i] = (a.r[i].H + a.heads - 1) / a.heads;
-    const dim3 grid((unsigned)tiles, (unsigned)(a.chunks[0] + a.chunks[1]));
-    if (head_dim == 128) qk_tile_kernel<128><<<grid, 256, 0, s>>>(a); else qk_tile_kernel<64><<<grid, 256, 0, s>>>(a);
-  }
-  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+  const int mode = mode_of(front, runs);
+  if (head_dim == 128) return mode == kSide ? launch_qk<128, kSide>(a, s) : mode == kHalves ? launch_qk<128, kHalves>(a, s) : launch_qk<128, kSingle>(a, s);
+  return mode == kSide ? launch_qk<64, kSide>(a, s) : mode == kHalves ? launch_qk<64, kHalves>(a, s) : launch_qk<64, kSingle>(a, s);
 }
 
 KVM_API kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_call_t* call, const kvm_front_t* front, const void* q, int32_t n_q_heads,
@@ -584,11 +586,15 @@ KVM_API kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_
   a.p = cache::params_of(cache, call, status);
   const int64_t B = a.p.batch, T = a.p.T;
   const int d = cache->head_dim;
-  if (q && !rows_of(a.q, front, 0, q, q_out, B, n_q_heads, T, d, q_strides, q_out_strides)) return KVM_ERR_INVALID_ARG;
-  if (!rows_of(a.k, front, 1, k, nullptr, B, a.p.Hkv, T, d, k_strides, nullptr) || !rows_of(a.v, front, 2, v, nullptr, B, a.p.Hkv, T, d, v_strides, nullptr)) return KVM_ERR_INVALID_ARG;
+  bool runs = true;
+  if (q && !rows_of(a.q, runs, front, 0, q, q_out, B, n_q_heads, T, d, q_strides, q_out_strides)) return KVM_ERR_INVALID_ARG;
+  if (!rows_of(a.k, runs, front, 1, k, nullptr, B, a.p.Hkv, T, d, k_strides, nullptr) || !rows_of(a.v, runs, front, 2, v, nullptr, B, a.p.Hkv, T, d, v_strides, nullptr)) return KVM_ERR_INVALID_ARG;
   a.o.codes[0] = (uint8_t*)cache->k; a.o.codes[1] = (uint8_t*)cache->v;
   a.o.scales[0] = cache->k_scale; a.o.scales[1] = cache->v_scale;
-  return d == 128 ? launch_ingest_d<128>(a, (cudaStream_t)cuda_stream) : launch_ingest_d<64>(a, (cudaStream_t)cuda_stream);
+  cudaStream_t s = (cudaStream_t)cuda_stream;
+  const int mode = mode_of(front, runs);
+  if (d == 128) return mode == kSide ? launch_ingest<128, kSide>(a, s) : mode == kHalves ? launch_ingest<128, kHalves>(a, s) : launch_ingest<128, kSingle>(a, s);
+  return mode == kSide ? launch_ingest<64, kSide>(a, s) : mode == kHalves ? launch_ingest<64, kHalves>(a, s) : launch_ingest<64, kSingle>(a, s);
 }
 
 }  // extern "C"
