@@ -1,6 +1,7 @@
 // Front end of an exact layer: norm of every head's queries and keys and rotary positions in one pass (kvm_qk_norm_rope), and the same on the
 // way into the 8-bit cache (kvm_cache_ingest), where the keys are normalised, rotated and quantised as they are written.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "kvm_cache.cuh"
@@ -11,8 +12,10 @@ namespace front {
 
 using cache::AppendOut;
 
-constexpr int kTokens = 2;    // tokens of a lane in the kernel over many rows
+constexpr int kTokens = 4;    // tokens of a lane in the kernel over many rows
 constexpr int kRows = 4;      // rows of a lane in the kernel over pages
+constexpr int kPagesAhead = 3;
+constexpr int kAhead = 3;     // stages of rows on their way (one of them is in use)
 
 struct QkArgs {
   FrontDev f;
@@ -30,16 +33,18 @@ __device__ __forceinline__ bool qk_lengths(const QkArgs& a, int b, int& start, i
   return start >= 0 && n >= 0 && n <= a.T;
 }
 
-// One row through the front end.
-template <int D, int MODE>
-__device__ __forceinline__ void row_through(const FrontDev& f, const Lane<D, MODE>& L, const Raw& raw, bool live, const float (&c)[4], const float (&s)[4],
-                                            const float (&wx)[4], const float (&wy)[4], const float (&bx)[4], const float (&by)[4], __nv_bfloat16* dst) {
-  float v[8], x[4], y[4];
-  values_of(raw, v);
-  to_pairs<MODE>(v, x, y);
-  norm<D>(f, wx, wy, bx, by, x, y);
-  rotate(L, c, s, x, y);
-  if (live) store_row(dst, L, x, y);
+// Rows of a lane through the front end.
+template <int D, int MODE, int N>
+__device__ __forceinline__ void rows_through(const FrontDev& f, const Lane<D, MODE>& L, const Raw (&raw)[N], const Turn (&turn)[N], const Pairs& w, const Pairs& b, Pairs (&p)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float v[8];
+    values_of(raw[i], v);
+    p[i] = to_pairs<MODE>(v);
+  }
+  norm<D>(f, w, b, p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) rotate(L, turn[i], p[i]);
 }
 
 // Few rows: D / 8 lanes per row, every row by itself.
@@ -57,28 +62,34 @@ __global__ void __launch_bounds__(128) qk_rows_kernel(const __grid_constant__ Qk
   const int which = hh >= a.r[0].H, head = hh - (which ? a.r[0].H : 0);
   const Rows& r = a.r[which];
   // (a row that the lengths leave out is read all the same: it is there)
-  const Raw raw = load_raw(r.x + b * r.sx[0] + head * r.sx[1] + t * r.sx[2], L);
+  const Raw raw[1] = {load_raw(r.x + b * r.sx[0] + head * r.sx[1] + t * r.sx[2], L)};
   int start, n;
   const bool valid = qk_lengths(a, b, start, n);
   if (!valid && there && hh == 0 && t == 0 && L.i0 == 0) cache::report(a.status, KVM_ERR_INVALID_ARG);
-  float wx[4], wy[4], bx[4], by[4], c[4], s[4];
-  load_affine(r.w, head, L, 1.f, wx, wy);
-  load_affine(r.b, head, L, 0.f, bx, by);
-  angles(a.f, L, (int64_t)start + t, c, s);
-  row_through(a.f, L, raw, there && valid && t < n, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2]);
+  const Pairs w = load_affine(r.w, head, L, 1.f), bias = load_affine(r.b, head, L, 0.f);
+  const Turn turn[1] = {angles(a.f, L, (int64_t)start + t)};
+  Pairs p[1];
+  rows_through(a.f, L, raw, turn, w, bias, p);
+  store_row(r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2], L, p[0], there && valid && t < n, nullptr);
 }
 
 // Many rows: a block takes 256 / LPR * 2 tokens (of the whole batch, one behind the other) through a run of heads.  A lane has two tokens: their
-// angles stay in registers over the heads, a head's weights over the tokens, and the next head's rows are on their way.
+// angles stay in registers over the heads, a head's weights over the tokens, and the rows of the next heads are on their way (in registers one head ahead was as
+// many as there was room for: 79 us instead of NN for two prompts of 8192 tokens, 32 heads, d = 128).
 template <int D, int MODE, class A>
 __device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t token0, int h0, int h1) {
-  constexpr int LPR = D / 8, RP = 256 / LPR, CH = kTokens;
+  constexpr int LPR = D / 8, RP = 256 / LPR, CH = kTokens, S = kAhead;
+  constexpr bool STAGED = MODE != kSingle;
+  using Stages = Stage<D, 256, CH, S>;
+  extern __shared__ __align__(16) uint8_t stage_mem[];
+  const Stages stages{stage_mem};
   const FrontDev& f = a.f;
   const Lane<D, MODE> L(f, threadIdx.x % LPR);
   const __nv_bfloat16* px[CH];
   __nv_bfloat16* py[CH];
-  float c[CH][4], s[CH][4];
+  Turn turn[CH];
   uint32_t live = 0;
+  int64_t pos[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int64_t token = token0 + threadIdx.x / LPR + i * RP;
@@ -90,30 +101,51 @@ __device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t tok
       start = n = 0;
     }
     if (t < n) live |= 1u << i;
+    pos[i] = start + t;
     px[i] = r.x + b * r.sx[0] + t * r.sx[2] + h0 * r.sx[1];
     py[i] = r.y + b * r.sy[0] + t * r.sy[2] + h0 * r.sy[1];
-    angles(f, L, start + t, c[i], s[i]);
   }
-  Raw raw[CH];
+  if (!__any_sync(0xffffffffu, live)) return;   // (a warp's rows are its own)
+  int ahead = h0;   // heads that have been asked for
+  auto ask = [&](int stage) {
+    if (ahead < h1) {
 #pragma unroll
-  for (int i = 0; i < CH; ++i) raw[i] = load_raw(px[i], L);
+      for (int i = 0; i < CH; ++i) {
+        if (live >> i & 1) stages.copy(stage, i, px[i]);
+        px[i] += r.sx[1];
+      }
+      ++ahead;
+    }
+    stages.commit();
+  };
+  if (STAGED) {
+#pragma unroll
+    for (int k = 0; k < S - 1; ++k) ask(k);
+  }
+#pragma unroll
+  for (int i = 0; i < CH; ++i) turn[i] = angles(f, L, pos[i]);
+  int stage = 0;
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
-    float wx[4], wy[4], bx[4], by[4];
-    load_affine(r.w, h, L, 1.f, wx, wy);
-    load_affine(r.b, h, L, 0.f, bx, by);
-    Raw now[CH];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) now[i] = raw[i];
-    if (h + 1 < h1) {
-#pragma unroll
-      for (int i = 0; i < CH; ++i) raw[i] = load_raw(px[i] += r.sx[1], L);
+    const Pairs w = load_affine(r.w, h, L, 1.f), bias = load_affine(r.b, h, L, 0.f);
+    Raw raw[CH];
+    if (STAGED) {
+      stages.wait();                                  // (all lanes have read the stage that is asked for next)
+      ask(stage == 0 ? S - 1 : stage - 1);
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      row_through(f, L, now[i], live >> i & 1, c[i], s[i], wx, wy, bx, by, py[i]);
+      raw[i] = load_raw(STAGED ? stages.row(stage, i) : px[i], L);
+      if (!STAGED) px[i] += r.sx[1];
+    }
+    Pairs p[CH];
+    rows_through(f, L, raw, turn, w, bias, p);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      store_row(py[i], L, p[i], live >> i & 1, STAGED ? stages.row(stage, i) : nullptr);
       py[i] += r.sy[1];
     }
+    if (++stage == S) stage = 0;
   }
 }
 
@@ -126,7 +158,7 @@ struct QkTile {   // what rows_tile asks of a call without a cache
   __device__ int32_t* status_word() const { return a.status; }
 };
 template <int D, int MODE>
-__global__ void __launch_bounds__(256, 3) qk_tile_kernel(const __grid_constant__ QkArgs a) {
+__global__ void __launch_bounds__(256, 2) qk_tile_kernel(const __grid_constant__ QkArgs a) {
   const int which = (int)blockIdx.y >= a.chunks[0], chunk = blockIdx.y - (which ? a.chunks[0] : 0);
   const int h0 = chunk * a.heads;
   rows_tile<D, MODE>(QkTile{a, a.f}, a.r[which], (int64_t)blockIdx.x * (256 / (D / 8) * kTokens), h0, min(h0 + a.heads, a.r[which].H));
@@ -164,7 +196,7 @@ __device__ __forceinline__ void codes_of(const float (&v)[8], float inv, uint32_
 }
 template <int D, int MODE>
 __device__ __forceinline__ void store_codes(uint8_t* row, const Lane<D, MODE>& L, uint32_t a, uint32_t b) {
-  if (MODE != kSingle) {
+  if (MODE <= kHalves) {
     *reinterpret_cast<uint32_t*>(row + L.c0) = a;
     *reinterpret_cast<uint32_t*>(row + L.c1) = b;
   } else {   // (x0 y0 x1 y1 ...)
@@ -185,8 +217,11 @@ __device__ __forceinline__ uint32_t rescaled4(uint32_t w, float m) {
 // the codes, which follow the maximum over the rows of a page.
 template <int D, int TH, int MODE, bool KEYS>
 __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int chunk, int b) {
-  constexpr int LPR = D / 8, CH = kRows;
+  constexpr int LPR = D / 8, CH = kRows, S = kPagesAhead;
+  constexpr bool STAGED = MODE != kSingle;
+  extern __shared__ __align__(16) uint8_t stage_mem[];
   __shared__ uint32_t s_top[2][TH / 32];
+  const Stage<D, TH, CH, S> stages{stage_mem};
   const cache::Params& p = a.p;
   const Rows& r = KEYS ? a.k : a.v;
   const FrontDev& f = a.f;
@@ -213,46 +248,60 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
   const Lane<D, MODE> L(f, tt % LPR);
   const int h0 = chunk * a.heads, h1 = min(h0 + a.heads, p.Hkv), row0 = tt / LPR;
   const __nv_bfloat16* px = r.x + b * r.sx[0] + h0 * r.sx[1] + (pos0 + row0 - start) * r.sx[2];   // (rows in front of the call's: not looked at)
-  float c[CH][4], s[CH][4];
+  Turn turn[CH];
   uint32_t fresh = 0;
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int row = row0 + i * step;
-    if (row >= r0 && row < r1) {
-      fresh |= 1u << i;
-      if (KEYS) angles(f, L, pos0 + row, c[i], s[i]);
-    }
+    if (row >= r0 && row < r1) fresh |= 1u << i;
   }
-  auto fetch = [&](Raw (&raw)[CH]) {
+  const int64_t apart = step * r.sx[2];
+  int ahead = h0;   // heads that have been asked for
+  auto ask = [&](int stage) {
+    if (ahead < h1) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      raw[i].a = raw[i].b = make_uint2(0, 0);
-      if (fresh >> i & 1) raw[i] = load_raw(px + i * step * r.sx[2], L);
+      for (int i = 0; i < CH; ++i)
+        if (fresh >> i & 1) stages.copy(stage, i, px + i * apart);
+      px += r.sx[1];
+      ++ahead;
     }
+    stages.commit();
   };
+  if (STAGED) {
+#pragma unroll
+    for (int k = 0; k < S - 1; ++k) ask(k);
+  }
+  if (KEYS) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) turn[i] = angles(f, L, pos0 + row0 + i * step);
+  }
+  int stage = 0;
 #pragma unroll 1
-  for (int h = h0; h < h1; ++h, px += r.sx[1]) {
+  for (int h = h0; h < h1; ++h) {
     const int64_t unit = (int64_t)page * p.Hkv + h;
     uint8_t* codes = a.o.codes[KEYS ? 0 : 1] + (unit * p.page + row0) * D;
     float* scale = a.o.scales[KEYS ? 0 : 1] + unit;
     const float old = live && r0 > 0 ? *scale : 0.f;
     Raw raw[CH];
-    fetch(raw);
+    if (STAGED) {
+      stages.wait();                                  // (all lanes have read the stage that is asked for next)
+      ask(stage == 0 ? S - 1 : stage - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      raw[i].a = raw[i].b = make_uint2(0, 0);
+      if (fresh >> i & 1) raw[i] = load_raw(STAGED ? stages.row(stage, i) : px + i * apart, L);
+    }
+    if (!STAGED) px += r.sx[1];
+    if (++stage == S) stage = 0;
     float v[CH][8];
     uint32_t top = 0;
     if (KEYS) {
-      float wx[4], wy[4], bx[4], by[4];
-      load_affine(r.w, h, L, 1.f, wx, wy);
-      load_affine(r.b, h, L, 0.f, bx, by);
+      const Pairs w = load_affine(r.w, h, L, 1.f), bias = load_affine(r.b, h, L, 0.f);
+      Pairs x[CH];
+      rows_through(f, L, raw, turn, w, bias, x);
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        float x[4], y[4];
-        values_of(raw[i], v[i]);
-        to_pairs<MODE>(v[i], x, y);
-        norm<D>(f, wx, wy, bx, by, x, y);
-        rotate(L, c[i], s[i], x, y);
-        from_pairs<MODE>(x, y, v[i]);
-      }
+      for (int i = 0; i < CH; ++i) from_pairs<MODE>(x[i], v[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < CH; ++i) values_of(raw[i], v[i]);
@@ -306,10 +355,10 @@ __global__ void __launch_bounds__(TH, 512 / TH) ingest_pages_kernel(const __grid
   i /= a.chunks;
   const int group = (int)(i % a.groups), b = (int)(i / a.groups);
   if (keys) pages_tile<D, TH, MODE, true>(a, group, chunk, b);
-  else pages_tile<D, TH, MODE == kSingle ? kSingle : kSide, false>(a, group, chunk, b);
+  else pages_tile<D, TH, MODE == kSingle ? kSingle : kSide, false>(a, group, chunk, b);   // (values: eight channels side by side)
 }
 template <int D, int MODE>
-__global__ void __launch_bounds__(256, 3) ingest_q_kernel(const __grid_constant__ IngestArgs a) {
+__global__ void __launch_bounds__(256, 2) ingest_q_kernel(const __grid_constant__ IngestArgs a) {
   const int h0 = blockIdx.y * a.heads_q;
   rows_tile<D, MODE>(IngestTile{a, a.f}, a.q, (int64_t)blockIdx.x * (256 / (D / 8) * kTokens), h0, min(h0 + a.heads_q, a.q.H));
 }
@@ -325,9 +374,7 @@ __device__ __forceinline__ void token_into(const IngestArgs& a, int64_t unit_of_
   const Rows& r = KEYS ? a.k : a.v;
   const int b = (int)(unit_of_call / p.Hkv), h = (int)(unit_of_call - (int64_t)b * p.Hkv);
   const Raw raw = load_raw(r.x + b * r.sx[0] + h * r.sx[1], L);   // (there whatever the lengths are)
-  float wx[4], wy[4], bx[4], by[4], c[4], s[4];
-  load_affine(KEYS ? r.w : nullptr, h, L, 1.f, wx, wy);
-  load_affine(KEYS ? r.b : nullptr, h, L, 0.f, bx, by);
+  const Pairs w = load_affine(KEYS ? r.w : nullptr, h, L, 1.f), bias = load_affine(KEYS ? r.b : nullptr, h, L, 0.f);
   int start, n;
   if (!cache::seq_lengths(p, b, start, n)) {
     if (KEYS && h == 0 && lane == 0) cache::report(p.status, KVM_ERR_INVALID_ARG);
@@ -346,12 +393,11 @@ __device__ __forceinline__ void token_into(const IngestArgs& a, int64_t unit_of_
   float v[8];
   values_of(raw, v);
   if (KEYS) {
-    float x[4], y[4];
-    to_pairs<MODE>(v, x, y);
-    angles(f, L, start, c, s);
-    norm<D>(f, wx, wy, bx, by, x, y);
-    rotate(L, c, s, x, y);
-    from_pairs<MODE>(x, y, v);
+    const Raw raws[1] = {raw};
+    const Turn turn[1] = {angles(f, L, start)};
+    Pairs x[1];
+    rows_through(f, L, raws, turn, w, bias, x);
+    from_pairs<MODE>(x[0], v);
   }
   uint32_t top = 0;
 #pragma unroll
@@ -394,14 +440,14 @@ __global__ void __launch_bounds__(128) ingest_token_kernel(const __grid_constant
     const bool there = row < (int64_t)p.batch * r.H;
     if (!there) row = 0;
     const int b = (int)(row / r.H), h = (int)(row - (int64_t)b * r.H);
-    const Raw raw = load_raw(r.x + b * r.sx[0] + h * r.sx[1], L);
-    float c[4], s[4], wx[4], wy[4], bx[4], by[4];
-    load_affine(r.w, h, L, 1.f, wx, wy);
-    load_affine(r.b, h, L, 0.f, bx, by);
+    const Raw raw[1] = {load_raw(r.x + b * r.sx[0] + h * r.sx[1], L)};
+    const Pairs w = load_affine(r.w, h, L, 1.f), bias = load_affine(r.b, h, L, 0.f);
     int start, n;
     const bool valid = cache::seq_lengths(p, b, start, n);
-    angles(a.f, L, start, c, s);
-    row_through(a.f, L, raw, there && valid && n > 0, c, s, wx, wy, bx, by, r.y + b * r.sy[0] + h * r.sy[1]);
+    const Turn turn[1] = {angles(a.f, L, start)};
+    Pairs x[1];
+    rows_through(a.f, L, raw, turn, w, bias, x);
+    store_row(r.y + b * r.sy[0] + h * r.sy[1], L, x[0], there && valid && n > 0, nullptr);
   }
 }
 
@@ -452,10 +498,8 @@ static FrontDev device_front(const kvm_front_t* f) {
   return x;
 }
 
-static bool runs_aligned(const void* p, const int64_t (&st)[3]) { return cache::aligned(p, 8) && st[0] % 4 == 0 && st[1] % 4 == 0 && st[2] % 4 == 0; }
-
-// Rows of q, k or v with their strides; y may be NULL (nothing is written).  runs: cleared where they cannot be accessed as runs of four channels.
-static bool rows_of(Rows& r, bool& runs, const kvm_front_t* f, int which, const void* x, void* y, int64_t B, int64_t H, int64_t T, int d, const int64_t* sx, const int64_t* sy) {
+// Rows of q, k or v with their strides; y may be NULL (nothing is written).  aligned: cleared where they cannot be accessed 16 bytes at a time.
+static bool rows_of(Rows& r, bool& aligned, const kvm_front_t* f, int which, const void* x, void* y, int64_t B, int64_t H, int64_t T, int d, const int64_t* sx, const int64_t* sy) {
   if (!x || !cache::aligned(x, 2) || !cache::aligned(y, 2)) return false;
   if (!cache::strides_of(sx, B, H, T, d, false, r.sx) || !cache::strides_of(sy, B, H, T, d, true, r.sy)) return false;
   if (x == y) {   // in place: the same rows
@@ -467,14 +511,14 @@ static bool rows_of(Rows& r, bool& runs, const kvm_front_t* f, int which, const 
   r.H = (int)H;
   r.w = which == 0 ? f->q_weight : which == 1 ? f->k_weight : nullptr;
   r.b = which == 0 ? f->q_bias : which == 1 ? f->k_bias : nullptr;
-  runs = runs && runs_aligned(x, r.sx) && runs_aligned(y, r.sy) && cache::aligned(r.w, 16) && cache::aligned(r.b, 16);
+  aligned = aligned && cache::rows_aligned(x, r.sx) && cache::rows_aligned(y, r.sy) && cache::aligned(r.w, 16) && cache::aligned(r.b, 16);
   return true;
 }
 
-static int mode_of(const kvm_front_t* f, bool runs) {
-  if (!runs) return kSingle;
+static int mode_of(const kvm_front_t* f, bool aligned) {
+  if (!aligned) return kSingle;
   if (f->layout == KVM_ROPE_INTERLEAVED || f->rope_dims == 0) return kSide;
-  return f->rope_dims / 2 % 4 == 0 ? kHalves : kSingle;
+  return f->rope_dims / 2 % 4 == 0 ? kHalves : kMixed;
 }
 
 // Heads of a chunk: as many as leave `want` blocks, 16 at most (the angles of a block's tokens are computed once per chunk).
@@ -484,29 +528,50 @@ static int heads_of_chunk(int64_t blocks_per_head, int H, int64_t want) {
   return (H + chunks - 1) / chunks;
 }
 
+// Raises the limit of shared memory of a kernel on the current device (once per device).
+template <auto KERNEL, int SMEM>
+static bool room_for() {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return false; }
+  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) { cudaGetLastError(); return false; }
+    if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return true;
+}
+
 template <int D, int MODE>
 static kvm_status_t launch_qk(QkArgs& a, cudaStream_t s) {
-  constexpr int LPR = D / 8, TOK = 256 / LPR * kTokens;
+  constexpr int LPR = D / 8, TOK = 256 / LPR * kTokens, SMEM = MODE == kSingle ? 0 : Stage<D, 256, kTokens, kAhead>::kBytes;
   const int H = a.r[0].H + a.r[1].H;
   const int64_t tokens = a.batch * a.T, tiles = (tokens + TOK - 1) / TOK;
   if (tokens * H <= 16384) {
-    qk_rows_kernel<D, MODE><<<(unsigned)((tokens * H * LPR + 127) / 128), 128, 0, s>>>(a);
+    qk_rows_kernel<D, MODE == kMixed ? kSingle : MODE><<<(unsigned)((tokens * H * LPR + 127) / 128), 128, 0, s>>>(a);
   } else {
     if (tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
-    a.heads = heads_of_chunk(tiles, H, 6 * 148);
+    a.heads = heads_of_chunk(tiles, H, 4 * 148);
     for (int i = 0; i < 2; ++i) a.chunks[i] = (a.r[i].H + a.heads - 1) / a.heads;
-    qk_tile_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)(a.chunks[0] + a.chunks[1])), 256, 0, s>>>(a);
+    if (!room_for<qk_tile_kernel<D, MODE>, SMEM>()) return KVM_ERR_CUDA;
+    qk_tile_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)(a.chunks[0] + a.chunks[1])), 256, SMEM, s>>>(a);
   }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 
+template <int D, int TH, int MODE>
+static kvm_status_t launch_pages(const IngestArgs& a, cudaStream_t s) {
+  constexpr int SMEM = MODE == kSingle ? 0 : Stage<D, TH, kRows, kPagesAhead>::kBytes;
+  if (!room_for<ingest_pages_kernel<D, TH, MODE>, SMEM>()) return KVM_ERR_CUDA;
+  ingest_pages_kernel<D, TH, MODE><<<(unsigned)(2 * a.k_blocks), TH, SMEM, s>>>(a);
+  return KVM_OK;
+}
 template <int D, int MODE>
 static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   const cache::Params& p = a.p;
   if (p.T == 1) {
     const int64_t units = (int64_t)p.batch * p.Hkv, rpw = 32 / (D / 8);
     const int64_t warps = 2 * units + ((int64_t)p.batch * a.q.H + rpw - 1) / rpw;
-    ingest_token_kernel<D, MODE><<<(unsigned)((warps + 3) / 4), 128, 0, s>>>(a);
+    ingest_token_kernel<D, MODE == kMixed ? kSingle : MODE><<<(unsigned)((warps + 3) / 4), 128, 0, s>>>(a);
     return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
   }
   a.tpp = p.page * D / 8 / kRows;
@@ -520,14 +585,35 @@ static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   constexpr int TOK = 256 / (D / 8) * kTokens;
   const int64_t tiles = (p.T * p.batch + TOK - 1) / TOK;
   if (2 * a.k_blocks > INT32_MAX || tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
-  if (TH == 256) ingest_pages_kernel<D, 256, MODE><<<(unsigned)(2 * a.k_blocks), 256, 0, s>>>(a);
-  else ingest_pages_kernel<D, 512, MODE><<<(unsigned)(2 * a.k_blocks), 512, 0, s>>>(a);
+  const kvm_status_t rc = TH == 256 ? launch_pages<D, 256, MODE>(a, s) : launch_pages<D, 512, MODE>(a, s);
+  if (rc != KVM_OK) return rc;
   if (a.q.H > 0) {
-    a.heads_q = heads_of_chunk(tiles, a.q.H, 6 * 148);
+    constexpr int SMEM = MODE == kSingle ? 0 : Stage<D, 256, kTokens, kAhead>::kBytes;
+    if (!room_for<ingest_q_kernel<D, MODE>, SMEM>()) return KVM_ERR_CUDA;
+    a.heads_q = heads_of_chunk(tiles, a.q.H, 4 * 148);
     a.chunks_q = (a.q.H + a.heads_q - 1) / a.heads_q;
-    ingest_q_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)a.chunks_q), 256, 0, s>>>(a);
+    ingest_q_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)a.chunks_q), 256, SMEM, s>>>(a);
   }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+}
+
+template <int D>
+static kvm_status_t launch_qk_d(QkArgs& a, int mode, cudaStream_t s) {
+  switch (mode) {
+    case kSide: return launch_qk<D, kSide>(a, s);
+    case kHalves: return launch_qk<D, kHalves>(a, s);
+    case kMixed: return launch_qk<D, kMixed>(a, s);
+    default: return launch_qk<D, kSingle>(a, s);
+  }
+}
+template <int D>
+static kvm_status_t launch_ingest_d(IngestArgs& a, int mode, cudaStream_t s) {
+  switch (mode) {
+    case kSide: return launch_ingest<D, kSide>(a, s);
+    case kHalves: return launch_ingest<D, kHalves>(a, s);
+    case kMixed: return launch_ingest<D, kMixed>(a, s);
+    default: return launch_ingest<D, kSingle>(a, s);
+  }
 }
 
 }  // namespace front
@@ -561,15 +647,14 @@ KVM_API kvm_status_t kvm_qk_norm_rope(const kvm_front_t* front, const void* q, c
   if (batch > 65535 || n_tokens > (1 << 30) || (q && n_q_heads > 16384) || (k && n_kv_heads > 16384)) return KVM_ERR_UNSUPPORTED;
   QkArgs a = {};
   a.f = device_front(front);
-  bool runs = true;
-  if (q && (!q_out || !rows_of(a.r[0], runs, front, 0, q, q_out, batch, n_q_heads, n_tokens, head_dim, q_strides, q_out_strides))) return KVM_ERR_INVALID_ARG;
-  if (k && (!k_out || !rows_of(a.r[1], runs, front, 1, k, k_out, batch, n_kv_heads, n_tokens, head_dim, k_strides, k_out_strides))) return KVM_ERR_INVALID_ARG;
+  bool aligned = true;
+  if (q && (!q_out || !rows_of(a.r[0], aligned, front, 0, q, q_out, batch, n_q_heads, n_tokens, head_dim, q_strides, q_out_strides))) return KVM_ERR_INVALID_ARG;
+  if (k && (!k_out || !rows_of(a.r[1], aligned, front, 1, k, k_out, batch, n_kv_heads, n_tokens, head_dim, k_strides, k_out_strides))) return KVM_ERR_INVALID_ARG;
   a.start = start; a.count = count; a.status = status;
   a.T = n_tokens; a.batch = batch;
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  const int mode = mode_of(front, runs);
-  if (head_dim == 128) return mode == kSide ? launch_qk<128, kSide>(a, s) : mode == kHalves ? launch_qk<128, kHalves>(a, s) : launch_qk<128, kSingle>(a, s);
-  return mode == kSide ? launch_qk<64, kSide>(a, s) : mode == kHalves ? launch_qk<64, kHalves>(a, s) : launch_qk<64, kSingle>(a, s);
+  const int mode = mode_of(front, aligned);
+  return head_dim == 128 ? launch_qk_d<128>(a, mode, s) : launch_qk_d<64>(a, mode, s);
 }
 
 KVM_API kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_call_t* call, const kvm_front_t* front, const void* q, int32_t n_q_heads,
@@ -586,15 +671,14 @@ KVM_API kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_
   a.p = cache::params_of(cache, call, status);
   const int64_t B = a.p.batch, T = a.p.T;
   const int d = cache->head_dim;
-  bool runs = true;
-  if (q && !rows_of(a.q, runs, front, 0, q, q_out, B, n_q_heads, T, d, q_strides, q_out_strides)) return KVM_ERR_INVALID_ARG;
-  if (!rows_of(a.k, runs, front, 1, k, nullptr, B, a.p.Hkv, T, d, k_strides, nullptr) || !rows_of(a.v, runs, front, 2, v, nullptr, B, a.p.Hkv, T, d, v_strides, nullptr)) return KVM_ERR_INVALID_ARG;
+  bool aligned = true;
+  if (q && !rows_of(a.q, aligned, front, 0, q, q_out, B, n_q_heads, T, d, q_strides, q_out_strides)) return KVM_ERR_INVALID_ARG;
+  if (!rows_of(a.k, aligned, front, 1, k, nullptr, B, a.p.Hkv, T, d, k_strides, nullptr) || !rows_of(a.v, aligned, front, 2, v, nullptr, B, a.p.Hkv, T, d, v_strides, nullptr)) return KVM_ERR_INVALID_ARG;
   a.o.codes[0] = (uint8_t*)cache->k; a.o.codes[1] = (uint8_t*)cache->v;
   a.o.scales[0] = cache->k_scale; a.o.scales[1] = cache->v_scale;
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  const int mode = mode_of(front, runs);
-  if (d == 128) return mode == kSide ? launch_ingest<128, kSide>(a, s) : mode == kHalves ? launch_ingest<128, kHalves>(a, s) : launch_ingest<128, kSingle>(a, s);
-  return mode == kSide ? launch_ingest<64, kSide>(a, s) : mode == kHalves ? launch_ingest<64, kHalves>(a, s) : launch_ingest<64, kSingle>(a, s);
+  const int mode = mode_of(front, aligned);
+  return d == 128 ? launch_ingest_d<128>(a, mode, s) : launch_ingest_d<64>(a, mode, s);
 }
 
 }  // extern "C"
