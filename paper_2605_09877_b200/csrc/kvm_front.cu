@@ -23,7 +23,7 @@ struct QkArgs {
   const int32_t *start, *count;
   int32_t* status;
   int64_t T;
-  int batch, chunks[2], heads;   // head chunks of q and k, heads of a chunk
+  int batch;
 };
 
 // Tokens before the call and in it; false: lengths that the call does not allow.
@@ -73,70 +73,103 @@ __global__ void __launch_bounds__(128) qk_rows_kernel(const __grid_constant__ Qk
   store_row(r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2], L, p[0], there && valid && t < n, nullptr);
 }
 
-// Many rows: a block takes 256 / LPR * 2 tokens (of the whole batch, one behind the other) through a run of heads.  A lane has two tokens: their
-// angles stay in registers over the heads, a head's weights over the tokens, and the rows of the next heads are on their way (in registers one head ahead was as
-// many as there was room for: 79 us instead of NN for two prompts of 8192 tokens, 32 heads, d = 128).
+// Many rows: a tile is 256 / LPR * 4 tokens (of the whole batch, one behind the other), and an item one head of a tile, q's then k's.  Every block takes an equal
+// run of items, two blocks per SM.  A lane has four tokens: their angles stay in registers over the heads, a head's weights over the tokens, and the rows of the
+// items ahead are on their way.
+struct Tiles {
+  cache::FastDiv by_T, by_H;
+  int tokens, T, H;     // tokens of the batch, of a sequence; heads of q and k
+  int items, per;       // of the call; of a block
+};
 template <int D, int MODE, class A>
-__device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t token0, int h0, int h1) {
+__device__ __forceinline__ void rows_tiles(const A& a, const Tiles& ts) {
   constexpr int LPR = D / 8, RP = 256 / LPR, CH = kTokens, S = kAhead;
   constexpr bool STAGED = MODE != kSingle;
-  using Stages = Stage<D, 256, CH, S>;
   extern __shared__ __align__(16) uint8_t stage_mem[];
-  const Stages stages{stage_mem};
-  const FrontDev& f = a.f;
+  const Stage<D, 256, CH, S> stages{stage_mem};
+  const FrontDev& f = a.front();
   const Lane<D, MODE> L(f, threadIdx.x % LPR);
+  const int begin = blockIdx.x * ts.per, end = min(ts.items, begin + ts.per), Hq = a.rows(0).H;
+  // the lane's tokens of a tile: (sequence, token), whether there is one
+  auto token_of = [&](int tile, int i, int& b, int& t) {
+    const int token = tile * (RP * CH) + i * RP + (int)threadIdx.x / LPR;
+    b = ts.by_T.div(token);
+    t = token - b * ts.T;
+    return token < ts.tokens;
+  };
+  // what is asked for: item, its head, where its rows are
+  int ahead = begin, ahead_h = begin - ts.by_H.div(begin) * ts.H;
   const __nv_bfloat16* px[CH];
-  __nv_bfloat16* py[CH];
-  Turn turn[CH];
-  uint32_t live = 0;
-  int64_t pos[CH];
+  uint32_t there = 0;
+  auto ask = [&](int stage, bool first) {
+    if (ahead < end) {
+      const Rows& r = a.rows(ahead_h >= Hq);
+      if (first || ahead_h == 0 || ahead_h == Hq) {
+        const int tile = ts.by_H.div(ahead);
+        there = 0;
 #pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    const int64_t token = token0 + threadIdx.x / LPR + i * RP;
-    int64_t b = token / a.tokens(), t = token - b * a.tokens();
-    int start = 0, n = 0;
-    if (b >= a.sequences()) b = t = 0;
-    else if (!a.lengths((int)b, start, n)) {
-      if (t == 0 && h0 == 0 && L.i0 == 0) cache::report(a.status_word(), KVM_ERR_INVALID_ARG);
-      start = n = 0;
-    }
-    if (t < n) live |= 1u << i;
-    pos[i] = start + t;
-    px[i] = r.x + b * r.sx[0] + t * r.sx[2] + h0 * r.sx[1];
-    py[i] = r.y + b * r.sy[0] + t * r.sy[2] + h0 * r.sy[1];
-  }
-  if (!__any_sync(0xffffffffu, live)) return;   // (a warp's rows are its own)
-  int ahead = h0;   // heads that have been asked for
-  auto ask = [&](int stage) {
-    if (ahead < h1) {
+        for (int i = 0; i < CH; ++i) {
+          int b, t;
+          if (token_of(tile, i, b, t)) there |= 1u << i; else b = t = 0;
+          px[i] = r.x + b * r.sx[0] + t * r.sx[2] + (ahead_h - (ahead_h >= Hq ? Hq : 0)) * r.sx[1];
+        }
+      }
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        if (live >> i & 1) stages.copy(stage, i, px[i]);
+        if (there >> i & 1) stages.copy(stage, i, px[i]);
         px[i] += r.sx[1];
       }
       ++ahead;
+      if (++ahead_h == ts.H) ahead_h = 0;
     }
     stages.commit();
   };
+  int h = ahead_h;
   if (STAGED) {
 #pragma unroll
-    for (int k = 0; k < S - 1; ++k) ask(k);
+    for (int k = 0; k < S - 1; ++k) ask(k, k == 0);
   }
-#pragma unroll
-  for (int i = 0; i < CH; ++i) turn[i] = angles(f, L, pos[i]);
+  __nv_bfloat16* py[CH];
+  const __nv_bfloat16* pd[CH];   // kSingle: the rows themselves
+  Turn turn[CH];
+  uint32_t live = 0;
   int stage = 0;
 #pragma unroll 1
-  for (int h = h0; h < h1; ++h) {
-    const Pairs w = load_affine(r.w, h, L, 1.f), bias = load_affine(r.b, h, L, 0.f);
+  for (int item = begin; item < end; ++item) {
+    const int which = h >= Hq, head = h - (which ? Hq : 0);
+    const Rows& r = a.rows(which);
+    if (item == begin || h == 0 || h == Hq) {
+      const int tile = ts.by_H.div(item);
+      const bool fresh = item == begin || h == 0;
+      if (fresh) live = 0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        int b, t;
+        const bool in = token_of(tile, i, b, t);
+        if (!in) b = t = 0;
+        if (fresh) {
+          int start = 0, n = 0;
+          if (in && !a.lengths(b, start, n)) {
+            if (t == 0 && h == 0 && L.i0 == 0) a.invalid();
+            start = n = 0;
+          }
+          if (in && t < n) live |= 1u << i;
+          turn[i] = angles(f, L, (int64_t)start + t);
+        }
+        py[i] = r.y + b * r.sy[0] + t * r.sy[2] + head * r.sy[1];
+        if (!STAGED) pd[i] = r.x + b * r.sx[0] + t * r.sx[2] + head * r.sx[1];
+      }
+    }
+    const Pairs w = load_affine(r.w, head, L, 1.f), bias = load_affine(r.b, head, L, 0.f);
     Raw raw[CH];
     if (STAGED) {
       stages.wait();                                  // (all lanes have read the stage that is asked for next)
-      ask(stage == 0 ? S - 1 : stage - 1);
+      ask(stage == 0 ? S - 1 : stage - 1, false);
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      raw[i] = load_raw(STAGED ? stages.row(stage, i) : px[i], L);
-      if (!STAGED) px[i] += r.sx[1];
+      raw[i] = load_raw(STAGED ? stages.row(stage, i) : pd[i], L);
+      if (!STAGED) pd[i] += r.sx[1];
     }
     Pairs p[CH];
     rows_through(f, L, raw, turn, w, bias, p);
@@ -146,22 +179,20 @@ __device__ __forceinline__ void rows_tile(const A& a, const Rows& r, int64_t tok
       py[i] += r.sy[1];
     }
     if (++stage == S) stage = 0;
+    if (++h == ts.H) h = 0;
   }
 }
 
-struct QkTile {   // what rows_tile asks of a call without a cache
+struct QkTiles {        // what rows_tiles asks of a call without a cache
   const QkArgs& a;
-  const FrontDev& f;
-  __device__ int64_t tokens() const { return a.T; }
-  __device__ int sequences() const { return a.batch; }
+  __device__ const FrontDev& front() const { return a.f; }
+  __device__ const Rows& rows(int which) const { return a.r[which]; }
   __device__ bool lengths(int b, int& start, int& n) const { return qk_lengths(a, b, start, n); }
-  __device__ int32_t* status_word() const { return a.status; }
+  __device__ void invalid() const { cache::report(a.status, KVM_ERR_INVALID_ARG); }
 };
 template <int D, int MODE>
-__global__ void __launch_bounds__(256, 2) qk_tile_kernel(const __grid_constant__ QkArgs a) {
-  const int which = (int)blockIdx.y >= a.chunks[0], chunk = blockIdx.y - (which ? a.chunks[0] : 0);
-  const int h0 = chunk * a.heads;
-  rows_tile<D, MODE>(QkTile{a, a.f}, a.r[which], (int64_t)blockIdx.x * (256 / (D / 8) * kTokens), h0, min(h0 + a.heads, a.r[which].H));
+__global__ void __launch_bounds__(256, 2) qk_tiles_kernel(const __grid_constant__ QkArgs a, const __grid_constant__ Tiles ts) {
+  rows_tiles<D, MODE>(QkTiles{a}, ts);
 }
 
 // ---- into the cache ----------------------------------------------------------------------------------------------------------
@@ -171,18 +202,17 @@ struct IngestArgs {
   cache::Params p;
   Rows q, k, v;         // (k.y, v.y and their strides are not used)
   AppendOut o;
-  int chunks_q, heads_q, chunks, heads;       // head chunks of q; of k and v
+  int chunks, heads;    // head chunks of k and v
   int tpp;              // threads per page
   int groups;           // blocks that share the pages of one sequence
   int64_t k_blocks;     // blocks of k, those of v follow
 };
-struct IngestTile {     // what rows_tile asks of a call over a cache
+struct IngestTiles {    // what rows_tiles asks of a call over a cache
   const IngestArgs& a;
-  const FrontDev& f;
-  __device__ int64_t tokens() const { return a.p.T; }
-  __device__ int sequences() const { return a.p.batch; }
+  __device__ const FrontDev& front() const { return a.f; }
+  __device__ const Rows& rows(int) const { return a.q; }
   __device__ bool lengths(int b, int& start, int& n) const { return cache::seq_lengths(a.p, b, start, n); }
-  __device__ int32_t* status_word() const { return nullptr; }   // (the blocks of k report)
+  __device__ void invalid() const {}   // (the blocks of k report)
 };
 
 // Least e >= -64 with x <= 448 * 2^e, from the bits of x >= 0.
@@ -358,9 +388,8 @@ __global__ void __launch_bounds__(TH, 512 / TH) ingest_pages_kernel(const __grid
   else pages_tile<D, TH, MODE == kSingle ? kSingle : kSide, false>(a, group, chunk, b);   // (values: eight channels side by side)
 }
 template <int D, int MODE>
-__global__ void __launch_bounds__(256, 2) ingest_q_kernel(const __grid_constant__ IngestArgs a) {
-  const int h0 = blockIdx.y * a.heads_q;
-  rows_tile<D, MODE>(IngestTile{a, a.f}, a.q, (int64_t)blockIdx.x * (256 / (D / 8) * kTokens), h0, min(h0 + a.heads_q, a.q.H));
+__global__ void __launch_bounds__(256, 2) ingest_q_kernel(const __grid_constant__ IngestArgs a, const __grid_constant__ Tiles ts) {
+  rows_tiles<D, MODE>(IngestTiles{a}, ts);
 }
 
 // One token per sequence: a warp per row of k or v, D / 8 lanes per row of q.
@@ -541,19 +570,35 @@ static bool room_for() {
   return true;
 }
 
+// The items of a call over its blocks; false: more than is numbered in 32 bits.
+template <int D>
+static bool tiles_of_call(int64_t batch, int64_t T, int H, Tiles& ts, int& blocks) {
+  constexpr int TOK = 256 / (D / 8) * kTokens;
+  const int64_t tokens = batch * T, items = (tokens + TOK - 1) / TOK * H;
+  if (tokens > INT32_MAX - TOK || items > INT32_MAX) return false;
+  ts.by_T = cache::FastDiv((uint32_t)T); ts.by_H = cache::FastDiv(H);
+  ts.tokens = (int)tokens; ts.T = (int)T; ts.H = H;
+  ts.items = (int)items;
+  ts.per = (int)((items + 2 * 148 - 1) / (2 * 148));
+  blocks = (int)((items + ts.per - 1) / ts.per);
+  return true;
+}
+template <int D, int MODE>
+constexpr int kTilesSmem = MODE == kSingle ? 0 : Stage<D, 256, kTokens, kAhead>::kBytes;
+
 template <int D, int MODE>
 static kvm_status_t launch_qk(QkArgs& a, cudaStream_t s) {
-  constexpr int LPR = D / 8, TOK = 256 / LPR * kTokens, SMEM = MODE == kSingle ? 0 : Stage<D, 256, kTokens, kAhead>::kBytes;
+  constexpr int LPR = D / 8;
   const int H = a.r[0].H + a.r[1].H;
-  const int64_t tokens = a.batch * a.T, tiles = (tokens + TOK - 1) / TOK;
+  const int64_t tokens = a.batch * a.T;
   if (tokens * H <= 16384) {
     qk_rows_kernel<D, MODE == kMixed ? kSingle : MODE><<<(unsigned)((tokens * H * LPR + 127) / 128), 128, 0, s>>>(a);
   } else {
-    if (tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
-    a.heads = heads_of_chunk(tiles, H, 4 * 148);
-    for (int i = 0; i < 2; ++i) a.chunks[i] = (a.r[i].H + a.heads - 1) / a.heads;
-    if (!room_for<qk_tile_kernel<D, MODE>, SMEM>()) return KVM_ERR_CUDA;
-    qk_tile_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)(a.chunks[0] + a.chunks[1])), 256, SMEM, s>>>(a);
+    Tiles ts;
+    int blocks;
+    if (!tiles_of_call<D>(a.batch, a.T, H, ts, blocks)) return KVM_ERR_UNSUPPORTED;
+    if (!room_for<qk_tiles_kernel<D, MODE>, kTilesSmem<D, MODE>>()) return KVM_ERR_CUDA;
+    qk_tiles_kernel<D, MODE><<<blocks, 256, kTilesSmem<D, MODE>, s>>>(a, ts);
   }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
@@ -582,17 +627,14 @@ static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   a.heads = heads_of_chunk(groups * p.batch, p.Hkv, 4 * 148);
   a.chunks = (p.Hkv + a.heads - 1) / a.heads;
   a.k_blocks = groups * p.batch * a.chunks;
-  constexpr int TOK = 256 / (D / 8) * kTokens;
-  const int64_t tiles = (p.T * p.batch + TOK - 1) / TOK;
-  if (2 * a.k_blocks > INT32_MAX || tiles > INT32_MAX) return KVM_ERR_UNSUPPORTED;
+  Tiles ts;
+  int blocks = 0;
+  if (2 * a.k_blocks > INT32_MAX || (a.q.H > 0 && !tiles_of_call<D>(p.batch, p.T, a.q.H, ts, blocks))) return KVM_ERR_UNSUPPORTED;
   const kvm_status_t rc = TH == 256 ? launch_pages<D, 256, MODE>(a, s) : launch_pages<D, 512, MODE>(a, s);
   if (rc != KVM_OK) return rc;
   if (a.q.H > 0) {
-    constexpr int SMEM = MODE == kSingle ? 0 : Stage<D, 256, kTokens, kAhead>::kBytes;
-    if (!room_for<ingest_q_kernel<D, MODE>, SMEM>()) return KVM_ERR_CUDA;
-    a.heads_q = heads_of_chunk(tiles, a.q.H, 4 * 148);
-    a.chunks_q = (a.q.H + a.heads_q - 1) / a.heads_q;
-    ingest_q_kernel<D, MODE><<<dim3((unsigned)tiles, (unsigned)a.chunks_q), 256, SMEM, s>>>(a);
+    if (!room_for<ingest_q_kernel<D, MODE>, kTilesSmem<D, MODE>>()) return KVM_ERR_CUDA;
+    ingest_q_kernel<D, MODE><<<blocks, 256, kTilesSmem<D, MODE>, s>>>(a, ts);
   }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }

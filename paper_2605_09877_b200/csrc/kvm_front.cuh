@@ -288,7 +288,8 @@ __device__ __forceinline__ void norm(const FrontDev& f, const Pairs& w, const Pa
   sum_rows<D>(s);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float rstd = rsqrtf(fmaf(s[i], 1.f / D, f.eps));
+    float rstd;   // (2^-22.9; a variance that is no normal number counts as 0)
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(rstd) : "f"(fmaf(s[i], 1.f / D, f.eps)));
     const uint64_t r2 = pack2(rstd, rstd);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
