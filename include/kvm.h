@@ -398,6 +398,8 @@ typedef struct {
   double magnitude;                        /* of cos and sin; 1 unless a long context asks for another */
   int64_t original_len;                    /* PARTS: tokens, >= 1 */
   float eps;                               /* >= 0, with a norm */
+  const double* frequencies;               /* HOST [rope_dims / 2], f_i as kvm_rope_frequencies gives them (a program that calls often computes them
+                                              once), or any others: finite, 0 <= f_i <= 1; NULL: by the formula.  Read during the call */
   const float *q_weight, *q_bias;          /* device fp32 [n_q_heads, head_dim] or NULL (1, 0); NULL without a norm */
   const float *k_weight, *k_bias;          /* device fp32 [n_kv_heads, head_dim] */
 } kvm_front_t;

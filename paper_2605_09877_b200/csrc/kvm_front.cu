@@ -14,6 +14,7 @@ using cache::AppendOut;
 
 constexpr int kTokens = 4;    // tokens of a lane in the kernel over many rows
 constexpr int kRows = 4;      // rows of a lane in the kernel over pages
+constexpr int kFewRows = 16384;   // up to so many rows of q (and k) each is done by itself
 constexpr int kPagesAhead = 3;
 constexpr int kAhead = 3;     // stages of rows on their way (one of them is in use)
 
@@ -205,7 +206,7 @@ struct IngestArgs {
   int chunks, heads;    // head chunks of k and v
   int tpp;              // threads per page
   int groups;           // blocks that share the pages of one sequence
-  int64_t k_blocks;     // blocks of k, those of v follow
+  int64_t k_blocks;     // blocks of k, those of v follow, and of q where there are few rows
 };
 struct IngestTiles {    // what rows_tiles asks of a call over a cache
   const IngestArgs& a;
@@ -376,9 +377,35 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
   }
 }
 
+// Rows of q one by one, D / 8 lanes each.
+template <int D, int TH, int MODE>
+__device__ __forceinline__ void q_rows(const IngestArgs& a, int64_t block) {
+  constexpr int LPR = D / 8;
+  const Lane<D, MODE> L(a.f, threadIdx.x % LPR);
+  const Rows& r = a.q;
+  const int64_t row = block * (TH / LPR) + threadIdx.x / LPR;
+  const bool there = row < (int64_t)a.p.batch * a.p.T * r.H;
+  int64_t rest = there ? row : 0;
+  const int head = (int)(rest % r.H);
+  rest /= r.H;
+  const int b = (int)(rest / a.p.T), t = (int)(rest - b * a.p.T);
+  const Raw raw[1] = {load_raw(r.x + b * r.sx[0] + head * r.sx[1] + t * r.sx[2], L)};
+  int start, n;
+  const bool valid = cache::seq_lengths(a.p, b, start, n);
+  const Pairs w = load_affine(r.w, head, L, 1.f), bias = load_affine(r.b, head, L, 0.f);
+  const Turn turn[1] = {angles(a.f, L, (int64_t)start + t)};
+  Pairs p[1];
+  rows_through(a.f, L, raw, turn, w, bias, p);
+  store_row(r.y + b * r.sy[0] + head * r.sy[1] + t * r.sy[2], L, p[0], there && valid && t < n, nullptr);
+}
+
 template <int D, int TH, int MODE>
 __global__ void __launch_bounds__(TH, 512 / TH) ingest_pages_kernel(const __grid_constant__ IngestArgs a) {
   int64_t i = blockIdx.x;
+  if (i >= 2 * a.k_blocks) {   // (a call of few rows)
+    q_rows<D, TH, MODE == kMixed ? kSingle : MODE>(a, i - 2 * a.k_blocks);
+    return;
+  }
   const bool keys = i < a.k_blocks;
   if (!keys) i -= a.k_blocks;
   const int chunk = (int)(i % a.chunks);
@@ -499,6 +526,11 @@ static kvm_status_t check_front(const kvm_front_t* f, int d) {
     if (f->scaling != KVM_ROPE_PLAIN && !within(f->factor, 1.0, 1e30)) return KVM_ERR_INVALID_ARG;
     if (f->scaling == KVM_ROPE_PARTS && (f->original_len < 1 || !within(f->low, 0.0, 1e30) || !within(f->high, 0.0, 1e30) || f->low >= f->high)) return KVM_ERR_INVALID_ARG;
   }
+  if (f->frequencies) {
+    if (!cache::aligned(f->frequencies, 8)) return KVM_ERR_INVALID_ARG;
+    for (int i = 0; i < f->rope_dims / 2; ++i)
+      if (!within(f->frequencies[i], 0.0, 1.0)) return KVM_ERR_INVALID_ARG;
+  }
   for (const float* w : {f->q_weight, f->q_bias, f->k_weight, f->k_bias})
     if (!cache::aligned(w, 4)) return KVM_ERR_INVALID_ARG;
   return KVM_OK;
@@ -506,6 +538,7 @@ static kvm_status_t check_front(const kvm_front_t* f, int d) {
 
 // Radians per position of pair i.
 static double frequency(const kvm_front_t* f, int i) {
+  if (f->frequencies) return f->frequencies[i];
   const double w = std::pow(f->base, -2.0 * i / f->rope_dims);
   if (f->scaling == KVM_ROPE_LINEAR) return w / f->factor;
   if (f->scaling == KVM_ROPE_PARTS) {
@@ -591,7 +624,7 @@ static kvm_status_t launch_qk(QkArgs& a, cudaStream_t s) {
   constexpr int LPR = D / 8;
   const int H = a.r[0].H + a.r[1].H;
   const int64_t tokens = a.batch * a.T;
-  if (tokens * H <= 16384) {
+  if (tokens * H <= kFewRows) {
     qk_rows_kernel<D, MODE == kMixed ? kSingle : MODE><<<(unsigned)((tokens * H * LPR + 127) / 128), 128, 0, s>>>(a);
   } else {
     Tiles ts;
@@ -604,10 +637,10 @@ static kvm_status_t launch_qk(QkArgs& a, cudaStream_t s) {
 }
 
 template <int D, int TH, int MODE>
-static kvm_status_t launch_pages(const IngestArgs& a, cudaStream_t s) {
+static kvm_status_t launch_pages(const IngestArgs& a, int64_t q_rows, cudaStream_t s) {
   constexpr int SMEM = MODE == kSingle ? 0 : Stage<D, TH, kRows, kPagesAhead>::kBytes;
   if (!room_for<ingest_pages_kernel<D, TH, MODE>, SMEM>()) return KVM_ERR_CUDA;
-  ingest_pages_kernel<D, TH, MODE><<<(unsigned)(2 * a.k_blocks), TH, SMEM, s>>>(a);
+  ingest_pages_kernel<D, TH, MODE><<<(unsigned)(2 * a.k_blocks + (q_rows * (D / 8) + TH - 1) / TH), TH, SMEM, s>>>(a);
   return KVM_OK;
 }
 template <int D, int MODE>
@@ -624,15 +657,17 @@ static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   const int64_t pages = (p.T + p.page - 2) / p.page + 1;   // pages that T consecutive tokens can touch
   const int64_t groups = (pages + TH / a.tpp - 1) / (TH / a.tpp);
   a.groups = (int)groups;
-  a.heads = heads_of_chunk(groups * p.batch, p.Hkv, 4 * 148);
+  a.heads = heads_of_chunk(groups * p.batch, p.Hkv, 2 * 148);
   a.chunks = (p.Hkv + a.heads - 1) / a.heads;
   a.k_blocks = groups * p.batch * a.chunks;
   Tiles ts;
   int blocks = 0;
   if (2 * a.k_blocks > INT32_MAX || (a.q.H > 0 && !tiles_of_call<D>(p.batch, p.T, a.q.H, ts, blocks))) return KVM_ERR_UNSUPPORTED;
-  const kvm_status_t rc = TH == 256 ? launch_pages<D, 256, MODE>(a, s) : launch_pages<D, 512, MODE>(a, s);
+  const int64_t q_rows = (int64_t)p.batch * p.T * a.q.H;
+  const bool few = q_rows <= kFewRows;   // (they go with the pages: one launch)
+  const kvm_status_t rc = TH == 256 ? launch_pages<D, 256, MODE>(a, few ? q_rows : 0, s) : launch_pages<D, 512, MODE>(a, few ? q_rows : 0, s);
   if (rc != KVM_OK) return rc;
-  if (a.q.H > 0) {
+  if (!few) {
     if (!room_for<ingest_q_kernel<D, MODE>, kTilesSmem<D, MODE>>()) return KVM_ERR_CUDA;
     ingest_q_kernel<D, MODE><<<blocks, 256, kTilesSmem<D, MODE>, s>>>(a, ts);
   }

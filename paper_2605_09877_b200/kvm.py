@@ -85,7 +85,7 @@ class CacheCall(C.Structure):
 class FrontDesc(C.Structure):
     _fields_ = [("norm", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("rope_dims", C.c_int32),
                 ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double),
-                ("original_len", C.c_int64), ("eps", C.c_float),
+                ("original_len", C.c_int64), ("eps", C.c_float), ("frequencies", C.POINTER(C.c_double)),
                 ("q_weight", C.c_void_p), ("q_bias", C.c_void_p), ("k_weight", C.c_void_p), ("k_bias", C.c_void_p)]
 
 
@@ -525,13 +525,17 @@ class KVMState:
         return slot, app
 
 
+_THREE = C.c_int64 * 3
+
+
 def _strides3(t):
     """Element strides of the first three dims; None where the tensor is contiguous."""
     if t.is_contiguous():
         return None
-    if t.shape[3] > 1 and t.stride(3) != 1:
+    b, h, n, c = t.stride()
+    if c != 1 and t.shape[3] > 1:
         raise ValueError("the channels of a row must be contiguous")
-    return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
+    return _THREE(b, h, n)
 
 
 def _int(x, bits=32):
@@ -572,19 +576,27 @@ class Front:
                 raise ValueError(f"{x!r} is none of {names}")
             kinds.append(names.index(x))
         self._affine = (q_weight, q_bias, k_weight, k_bias)
-        self._device = None
+        self._device = -1
         for t in self._affine:
             if t is not None:
-                if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or self._device not in (None, t.device):
+                if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or self._device not in (-1, t.get_device()):
                     raise ValueError("weights and biases are contiguous float32 [heads, head_dim] on one CUDA device")
-                self._device = t.device
+                self._device = t.get_device()
+        self._shapes = []
         for pair in (self._affine[:2], self._affine[2:]):
-            if None not in pair and pair[0].shape != pair[1].shape:
+            shapes = [tuple(t.shape) for t in pair if t is not None]
+            if len(set(shapes)) > 1:
                 raise ValueError("a bias has its weight's shape")
+            self._shapes.append(shapes[0] if shapes else None)
         self.rope_dims = _int(rope_dims)
-        self._desc = FrontDesc(*kinds, self.rope_dims, base, factor, low, high, magnitude, _int(original_len, 64), eps,
+        self._desc = FrontDesc(*kinds, self.rope_dims, base, factor, low, high, magnitude, _int(original_len, 64), eps, None,
                                *(t.data_ptr() if t is not None else None for t in self._affine))
         self._ref = C.byref(self._desc)
+        if self.rope_dims > 0:
+            # computed once (for one of the two widths of heads that there are: they do not depend on it)
+            self._frequencies = (C.c_double * 64)()
+            if lib.kvm_rope_frequencies(self._ref, 128, self._frequencies) == KVM_OK:   # (what is wrong with the rest, a call says)
+                self._desc.frequencies = C.cast(self._frequencies, C.POINTER(C.c_double))
 
     def frequencies(self, head_dim: int):
         """Radians per position of each pair (kvm_rope_frequencies), a list of rope_dims / 2."""
@@ -594,57 +606,56 @@ class Front:
             raise KVMError(rc, "kvm_rope_frequencies")
         return list(out[:self.rope_dims // 2])
 
-    def _check(self, q, k, device):
-        """That the weights are those of q's and k's heads."""
-        if self._device not in (None, device):
-            raise ValueError("weights and biases are on the rows' device")
-        for x, pair in ((q, self._affine[:2]), (k, self._affine[2:])):
-            for t in pair:
-                if x is not None and t is not None and tuple(t.shape) != (x.shape[1], x.shape[3]):
-                    raise ValueError("weights and biases [heads, head_dim]")
+
+def _front_rows(x, out, device, front, which, batch, tokens, head_dim):
+    """Checks rows of q (which 0), k (1) or v (2) and their out, or None, for a front-end call; their number of heads."""
+    if x.dtype != torch.bfloat16 or x.get_device() != device or x.dim() != 4:
+        raise ValueError("rows are bfloat16 [batch, heads, tokens, head_dim] on one CUDA device")
+    B, H, T, d = shape = x.shape
+    if B != batch or T != tokens or d != head_dim:
+        raise ValueError("q, k and v have the same batch, tokens and head_dim")
+    if out is not None and (out.shape != shape or out.dtype != torch.bfloat16 or out.get_device() != device):
+        raise ValueError("an out has its input's shape, type and device")
+    if which < 2 and front._shapes[which] is not None and (front._shapes[which] != (H, d) or front._device != device):
+        raise ValueError("weights and biases [heads, head_dim] on the rows' device")
+    return H
 
 
-def _front_rows(pairs, lengths):
-    """Checks (rows, their out or None) pairs and the int32 tensors of a front-end call."""
-    first = next(x for x, _ in pairs if x is not None)
-    for x, y in pairs:
-        for t in (x, y):
-            if t is not None and (t.dtype != torch.bfloat16 or not t.is_cuda or t.device != first.device or t.dim() != 4):
-                raise ValueError("rows are bfloat16 [batch, heads, tokens, head_dim] on one CUDA device")
-        if x is not None:
-            if (x.shape[0], x.shape[2], x.shape[3]) != (first.shape[0], first.shape[2], first.shape[3]):
-                raise ValueError("q and k have the same batch, tokens and head_dim")
-            if y is not None and y.shape != x.shape:
-                raise ValueError("an out has its input's shape")
-    for t in lengths:
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != first.device):
-            raise ValueError("start, count and status are contiguous int32 tensors on the rows' device")
-    return first
+def _other_stream(stream):
+    """Whether a stream is given that is not the current one."""
+    return stream is not None and stream != torch.cuda.current_stream()
 
 
 def qk_norm_rope(q, k, front: Front, start=None, count=None, q_out=None, k_out=None, status=None, stream=None):
     """kvm_qk_norm_rope: q bf16 [B, n_q_heads, T, head_dim] and k bf16 [B, n_kv_heads, T, head_dim] (channels contiguous; either may be None) through
     `front`, at positions start[b] + t (start None: t).  Returns (q_out, k_out), made here unless given; an out may be its input.  Rows behind a sequence's
     count are left as they were (unset where the out is made here).  `status` as in Cache."""
-    if q is None and k is None:
+    x = q if q is not None else k
+    if x is None:
         raise ValueError("q or k")
-    x = _front_rows(((q, q_out), (k, k_out)), (start, count, status))
+    device = x.get_device()
+    if device < 0 or x.dim() != 4:
+        raise ValueError("rows are bfloat16 [batch, heads, tokens, head_dim] on one CUDA device")
     B, _, T, d = x.shape
-    for t in (start, count):
-        if t is not None and t.numel() != B:
-            raise ValueError("start [batch], count [batch]")
-    front._check(q, k, x.device)
-    if torch._C._cuda_getDevice() != x.device.index or (stream is not None and stream != torch.cuda.current_stream()):
-        with torch.cuda.device(x.device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
+    Hq = _front_rows(q, q_out, device, front, 0, B, T, d) if q is not None else 0
+    Hk = _front_rows(k, k_out, device, front, 1, B, T, d) if k is not None else 0
+    for t in (start, count, status):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != device or (t is not status and t.numel() != B)):
+            raise ValueError("start [batch], count [batch] and status are contiguous int32 tensors on the rows' device")
+    if torch._C._cuda_getDevice() != device or _other_stream(stream):
+        with torch.cuda.device(device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
             return qk_norm_rope(q, k, front, start, count, q_out, k_out, status)
-    outs = [y if y is not None or t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t, y in ((q, q_out), (k, k_out))]
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    st = lambda t: _strides3(t) if t is not None else None  # noqa: E731
-    rc = lib.kvm_qk_norm_rope(front._ref, ptr(q), ptr(k), ptr(start), ptr(count), B, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, T, d,
-                              ptr(outs[0]), ptr(outs[1]), st(q), st(k), st(outs[0]), st(outs[1]), ptr(status), _stream_ptr(None))
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=k.device)
+    rc = lib.kvm_qk_norm_rope(front._ref, q.data_ptr() if Hq else None, k.data_ptr() if Hk else None, start.data_ptr() if start is not None else None,
+                              count.data_ptr() if count is not None else None, B, Hq, Hk, T, d, q_out.data_ptr() if Hq else None, k_out.data_ptr() if Hk else None,
+                              _strides3(q) if Hq else None, _strides3(k) if Hk else None, _strides3(q_out) if Hq else None, _strides3(k_out) if Hk else None,
+                              status.data_ptr() if status is not None else None, _stream_ptr(None))
     if rc != KVM_OK:
         raise KVMError(rc, "kvm_qk_norm_rope")
-    return tuple(outs)
+    return q_out, k_out
 
 
 class Cache:
@@ -709,21 +720,27 @@ class Cache:
     def ingest(self, q, k, v, front: Front, pages, start, count=None, q_out=None, status=None, stream=None):
         """kvm_cache_ingest: q and k bf16 [B, heads, T, head_dim] through `front` at positions start[b] + t, k and v into the cache behind the tokens that the
         sequences hold.  Returns q_out, made here unless given; it may be q.  q may be None: k and v only."""
-        if k.dim() != 4 or v.shape != k.shape or k.shape[1] != self.n_kv_heads or k.shape[3] != self.head_dim:
+        if k.dim() != 4 or k.shape[1] != self.n_kv_heads or k.shape[3] != self.head_dim or v.shape != k.shape:
             raise ValueError("k, v [batch, n_kv_heads, tokens, head_dim]")
-        if q is None and q_out is not None:
-            raise ValueError("q_out without q")
-        _front_rows(((k, None), (v, None), (q, q_out)), ())
-        front._check(q, k, k.device)
-        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+        device = self._device.index
+        B, _, T, d = k.shape
+        _front_rows(k, None, device, front, 1, B, T, d)
+        _front_rows(v, None, device, front, 2, B, T, d)
+        if q is None:
+            if q_out is not None:
+                raise ValueError("q_out without q")
+            Hq = 0
+        else:
+            Hq = _front_rows(q, q_out, device, front, 0, B, T, d)
+        if torch._C._cuda_getDevice() != device or _other_stream(stream):
             with torch.cuda.device(self._device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
                 return self.ingest(q, k, v, front, pages, start, count, q_out, status)
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        call = self._call(pages, start, count, (k, v), status)
-        rc = lib.kvm_cache_ingest(self._ref, call, front._ref, q.data_ptr() if q is not None else None, q.shape[1] if q is not None else 0, k.data_ptr(), v.data_ptr(),
-                                  q_out.data_ptr() if q is not None else None, _strides3(q) if q is not None else None, _strides3(k), _strides3(v),
-                                  _strides3(q_out) if q is not None else None, status.data_ptr() if status is not None else None, _stream_ptr(None))
+        if Hq and q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        call = self._call(pages, start, count, (k,), status)
+        rc = lib.kvm_cache_ingest(self._ref, call, front._ref, q.data_ptr() if Hq else None, Hq, k.data_ptr(), v.data_ptr(), q_out.data_ptr() if Hq else None,
+                                  _strides3(q) if Hq else None, _strides3(k), _strides3(v), _strides3(q_out) if Hq else None,
+                                  status.data_ptr() if status is not None else None, _stream_ptr(None))
         if rc != KVM_OK:
             raise KVMError(rc, "kvm_cache_ingest")
         return q_out
@@ -735,7 +752,7 @@ class Cache:
         for t in (k_out, v_out):
             if t is not None and tuple(t.shape) != shape:
                 raise ValueError("k_out, v_out [batch, n_kv_heads, n_tokens, head_dim]")
-        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+        if self._elsewhere() or _other_stream(stream):
             with torch.cuda.device(self._device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
                 return self.read(pages, start, n_tokens, count, k_out, v_out, status)
         k_out, v_out = (torch.empty(shape, dtype=torch.bfloat16, device=self._device) if t is None else t for t in (k_out, v_out))
@@ -780,7 +797,7 @@ class Cache:
                 raise ValueError("groups and shared are contiguous int32 tensors on the cache's device")
         if groups.numel() != shared.numel() + 1:
             raise ValueError("groups [n_groups + 1], shared [n_groups]")
-        if self._elsewhere() or (stream is not None and stream != torch.cuda.current_stream()):
+        if self._elsewhere() or _other_stream(stream):
             with torch.cuda.device(self._device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
                 return self.attend_shared(q, pages, start, groups, shared, count, scale, out, status)
         if out is None:

@@ -53,6 +53,17 @@ def test_frequencies(kvm, r, rope):
     assert len(got) == r // 2 and np.allclose(got, want, rtol=2.0 ** -49, atol=0)
 
 
+def test_frequencies_of_ones_own(kvm):
+    own = (C.c_double * 16)(*[0.5 ** i for i in range(16)])
+    out = (C.c_double * 16)()
+    assert kvm.lib.kvm_rope_frequencies(C.byref(_front(kvm, frequencies=C.cast(own, C.POINTER(C.c_double)))), 128, out) == 0 and list(out) == list(own)
+    for bad in (math.nan, -0.1, 1.5, math.inf):
+        own[15] = bad
+        assert kvm.lib.kvm_rope_frequencies(C.byref(_front(kvm, frequencies=C.cast(own, C.POINTER(C.c_double)))), 128, out) == 1
+    own[15] = 7.0                                      # (behind the pairs that there are: not looked at)
+    assert kvm.lib.kvm_rope_frequencies(C.byref(_front(kvm, rope_dims=30, frequencies=C.cast(own, C.POINTER(C.c_double)))), 128, out) == 0
+
+
 def test_frequencies_by_parts_keep_the_fast_pairs_and_interpolate_the_slow_ones(kvm):
     plain = kvm.Front(norm="none", rope_dims=128).frequencies(128)
     parts = kvm.Front(norm="none", rope_dims=128, scaling="parts", factor=16.0, original_len=8192).frequencies(128)
@@ -64,7 +75,7 @@ def test_frequencies_by_parts_keep_the_fast_pairs_and_interpolate_the_slow_ones(
 # ---- refusals: before anything is launched ---------------------------------------------------------------------------
 
 def _front(kvm, **kw):
-    c = dict(norm=1, layout=0, scaling=0, rope_dims=32, base=1e4, factor=1.0, low=1.0, high=32.0, magnitude=1.0, original_len=0, eps=1e-5,
+    c = dict(norm=1, layout=0, scaling=0, rope_dims=32, base=1e4, factor=1.0, low=1.0, high=32.0, magnitude=1.0, original_len=0, eps=1e-5, frequencies=None,
              q_weight=None, q_bias=None, k_weight=None, k_bias=None)
     c.update(kw)
     return kvm.FrontDesc(*[c[f[0]] for f in kvm.FrontDesc._fields_])
