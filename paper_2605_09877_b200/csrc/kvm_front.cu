@@ -220,6 +220,12 @@ struct IngestTiles {    // what rows_tiles asks of a call over a cache
 __device__ __forceinline__ int least_exp(uint32_t bits) {
   return max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), cache::kLeastExp);
 }
+// max(|a|, |b|, |c|); NaN if one is
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // A lane's eight values as codes, in the order of memory (two runs of four channels) where the layout has runs.
 __device__ __forceinline__ void codes_of(const float (&v)[8], float inv, uint32_t& a, uint32_t& b) {
   a = cache::to_e4m3x2(v[0] * inv, v[1] * inv) | (cache::to_e4m3x2(v[2] * inv, v[3] * inv) << 16);
@@ -326,7 +332,6 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
     if (!STAGED) px += r.sx[1];
     if (++stage == S) stage = 0;
     float v[CH][8];
-    uint32_t top = 0;
     if (KEYS) {
       const Pairs w = load_affine(r.w, h, L, 1.f), bias = load_affine(r.b, h, L, 0.f);
       Pairs x[CH];
@@ -337,20 +342,20 @@ __device__ __forceinline__ void pages_tile(const IngestArgs& a, int group, int c
 #pragma unroll
       for (int i = 0; i < CH; ++i) values_of(raw[i], v[i]);
     }
+    float most = 0.f;   // (a NaN stays one: above all others in what follows)
 #pragma unroll
     for (int i = 0; i < CH; ++i)
       if (fresh >> i & 1) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+        for (int j = 0; j < 8; j += 2) most = max_abs(most, v[i][j], v[i][j + 1]);
       }
-    top = __reduce_max_sync(0xffffffffu, top);
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu);
     if (tpp > 32) {   // (uniform)
       const int at = (h - h0) & 1;   // (two sets: a thread is never two heads ahead of another)
       if ((threadIdx.x & 31) == 0) s_top[at][warp] = top;
       __syncthreads();
-      const int warps = tpp / 32, w0 = warp & ~(warps - 1);
-#pragma unroll 1
-      for (int w = 0; w < warps; ++w) top = max(top, s_top[at][w0 + w]);
+      const int warps = tpp / 32;
+      top = __reduce_max_sync(0xffffffffu, s_top[at][(warp & ~(warps - 1)) + (threadIdx.x & (warps - 1))]);
     } else {
       __syncwarp();   // (every lane has read the old scale before one writes the new one)
     }
@@ -556,7 +561,7 @@ static FrontDev device_front(const kvm_front_t* f) {
   x.half = f->layout == KVM_ROPE_HALF;
   x.h = f->rope_dims / 2;
   x.mag = x.h ? (float)f->magnitude : 1.f;
-  for (int i = 0; i < x.h; ++i) x.quarter[i] = frequency(f, i) / 1.570796326794896619231;
+  for (int i = 0; i < x.h; ++i) x.turns[i] = (uint64_t)std::ldexp((long double)frequency(f, i) / 6.283185307179586476925L, 64);   // (f_i <= 1: below a sixth)
   return x;
 }
 

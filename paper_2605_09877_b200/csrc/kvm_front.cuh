@@ -10,8 +10,9 @@
 // Aligned rows come by way of shared memory, 16 bytes per lane (Stage): what a kernel has on its way costs no registers, several heads ahead, and a lane
 // takes its channels from there.
 //
-// Angles: position * f_i in quarter turns in fp64 (off by 2^-52 of the angle: 2^-32 of a quarter turn at position 2^20), the nearest whole number taken
-// off and counted as a quadrant, so that the fp32 argument of sin and cos is at most 1/8 turn and rounded to 2^-26 of a quarter turn.
+// Angles: f_i as a fraction of a turn in units of 2^-64, so that the product with a position, which drops whole turns, is off by 2^-34 of a turn at position 2^31
+// at most; the quadrant is its top two bits (rounded), what is left is within 1/8 turn, and sin and cos of that are their Taylor polynomials (the terms left out are
+// below 2e-9).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -23,7 +24,7 @@ namespace kvm {
 namespace front {
 
 struct FrontDev {
-  double quarter[64];   // quarter turns per position of each pair
+  uint64_t turns[64];   // 2^64 turns per position of each pair
   float mag, eps;
   int norm, half, h;    // half: pairs (i, i + h)
 };
@@ -198,11 +199,12 @@ __device__ __forceinline__ Turn angles(const FrontDev& f, const Lane<D, MODE>& L
     c[j] = 1.f;
     s[j] = 0.f;
     if (!L.rotated(j)) continue;
-    const double t = (double)pos * f.quarter[L.i0 + j], n = rint(t);
-    const int q = (int)((long long)n & 3);
-    float sn, cs;
-    sincospif((float)(t - n) * 0.5f, &sn, &cs);
-    const float a = q & 1 ? sn : cs, b = q & 1 ? cs : sn;   // cos(u + q pi/2), sin(u + q pi/2)
+    const uint64_t u = f.turns[L.i0 + j] * (uint64_t)pos + (1ull << 61);         // (modulo whole turns)
+    const int q = (int)(u >> 62), rest = (int)((u >> 32) & 0x3fffffffu) - (1 << 29);   // quadrant, and 2^-32 turns within it
+    const float x = (float)rest * 1.4629180792671596e-09f, xx = x * x;           // 2 pi / 2^32
+    const float sn = x * fmaf(fmaf(fmaf(fmaf(1.f / 362880, xx, -1.f / 5040), xx, 1.f / 120), xx, -1.f / 6), xx, 1.f);
+    const float cs = fmaf(fmaf(fmaf(fmaf(fmaf(-1.f / 3628800, xx, 1.f / 40320), xx, -1.f / 720), xx, 1.f / 24), xx, -0.5f), xx, 1.f);
+    const float a = q & 1 ? sn : cs, b = q & 1 ? cs : sn;   // cos(x + q pi/2), sin(x + q pi/2)
     c[j] = f.mag * (q == 1 || q == 2 ? -a : a);
     s[j] = f.mag * (q >= 2 ? -b : b);
   }
