@@ -22,6 +22,7 @@
 //   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "kvm_cache.cuh"
 #include "kvm_internal.h"
@@ -49,11 +50,16 @@ static_assert(kHigh + kBias <= 124 && kBias - kLow - kCode - 6 >= -126 + 24, "ra
 constexpr float kShift = 6.f;    // what the kernels for few and for many tokens count their weights in (of 2^-8 and 2^-6 of the reference)
 constexpr float kDecodeShift = 8.f;
 
+// A sequence, as shared_kernel leaves it for the merge: lengths (n = 0: no rows), its group's shared blocks and rows, its first row among them, the group's
+// place in the list, and how the list is dealt.
+struct alignas(16) SeqInfo { int start, n, blocks, rows, row0, pre, at, deal; };
+
 struct SharedArgs {
   AttendArgs a;
   FastDiv by_seq, by_group;      // rows of a sequence, heads of a group
   int seq_rows, grid, q_vec, out_vec;
   float* part;                   // partial results of shared_kernel
+  struct SeqInfo* seqs;          // [batch]: what the merge has to know
   // what the kernels over the other blocks leave: of few tokens (cols columns), of many (cols = 0)
   const float* own;
   int cols, workers;
@@ -62,8 +68,10 @@ struct SharedArgs {
 
 // What there is to do: prefix sums over the groups, in shared memory.
 struct Plan {
-  const int *offsets, *pre, *rows;   // sequences, weight of the list, rows of the partial results before each group
-  int total, share;
+  const int *offsets, *pre, *rows;   // sequences, positions of the list, rows of the partial results before each group
+  int total, share;                  // positions; of a CTA
+  bool whole;                        // every unit begins with a share: its positions are rounded up to whole ones
+  __device__ __forceinline__ int length(int weight) const { return whole ? (weight + share - 1u) / (uint32_t)share * share : weight; }
 };
 // One unit, as a CTA sees it that begins at position f of the list and ends at most at `end`.
 struct Unit {
@@ -93,50 +101,91 @@ __device__ __forceinline__ int pad8(int x) { return (x + 7) & ~7; }
 __device__ __forceinline__ int weight_of(int n) { return n > 128 ? 2 : 1; }
 __device__ __forceinline__ int space_of(int n) { return n > 128 ? 256 : 2 * pad8(n); }
 
-// The plan, by all NT threads of a block; mem: 3 (n_groups + 1) ints and a scratch of NT / 32 (two sums each).  false: groups that are none.
-template <int NT>
-__device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, int2* scratch, Plan& plan) {
+// The plan, by one warp; mem: 3 (n_groups + 1) ints.  false: groups that are none.
+// Where there are no more units than CTAs, a share is the least of 32 lengths (or that of the longest unit) with which every CTA has tiles of one unit only: a unit
+// that begins in the middle of a share costs its CTA a start and an end more, 6 us, and the others wait for it.
+__device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& plan) {
   const Groups& gr = s.a.groups;
   const Params& p = s.a.p;
   int *offsets = mem, *pre = offsets + gr.n + 1, *rows = pre + gr.n + 1;
   plan.offsets = offsets; plan.pre = pre; plan.rows = rows;
   plan.total = 0;
-  plan.share = 1;
-  if (!load_groups<NT>(gr, p.batch, offsets)) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
-    return false;
-  }
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = (gr.n + NT - 1) / NT, g0 = tid * per;
-  int2 sum = make_int2(0, 0);
+  plan.share = 2;
+  plan.whole = false;
+  constexpr uint32_t kAll = 0xffffffffu;
+  const int lane = threadIdx.x & 31;
+  bool ok = true;
+  int tiles_sum = 0, units = 0, most = 0;   // weights of all units, their number, the largest
 #pragma unroll 1
-  for (int g = g0; g < min(g0 + per, gr.n); ++g) {
-    pre[g] = sum.x;
-    rows[g] = sum.y;
-    const int n = rows_of_group(s, offsets, g), blocks = blocks_of_group(s, g);
-    if (blocks < 0 && blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
-    if (n > 0 && blocks > 0) {
-      const int full = n >> 8, left = n & 255;
-      sum.x += p.Hkv * tiles_of(p, blocks) * (2 * full + (left ? weight_of(left) : 0));
-      sum.y += p.Hkv * (256 * full + (left ? space_of(left) : 0));
+  for (int g0 = 0; g0 <= gr.n; g0 += 32) {
+    // sequences before a group; its key tiles (in `pre` for now)
+    const int g = g0 + lane;
+    if (g <= gr.n) {
+      const int at = gr.offsets[g], end = g < gr.n ? gr.offsets[g + 1] : at, blocks = g < gr.n ? blocks_of_group(s, g) : 0;
+      offsets[g] = at;
+      ok = ok && end >= at && (g > 0 || at == 0) && (g < gr.n || at == p.batch);
+      if (blocks < 0 && blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
+      const int n = (end - at) * s.seq_rows, tiles = n > 0 && blocks > 0 ? tiles_of(p, blocks) : 0, full = n >> 8, left = n & 255;
+      pre[g] = tiles;
+      if (tiles > 0) {
+        tiles_sum += p.Hkv * tiles * (2 * full + (left ? weight_of(left) : 0));
+        units += p.Hkv * (full + (left ? 1 : 0));
+        most = max(most, tiles * weight_of(n));
+      }
     }
   }
-  int2 incl = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, incl.x, o), y = __shfl_up_sync(0xffffffffu, incl.y, o);
-    if (lane >= o) { incl.x += x; incl.y += y; }
+  if (!__all_sync(kAll, ok)) {
+    if (blockIdx.x == 0 && lane == 0) report(p.status, KVM_ERR_INVALID_ARG);
+    return false;
   }
-  if (lane == 31) scratch[warp] = incl;
-  __syncthreads();
-  int2 add = make_int2(incl.x - sum.x, incl.y - sum.y);
+  __syncwarp();
+  units = __reduce_add_sync(kAll, units);
+  plan.share = max(2, (__reduce_add_sync(kAll, tiles_sum) + s.grid - 1) / s.grid);   // (both streams have something to do, and no share within a unit is empty)
+  if (units <= s.grid && units > 0) {
+    // every lane: how many CTAs the length share * (1 + lane / 16) takes
+    const uint32_t length = plan.share + plan.share * lane / 16;
+    int ctas = 0;
 #pragma unroll 1
-  for (int w = 0; w < warp; ++w) { add.x += scratch[w].x; add.y += scratch[w].y; }
+    for (int g0 = 0; g0 < gr.n; g0 += 32) {
+      const int g = g0 + lane, t = g < gr.n ? pre[g] : 0, n = t > 0 ? rows_of_group(s, offsets, g) : 0;
 #pragma unroll 1
-  for (int g = g0; g < min(g0 + per, gr.n); ++g) { pre[g] += add.x; rows[g] += add.y; }
-  if (tid == NT - 1) pre[gr.n] = add.x + sum.x;
-  __syncthreads();
-  plan.total = pre[gr.n];
-  plan.share = max(2, (plan.total + s.grid - 1) / s.grid);   // (both streams have something to do, and no share within a unit is empty)
+      for (uint32_t there = __ballot_sync(kAll, t > 0); there; there &= there - 1) {
+        const int i = __ffs(there) - 1, rows_i = __shfl_sync(kAll, n, i), full = rows_i >> 8, left = rows_i & 255;
+        const uint32_t tiles = __shfl_sync(kAll, t, i);
+        if (full) ctas += full * ((2 * tiles + length - 1) / length);
+        if (left) ctas += (weight_of(left) * tiles + length - 1) / length;
+      }
+    }
+    const uint32_t fits = __ballot_sync(kAll, ctas * p.Hkv <= s.grid);
+    most = __reduce_max_sync(kAll, most);
+    plan.share = fits ? __shfl_sync(kAll, length, __ffs(fits) - 1) : max(2, most);
+    plan.whole = true;
+  }
+  int at_pre = 0, at_rows = 0;   // before the next 32 groups
+#pragma unroll 1
+  for (int g0 = 0; g0 <= gr.n; g0 += 32) {
+    const int g = g0 + lane, tiles = g < gr.n ? pre[g] : 0;
+    int x = 0, y = 0;
+    if (tiles > 0) {
+      const int n = rows_of_group(s, offsets, g), full = n >> 8, left = n & 255;
+      x = p.Hkv * ((full ? full * plan.length(2 * tiles) : 0) + (left ? plan.length(weight_of(left) * tiles) : 0));
+      y = p.Hkv * (256 * full + (left ? space_of(left) : 0));
+    }
+    const int x0 = x, y0 = y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int dx = __shfl_up_sync(kAll, x, o), dy = __shfl_up_sync(kAll, y, o);
+      if (lane >= o) { x += dx; y += dy; }
+    }
+    if (g <= gr.n) {
+      pre[g] = at_pre + x - x0;
+      rows[g] = at_rows + y - y0;
+    }
+    at_pre += __shfl_sync(kAll, x, 31);
+    at_rows += __shfl_sync(kAll, y, 31);
+  }
+  plan.total = at_pre;
+  __syncwarp();
   return true;
 }
 // Last g with pre[g] <= f < pre[n].
@@ -149,25 +198,29 @@ __device__ __forceinline__ int last_before(const int* pre, int n, int f) {
   }
   return lo;
 }
-// The unit of rows 256 rb .. of a (group, kv head).
-__device__ __forceinline__ Unit unit_of(const SharedArgs& s, const Plan& plan, int g, int blocks, int hk, int rb) {
+// The unit of rows 256 rb .. of kv head hk of a group: n rows behind `blocks` shared blocks, at position pre of the list, rows `at` of the partial results.
+__device__ __forceinline__ Unit unit_of(const Params& p, const Plan& plan, int n, int blocks, int pre, int at, int hk, int rb) {
   Unit u;
-  const int n = rows_of_group(s, plan.offsets, g), full = n >> 8, left = n & 255;
-  u.g = g; u.hk = hk; u.blocks = blocks;
-  u.tiles = tiles_of(s.a.p, blocks);
+  const int full = n >> 8, left = n & 255;
+  u.hk = hk; u.blocks = blocks;
+  u.tiles = tiles_of(p, blocks);
   u.row0 = rb * 256;
   u.n = min(256, n - u.row0);
   u.w = weight_of(u.n);
   u.pitch = u.w == 2 ? 128 : pad8(u.n);
-  u.begin = plan.pre[g] + u.tiles * (hk * (2 * full + (left ? weight_of(left) : 0)) + 2 * rb);
-  u.at = plan.rows[g] + hk * (256 * full + (left ? space_of(left) : 0)) + 256 * rb;
+  const int long_one = plan.length(2 * u.tiles), per = full * long_one + (left ? plan.length(weight_of(left) * u.tiles) : 0);
+  u.begin = pre + hk * per + rb * long_one;
+  u.at = at + hk * (256 * full + (left ? space_of(left) : 0)) + 256 * rb;
   return u;
 }
 __device__ __forceinline__ Unit unit_at(const SharedArgs& s, const Plan& plan, int f) {
   const int g = last_before(plan.pre, s.a.groups.n, f), blocks = blocks_of_group(s, g), tiles = tiles_of(s.a.p, blocks);
   const int n = rows_of_group(s, plan.offsets, g), full = n >> 8, left = n & 255;
-  const int per = tiles * (2 * full + (left ? weight_of(left) : 0)), rest = f - plan.pre[g], hk = rest / per;
-  return unit_of(s, plan, g, blocks, hk, min(full, (rest - hk * per) / (2 * tiles)));
+  const int long_one = plan.length(2 * tiles), per = full * long_one + (left ? plan.length(weight_of(left) * tiles) : 0);
+  const int rest = f - plan.pre[g], hk = rest / per;
+  Unit u = unit_of(s.a.p, plan, n, blocks, plan.pre[g], plan.rows[g], hk, min(full, (rest - hk * per) / long_one));
+  u.g = g;
+  return u;
 }
 // The CTA's next unit with tiles behind position f of the list; its share is [w0, w1).
 template <class Segment>
@@ -177,7 +230,7 @@ __device__ __forceinline__ bool segment_at(const SharedArgs& s, const Plan& plan
     int je;
     g.u.of(w0, plan.share, g.jb, je);
     g.n = je - g.jb;
-    f = g.u.begin + g.u.tiles * g.u.w;
+    f = g.u.begin + plan.length(g.u.tiles * g.u.w);
     if (g.n > 0) return true;
   }
   return false;
@@ -201,13 +254,14 @@ struct alignas(16) KeyTile {
 };
 
 enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 26, SB_PVDONE = 28, SB_QFULL = 30,
-       SB_VBASE = 32, SB_COUNT = 36 };
+       SB_VBASE = 32, SB_COUNT = 36 };   // SB_QFULL: per row tile
 
 struct Segment { Unit u; int jb, n; };
-struct Walk {           // how far the softmax warps are, so that their registers need not hold it
+struct Walk {           // a CTA's place in the list: its first one, and how far the softmax warps are (their registers need not hold it)
   Plan plan;
-  int f, w0, w1;
-  Segment g;
+  int f, w0, w1;        // where the next segment may begin; the share
+  bool planned;
+  Segment g;            // (n = 0: none)
 };
 
 template <int D>
@@ -223,13 +277,13 @@ struct SharedCfg {
   static constexpr int OFF_X = OFF_CQ + 2 * 128 * 4;                       // float [stream][half][128]: maxima, sums
   static constexpr int OFF_BAR = OFF_X + 4 * 128 * 4;
   static constexpr int OFF_WALK = OFF_BAR + 512;
-  static constexpr int OFF_PLAN = OFF_WALK + 128;        // int [3][n_groups + 1]
+  static constexpr int OFF_PLAN = OFF_WALK + 256;        // int [3][n_groups + 1]
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static int smem(int n_groups) { return std::max(OFF_PLAN + 12 * (n_groups + 1) + 1024, 120 * 1024); }
   static constexpr uint32_t COL_S = 0, COL_O = 256;      // of stream s: + 128 s
   static_assert(NK <= 6 && NV8 <= 4 && NK + 2 <= kInfo, "rings");
   static_assert(OFF_K % 1024 == 0 && OFF_V8 % 1024 == 0 && OFF_V % 1024 == 0 && OFF_INFO % 16 == 0 && OFF_CQ % 16 == 0 && OFF_BAR % 8 == 0 && OFF_PLAN % 8 == 0, "alignment");
-  static_assert(sizeof(Walk) <= 128 && OFF_WALK % 8 == 0, "shared memory");
+  static_assert(sizeof(Walk) <= 128 && sizeof(Walk) % 8 == 0 && OFF_WALK % 8 == 0, "shared memory");
   static_assert(SB_COUNT * 8 + 128 <= 512 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
 };
 
@@ -251,8 +305,19 @@ __device__ __forceinline__ void pair_barrier(int id) {
   __syncwarp();
   asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
 }
-__device__ __forceinline__ void copy16_async(void* smem, const void* global) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(smem)), "l"(global) : "memory");
+// One thread of a warp (the same one every time).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+// Eight bf16 of any alignment.
+__device__ __forceinline__ uint4 load8(const __nv_bfloat16* src) {
+  const uint16_t* s = reinterpret_cast<const uint16_t*>(src);
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = s[2 * i] | (uint32_t)s[2 * i + 1] << 16;
+  return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
 template <int D>
@@ -277,7 +342,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   if (warp == 0) {
     for (int i = lane; i < SB_COUNT; i += 32) {
       auto in = [&](int first, int n) { return i >= first && i < first + n; };
-      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) ? 4 : in(SB_PREADY, 2) ? 8 : in(SB_QFULL, 1) ? 16 : 1);
+      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) ? 4 : in(SB_PREADY, 2) ? 8 : in(SB_QFULL, 2) ? 16 : 1);
     }
     if (lane == 0) {
       tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
@@ -291,23 +356,52 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   tc::tc_fence_before();
-  Plan plan;
-  const bool planned = make_plan<kThreads>(args, reinterpret_cast<int*>(base + Cfg::OFF_PLAN), reinterpret_cast<int2*>(base), plan);   // (scratch: where the queries go)
+  Walk& start = *reinterpret_cast<Walk*>(base + Cfg::OFF_WALK);
+  if (warp == 2) {
+    Walk x;
+    x.planned = make_plan(args, reinterpret_cast<int*>(base + Cfg::OFF_PLAN), x.plan);
+    x.f = x.w0 = x.planned ? (int)min((int64_t)x.plan.total, (int64_t)blockIdx.x * x.plan.share) : 0;
+    x.w1 = x.planned ? min(x.plan.total, x.w0 + x.plan.share) : 0;
+    x.g.n = 0;
+    if (!segment_at(args, x.plan, x.w0, x.w1, x.f, x.g)) x.g.n = 0;
+    if (lane == 0) start = x;
+  }
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int w0 = planned ? min(plan.total, (int)blockIdx.x * plan.share) : 0, w1 = planned ? min(plan.total, w0 + plan.share) : 0;
   auto fail = [&]() {
     if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
     *abort_flag = 1;
   };
   // The CTA's segments: (unit, key tiles).  Every warp walks them by itself, but for those of the softmax.
-  auto next_segment = [&](int& f, Segment& g) { return segment_at(args, plan, w0, w1, f, g); };
+  const Plan& plan = start.plan;
+  auto next_segment = [&](int& f, Segment& g) {
+    if (f >= 0) return segment_at(args, plan, start.w0, start.w1, f, g);
+    g = start.g;
+    f = start.f;
+    return g.n > 0;
+  };
   const int tshift = 7 - p.page_shift, ppt = 1 << tshift;
   Segment g;
-  int f = w0;
+  int f = -1;
   if (warp < 4) {
-    if (warp == 0 || warp == 3) {
+    if (warp == 2) {
+      // ------------------------------ what the merge has to know ------------------------------
+#pragma unroll 1
+      for (int b = blockIdx.x * 32 + lane; b < p.batch; b += args.grid * 32) {
+        SeqInfo x{0, 0, 0, 0, 0, 0, 0, plan.share * 2 + (plan.whole ? 1 : 0)};
+        if (start.planned) {
+          const int g = last_before(plan.offsets, a.groups.n, b);
+          x.blocks = blocks_of_group(args, g);
+          x.rows = rows_of_group(args, plan.offsets, g);
+          x.row0 = (b - plan.offsets[g]) * args.seq_rows;
+          x.pre = plan.pre[g];
+          x.at = plan.rows[g];
+          if (!shared_lengths(p, b, x.blocks, x.start, x.n)) x.n = 0;
+        }
+        args.seqs[b] = x;
+      }
+    } else if (warp == 0 || warp == 3) {
       // ------------------------------ producers of keys (warp 0) and values (warp 3) ------------------------------
       const bool keys = warp == 0;
       const int ring = keys ? Cfg::NK : Cfg::NV8, full = keys ? SB_KFULL : SB_V8FULL, empty = keys ? SB_KFREE : SB_V8FREE;
@@ -379,77 +473,107 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll 1
         for (int j = max(0, issued - ring); j < issued; ++j) tc::mbar_wait_tight(&bars[full + j % ring], (j / ring) & 1);
       }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
       // ------------------------------ products ------------------------------
-      // Items of a segment: row tile i % 2 on key tile i / 2, or key tile i, in either case stream i % 2.  One thread issues P V of item i and then, when it is
+      // Items of a segment: row tile i % 2 on key tile i / 2, or key tile i, in either case stream i % 2.  P V of item i is issued and then, when it is
       // done (its weights lie where S goes), S of item i + 2: while the tensor core does these two, the other stream is in its softmax.  (With S and
-      // P V issued by two threads they ran as P V, P V, S, S, and both streams were in their softmax at the same time.)
+      // P V issued by two threads they ran as P V, P V, S, S, and both streams were in their softmax at the same time.)  The whole warp walks through this and one
+      // thread issues, so that addresses and descriptors are uniform.
       constexpr uint32_t ID_S = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
       constexpr uint32_t ID_O = tc::idesc_f16(128, D, true) | (1u << 7) | (1u << 10);   // (format 1: bf16)
       auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
       const uint64_t dQ = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
       const uint64_t dV = tc::smem_desc_sw128(tc::smem_u32(base + Cfg::OFF_V), 128 * 128, 1024);
+      const bool leader = elect_one();
       bool ok = true;
-      int turn[2] = {0, 0};     // turns that the streams' softmax has been given (S, the same again, the end of a segment)
-      int back[2] = {0, 0};     // weights that have come back
-      int it[2] = {0, 0};       // P V so far
+      int turn0 = 0, turn1 = 0; // turns that the streams' softmax has been given (S, the same again, the end of a segment)
+      int back0 = 0, back1 = 0; // weights that have come back
+      int it0 = 0, it1 = 0;     // P V so far
       int J = 0;                // value tiles so far
+      int talls = 0;            // segments of two row tiles so far
       uint32_t s = 0, par = 0;  // ring of keys
-      auto wait = [&](int bar, uint32_t parity) { ok = ok && tc::mbar_wait_tight(&bars[bar], parity); return ok; };
+      auto wait = [&](int bar, uint32_t parity) {   // the same answer in every lane
+        ok = ok && __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[bar], parity));
+        return ok;
+      };
 #pragma unroll 1
       for (int seg = 0; ok && next_segment(f, g); ++seg) {
-        const int tall = g.u.tall() ? 1 : 0, items = g.n << tall;
-        if (!wait(SB_QFULL, seg & 1)) break;
-#pragma unroll 1
-        for (int i = -2; i < items; ++i) {
-          const int st = i & 1;
-          if (i >= 0) {
-            if ((!tall || st == 0) && !wait(SB_VFULL + (J & 1), (J >> 1) & 1)) break;
-            if (!wait(SB_PREADY + st, back[st]++ & 1)) break;
-            if (s_flag[st] == turn[st] - 1) {   // (at most once)
-              s_redo[st] = turn[st]++;
-              tc::mbar_arrive(&bars[SB_SFULL + st]);
-              if (!wait(SB_PREADY + st, back[st]++ & 1)) break;
-            }
-            tc::tc_fence_after();
-            const uint64_t v = dV + (J & 1) * (Cfg::T16 >> 4);
-            const uint32_t dO = tmem + Cfg::COL_O + 128 * st, aP = tmem + Cfg::COL_S + 128 * st;
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
-              tc::mma_f16_ts(dO, aP + 64 * (kk >> 2) + 8 * (kk & 3), v + kk * (2048 >> 4), ID_O, (i >= 2 || kk > 0) ? 1u : 0u);
-            tc::mma_commit(&bars[SB_PVDONE + st]);
-            if (!tall || st == 1) {
-              tc::mma_commit(&bars[SB_VFREE + (J & 1)]);
-              ++J;
-            }
-            if (i + 2 < items && !wait(SB_PVDONE + st, it[st] & 1)) break;
-            ++it[st];
-          }
-          if (i + 2 < items) {
-            if ((!tall || st == 0) && !wait(SB_KFULL + s, par)) break;
-            tc::tc_fence_after();
-            const uint64_t k = dK + s * (Cfg::T8 >> 4), q = dQ + (tall & st) * (2 * Cfg::T8 >> 4);
-            const uint32_t dS = tmem + Cfg::COL_S + 128 * st;
+        const bool tall = g.u.tall();
+        const int items = g.n << (tall ? 1 : 0);
+        // S of the next item of stream ST
+        auto issue_s = [&](auto ST) {
+          constexpr int st = decltype(ST)::value;
+          if ((!tall || st == 0) && !wait(SB_KFULL + s, par)) return;
+          tc::tc_fence_after();
+          const uint64_t k = dK + s * (Cfg::T8 >> 4), q = dQ + (tall && st ? 2 * Cfg::T8 >> 4 : 0);
+          const uint32_t dS = tmem + Cfg::COL_S + 128 * st;
+          if (leader) {
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, q + 2 * ks, k + 2 * ks, ID_S, ks > 0);
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, q + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID_S, 1u);
             tc::mma_commit(&bars[SB_SFULL + st]);
-            ++turn[st];
-            if (!tall || st == 1) {
-              tc::mma_commit(&bars[SB_KFREE + s]);
-              if (++s == Cfg::NK) { s = 0; par ^= 1; }
-            }
+            if (!tall || st == 1) tc::mma_commit(&bars[SB_KFREE + s]);
           }
+          __syncwarp();
+          ++(st ? turn1 : turn0);
+          if (!tall || st == 1) {
+            if (++s == Cfg::NK) { s = 0; par ^= 1; }
+          }
+        };
+        // P V of item i, of stream ST, and S of item i + 2
+        auto item = [&](int i, auto ST) {
+          constexpr int st = decltype(ST)::value;
+          int &turn = st ? turn1 : turn0, &back = st ? back1 : back0, &it = st ? it1 : it0;
+          if ((!tall || st == 0) && !wait(SB_VFULL + (J & 1), (J >> 1) & 1)) return;
+          if (!wait(SB_PREADY + st, back++ & 1)) return;
+          if (__any_sync(0xffffffffu, s_flag[st] == turn - 1)) {   // (at most once)
+            if (leader) {
+              s_redo[st] = turn;
+              tc::mbar_arrive(&bars[SB_SFULL + st]);
+            }
+            __syncwarp();
+            ++turn;
+            if (!wait(SB_PREADY + st, back++ & 1)) return;
+          }
+          tc::tc_fence_after();
+          const uint64_t v = dV + (J & 1) * (Cfg::T16 >> 4);
+          const uint32_t dO = tmem + Cfg::COL_O + 128 * st, aP = tmem + Cfg::COL_S + 128 * st, more = i >= 2 ? 1u : 0u;
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
+              tc::mma_f16_ts(dO, aP + 64 * (kk >> 2) + 8 * (kk & 3), v + kk * (2048 >> 4), ID_O, kk > 0 ? 1u : more);
+            tc::mma_commit(&bars[SB_PVDONE + st]);
+            if (!tall || st == 1) tc::mma_commit(&bars[SB_VFREE + (J & 1)]);
+          }
+          __syncwarp();
+          if (!tall || st == 1) ++J;
+          if (i + 2 < items && wait(SB_PVDONE + st, it & 1)) issue_s(ST);
+          ++it;
+        };
+        constexpr std::integral_constant<int, 0> S0{};
+        constexpr std::integral_constant<int, 1> S1{};
+        if (!wait(SB_QFULL, seg & 1)) break;
+        issue_s(S0);
+        if (items > 1) {
+          if (tall) wait(SB_QFULL + 1, talls++ & 1);
+          if (ok) issue_s(S1);
+        }
+#pragma unroll 1
+        for (int i = 0; i < items && ok; i += 2) {
+          item(i, S0);
+          if (ok && i + 1 < items) item(i + 1, S1);
         }
         if (!ok) break;
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {   // the end, when all products have landed
-          tc::mma_commit(&bars[SB_SFULL + st]);
-          ++turn[st];
+        if (leader) {   // the end, when all products have landed
+          tc::mma_commit(&bars[SB_SFULL]);
+          tc::mma_commit(&bars[SB_SFULL + 1]);
         }
+        __syncwarp();
+        ++turn0;
+        ++turn1;
       }
-      if (!ok) fail();
+      if (!ok && leader) fail();
     }
   } else if (warp >= 20) {
     // ------------------------------ values to fp16 ------------------------------
@@ -476,7 +600,6 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           tc::mbar_arrive(&bars[SB_VBASE + (seg & 3)]);
         }
       }
-      ok = tc::mbar_wait_tight(&bars[SB_QFULL], seg & 1);   // (the queries lay where the first tiles go)
 #pragma unroll 1
       for (int j = 0; j < g.n; ++j, ++J) {
         const int sv = J & 1, s8 = J % Cfg::NV8;
@@ -525,83 +648,74 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     auto rows_barrier = []() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
     bool ok = true;
     int turn = 0, J0 = 0;   // turns of this stream, tiles of the CTA
-    Walk& walk = *reinterpret_cast<Walk*>(base + Cfg::OFF_WALK);
-    if (tid == 128) {
-      walk.plan = plan;
-      walk.f = walk.w0 = w0;
-      walk.w1 = w1;
-    }
+    Walk& walk = (&start)[1];
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
-      if (tid == 128 && !segment_at(args, walk.plan, walk.w0, walk.w1, walk.f, walk.g)) walk.g.n = 0;
+      if (tid == 128) {
+        if (seg == 0) walk = start;
+        else if (!segment_at(args, plan, walk.w0, walk.w1, walk.f, walk.g)) walk.g.n = 0;
+      }
       rows_barrier();
       const Segment& g = walk.g;   // (nobody reads it any more when all have passed the barrier behind the results)
       if (g.n == 0) break;
       const bool tall = g.u.tall();
-      const int b0 = walk.plan.offsets[g.u.g], padded = tall ? 256 : 128;
-      uint8_t* raw = base + Cfg::OFF_V;   // the queries as they are (the converting warps wait for them to be used up)
-      {
-        constexpr int CPR = D / 8;        // 16-byte pieces of a row
-#pragma unroll 1
-        for (int i = tid - 128; i < padded * CPR; i += 512) {
-          const int r = i / CPR, c = i % CPR;
-          uint4* dst = reinterpret_cast<uint4*>(raw + r * (2 * D) + ((c ^ (r & 7)) << 4));
-          if (r >= g.u.n) {
-            *dst = make_uint4(0, 0, 0, 0);
-            continue;
-          }
+      const int b0 = plan.offsets[g.u.g];
+      // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split.
+      constexpr int TPR = D / 16, ITER = 128 * TPR / 512;   // threads per row; rows of a thread per row tile
+      const int piece = tid % TPR, row0 = (tid - 128) / TPR;
+      uint4 raw[4 * ITER];
+#pragma unroll
+      for (int i = 0; i < 2 * ITER; ++i) {
+        const int r = row0 + 512 / TPR * i;
+        raw[2 * i] = raw[2 * i + 1] = make_uint4(0, 0, 0, 0);
+        if (r < g.u.n) {
           const Row rw = row_of(args, b0, g.u.row0 + r);
-          const __nv_bfloat16* src = a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 8 * c;
+          const __nv_bfloat16* src = a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
           if (args.q_vec) {
-            copy16_async(dst, src);
+            raw[2 * i] = reinterpret_cast<const uint4*>(src)[0];
+            raw[2 * i + 1] = reinterpret_cast<const uint4*>(src)[1];
           } else {
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) reinterpret_cast<__nv_bfloat16*>(dst)[e] = src[e];
+            raw[2 * i] = load8(src);
+            raw[2 * i + 1] = load8(src + 8);
           }
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        rows_barrier();
       }
-      {
-        // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys; D / 16 threads per row
-        constexpr int TPR = D / 16;
 #pragma unroll 1
-        for (int i = tid - 128; i < padded * TPR; i += 512) {
-          const int r = i / TPR, piece = i % TPR;
-          uint32_t x[8];
-          {
-            const uint4 u = *reinterpret_cast<const uint4*>(raw + r * (2 * D) + (((2 * piece) ^ (r & 7)) << 4));
-            const uint4 v = *reinterpret_cast<const uint4*>(raw + r * (2 * D) + (((2 * piece + 1) ^ (r & 7)) << 4));
-            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-          }
-          uint32_t top2 = 0;
+      for (int i = 0; i < (tall ? 2 : 1) * ITER; ++i) {
+        // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
+        const int r = row0 + 512 / TPR * i;
+        uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
-          for (int q = 0; q < 8; ++q) top2 = __vmaxu2(top2, x[q] & 0x7fff7fffu);
-          uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+        for (int j = 0; j < 4 * ITER - 2; ++j) raw[j] = raw[j + 2];
+        uint32_t top2 = 0;
 #pragma unroll
-          for (int o = 1; o < TPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const bool nan = top >= 0x7f80u;
-          const int e = max((int)(top >> 7), 10);
-          const float mul = nan ? 0.f : exp2i(134 - e);
-          uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+        for (int q = 0; q < 8; ++q) top2 = __vmaxu2(top2, x[q] & 0x7fff7fffu);
+        uint32_t top = max(top2 & 0xffffu, top2 >> 16);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const uint32_t v = nan ? 0u : x[q];
-            uint32_t h, l;
-            split_e4m3x2(__uint_as_float(v << 16) * mul, __uint_as_float(v & 0xffff0000u) * mul, h, l);
-            hi[q >> 1] |= h << (16 * (q & 1));
-            lo[q >> 1] |= l << (16 * (q & 1));
-          }
-          uint8_t* at = base + Cfg::OFF_Q + (r >> 7) * 2 * Cfg::T8 + (r & 127) * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
-          *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          if (piece == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
+        for (int o = 1; o < TPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool nan = top >= 0x7f80u;
+        const int e = max((int)(top >> 7), 10);
+        const float mul = nan ? 0.f : exp2i(134 - e);
+        uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const uint32_t v = nan ? 0u : x[q];
+          uint32_t h, l;
+          split_e4m3x2(__uint_as_float(v << 16) * mul, __uint_as_float(v & 0xffff0000u) * mul, h, l);
+          hi[q >> 1] |= h << (16 * (q & 1));
+          lo[q >> 1] |= l << (16 * (q & 1));
         }
-        tc::fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bars[SB_QFULL]);
-        rows_barrier();
+        uint8_t* at = base + Cfg::OFF_Q + i / ITER * 2 * Cfg::T8 + (r & 127) * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
+        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        if (piece == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
+        if (i % ITER == ITER - 1) {
+          tc::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&bars[SB_QFULL + i / ITER]);
+        }
       }
+      rows_barrier();
       float cq = s_cq[(tall ? 128 * st : 0) + row];
       bool bad = !(cq == cq);   // NaN rows are marked, not computed with
       if (bad) cq = 0.f;
@@ -779,50 +893,38 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   }
 }
 
-// Merge: thread = row (b, t, head of the kv head's group), block (128 rows, CH channels, kv head).
+// Merge.  Block: 128 rows (b, t, head of the kv head's group), CH channels, one kv head; kLists threads per row, which take the row's partial results in turn.
+constexpr int kLists = 2;
 template <int D, int CH>
-__global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant__ SharedArgs s) {
-  extern __shared__ int s_plan[];
-  __shared__ int2 scratch[4];
+__global__ void __launch_bounds__(128 * kLists) shared_merge_kernel(const __grid_constant__ SharedArgs s) {
+  __shared__ float s_part[kLists - 1][CH + 2][128];
   const AttendArgs& a = s.a;
   const Params& p = a.p;
-  Plan plan;
-  const bool planned = make_plan<128>(s, s_plan, scratch, plan);
-  const int r = blockIdx.x * 128 + threadIdx.x, c0 = blockIdx.y * CH, hk = blockIdx.z;
-  int start, n = 0;
-  Row rw{0, 0, 0};
-  Unit u;
-  u.tiles = 0;
-  int row = 0, blocks = 0;
-  bool live = planned && r < p.batch * s.seq_rows;
-  if (live) {
-    rw = row_of(s, 0, r);
-    const int g = last_before(plan.offsets, a.groups.n, rw.b);
-    blocks = blocks_of_group(s, g);
-    live = shared_lengths(p, rw.b, blocks, start, n) && rw.t < n;
-    if (live && blocks > 0) {
-      row = r - plan.offsets[g] * s.seq_rows;
-      u = unit_of(s, plan, g, blocks, hk, row >> 8);
-      row &= 255;
-    }
-  }
+  const int lane = threadIdx.x & 127, list = threadIdx.x >> 7;
+  const int r = blockIdx.x * 128 + lane, c0 = blockIdx.y * CH, hk = blockIdx.z;
+  const Row rw = row_of(s, 0, r);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (!live) return;
+  SeqInfo x{};
+  if (rw.b < p.batch) x = s.seqs[rw.b];
+  const bool live = rw.t < x.n;
+  const int start = x.start, n = x.n, blocks = x.blocks;
   float m = -INFINITY, l = 0.f, o[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) o[i] = 0.f;
+  int turn = 0, seen = 0;   // this thread's next partial result; those of the lists before
   // Partial results z = 0 .. n - 1 at x + z * next (z = 0: at x0): channel i at [i * step], m, l; FOUR of them on their way at a time.
   auto add = [&](const float* x0, const float* x, int64_t next, int count, int64_t step, float below) {
     constexpr int FOUR = 4;
     const int64_t at_m = (D - c0) * step, at_l = at_m + step;
-    for (int z0 = 0; z0 < count; z0 += FOUR) {
+    for (; turn < count; turn += FOUR * kLists) {
       float mz[FOUR], lz[FOUR], v[FOUR][CH];
 #pragma unroll
       for (int k = 0; k < FOUR; ++k) {
-        const float* y = z0 + k == 0 ? x0 : x + (z0 + k) * next;
+        const int z = turn + k * kLists;
+        const float* y = z == 0 ? x0 : x + z * next;
         mz[k] = -INFINITY;
         lz[k] = 0.f;
-        if (z0 + k < count) {
+        if (z < count) {
           mz[k] = y[at_m] - below;
           lz[k] = y[at_l];
 #pragma unroll
@@ -848,8 +950,19 @@ __global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant
       }
     }
   };
+  auto add_after = [&](const float* x0, const float* x, int64_t next, int count, int64_t step, float below) {
+    turn = (list - seen) & (kLists - 1);
+    add(x0, x, next, count, step, below);
+    seen += count;
+  };
   // the shared blocks: the CTAs that had tiles of the unit
-  if (u.tiles > 0) {
+  if (live && blocks > 0) {
+    Plan plan;
+    plan.share = x.deal >> 1;
+    plan.whole = x.deal & 1;
+    int row = x.row0 + r - rw.b * s.seq_rows;
+    const Unit u = unit_of(p, plan, x.rows, blocks, x.pre, x.at, hk, row >> 8);
+    row &= 255;
     int first = u.begin / plan.share, last = (u.begin + u.tiles * u.w - 1) / plan.share, jb, je;
     u.of(first * plan.share, plan.share, jb, je);
     if (jb >= je) ++first;                     // (at either end: a tile that counts twice belongs to the share in which it begins)
@@ -857,26 +970,51 @@ __global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant
     if (jb >= je) --last;
     const float* x = s.part + (u.slot(first) + (u.tall() && row >= 128 ? 128 : 0)) * (D + 2) + (row & (u.tall() ? 127 : 255)) + (int64_t)c0 * u.pitch;
     const int64_t next = 256 * (D + 2);
-    add(x, x, next, last - first + 1, u.pitch, 0.f);
+    add_after(x, x, next, last - first + 1, u.pitch, 0.f);
     x += (int64_t)u.pitch * (D + 2);
-    if (!u.tall()) add(x, x, next, last - first + 1, u.pitch, 0.f);
+    if (!u.tall()) add_after(x, x, next, last - first + 1, u.pitch, 0.f);
   }
   // the sequence's own
-  const int64_t unit = (int64_t)rw.b * p.Hkv + hk;
-  const int col = rw.t * a.G + rw.h;
-  if (s.cols == 0) {
-    const int qt = col >> 7, row0 = qt * 128, last = min(n * a.G, row0 + 128) - 1;   // (as prompt_work has it)
-    const int tiles = pages_of(p, start + s.by_group.div(row0), start + s.by_group.div(last), INT32_MAX, 0, blocks).tiles, per = split_tiles(tiles, s.many.nsplit);
-    const float* x = s.own + ((int64_t)(s.many.qtiles - 1 - qt) * p.batch * p.Hkv + unit) * s.many.nsplit * (D + 2) * 128 + (col & 127) + c0 * 128;
-    add(x, x, (D + 2) * 128, (tiles + per - 1) / per, 128, kShift);
-  } else {
-    const int2 from = a.found[unit];
-    const float* whole = a.side + (unit * s.cols + col) * (D + 2) + c0;
-    const int z0 = max(0, min(from.x, s.workers - 1)), z1 = min(from.y, s.workers - 1);   // (what a call leaves whose waits ran out may be anything)
-    const float* x = s.own + ((int64_t)2 * z0 * s.cols + col) * (D + 2) + c0;
-    const int64_t slot = (int64_t)s.cols * (D + 2);
-    if (from.y < 0) add(whole, whole, 0, 1, 1, kDecodeShift);
-    else add(x + slot, x, 2 * slot, z1 - z0 + 1, 1, kDecodeShift);   // (the first worker's share begins with the unit)
+  if (live) {
+    const int64_t unit = (int64_t)rw.b * p.Hkv + hk;
+    const int col = rw.t * a.G + rw.h;
+    if (s.cols == 0) {
+      const int qt = col >> 7, row0 = qt * 128, last = min(n * a.G, row0 + 128) - 1;   // (as prompt_work has it)
+      const int tiles = pages_of(p, start + s.by_group.div(row0), start + s.by_group.div(last), INT32_MAX, 0, blocks).tiles, per = split_tiles(tiles, s.many.nsplit);
+      const float* x = s.own + ((int64_t)(s.many.qtiles - 1 - qt) * p.batch * p.Hkv + unit) * s.many.nsplit * (D + 2) * 128 + (col & 127) + c0 * 128;
+      add_after(x, x, (D + 2) * 128, (tiles + per - 1) / per, 128, kShift);
+    } else {
+      const int2 from = a.found[unit];
+      const float* whole = a.side + (unit * s.cols + col) * (D + 2) + c0;
+      const int z0 = max(0, min(from.x, s.workers - 1)), z1 = min(from.y, s.workers - 1);   // (what a call leaves whose waits ran out may be anything)
+      const float* x = s.own + ((int64_t)2 * z0 * s.cols + col) * (D + 2) + c0;
+      const int64_t slot = (int64_t)s.cols * (D + 2);
+      if (from.y < 0) add_after(whole, whole, 0, 1, 1, kDecodeShift);
+      else add_after(x + slot, x, 2 * slot, z1 - z0 + 1, 1, kDecodeShift);   // (the first worker's share begins with the unit)
+    }
+  }
+  if (list > 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) s_part[list - 1][i][lane] = o[i];
+    s_part[list - 1][CH][lane] = m;
+    s_part[list - 1][CH + 1][lane] = l;
+  }
+  __syncthreads();
+  if (list > 0 || !live) return;
+  float mn = m;
+#pragma unroll
+  for (int k = 0; k < kLists - 1; ++k) mn = fmaxf(mn, s_part[k][CH][lane]);
+  float f = m == -INFINITY ? 0.f : tc::ex2_approx(m - mn);
+  l *= f;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) o[i] *= f;
+#pragma unroll
+  for (int k = 0; k < kLists - 1; ++k) {
+    const float mz = s_part[k][CH][lane], lz = s_part[k][CH + 1][lane];
+    f = mz == -INFINITY ? 0.f : tc::ex2_approx(mz - mn);
+    l = lz == lz ? fmaf(lz, f, l) : lz;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) o[i] = fmaf(s_part[k][i][lane], f, o[i]);
   }
   __nv_bfloat16* out = a.out + rw.b * a.so[0] + (int64_t)(hk * a.G + rw.h) * a.so[1] + rw.t * a.so[2] + c0;
   const float inv = 1.f / l;
@@ -895,7 +1033,7 @@ __global__ void __launch_bounds__(128) shared_merge_kernel(const __grid_constant
 // ---- arguments ----
 
 struct Space {
-  int64_t part, own, side, found, all;   // bytes
+  int64_t part, own, side, found, seqs, all;   // bytes
 };
 int64_t align16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 // Sizes of what a call leaves; false: beyond what is numbered in 32 bits.
@@ -911,7 +1049,8 @@ bool space_of_call(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t n
   x.own = align16(few ? decode_workspace(units, tiles, (int)d, (int)cols) : prompt_side_workspace(units, cols, tiles, (int)d));
   x.side = few ? align16(units * (cols <= 8 ? 8 : 16) * (d + 2) * 4) : 0;
   x.found = few ? align16(units * 8) : 0;
-  x.all = x.part + x.own + x.side + x.found;
+  x.seqs = B * (int64_t)sizeof(SeqInfo);
+  x.all = x.part + x.own + x.side + x.found + x.seqs;
   return true;
 }
 
@@ -935,8 +1074,7 @@ kvm_status_t launch_merge(const SharedArgs& args, cudaStream_t s) {
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   lc.attrs = at; lc.numAttrs = 1; lc.stream = s;
-  lc.gridDim = dim3((unsigned)((args.a.p.batch * (int64_t)args.seq_rows + 127) / 128), D / CH, args.a.p.Hkv); lc.blockDim = dim3(128);
-  lc.dynamicSmemBytes = 12 * (args.a.groups.n + 1);
+  lc.gridDim = dim3((unsigned)((args.a.p.batch * (int64_t)args.seq_rows + 127) / 128), D / CH, args.a.p.Hkv); lc.blockDim = dim3(128 * kLists);
   if (cudaLaunchKernelEx(&lc, shared_merge_kernel<D, CH>, args) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   return KVM_OK;
 }
@@ -975,6 +1113,7 @@ KVM_API kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm
   args.own = a.part = (float*)(ws + x.part);
   a.side = (float*)(ws + x.part + x.own);
   a.found = (int2*)(ws + x.part + x.own + x.side);
+  args.seqs = (SeqInfo*)(ws + x.part + x.own + x.side + x.found);
   a.groups = Groups{groups, shared, n_groups};
   args.seq_rows = (int)(a.p.T * a.G);
   args.cols = args.seq_rows <= 8 ? 8 : args.seq_rows <= kDecodeCols ? 16 : 0;
