@@ -386,8 +386,9 @@ kvm_status_t kvm_head_layernorm(void* x, const float* weight, const float* bias,
  *     KVM_ROPE_PARTS        f_i = g w_i + (1 - g) w_i / factor,  g = clamp((n_i - low) / (high - low), 0, 1),  n_i = original_len * w_i / (2 pi):
  *                           pairs that turn more than `high` times within the length that the model was made for keep their frequency,
  *                           those that turn less than `low` times are interpolated (arXiv 2309.00071, section 3.2)
- * Statistics, rotation and sums in fp32 (the mean taken off before the squares), angles in fp64, one rounding at the end.  Values up to
- * 2^60 in magnitude: beyond, the sums of squares of a norm may leave fp32's range. */
+ * Statistics, rotation and sums in fp32 (the mean taken off before the squares), angles as fractions of a turn in steps of 2^-64, times the
+ * position, one rounding at the end.  Values up to 2^60 in magnitude: beyond, the sums of squares of a norm may leave fp32's range; var + eps (mean(x^2) + eps)
+ * at least 2^-126, or 0 counts in its place and the row is not finite. */
 typedef enum { KVM_NORM_NONE = 0, KVM_NORM_LAYER = 1, KVM_NORM_RMS = 2 } kvm_norm_kind_t;
 typedef enum { KVM_ROPE_HALF = 0, KVM_ROPE_INTERLEAVED = 1 } kvm_rope_layout_t;
 typedef enum { KVM_ROPE_PLAIN = 0, KVM_ROPE_LINEAR = 1, KVM_ROPE_PARTS = 2 } kvm_rope_scaling_t;
@@ -416,7 +417,7 @@ kvm_status_t kvm_rope_frequencies(const kvm_front_t* front, int32_t head_dim, do
  *             there may be read, but nothing comes of them
  *   status    device int32 word or NULL: KVM_ERR_INVALID_ARG where start < 0, count < 0 or count > n_tokens (no row of that
  *             sequence is written); never cleared by the library
- * head_dim 64 or 128, batch <= 65535, heads <= 16384, n_tokens <= 2^30, else UNSUPPORTED.
+ * head_dim 64 or 128, batch <= 65535, heads <= 16384, n_tokens <= 2^30, batch * n_tokens <= 2^31 - 256, else UNSUPPORTED.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
 kvm_status_t kvm_qk_norm_rope(const kvm_front_t* front, const void* q, const void* k, const int32_t* start, const int32_t* count, int32_t batch,
                               int32_t n_q_heads, int32_t n_kv_heads, int64_t n_tokens, int32_t head_dim, void* q_out, void* k_out,
@@ -466,7 +467,8 @@ kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* 
  * v into the cache.  The codes of k are those of the normalised and rotated row in fp32, rounded once (not by way of bf16); a row that leaves fp32's
  * range there counts as infinite.  q may be NULL: k and v only.  Rows of q_out behind a sequence's count, and of a sequence that is reported, are
  * left as they were; rows of q, k and v behind the count may be read, but nothing comes of them.  q_out may be q (same strides), and must not overlap
- * k or v.  What kvm_cache_append says of pages, scales, distinct pages and infinities holds here.
+ * k or v.  What kvm_cache_append says of pages, scales, distinct pages and infinities holds here; n_q_heads <= 16384, batch * n_tokens <= 2^31 - 256 with q,
+ * else UNSUPPORTED.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
 kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_call_t* call, const kvm_front_t* front, const void* q, int32_t n_q_heads,
                               const void* k, const void* v, void* q_out, const int64_t* q_strides, const int64_t* k_strides,
@@ -510,7 +512,9 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
  *   groups   device int32 [n_groups + 1]: ascends (groups of no sequences are allowed) from 0 to batch
  *   shared   device int32 [n_groups], 0 <= shared[g] <= max_pages, and shared[g] * page_tokens <= start[b] for the sequences of g
  * Groups that are none, or a number of blocks that is not allowed, are reported like lengths that are not, and their sequences get no rows.
- * Otherwise as kvm_cache_attend, the precision of a weight and of q included; workspace: kvm_cache_shared_workspace() bytes.
+ * Otherwise as kvm_cache_attend, the precision of q included; weights over shared blocks go into the products in fp16, as there beyond 16 pairs, those over a
+ * sequence's own blocks as they do there.  Codes of NaN under a finite scale, which append never writes,
+ * count as 480 among the values of shared blocks.  workspace: kvm_cache_shared_workspace() bytes.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA; nothing is launched on an error. */
 kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm_cache_call_t* call, const int32_t* groups, const int32_t* shared, int32_t n_groups,
                                      const void* q, int32_t n_q_heads, float scale, void* out, const int64_t* q_strides, const int64_t* out_strides,

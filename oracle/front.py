@@ -25,7 +25,7 @@ def front(x, pos, norm="layer", eps=1e-5, rope_dims=0, layout="half", magnitude=
 
     The bound counts roundings of fp32 (u = 2^-24 each): the mean 12 of the largest |x|, the difference to it 2; the variance twice the relative error
     of what is squared, and 14 for its sum; the root 4 (2 ulp), the product with it, the weight and the bias 3; sin and cos 3 each (2 ulp and the
-    argument's), 2^-50 of the angle for its fp64, the rotation 3."""
+    argument's), 2^-50 of the angle for the way it is represented, the rotation 3."""
     x, d = np.asarray(x, np.float64), np.asarray(x).shape[1]
     err = np.zeros_like(x)
     if norm != "none":

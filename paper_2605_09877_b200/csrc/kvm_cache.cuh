@@ -1,4 +1,4 @@
-// Shared by the kernels over the 8-bit cache (kvm_cache.cu, kvm_cache_decode.cu, kvm_cache_prompt.cu): what a launch is given, which keys a
+// Shared by the kernels over the 8-bit cache (kvm_cache.cu, kvm_cache_decode.cu, kvm_cache_prompt.cu, kvm_cache_shared.cu, kvm_front.cu): what a launch is given, which keys a
 // position sees, and the e4m3 conversions.
 #pragma once
 #include <cuda_bf16.h>

@@ -9,17 +9,24 @@
 // list, in which a tile of more than 128 rows counts twice; every CTA takes an equal, contiguous share of it, whatever the lengths and the sizes of
 // the groups are, and leaves one partial result per unit that it has tiles of.
 //     S = (q_hi + q_lo) K8^T   kind::f8f6f4: the codes as they lie in memory, q in two parts of e4m3
-//     O += P V16               kind::f16: P in bf16 from tensor memory, V16 = the codes of the values as bf16 numbers (exact)
+//     O += P V16               kind::f16: P in fp16 from tensor memory, V16 = the codes of the values as fp16 numbers (exact)
 // as in kvm_cache_prompt.cu, but with two streams of one S and one O each: of two row tiles on the same keys (a tile of values is widened once for
 // 256 rows), or of one row tile on the even and the odd key tiles.  A stream goes S, softmax, P V, S, ...; while one is in its softmax the other is in the
-// tensor core, and nothing is handed from stream to stream.  bf16 weights have fp32's range, so a row's reference is not its maximum but a number that
-// has hardly ever to be changed: S is read once, no maximum is taken, and the two threads of a row, 64 columns each, need not meet.  What leaves the range shows in the sums
-// of weights; then the products wait, the stream's warps agree on references in a turn of their own, and go on.
+// tensor core, and nothing is handed from stream to stream.  A row's reference is the maximum of its first tile, and hardly ever has to be changed: later, S is read once, no
+// maximum is taken, and the two threads of a row, 64 columns each, need not meet.  What leaves the range shows in the sums of weights; then the products wait, the
+// stream's warps agree on references in a turn of their own, and go on.
 // Scales of values go into the exponents of the weights, relative to the largest of the share's blocks, and out of the row sums again.
 //   warp 0       producer of keys (TMA, page numbers and scales ahead), warp 3 of values
 //   warp 1       issues the products (one thread)
 //   warps 4-19   queries (scaled, split); softmax, eight warps per stream, two threads per row, 64 columns each; results
 //   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
+//
+// What bounds it: per 128 rows and 128 keys the products take 1024 cycles of the tensor core (q is there twice, so that S costs as much as in bf16), the powers 1024
+// of the special-function unit, operands and tiles some 1000 of shared memory.  A stream goes through S, softmax and P V one after the other, 4600 cycles with the other
+// stream's in between, so that two streams take 2300 per item; a third one has no tensor memory (2 S and 2 O of 128 columns are all 512).  64 sequences of 32 heads
+// on a document of 32768 tokens: 56 us, of which 9 are start (the plan, the queries) and 3 the results; the tensor core is active for 32% of it.  Half of the powers
+// left to a polynomial were slower (+9%: instructions).
+// Weights in bf16 need no maximum at all (88 instead of 90 us), but add as much error again as the result's own rounding has.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -40,13 +47,14 @@ namespace {
 constexpr int kCtas = 148;
 constexpr int kThreads = 768;
 constexpr int kInfo = 8;
-// Weights of a row, 2^(y - m), y = logit + exponent of the value's scale relative to the largest, go into the products as bf16 numbers in units of 2^-kBias,
-// and the codes of the values as bf16 numbers of 2^-kCode of what they stand for (their bits, shifted: nothing is multiplied).  bf16 has fp32's range, so the
-// reference m need not be the row's maximum: it is 0 to begin with, and anything will do that lies between kHigh below the largest y and kLow above
-// it.  A weight is then at most 2^(kHigh + kBias), and with the largest one at least 2^(kBias - kLow) even products with the smallest normal code,
-// 2^(-6 - kCode), have all their bits in fp32 (2^-126 2^24).  Sums of weights (without the values' scales, which may be 2^-kFoldMost) are held in units of 2^kBias.
-constexpr int kBias = 64, kCode = 120, kHigh = 60, kLow = 40;
-static_assert(kHigh + kBias <= 124 && kBias - kLow - kCode - 6 >= -126 + 24, "range");
+// Weights of a row, 2^(y - m), y = logit + exponent of the value's scale relative to the largest (2^-kFoldMost at least), go into the products as fp16 numbers in units of
+// 2^-kBias, and the codes of the values as fp16 numbers of 2^-kCode of what they stand for (their bits, shifted: nothing is multiplied).  The reference m need not be the
+// row's maximum: anything will do between the largest y so far, rounded up, and where 16 weights sum up to more than kMost (fp16 ends at 65504, 2^9 of the reference).
+// It is the largest y of the first tile to begin with; the largest weight is then at least 2^6, and half a step of fp16's least number 2^-31 of it.  Row sums take
+// the weights before they are rounded, in fp32 and without the values' scales: at most 2^(9 + kFoldMost).
+constexpr int kBias = 7, kCode = 8;
+constexpr float kMost = 60000.f;
+constexpr int kLowValues = 24;   // where the values are small their sums are held in units smaller by that, so that all bits stay above 2^-126
 constexpr float kShift = 6.f;    // what the kernels for few and for many tokens count their weights in (of 2^-8 and 2^-6 of the reference)
 constexpr float kDecodeShift = 8.f;
 
@@ -287,19 +295,13 @@ struct SharedCfg {
   static_assert(SB_COUNT * 8 + 128 <= 512 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
 };
 
-// Four e4m3 codes (channels 0 .. 3) as bf16 numbers of 2^-kCode of what they stand for, channels 0 and 2, then 1 and 3: sign, four bits of exponent and three
+// Four e4m3 codes (channels 0 .. 3) as fp16 numbers of 2^-kCode of what they stand for, channels 0 and 2, then 1 and 3: sign, four bits of exponent and three
 // of mantissa where they belong (a subnormal code is a subnormal number).  The results' channels are put in order when they are read.
 __device__ __forceinline__ void widen4(uint32_t c, uint32_t& even, uint32_t& odd) {
-  even = ((c & 0x007f007fu) << 4) | ((c << 8) & 0x80008000u);
-  odd = ((c & 0x7f007f00u) >> 4) | (c & 0x80008000u);
+  even = ((c & 0x007f007fu) << 7) | ((c << 8) & 0x80008000u);
+  odd = ((c & 0x7f007f00u) >> 1) | (c & 0x80008000u);
 }
 __device__ __forceinline__ int channel_of(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
-// two floats -> two bf16 (a in the low half)
-__device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
 // Barrier of the two warps that share 32 rows of a stream.
 __device__ __forceinline__ void pair_barrier(int id) {
   __syncwarp();
@@ -480,7 +482,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       // P V issued by two threads they ran as P V, P V, S, S, and both streams were in their softmax at the same time.)  The whole warp walks through this and one
       // thread issues, so that addresses and descriptors are uniform.
       constexpr uint32_t ID_S = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
-      constexpr uint32_t ID_O = tc::idesc_f16(128, D, true) | (1u << 7) | (1u << 10);   // (format 1: bf16)
+      constexpr uint32_t ID_O = tc::idesc_f16(128, D, true);
       auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
       const uint64_t dQ = desc(tc::smem_u32(base + Cfg::OFF_Q)), dK = desc(tc::smem_u32(base + Cfg::OFF_K));
       const uint64_t dV = tc::smem_desc_sw128(tc::smem_u32(base + Cfg::OFF_V), 128 * 128, 1024);
@@ -742,11 +744,11 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         const KeyTile& ti = info[tile % kInfo];
         const int n = ti.n - 64 * half;         // the half's columns that are there: pages are whole, 16 columns are there or not
-        if (redo) {
-          // Some row of the stream has weights beyond the range.  A new reference for the row, the largest y (or logit - kHigh) of the halves whose weights
-          // are held back; the other half's are shifted to it where they lie.
+        if (first || redo) {
+          // The row's reference in its first tile.  Or some row of the stream has weights beyond the range: a new reference for the row, the largest y of the
+          // halves whose weights are held back; the other half's are shifted to it where they lie.
           float mx = -INFINITY;
-          if (held) {
+          if (!redo || held) {
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
               uint32_t x[16];
@@ -756,7 +758,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
               for (int i = 0; i < 16; ++i) m0 = fmaxf(m0, __uint_as_float(x[i]));
               const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f), fold = fmaxf(ti.ve[4 * half + c] - vbase, -(float)kFoldMost);
-              if (16 * c < n) mx = fmaxf(mx, m0 * fac + fmaxf(fold, -(float)kHigh));
+              if (16 * c < n) mx = fmaxf(mx, m0 * fac + fold);
             }
           } else if (n > 0) {
             mx = m;
@@ -778,12 +780,15 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             l *= corr;
           }
           m = mnew;
-          if (!held) {
+          if (redo && !held) {
             uint32_t r[32];
             tc::tmem_ld32(tS + 64 * half, r);
             tc::tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = to_bf16x2(__uint_as_float(r[i] << 16) * corr, __uint_as_float(r[i] & 0xffff0000u) * corr);
+            for (int i = 0; i < 32; ++i) {
+              const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+              r[i] = to_f16x2(w.x * corr, w.y * corr);
+            }
             tc::tmem_st32(tS + 64 * half, r);
             sum *= corr;
           }
@@ -792,7 +797,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           if (ti.flags) bad = true;
           uint32_t pr[32];   // weights of columns 64 half .. + 63, two to a word
           const float neg_m = (float)kBias - m;
-          float top = 0.f, low = 0.f;   // largest sum of 16 weights, without and with the values' scales
+          float top = 0.f;   // largest sum of 16 weights
           sum = 0.f;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -811,11 +816,10 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             for (int i = 0; i < 8; ++i) {
               float p0, p1;
               unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, a2), p0, p1);
-              const uint32_t w = to_bf16x2(tc::ex2_approx(p0), tc::ex2_approx(p1));
-              // (the row sum takes the weights as the products get them, so that their rounding does not shift a flat row)
-              const uint64_t p2 = pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-              if (i & 1) s1 = add2(s1, p2); else s0 = add2(s0, p2);
-              pr[8 * c + i] = w;
+              p0 = tc::ex2_approx(p0);
+              p1 = tc::ex2_approx(p1);
+              if (i & 1) s1 = add2(s1, pack2(p0, p1)); else s0 = add2(s0, pack2(p0, p1));
+              pr[8 * c + i] = to_f16x2(p0, p1);
             }
             if (vr < fold) {
 #pragma unroll
@@ -824,13 +828,10 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             float l0, l1;
             unpack2(add2(s0, s1), l0, l1);
             l0 += l1;
-            l1 = l0 * exp2i(-(int)fold - kBias);
-            sum += l1;
-            top = fmaxf(top, l1);
-            low = fmaxf(low, l0);
+            sum += l0 * exp2i(-(int)fold - kBias);
+            top = fmaxf(top, l0);
           }
-          // in range: no sum of 16 above 2^kHigh (infinite ones among them); in the first tile, where the reference is a guess, one above 2^-kLow
-          held = !redo && __any_sync(0xffffffffu, top > 1.15e18f || (first && n > 0 && low < 1.6e7f));   // (2^60; 2^(kBias - kLow))
+          held = !redo && __any_sync(0xffffffffu, top > kMost);
           if (!held) tc::tmem_st32(tS + 64 * half, pr);   // (columns that the warp has read)
           else if (lane == 0) s_flag[st] = turn;
         }
@@ -858,7 +859,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       if (!ok) break;
       const bool any = g.n > (tall ? 0 : st);   // (the odd stream may have had no tile)
       float* mine = args.part + (g.u.slot(blockIdx.x) + st * g.u.pitch) * (D + 2);
-      const float nan = __int_as_float(0x7fc00000), low_values = vbase > 0.f ? 0.f : (float)(kCode - kBias);   // (so that neither the largest nor the smallest leave fp32's range)
+      const float nan = __int_as_float(0x7fc00000), low_values = vbase > 0.f ? 0.f : (float)kLowValues;   // (so that neither the largest nor the smallest leave fp32's range)
       const float unit = bad ? nan : exp2i((int)vbase - kUnitExp + (int)low_values);
       const bool live = (tall ? 128 * st : 0) + row < g.u.n;
       if (any) {
@@ -894,6 +895,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 }
 
 // Merge.  Block: 128 rows (b, t, head of the kv head's group), CH channels, one kv head; kLists threads per row, which take the row's partial results in turn.
+// Bound by the latency of what it reads (19 MB, mostly out of L2).  Two lists, eight channels: 88 us for the whole call on 64 samples of a document; four lists 90 (but
+// 52 instead of 55 for 24 x 4 tokens of 64 channels), four channels 91, eight partial results on their way 92.
 constexpr int kLists = 2;
 template <int D, int CH>
 __global__ void __launch_bounds__(128 * kLists) shared_merge_kernel(const __grid_constant__ SharedArgs s) {
