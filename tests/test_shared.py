@@ -461,3 +461,60 @@ def test_values_far_below_the_largest_of_their_block(kvm, n, d):
     want = v[live].sum(0) / (live.sum() + 1)                       # (its own key: weight 1, value 0)
     # equal weights: 2^-8 for the output; sums of 2^9 terms in fp32, 2^-24 2^9 of the sum of magnitudes
     assert (abs(out - want) <= 2.0 ** -8 * abs(want) + 2.0 ** -15 * v[live].abs().mean(0)).all(), float(abs(out - want).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [2, 40, 70])
+@pytest.mark.parametrize("d", [64, 128])
+def test_references_that_move_by_a_little(kvm, n, d):
+    """Rows whose maximum grows by a few powers of two from tile to tile, each at its own rate, in one half of a tile or the other, over blocks of several scales."""
+    H, P, L = 3, 32, 128 * 9 + 32
+    m = Shared(kvm, [n], [0], [0] * n, H, d, P, room=L + 100)
+    k, v = rows((n, H, L, d), 1), rows((n, H, L, d), 2)
+    u = torch.ones(d) / math.sqrt(d)
+    t = torch.arange(L)
+    steps = [t // 128, (t + 58) // 128, 9 - t // 128]              # from the first column, from the 71st, downwards
+    for h in range(H):
+        k[:, h] = (k[:, h].float() * 0.05 + steps[h][:, None] * u).bfloat16()
+    v = (v.float() * torch.exp2(((t // 32) % 5 - 2).float())[:, None]).bfloat16()
+    m.append(k[:1].expand(n, -1, -1, -1).contiguous(), v[:1].expand(n, -1, -1, -1).contiguous(), [L] + [0] * (n - 1))
+    for b in range(1, n):
+        m.table[b, :L // P] = m.table[0, :L // P]
+        m.k[b], m.v[b], m.len[b] = copy.deepcopy(m.k[0]), copy.deepcopy(m.v[0]), L
+    m.lead, m.shared = [L // P], i32([L // P])
+    m.append(rows((n, H, 1, d), 7), rows((n, H, 1, d), 8), [1] * n)
+    G = 4
+    rate = torch.linspace(-3.0, 10.0, n * H * G).view(n, H * G, 1, 1)   # logits per tile: up to 2^14 from tile to tile
+    q = (rows((n, H * G, 1, d), 9).float() * 0.05 + rate * u).bfloat16()
+    out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+    m.cache.attend_shared(q.cuda(), m.hidden(), i32([x - 1 for x in m.len]), m.groups, m.shared, scale=1.0, out=out, status=status)
+    assert status.item() == 0
+    m.compare(q, out, [1] * n, 0, 0, 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d", [(24, 128), (48, 64)])
+def test_few_results_are_rounded_otherwise_than_the_definition(kvm, n, d):
+    """A weight of fp16 is off by 2^-11 / sqrt(3) of itself (standard deviation) at most, q in two parts and fp32 by less than 2^-16: a result is rounded to the
+    neighbour only where the definition's lies that near to the border between them."""
+    P, L = 64, 2048
+    c = kvm.Cache.empty(L // P + n, 1, d, P)
+    k, v = rows((1, 1, L, d), 1), rows((1, 1, L, d), 2)
+    head = torch.arange(L // P, dtype=torch.int32)[None]
+    c.append(k.cuda(), v.cuda(), head.cuda(), i32([0]))
+    table = torch.cat([head.repeat(n, 1), L // P + torch.arange(n, dtype=torch.int32)[:, None]], 1).cuda()
+    own = torch.zeros((n, 1, 1, d), dtype=torch.bfloat16, device="cuda")
+    q = rows((n, 4, 1, d), 3)
+    c.append(own, own, table, i32([L] * n))
+    out = c.attend_shared(q.cuda(), table, i32([L] * n), i32([0, n]), i32([L // P])).cpu()
+    value = lambda codes, s: (codes[:L // P].float().cpu().double() * s[:L // P].cpu().double()[:, :, None, None]).reshape(L, d)  # noqa: E731
+    kk, vv = value(c.k8, c.k_scale), value(c.v8, c.v_scale)
+    x = q[:, :, 0].double() @ kk.T * float(np.float32(d ** -0.5))
+    p = torch.exp(x)
+    p = p / (p.sum(-1, keepdim=True) + 1)                          # (its own key: logit 0, value 0)
+    want = p @ vv
+    off = torch.sqrt((p * p) @ (vv * vv)) * math.sqrt(2.0 ** -22 / 3 + 2.0 ** -32)
+    step = torch.exp2(torch.floor(torch.log2(want.abs())) - 7)
+    chance = torch.clamp(off / step, max=1.0)                      # (the mean of |x| is no more than its standard deviation)
+    others = (out[:, :, 0].double() != want.bfloat16().double()).sum().item()
+    assert others <= chance.sum().item() + 6 * math.sqrt(chance.sum().item()), (others, chance.sum().item())
