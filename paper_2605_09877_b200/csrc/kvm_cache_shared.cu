@@ -83,7 +83,7 @@ struct Plan {
 };
 // One unit, as a CTA sees it that begins at position f of the list and ends at most at `end`.
 struct Unit {
-  int g, hk, blocks, tiles;      // group, kv head; shared blocks, key tiles of the unit
+  int b0, hk, blocks, tiles;     // the group's first sequence, kv head; shared blocks, key tiles of the unit
   int row0, n;                   // the unit's rows among the group's
   int w, begin;                  // weight of a tile, position of the first one
   int at;                        // rows of partial results before the unit's first
@@ -227,7 +227,7 @@ __device__ __forceinline__ Unit unit_at(const SharedArgs& s, const Plan& plan, i
   const int long_one = plan.length(2 * tiles), per = full * long_one + (left ? plan.length(weight_of(left) * tiles) : 0);
   const int rest = f - plan.pre[g], hk = rest / per;
   Unit u = unit_of(s.a.p, plan, n, blocks, plan.pre[g], plan.rows[g], hk, min(full, (rest - hk * per) / long_one));
-  u.g = g;
+  u.b0 = plan.offsets[g];
   return u;
 }
 // The CTA's next unit with tiles behind position f of the list; its share is [w0, w1).
@@ -262,16 +262,9 @@ struct alignas(16) KeyTile {
 };
 
 enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 26, SB_PVDONE = 28, SB_QFULL = 30,
-       SB_VBASE = 32, SB_COUNT = 36 };   // SB_QFULL: per row tile
+       SB_VBASE = 32, SB_SEGFULL = 36, SB_SEGFREE = 40, SB_COUNT = 44 };   // SB_QFULL: per row tile
 
-struct Segment { Unit u; int jb, n; };
-struct Walk {           // a CTA's place in the list: its first one, and how far the softmax warps are (their registers need not hold it)
-  Plan plan;
-  int f, w0, w1;        // where the next segment may begin; the share
-  bool planned;
-  Segment g;            // (n = 0: none)
-};
-
+struct Segment { Unit u; int jb, n; };   // tiles [jb, jb + n) of the unit; n = 0: there are no more
 template <int D>
 struct SharedCfg {
   static constexpr int NK = 3 * (128 / D), NV8 = 2 * (128 / D), NV = 2;
@@ -284,14 +277,14 @@ struct SharedCfg {
   static constexpr int OFF_CQ = OFF_INFO + kInfo * (int)sizeof(KeyTile);   // float [2][128]
   static constexpr int OFF_X = OFF_CQ + 2 * 128 * 4;                       // float [stream][half][128]: maxima, sums
   static constexpr int OFF_BAR = OFF_X + 4 * 128 * 4;
-  static constexpr int OFF_WALK = OFF_BAR + 512;
-  static constexpr int OFF_PLAN = OFF_WALK + 256;        // int [3][n_groups + 1]
+  static constexpr int OFF_SEG = OFF_BAR + 512;          // Segment [4]
+  static constexpr int OFF_PLAN = OFF_SEG + 256;         // int [3][n_groups + 1]
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static int smem(int n_groups) { return std::max(OFF_PLAN + 12 * (n_groups + 1) + 1024, 120 * 1024); }
   static constexpr uint32_t COL_S = 0, COL_O = 256;      // of stream s: + 128 s
   static_assert(NK <= 6 && NV8 <= 4 && NK + 2 <= kInfo, "rings");
   static_assert(OFF_K % 1024 == 0 && OFF_V8 % 1024 == 0 && OFF_V % 1024 == 0 && OFF_INFO % 16 == 0 && OFF_CQ % 16 == 0 && OFF_BAR % 8 == 0 && OFF_PLAN % 8 == 0, "alignment");
-  static_assert(sizeof(Walk) <= 128 && sizeof(Walk) % 8 == 0 && OFF_WALK % 8 == 0, "shared memory");
+  static_assert(4 * sizeof(Segment) <= 256, "shared memory");
   static_assert(SB_COUNT * 8 + 128 <= 512 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
 };
 
@@ -313,15 +306,6 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
   return r != 0;
 }
-// Eight bf16 of any alignment.
-__device__ __forceinline__ uint4 load8(const __nv_bfloat16* src) {
-  const uint16_t* s = reinterpret_cast<const uint16_t*>(src);
-  uint32_t x[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = s[2 * i] | (uint32_t)s[2 * i + 1] << 16;
-  return make_uint4(x[0], x[1], x[2], x[3]);
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ SharedArgs args) {
@@ -344,7 +328,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   if (warp == 0) {
     for (int i = lane; i < SB_COUNT; i += 32) {
       auto in = [&](int first, int n) { return i >= first && i < first + n; };
-      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) ? 4 : in(SB_PREADY, 2) ? 8 : in(SB_QFULL, 2) ? 16 : 1);
+      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) ? 4 : in(SB_PREADY, 2) ? 8 : in(SB_QFULL, 2) ? 16 : in(SB_SEGFREE, 4) ? 8 : 1);
     }
     if (lane == 0) {
       tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
@@ -358,15 +342,17 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   tc::tc_fence_before();
-  Walk& start = *reinterpret_cast<Walk*>(base + Cfg::OFF_WALK);
+  // The CTA's segments, as warp 2 finds them: a ring of four, for the three other single warps, the four that widen values and the softmax.
+  Segment* segs = reinterpret_cast<Segment*>(base + Cfg::OFF_SEG);
+  Plan plan;
+  bool planned = false;
+  int f = 0, w0 = 0, w1 = 0;   // where the next segment may begin; the share
   if (warp == 2) {
-    Walk x;
-    x.planned = make_plan(args, reinterpret_cast<int*>(base + Cfg::OFF_PLAN), x.plan);
-    x.f = x.w0 = x.planned ? (int)min((int64_t)x.plan.total, (int64_t)blockIdx.x * x.plan.share) : 0;
-    x.w1 = x.planned ? min(x.plan.total, x.w0 + x.plan.share) : 0;
-    x.g.n = 0;
-    if (!segment_at(args, x.plan, x.w0, x.w1, x.f, x.g)) x.g.n = 0;
-    if (lane == 0) start = x;
+    planned = make_plan(args, reinterpret_cast<int*>(base + Cfg::OFF_PLAN), plan);
+    if (planned) {
+      f = w0 = (int)min((int64_t)plan.total, (int64_t)blockIdx.x * plan.share);
+      w1 = min(plan.total, w0 + plan.share);
+    }
   }
   __syncthreads();
   tc::tc_fence_after();
@@ -375,34 +361,49 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!*abort_flag) report(p.status, KVM_ERR_TIMEOUT);
     *abort_flag = 1;
   };
-  // The CTA's segments: (unit, key tiles).  Every warp walks them by itself, but for those of the softmax.
-  const Plan& plan = start.plan;
-  auto next_segment = [&](int& f, Segment& g) {
-    if (f >= 0) return segment_at(args, plan, start.w0, start.w1, f, g);
-    g = start.g;
-    f = start.f;
+  auto next_segment = [&](int seg, Segment& g, bool& ok) {   // (by a whole warp)
+    ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SEGFULL + (seg & 3)], (seg >> 2) & 1));
+    if (!ok) return false;
+    g = segs[seg & 3];
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(&bars[SB_SEGFREE + (seg & 3)]);
     return g.n > 0;
   };
   const int tshift = 7 - p.page_shift, ppt = 1 << tshift;
   Segment g;
-  int f = -1;
   if (warp < 4) {
     if (warp == 2) {
-      // ------------------------------ what the merge has to know ------------------------------
+      // ------------------------------ segments; what the merge has to know ------------------------------
+      bool ok = true;
 #pragma unroll 1
-      for (int b = blockIdx.x * 32 + lane; b < p.batch; b += args.grid * 32) {
-        SeqInfo x{0, 0, 0, 0, 0, 0, 0, plan.share * 2 + (plan.whole ? 1 : 0)};
-        if (start.planned) {
-          const int g = last_before(plan.offsets, a.groups.n, b);
-          x.blocks = blocks_of_group(args, g);
-          x.rows = rows_of_group(args, plan.offsets, g);
-          x.row0 = (b - plan.offsets[g]) * args.seq_rows;
-          x.pre = plan.pre[g];
-          x.at = plan.rows[g];
-          if (!shared_lengths(p, b, x.blocks, x.start, x.n)) x.n = 0;
+      for (int seg = 0; ok; ++seg) {
+        if (seg >= 4) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SEGFREE + (seg & 3)], ((seg >> 2) - 1) & 1));
+        if (!ok) break;
+        if (!segment_at(args, plan, w0, w1, f, g)) g.n = 0;
+        if (lane == 0) {
+          segs[seg & 3] = g;
+          tc::mbar_arrive(&bars[SB_SEGFULL + (seg & 3)]);
         }
-        args.seqs[b] = x;
+        if (seg == 0) {
+#pragma unroll 1
+          for (int b = blockIdx.x * 32 + lane; b < p.batch; b += args.grid * 32) {
+            SeqInfo x{0, 0, 0, 0, 0, 0, 0, plan.share * 2 + (plan.whole ? 1 : 0)};
+            if (planned) {
+              const int g = last_before(plan.offsets, a.groups.n, b);
+              x.blocks = blocks_of_group(args, g);
+              x.rows = rows_of_group(args, plan.offsets, g);
+              x.row0 = (b - plan.offsets[g]) * args.seq_rows;
+              x.pre = plan.pre[g];
+              x.at = plan.rows[g];
+              if (!shared_lengths(p, b, x.blocks, x.start, x.n)) x.n = 0;
+            }
+            args.seqs[b] = x;
+          }
+          __syncwarp();
+        }
+        if (g.n == 0) break;
       }
+      if (!ok && lane == 0) fail();
     } else if (warp == 0 || warp == 3) {
       // ------------------------------ producers of keys (warp 0) and values (warp 3) ------------------------------
       const bool keys = warp == 0;
@@ -415,8 +416,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       int s = 0, issued = 0;
       uint32_t par = 0;
 #pragma unroll 1
-      while (ok && next_segment(f, g)) {
-        const int32_t* table = p.pages + (int64_t)plan.offsets[g.u.g] * p.max_pages;
+      for (int seg = 0; ok && next_segment(seg, g, ok); ++seg) {
+        const int32_t* table = p.pages + (int64_t)g.u.b0 * p.max_pages;
         auto fetch = [&](int k) {
           Page x{-1, 0, 0};
           const int j = k * tpb + lt, block = (g.jb + j) * ppt + lp;
@@ -499,7 +500,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         return ok;
       };
 #pragma unroll 1
-      for (int seg = 0; ok && next_segment(f, g); ++seg) {
+      for (int seg = 0; ok && next_segment(seg, g, ok); ++seg) {
         const bool tall = g.u.tall();
         const int items = g.n << (tall ? 1 : 0);
         // S of the next item of stream ST
@@ -523,7 +524,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             if (++s == Cfg::NK) { s = 0; par ^= 1; }
           }
         };
-        // P V of item i, of stream ST, and S of item i + 2
+        // P V of item i, of stream ST; where there is an item i + 2, S may follow
         auto item = [&](int i, auto ST) {
           constexpr int st = decltype(ST)::value;
           int &turn = st ? turn1 : turn0, &back = st ? back1 : back0, &it = st ? it1 : it0;
@@ -550,21 +551,19 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           }
           __syncwarp();
           if (!tall || st == 1) ++J;
-          if (i + 2 < items && wait(SB_PVDONE + st, it & 1)) issue_s(ST);
+          if (i + 2 < items) wait(SB_PVDONE + st, it & 1);
           ++it;
         };
         constexpr std::integral_constant<int, 0> S0{};
         constexpr std::integral_constant<int, 1> S1{};
         if (!wait(SB_QFULL, seg & 1)) break;
-        issue_s(S0);
-        if (items > 1) {
-          if (tall) wait(SB_QFULL + 1, talls++ & 1);
-          if (ok) issue_s(S1);
-        }
 #pragma unroll 1
-        for (int i = 0; i < items && ok; i += 2) {
-          item(i, S0);
-          if (ok && i + 1 < items) item(i + 1, S1);
+        for (int i = 0; i < items + 2 && ok; i += 2) {
+          if (i > 0) item(i - 2, S0);
+          if (ok && i < items) issue_s(S0);
+          if (i == 0 && tall && ok) wait(SB_QFULL + 1, talls++ & 1);
+          if (ok && i > 0 && i - 1 < items) item(i - 1, S1);
+          if (ok && i + 1 < items) issue_s(S1);
         }
         if (!ok) break;
         if (leader) {   // the end, when all products have landed
@@ -584,9 +583,9 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     bool ok = true;
     int J = 0;
 #pragma unroll 1
-    for (int seg = 0; ok && next_segment(f, g); ++seg) {
+    for (int seg = 0; ok && next_segment(seg, g, ok); ++seg) {
       {   // largest exponent of the values' scales
-        const int32_t* table = p.pages + (int64_t)plan.offsets[g.u.g] * p.max_pages;
+        const int32_t* table = p.pages + (int64_t)g.u.b0 * p.max_pages;
         int v = -1000;
 #pragma unroll 1
         for (int i = g.jb * ppt + tid - 640; i < min((g.jb + g.n) * ppt, g.u.blocks); i += 128) {
@@ -650,36 +649,30 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     auto rows_barrier = []() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
     bool ok = true;
     int turn = 0, J0 = 0;   // turns of this stream, tiles of the CTA
-    Walk& walk = (&start)[1];
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
-      if (tid == 128) {
-        if (seg == 0) walk = start;
-        else if (!segment_at(args, plan, walk.w0, walk.w1, walk.f, walk.g)) walk.g.n = 0;
-      }
-      rows_barrier();
-      const Segment& g = walk.g;   // (nobody reads it any more when all have passed the barrier behind the results)
+      ok = tc::mbar_wait_tight(&bars[SB_SEGFULL + (seg & 3)], (seg >> 2) & 1);
+      const Segment& g = segs[seg & 3];   // (free again behind the results)
+      if (!ok || g.n == 0) break;
       if (g.n == 0) break;
       const bool tall = g.u.tall();
-      const int b0 = plan.offsets[g.u.g];
-      // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split.
+      
+      // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split (those of any alignment one after the other).
       constexpr int TPR = D / 16, ITER = 128 * TPR / 512;   // threads per row; rows of a thread per row tile
       const int piece = tid % TPR, row0 = (tid - 128) / TPR;
+      auto row_at = [&](int r) {
+        const Row rw = row_of(args, g.u.b0, g.u.row0 + r);
+        return a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
+      };
       uint4 raw[4 * ITER];
 #pragma unroll
       for (int i = 0; i < 2 * ITER; ++i) {
         const int r = row0 + 512 / TPR * i;
         raw[2 * i] = raw[2 * i + 1] = make_uint4(0, 0, 0, 0);
-        if (r < g.u.n) {
-          const Row rw = row_of(args, b0, g.u.row0 + r);
-          const __nv_bfloat16* src = a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
-          if (args.q_vec) {
-            raw[2 * i] = reinterpret_cast<const uint4*>(src)[0];
-            raw[2 * i + 1] = reinterpret_cast<const uint4*>(src)[1];
-          } else {
-            raw[2 * i] = load8(src);
-            raw[2 * i + 1] = load8(src + 8);
-          }
+        if (r < g.u.n && args.q_vec) {
+          const uint4* src = reinterpret_cast<const uint4*>(row_at(r));
+          raw[2 * i] = src[0];
+          raw[2 * i + 1] = src[1];
         }
       }
 #pragma unroll 1
@@ -689,6 +682,11 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
         for (int j = 0; j < 4 * ITER - 2; ++j) raw[j] = raw[j + 2];
+        if (r < g.u.n && !args.q_vec) {
+          const uint16_t* src = reinterpret_cast<const uint16_t*>(row_at(r));
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] = src[2 * q] | (uint32_t)src[2 * q + 1] << 16;
+        }
         uint32_t top2 = 0;
 #pragma unroll
         for (int q = 0; q < 8; ++q) top2 = __vmaxu2(top2, x[q] & 0x7fff7fffu);
@@ -769,27 +767,30 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           const float mnew = first ? mx : fmaxf(m, mx), corr = tc::ex2_approx(m - mnew);
           if (!first) {
 #pragma unroll 1
-            for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
-              uint32_t r[32];
-              tc::tmem_ld32(tO + c * 32, r);
+            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
+              uint32_t r[16];
+              tc::tmem_ld16(tO + c, r);
               tc::tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
-              tc::tmem_st32(tO + c * 32, r);
+              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
+              tc::tmem_st16(tO + c, r);
             }
             l *= corr;
           }
           m = mnew;
           if (redo && !held) {
-            uint32_t r[32];
-            tc::tmem_ld32(tS + 64 * half, r);
-            tc::tmem_wait_ld();
+#pragma unroll 1
+            for (int c = 0; c < 32; c += 16) {
+              uint32_t r[16];
+              tc::tmem_ld16(tS + 64 * half + c, r);
+              tc::tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
-              r[i] = to_f16x2(w.x * corr, w.y * corr);
+              for (int i = 0; i < 16; ++i) {
+                const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+                r[i] = to_f16x2(w.x * corr, w.y * corr);
+              }
+              tc::tmem_st16(tS + 64 * half + c, r);
             }
-            tc::tmem_st32(tS + 64 * half, r);
             sum *= corr;
           }
         }
@@ -882,8 +883,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::tc_fence_before();   // (O has been read: the next product may be issued behind the barriers to come)
       J0 += ntiles;
       rows_barrier();
+      if (tid == 128) tc::mbar_arrive(&bars[SB_SEGFREE + (seg & 3)]);
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
     if (!ok) fail();
   }
   tc::tc_fence_before();
