@@ -265,7 +265,7 @@ static void launch_read(const ReadArgs& a, cudaStream_t s) {
 }
 
 // Codes as rows of d bytes, a box of one page of one head; rows land swizzled as the tensor core reads them (128 or 64 bytes).
-bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page) {
+static bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page) {
   typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -284,6 +284,10 @@ bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, 
   return reinterpret_cast<EncodeFn>(f)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstr, box, estr,
                                        CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode_tmaps(CUtensorMap (&maps)[2], const Params& p, int d) {
+  const int64_t rows = p.n_pages * p.Hkv * p.page;
+  return encode_tmap_codes(&maps[0], p.k, d, rows, p.page) && encode_tmap_codes(&maps[1], p.v, d, rows, p.page);
 }
 
 template <int BYTES>

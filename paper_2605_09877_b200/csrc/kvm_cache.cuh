@@ -1,6 +1,7 @@
 // Shared by the kernels over the 8-bit cache (kvm_cache.cu, kvm_cache_decode.cu, kvm_cache_prompt.cu, kvm_cache_shared.cu, kvm_front.cu): what a launch is given, which keys a
 // position sees, and the e4m3 conversions.
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -183,18 +184,20 @@ struct AttendArgs {
   float* side;                   // few tokens: [unit][column][D + 2] of the units that one worker did
   int2* found;                   // few tokens: per unit its first and last worker (last -1: it is in `side`)
 };
+// maps of the codes of the keys and of the values (kvm_cache.cu)
+bool encode_tmaps(CUtensorMap (&maps)[2], const Params& p, int d);
 // tokens times heads of a group <= kDecodeCols; tiles: most key tiles of a sequence
 constexpr int kDecodeCols = 16;
 kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s);
 int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols);
 // ... SIDE: how many workers there are
-kvm_status_t launch_decode8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, int& workers);
+kvm_status_t launch_decode8_side(const AttendArgs& a, int64_t tiles, bool q_vec, const CUtensorMap (&maps)[2], cudaStream_t s, int& workers);
 // more than that; rows: tokens times heads of a group
 kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s);
 int64_t prompt_workspace(int64_t units, int64_t rows, int64_t tiles, int d);
 // ... SIDE: row tiles of a unit and key splits, [((row tiles - 1 - row tile) * units + unit) * splits + split][D + 2][128] in a.part
 struct PromptSide { int qtiles, nsplit; };
-kvm_status_t launch_prompt8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, PromptSide& side);
+kvm_status_t launch_prompt8_side(const AttendArgs& a, int64_t tiles, bool q_vec, const CUtensorMap (&maps)[2], cudaStream_t s, PromptSide& side);
 int64_t prompt_side_workspace(int64_t units, int64_t rows, int64_t tiles, int d);
 constexpr int kSplitTiles = 4;    // least key tiles of a split
 __host__ __device__ __forceinline__ int split_tiles(int tiles, int nsplit) {   // key tiles of a split, of a row tile that sees so many

@@ -37,7 +37,6 @@
 namespace kvm {
 namespace cache {
 
-bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page);   // kvm_cache.cu
 
 constexpr int kCtas = 148;
 constexpr float kPShift = 8.f;   // the largest weight of a tile is 2^8 (e4m3 ends at 448)
@@ -861,7 +860,7 @@ static kvm_status_t launch_decode_nc(const DecodeArgs8& args, const CUtensorMap&
 }
 
 template <bool SIDE>
-static kvm_status_t launch_decode8_any(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, int& workers) {
+static kvm_status_t launch_decode8_any(const AttendArgs& a, int64_t tiles, bool q_vec, const CUtensorMap (&maps)[2], cudaStream_t s, int& workers) {
   DecodeArgs8 args;
   args.a = a;
   args.grid = decode_grid((int64_t)a.p.batch * a.p.Hkv, tiles);
@@ -869,19 +868,19 @@ static kvm_status_t launch_decode8_any(const AttendArgs& a, int64_t tiles, bool 
   workers = args.grid * (cols <= 8 ? 4 : 3);
   args.cuts = reinterpret_cast<Cut*>(reinterpret_cast<uint8_t*>(a.part) + decode_partials(workers, a.d, cols));
   args.q_vec = q_vec ? 1 : 0;
-  CUtensorMap mapK, mapV;
-  const int64_t rows = a.p.n_pages * a.p.Hkv * a.p.page;
-  if (!encode_tmap_codes(&mapK, a.p.k, a.d, rows, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, rows, a.p.page)) return KVM_ERR_CUDA;
+  const CUtensorMap &mapK = maps[0], &mapV = maps[1];
   const bool few = cols <= 8;
   if (a.d == 128) return few ? launch_decode_nc<128, 8, SIDE>(args, mapK, mapV, s) : launch_decode_nc<128, 16, SIDE>(args, mapK, mapV, s);
   return few ? launch_decode_nc<64, 8, SIDE>(args, mapK, mapV, s) : launch_decode_nc<64, 16, SIDE>(args, mapK, mapV, s);
 }
 kvm_status_t launch_decode8(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s) {
+  CUtensorMap maps[2];
+  if (!encode_tmaps(maps, a.p, a.d)) return KVM_ERR_CUDA;
   int workers;
-  return launch_decode8_any<false>(a, tiles, q_vec, s, workers);
+  return launch_decode8_any<false>(a, tiles, q_vec, maps, s, workers);
 }
-kvm_status_t launch_decode8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, int& workers) {
-  return launch_decode8_any<true>(a, tiles, q_vec, s, workers);
+kvm_status_t launch_decode8_side(const AttendArgs& a, int64_t tiles, bool q_vec, const CUtensorMap (&maps)[2], cudaStream_t s, int& workers) {
+  return launch_decode8_any<true>(a, tiles, q_vec, maps, s, workers);
 }
 
 }  // namespace cache

@@ -42,7 +42,6 @@
 namespace kvm {
 namespace cache {
 
-bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page);   // kvm_cache.cu
 
 constexpr int kMaxSplits = 32;
 
@@ -927,7 +926,7 @@ static kvm_status_t launch_prompt_d(const PromptArgs& args, const CUtensorMap& m
 }
 
 template <bool SIDE>
-static kvm_status_t launch_prompt8_any(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s, PromptSide& side) {
+static kvm_status_t launch_prompt8_any(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, const CUtensorMap (&maps)[2], cudaStream_t s, PromptSide& side) {
   PromptArgs args;
   args.a = a;
   args.units = a.p.batch * a.p.Hkv;
@@ -942,9 +941,7 @@ static kvm_status_t launch_prompt8_any(const AttendArgs& a, int64_t tiles, bool 
   args.nsplit = std::min(args.nsplit, most);
   args.by_units = FastDiv(args.units); args.by_heads = FastDiv(a.p.Hkv); args.by_group = FastDiv(a.G);
   args.q_vec = q_vec ? 1 : 0; args.out_vec = out_vec ? 1 : 0;
-  CUtensorMap mapK, mapV;
-  const int64_t rows = a.p.n_pages * a.p.Hkv * a.p.page;
-  if (!encode_tmap_codes(&mapK, a.p.k, a.d, rows, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, rows, a.p.page)) return KVM_ERR_CUDA;
+  const CUtensorMap &mapK = maps[0], &mapV = maps[1];
   // Going on saves the start of a CTA, and costs registers in the loop over the tiles: it pays where rows see few of them (two prompts of 8192, 16 heads,
   // d = 128, without and with: window 128 193 -> 177 us, 512 239 -> 224, 2048 387 -> 384, 4096 524 -> 534, all 622 -> 641; d = 64 on 4 heads:
   // 144 -> 128, 192 -> 179, 326 -> 317, 453 -> 451, 548 -> 554).  Not where a merge waits for the grid.
@@ -956,11 +953,13 @@ static kvm_status_t launch_prompt8_any(const AttendArgs& a, int64_t tiles, bool 
   return more ? launch_prompt_d<64, true, false>(args, mapK, mapV, s) : launch_prompt_d<64, false, false>(args, mapK, mapV, s);
 }
 kvm_status_t launch_prompt8(const AttendArgs& a, int64_t tiles, bool q_vec, bool out_vec, cudaStream_t s) {
+  CUtensorMap maps[2];
+  if (!encode_tmaps(maps, a.p, a.d)) return KVM_ERR_CUDA;
   PromptSide side;
-  return launch_prompt8_any<false>(a, tiles, q_vec, out_vec, s, side);
+  return launch_prompt8_any<false>(a, tiles, q_vec, out_vec, maps, s, side);
 }
-kvm_status_t launch_prompt8_side(const AttendArgs& a, int64_t tiles, bool q_vec, cudaStream_t s, PromptSide& side) {
-  return launch_prompt8_any<true>(a, tiles, q_vec, true, s, side);
+kvm_status_t launch_prompt8_side(const AttendArgs& a, int64_t tiles, bool q_vec, const CUtensorMap (&maps)[2], cudaStream_t s, PromptSide& side) {
+  return launch_prompt8_any<true>(a, tiles, q_vec, true, maps, s, side);
 }
 
 }  // namespace cache

@@ -38,7 +38,6 @@
 namespace kvm {
 namespace cache {
 
-bool encode_tmap_codes(CUtensorMap* map, const void* base, int d, int64_t rows, int page);   // kvm_cache.cu
 kvm_status_t attend_args(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* q, int32_t n_q_heads, float scale, int32_t window, int32_t sinks, void* out,
                          const int64_t* q_strides, const int64_t* out_strides, int32_t* status, AttendArgs& a);
 
@@ -1125,12 +1124,11 @@ KVM_API kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm
   args.q_vec = rows_aligned(q, a.sq); args.out_vec = rows_aligned(out, a.so);
   const int64_t tiles = ((int64_t)a.p.max_pages * a.p.page + kTile - 1) / kTile, rows = (int64_t)a.p.batch * args.seq_rows;
   args.grid = (int)std::min<int64_t>(kCtas, (rows / 256 + n_groups) * 2 * a.p.Hkv * tiles);
-  CUtensorMap mapK, mapV;
-  const int64_t pool = a.p.n_pages * a.p.Hkv * a.p.page;
-  if (!encode_tmap_codes(&mapK, a.p.k, a.d, pool, a.p.page) || !encode_tmap_codes(&mapV, a.p.v, a.d, pool, a.p.page)) return KVM_ERR_CUDA;
+  CUtensorMap maps[2];
+  if (!encode_tmaps(maps, a.p, a.d)) return KVM_ERR_CUDA;
   cudaStream_t s = (cudaStream_t)cuda_stream;
-  kvm_status_t r = a.d == 128 ? launch_shared<128>(args, mapK, mapV, s) : launch_shared<64>(args, mapK, mapV, s);
-  if (r == KVM_OK) r = args.cols ? launch_decode8_side(a, tiles, args.q_vec, s, args.workers) : launch_prompt8_side(a, tiles, args.q_vec, s, args.many);
+  kvm_status_t r = a.d == 128 ? launch_shared<128>(args, maps[0], maps[1], s) : launch_shared<64>(args, maps[0], maps[1], s);
+  if (r == KVM_OK) r = args.cols ? launch_decode8_side(a, tiles, args.q_vec, maps, s, args.workers) : launch_prompt8_side(a, tiles, args.q_vec, maps, s, args.many);
   if (r == KVM_OK) r = a.d == 128 ? launch_merge<128>(args, s) : launch_merge<64>(args, s);
   return r;
 }

@@ -572,7 +572,8 @@ static FrontDev device_front(const kvm_front_t* f) {
   x.half = f->layout == KVM_ROPE_HALF;
   x.h = f->rope_dims / 2;
   x.mag = x.h ? (float)f->magnitude : 1.f;
-  for (int i = 0; i < x.h; ++i) x.turns[i] = (uint64_t)std::ldexp((long double)frequency(f, i) / 6.283185307179586476925L, 64);   // (f_i <= 1: below a sixth)
+  constexpr long double kTurns = 18446744073709551616.0L / 6.283185307179586476925286766559L;   // 2^64 / (2 pi)
+  for (int i = 0; i < x.h; ++i) x.turns[i] = (uint64_t)(frequency(f, i) * kTurns);   // (f_i <= 1: below 2^62)
   return x;
 }
 

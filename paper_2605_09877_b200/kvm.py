@@ -526,6 +526,7 @@ class KVMState:
 
 
 _THREE = C.c_int64 * 3
+_INT32, _BF16 = torch.int32, torch.bfloat16
 
 
 def _strides3(t):
@@ -609,12 +610,12 @@ class Front:
 
 def _front_rows(x, out, device, front, which, batch, tokens, head_dim):
     """Checks rows of q (which 0), k (1) or v (2) and their out, or None, for a front-end call; their number of heads."""
-    if x.dtype != torch.bfloat16 or x.get_device() != device or x.dim() != 4:
+    if x.dtype is not _BF16 or x.get_device() != device or x.dim() != 4:
         raise ValueError("rows are bfloat16 [batch, heads, tokens, head_dim] on one CUDA device")
     B, H, T, d = shape = x.shape
     if B != batch or T != tokens or d != head_dim:
         raise ValueError("q, k and v have the same batch, tokens and head_dim")
-    if out is not None and (out.shape != shape or out.dtype != torch.bfloat16 or out.get_device() != device):
+    if out is not None and (out.shape != shape or out.dtype is not _BF16 or out.get_device() != device):
         raise ValueError("an out has its input's shape, type and device")
     if which < 2 and front._shapes[which] is not None and (front._shapes[which] != (H, d) or front._device != device):
         raise ValueError("weights and biases [heads, head_dim] on the rows' device")
@@ -640,7 +641,7 @@ def qk_norm_rope(q, k, front: Front, start=None, count=None, q_out=None, k_out=N
     Hq = _front_rows(q, q_out, device, front, 0, B, T, d) if q is not None else 0
     Hk = _front_rows(k, k_out, device, front, 1, B, T, d) if k is not None else 0
     for t in (start, count, status):
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != device or (t is not status and t.numel() != B)):
+        if t is not None and (t.dtype is not _INT32 or not t.is_contiguous() or t.get_device() != device or (t is not status and t.numel() != B)):
             raise ValueError("start [batch], count [batch] and status are contiguous int32 tensors on the rows' device")
     if torch._C._cuda_getDevice() != device or _other_stream(stream):
         with torch.cuda.device(device), torch.cuda.stream(stream):   # (memory made here comes from the stream's own)
@@ -689,12 +690,12 @@ class Cache:
 
     def _call(self, pages, start, count, rows, status):
         B, _, T, _ = rows[0].shape
-        dev = self._device
+        dev = self._device.index
         for t in (pages, start, count, status):
-            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != dev):
+            if t is not None and (t.dtype is not _INT32 or t.get_device() != dev or not t.is_contiguous()):
                 raise ValueError("pages, start, count and status are contiguous int32 tensors on the cache's device")
         for t in rows:
-            if t.dtype != torch.bfloat16 or t.device != dev:
+            if t.dtype is not _BF16 or t.get_device() != dev:
                 raise ValueError("rows are bfloat16 on the cache's device")
         if pages.dim() != 2 or pages.shape[0] != B or start.numel() != B or (count is not None and count.numel() != B):
             raise ValueError("pages [batch, max_pages], start [batch], count [batch]")
