@@ -417,6 +417,7 @@ __device__ __forceinline__ void q_rows(const IngestArgs& a, int64_t block) {
 
 template <int D, int TH, int MODE>
 __global__ void __launch_bounds__(TH, 512 / TH) ingest_pages_kernel(const __grid_constant__ IngestArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (ingest_q_kernel, which has nothing to wait for before its end)
   int64_t i = blockIdx.x;
   if (i >= 2 * a.k_blocks) {   // (a call of few rows)
     q_rows<D, TH, MODE == kMixed ? kSingle : MODE>(a, i - 2 * a.k_blocks);
@@ -433,6 +434,7 @@ __global__ void __launch_bounds__(TH, 512 / TH) ingest_pages_kernel(const __grid
 template <int D, int MODE>
 __global__ void __launch_bounds__(256, 2) ingest_q_kernel(const __grid_constant__ IngestArgs a, const __grid_constant__ Tiles ts) {
   rows_tiles<D, MODE>(IngestTiles{a}, ts);
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // (what follows this grid counts on the end of the one before it)
 }
 
 // One token per sequence: a warp per row of k or v, D / 8 lanes per row of q.
@@ -686,7 +688,13 @@ static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   if (rc != KVM_OK) return rc;
   if (!few) {
     if (!room_for<ingest_q_kernel<D, MODE>, kTilesSmem<D, MODE>>()) return KVM_ERR_CUDA;
-    ingest_q_kernel<D, MODE><<<blocks, 256, kTilesSmem<D, MODE>, s>>>(a, ts);
+    cudaLaunchConfig_t lc = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (as the last blocks of the pages leave room)
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at; lc.numAttrs = 1; lc.stream = s;
+    lc.gridDim = dim3(blocks); lc.blockDim = dim3(256); lc.dynamicSmemBytes = kTilesSmem<D, MODE>;
+    if (cudaLaunchKernelEx(&lc, ingest_q_kernel<D, MODE>, a, ts) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   }
   return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
