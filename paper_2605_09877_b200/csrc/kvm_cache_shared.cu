@@ -17,16 +17,16 @@
 // stream's warps agree on references in a turn of their own, and go on.
 // Scales of values go into the exponents of the weights, relative to the largest of the share's blocks, and out of the row sums again.
 //   warp 0       producer of keys (TMA, page numbers and scales ahead), warp 3 of values
-//   warp 1       issues the products (one thread)
+//   warp 1       issues the products, warp 2 finds the CTA's segments and writes down what the merge has to know
 //   warps 4-19   queries (scaled, split); softmax, eight warps per stream, two threads per row, 64 columns each; results
 //   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 //
 // What bounds it: per 128 rows and 128 keys the products take 1024 cycles of the tensor core (q is there twice, so that S costs as much as in bf16), the powers 1024
 // of the special-function unit, operands and tiles some 1000 of shared memory.  A stream goes through S, softmax and P V one after the other, 4600 cycles with the other
 // stream's in between, so that two streams take 2300 per item; a third one has no tensor memory (2 S and 2 O of 128 columns are all 512).  64 sequences of 32 heads
-// on a document of 32768 tokens: 56 us, of which 9 are start (the plan, the queries) and 3 the results; the tensor core is active for 32% of it.  Half of the powers
-// left to a polynomial were slower (+9%: instructions).
-// Weights in bf16 need no maximum at all (88 instead of 90 us), but add as much error again as the result's own rounding has.
+// on a document of 32768 tokens: 54 us, of which 8 are start (the plan, the queries) and 3 the results; the tensor core is active for a third of it.  Half of the
+// powers left to a polynomial were slower (+9%: instructions).  Code is read from memory by every CTA that begins: 93 -> 75 KB of it saved 2.5 us.
+// Weights in bf16 need no maximum at all (2 us less), but add as much error again as the result's own rounding has.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
