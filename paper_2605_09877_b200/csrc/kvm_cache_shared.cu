@@ -45,7 +45,7 @@ namespace {
 
 constexpr int kCtas = 148;
 constexpr int kThreads = 768;
-constexpr int kInfo = 8;
+constexpr int kInfo = 16;
 // Weights of a row, 2^(y - m), y = logit + exponent of the value's scale relative to the largest (2^-kFoldMost at least), go into the products as fp16 numbers in units of
 // 2^-kBias, and the codes of the values as fp16 numbers of 2^-kCode of what they stand for (their bits, shifted: nothing is multiplied).  The reference m need not be the
 // row's maximum: anything will do between the largest y so far, rounded up, and where 16 weights sum up to more than kMost (fp16 ends at 65504, 2^9 of the reference).
@@ -78,23 +78,22 @@ struct Plan {
   const int *offsets, *pre, *rows;   // sequences, positions of the list, rows of the partial results before each group
   int total, share;                  // positions; of a CTA
   bool whole;                        // every unit begins with a share: its positions are rounded up to whole ones
-  __device__ __forceinline__ int length(int weight) const { return whole ? (weight + share - 1u) / (uint32_t)share * share : weight; }
+  __device__ __forceinline__ int length(int tiles) const { return whole ? (tiles + share - 1u) / (uint32_t)share * share : tiles; }   // of a unit
 };
 // One unit, as a CTA sees it that begins at position f of the list and ends at most at `end`.
 struct Unit {
   int b0, hk, blocks, tiles;     // the group's first sequence, kv head; shared blocks, key tiles of the unit
   int row0, n;                   // the unit's rows among the group's
-  int w, begin;                  // weight of a tile, position of the first one
+  int begin;                     // position of the first tile
   int at;                        // rows of partial results before the unit's first
   int pitch;                     // rows that a channel of a partial result takes
-  __device__ __forceinline__ bool tall() const { return w == 2; }
   // tiles [jb, je) of the CTA whose share begins at w0
   __device__ __forceinline__ void of(int w0, int share, int& jb, int& je) const {
-    jb = max(0, w0 - begin + w - 1) >> (w - 1);   // (w is 1 or 2)
-    je = min(tiles, max(0, w0 + share - begin + w - 1) >> (w - 1));
+    jb = max(0, w0 - begin);
+    je = min(tiles, max(0, w0 + share - begin));
   }
   // where the partial result of that CTA (its number: cta) is: one step further in the list is one unit or one CTA further
-  __device__ __forceinline__ int64_t slot(int cta) const { return at + (int64_t)cta * 256; }
+  __device__ __forceinline__ int64_t slot(int cta) const { return at + (int64_t)cta * 128; }
 };
 __device__ __forceinline__ int rows_of_group(const SharedArgs& s, const int* offsets, int g) { return (offsets[g + 1] - offsets[g]) * s.seq_rows; }
 // The shared blocks of a group (out of range: none, and the call is reported).
@@ -104,9 +103,9 @@ __device__ __forceinline__ int blocks_of_group(const SharedArgs& s, int g) {
 }
 __device__ __forceinline__ int tiles_of(const Params& p, int blocks) { return (blocks + (kTile >> p.page_shift) - 1) >> (7 - p.page_shift); }
 __device__ __forceinline__ int pad8(int x) { return (x + 7) & ~7; }
-// weight of a unit of n rows per tile, rows of its partial results
-__device__ __forceinline__ int weight_of(int n) { return n > 128 ? 2 : 1; }
-__device__ __forceinline__ int space_of(int n) { return n > 128 ? 256 : 2 * pad8(n); }
+// units of n rows of a group, per kv head; rows of their partial results
+__device__ __forceinline__ int units_of(int n) { return (n + 127) >> 7; }
+__device__ __forceinline__ int space_of(int n) { return (n & ~127) + pad8(n & 127); }
 
 // The plan, by one warp; mem: 3 (n_groups + 1) ints.  false: groups that are none.
 // Where there are no more units than CTAs, a share is the least of 32 lengths (or that of the longest unit) with which every CTA has tiles of one unit only: a unit
@@ -122,7 +121,7 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
   constexpr uint32_t kAll = 0xffffffffu;
   const int lane = threadIdx.x & 31;
   bool ok = true;
-  int tiles_sum = 0, units = 0, most = 0;   // weights of all units, their number, the largest
+  int tiles_sum = 0, units = 0, most = 0;   // tiles of all units, units, tiles of the longest
 #pragma unroll 1
   for (int g0 = 0; g0 <= gr.n; g0 += 32) {
     // sequences before a group; its key tiles (in `pre` for now)
@@ -132,12 +131,12 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
       offsets[g] = at;
       ok = ok && end >= at && (g > 0 || at == 0) && (g < gr.n || at == p.batch);
       if (blocks < 0 && blockIdx.x == 0) report(p.status, KVM_ERR_INVALID_ARG);
-      const int n = (end - at) * s.seq_rows, tiles = n > 0 && blocks > 0 ? tiles_of(p, blocks) : 0, full = n >> 8, left = n & 255;
+      const int n = (end - at) * s.seq_rows, tiles = n > 0 && blocks > 0 ? tiles_of(p, blocks) : 0;
       pre[g] = tiles;
       if (tiles > 0) {
-        tiles_sum += p.Hkv * tiles * (2 * full + (left ? weight_of(left) : 0));
-        units += p.Hkv * (full + (left ? 1 : 0));
-        most = max(most, tiles * weight_of(n));
+        tiles_sum += p.Hkv * tiles * units_of(n);
+        units += p.Hkv * units_of(n);
+        most = max(most, tiles);
       }
     }
   }
@@ -147,7 +146,7 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
   }
   __syncwarp();
   units = __reduce_add_sync(kAll, units);
-  plan.share = max(2, (__reduce_add_sync(kAll, tiles_sum) + s.grid - 1) / s.grid);   // (both streams have something to do, and no share within a unit is empty)
+  plan.share = max(2, (__reduce_add_sync(kAll, tiles_sum) + s.grid - 1) / s.grid);   // (both groups of softmax warps have something to do)
   if (units <= s.grid && units > 0) {
     // every lane: how many CTAs the length share * (1 + lane / 16) takes
     const uint32_t length = plan.share + plan.share * lane / 16;
@@ -157,10 +156,9 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
       const int g = g0 + lane, t = g < gr.n ? pre[g] : 0, n = t > 0 ? rows_of_group(s, offsets, g) : 0;
 #pragma unroll 1
       for (uint32_t there = __ballot_sync(kAll, t > 0); there; there &= there - 1) {
-        const int i = __ffs(there) - 1, rows_i = __shfl_sync(kAll, n, i), full = rows_i >> 8, left = rows_i & 255;
+        const int i = __ffs(there) - 1, rows_i = __shfl_sync(kAll, n, i);
         const uint32_t tiles = __shfl_sync(kAll, t, i);
-        if (full) ctas += full * ((2 * tiles + length - 1) / length);
-        if (left) ctas += (weight_of(left) * tiles + length - 1) / length;
+        ctas += units_of(rows_i) * ((tiles + length - 1) / length);
       }
     }
     const uint32_t fits = __ballot_sync(kAll, ctas * p.Hkv <= s.grid);
@@ -174,9 +172,9 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
     const int g = g0 + lane, tiles = g < gr.n ? pre[g] : 0;
     int x = 0, y = 0;
     if (tiles > 0) {
-      const int n = rows_of_group(s, offsets, g), full = n >> 8, left = n & 255;
-      x = p.Hkv * ((full ? full * plan.length(2 * tiles) : 0) + (left ? plan.length(weight_of(left) * tiles) : 0));
-      y = p.Hkv * (256 * full + (left ? space_of(left) : 0));
+      const int n = rows_of_group(s, offsets, g);
+      x = p.Hkv * units_of(n) * plan.length(tiles);
+      y = p.Hkv * space_of(n);
     }
     const int x0 = x, y0 = y;
 #pragma unroll
@@ -205,27 +203,22 @@ __device__ __forceinline__ int last_before(const int* pre, int n, int f) {
   }
   return lo;
 }
-// The unit of rows 256 rb .. of kv head hk of a group: n rows behind `blocks` shared blocks, at position pre of the list, rows `at` of the partial results.
+// The unit of rows 128 rb .. of kv head hk of a group: n rows behind `blocks` shared blocks, at position pre of the list, rows `at` of the partial results.
 __device__ __forceinline__ Unit unit_of(const Params& p, const Plan& plan, int n, int blocks, int pre, int at, int hk, int rb) {
   Unit u;
-  const int full = n >> 8, left = n & 255;
   u.hk = hk; u.blocks = blocks;
   u.tiles = tiles_of(p, blocks);
-  u.row0 = rb * 256;
-  u.n = min(256, n - u.row0);
-  u.w = weight_of(u.n);
-  u.pitch = u.w == 2 ? 128 : pad8(u.n);
-  const int long_one = plan.length(2 * u.tiles), per = full * long_one + (left ? plan.length(weight_of(left) * u.tiles) : 0);
-  u.begin = pre + hk * per + rb * long_one;
-  u.at = at + hk * (256 * full + (left ? space_of(left) : 0)) + 256 * rb;
+  u.row0 = rb * 128;
+  u.n = min(128, n - u.row0);
+  u.pitch = pad8(u.n);
+  u.begin = pre + (hk * units_of(n) + rb) * plan.length(u.tiles);
+  u.at = at + hk * space_of(n) + u.row0;
   return u;
 }
 __device__ __forceinline__ Unit unit_at(const SharedArgs& s, const Plan& plan, int f) {
-  const int g = last_before(plan.pre, s.a.groups.n, f), blocks = blocks_of_group(s, g), tiles = tiles_of(s.a.p, blocks);
-  const int n = rows_of_group(s, plan.offsets, g), full = n >> 8, left = n & 255;
-  const int long_one = plan.length(2 * tiles), per = full * long_one + (left ? plan.length(weight_of(left) * tiles) : 0);
-  const int rest = f - plan.pre[g], hk = rest / per;
-  Unit u = unit_of(s.a.p, plan, n, blocks, plan.pre[g], plan.rows[g], hk, min(full, (rest - hk * per) / long_one));
+  const int g = last_before(plan.pre, s.a.groups.n, f), blocks = blocks_of_group(s, g), n = rows_of_group(s, plan.offsets, g);
+  const uint32_t which = (uint32_t)(f - plan.pre[g]) / (uint32_t)plan.length(tiles_of(s.a.p, blocks)), hk = which / (uint32_t)units_of(n);
+  Unit u = unit_of(s.a.p, plan, n, blocks, plan.pre[g], plan.rows[g], hk, which - hk * units_of(n));
   u.b0 = plan.offsets[g];
   return u;
 }
@@ -237,7 +230,7 @@ __device__ __forceinline__ bool segment_at(const SharedArgs& s, const Plan& plan
     int je;
     g.u.of(w0, plan.share, g.jb, je);
     g.n = je - g.jb;
-    f = g.u.begin + plan.length(g.u.tiles * g.u.w);
+    f = g.u.begin + plan.length(g.u.tiles);
     if (g.n > 0) return true;
   }
   return false;
@@ -260,31 +253,33 @@ struct alignas(16) KeyTile {
   float ks[8], ve[8]; // per 16 keys: scale of the keys, exponent of the values' scale
 };
 
-enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 26, SB_PVDONE = 28, SB_QFULL = 30,
-       SB_VBASE = 32, SB_SEGFULL = 36, SB_SEGFREE = 40, SB_COUNT = 44 };   // SB_QFULL: per row tile
+// SB_SFULL: [group][number of its tile & 1]; SB_PREADY, SB_VERDICT: per group of softmax warps
+enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 23, SB_SFULL = 26, SB_PREADY = 30, SB_VERDICT = 32, SB_PVDONE = 34,
+       SB_END = 35, SB_REF = 36, SB_QFULL = 37, SB_VBASE = 38, SB_SEGFULL = 42, SB_SEGFREE = 46, SB_COUNT = 50 };
 
 struct Segment { Unit u; int jb, n; };   // tiles [jb, jb + n) of the unit; n = 0: there are no more
 template <int D>
 struct SharedCfg {
-  static constexpr int NK = 3 * (128 / D), NV8 = 2 * (128 / D), NV = 2;
+  static constexpr int NK = 3 * (128 / D), NV8 = 2 * (128 / D), NV = 3;
   static constexpr int T8 = 128 * D, T16 = 256 * D;
-  static constexpr int OFF_Q = 0;                        // [row tile] hi, lo
-  static constexpr int OFF_K = OFF_Q + 4 * T8;
+  static constexpr int OFF_Q = 0;                        // hi, lo
+  static constexpr int OFF_K = OFF_Q + 2 * T8;
   static constexpr int OFF_V8 = OFF_K + NK * T8;
   static constexpr int OFF_V = OFF_V8 + NV8 * T8;
   static constexpr int OFF_INFO = OFF_V + NV * T16;
-  static constexpr int OFF_CQ = OFF_INFO + kInfo * (int)sizeof(KeyTile);   // float [2][128]
-  static constexpr int OFF_X = OFF_CQ + 2 * 128 * 4;                       // float [stream][half][128]: maxima, sums
+  static constexpr int OFF_CQ = OFF_INFO + kInfo * (int)sizeof(KeyTile);   // float [128]
+  static constexpr int OFF_REF = OFF_CQ + 128 * 4;                         // float [128]: references of the rows
+  static constexpr int OFF_X = OFF_REF + 128 * 4;                          // float [group][half][128]: maxima, sums
   static constexpr int OFF_BAR = OFF_X + 4 * 128 * 4;
-  static constexpr int OFF_SEG = OFF_BAR + 512;          // Segment [4]
+  static constexpr int OFF_SEG = OFF_BAR + 640;          // Segment [4]
   static constexpr int OFF_PLAN = OFF_SEG + 256;         // int [3][n_groups + 1]
   // never less than half an SM, so that one CTA with its 512 columns of tensor memory is resident
   static int smem(int n_groups) { return std::max(OFF_PLAN + 12 * (n_groups + 1) + 1024, 120 * 1024); }
-  static constexpr uint32_t COL_S = 0, COL_O = 256;      // of stream s: + 128 s
-  static_assert(NK <= 6 && NV8 <= 4 && NK + 2 <= kInfo, "rings");
+  static constexpr uint32_t COL_S = 0, COL_O = 384;      // S of buffer b: + 128 b
+  static_assert(NK <= 6 && NV8 <= 4 && NK + 3 <= kInfo, "rings");   // (S is at most three tiles ahead of the softmax)
   static_assert(OFF_K % 1024 == 0 && OFF_V8 % 1024 == 0 && OFF_V % 1024 == 0 && OFF_INFO % 16 == 0 && OFF_CQ % 16 == 0 && OFF_BAR % 8 == 0 && OFF_PLAN % 8 == 0, "alignment");
   static_assert(4 * sizeof(Segment) <= 256, "shared memory");
-  static_assert(SB_COUNT * 8 + 128 <= 512 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
+  static_assert(SB_COUNT * 8 + 192 <= 640 && OFF_PLAN + 12 * (kMaxBatch + 1) + 1024 <= 227 * 1024, "shared memory");
 };
 
 // Four e4m3 codes (channels 0 .. 3) as fp16 numbers of 2^-kCode of what they stand for, channels 0 and 2, then 1 and 3: sign, four bits of exponent and three
@@ -320,19 +315,22 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_vmax = reinterpret_cast<int*>(tmem_slot + 2);                  // [segment % 4][4]
   volatile uint32_t* s_there = reinterpret_cast<uint32_t*>(s_vmax + 16); // [value tile of the ring]: pages that were loaded
-  volatile int* s_flag = reinterpret_cast<int*>(s_vmax + 20);           // [stream]: the turn whose reference will not do
-  volatile int* s_redo = s_flag + 2;                                    // [stream]: the turn that does it again
+  volatile int* s_flag = reinterpret_cast<int*>(s_vmax + 20);           // [group]: the tile whose weights leave the range
+  volatile int* s_redo = s_flag + 2;                                    // [group]: the tile that is done again
+  volatile int* s_used = s_redo + 2;                                    // [group][warp]: the version of the references that its weights are in
+  int* s_version = const_cast<int*>(s_used) + 16;                       // (written by the warp that issues the products alone)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (who waits for this kernel does so before reading what it wrote)
   if (warp == 0) {
     for (int i = lane; i < SB_COUNT; i += 32) {
       auto in = [&](int first, int n) { return i >= first && i < first + n; };
-      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) ? 4 : in(SB_PREADY, 2) ? 8 : in(SB_QFULL, 2) ? 16 : in(SB_SEGFREE, 4) ? 8 : 1);
+      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 3) || in(SB_VBASE, 4) || i == SB_REF ? 4 : in(SB_PREADY, 2) || in(SB_SEGFREE, 4) ? 8 : i == SB_QFULL ? 16 : 1);
     }
     if (lane == 0) {
       tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
       *abort_flag = 0;
       s_flag[0] = s_flag[1] = s_redo[0] = s_redo[1] = -1;
+      *s_version = 0;
     }
     tc::fence_barrier_init();
   }
@@ -477,10 +475,9 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       }
     } else if (warp == 1) {
       // ------------------------------ products ------------------------------
-      // Items of a segment: row tile i % 2 on key tile i / 2, or key tile i, in either case stream i % 2.  P V of item i is issued and then, when it is
-      // done (its weights lie where S goes), S of item i + 2: while the tensor core does these two, the other stream is in its softmax.  (With S and
-      // P V issued by two threads they ran as P V, P V, S, S, and both streams were in their softmax at the same time.)  The whole warp walks through this and one
-      // thread issues, so that addresses and descriptors are uniform.
+      // S of a segment's tiles goes into three buffers in turn, up to three tiles ahead; P V of tile i waits for its weights, and what is behind it in the
+      // buffer's place, S of tile i + 3, for P V.  Weights that leave the range, or are in units of references that have moved since, are done again before their P V, when
+      // all products before it have landed: verdict.  The whole warp walks through this and one thread issues, so that addresses and descriptors are uniform.
       constexpr uint32_t ID_S = tc::idesc_f16(128, 128, false);   // (format 0: e4m3 in kind::f8f6f4)
       constexpr uint32_t ID_O = tc::idesc_f16(128, D, true);
       auto desc = [](uint32_t addr) { return D == 128 ? tc::smem_desc_sw128(addr, 16, 1024) : tc::smem_desc_sw64(addr, 16, 512); };
@@ -488,90 +485,82 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       const uint64_t dV = tc::smem_desc_sw128(tc::smem_u32(base + Cfg::OFF_V), 128 * 128, 1024);
       const bool leader = elect_one();
       bool ok = true;
-      int turn0 = 0, turn1 = 0; // turns that the streams' softmax has been given (S, the same again, the end of a segment)
-      int back0 = 0, back1 = 0; // weights that have come back
-      int it0 = 0, it1 = 0;     // P V so far
-      int J = 0;                // value tiles so far
-      int talls = 0;            // segments of two row tiles so far
-      uint32_t s = 0, par = 0;  // ring of keys
+      uint32_t odd = 0, back = 0;            // per group: which of its two barriers S is next for; phase of the weights
+      int J = 0, version = 0;                // tiles so far
+      uint32_t s = 0, par = 0, v = 0, vpar = 0;   // rings of keys, of values
       auto wait = [&](int bar, uint32_t parity) {   // the same answer in every lane
         ok = ok && __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[bar], parity));
         return ok;
       };
 #pragma unroll 1
       for (int seg = 0; ok && next_segment(seg, g, ok); ++seg) {
-        const bool tall = g.u.tall();
-        const int items = g.n << (tall ? 1 : 0);
-        // S of the next item of stream ST
-        auto issue_s = [&](auto ST) {
-          constexpr int st = decltype(ST)::value;
-          if ((!tall || st == 0) && !wait(SB_KFULL + s, par)) return;
-          tc::tc_fence_after();
-          const uint64_t k = dK + s * (Cfg::T8 >> 4), q = dQ + (tall && st ? 2 * Cfg::T8 >> 4 : 0);
-          const uint32_t dS = tmem + Cfg::COL_S + 128 * st;
-          if (leader) {
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, q + 2 * ks, k + 2 * ks, ID_S, ks > 0);
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, q + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID_S, 1u);
-            tc::mma_commit(&bars[SB_SFULL + st]);
-            if (!tall || st == 1) tc::mma_commit(&bars[SB_KFREE + s]);
-          }
-          __syncwarp();
-          ++(st ? turn1 : turn0);
-          if (!tall || st == 1) {
-            if (++s == Cfg::NK) { s = 0; par ^= 1; }
-          }
-        };
-        // P V of item i, of stream ST; where there is an item i + 2, S may follow
-        auto item = [&](int i, auto ST) {
-          constexpr int st = decltype(ST)::value;
-          int &turn = st ? turn1 : turn0, &back = st ? back1 : back0, &it = st ? it1 : it0;
-          if ((!tall || st == 0) && !wait(SB_VFULL + (J & 1), (J >> 1) & 1)) return;
-          if (!wait(SB_PREADY + st, back++ & 1)) return;
-          if (__any_sync(0xffffffffu, s_flag[st] == turn - 1)) {   // (at most once)
+        if (!wait(SB_QFULL, seg & 1)) break;
+        int j = 0;                           // next S, and its buffer
+        uint32_t buf = 0, at = 0;            // (columns); at: buffer of the next P V
+#pragma unroll 1
+        for (int i = -3; i < g.n && ok; ++i) {
+          if (i >= 0) {
+            const uint32_t grp = i & 1;
+            auto weights = [&]() {
+              wait(SB_PREADY + grp, (back >> grp) & 1);
+              back ^= 1u << grp;
+            };
+            weights();
+            if (!wait(SB_VFULL + v, vpar)) break;
+            const bool moved = __any_sync(0xffffffffu, s_flag[grp] == J);
+            if (moved || __any_sync(0xffffffffu, lane < 8 && s_used[8 * grp + lane] != version)) {   // (at most once)
+              if (leader) {
+                s_redo[grp] = J;
+                tc::mbar_arrive(&bars[SB_VERDICT + grp]);
+              }
+              __syncwarp();
+              weights();
+              if (!ok) break;
+              if (moved) {
+                ++version;
+                if (leader) asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(s_version)), "r"(version) : "memory");
+              }
+            }
+            tc::tc_fence_after();
+            const uint64_t b = dV + v * (Cfg::T16 >> 4);
+            const uint32_t dO = tmem + Cfg::COL_O, aP = tmem + Cfg::COL_S + at, more = i > 0 ? 1u : 0u;
             if (leader) {
-              s_redo[st] = turn;
-              tc::mbar_arrive(&bars[SB_SFULL + st]);
+              tc::mbar_arrive(&bars[SB_VERDICT + grp]);
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
+                tc::mma_f16_ts(dO, aP + 64 * (kk >> 2) + 8 * (kk & 3), b + kk * (2048 >> 4), ID_O, kk > 0 ? 1u : more);
+              tc::mma_commit(&bars[SB_PVDONE]);
+              tc::mma_commit(&bars[SB_VFREE + v]);
             }
             __syncwarp();
-            ++turn;
-            if (!wait(SB_PREADY + st, back++ & 1)) return;
+            at = at == 256 ? 0 : at + 128;
+            if (++v == Cfg::NV) { v = 0; vpar ^= 1; }
+            if (!wait(SB_PVDONE, J & 1)) break;
+            ++J;
           }
-          tc::tc_fence_after();
-          const uint64_t v = dV + (J & 1) * (Cfg::T16 >> 4);
-          const uint32_t dO = tmem + Cfg::COL_O + 128 * st, aP = tmem + Cfg::COL_S + 128 * st, more = i >= 2 ? 1u : 0u;
-          if (leader) {
+          if (j < g.n) {
+            if (!wait(SB_KFULL + s, par)) break;
+            tc::tc_fence_after();
+            const uint64_t k = dK + s * (Cfg::T8 >> 4);
+            const uint32_t dS = tmem + Cfg::COL_S + buf, grp = j & 1;
+            if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk)   // 16 keys: 8 columns of P, 16 rows of 128 bytes of every 64-channel half of V
-              tc::mma_f16_ts(dO, aP + 64 * (kk >> 2) + 8 * (kk & 3), v + kk * (2048 >> 4), ID_O, kk > 0 ? 1u : more);
-            tc::mma_commit(&bars[SB_PVDONE + st]);
-            if (!tall || st == 1) tc::mma_commit(&bars[SB_VFREE + (J & 1)]);
+              for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + 2 * ks, k + 2 * ks, ID_S, ks > 0);
+#pragma unroll
+              for (int ks = 0; ks < D / 32; ++ks) tc::mma_f8_ss(dS, dQ + (Cfg::T8 >> 4) + 2 * ks, k + 2 * ks, ID_S, 1u);
+              tc::mma_commit(&bars[SB_SFULL + 2 * grp + ((odd >> grp) & 1)]);
+              tc::mma_commit(&bars[SB_KFREE + s]);
+            }
+            __syncwarp();
+            odd ^= 1u << grp;
+            buf = buf == 256 ? 0 : buf + 128;
+            if (++s == Cfg::NK) { s = 0; par ^= 1; }
+            ++j;
           }
-          __syncwarp();
-          if (!tall || st == 1) ++J;
-          if (i + 2 < items) wait(SB_PVDONE + st, it & 1);
-          ++it;
-        };
-        constexpr std::integral_constant<int, 0> S0{};
-        constexpr std::integral_constant<int, 1> S1{};
-        if (!wait(SB_QFULL, seg & 1)) break;
-#pragma unroll 1
-        for (int i = 0; i < items + 2 && ok; i += 2) {
-          if (i > 0) item(i - 2, S0);
-          if (ok && i < items) issue_s(S0);
-          if (i == 0 && tall && ok) wait(SB_QFULL + 1, talls++ & 1);
-          if (ok && i > 0 && i - 1 < items) item(i - 1, S1);
-          if (ok && i + 1 < items) issue_s(S1);
         }
         if (!ok) break;
-        if (leader) {   // the end, when all products have landed
-          tc::mma_commit(&bars[SB_SFULL]);
-          tc::mma_commit(&bars[SB_SFULL + 1]);
-        }
+        if (leader) tc::mbar_arrive(&bars[SB_END]);   // (all products have landed)
         __syncwarp();
-        ++turn0;
-        ++turn1;
       }
       if (!ok && leader) fail();
     }
@@ -602,9 +591,9 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       }
 #pragma unroll 1
       for (int j = 0; j < g.n; ++j, ++J) {
-        const int sv = J & 1, s8 = J % Cfg::NV8;
+        const int sv = J % Cfg::NV, s8 = J % Cfg::NV8;
         bool good = ok && tc::mbar_wait_tight(&bars[SB_V8FULL + s8], (J / Cfg::NV8) & 1);
-        if (good && J >= 2) good = tc::mbar_wait_tight(&bars[SB_VFREE + sv], ((J >> 1) - 1) & 1);
+        if (good && J >= Cfg::NV) good = tc::mbar_wait_tight(&bars[SB_VFREE + sv], (J / Cfg::NV - 1) & 1);
         ok = __all_sync(0xffffffffu, good);
         if (!ok) break;
         const uint32_t there = s_there[s8];
@@ -642,30 +631,28 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     if (!ok && lane == 0) fail();
   } else {
     // ------------------------------ q; softmax; results ------------------------------
-    const int st = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, pair = 2 + 4 * st + quarter;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), tS = lanes + Cfg::COL_S + 128 * st, tO = lanes + Cfg::COL_O + 128 * st;
-    float* s_x = reinterpret_cast<float*>(base + Cfg::OFF_X) + st * 256;   // [half][128]
+    const int grp = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, pair = 2 + 4 * grp + quarter;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), tO = lanes + Cfg::COL_O;
+    float* s_x = reinterpret_cast<float*>(base + Cfg::OFF_X);                // [group][half][128]
+    volatile float* s_ref = reinterpret_cast<float*>(base + Cfg::OFF_REF);
     auto rows_barrier = []() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
     bool ok = true;
-    int turn = 0, J0 = 0;   // turns of this stream, tiles of the CTA
+    int turn = 0, verdicts = 0, J0 = 0;   // tiles of this group, verdicts on them; tiles of the CTA
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
       ok = tc::mbar_wait_tight(&bars[SB_SEGFULL + (seg & 3)], (seg >> 2) & 1);
       const Segment& g = segs[seg & 3];   // (free again behind the results)
       if (!ok || g.n == 0) break;
-      if (g.n == 0) break;
-      const bool tall = g.u.tall();
-      
       // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split (those of any alignment one after the other).
-      constexpr int TPR = D / 16, ITER = 128 * TPR / 512;   // threads per row; rows of a thread per row tile
+      constexpr int TPR = D / 16, ITER = 128 * TPR / 512;   // threads per row; rows of a thread
       const int piece = tid % TPR, row0 = (tid - 128) / TPR;
       auto row_at = [&](int r) {
         const Row rw = row_of(args, g.u.b0, g.u.row0 + r);
         return a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
       };
-      uint4 raw[4 * ITER];
+      uint4 raw[2 * ITER];
 #pragma unroll
-      for (int i = 0; i < 2 * ITER; ++i) {
+      for (int i = 0; i < ITER; ++i) {
         const int r = row0 + 512 / TPR * i;
         raw[2 * i] = raw[2 * i + 1] = make_uint4(0, 0, 0, 0);
         if (r < g.u.n && args.q_vec) {
@@ -675,12 +662,12 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
       }
 #pragma unroll 1
-      for (int i = 0; i < (tall ? 2 : 1) * ITER; ++i) {
+      for (int i = 0; i < ITER; ++i) {
         // power-of-two scale of the row's largest channel to [2^7, 2^8), two parts of e4m3, swizzled like the keys
         const int r = row0 + 512 / TPR * i;
         uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
-        for (int j = 0; j < 4 * ITER - 2; ++j) raw[j] = raw[j + 2];
+        for (int j = 0; j < 2 * ITER - 2; ++j) raw[j] = raw[j + 2];
         if (r < g.u.n && !args.q_vec) {
           const uint16_t* src = reinterpret_cast<const uint16_t*>(row_at(r));
 #pragma unroll
@@ -704,147 +691,167 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           hi[q >> 1] |= h << (16 * (q & 1));
           lo[q >> 1] |= l << (16 * (q & 1));
         }
-        uint8_t* at = base + Cfg::OFF_Q + i / ITER * 2 * Cfg::T8 + (r & 127) * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
+        uint8_t* at = base + Cfg::OFF_Q + r * D + ((D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(at + Cfg::T8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         if (piece == 0) s_cq[r] = nan ? __int_as_float(0x7fc00000) : a.scale_log2 * exp2i(e - 134);
-        if (i % ITER == ITER - 1) {
-          tc::fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&bars[SB_QFULL + i / ITER]);
-        }
       }
+      tc::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&bars[SB_QFULL]);
       rows_barrier();
-      float cq = s_cq[(tall ? 128 * st : 0) + row];
+      float cq = s_cq[row];
       bool bad = !(cq == cq);   // NaN rows are marked, not computed with
       if (bad) cq = 0.f;
       ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_VBASE + (seg & 3)], (seg >> 2) & 1));
       const int* vm = s_vmax + 4 * (seg & 3);
       const int vb = max(max(vm[0], vm[1]), max(vm[2], vm[3]));
       const float vbase = vb == -1000 ? 0.f : (float)vb;
-      float m = 0.f, l = 0.f, sum = 0.f;   // reference (whole numbers); sums of the thread's weights: before the last tile, of the last tile
-      int left = tall ? g.n : (g.n + 1 - st) >> 1, tile = J0 + (tall ? 0 : st) - (tall ? 1 : 2);
-      const int ntiles = g.n;
-      bool first = true, held = false;     // the stream's first tile of the segment; weights that are not given away: the reference will not do
+      float m = 0.f, l = 0.f;   // reference of the thread's weights (a whole number), their sum
+      if (ok && grp == 1 && g.n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_REF], seg & 1));
+      uint32_t tS = lanes + Cfg::COL_S + 128 * grp + 64 * half;
 #pragma unroll 1
-      while (ok) {
-        ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SFULL + st], turn & 1));
+      for (int i = grp; i < g.n && ok; i += 2) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SFULL + 2 * grp + (turn & 1)], (turn >> 1) & 1));
+        ++turn;
         if (!ok) break;
         tc::tc_fence_after();
-        const bool redo = s_redo[st] == turn;   // (uniform)
-        if (!redo) {
-          l += sum;
-          if (left == 0) break;                 // the end: all products have landed
-          first = tile < J0;
-          tile += tall ? 1 : 2;
-          --left;
-        }
-        const KeyTile& ti = info[tile % kInfo];
+        const KeyTile& ti = info[(J0 + i) % kInfo];
         const int n = ti.n - 64 * half;         // the half's columns that are there: pages are whole, 16 columns are there or not
-        if (first || redo) {
-          // The row's reference in its first tile.  Or some row of the stream has weights beyond the range: a new reference for the row, the largest y of the
-          // halves whose weights are held back; the other half's are shifted to it where they lie.
-          float mx = -INFINITY;
-          if (!redo || held) {
+        if (ti.flags) bad = true;
+        int version;
+        asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(version) : "r"(tc::smem_u32(s_version)) : "memory");
+        float sum = 0.f;
+        bool held = false, redo = false;        // weights that are not given away: some leave the range
+        if (i > 0) {
+          const float now = s_ref[row];
+          if (i > 1 && m != now) l *= tc::ex2_approx(m - now);   // (nothing to shift in the group's first tile)
+          m = now;
+        }
 #pragma unroll 1
+        for (;;) {
+          if (i == 0 || redo) {
+            // The row's reference in the first tile: its largest y.  Or some row has weights beyond the range, or references have moved since these weights were computed: the
+            // largest y of the halves whose weights are held back, or what it is by now; weights that are not held back are shifted to it where they lie.
+            const float now = redo ? s_ref[row] : -INFINITY;
+            float mx = -INFINITY;
+            if (!redo || held) {
+#pragma unroll 1
+              for (int c = 0; c < 4; ++c) {
+                uint32_t x[16];
+                tc::tmem_ld16(tS + 16 * c, x);
+                tc::tmem_wait_ld();
+                float m0 = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) m0 = fmaxf(m0, __uint_as_float(x[k]));
+                const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f), fold = fmaxf(ti.ve[4 * half + c] - vbase, -(float)kFoldMost);
+                if (16 * c < n) mx = fmaxf(mx, m0 * fac + fold);
+              }
+            }
+            float* mine = s_x + 256 * grp + row;
+            mine[128 * half] = mx;
+            pair_barrier(pair);
+            mx = ceilf(fmaxf(mx, mine[128 * (1 - half)]));
+            const float next = redo ? fmaxf(now, mx) : mx;
+            if (half == 0) s_ref[row] = next;
+            if (redo) {
+              if (i > 0 && __any_sync(0xffffffffu, next != now)) {
+                const float corr = tc::ex2_approx(now - next);
+#pragma unroll 1
+                for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
+                  uint32_t r[16];
+                  tc::tmem_ld16(tO + c, r);
+                  tc::tmem_wait_ld();
+#pragma unroll
+                  for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * corr);
+                  tc::tmem_st16(tO + c, r);
+                }
+              }
+              const float corr = tc::ex2_approx(m - next);
+              if (i > 1) l *= corr;
+              if (!held) {
+#pragma unroll 1
+                for (int c = 0; c < 32; c += 16) {
+                  uint32_t r[16];
+                  tc::tmem_ld16(tS + c, r);
+                  tc::tmem_wait_ld();
+#pragma unroll
+                  for (int k = 0; k < 16; ++k) {
+                    const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&r[k]));
+                    r[k] = to_f16x2(w.x * corr, w.y * corr);
+                  }
+                  tc::tmem_st16(tS + c, r);
+                }
+                sum *= corr;
+              }
+            } else if (half == 0) {
+              __syncwarp();
+              if (lane == 0) tc::mbar_arrive(&bars[SB_REF]);
+            }
+            m = next;
+          }
+          if (!redo || held) {
+            uint32_t pr[32];   // weights of columns 64 half .. + 63, two to a word
+            const float neg_m = (float)kBias - m;
+            float top = 0.f;   // largest sum of 16 weights
+            sum = 0.f;
+#pragma unroll
             for (int c = 0; c < 4; ++c) {
               uint32_t x[16];
-              tc::tmem_ld16(tS + 64 * half + 16 * c, x);
+              tc::tmem_ld16(tS + 16 * c, x);
+              const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f);   // (never 0: what is not there is -inf)
+              const float vr = ti.ve[4 * half + c] - vbase, fold = fmaxf(vr, -(float)kFoldMost);
+              const uint64_t f2 = pack2(fac, fac), a2 = pack2(neg_m + fold, neg_m + fold);
               tc::tmem_wait_ld();
-              float m0 = -INFINITY;
+              if (n <= 16 * c) {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) m0 = fmaxf(m0, __uint_as_float(x[i]));
-              const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f), fold = fmaxf(ti.ve[4 * half + c] - vbase, -(float)kFoldMost);
-              if (16 * c < n) mx = fmaxf(mx, m0 * fac + fold);
-            }
-          } else if (n > 0) {
-            mx = m;
-          }
-          s_x[128 * half + row] = mx;
-          pair_barrier(pair);
-          mx = ceilf(fmaxf(mx, s_x[128 * (1 - half) + row]));
-          const float mnew = first ? mx : fmaxf(m, mx), corr = tc::ex2_approx(m - mnew);
-          if (!first) {
-#pragma unroll 1
-            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
-              uint32_t r[16];
-              tc::tmem_ld16(tO + c, r);
-              tc::tmem_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr);
-              tc::tmem_st16(tO + c, r);
-            }
-            l *= corr;
-          }
-          m = mnew;
-          if (redo && !held) {
-#pragma unroll 1
-            for (int c = 0; c < 32; c += 16) {
-              uint32_t r[16];
-              tc::tmem_ld16(tS + 64 * half + c, r);
-              tc::tmem_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
-                r[i] = to_f16x2(w.x * corr, w.y * corr);
+                for (int k = 0; k < 16; ++k) x[k] = 0xff800000u;
               }
-              tc::tmem_st16(tS + 64 * half + c, r);
+              uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                float p0, p1;
+                unpack2(fma2(pack2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), f2, a2), p0, p1);
+                p0 = tc::ex2_approx(p0);
+                p1 = tc::ex2_approx(p1);
+                if (k & 1) s1 = add2(s1, pack2(p0, p1)); else s0 = add2(s0, pack2(p0, p1));
+                pr[8 * c + k] = to_f16x2(p0, p1);
+              }
+              if (vr < fold) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) pr[8 * c + k] = 0;
+              }
+              float l0, l1;
+              unpack2(add2(s0, s1), l0, l1);
+              l0 += l1;
+              sum += l0 * exp2i(-(int)fold - kBias);
+              top = fmaxf(top, l0);
             }
-            sum *= corr;
+            held = !redo && __any_sync(0xffffffffu, top > kMost);
+            if (!held) tc::tmem_st32(tS, pr);   // (columns that the warp has read)
+            else if (lane == 0) s_flag[grp] = J0 + i;
           }
-        }
-        if (!redo || held) {
-          if (ti.flags) bad = true;
-          uint32_t pr[32];   // weights of columns 64 half .. + 63, two to a word
-          const float neg_m = (float)kBias - m;
-          float top = 0.f;   // largest sum of 16 weights
-          sum = 0.f;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t x[16];
-            tc::tmem_ld16(tS + 64 * half + 16 * c, x);
-            const float fac = fmaxf(cq * ti.ks[4 * half + c], 1.17549435e-38f);   // (never 0: what is not there is -inf)
-            const float vr = ti.ve[4 * half + c] - vbase, fold = fmaxf(vr, -(float)kFoldMost);
-            const uint64_t f2 = pack2(fac, fac), a2 = pack2(neg_m + fold, neg_m + fold);
-            tc::tmem_wait_ld();
-            if (n <= 16 * c) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] = 0xff800000u;
-            }
-            uint64_t s0 = 0, s1 = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float p0, p1;
-              unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, a2), p0, p1);
-              p0 = tc::ex2_approx(p0);
-              p1 = tc::ex2_approx(p1);
-              if (i & 1) s1 = add2(s1, pack2(p0, p1)); else s0 = add2(s0, pack2(p0, p1));
-              pr[8 * c + i] = to_f16x2(p0, p1);
-            }
-            if (vr < fold) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) pr[8 * c + i] = 0;
-            }
-            float l0, l1;
-            unpack2(add2(s0, s1), l0, l1);
-            l0 += l1;
-            sum += l0 * exp2i(-(int)fold - kBias);
-            top = fmaxf(top, l0);
+          tc::tmem_wait_st();
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (!redo) s_used[8 * grp + ((warp - 4) & 7)] = version;
+            tc::mbar_arrive(&bars[SB_PREADY + grp]);
           }
-          held = !redo && __any_sync(0xffffffffu, top > kMost);
-          if (!held) tc::tmem_st32(tS + 64 * half, pr);   // (columns that the warp has read)
-          else if (lane == 0) s_flag[st] = turn;
+          ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_VERDICT + grp], verdicts & 1));
+          ++verdicts;
+          if (!ok || redo || s_redo[grp] != J0 + i) break;
+          redo = true;
+          tc::tc_fence_after();
         }
-        tc::tmem_wait_st();
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bars[SB_PREADY + st]);
-        ++turn;
+        l += sum;
+        tS = tS >= lanes + Cfg::COL_S + 128 + 64 * half ? tS - 128 : tS + 256;   // (two buffers further of three)
       }
-      ++turn;
+      ok = ok && tc::mbar_wait_tight(&bars[SB_END], seg & 1);
       tc::tc_fence_after();
-      // the two halves' sums; whether all are well, and so whether there is a next time: the same for all
-      s_x[128 * half + row] = l;
+      // the four threads' sums; whether all are well, and so whether there is a next time: the same for all
+      const float nan = __int_as_float(0x7fc00000), ref = s_ref[row];
+      s_x[256 * grp + 128 * half + row] = bad ? nan : g.n > grp ? l * tc::ex2_approx(m - ref) : 0.f;
       {
         uint32_t r;
         __syncwarp();
@@ -857,30 +864,28 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         ok = r != 0;
       }
       if (!ok) break;
-      const bool any = g.n > (tall ? 0 : st);   // (the odd stream may have had no tile)
-      float* mine = args.part + (g.u.slot(blockIdx.x) + st * g.u.pitch) * (D + 2);
-      const float nan = __int_as_float(0x7fc00000), low_values = vbase > 0.f ? 0.f : (float)kLowValues;   // (so that neither the largest nor the smallest leave fp32's range)
-      const float unit = bad ? nan : exp2i((int)vbase - kUnitExp + (int)low_values);
-      const bool live = (tall ? 128 * st : 0) + row < g.u.n;
-      if (any) {
+      float* mine = args.part + g.u.slot(blockIdx.x) * (D + 2) + row;
+      const float total = (s_x[row] + s_x[128 + row]) + (s_x[256 + row] + s_x[384 + row]);
+      const float low_values = vbase > 0.f ? 0.f : (float)kLowValues;   // (so that neither the largest nor the smallest leave fp32's range)
+      const float unit = total == total ? exp2i((int)vbase - kUnitExp + (int)low_values) : nan;
+      const bool live = row < g.u.n;
 #pragma unroll 1
-        for (int c = half * (D / 64); c < (half + 1) * (D / 64); ++c) {
-          uint32_t r[32];
-          tc::tmem_ld32(tO + c * 32, r);
-          tc::tmem_wait_ld();
-          if (live) {
+      for (int c = (2 * grp + half) * (D / 4); c < (2 * grp + half + 1) * (D / 4); c += 16) {
+        uint32_t r[16];
+        tc::tmem_ld16(tO + c, r);
+        tc::tmem_wait_ld();
+        if (live) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) mine[(c * 32 + channel_of(i)) * g.u.pitch + row] = __uint_as_float(r[i]) * unit;
-          }
+          for (int k = 0; k < 16; ++k) mine[(c + channel_of(k)) * g.u.pitch] = __uint_as_float(r[k]) * unit;
         }
       }
-      if (live && half == 0) {
-        const float ref = (float)(kCode - kBias) - low_values;
-        mine[D * g.u.pitch + row] = any ? m + ref : -INFINITY;
-        mine[(D + 1) * g.u.pitch + row] = !any ? 0.f : bad ? nan : (s_x[row] + s_x[128 + row]) * exp2i(-(int)ref);
+      if (live && grp == 0 && half == 0) {
+        const float shift = (float)(kCode - kBias) - low_values;
+        mine[D * g.u.pitch] = ref + shift;
+        mine[(D + 1) * g.u.pitch] = total * exp2i(-(int)shift);
       }
       tc::tc_fence_before();   // (O has been read: the next product may be issued behind the barriers to come)
-      J0 += ntiles;
+      J0 += g.n;
       rows_barrier();
       if (tid == 128) tc::mbar_arrive(&bars[SB_SEGFREE + (seg & 3)]);
     }
@@ -964,18 +969,10 @@ __global__ void __launch_bounds__(128 * kLists) shared_merge_kernel(const __grid
     plan.share = x.deal >> 1;
     plan.whole = x.deal & 1;
     int row = x.row0 + r - rw.b * s.seq_rows;
-    const Unit u = unit_of(p, plan, x.rows, blocks, x.pre, x.at, hk, row >> 8);
-    row &= 255;
-    int first = u.begin / plan.share, last = (u.begin + u.tiles * u.w - 1) / plan.share, jb, je;
-    u.of(first * plan.share, plan.share, jb, je);
-    if (jb >= je) ++first;                     // (at either end: a tile that counts twice belongs to the share in which it begins)
-    u.of(last * plan.share, plan.share, jb, je);
-    if (jb >= je) --last;
-    const float* x = s.part + (u.slot(first) + (u.tall() && row >= 128 ? 128 : 0)) * (D + 2) + (row & (u.tall() ? 127 : 255)) + (int64_t)c0 * u.pitch;
-    const int64_t next = 256 * (D + 2);
-    add_after(x, x, next, last - first + 1, u.pitch, 0.f);
-    x += (int64_t)u.pitch * (D + 2);
-    if (!u.tall()) add_after(x, x, next, last - first + 1, u.pitch, 0.f);
+    const Unit u = unit_of(p, plan, x.rows, blocks, x.pre, x.at, hk, row >> 7);
+    const int first = u.begin / plan.share, last = (u.begin + u.tiles - 1) / plan.share;
+    const float* x0 = s.part + u.slot(first) * (D + 2) + (row & 127) + (int64_t)c0 * u.pitch;
+    add_after(x0, x0, 128 * (D + 2), last - first + 1, u.pitch, 0.f);
   }
   // the sequence's own
   if (live) {
@@ -1044,8 +1041,8 @@ bool space_of_call(const kvm_cache_t* c, const kvm_cache_call_t* call, int32_t n
   const int64_t Hkv = c->n_kv_heads, G = n_q_heads / Hkv, B = call->batch, units = B * Hkv, cols = call->n_tokens * G, d = c->head_dim;
   const int64_t tiles = ((int64_t)call->max_pages * c->page_tokens + kTile - 1) / kTile;
   const int64_t rows = B * cols;
-  if (rows > INT32_MAX / 4 || (rows / 256 + n_groups) * 2 * Hkv * tiles > INT32_MAX / 2) return false;
-  const int64_t slots = Hkv * (2 * rows + 16 * (int64_t)n_groups) + 256 * (kCtas + 1);
+  if (rows > INT32_MAX / 4 || (rows / 128 + n_groups) * Hkv * tiles > INT32_MAX / 2) return false;
+  const int64_t slots = Hkv * (rows + 8 * (int64_t)n_groups) + 128 * (kCtas + 1);
   if (slots > INT32_MAX / 2) return false;
   x.part = align16(slots * (d + 2) * 4);
   const bool few = cols <= kDecodeCols;
@@ -1123,7 +1120,7 @@ KVM_API kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm
   args.by_seq = FastDiv(args.seq_rows); args.by_group = FastDiv(a.G);
   args.q_vec = rows_aligned(q, a.sq); args.out_vec = rows_aligned(out, a.so);
   const int64_t tiles = ((int64_t)a.p.max_pages * a.p.page + kTile - 1) / kTile, rows = (int64_t)a.p.batch * args.seq_rows;
-  args.grid = (int)std::min<int64_t>(kCtas, (rows / 256 + n_groups) * 2 * a.p.Hkv * tiles);
+  args.grid = (int)std::min<int64_t>(kCtas, (rows / 128 + n_groups) * a.p.Hkv * tiles);
   CUtensorMap maps[2];
   if (!encode_tmaps(maps, a.p, a.d)) return KVM_ERR_CUDA;
   cudaStream_t s = (cudaStream_t)cuda_stream;
