@@ -499,16 +499,21 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         uint32_t buf = 0, at = 0;            // (columns); at: buffer of the next P V
 #pragma unroll 1
         for (int i = -3; i < g.n && ok; ++i) {
+          // (what is there as a rule is asked for first, so that nothing but the products lies between the weights, P V and S)
+          if (j < g.n && !wait(SB_KFULL + s, par)) break;
           if (i >= 0) {
             const uint32_t grp = i & 1;
             auto weights = [&]() {
               wait(SB_PREADY + grp, (back >> grp) & 1);
               back ^= 1u << grp;
             };
-            weights();
             if (!wait(SB_VFULL + v, vpar)) break;
-            const bool moved = __any_sync(0xffffffffu, s_flag[grp] == J);
-            if (moved || __any_sync(0xffffffffu, lane < 8 && s_used[8 * grp + lane] != version)) {   // (at most once)
+            weights();
+            if (!ok) break;
+            const int said = lane < 8 ? s_used[8 * grp + lane] : s_flag[grp];
+            const uint32_t again = __ballot_sync(0xffffffffu, lane < 8 ? said != version : said == J);
+            const bool moved = again >> 8;
+            if (again) {   // (at most once)
               if (leader) {
                 s_redo[grp] = J;
                 tc::mbar_arrive(&bars[SB_VERDICT + grp]);
@@ -539,7 +544,6 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             ++J;
           }
           if (j < g.n) {
-            if (!wait(SB_KFULL + s, par)) break;
             tc::tc_fence_after();
             const uint64_t k = dK + s * (Cfg::T8 >> 4);
             const uint32_t dS = tmem + Cfg::COL_S + buf, grp = j & 1;
