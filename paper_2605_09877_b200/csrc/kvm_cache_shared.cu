@@ -5,27 +5,26 @@
 // all of them see.  The kernels of kvm_cache_attend in their SIDE builds: every sequence's rows over its own blocks.  shared_merge_kernel: partial
 // results (O, reference m and sum l of a row, over some of its keys) to out = sum_z 2^(m_z - m) O_z / sum_z 2^(m_z - m) l_z.
 //
-// shared_kernel.  A unit is a (group, kv head) and 256 of the group's rows, or what is left of them.  The key tiles (128 tokens) of all units form one
-// list, in which a tile of more than 128 rows counts twice; every CTA takes an equal, contiguous share of it, whatever the lengths and the sizes of
-// the groups are, and leaves one partial result per unit that it has tiles of.
+// shared_kernel.  A unit is a (group, kv head) and 128 of the group's rows, or what is left of them.  The key tiles (128 tokens) of all units form one list; every CTA
+// takes an equal, contiguous share of it, whatever the lengths and the sizes of the groups are, and leaves one partial result per unit that it has tiles of.
 //     S = (q_hi + q_lo) K8^T   kind::f8f6f4: the codes as they lie in memory, q in two parts of e4m3
 //     O += P V16               kind::f16: P in fp16 from tensor memory, V16 = the codes of the values as fp16 numbers (exact)
-// as in kvm_cache_prompt.cu, but with two streams of one S and one O each: of two row tiles on the same keys (a tile of values is widened once for
-// 256 rows), or of one row tile on the even and the odd key tiles.  A stream goes S, softmax, P V, S, ...; while one is in its softmax the other is in the
-// tensor core, and nothing is handed from stream to stream.  A row's reference is the maximum of its first tile, and hardly ever has to be changed: later, S is read once, no
-// maximum is taken, and the two threads of a row, 64 columns each, need not meet.  What leaves the range shows in the sums of weights; then the products wait, the
-// stream's warps agree on references in a turn of their own, and go on.
+// S goes into three buffers in turn, P takes the place of its S; two groups of softmax warps take the tiles alternately, so that S of a tile and P V of another are
+// under way beside the softmax of a third.  A row's reference, common to both groups, is the maximum of the unit's first tile, and hardly ever has to be changed: later, S is
+// read once, no maximum is taken, and the two threads of a row, 64 columns each, need not meet.  What leaves the range shows in the sums of weights: then the products wait, the
+// group takes new references and shifts O to them, and weights of the other group that are in units of older ones are shifted before they are used (a version tells).
 // Scales of values go into the exponents of the weights, relative to the largest of the share's blocks, and out of the row sums again.
 //   warp 0       producer of keys (TMA, page numbers and scales ahead), warp 3 of values
 //   warp 1       issues the products, warp 2 finds the CTA's segments and writes down what the merge has to know
-//   warps 4-19   queries (scaled, split); softmax, eight warps per stream, two threads per row, 64 columns each; results
+//   warps 4-19   queries (scaled, split); softmax, eight warps per group, two threads per row, 64 columns each; results
 //   warps 20-23  value codes -> fp16, swizzled as the MMA reads them
 //
 // What bounds it: per 128 rows and 128 keys the products take 1024 cycles of the tensor core (q is there twice, so that S costs as much as in bf16), the powers 1024
-// of the special-function unit, operands and tiles some 1000 of shared memory.  A stream goes through S, softmax and P V one after the other, 4600 cycles with the other
-// stream's in between, so that two streams take 2300 per item; a third one has no tensor memory (2 S and 2 O of 128 columns are all 512).  64 sequences of 32 heads
-// on a document of 32768 tokens: 54 us, of which 8 are start (the plan, the queries) and 3 the results; the tensor core is active for a third of it.  Half of the
-// powers left to a polynomial were slower (+9%: instructions).  Code is read from memory by every CTA that begins: 93 -> 75 KB of it saved 2.5 us.
+// of the special-function unit, operands and tiles some 1400 of shared memory; the chain from S to S of a buffer makes 2300 of it.  64 sequences of 32 heads on a document of
+// 32768 tokens: 58 us, of which 7 are start (the list, the queries) and 2 the results; the tensor core is active for a third of it.  (Without powers, stores of widened values and most
+// of the products the whole call would take 70 us instead of 85: what is left is start, end, the keys' way and the two kernels behind.)  Half of the powers by a polynomial were
+// slower (+9%: instructions).  Two row tiles on the same keys, each with its own O and one S, widened the values once for both, 88 us: more partial results, and nothing
+// under way while a stream's weights are computed.  Code is read from memory by every CTA that begins: 93 -> 75 KB of it saved 2.5 us.
 // Weights in bf16 need no maximum at all (2 us less), but add as much error again as the result's own rounding has.
 #include <algorithm>
 #include <atomic>
@@ -289,10 +288,15 @@ __device__ __forceinline__ void widen4(uint32_t c, uint32_t& even, uint32_t& odd
   odd = ((c & 0x7f007f00u) >> 1) | (c & 0x80008000u);
 }
 __device__ __forceinline__ int channel_of(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
-// Barrier of the two warps that share 32 rows of a stream.
+// Barrier of the two warps of a group that share 32 rows.
 __device__ __forceinline__ void pair_barrier(int id) {
   __syncwarp();
   asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+}
+// A warp that gives up does not keep the other one waiting.
+__device__ __forceinline__ void pair_leave(int id) {
+  __syncwarp();
+  asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory");
 }
 // One thread of a warp (the same one every time).
 __device__ __forceinline__ bool elect_one() {
@@ -318,7 +322,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   volatile int* s_flag = reinterpret_cast<int*>(s_vmax + 20);           // [group]: the tile whose weights leave the range
   volatile int* s_redo = s_flag + 2;                                    // [group]: the tile that is done again
   volatile int* s_used = s_redo + 2;                                    // [group][warp]: the version of the references that its weights are in
-  int* s_version = const_cast<int*>(s_used) + 16;                       // (written by the warp that issues the products alone)
+  volatile int* s_version = s_used + 16;                                // (written by the warp that issues the products alone)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (who waits for this kernel does so before reading what it wrote)
   if (warp == 0) {
@@ -350,6 +354,9 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       f = w0 = (int)min((int64_t)plan.total, (int64_t)blockIdx.x * plan.share);
       w1 = min(plan.total, w0 + plan.share);
     }
+    Segment first;
+    if (!segment_at(args, plan, w0, w1, f, first)) first.n = 0;
+    if (lane == 0) segs[0] = first;
   }
   __syncthreads();
   tc::tc_fence_after();
@@ -359,7 +366,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     *abort_flag = 1;
   };
   auto next_segment = [&](int seg, Segment& g, bool& ok) {   // (by a whole warp)
-    ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SEGFULL + (seg & 3)], (seg >> 2) & 1));
+    if (seg > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SEGFULL + (seg & 3)], (seg >> 2) & 1));
     if (!ok) return false;
     g = segs[seg & 3];
     __syncwarp();
@@ -376,9 +383,10 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       for (int seg = 0; ok; ++seg) {
         if (seg >= 4) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_SEGFREE + (seg & 3)], ((seg >> 2) - 1) & 1));
         if (!ok) break;
-        if (!segment_at(args, plan, w0, w1, f, g)) g.n = 0;
+        if (seg == 0) g.n = segs[0].n;   // (it has been there since the block's barrier)
+        else if (!segment_at(args, plan, w0, w1, f, g)) g.n = 0;
         if (lane == 0) {
-          segs[seg & 3] = g;
+          if (seg > 0) segs[seg & 3] = g;
           tc::mbar_arrive(&bars[SB_SEGFULL + (seg & 3)]);
         }
         if (seg == 0) {
@@ -514,6 +522,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             const uint32_t again = __ballot_sync(0xffffffffu, lane < 8 ? said != version : said == J);
             const bool moved = again >> 8;
             if (again) {   // (at most once)
+              tc::tc_fence_after();
+              tc::tc_fence_before();
               if (leader) {
                 s_redo[grp] = J;
                 tc::mbar_arrive(&bars[SB_VERDICT + grp]);
@@ -523,7 +533,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
               if (!ok) break;
               if (moved) {
                 ++version;
-                if (leader) asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(s_version)), "r"(version) : "memory");
+                if (leader) *s_version = version;   // (read behind a verdict to come)
               }
             }
             tc::tc_fence_after();
@@ -563,6 +573,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
           }
         }
         if (!ok) break;
+        tc::tc_fence_after();
+        tc::tc_fence_before();
         if (leader) tc::mbar_arrive(&bars[SB_END]);   // (all products have landed)
         __syncwarp();
       }
@@ -644,9 +656,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     int turn = 0, verdicts = 0, J0 = 0;   // tiles of this group, verdicts on them; tiles of the CTA
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
-      ok = tc::mbar_wait_tight(&bars[SB_SEGFULL + (seg & 3)], (seg >> 2) & 1);
       const Segment& g = segs[seg & 3];   // (free again behind the results)
-      if (!ok || g.n == 0) break;
+      if (g.n == 0) break;
       // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split (those of any alignment one after the other).
       constexpr int TPR = D / 16, ITER = 128 * TPR / 512;   // threads per row; rows of a thread
       const int piece = tid % TPR, row0 = (tid - 128) / TPR;
@@ -703,6 +714,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       tc::fence_proxy_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&bars[SB_QFULL]);
+      int version = *s_version;   // of the references that the group knows (nobody moves any before the first weights, which are given away behind this barrier)
       rows_barrier();
       float cq = s_cq[row];
       bool bad = !(cq == cq);   // NaN rows are marked, not computed with
@@ -712,7 +724,10 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
       const int vb = max(max(vm[0], vm[1]), max(vm[2], vm[3]));
       const float vbase = vb == -1000 ? 0.f : (float)vb;
       float m = 0.f, l = 0.f;   // reference of the thread's weights (a whole number), their sum
-      if (ok && grp == 1 && g.n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_REF], seg & 1));
+      if (ok && grp == 1 && g.n > 1) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_REF], seg & 1));
+        m = s_ref[row];
+      }
       uint32_t tS = lanes + Cfg::COL_S + 128 * grp + 64 * half;
 #pragma unroll 1
       for (int i = grp; i < g.n && ok; i += 2) {
@@ -723,21 +738,16 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const KeyTile& ti = info[(J0 + i) % kInfo];
         const int n = ti.n - 64 * half;         // the half's columns that are there: pages are whole, 16 columns are there or not
         if (ti.flags) bad = true;
-        int version;
-        asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(version) : "r"(tc::smem_u32(s_version)) : "memory");
         float sum = 0.f;
         bool held = false, redo = false;        // weights that are not given away: some leave the range
-        if (i > 0) {
-          const float now = s_ref[row];
-          if (i > 1 && m != now) l *= tc::ex2_approx(m - now);   // (nothing to shift in the group's first tile)
-          m = now;
-        }
 #pragma unroll 1
         for (;;) {
           if (i == 0 || redo) {
-            // The row's reference in the first tile: its largest y.  Or some row has weights beyond the range, or references have moved since these weights were computed: the
-            // largest y of the halves whose weights are held back, or what it is by now; weights that are not held back are shifted to it where they lie.
+            // The row's reference in the first tile: its largest y.  Or some row has weights beyond the range, or references have moved for the tile before: the largest y of the
+            // halves whose weights are held back, or what it is by now; weights that are not held back are shifted to it where they lie.  (References that the other
+            // group has moved are taken over here only, however early they are there: results do not depend on who is faster.)
             const float now = redo ? s_ref[row] : -INFINITY;
+            if (redo) version = *s_version + (s_flag[grp] == J0 + i ? 1 : 0);   // (once this is done)
             float mx = -INFINITY;
             if (!redo || held) {
 #pragma unroll 1
@@ -831,7 +841,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
               sum += l0 * exp2i(-(int)fold - kBias);
               top = fmaxf(top, l0);
             }
-            held = !redo && __any_sync(0xffffffffu, top > kMost);
+            held = !redo && i > 0 && __any_sync(0xffffffffu, top > kMost);   // (the first tile has its own maximum)
             if (!held) tc::tmem_st32(tS, pr);   // (columns that the warp has read)
             else if (lane == 0) s_flag[grp] = J0 + i;
           }
@@ -851,7 +861,9 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         l += sum;
         tS = tS >= lanes + Cfg::COL_S + 128 + 64 * half ? tS - 128 : tS + 256;   // (two buffers further of three)
       }
-      ok = ok && tc::mbar_wait_tight(&bars[SB_END], seg & 1);
+      if (!ok) pair_leave(pair);
+      // (the next segment is waited for here, so that all warps begin it or none)
+      ok = ok && __all_sync(0xffffffffu, tc::mbar_wait_tight(&bars[SB_END], seg & 1) && tc::mbar_wait_tight(&bars[SB_SEGFULL + ((seg + 1) & 3)], ((seg + 1) >> 2) & 1));
       tc::tc_fence_after();
       // the four threads' sums; whether all are well, and so whether there is a next time: the same for all
       const float nan = __int_as_float(0x7fc00000), ref = s_ref[row];

@@ -518,3 +518,30 @@ def test_few_results_are_rounded_otherwise_than_the_definition(kvm, n, d):
     chance = torch.clamp(off / step, max=1.0)                      # (the mean of |x| is no more than its standard deviation)
     others = (out[:, :, 0].double() != want.bfloat16().double()).sum().item()
     assert others <= chance.sum().item() + 6 * math.sqrt(chance.sum().item()), (others, chance.sum().item())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d", [(8, 64), (70, 128)])
+def test_results_are_the_same_every_time(kvm, n, d):
+    """Also where references move for some rows in most tiles, alone and beside another call on a second stream."""
+    P, L = 64, 4096
+    c = kvm.Cache.empty(L // P + n, 2, d, P)
+    u = torch.ones(d) / math.sqrt(d)
+    k = (rows((1, 2, L, d), 1).float() * 0.3 + (torch.arange(L) // 130)[:, None] * 0.6 * u).bfloat16()
+    head = torch.arange(L // P, dtype=torch.int32)[None]
+    c.append(k.cuda(), rows((1, 2, L, d), 2).cuda(), head.cuda(), i32([0]))
+    table = torch.cat([head.repeat(n, 1), L // P + torch.arange(n, dtype=torch.int32)[:, None]], 1).cuda()
+    start = i32([L] * n)
+    c.append(rows((n, 2, 1, d), 4).cuda(), rows((n, 2, 1, d), 5).cuda(), table, start)
+    q = (rows((n, 8, 1, d), 3).float() + torch.linspace(0.0, 16.0, n * 8).view(n, 8, 1, 1) * u).bfloat16().cuda()
+    args = (q, table, start, i32([0, n]), i32([L // P]))
+    want = c.attend_shared(*args, scale=1.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        with torch.cuda.stream(side):
+            other = c.attend_shared(*args, scale=1.0)
+        assert torch.equal(c.attend_shared(*args, scale=1.0).view(torch.int16), want.view(torch.int16))
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(other.view(torch.int16), want.view(torch.int16))
+    assert not torch.isnan(want.float()).any()
