@@ -396,7 +396,7 @@ typedef struct {
   int32_t norm, layout, scaling;           /* the kinds above */
   int32_t rope_dims;                       /* r: even, 0 .. head_dim; 0: no rotation (what follows is not looked at) */
   double base, factor, low, high;          /* base >= 1; factor >= 1 (LINEAR, PARTS); 0 <= low < high (PARTS) */
-  double magnitude;                        /* of cos and sin; 1 unless a long context asks for another */
+  double magnitude;                        /* of cos and sin, 1e-30 .. 1e30; 1 unless a long context asks for another */
   int64_t original_len;                    /* PARTS: tokens, >= 1 */
   float eps;                               /* >= 0, with a norm */
   const double* frequencies;               /* HOST [rope_dims / 2], f_i as kvm_rope_frequencies gives them (a program that calls often computes them

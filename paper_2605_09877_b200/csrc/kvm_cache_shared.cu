@@ -253,13 +253,13 @@ struct alignas(16) KeyTile {
 };
 
 // SB_SFULL: [group][number of its tile & 1]; SB_PREADY, SB_VERDICT: per group of softmax warps
-enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 23, SB_SFULL = 26, SB_PREADY = 30, SB_VERDICT = 32, SB_PVDONE = 34,
-       SB_END = 35, SB_REF = 36, SB_QFULL = 37, SB_VBASE = 38, SB_SEGFULL = 42, SB_SEGFREE = 46, SB_COUNT = 50 };
+enum { SB_KFULL = 0, SB_KFREE = 6, SB_V8FULL = 12, SB_V8FREE = 16, SB_VFULL = 20, SB_VFREE = 22, SB_SFULL = 24, SB_PREADY = 28, SB_VERDICT = 30, SB_PVDONE = 32,
+       SB_END = 33, SB_REF = 34, SB_QFULL = 35, SB_VBASE = 36, SB_SEGFULL = 40, SB_SEGFREE = 44, SB_COUNT = 48 };
 
 struct Segment { Unit u; int jb, n; };   // tiles [jb, jb + n) of the unit; n = 0: there are no more
 template <int D>
 struct SharedCfg {
-  static constexpr int NK = 3 * (128 / D), NV8 = 2 * (128 / D), NV = 3;
+  static constexpr int NK = D == 128 ? 5 : 6, NV8 = 2 * (128 / D), NV = 2;   // (3 of each with 128 channels: 84.4 us instead of 84.0 on a document)
   static constexpr int T8 = 128 * D, T16 = 256 * D;
   static constexpr int OFF_Q = 0;                        // hi, lo
   static constexpr int OFF_K = OFF_Q + 2 * T8;
@@ -328,7 +328,7 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
   if (warp == 0) {
     for (int i = lane; i < SB_COUNT; i += 32) {
       auto in = [&](int first, int n) { return i >= first && i < first + n; };
-      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 3) || in(SB_VBASE, 4) || i == SB_REF ? 4 : in(SB_PREADY, 2) || in(SB_SEGFREE, 4) ? 8 : i == SB_QFULL ? 16 : 1);
+      tc::mbar_init(&bars[i], in(SB_V8FREE, 4) || in(SB_VFULL, 2) || in(SB_VBASE, 4) || i == SB_REF ? 4 : in(SB_PREADY, 2) || in(SB_SEGFREE, 4) ? 8 : i == SB_QFULL ? 16 : 1);
     }
     if (lane == 0) {
       tc::prefetch_tmap(&mapK); tc::prefetch_tmap(&mapV);
@@ -916,8 +916,8 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 }
 
 // Merge.  Block: 128 rows (b, t, head of the kv head's group), CH channels, one kv head; kLists threads per row, which take the row's partial results in turn.
-// Bound by the latency of what it reads (19 MB, mostly out of L2).  Two lists, eight channels: 88 us for the whole call on 64 samples of a document; four lists 90 (but
-// 52 instead of 55 for 24 x 4 tokens of 64 channels), four channels 91, eight partial results on their way 92.
+// Bound by the latency of what it reads (10 MB, mostly out of L2).  Two lists, four partial results on their way, eight channels: 84.6 us for the whole call on 64 samples of a
+// document, 50.9 for 24 x 4 tokens of 64 channels; four lists 87.5 and 50.3 (of two results 87.2 and 49.4), two results 85.9 and 52.9, six 84.8 and 51.0.
 constexpr int kLists = 2;
 template <int D, int CH>
 __global__ void __launch_bounds__(128 * kLists) shared_merge_kernel(const __grid_constant__ SharedArgs s) {
