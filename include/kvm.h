@@ -507,7 +507,7 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
 
 /* kvm_cache_attend (window = 0) for a batch whose sequences share their first blocks in groups: a system prompt, a document, the samples or beams of one
  * prompt.  Group g is sequences groups[g] .. groups[g + 1] - 1, and the first shared[g] blocks of their tables hold the same tokens (forks: the same
- * pages; kvm_pages_shared counts them).  Those blocks are read once for the group, from the table of its first sequence; entries of the other tables there
+ * pages; kvm_pages_shared counts them).  Those blocks are read for the group together, from the table of its first sequence, once per 128 rows of queries (tokens times heads of a kv head's group); entries of the other tables there
  * may be anything.  Every token sees what it sees in kvm_cache_attend; the results differ by rounding.
  *   groups   device int32 [n_groups + 1]: ascends (groups of no sequences are allowed) from 0 to batch
  *   shared   device int32 [n_groups], 0 <= shared[g] <= max_pages, and shared[g] * page_tokens <= start[b] for the sequences of g

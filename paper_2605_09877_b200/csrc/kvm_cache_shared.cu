@@ -1,5 +1,5 @@
 // Attention for a batch whose sequences share their first blocks in groups (a system prompt, a document, the samples or beams of one prompt):
-// every shared block is read, and multiplied with the queries of its whole group, once.
+// every shared block is multiplied with the queries of its whole group, and read once per 128 rows of them.
 //
 // Three launches.  shared_kernel: the rows of a group, (sequence, token, head of a kv head's group), over the group's shared blocks, all of which
 // all of them see.  The kernels of kvm_cache_attend in their SIDE builds: every sequence's rows over its own blocks.  shared_merge_kernel: partial
