@@ -511,7 +511,8 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
  * may be anything.  Every token sees what it sees in kvm_cache_attend; the results differ by rounding.
  *   groups   device int32 [n_groups + 1]: ascends (groups of no sequences are allowed) from 0 to batch
  *   shared   device int32 [n_groups], 0 <= shared[g] <= max_pages, and shared[g] * page_tokens <= start[b] for the sequences of g
- * Groups that are none, or a number of blocks that is not allowed, are reported like lengths that are not, and their sequences get no rows.
+ * Groups that are none, or a number of blocks that is not allowed, are reported like lengths that are not, and their sequences get no rows. Rows of
+ * q behind a sequence's count may be read, but nothing comes of them.
  * Otherwise as kvm_cache_attend, the precision of q included; weights over shared blocks go into the products in fp16, as there beyond 16 pairs, those over a
  * sequence's own blocks as they do there.  Codes of NaN under a finite scale, which append never writes,
  * count as 480 among the values of shared blocks.  workspace: kvm_cache_shared_workspace() bytes.

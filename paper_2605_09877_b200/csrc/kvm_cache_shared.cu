@@ -658,22 +658,25 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     for (int seg = 0;; ++seg) {
       const Segment& g = segs[seg & 3];   // (free again behind the results)
       if (g.n == 0) break;
-      // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split (those of any alignment one after the other).
+      // The queries: every thread takes 32 bytes of a few rows, all on their way before the first is split (those of any alignment one after the other).  Rows behind a
+      // sequence's count are taken as 0: whatever they hold must not move references that its warp shares (the results of other rows would be rounded otherwise).
       constexpr int TPR = D / 16, ITER = 128 * TPR / 512;   // threads per row; rows of a thread
       const int piece = tid % TPR, row0 = (tid - 128) / TPR;
-      auto row_at = [&](int r) {
-        const Row rw = row_of(args, g.u.b0, g.u.row0 + r);
-        return a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece;
-      };
+      auto row_at = [&](const Row& rw) { return a.q + rw.b * a.sq[0] + (int64_t)(g.u.hk * a.G + rw.h) * a.sq[1] + rw.t * a.sq[2] + 16 * piece; };
       uint4 raw[2 * ITER];
+      uint32_t there = 0;   // of the thread's rows: those in front of the count
 #pragma unroll
       for (int i = 0; i < ITER; ++i) {
         const int r = row0 + 512 / TPR * i;
         raw[2 * i] = raw[2 * i + 1] = make_uint4(0, 0, 0, 0);
-        if (r < g.u.n && args.q_vec) {
-          const uint4* src = reinterpret_cast<const uint4*>(row_at(r));
-          raw[2 * i] = src[0];
-          raw[2 * i + 1] = src[1];
+        if (r < g.u.n) {
+          const Row rw = row_of(args, g.u.b0, g.u.row0 + r);
+          if (args.q_vec) {   // (on its way beside the count)
+            const uint4* src = reinterpret_cast<const uint4*>(row_at(rw));
+            raw[2 * i] = src[0];
+            raw[2 * i + 1] = src[1];
+          }
+          if (!p.count || rw.t < p.count[rw.b]) there |= 1u << i;
         }
       }
 #pragma unroll 1
@@ -683,8 +686,11 @@ shared_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
         for (int j = 0; j < 2 * ITER - 2; ++j) raw[j] = raw[j + 2];
-        if (r < g.u.n && !args.q_vec) {
-          const uint16_t* src = reinterpret_cast<const uint16_t*>(row_at(r));
+        if (!(there >> i & 1)) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] = 0;
+        } else if (!args.q_vec) {
+          const uint16_t* src = reinterpret_cast<const uint16_t*>(row_at(row_of(args, g.u.b0, g.u.row0 + r)));
 #pragma unroll
           for (int q = 0; q < 8; ++q) x[q] = src[2 * q] | (uint32_t)src[2 * q + 1] << 16;
         }

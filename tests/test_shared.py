@@ -545,3 +545,28 @@ def test_results_are_the_same_every_time(kvm, n, d):
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(other.view(torch.int16), want.view(torch.int16))
     assert not torch.isnan(want.float()).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,P,T,G,n,aligned", [(128, 64, 4, 4, 20, True), (64, 16, 6, 2, 40, True), (128, 32, 2, 4, 70, False), (64, 64, 70, 4, 6, False)])
+def test_rows_behind_the_counts_reach_nothing(kvm, d, P, T, G, n, aligned):
+    """Whatever the padding of q holds, every bit of the results in front of it is the same, and the rows of out behind it are left as they were."""
+    Hkv, lead = 2, 40
+    m = Shared(kvm, [n], [lead], [50 + b % 7 for b in range(n)], Hkv, d, P)
+    counts = [b % T + (1 if b % 3 else 0) if b % 5 else 0 for b in range(n)]
+    m.append(rows((n, Hkv, T, d), 1), rows((n, Hkv, T, d), 2), counts)
+    q, start = rows((n, G * Hkv, T, d), 3).cuda(), i32([x - c for x, c in zip(m.len, counts)])
+    live = (torch.arange(T)[None] < torch.tensor(counts)[:, None]).cuda()[:, None, :, None]
+    want = None
+    for i, fill in enumerate((0.0, 1.0, 50.0, 3e4, 1e38, math.inf, math.nan)):
+        x = torch.where(live, q, rows(q.shape, 4).cuda() * 50.0 if i == 2 else torch.full_like(q, fill))
+        if not aligned:
+            wide = torch.empty((n, G * Hkv, T, d + 1), dtype=torch.bfloat16, device="cuda")
+            wide[..., 1:] = x
+            x = wide[..., 1:]
+        out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+        m.cache.attend_shared(x, m.hidden(), start, m.groups, m.shared, i32(counts), out=out, status=status)
+        assert status.item() == 0 and (torch.where(live, 7.0, out.float()) == 7.0).all()
+        want = out if want is None else want
+        assert torch.equal(out, want), (fill, int((out != want).sum()))
+    m.compare(q.cpu(), want, counts, 0, 0)
