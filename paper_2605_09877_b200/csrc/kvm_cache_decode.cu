@@ -68,7 +68,8 @@ struct DecodeCfg {
   static constexpr int OFF_AB = OFF_MAX + NG * 2 * NC * 16;              // float4 [group][2][NC]
   static constexpr int OFF_L = OFF_AB + NG * 2 * NC * 16;                // float [group][4][NC]
   static constexpr int OFF_BAR = OFF_L + NG * 4 * NC * 4;
-  static constexpr int OFF_PRE = OFF_BAR + 1024;         // int [batch + 1]; SIDE: and [batch], the shared blocks of each sequence
+  static constexpr int OFF_PRE = OFF_BAR + 1024;         // int [batch + 1]; SIDE: and [batch], the shared blocks of each sequence, and [groups + 1], their offsets
+  static constexpr int smem(int batch, int groups) { return OFF_PRE + (SIDE ? 2 * batch + groups + 2 : batch + 1) * 4 + 1024; }
   static constexpr uint32_t TMEM_COLS = NC == 8 ? 256 : 512;
   static constexpr uint32_t GROUP_COLS = 3 * NB;         // two S, then O
   // barriers
@@ -173,7 +174,8 @@ __device__ __forceinline__ int seq_of(const int* pre, int batch, int f) {
 }
 
 // pre[0 .. batch]: tiles of the sequences before b, all heads; by all NT threads of the block.  SIDE: skip[b], the shared blocks of each sequence
-// (offsets: room for the groups' offsets, n + 1); groups that are none leave nothing to do.
+// (offsets: room for the groups' offsets, n + 1; not where a tile goes, since nothing orders ordinary stores before the copies of a tile); groups that are none leave
+// nothing to do.
 template <int NT, bool SIDE>
 __device__ __forceinline__ void list_tiles(const AttendArgs& a, int* pre, int* scratch, int* skip, int* offsets) {
   const Params& p = a.p;
@@ -268,7 +270,7 @@ decode_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   tc::tc_fence_before();
-  list_tiles<Cfg::THREADS, SIDE>(a, pre, reinterpret_cast<int*>(base + Cfg::OFF_AB), pre + p.batch + 1, reinterpret_cast<int*>(base));   // (offsets: where the first tiles go)
+  list_tiles<Cfg::THREADS, SIDE>(a, pre, reinterpret_cast<int*>(base + Cfg::OFF_AB), pre + p.batch + 1, pre + 2 * p.batch + 1);
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Shares<NG> sh(pre[p.batch], args.grid, blockIdx.x);
@@ -833,9 +835,9 @@ int64_t decode_workspace(int64_t units, int64_t tiles, int d, int cols) {
 template <int D, int NC, bool SIDE>
 static kvm_status_t launch_decode_nc(const DecodeArgs8& args, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
   using Cfg = DecodeCfg<D, NC, SIDE>;
-  constexpr int most = Cfg::OFF_PRE + (kMaxBatch + 1) * (SIDE ? 8 : 4) + 1024;
+  constexpr int most = Cfg::smem(kMaxBatch, kMaxBatch);
   static_assert(most <= 227 * 1024, "shared memory");
-  const int smem = Cfg::OFF_PRE + (args.a.p.batch + 1) * (SIDE ? 8 : 4) + 1024;
+  const int smem = Cfg::smem(args.a.p.batch, args.a.groups.n);
   static std::atomic<uint64_t> ready{0};   // devices on which the limit has been raised
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }

@@ -570,3 +570,15 @@ def test_rows_behind_the_counts_reach_nothing(kvm, d, P, T, G, n, aligned):
         want = out if want is None else want
         assert torch.equal(out, want), (fill, int((out != want).sum()))
     m.compare(q.cpu(), want, counts, 0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,P,T,n", [(64, 16, 1, 1024), (128, 16, 4, 300), (64, 32, 2, 700), (128, 64, 1, 200)])
+def test_offsets_of_many_groups_beside_the_first_tiles(kvm, d, P, T, n):
+    """As many groups as sequences, each with blocks of its own behind its shared one: what a CTA knows of the groups is not where it loads tiles."""
+    m = Shared(kvm, [1] * n, [1] * n, [3 * P + b % 40 for b in range(n)], 1, d, P, room=10)
+    m.step(T, 4, [T] * n, 0)
+    q, start, out = m.step(T, 4, [b % T + 1 for b in range(n)], 1)
+    count = i32([b % T + 1 for b in range(n)])
+    for _ in range(3):
+        assert torch.equal(m.cache.attend_shared(q.cuda(), m.hidden(), start, m.groups, m.shared, count, out=torch.full_like(out, 7.0)), out)
