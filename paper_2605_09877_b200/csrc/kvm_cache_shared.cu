@@ -55,6 +55,7 @@ constexpr float kMost = 60000.f;
 constexpr int kLowValues = 24;   // where the values are small their sums are held in units smaller by that, so that all bits stay above 2^-126
 constexpr float kShift = 6.f;    // what the kernels for few and for many tokens count their weights in (of 2^-8 and 2^-6 of the reference)
 constexpr float kDecodeShift = 8.f;
+constexpr int kStartTiles = 4;   // key tiles that take as long as a unit's start and end
 
 // A sequence, as shared_kernel leaves it for the merge: lengths (n = 0: no rows), its group's shared blocks and rows, its first row among them, the group's
 // place in the list, and how the list is dealt.
@@ -107,8 +108,11 @@ __device__ __forceinline__ int units_of(int n) { return (n + 127) >> 7; }
 __device__ __forceinline__ int space_of(int n) { return (n & ~127) + pad8(n & 127); }
 
 // The plan, by one warp; mem: 3 (n_groups + 1) ints.  false: groups that are none.
-// Where there are no more units than CTAs, a share is the least of 32 lengths (or that of the longest unit) with which every CTA has tiles of one unit only: a unit
-// that begins in the middle of a share costs its CTA a start and an end more, 6 us, and the others wait for it.
+// Where there are no more units than CTAs, a share is the least of 32 lengths with which every CTA has tiles of one unit only: a unit that begins in the middle of a share
+// costs its CTA a start and an end more, 6 us (kStartTiles), and the others wait for it.  Where none of them does (many short units beside long ones), either the longest unit is
+// a share, or the list is dealt in equal ones whatever begins in them: what takes less for the CTA with the most to do.  Units of 128 channels, us as a list and with the
+// longest as a share: 8 of 256 tiles and 112 of 2 (8 heads) 108 and 382; 16 of 150 and 130 of 1 144 and 234; 24 of 100 and 120 of 1 144 and 169; 38 of 60 and 110 of 2 103 and
+// 118; and 38 of 60, 90 and 120 and 110 of 1 139, 183, 230 and 118, 158, 197.
 __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& plan) {
   const Groups& gr = s.a.groups;
   const Params& p = s.a.p;
@@ -120,7 +124,7 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
   constexpr uint32_t kAll = 0xffffffffu;
   const int lane = threadIdx.x & 31;
   bool ok = true;
-  int tiles_sum = 0, units = 0, most = 0;   // tiles of all units, units, tiles of the longest
+  int tiles_sum = 0, units = 0, most = 0, least = INT32_MAX;   // tiles of all units, units, tiles of the longest and of the shortest
 #pragma unroll 1
   for (int g0 = 0; g0 <= gr.n; g0 += 32) {
     // sequences before a group; its key tiles (in `pre` for now)
@@ -136,6 +140,7 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
         tiles_sum += p.Hkv * tiles * units_of(n);
         units += p.Hkv * units_of(n);
         most = max(most, tiles);
+        least = min(least, tiles);
       }
     }
   }
@@ -162,8 +167,14 @@ __device__ __forceinline__ bool make_plan(const SharedArgs& s, int* mem, Plan& p
     }
     const uint32_t fits = __ballot_sync(kAll, ctas * p.Hkv <= s.grid);
     most = __reduce_max_sync(kAll, most);
-    plan.share = fits ? __shfl_sync(kAll, length, __ffs(fits) - 1) : max(2, most);
-    plan.whole = true;
+    least = __reduce_min_sync(kAll, least);
+    if (fits) {
+      plan.share = __shfl_sync(kAll, length, __ffs(fits) - 1);
+      plan.whole = true;
+    } else if (most <= plan.share + kStartTiles * ((plan.share - 2) / least + 1)) {   // (a run of so many tiles lies in that many units more than one, at most)
+      plan.share = max(2, most);
+      plan.whole = true;
+    }
   }
   int at_pre = 0, at_rows = 0;   // before the next 32 groups
 #pragma unroll 1

@@ -582,3 +582,113 @@ def test_offsets_of_many_groups_beside_the_first_tiles(kvm, d, P, T, n):
     count = i32([b % T + 1 for b in range(n)])
     for _ in range(3):
         assert torch.equal(m.cache.attend_shared(q.cuda(), m.hidden(), start, m.groups, m.shared, count, out=torch.full_like(out, 7.0)), out)
+
+
+def dealt(m, q, table, start, groups, shared):
+    """How a call deals its key tiles: (those of a CTA, whether a CTA has tiles of one unit only), from the last 32 bytes that it leaves per sequence in the workspace."""
+    L, c, B = m.lib, C.byref(m.CacheCall(table.data_ptr(), start.data_ptr(), None, table.shape[0], table.shape[1], q.shape[2])), table.shape[0]
+
+    def run(cache):
+        n = L.kvm_cache_shared_workspace(cache._ref, c, shared.numel(), q.shape[1])
+        ws, out = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+        assert L.kvm_cache_attend_shared(cache._ref, c, groups.data_ptr(), shared.data_ptr(), shared.numel(), q.data_ptr(), q.shape[1], 1.0, out.data_ptr(), None, None,
+                                         ws.data_ptr(), n, None, torch.cuda.current_stream().cuda_stream) == 0
+        deal = set(ws[n - 32 * B:].view(torch.int32).view(B, 8)[:, 7].tolist())
+        assert len(deal) == 1
+        return deal.pop() >> 1, bool(ws[n - 4:].view(torch.int32).item() & 1)
+    return run
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("short,short_tiles,long,long_tiles,Hkv,share,whole", [
+    (12, 2, 1, 256, 8, 43, True),            # (a length of the 32 fits: 96 units and 8 times six CTAs)
+    (13, 2, 1, 256, 8, 16, False),           # (none does: the longest unit would be 256 tiles, an equal share is 16)
+    (17, 2, 1, 256, 8, 16, False),
+    (110, 1, 38, 60, 1, 60, True),           # (none does either, but an equal share of 17 tiles may lie in 17 units of one tile)
+    (140, 1, 1, 40, 1, 5, True),             # (180 tiles: shares of 2, or of up to 5, and 140 + 40 / 5 are 148 CTAs)
+    (142, 1, 1, 40, 1, 2, False)])           # (two more than there are)
+def test_short_prompts_beside_long_documents(kvm, short, short_tiles, long, long_tiles, Hkv, share, whole):
+    """No CTA gets a long unit whole where most units are short, and every row is right however the tiles are dealt."""
+    d, P, G, per = 64, 128, 2, 2
+    lead = [short_tiles] * (short // 2) + [long_tiles] * long + [short_tiles] * (short - short // 2)
+    B, width = per * len(lead), max(lead) + 1
+    c = kvm.Cache.empty(sum(lead) + B, Hkv, d, P)
+    for i, (codes, scale) in enumerate(((c.k8, c.k_scale), (c.v8, c.v_scale))):       # values of +-2^-3 .. 2^1, scales of a few powers of two
+        g = torch.Generator().manual_seed(i)
+        codes.view(torch.uint8).copy_(torch.randint(0x20, 0x40, codes.shape, generator=g) | (torch.randint(0, 2, codes.shape, generator=g) << 7))
+        scale.copy_(torch.exp2(torch.randint(-2, 2, scale.shape, generator=g).float()))
+    table, at = torch.full((B, width), -1, dtype=torch.int32), 0
+    for i, n in enumerate(lead):
+        table[per * i:per * i + per, :n] = torch.arange(at, at + n)
+        at += n
+    for b in range(B):
+        table[b, lead[b // per]] = at + b
+    own = [1 + b % 90 for b in range(B)]
+    start = i32([lead[b // per] * P + own[b] - 1 for b in range(B)])
+    groups, shared, q, t = i32(list(range(0, B + 1, per))), i32(lead), rows((B, G * Hkv, 1, d), 3, outliers=False).cuda(), table.cuda()
+    out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+    c.attend_shared(q, t, start, groups, shared, scale=0.2, out=out, status=status)
+    assert status.item() == 0
+    for _ in range(3):
+        assert torch.equal(c.attend_shared(q, t, start, groups, shared, scale=0.2), out)
+    K, V = ((x.view(torch.float8_e4m3fn).float() * s[:, :, None, None]).cpu().double().numpy() for x, s in ((c.k8, c.k_scale), (c.v8, c.v_scale)))
+    qn, on = q.float().cpu().double().numpy(), out.float().cpu().double().numpy()
+    for b in range(B):
+        n = lead[b // per] * P + own[b]
+        pages = table[b, :lead[b // per] + 1].numpy()
+        for h in range(Hkv):
+            ref, bound = ec.attend(qn[b, G * h:G * h + G, 0], K[pages, h].reshape(-1, d)[:n], V[pages, h].reshape(-1, d)[:n], np.full(G, n - 1), float(np.float32(0.2)))
+            assert (np.abs(on[b, G * h:G * h + G, 0] - ref) <= bound).all(), (b, h)
+    assert dealt(kvm, q, t, start, groups, shared)(c) == (share, whole)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,P,T,moving", [(64, 16, 2, False), (128, 32, 1, True), (64, 64, 1, True), (128, 16, 3, True)])
+def test_runs_of_tiles_through_units_of_all_lengths(kvm, d, P, T, moving):
+    """More units than CTAs, of 1 to 20 tiles and 3 to 128 rows, the borders of the CTAs' shares anywhere in them: every row against the definition, with references that move in
+    most of the units, the same every time, and with a NaN in one unit alone."""
+    r = random.Random(d + P)
+    Hkv, G, per = 3, 4, 128 // P
+    sizes = [1, 2, 1, 45, 1, 3, 1, 1] + [r.choice([1, 1, 2, 3]) for _ in range(44)]
+    lead = [per * (1 + i * 7 % 20) - r.choice([0, 0, per // 2, 1]) * (per > 1) for i in range(len(sizes))]
+    lead = [max(1, x) for x in lead]
+    n = sum(sizes)
+    m = Shared(kvm, sizes, [0] * len(sizes), [0] * n, Hkv, d, P, room=max(lead) * P + 200)
+    L = max(lead) * P
+    k, v = rows((n, Hkv, L, d), 1), rows((n, Hkv, L, d), 2)
+    u = torch.ones(d) / math.sqrt(d)
+    if moving:                                                     # logits that grow from tile to tile, from another column on in every head, over blocks of several scales
+        for h in range(Hkv):
+            k[:, h] = (k[:, h].float() * 0.05 + ((torch.arange(L) + 43 * h) // 128)[:, None] * u).bfloat16()
+        v = (v.float() * torch.exp2(((torch.arange(L) // P) % 5 - 2).float())[:, None]).bfloat16()
+    counts = [0] * n
+    for g in range(len(sizes)):
+        counts[m.first[g]] = lead[g] * P
+    m.append(k, v, counts)
+    for g, size in enumerate(sizes):
+        f = m.first[g]
+        for b in range(f + 1, f + size):
+            m.table[b, :lead[g]] = m.table[f, :lead[g]]
+            m.k[b], m.v[b], m.len[b] = copy.deepcopy(m.k[f]), copy.deepcopy(m.v[f]), m.len[f]
+    m.lead, m.shared = lead, i32(lead)
+    own = [b % 37 for b in range(n)]
+    m.append(rows((n, Hkv, 40, d), 5), rows((n, Hkv, 40, d), 6), own)
+    m.append(rows((n, Hkv, T, d), 7), rows((n, Hkv, T, d), 8), [T] * n)
+    q, scale = rows((n, Hkv * G, T, d), 9), None
+    if moving:                                                     # up to 2^14 from tile to tile, for some rows downwards
+        q, scale = (q.float() * 0.05 + torch.linspace(-3.0, 10.0, n * Hkv * G).view(n, Hkv * G, 1, 1) * u).bfloat16(), 1.0
+    start, t, q = i32([x - T for x in m.len]), m.hidden(), q.cuda()
+    tiles = sum(Hkv * -(-size * T * G // 128) * -(-x // per) for size, x in zip(sizes, lead))
+    assert dealt(kvm, q, t, start, m.groups, m.shared)(m.cache) == (-(-tiles // 148), False)
+    run = lambda: m.cache.attend_shared(q, t, start, m.groups, m.shared, scale=scale, out=torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), status=status)  # noqa: E731
+    status = i32([0])
+    out = run()
+    assert status.item() == 0
+    m.compare(q.cpu(), out, [T] * n, 0, 0, scale)
+    for _ in range(10):
+        assert torch.equal(run(), out)
+    g = 20                                                         # (neither a CTA's first unit nor its last, wherever the shares end)
+    m.cache.v_scale[m.table[m.first[g], lead[g] - 1], 1] = math.nan
+    got, want = run(), torch.zeros((n, Hkv * G), dtype=torch.bool)
+    want[m.first[g]:m.first[g] + sizes[g], G:2 * G] = True
+    assert torch.equal(torch.isnan(got.float()).all(-1).all(-1).cpu(), want) and torch.equal(got[~want], out[~want])
