@@ -394,7 +394,7 @@ typedef enum { KVM_ROPE_HALF = 0, KVM_ROPE_INTERLEAVED = 1 } kvm_rope_layout_t;
 typedef enum { KVM_ROPE_PLAIN = 0, KVM_ROPE_LINEAR = 1, KVM_ROPE_PARTS = 2 } kvm_rope_scaling_t;
 typedef struct {
   int32_t norm, layout, scaling;           /* the kinds above */
-  int32_t rope_dims;                       /* r: even, 0 .. head_dim; 0: no rotation (what follows is not looked at) */
+  int32_t rope_dims;                       /* r: even, 0 .. head_dim; 0: no rotation (base to original_len and frequencies are not looked at) */
   double base, factor, low, high;          /* base >= 1; factor >= 1 (LINEAR, PARTS); 0 <= low < high (PARTS) */
   double magnitude;                        /* of cos and sin, 1e-30 .. 1e30; 1 unless a long context asks for another */
   int64_t original_len;                    /* PARTS: tokens, >= 1 */

@@ -544,7 +544,7 @@ static kvm_status_t check_front(const kvm_front_t* f, int d) {
     if (f->scaling != KVM_ROPE_PLAIN && !within(f->factor, 1.0, 1e30)) return KVM_ERR_INVALID_ARG;
     if (f->scaling == KVM_ROPE_PARTS && (f->original_len < 1 || !within(f->low, 0.0, 1e30) || !within(f->high, 0.0, 1e30) || f->low >= f->high)) return KVM_ERR_INVALID_ARG;
   }
-  if (f->frequencies) {
+  if (f->rope_dims > 0 && f->frequencies) {
     if (!cache::aligned(f->frequencies, 8)) return KVM_ERR_INVALID_ARG;
     for (int i = 0; i < f->rope_dims / 2; ++i)
       if (!within(f->frequencies[i], 0.0, 1.0)) return KVM_ERR_INVALID_ARG;

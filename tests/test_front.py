@@ -577,3 +577,11 @@ def test_front_of_the_largest_offsets(kvm):
     want = kvm.qk_norm_rope(x.contiguous(), None, f, i32([4, 5]))[0]
     kvm.qk_norm_rope(x, None, f, i32([4, 5]), q_out=x)
     assert torch.equal(x, want)
+
+
+def test_without_rotation_frequencies_are_not_looked_at(kvm):
+    for at in (1, 4, 1 << 20):                         # (no address that may be read, nor aligned)
+        f = _front(kvm, rope_dims=0, frequencies=C.cast(C.c_void_p(at), C.POINTER(C.c_double)))
+        assert kvm.lib.kvm_rope_frequencies(C.byref(f), 128, None) == 0
+    f = _front(kvm, rope_dims=2, frequencies=C.cast(C.c_void_p(4), C.POINTER(C.c_double)))
+    assert kvm.lib.kvm_rope_frequencies(C.byref(f), 128, (C.c_double * 1)()) == 1
