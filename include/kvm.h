@@ -463,13 +463,14 @@ typedef struct {
 kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* k, const void* v,
                               const int64_t* k_strides, const int64_t* v_strides, int32_t* status, void* cuda_stream);
 
-/* kvm_qk_norm_rope and kvm_cache_append in one launch: q (with the positions start[b] ..) to q_out, k through the same front end into the cache,
+/* kvm_qk_norm_rope and kvm_cache_append together, in one launch (two beyond 16384 rows of q): q (with the positions start[b] ..) to q_out, k through the same front end into the cache,
  * v into the cache.  The codes of k are those of the normalised and rotated row in fp32, rounded once (not by way of bf16); a row that leaves fp32's
  * range there counts as infinite.  q may be NULL: k and v only.  Rows of q_out behind a sequence's count, and of a sequence that is reported, are
  * left as they were; rows of q, k and v behind the count may be read, but nothing comes of them.  q_out may be q (same strides), and must not overlap
  * k or v.  What kvm_cache_append says of pages, scales, distinct pages and infinities holds here; n_q_heads <= 16384, batch * n_tokens <= 2^31 - 256 with q,
  * else UNSUPPORTED.
- * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error.  No allocation, no synchronisation. */
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA; nothing is launched on an error, but that a CUDA error of the second launch finds the first one made: k and v are
+ * in the cache then, q_out is as it was, and the same call may be made again.  No allocation, no synchronisation. */
 kvm_status_t kvm_cache_ingest(const kvm_cache_t* cache, const kvm_cache_call_t* call, const kvm_front_t* front, const void* q, int32_t n_q_heads,
                               const void* k, const void* v, void* q_out, const int64_t* q_strides, const int64_t* k_strides,
                               const int64_t* v_strides, const int64_t* q_out_strides, int32_t* status, void* cuda_stream);
@@ -516,7 +517,8 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
  * Otherwise as kvm_cache_attend, the precision of q included; weights over shared blocks go into the products in fp16, as there beyond 16 pairs, those over a
  * sequence's own blocks as they do there.  Codes of NaN under a finite scale, which append never writes,
  * count as 480 among the values of shared blocks.  workspace: kvm_cache_shared_workspace() bytes.
- * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA; nothing is launched on an error. */
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA; nothing is launched on an error, but that a CUDA error of a later launch finds the first ones made, which
+ * write to the workspace alone. */
 kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm_cache_call_t* call, const int32_t* groups, const int32_t* shared, int32_t n_groups,
                                      const void* q, int32_t n_q_heads, float scale, void* out, const int64_t* q_strides, const int64_t* out_strides,
                                      void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);

@@ -660,7 +660,7 @@ static kvm_status_t launch_pages(const IngestArgs& a, int64_t q_rows, cudaStream
   constexpr int SMEM = MODE == kSingle ? 0 : Stage<D, TH, kRows, kPagesAhead>::kBytes;
   if (!room_for<ingest_pages_kernel<D, TH, MODE>, SMEM>()) return KVM_ERR_CUDA;
   ingest_pages_kernel<D, TH, MODE><<<(unsigned)(2 * a.k_blocks + (q_rows * (D / 8) + TH - 1) / TH), TH, SMEM, s>>>(a);
-  return KVM_OK;
+  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
 }
 template <int D, int MODE>
 static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
@@ -681,13 +681,13 @@ static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
   a.k_blocks = groups * p.batch * a.chunks;
   Tiles ts;
   int blocks = 0;
-  if (2 * a.k_blocks > INT32_MAX || (a.q.H > 0 && !tiles_of_call<D>(p.batch, p.T, a.q.H, ts, blocks))) return KVM_ERR_UNSUPPORTED;
+  if (2 * a.k_blocks > INT32_MAX - kFewRows || (a.q.H > 0 && !tiles_of_call<D>(p.batch, p.T, a.q.H, ts, blocks))) return KVM_ERR_UNSUPPORTED;
   const int64_t q_rows = (int64_t)p.batch * p.T * a.q.H;
   const bool few = q_rows <= kFewRows;   // (they go with the pages: one launch)
+  if (!few && !room_for<ingest_q_kernel<D, MODE>, kTilesSmem<D, MODE>>()) return KVM_ERR_CUDA;   // (before anything is written)
   const kvm_status_t rc = TH == 256 ? launch_pages<D, 256, MODE>(a, few ? q_rows : 0, s) : launch_pages<D, 512, MODE>(a, few ? q_rows : 0, s);
   if (rc != KVM_OK) return rc;
   if (!few) {
-    if (!room_for<ingest_q_kernel<D, MODE>, kTilesSmem<D, MODE>>()) return KVM_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (as the last blocks of the pages leave room)
@@ -696,7 +696,7 @@ static kvm_status_t launch_ingest(IngestArgs& a, cudaStream_t s) {
     lc.gridDim = dim3(blocks); lc.blockDim = dim3(256); lc.dynamicSmemBytes = kTilesSmem<D, MODE>;
     if (cudaLaunchKernelEx(&lc, ingest_q_kernel<D, MODE>, a, ts) != cudaSuccess) { cudaGetLastError(); return KVM_ERR_CUDA; }
   }
-  return cudaGetLastError() == cudaSuccess ? KVM_OK : KVM_ERR_CUDA;
+  return KVM_OK;
 }
 
 template <int D>
