@@ -585,3 +585,130 @@ def test_without_rotation_frequencies_are_not_looked_at(kvm):
         assert kvm.lib.kvm_rope_frequencies(C.byref(f), 128, None) == 0
     f = _front(kvm, rope_dims=2, frequencies=C.cast(C.c_void_p(4), C.POINTER(C.c_double)))
     assert kvm.lib.kvm_rope_frequencies(C.byref(f), 128, (C.c_double * 1)()) == 1
+
+
+# ---- every build over many rows --------------------------------------------------------------------------------------
+
+SIDE, HALVES, MIXED = dict(rope_dims=40, layout="interleaved"), dict(rope_dims=48), dict(rope_dims=60)   # (pairs side by side; two runs; 30 pairs, no whole runs of four)
+
+
+def placed(x, by):
+    """x [..., d] in memory that begins `by` elements behind a border of 16 bytes, its rows 1 element apart if by is odd."""
+    if not by:
+        return x.cuda().contiguous()
+    wide = torch.empty(x.numel() // x.shape[-1] * (x.shape[-1] + by % 2) + by + 16, dtype=x.dtype, device="cuda")
+    y = wide[by:by + x.numel() // x.shape[-1] * (x.shape[-1] + by % 2)].view(*x.shape[:-1], x.shape[-1] + by % 2)[..., :x.shape[-1]]
+    y.copy_(x)
+    return y
+
+
+def front_of(kvm, Hq, Hk, d, kw, by=0):
+    """A front end with weights 8 `by` bytes behind a border of 16; it, and they on the host."""
+    qp, kp = params(Hq, d, kw["norm"], 3), params(Hk, d, kw["norm"], 4)
+    dev = lambda t: None if t is None else placed(t.reshape(-1), 2 * by).view(t.shape)  # noqa: E731
+    return kvm.Front(q_weight=dev(qp[0]), q_bias=dev(qp[1]), k_weight=dev(kp[0]), k_bias=dev(kp[1]), **kw), qp, kp
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kw,rows_by,weights_by", [(SIDE, 0, 0), (HALVES, 0, 0), (MIXED, 0, 0), (SIDE, 1, 0), (HALVES, 4, 0), (MIXED, 1, 0), (HALVES, 0, 1), (SIDE, 0, 1)])
+def test_norm_rope_of_many_rows_in_every_layout_and_alignment(kvm, d, kw, rows_by, weights_by):
+    B, Hq, Hk, T, start, counts = 2, 11, 6, 500, [7, 90000], [500, 333]
+    assert B * T * (Hq + Hk) > 16384
+    kw = dict(kw, norm="rms" if kw is MIXED else "layer")
+    q, k = rows((B, Hq, T, d), 1), rows((B, Hk, T, d), 2)
+    f, qp, kp = front_of(kvm, Hq, Hk, d, kw, weights_by)
+    qd, kd, status = placed(q, rows_by), placed(k, rows_by), i32([0])
+    assert (qd.data_ptr() % 16 == 0) == (rows_by == 0) and (f._desc.q_weight % 16 == 0) == (weights_by == 0)
+    qo, ko = torch.full((B, Hq, T, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((B, Hk, T, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    kvm.qk_norm_rope(qd, kd, f, i32(start), i32(counts), q_out=qo, k_out=ko, status=status)
+    assert status.item() == 0
+    check_rows(qo, *reference(q, start, counts, *qp, kw), counts)
+    check_rows(ko, *reference(k, start, counts, *kp, kw), counts)
+    kvm.qk_norm_rope(qd, kd, f, i32(start), i32(counts), q_out=qd, k_out=kd)           # in place
+    for b, n in enumerate(counts):
+        for got, out, x in ((qd, qo, q), (kd, ko, k)):
+            assert torch.equal(got[b, :, :n], out[b, :, :n]) and torch.equal(got[b, :, n:].cpu(), x[b, :, n:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,P", [(64, 16), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("kw,rows_by,weights_by", [(SIDE, 0, 0), (HALVES, 0, 0), (MIXED, 0, 0), (HALVES, 1, 0), (MIXED, 4, 0), (SIDE, 0, 1)])
+@pytest.mark.parametrize("Hq", [2, 15])
+def test_ingest_of_many_rows_in_every_layout_and_alignment(kvm, d, P, kw, rows_by, weights_by, Hq):
+    """Rows of q in the launch of the pages and in one of their own, q_out apart and in place, and the same call once more."""
+    B, Hkv, T, counts = 2, 3, 600, [600, 411]
+    assert (B * T * Hq > 16384) == (Hq == 15)
+    kw = dict(kw, norm="rms" if kw is MIXED else "layer")
+    f, qp, kp = front_of(kvm, Hq, Hkv, d, kw, weights_by)
+    blocks = (T + 30) // P + 2
+    table = torch.randperm(B * blocks + 3, generator=torch.Generator().manual_seed(1))[:B * blocks].to(torch.int32).view(B, blocks).cuda()
+    cache, twin, start = garbage_cache(kvm, B * blocks + 3, Hkv, d, P), garbage_cache(kvm, B * blocks + 3, Hkv, d, P), [0, 0]
+    bits = lambda c: [c.k8.view(torch.uint8).clone(), c.v8.view(torch.uint8).clone(), c.k_scale.view(torch.int32).clone(), c.v_scale.view(torch.int32).clone()]  # noqa: E731
+    for step, n in enumerate(([5, 30], counts)):                  # (the second call begins in the middle of a block)
+        q, k, v = (rows((B, H, T, d), 10 * step + i) for i, H in enumerate((Hq, Hkv, Hkv)))
+        qd, kd, vd = (placed(x, rows_by) for x in (q, k, v))
+        out, status = torch.full((B, Hq, T, d), 7.0, dtype=torch.bfloat16, device="cuda"), i32([0])
+        cache.ingest(qd, kd, vd, f, table, i32(start), i32(n), q_out=out, status=status)
+        twin.append(kd, vd, table, i32(start), i32(n))
+        assert status.item() == 0
+        check_rows(out, *reference(q, start, n, *qp, kw), n)
+        check_keys(cache, table, start, n, *reference(k, start, n, *kp, kw))
+        want = bits(cache)
+        assert torch.equal(want[1], twin.v8.view(torch.uint8)) and torch.equal(want[3], twin.v_scale.view(torch.int32))
+        cache.ingest(qd, kd, vd, f, table, i32(start), i32(n), q_out=qd)
+        assert all(torch.equal(x, y) for x, y in zip(bits(cache), want))
+        for b in range(B):
+            assert torch.equal(qd[b, :, :n[b]], out[b, :, :n[b]]) and torch.equal(qd[b, :, n[b]:].cpu(), q[b, :, n[b]:])
+        start = [a + b for a, b in zip(start, n)]
+
+
+def far(x, at=0):
+    """x [2, ...] with its second sequence 2^31 elements behind the first."""
+    big = torch.empty((1 << 31) + x[0].numel() + at, dtype=torch.bfloat16, device="cuda")
+    y = torch.as_strided(big, x.shape, (1 << 31, *x[0].stride()), at)
+    y.copy_(x)
+    return y
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("at,kw", [(0, dict(rope_dims=32)), (0, dict(rope_dims=20)), (1, dict(rope_dims=32, layout="interleaved"))])
+def test_many_rows_of_the_largest_offsets(kvm, at, kw):
+    """Rows in front of and behind offsets of 32 bits in the kernel over many rows: 18000 of them."""
+    x = rows((2, 9, 1000, 64), 1)
+    f, start = kvm.Front(norm="layer", **kw), i32([4, 70000])
+    want = kvm.qk_norm_rope(x.cuda(), None, f, start)[0]
+    y = far(x, at)
+    assert torch.equal(kvm.qk_norm_rope(y, None, f, start, q_out=torch.empty_like(want))[0], want)
+    kvm.qk_norm_rope(y, None, f, start, q_out=y)
+    assert torch.equal(y, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,Hq", [(1, 4), (300, 4), (300, 40)])
+def test_ingest_and_read_of_the_largest_offsets(kvm, T, Hq):
+    """A pool of more than 2^31 bytes per tensor and rows 2^31 elements apart, against pages at its front and contiguous rows."""
+    H, d, P = 16, 128, 128
+    N = (1 << 31) // (H * d * P) + 40
+    c, f = kvm.Cache.empty(N, H, d, P), kvm.Front(norm="rms", rope_dims=128)
+    q, k, v = rows((2, Hq, T, d), 1), rows((2, H, T, d), 2), rows((2, H, T, d), 3)
+    low, start = i32([[0, 1, 2, 3], [4, 5, 6, 7]]), i32([100, 64])
+    high = N - 1 - low
+    first = rows((2, H, 100, d), 4).cuda()
+    for t in (low, high):
+        c.append(first, first, t, i32([0, 0]), start)
+    want = c.ingest(q.cuda(), k.cuda(), v.cuda(), f, low, start)
+    qf = far(q)
+    assert c.ingest(qf, far(k), far(v), f, high, start, q_out=qf) is qf
+    assert torch.equal(qf, want)
+    del qf
+    for codes in (c.k8, c.v8):
+        x = codes.view(torch.uint8)
+        assert torch.equal(x[:8], x[N - 8:].flip(0))
+    for s in (c.k_scale, c.v_scale):
+        assert torch.equal(s[:8], s[N - 8:].flip(0))
+    n = i32([100 + T, 64 + T])
+    a = c.read(low, i32([0, 0]), 100 + T, n, *(torch.zeros((2, H, 100 + T, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    b = [far(torch.zeros((2, H, 100 + T, d), dtype=torch.bfloat16)) for _ in range(2)]
+    c.read(high, i32([0, 0]), 100 + T, n, *b)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[0].float().abs().max() > 0.1
