@@ -463,8 +463,8 @@ typedef struct {
 kvm_status_t kvm_cache_append(const kvm_cache_t* cache, const kvm_cache_call_t* call, const void* k, const void* v,
                               const int64_t* k_strides, const int64_t* v_strides, int32_t* status, void* cuda_stream);
 
-/* kvm_qk_norm_rope and kvm_cache_append together, in one launch (two beyond 16384 rows of q): q (with the positions start[b] ..) to q_out, k through the same front end into the cache,
- * v into the cache.  The codes of k are those of the normalised and rotated row in fp32, rounded once (not by way of bf16); a row that leaves fp32's
+/* kvm_qk_norm_rope and kvm_cache_append together, in one launch (two beyond 16384 rows of q): q (with the positions start[b] ..) to q_out,
+ * k through the same front end into the cache, v into the cache.  The codes of k are those of the normalised and rotated row in fp32, rounded once (not by way of bf16); a row that leaves fp32's
  * range there counts as infinite.  q may be NULL: k and v only.  Rows of q_out behind a sequence's count, and of a sequence that is reported, are
  * left as they were; rows of q, k and v behind the count may be read, but nothing comes of them.  q_out may be q (same strides), and must not overlap
  * k or v.  What kvm_cache_append says of pages, scales, distinct pages and infinities holds here; n_q_heads <= 16384, batch * n_tokens <= 2^31 - 256 with q,
@@ -516,7 +516,14 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
  * q behind a sequence's count may be read, but nothing comes of them.
  * Otherwise as kvm_cache_attend, the precision of q included; weights over shared blocks go into the products in fp16, as there beyond 16 pairs, those over a
  * sequence's own blocks as they do there.  Codes of NaN under a finite scale, which append never writes,
- * count as 480 among the values of shared blocks.  workspace: kvm_cache_shared_workspace() bytes.
+ * count as 480 among the values of shared blocks.
+ * When to call it: it saves what kvm_cache_attend takes to read blocks again, and costs a launch more, 8 to 9 us on a B200.  The two take the same, one token per sequence and 8 kv heads
+ * of 128, for 8 samples of 4096 shared tokens, 16 of 2048, 32 of 1024, 64 of 512 (64 MB of codes that kvm_cache_attend reads, sequences * shared tokens * 2 * head_dim * n_kv_heads
+ * bytes), and for 4 of 16384 (128 MB); with more this call is the faster one, with less, and for two samples of up to 32768 tokens, the other.  So it is for prompts: a sequence of more
+ * than 64 rows (tokens times heads of a group) meets a block that many rows at a time in either (8 sequences behind 8192, 4 heads to a group: 16 tokens 47 us here and 51 there, 64
+ * tokens 118 and 82, 300 tokens 497 and 396).
+ * workspace: kvm_cache_shared_workspace() bytes: partial results of every row in fp32, (head_dim + 2) * 4 bytes of each over the shared blocks and as much, or a few times as much where
+ * the keys are split, over its own (64 sequences of 512 tokens and 32 heads of 128: 1 GB).
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA; nothing is launched on an error, but that a CUDA error of a later launch finds the first ones made, which
  * write to the workspace alone. */
 kvm_status_t kvm_cache_attend_shared(const kvm_cache_t* cache, const kvm_cache_call_t* call, const int32_t* groups, const int32_t* shared, int32_t n_groups,

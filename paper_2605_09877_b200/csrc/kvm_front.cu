@@ -8,8 +8,9 @@
 //   - angles are fixed-point fractions of a turn: position times frequency modulo one turn is one 64-bit product, whatever the position, and the sine and cosine of
 //     the eighth of a turn that is left a short polynomial.  (With angles in fp64 and the library's sincosf the pages of 4 x 8192 tokens took 74 us, now 63.)
 //     They are computed once per token and kept over the heads;
-//   - rows come by way of shared memory (cp.async), three items ahead: the registers are the rows' in work.  (2 x 8192 tokens, 32 heads of 128, RMS norm: 79 us with
-//     loads into registers and 16 warps per SM, 63 by way of shared memory, 55.5 with equal runs of items per block; a plain copy of the same 268 MB takes 44.)
+//   - rows come by way of shared memory (cp.async), three items ahead: the registers are the rows' in work.  (2 x 8192 tokens, 32 heads of 128, LayerNorm: 79 us with
+//     loads into registers and 16 warps per SM, 63 by way of shared memory, 57 with equal runs of items per block, 55.5 with the angles as above; a plain copy of the same
+//     268 MB takes 44.)
 // Few rows are bound by latency: one row per group of lanes, no loop (one token far into a sequence: 2.6 us).
 #include <algorithm>
 #include <atomic>
@@ -25,7 +26,10 @@ using cache::AppendOut;
 
 constexpr int kTokens = 4;    // tokens of a lane in the kernel over many rows
 constexpr int kRows = 4;      // rows of a lane in the kernel over pages
-constexpr int kFewRows = 16384;   // up to so many rows of q (and k) each is done by itself
+// Up to so many rows of q (and k) each is done by itself.  us, one row at a time and over tiles: LayerNorm, 128 channels, 8192 rows 3.7 and 4.9, 16384 6.1 and 6.2, 24576 8.1 and
+// 7.6, 32768 10.4 and 7.7; RMS, interleaved, 16384 7.7 and 8.4, 24576 10.2 and 9.7; 64 channels meet at 32768, 6.4 and 6.5.  Ingest, where few rows go with the pages and others have
+// a launch of their own: 16384 9.4 and 10.4 (64 channels 6.4 and 7.0), 32768 16.7 and 12.4 (9.6 and 10.7).
+constexpr int kFewRows = 16384;
 constexpr int kPagesAhead = 3;
 constexpr int kAhead = 3;     // stages of rows on their way (one of them is in use)
 

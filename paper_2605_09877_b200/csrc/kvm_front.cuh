@@ -10,8 +10,9 @@
 // Aligned rows come by way of shared memory, 16 bytes per lane (Stage): what a kernel has on its way costs no registers, several heads ahead, and a lane
 // takes its channels from there.
 //
-// Angles: f_i as a fraction of a turn in units of 2^-64, so that the product with a position, which drops whole turns, is off by 2^-34 of a turn at position 2^31
-// at most; the quadrant is its top two bits (rounded), what is left is within 1/8 turn, and sin and cos of that are their Taylor polynomials (the terms left out are
+// Angles: f_i, an fp64 number (off by 2^-52 of itself, which is less than 2^-54 of a turn per position), as a fraction of a turn cut to units of 2^-64.  The product with a
+// position drops whole turns and no bits of the rest: it is off by less than 2^-53 of a turn times the position, 2^-22 at 2^31.  The quadrant is its top two bits (rounded), what is
+// left, of which 30 bits are taken (2^-32 of a turn, and fp32's 2^-28), is within 1/8 turn, and sin and cos of that are their Taylor polynomials (the terms left out are
 // below 2e-9).
 #pragma once
 #include <cuda_bf16.h>
