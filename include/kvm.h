@@ -510,7 +510,7 @@ kvm_status_t kvm_cache_attend(const kvm_cache_t* cache, const kvm_cache_call_t* 
  * prompt.  Group g is sequences groups[g] .. groups[g + 1] - 1, and the first shared[g] blocks of their tables hold the same tokens (forks: the same
  * pages; kvm_pages_shared counts them).  Those blocks are read for the group together, from the table of its first sequence, once per 128 rows of queries (tokens times heads of a kv head's group); entries of the other tables there
  * may be anything.  Every token sees what it sees in kvm_cache_attend; the results differ by rounding.
- *   groups   device int32 [n_groups + 1]: ascends (groups of no sequences are allowed) from 0 to batch
+ *   groups   device int32 [n_groups + 1], 1 <= n_groups <= batch: ascends (groups of no sequences are allowed) from 0 to batch
  *   shared   device int32 [n_groups], 0 <= shared[g] <= max_pages, and shared[g] * page_tokens <= start[b] for the sequences of g
  * Groups that are none, or a number of blocks that is not allowed, are reported like lengths that are not, and their sequences get no rows. Rows of
  * q behind a sequence's count may be read, but nothing comes of them.
