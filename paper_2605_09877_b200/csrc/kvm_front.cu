@@ -575,8 +575,8 @@ static FrontDev device_front(const kvm_front_t* f) {
   FrontDev x = {};
   x.norm = f->norm;
   x.eps = f->norm == KVM_NORM_NONE ? 0.f : f->eps;
-  x.half = f->layout == KVM_ROPE_HALF;
   x.h = f->rope_dims / 2;
+  x.half = f->layout == KVM_ROPE_HALF && x.h > 0;   // (without rotation kSide and kSingle have the same pairs, and sums the same order)
   x.mag = x.h ? (float)f->magnitude : 1.f;
   constexpr long double kTurns = 18446744073709551616.0L / 6.283185307179586476925286766559L;   // 2^64 / (2 pi)
   for (int i = 0; i < x.h; ++i) x.turns[i] = (uint64_t)(frequency(f, i) * kTurns);   // (f_i <= 1: below 2^62)

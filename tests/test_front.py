@@ -712,3 +712,22 @@ def test_ingest_and_read_of_the_largest_offsets(kvm, T, Hq):
     b = [far(torch.zeros((2, H, 100 + T, d), dtype=torch.bfloat16)) for _ in range(2)]
     c.read(high, i32([0, 0]), 100 + T, n, *b)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[0].float().abs().max() > 0.1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+@pytest.mark.parametrize("layout,r", [("half", 0), ("interleaved", 0), ("half", 16), ("half", 44), ("interleaved", 22)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_results_do_not_depend_on_alignment(kvm, norm, layout, r, d):
+    """The same bits from rows and weights on 16-byte borders and off them, few rows and many, alone and in ingest."""
+    f, odd = (front_of(kvm, 9, 3, d, dict(norm=norm, layout=layout, rope_dims=r), by)[0] for by in (0, 1))
+    for T in (1, 100, 2000):
+        x, start = rows((1, 9, T, d), T), i32([77])
+        want = kvm.qk_norm_rope(x.cuda(), None, f, start)[0]
+        for g, by in ((f, 1), (f, 4), (odd, 0)):
+            assert torch.equal(kvm.qk_norm_rope(placed(x, by), None, g, start)[0], want)
+        c, twin = (garbage_cache(kvm, T // 16 + 8, 3, d, 16) for _ in range(2))
+        table = torch.arange(T // 16 + 8, dtype=torch.int32, device="cuda")[None]
+        assert torch.equal(c.ingest(x.cuda(), x[:, :3].cuda(), x[:, 3:6].cuda(), f, table, start), want)
+        assert torch.equal(twin.ingest(placed(x, 1), placed(x[:, :3], 1), placed(x[:, 3:6], 1), f, table, start), want)
+        assert torch.equal(c.k8.view(torch.uint8), twin.k8.view(torch.uint8)) and torch.equal(c.v8.view(torch.uint8), twin.v8.view(torch.uint8))
